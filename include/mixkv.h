@@ -39,7 +39,7 @@
 extern "C" {
 #endif
 
-#define MIXKV_VERSION 10
+#define MIXKV_VERSION 11
 #define MIXKV_MAX_LAYERS 128      /* layers per call */
 #define MIXKV_MAX_WINDOW 64
 #define MIXKV_MAX_GROUP_ROWS 512  /* G * W */
@@ -308,6 +308,107 @@ typedef struct {
 } mixkv_append_layer;
 mixkv_status mixkv_append(const mixkv_params *params, const mixkv_append_layer *layers, int32_t n_layers,
                           int32_t position, int32_t tail_capacity, void *hip_stream);
+
+/*
+ * The paged cache: a compacted (or full) cache that decoding continues on, held in pages.
+ *
+ * A page holds page_rows rows of one KV head, keys and values apart.  page_table[b][h][i] is the page with the rows
+ * [i * page_rows, (i + 1) * page_rows) of KV head h of sequence b; heads of one sequence may have different lengths, as
+ * head-adaptive budgets give them (Sec. 3.1, Sec. 4.1), and a sequence of length 0 is padding.  An entry outside
+ * [0, n_pages) is no page: rows that would go there are dropped, rows that would come from there do not exist.
+ *
+ * MIXKV_PAGE_ROWS: a page is page_rows rows of head_dim elements in the dtype of the params.
+ * MIXKV_PAGE_4BIT (bf16 only): 32 neighbouring elements of a row share a step S and a base B, both fp16, and an element is
+ * stored as a code of 4 bits that stands for B + S (1 + code / 16): 5 bits an element in all.  With lo and hi the smallest and
+ * largest of the 32 elements x, each first brought into [-16384, 16384],
+ *     S = fp16((hi - lo) 16 / 15),  B = fp16(lo - S),  code = min(max(round(16 (x - B - S) / S), 0), 15)  (0 where S = 0),
+ * the differences in 64 bits, each fp16 rounded to nearest even through fp32, the code to nearest even.  An element is off by at
+ * most S / 32, where fp16 resolves B and S.  D = head_dim, P = page_rows, code e of a word in its bits [4 n, 4 n + 4),
+ * n = e / 2 + 4 (e % 2); a page of keys or values has P D 5 / 8 bytes, the codes first:
+ *   keys    word r D/8 + s D/32 + g' of the page: the codes of the elements 32 g + 8 s + e of row r; then (S, B) of (r, g) at fp16
+ *           2 (r D/32 + g').  g' is 0, 2, 1, 3 for g = 0 ... 3 if D = 128, g if D = 64.
+ *   values  strip q of the 32 rows from row 32 t: the rows 32 t + 4 q + i and 32 t + 16 + 4 q + i, i = 0 ... 3, as e = 2 i and 2 i + 1.
+ *           Word (4 t + q) D + 64 j + 4 m + w: the codes of the element 64 j + 16 w + m of the strip's rows; then S of the strip's
+ *           row e and group g at fp16 ((4 t + q) D/32 + g) 16 + e, B eight further.
+ * A program that builds pages itself may write them in this form.  Pages need no initialisation; rows of a page that have not
+ * been written are never used.  Pages written by one call must be written for one (sequence, head) only.
+ *
+ * lengths[b][h] counts the rows of a head, those that a call appends among them: a program adds the new rows to the
+ * lengths first.  Lengths are clamped to [0, max_pages * page_rows].
+ */
+typedef enum { MIXKV_PAGE_ROWS = 0, MIXKV_PAGE_4BIT = 1 } mixkv_page_format;
+
+typedef struct {
+  mixkv_dtype dtype;         /* element type of rows, queries, outputs and key bounds */
+  mixkv_page_format format;  /* of the pages; 4BIT needs MIXKV_BF16 */
+  int32_t batch;
+  int32_t n_q_heads;         /* multiple of n_kv_heads */
+  int32_t n_kv_heads;
+  int32_t head_dim;          /* 64 or 128 */
+  int32_t page_rows;         /* 32, 64 or 128 */
+  int32_t max_pages;         /* entries of a head in the page table; max_pages * page_rows <= 2^30 */
+  int32_t n_pages;           /* pages in a layer's K_pages and V_pages */
+  float softmax_scale;       /* finite, > 0 */
+} mixkv_paged_params;
+
+/* One layer's pages.  DEVICE pointers owned by the caller, K_pages, V_pages and K_bounds 16-byte aligned. */
+typedef struct {
+  void *K_pages, *V_pages;   /* n_pages pages each, back to back */
+  void *K_bounds;            /* [n_pages, 2, D], dtype of the params: per element the smallest and the largest key that was written to
+                                the page since its first row was; NULL where no call needs it */
+  const int32_t *page_table; /* [batch, n_kv_heads, max_pages] */
+  const int32_t *lengths;    /* [batch, n_kv_heads] */
+} mixkv_paged_cache;
+
+/* Bytes of a page of keys (or values).  Host only. */
+mixkv_status mixkv_page_bytes(const mixkv_paged_params *params, size_t *bytes);
+
+/* Dense rows of one layer that go into pages or come out of them.  Row r of KV head h starts at element r * stride_n + h * stride_h of K
+ * (and of V); stride_n >= D, stride_h >= 0 (0: the heads' rows lie among one another, as in packed caches), row starts 16-byte
+ * aligned.  The rows of (b, h) are [row_start[b][h], row_start[b][h] + row_count[b][h]); those outside [0, n_rows) are left out. */
+typedef struct {
+  void *K, *V;               /* read by mixkv_paged_append, written by mixkv_paged_read */
+  int64_t stride_n, stride_h;
+  const int32_t *row_start, *row_count;  /* DEVICE [batch, n_kv_heads] */
+  const void *Q;             /* append only, may be NULL: queries of the same rows, head g of row r at r * q_stride_n + g * q_stride_h;
+                                for a KV head's rows the G query heads that it serves; for every layer of a call or none */
+  int64_t q_stride_n, q_stride_h;
+  void *Q_out;               /* [n_rows, n_q_heads, D] contiguous: the rotated queries; required with Q, may not overlap K, V or Q */
+} mixkv_paged_rows;
+
+/* Rotation of keys and queries to their positions: with the elements i and i + D/2 of a row as a pair (a, b), c and s the cosine and
+ * sine of its angle, (a c - b s, b c + a s), in 64 bits, rounded once to the dtype.  The angle of pair i is that of
+ * positions[axis][r] for the row's index r: axis 0 everywhere (n_axes 1), or (n_axes 3) axis 0 for the first sections[0] pairs, 1 for
+ * the next sections[1], 2 for the last sections[2] (time, height and width of vision-language models).  Positions are
+ * clamped to the tables.  Shared by the layers of a call. */
+typedef struct {
+  const float *cos, *sin;    /* DEVICE [n_positions, D / 2] */
+  int32_t n_positions;
+  const int32_t *positions;  /* DEVICE [n_axes, n_rows] */
+  int32_t n_axes;            /* 1 or 3 */
+  int32_t sections[3];       /* n_axes 3: each >= 0, sum D / 2; else ignored */
+} mixkv_rope;
+
+/*
+ * Appends rows to the paged caches of `n_layers` layers (Sec. 3.1: decoding continues on the compressed cache): row t of
+ * the row_count[b][h] rows of (b, h) becomes row lengths[b][h] - row_count[b][h] + t of the head.  Keys and queries are
+ * rotated (rope, or NULL: not; keys that mixkv_compress kept are rotated already), values are stored as they are; pages
+ * hold them in params->format.  K_bounds, where given, take in the new keys as stored rows of the dtype; a page whose first row is
+ * written forgets what it bounded.  One call serves a decoding step (a row per sequence), prompts (ragged rows, one after
+ * another, with unused rows behind them) and a cache that mixkv_compress has written (row_start from its offsets, stride_h 0).  Rows of
+ * pages, queries and bounds that no row goes to keep their contents; a repeated call stores the same again.
+ * max_count: the largest row_count, as far as the host knows it (>= 1): it sizes the launch; larger counts are served, slower.
+ */
+mixkv_status mixkv_paged_append(const mixkv_paged_params *params, const mixkv_paged_cache *caches, const mixkv_paged_rows *rows,
+                                int32_t n_layers, const mixkv_rope *rope, int32_t n_rows, int32_t max_count, void *hip_stream);
+
+/*
+ * The way back: the newest row_count[b][h] rows of every head (all of them with row_count = lengths) into dense rows of the
+ * dtype (4-bit elements rounded to it), for a cache that is to be compressed again with mixkv_compress, moved, or looked
+ * at.  Dense rows that nothing comes to keep their contents.  Q, Q_out and K_bounds are not used.
+ */
+mixkv_status mixkv_paged_read(const mixkv_paged_params *params, const mixkv_paged_cache *caches, const mixkv_paged_rows *rows,
+                              int32_t n_layers, int32_t n_rows, int32_t max_count, void *hip_stream);
 
 const char *mixkv_status_string(mixkv_status status);
 int32_t mixkv_version(void);

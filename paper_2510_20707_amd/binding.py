@@ -27,6 +27,7 @@ BUDGET_MODE = {"fixed": 0, "adaptive": 1, "per_head": 2}
 INTRINSIC = {"none": 0, "vnorm": 1, "knorm": 2}
 MIX = {"head_adaptive": 0, "sum": 1, "div_only": 2, "imp_only": 3, "given_r": 4}
 TORCH_DTYPE = {0: torch.float32, 1: torch.bfloat16}
+PAGE_FORMAT = {"rows": 0, "4bit": 1}
 N_STAGES = 5
 
 
@@ -66,6 +67,27 @@ class MixkvDecodeLayer(C.Structure):
 
 class MixkvAppendLayer(C.Structure):
     _fields_ = [("K_new", C.c_void_p), ("V_new", C.c_void_p), ("K_tail", C.c_void_p), ("V_tail", C.c_void_p)]
+
+
+class MixkvPagedParams(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("format", C.c_int), ("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("page_rows", C.c_int32), ("max_pages", C.c_int32), ("n_pages", C.c_int32),
+                ("softmax_scale", C.c_float)]
+
+
+class MixkvPagedCache(C.Structure):
+    _fields_ = [("K_pages", C.c_void_p), ("V_pages", C.c_void_p), ("K_bounds", C.c_void_p), ("page_table", C.c_void_p),
+                ("lengths", C.c_void_p)]
+
+
+class MixkvPagedRows(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("stride_n", C.c_int64), ("stride_h", C.c_int64), ("row_start", C.c_void_p),
+                ("row_count", C.c_void_p), ("Q", C.c_void_p), ("q_stride_n", C.c_int64), ("q_stride_h", C.c_int64), ("Q_out", C.c_void_p)]
+
+
+class MixkvRope(C.Structure):
+    _fields_ = [("cos", C.c_void_p), ("sin", C.c_void_p), ("n_positions", C.c_int32), ("positions", C.c_void_p), ("n_axes", C.c_int32),
+                ("sections", C.c_int32 * 3)]
 
 
 class MixkvError(RuntimeError):
@@ -110,6 +132,13 @@ def lib() -> C.CDLL:
         L.mixkv_append.restype = C.c_int
         L.mixkv_decode_workspace_size.argtypes = [pp, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
         L.mixkv_decode_workspace_size.restype = C.c_int
+        pg, pc, pr = C.POINTER(MixkvPagedParams), C.POINTER(MixkvPagedCache), C.POINTER(MixkvPagedRows)
+        L.mixkv_page_bytes.argtypes = [pg, C.POINTER(C.c_size_t)]
+        L.mixkv_page_bytes.restype = C.c_int
+        L.mixkv_paged_append.argtypes = [pg, pc, pr, C.c_int32, C.POINTER(MixkvRope), C.c_int32, C.c_int32, C.c_void_p]
+        L.mixkv_paged_append.restype = C.c_int
+        L.mixkv_paged_read.argtypes = [pg, pc, pr, C.c_int32, C.c_int32, C.c_int32, C.c_void_p]
+        L.mixkv_paged_read.restype = C.c_int
         L.mixkv_stage_name.argtypes = [C.c_int32]
         L.mixkv_stage_name.restype = C.c_char_p
         L.mixkv_status_string.argtypes = [C.c_int]
@@ -384,3 +413,182 @@ class PreparedCall:
     def score(self, stream=None):
         _check(self._L.mixkv_score(C.byref(self.p), self.ins, self.outs, self.n, self.wp, self.wb, _stream(stream)),
                "mixkv_score")
+
+
+# ---- the paged cache
+
+def make_paged_params(dtype: str, format: str, batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int, page_rows: int, max_pages: int,
+                      n_pages: int, softmax_scale: float = 1.0) -> MixkvPagedParams:
+    return MixkvPagedParams(DTYPE[dtype], PAGE_FORMAT[format], batch, n_q_heads, n_kv_heads, head_dim, page_rows, max_pages, n_pages,
+                            softmax_scale)
+
+
+def mixkv_page_bytes(p: MixkvPagedParams) -> int:
+    n = C.c_size_t(0)
+    _check(lib().mixkv_page_bytes(C.byref(p), C.byref(n)), "mixkv_page_bytes")
+    return n.value
+
+
+@dataclass
+class PagedCache:
+    """Device tensors of one layer's paged cache."""
+    K_pages: Optional[torch.Tensor]              # contiguous, n_pages pages (rows [n_pages, page_rows, D], or bytes in 4 bits)
+    V_pages: Optional[torch.Tensor]
+    page_table: torch.Tensor                     # [batch, Hkv, max_pages] i32
+    lengths: torch.Tensor                        # [batch, Hkv] i32
+    K_bounds: Optional[torch.Tensor] = None      # [n_pages, 2, D]
+
+
+@dataclass
+class PagedRows:
+    """Dense rows of one layer on their way into pages or out of them (strides like K's for V; an expanded head axis for heads packed
+    among one another)."""
+    K: torch.Tensor                              # [n_rows, Hkv, D]
+    V: torch.Tensor
+    row_start: torch.Tensor                      # [batch, Hkv] i32
+    row_count: torch.Tensor
+    Q: Optional[torch.Tensor] = None             # [n_rows, Hq, D]
+    Q_out: Optional[torch.Tensor] = None         # [n_rows, Hq, D] contiguous
+
+
+@dataclass
+class Rope:
+    cos: torch.Tensor                            # [n_positions, D / 2] f32
+    sin: torch.Tensor
+    positions: torch.Tensor                      # [1 or 3, n_rows] i32
+    sections: Optional[Sequence[int]] = None     # three of them with three axes
+
+
+def alloc_paged_cache(p: MixkvPagedParams, device, bounds: bool = False) -> PagedCache:
+    """Empty pages, an empty page table (no pages) and lengths of zero, allocated with torch (plumbing for tests and programs)."""
+    dt, shape = TORCH_DTYPE[p.dtype], (p.n_pages, p.page_rows, p.head_dim)
+    if p.format == PAGE_FORMAT["4bit"]:
+        dt, shape = torch.uint8, (p.n_pages, mixkv_page_bytes(p))
+    pages = [torch.empty(shape, dtype=dt, device=device) for _ in range(2)]
+    return PagedCache(pages[0], pages[1], torch.full((p.batch, p.n_kv_heads, p.max_pages), -1, dtype=torch.int32, device=device),
+                      torch.zeros((p.batch, p.n_kv_heads), dtype=torch.int32, device=device),
+                      torch.empty((p.n_pages, 2, p.head_dim), dtype=TORCH_DTYPE[p.dtype], device=device) if bounds else None)
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _tensor(t: torch.Tensor, name: str, dtype, shape, device, contiguous=True) -> torch.Tensor:
+    """The kernels trust shapes and types: what a pointer does not say is checked here."""
+    _need(t.dtype == dtype and tuple(t.shape) == tuple(shape), f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    _need(not contiguous or t.is_contiguous(), f"{name} has to be contiguous")
+    _need(t.device == device, f"{name} is on {t.device}, expected {device}")
+    return t
+
+
+def _paged_device(t: torch.Tensor) -> torch.device:
+    _need(t.is_cuda and t.device.index == torch.cuda.current_device(), "the tensors have to be on the current device")
+    return t.device
+
+
+def _paged_caches(p: MixkvPagedParams, caches: Sequence[PagedCache], pages: bool, bounds: bool, device):
+    _need(len(caches) > 0, "no layers")
+    units, pool = (p.batch, p.n_kv_heads), 0
+    if pages:
+        pool = p.n_pages * mixkv_page_bytes(p)
+    arr = (MixkvPagedCache * len(caches))()
+    for i, c in enumerate(caches):
+        _tensor(c.page_table, "page_table", torch.int32, units + (p.max_pages,), device)
+        _tensor(c.lengths, "lengths", torch.int32, units, device)
+        if pages:
+            for name, t in (("K_pages", c.K_pages), ("V_pages", c.V_pages)):
+                _need(t is not None and t.is_contiguous() and t.device == device and t.numel() * t.element_size() == pool,
+                      f"{name} has to be {pool} contiguous bytes on {device}")
+        _need(c.K_bounds is not None or not bounds, "K_bounds is needed")
+        if c.K_bounds is not None:
+            _tensor(c.K_bounds, "K_bounds", TORCH_DTYPE[p.dtype], (p.n_pages, 2, p.head_dim), device)
+        arr[i] = MixkvPagedCache(_ptr(c.K_pages), _ptr(c.V_pages), _ptr(c.K_bounds), _ptr(c.page_table), _ptr(c.lengths))
+    return arr
+
+
+def _paged_rows(p: MixkvPagedParams, rows: Sequence[PagedRows], queries: bool, device):
+    arr, n_rows, dt = (MixkvPagedRows * len(rows))(), rows[0].K.shape[0], TORCH_DTYPE[p.dtype]
+    for i, r in enumerate(rows):
+        shape = (n_rows, p.n_kv_heads, p.head_dim)
+        for name, t in (("K", r.K), ("V", r.V)):
+            _tensor(t, name, dt, shape, device, contiguous=False)
+            _need(t.stride(2) == 1 and t.stride() == r.K.stride(), "K and V need the same strides, the last one 1")
+        for name, t in (("row_start", r.row_start), ("row_count", r.row_count)):
+            _tensor(t, name, torch.int32, (p.batch, p.n_kv_heads), device)
+        q, qs = (r.Q, r.Q_out) if queries else (None, None)
+        if q is not None:
+            _tensor(q, "Q", dt, (n_rows, p.n_q_heads, p.head_dim), device, contiguous=False)
+            _need(q.stride(2) == 1 and qs is not None, "Q needs stride 1 along a row, and Q_out")
+            _tensor(qs, "Q_out", dt, (n_rows, p.n_q_heads, p.head_dim), device)
+        st = (0, 0) if q is None else (q.stride(0), q.stride(1))
+        arr[i] = MixkvPagedRows(_ptr(r.K), _ptr(r.V), r.K.stride(0), r.K.stride(1), _ptr(r.row_start), _ptr(r.row_count), _ptr(q), *st, _ptr(qs))
+    return arr, n_rows
+
+
+class PreparedPagedAppend:
+    """The C arguments of one mixkv_paged_append call, built once over buffers that a serving loop keeps.  `max_count`: the largest
+    row_count as far as the host knows it (None: the dense tensor's rows)."""
+
+    def __init__(self, p: MixkvPagedParams, caches: Sequence[PagedCache], rows: Sequence[PagedRows], rope: Optional[Rope] = None,
+                 max_count: Optional[int] = None):
+        device = _paged_device(caches[0].lengths)
+        _need(len(caches) == len(rows), "a rows entry for every cache")
+        self.p, self.n, self.caches = p, len(caches), _paged_caches(p, caches, True, False, device)
+        self.rows, self.n_rows = _paged_rows(p, rows, True, device)
+        self.max_count, self.rope = self.n_rows if max_count is None else max_count, None
+        if rope is not None:
+            half, axes = p.head_dim // 2, rope.positions.shape[0]
+            for name, t in (("cos", rope.cos), ("sin", rope.sin)):
+                _tensor(t, name, torch.float32, (rope.cos.shape[0], half), device)
+            _tensor(rope.positions, "positions", torch.int32, (axes, self.n_rows), device)
+            _need(axes != 3 or rope.sections is not None and len(rope.sections) == 3, "three axes need three sections")
+            self.rope = MixkvRope(_ptr(rope.cos), _ptr(rope.sin), rope.cos.shape[0], _ptr(rope.positions), axes,
+                                  (C.c_int32 * 3)(*(rope.sections if axes == 3 else (0, 0, 0))))
+        self._keep = (caches, rows, rope)
+        self._rope_arg = None if self.rope is None else C.byref(self.rope)
+        self._L = lib()
+
+    def run(self, stream=None):
+        _check(self._L.mixkv_paged_append(C.byref(self.p), self.caches, self.rows, self.n, self._rope_arg, self.n_rows, self.max_count,
+                                          _stream(stream)), "mixkv_paged_append")
+
+
+def mixkv_paged_append(p: MixkvPagedParams, caches: Sequence[PagedCache], rows: Sequence[PagedRows], rope: Optional[Rope] = None,
+                       max_count: Optional[int] = None, stream=None):
+    """Rows into pages, in place (with rows[i].Q: the rotated queries into rows[i].Q_out)."""
+    PreparedPagedAppend(p, caches, rows, rope, max_count).run(stream)
+
+
+class PreparedPagedRead:
+    """The C arguments of one mixkv_paged_read call: rows[i].K and .V receive the newest row_count rows of every head."""
+
+    def __init__(self, p: MixkvPagedParams, caches: Sequence[PagedCache], rows: Sequence[PagedRows], max_count: Optional[int] = None):
+        device = _paged_device(caches[0].lengths)
+        _need(len(caches) == len(rows), "a rows entry for every cache")
+        self.p, self.n, self.caches = p, len(caches), _paged_caches(p, caches, True, False, device)
+        self.rows, self.n_rows = _paged_rows(p, rows, False, device)
+        self.max_count = self.n_rows if max_count is None else max_count
+        self._keep = (caches, rows)
+        self._L = lib()
+
+    def run(self, stream=None):
+        _check(self._L.mixkv_paged_read(C.byref(self.p), self.caches, self.rows, self.n, self.n_rows, self.max_count, _stream(stream)),
+               "mixkv_paged_read")
+
+
+def mixkv_paged_read(p: MixkvPagedParams, caches: Sequence[PagedCache], rows: Sequence[PagedRows], max_count: Optional[int] = None, stream=None):
+    PreparedPagedRead(p, caches, rows, max_count).run(stream)
+
+
+def compacted_rows(p: MixkvParams, out: LayerOut) -> PagedRows:
+    """What mixkv_compress left of one layer, as dense rows for mixkv_paged_append (its counts are the lengths): no copies of rows."""
+    bt, h, d = p.batch, p.n_kv_heads, p.head_dim
+    first = torch.arange(bt, dtype=torch.int32, device=out.counts.device)[:, None] * (h * p.budget)
+    if p.budget_mode == BUDGET_MODE["fixed"]:
+        start = first + torch.arange(h, dtype=torch.int32, device=out.counts.device) * p.budget
+    else:
+        start = first + out.offsets[:, :h]
+    K, V = (t.view(-1, 1, d).expand(-1, h, -1) for t in (out.K_out, out.V_out))
+    return PagedRows(K, V, start.contiguous(), out.counts.contiguous())

@@ -1,0 +1,522 @@
+// The paged cache: rows into pages (mixkv_paged_append), and out of them (mixkv_paged_read).
+//
+// Both kernels give a workgroup the pages of one (layer, sequence, KV head), one page at a time, so that what a page's rows
+// share (the words of a 4-bit value strip, the key bounds) has one writer.  D/16 lanes hold a row: lane j the elements
+// [8 j, 8 j + 8) and [D/2 + 8 j, D/2 + 8 j + 8), the two halves of eight rotated pairs.
+#include "mixkv_paged.h"
+
+namespace mixkv {
+
+constexpr int kPagedLayers = 16;         // pointer-table entries of a launch: the dense rows' strides travel with them
+constexpr int kPagedThreads = 256;
+
+struct PRows {
+  char *K, *V;
+  int64_t sn, sh;                        // strides in bytes
+  const int32_t *start, *count;
+  const char *Q;
+  int64_t qsn, qsh;
+  char *Q_out;
+};
+struct PTable { PCache c[kPagedLayers]; PRows r[kPagedLayers]; };
+
+struct PRope {
+  const float *cos, *sin;                // null: no rotation
+  const int32_t *positions;
+  int32_t n_positions, n_axes, s0, s1;   // pairs below s0 are axis 0's, below s1 axis 1's
+};
+
+// The rows of one unit that a call moves: rows [r0, r1) of the head, row r being dense row r + shift.
+struct RowRange { int r0, r1; int64_t shift; };
+__device__ __forceinline__ RowRange row_range(const PShape &s, const PCache &c, const PRows &d, int u, int n_rows) {
+  const int len = head_rows(s, c, u);
+  const int64_t count = max(d.count[u], 0), first = (int64_t)len - count, src = d.start[u];
+  RowRange x;
+  x.shift = src - first;
+  x.r0 = (int)min((int64_t)len, max((int64_t)0, max(first, -x.shift)));
+  x.r1 = (int)max((int64_t)x.r0, min((int64_t)len, n_rows - x.shift));
+  return x;
+}
+
+// Eight elements of a row.
+template <int DT>
+__device__ __forceinline__ void load_run(const char *p, float *x) {
+  if constexpr (DT == MIXKV_BF16) {
+    const u32x4 v = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(v[i] << 16);
+      x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+    }
+  } else {
+    const f32x4 a = reinterpret_cast<const f32x4 *>(p)[0], b = reinterpret_cast<const f32x4 *>(p)[1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
+  }
+}
+template <int DT>
+__device__ __forceinline__ void store_run(char *p, const float *x) {
+  if constexpr (DT == MIXKV_BF16) {
+    u32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      v[i] = (uint32_t)f32_to_bf16_rne(x[2 * i]) | ((uint32_t)f32_to_bf16_rne(x[2 * i + 1]) << 16);
+    *reinterpret_cast<u32x4 *>(p) = v;
+  } else {
+    reinterpret_cast<f32x4 *>(p)[0] = f32x4{x[0], x[1], x[2], x[3]};
+    reinterpret_cast<f32x4 *>(p)[1] = f32x4{x[4], x[5], x[6], x[7]};
+  }
+}
+// A float as the dtype holds it.
+template <int DT>
+__device__ __forceinline__ float as_stored(float x) {
+  if constexpr (DT == MIXKV_BF16) return __uint_as_float((uint32_t)f32_to_bf16_rne(x) << 16);
+  return x;
+}
+
+// Rotates the lane's eight pairs (a[i], b[i]), elements 8 j + i and D/2 + 8 j + i of dense row `row`.  In 64 bits: the products of
+// a table entry and an element are exact there, so the result is the rounded exact rotation whatever the order, and a row that is then
+// quantised gets the codes of its definition.  The operator is bound by memory; the 64-bit unit is idle otherwise.
+template <int DT, int D>
+__device__ __forceinline__ void rotate(const PRope &rp, int64_t row, int n_rows, int j, float *a, float *b) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {                           // four pairs at a time: 16 bytes of each table
+    const int i0 = 8 * j + 4 * h;
+    f32x4 c, s;
+    if (rp.n_axes == 1 || i0 + 4 <= rp.s0 || (i0 >= rp.s0 && i0 + 4 <= rp.s1) || i0 >= rp.s1) {
+      const int axis = rp.n_axes == 1 || i0 + 4 <= rp.s0 ? 0 : (i0 >= rp.s1 ? 2 : 1);
+      const int pos = min(max(rp.positions[(int64_t)axis * n_rows + row], 0), rp.n_positions - 1);
+      const int64_t at = (int64_t)pos * (D / 2) + i0;
+      c = *reinterpret_cast<const f32x4 *>(rp.cos + at);
+      s = *reinterpret_cast<const f32x4 *>(rp.sin + at);
+    } else {                                              // an axis ends among the four
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int axis = i0 + i < rp.s0 ? 0 : (i0 + i < rp.s1 ? 1 : 2);
+        const int pos = min(max(rp.positions[(int64_t)axis * n_rows + row], 0), rp.n_positions - 1);
+        c[i] = rp.cos[(int64_t)pos * (D / 2) + i0 + i];
+        s[i] = rp.sin[(int64_t)pos * (D / 2) + i0 + i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const double x = a[4 * h + i], y = b[4 * h + i];
+      a[4 * h + i] = as_stored<DT>((float)(x * (double)c[i] - y * (double)s[i]));
+      b[4 * h + i] = as_stored<DT>((float)(y * (double)c[i] + x * (double)s[i]));
+    }
+  }
+}
+
+// ---- 4 bits.  Step and base of a group from its extremes: the differences in 64 bits, rounded to fp32 and then to fp16.
+struct GroupScale { float step, base; uint32_t bits; };    // bits: step, and base above it
+__device__ __forceinline__ GroupScale group_scale(float lo, float hi) {
+  GroupScale g;
+  const uint32_t sb = f16_bits((float)(((double)hi - (double)lo) * (16.0 / 15.0)));
+  g.step = f16_value(sb);
+  const uint32_t bb = f16_bits((float)((double)lo - (double)g.step));
+  g.base = f16_value(bb);
+  g.bits = sb | (bb << 16);
+  return g;
+}
+__device__ __forceinline__ float clip(float x) { return fminf(fmaxf(x, -16384.f), 16384.f); }
+
+// The codes of eight elements in a word.  (x - base - step) 16 / step in 32 bits is within 2^-15 of its value (the differences are at
+// most two steps and lose half a unit in the last place of that each); only where that could decide the rounding is it formed in 64 bits.
+__device__ __forceinline__ uint32_t run_codes(const float *x, const GroupScale &g) {
+#pragma clang fp contract(off)
+  const float r = g.step > 0.f ? 16.f / g.step : 0.f;
+  uint32_t w = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float v = clip(x[e]);
+    const float t = ((v - g.base) - g.step) * r;
+    float n = __builtin_rintf(t);
+    if (fabsf(fabsf(t - n) - 0.5f) < 0x1p-12f && g.step > 0.f)
+      n = (float)__builtin_rint(((double)v - (double)g.base - (double)g.step) * 16.0 / (double)g.step);
+    const uint32_t code = (uint32_t)fminf(fmaxf(n, 0.f), 15.f);
+    w |= code << code_shift(e);
+  }
+  return w;
+}
+
+// The extremes over the four lanes of a group.
+__device__ __forceinline__ void group_extremes(const float *x, float &lo, float &hi) {
+  lo = hi = clip(x[0]);
+#pragma unroll
+  for (int e = 1; e < 8; ++e) { const float v = clip(x[e]); lo = fminf(lo, v); hi = fmaxf(hi, v); }
+#pragma unroll
+  for (int off = 1; off <= 2; off <<= 1) { lo = fminf(lo, __shfl_xor(lo, off)); hi = fmaxf(hi, __shfl_xor(hi, off)); }
+}
+
+// ------------------------------------------------------------------------------------------------
+// append_paged_kernel.  blockIdx.x: (layer, sequence, KV head); blockIdx.y: workers on the head's pages, then workers on its
+// query rows.
+// ------------------------------------------------------------------------------------------------
+template <int DT, int D, bool Q4>
+__global__ __launch_bounds__(kPagedThreads) void append_paged_kernel(PShape s, PTable tab, PRope rp, int n_rows, int kv_workers) {
+  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RS = kPagedThreads / LPR, RB = D * EB, NG = D / 32, RUNS = D / 8;
+  __shared__ uint32_t words[Q4 ? RS * RUNS : 1];           // codes of the value rows of a pass, a word per eight elements
+  __shared__ float red[4][2][D];
+  const int tid = threadIdx.x, j = tid % LPR, slot = tid / LPR, lane = tid & 63, wave = tid >> 6;
+  const int layer = blockIdx.x / s.units_per_layer, u = blockIdx.x - layer * s.units_per_layer;
+  const int h = u % s.hkv;
+  const PCache c = tab.c[layer];
+  const PRows d = tab.r[layer];
+  const RowRange x = row_range(s, c, d, u, n_rows);
+  const bool turn = rp.cos != nullptr;
+
+  if ((int)blockIdx.y >= kv_workers) {                     // ---- queries
+    const int w = blockIdx.y - kv_workers, nw = gridDim.y - kv_workers;
+    const int64_t items = (int64_t)(x.r1 - x.r0) * s.G;
+    for (int64_t i = (int64_t)w * RS + slot; i < items; i += (int64_t)nw * RS) {
+      const int t = (int)(i / s.G), g = h * s.G + (int)(i - (int64_t)t * s.G);
+      const int64_t row = x.r0 + t + x.shift;
+      const char *src = d.Q + row * d.qsn + g * d.qsh;
+      char *dst = d.Q_out + (row * s.hq + g) * RB;
+      float a[8], b[8];
+      load_run<DT>(src + 8 * EB * j, a);
+      load_run<DT>(src + 8 * EB * (LPR + j), b);
+      if (turn) rotate<DT, D>(rp, row, n_rows, j, a, b);
+      store_run<DT>(dst + 8 * EB * j, a);
+      store_run<DT>(dst + 8 * EB * (LPR + j), b);
+    }
+    return;
+  }
+
+  for (int pg = (x.r0 >> s.lp) + (int)blockIdx.y; pg << s.lp < x.r1; pg += kv_workers) {
+    const int id = page_at(s, c, u, pg);
+    if (id < 0) continue;                                  // uniform: the rows of no page are dropped
+    const int first = pg << s.lp, lo_row = max(x.r0 - first, 0), hi_row = min(x.r1 - first, s.P);   // rows of the page to be written
+    if (lo_row >= hi_row) continue;
+    char *kp = c.K + (int64_t)id * s.page_bytes, *vp = c.V + (int64_t)id * s.page_bytes;
+    float blo[16], bhi[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) { blo[i] = INFINITY; bhi[i] = -INFINITY; }
+    for (int s0 = lo_row / RS * RS; s0 < hi_row; s0 += RS) {
+      const int r = s0 + slot;
+      const bool live = r >= lo_row && r < hi_row;
+      const int64_t row = first + r + x.shift;
+      const char *ks = d.K + row * d.sn + h * d.sh, *vs = d.V + row * d.sn + h * d.sh;
+      float ka[8] = {}, kb[8] = {}, va[8] = {}, vb[8] = {};
+      if (live) {
+        load_run<DT>(ks + 8 * EB * j, ka);
+        load_run<DT>(ks + 8 * EB * (LPR + j), kb);
+        load_run<DT>(vs + 8 * EB * j, va);
+        load_run<DT>(vs + 8 * EB * (LPR + j), vb);
+        if (turn) rotate<DT, D>(rp, row, n_rows, j, ka, kb);
+        if (c.bounds) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            blo[i] = fminf(blo[i], ka[i]); bhi[i] = fmaxf(bhi[i], ka[i]);
+            blo[8 + i] = fminf(blo[8 + i], kb[i]); bhi[8 + i] = fmaxf(bhi[8 + i], kb[i]);
+          }
+        }
+      }
+      if constexpr (!Q4) {
+        if (live) {
+          store_run<DT>(kp + (int64_t)r * RB + 8 * EB * j, ka);
+          store_run<DT>(kp + (int64_t)r * RB + 8 * EB * (LPR + j), kb);
+          store_run<DT>(vp + (int64_t)r * RB + 8 * EB * j, va);
+          store_run<DT>(vp + (int64_t)r * RB + 8 * EB * (LPR + j), vb);
+        }
+      } else {
+        // group of the lane's first run is j / 4, of its second D/64 more: neighbours in a key row's words
+        const int ga = j >> 2, gb = ga + NG / 2;
+        float lo, hi;
+        group_extremes(ka, lo, hi);
+        const GroupScale ska = group_scale(lo, hi);
+        group_extremes(kb, lo, hi);
+        const GroupScale skb = group_scale(lo, hi);
+        group_extremes(va, lo, hi);
+        const GroupScale sva = group_scale(lo, hi);
+        group_extremes(vb, lo, hi);
+        const GroupScale svb = group_scale(lo, hi);
+        const int64_t codes = (int64_t)s.P * D / 2;        // bytes of codes in front of the scales
+        if (live) {
+          uint32_t *kw = reinterpret_cast<uint32_t *>(kp) + r * RUNS + (j & 3) * NG + 2 * ga;
+          *reinterpret_cast<u32x2 *>(kw) = u32x2{run_codes(ka, ska), run_codes(kb, skb)};
+          if ((j & 3) == 0) {
+            *reinterpret_cast<u32x2 *>(kp + codes + (r * NG + 2 * ga) * 4) = u32x2{ska.bits, skb.bits};
+            // strip and place of the row among the strip's eight
+            const int strip = (r >> 5) * 4 + ((r & 15) >> 2), e = 2 * (r & 3) + ((r >> 4) & 1);
+            uint16_t *vsc = reinterpret_cast<uint16_t *>(vp + codes) + strip * NG * 16 + e;
+            vsc[ga * 16] = (uint16_t)sva.bits; vsc[ga * 16 + 8] = (uint16_t)(sva.bits >> 16);
+            vsc[gb * 16] = (uint16_t)svb.bits; vsc[gb * 16 + 8] = (uint16_t)(svb.bits >> 16);
+          }
+          words[slot * RUNS + j] = run_codes(va, sva);
+          words[slot * RUNS + LPR + j] = run_codes(vb, svb);
+        }
+        __syncthreads();
+        // the strips' words: eight rows' codes of an element each; rows that are not written keep theirs
+        for (int i = tid; i < RS / 8 * D; i += kPagedThreads) {
+          const int sl = i / D, wi = i - sl * D, el = (wi >> 6) * 64 + (wi & 3) * 16 + ((wi >> 2) & 15);   // strip of the pass, word, element
+          const int t0 = s0 + (sl >> 2) * 32 + (sl & 3) * 4;   // the strip's first row in the page
+          uint32_t w = 0, mask = 0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int rr = t0 + (e >> 1) + 16 * (e & 1);
+            if (rr >= lo_row && rr < hi_row) {
+              w |= ((words[(rr - s0) * RUNS + (el >> 3)] >> code_shift(el & 7)) & 15u) << code_shift(e);
+              mask |= 15u << code_shift(e);
+            }
+          }
+          if (mask == 0) continue;
+          uint32_t *dst = reinterpret_cast<uint32_t *>(vp) + (t0 >> 5) * 4 * D + ((t0 & 15) >> 2) * D + wi;
+          if (mask != 0xffffffffu) w |= *dst & ~mask;
+          *dst = w;
+        }
+        __syncthreads();
+      }
+    }
+    if (c.bounds) {                                        // uniform: over the lanes with the same elements, then the waves
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int off = LPR; off < 64; off <<= 1) {
+          blo[i] = fminf(blo[i], __shfl_xor(blo[i], off));
+          bhi[i] = fmaxf(bhi[i], __shfl_xor(bhi[i], off));
+        }
+      if (lane < LPR) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int el = (i < 8 ? 0 : D / 2) + 8 * j + (i & 7);
+          red[wave][0][el] = blo[i];
+          red[wave][1][el] = bhi[i];
+        }
+      }
+      __syncthreads();
+      for (int i = tid; i < 2 * D; i += kPagedThreads) {
+        const int side = i / D, el = i - side * D;
+        float v = red[0][side][el];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) v = side ? fmaxf(v, red[w][side][el]) : fminf(v, red[w][side][el]);
+        char *dst = c.bounds + ((int64_t)id * 2 * D + i) * EB;
+        if (lo_row > 0) {                                  // rows of an earlier call are in the page
+          float old;
+          if constexpr (DT == MIXKV_BF16) old = __uint_as_float((uint32_t)*reinterpret_cast<uint16_t *>(dst) << 16);
+          else old = *reinterpret_cast<float *>(dst);
+          v = side ? fmaxf(v, old) : fminf(v, old);
+        }
+        if constexpr (DT == MIXKV_BF16) *reinterpret_cast<uint16_t *>(dst) = (uint16_t)(__float_as_uint(v) >> 16);
+        else *reinterpret_cast<float *>(dst) = v;
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// read_paged_kernel.  blockIdx.x: (layer, sequence, KV head); blockIdx.y: workers on the head's passes of RS rows.
+// ------------------------------------------------------------------------------------------------
+template <int DT, int D, bool Q4>
+__global__ __launch_bounds__(kPagedThreads) void read_paged_kernel(PShape s, PTable tab, int n_rows) {
+  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RS = 32, RB = D * EB, NG = D / 32, RUNS = D / 8, THREADS = LPR * RS;
+  const int tid = threadIdx.x, j = tid % LPR, slot = tid / LPR;
+  const int layer = blockIdx.x / s.units_per_layer, u = blockIdx.x - layer * s.units_per_layer;
+  const int h = u % s.hkv;
+  const PCache c = tab.c[layer];
+  const PRows d = tab.r[layer];
+  const RowRange x = row_range(s, c, d, u, n_rows);
+  if (tid >= THREADS) return;
+  for (int t0 = x.r0 / RS + (int)blockIdx.y; t0 * RS < x.r1; t0 += gridDim.y) {
+    const int id = page_at(s, c, u, (t0 * RS) >> s.lp);
+    const int r = ((t0 * RS) & (s.P - 1)) + slot, at = t0 * RS + slot;   // row of the page, of the head
+    if (id < 0 || at < x.r0 || at >= x.r1) continue;
+    const char *kp = c.K + (int64_t)id * s.page_bytes, *vp = c.V + (int64_t)id * s.page_bytes;
+    float ka[8], kb[8], va[8], vb[8];
+    if constexpr (!Q4) {
+      load_run<DT>(kp + (int64_t)r * RB + 8 * EB * j, ka);
+      load_run<DT>(kp + (int64_t)r * RB + 8 * EB * (LPR + j), kb);
+      load_run<DT>(vp + (int64_t)r * RB + 8 * EB * j, va);
+      load_run<DT>(vp + (int64_t)r * RB + 8 * EB * (LPR + j), vb);
+    } else {
+      const int ga = j >> 2, gb = ga + NG / 2;
+      const int64_t codes = (int64_t)s.P * D / 2;
+      const u32x2 kw = *reinterpret_cast<const u32x2 *>(reinterpret_cast<const uint32_t *>(kp) + r * RUNS + (j & 3) * NG + 2 * ga);
+      const u32x2 ks = *reinterpret_cast<const u32x2 *>(kp + codes + (r * NG + 2 * ga) * 4);
+      const int strip = (r >> 5) * 4 + ((r & 15) >> 2), e = 2 * (r & 3) + ((r >> 4) & 1), sh = code_shift(e);
+      const uint16_t *vsc = reinterpret_cast<const uint16_t *>(vp + codes) + strip * NG * 16 + e;
+      const float sa = f16_value(vsc[ga * 16]), ba = f16_value(vsc[ga * 16 + 8]), sb = f16_value(vsc[gb * 16]), bb = f16_value(vsc[gb * 16 + 8]);
+      const uint32_t *vw = reinterpret_cast<const uint32_t *>(vp) + strip * D;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        ka[i] = code_value((kw[0] >> code_shift(i)) & 15u, f16_value(ks[0] & 0xffffu), f16_value(ks[0] >> 16));
+        kb[i] = code_value((kw[1] >> code_shift(i)) & 15u, f16_value(ks[1] & 0xffffu), f16_value(ks[1] >> 16));
+        const int ea = 8 * j + i, eb = D / 2 + 8 * j + i;
+        const int wa = (ea >> 6) * 64 + (ea & 15) * 4 + ((ea >> 4) & 3), wb = (eb >> 6) * 64 + (eb & 15) * 4 + ((eb >> 4) & 3);
+        va[i] = code_value((vw[wa] >> sh) & 15u, sa, ba);
+        vb[i] = code_value((vw[wb] >> sh) & 15u, sb, bb);
+      }
+    }
+    const int64_t row = at + x.shift;
+    char *kd = d.K + row * d.sn + h * d.sh, *vd = d.V + row * d.sn + h * d.sh;
+    store_run<DT>(kd + 8 * EB * j, ka);
+    store_run<DT>(kd + 8 * EB * (LPR + j), kb);
+    store_run<DT>(vd + 8 * EB * j, va);
+    store_run<DT>(vd + 8 * EB * (LPR + j), vb);
+  }
+}
+
+mixkv_status make_pshape(const mixkv_paged_params *p, PShape *s) {
+  if (!p) return MIXKV_ERR_INVALID_ARG;
+  if (p->dtype != MIXKV_F32 && p->dtype != MIXKV_BF16) return MIXKV_ERR_INVALID_ARG;
+  if (p->format != MIXKV_PAGE_ROWS && p->format != MIXKV_PAGE_4BIT) return MIXKV_ERR_INVALID_ARG;
+  if (p->batch < 1 || p->n_q_heads < 1 || p->n_kv_heads < 1 || p->n_q_heads % p->n_kv_heads != 0) return MIXKV_ERR_INVALID_ARG;
+  if (p->max_pages < 1 || p->n_pages < 1) return MIXKV_ERR_INVALID_ARG;
+  if (!(p->softmax_scale > 0.f) || p->softmax_scale > 3e38f) return MIXKV_ERR_INVALID_ARG;
+  if (p->head_dim != 64 && p->head_dim != 128) return MIXKV_ERR_UNSUPPORTED;
+  if (p->page_rows != 32 && p->page_rows != 64 && p->page_rows != 128) return MIXKV_ERR_UNSUPPORTED;
+  if (p->format == MIXKV_PAGE_4BIT && p->dtype != MIXKV_BF16) return MIXKV_ERR_UNSUPPORTED;
+  if ((int64_t)p->max_pages * p->page_rows > (1 << 30)) return MIXKV_ERR_UNSUPPORTED;
+  if ((int64_t)p->batch * p->n_q_heads > (1 << 20)) return MIXKV_ERR_UNSUPPORTED;      // units and heads of a launch stay in 32 bits
+  s->batch = p->batch; s->hq = p->n_q_heads; s->hkv = p->n_kv_heads; s->G = p->n_q_heads / p->n_kv_heads; s->D = p->head_dim;
+  s->P = p->page_rows; s->lp = p->page_rows == 32 ? 5 : p->page_rows == 64 ? 6 : 7;
+  s->max_pages = p->max_pages; s->n_pages = p->n_pages;
+  s->units_per_layer = p->batch * p->n_kv_heads;
+  s->q4 = p->format == MIXKV_PAGE_4BIT;
+  s->page_bytes = page_bytes_of(s->q4, p->dtype, s->P, s->D);
+  s->scale_log2e = p->softmax_scale * 1.44269504088896340736f;
+  return MIXKV_OK;
+}
+
+mixkv_status check_caches(const mixkv_paged_params *, const mixkv_paged_cache *c, int n_layers, bool pages, bool bounds) {
+  if (!c || n_layers < 1 || n_layers > MIXKV_MAX_LAYERS) return MIXKV_ERR_INVALID_ARG;
+  for (int l = 0; l < n_layers; ++l) {
+    if (pages && (!c[l].K_pages || !c[l].V_pages || c[l].K_pages == c[l].V_pages)) return MIXKV_ERR_INVALID_ARG;
+    if (misaligned(c[l].K_pages, 16) || misaligned(c[l].V_pages, 16) || misaligned(c[l].K_bounds, 16)) return MIXKV_ERR_INVALID_ARG;
+    if (bounds && !c[l].K_bounds) return MIXKV_ERR_INVALID_ARG;
+    if (!c[l].page_table || !c[l].lengths || misaligned(c[l].page_table, 4) || misaligned(c[l].lengths, 4)) return MIXKV_ERR_INVALID_ARG;
+  }
+  return MIXKV_OK;
+}
+
+static PCache cache_of(const mixkv_paged_cache &c) {
+  return PCache{static_cast<char *>(c.K_pages), static_cast<char *>(c.V_pages), static_cast<char *>(c.K_bounds), c.page_table, c.lengths};
+}
+
+static mixkv_status check_rows(const PShape &s, int eb, const mixkv_paged_rows *r, int n_layers, int64_t n_rows, bool append) {
+  if (!r) return MIXKV_ERR_INVALID_ARG;
+  auto bad_stride = [&](int64_t n, int64_t h) { return n < s.D || h < 0 || n > INT64_MAX / 16 / (n_rows + 1) || h > (INT64_MAX >> 30) || (n * eb) % 16 || (h * eb) % 16; };
+  auto span = [&](int64_t n, int64_t h, int heads) { return (uint64_t)((n_rows - 1) * n + (heads - 1) * h + s.D) * eb; };
+  auto overlap = [](const void *a, uint64_t na, const void *b, uint64_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + nb && y < x + na;
+  };
+  for (int l = 0; l < n_layers; ++l) {
+    const mixkv_paged_rows &d = r[l];
+    if (!d.K || !d.V || misaligned(d.K, 16) || misaligned(d.V, 16) || bad_stride(d.stride_n, d.stride_h)) return MIXKV_ERR_INVALID_ARG;
+    if (!d.row_start || !d.row_count || misaligned(d.row_start, 4) || misaligned(d.row_count, 4)) return MIXKV_ERR_INVALID_ARG;
+    const uint64_t kv = span(d.stride_n, d.stride_h, s.hkv);
+    if (!append) {
+      if (d.K == d.V) return MIXKV_ERR_INVALID_ARG;
+      continue;
+    }
+    if (!d.Q != !d.Q_out || !d.Q != !r[0].Q) return MIXKV_ERR_INVALID_ARG;    // for all layers of a call or none
+    if (!d.Q) continue;
+    if (misaligned(d.Q, 16) || misaligned(d.Q_out, 16) || bad_stride(d.q_stride_n, d.q_stride_h)) return MIXKV_ERR_INVALID_ARG;
+    const uint64_t out = (uint64_t)n_rows * s.hq * s.D * eb;
+    if (overlap(d.Q_out, out, d.Q, span(d.q_stride_n, d.q_stride_h, s.hq)) || overlap(d.Q_out, out, d.K, kv) || overlap(d.Q_out, out, d.V, kv))
+      return MIXKV_ERR_INVALID_ARG;
+  }
+  return MIXKV_OK;
+}
+
+static PTable table_of(const mixkv_paged_cache *c, const mixkv_paged_rows *r, int nl, int eb) {
+  PTable t;
+  for (int l = 0; l < kPagedLayers; ++l) {
+    t.c[l] = PCache{};
+    t.r[l] = PRows{};
+    if (l >= nl) continue;
+    t.c[l] = cache_of(c[l]);
+    t.r[l] = PRows{static_cast<char *>(r[l].K), static_cast<char *>(r[l].V), r[l].stride_n * eb, r[l].stride_h * eb, r[l].row_start,
+                   r[l].row_count, static_cast<const char *>(r[l].Q), r[l].q_stride_n * eb, r[l].q_stride_h * eb, static_cast<char *>(r[l].Q_out)};
+  }
+  return t;
+}
+
+// Workers of a unit: one for every `per` rows or pages that it may touch, as long as a launch has no more workgroups than keep the
+// chip busy several times over; the workers then walk.
+static int workers(int64_t wanted, int64_t units) {
+  const int64_t most = 16384 / units < 1 ? 1 : 16384 / units;
+  return (int)(wanted < most ? wanted : most);
+}
+
+}  // namespace mixkv
+
+extern "C" mixkv_status mixkv_page_bytes(const mixkv_paged_params *params, size_t *bytes) {
+  using namespace mixkv;
+  PShape s;
+  const mixkv_status st = make_pshape(params, &s);
+  if (st != MIXKV_OK) return st;
+  if (!bytes) return MIXKV_ERR_INVALID_ARG;
+  *bytes = (size_t)s.page_bytes;
+  return MIXKV_OK;
+}
+
+extern "C" mixkv_status mixkv_paged_append(const mixkv_paged_params *params, const mixkv_paged_cache *caches, const mixkv_paged_rows *rows,
+                                           int32_t n_layers, const mixkv_rope *rope, int32_t n_rows, int32_t max_count, void *hip_stream) {
+  using namespace mixkv;
+  PShape s;
+  mixkv_status st = make_pshape(params, &s);
+  if (st != MIXKV_OK) return st;
+  if (n_rows < 1 || max_count < 1) return MIXKV_ERR_INVALID_ARG;
+  if ((st = check_caches(params, caches, n_layers, true, false)) != MIXKV_OK) return st;
+  const int eb = params->dtype == MIXKV_BF16 ? 2 : 4;
+  if ((st = check_rows(s, eb, rows, n_layers, n_rows, true)) != MIXKV_OK) return st;
+  PRope rp{};
+  rp.n_axes = 1; rp.n_positions = 1;
+  if (rope) {
+    if (!rope->cos || !rope->sin || !rope->positions || misaligned(rope->cos, 16) || misaligned(rope->sin, 16) || misaligned(rope->positions, 4))
+      return MIXKV_ERR_INVALID_ARG;
+    if (rope->n_positions < 1 || (rope->n_axes != 1 && rope->n_axes != 3)) return MIXKV_ERR_INVALID_ARG;
+    rp = PRope{rope->cos, rope->sin, rope->positions, rope->n_positions, rope->n_axes, s.D / 2, s.D / 2};
+    if (rope->n_axes == 3) {
+      const int32_t *q = rope->sections;
+      if (q[0] < 0 || q[1] < 0 || q[2] < 0 || (int64_t)q[0] + q[1] + q[2] != s.D / 2) return MIXKV_ERR_INVALID_ARG;
+      rp.s0 = q[0]; rp.s1 = q[0] + q[1];
+    }
+  }
+  hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+  if (max_count > n_rows) max_count = n_rows;
+  for (int l0 = 0; l0 < n_layers; l0 += kPagedLayers) {
+    const int nl = n_layers - l0 < kPagedLayers ? n_layers - l0 : kPagedLayers;
+    const PTable t = table_of(caches + l0, rows + l0, nl, eb);
+    const int64_t units = (int64_t)nl * s.units_per_layer;
+    const int kvw = workers(((int64_t)max_count + s.P - 2) / s.P + 1, units);
+    const int qw = rows[0].Q ? workers(((int64_t)max_count * s.G + 31) / 32, units) : 0;
+    auto go = [&](auto kern) {
+      hipLaunchKernelGGL(kern, dim3((unsigned)units, (unsigned)(kvw + qw)), dim3(kPagedThreads), 0, stream, s, t, rp, n_rows, kvw);
+    };
+    if (s.q4) { if (s.D == 128) go(append_paged_kernel<MIXKV_BF16, 128, true>); else go(append_paged_kernel<MIXKV_BF16, 64, true>); }
+    else if (params->dtype == MIXKV_BF16) { if (s.D == 128) go(append_paged_kernel<MIXKV_BF16, 128, false>); else go(append_paged_kernel<MIXKV_BF16, 64, false>); }
+    else { if (s.D == 128) go(append_paged_kernel<MIXKV_F32, 128, false>); else go(append_paged_kernel<MIXKV_F32, 64, false>); }
+    if (hipGetLastError() != hipSuccess) return MIXKV_ERR_HIP;
+  }
+  return MIXKV_OK;
+}
+
+extern "C" mixkv_status mixkv_paged_read(const mixkv_paged_params *params, const mixkv_paged_cache *caches, const mixkv_paged_rows *rows,
+                                         int32_t n_layers, int32_t n_rows, int32_t max_count, void *hip_stream) {
+  using namespace mixkv;
+  PShape s;
+  mixkv_status st = make_pshape(params, &s);
+  if (st != MIXKV_OK) return st;
+  if (n_rows < 1 || max_count < 1) return MIXKV_ERR_INVALID_ARG;
+  if ((st = check_caches(params, caches, n_layers, true, false)) != MIXKV_OK) return st;
+  const int eb = params->dtype == MIXKV_BF16 ? 2 : 4;
+  if ((st = check_rows(s, eb, rows, n_layers, n_rows, false)) != MIXKV_OK) return st;
+  hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+  if (max_count > n_rows) max_count = n_rows;
+  for (int l0 = 0; l0 < n_layers; l0 += kPagedLayers) {
+    const int nl = n_layers - l0 < kPagedLayers ? n_layers - l0 : kPagedLayers;
+    const PTable t = table_of(caches + l0, rows + l0, nl, eb);
+    const int64_t units = (int64_t)nl * s.units_per_layer;
+    const int w = workers(((int64_t)max_count + 30) / 32 + 1, units);
+    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)units, (unsigned)w), dim3(kPagedThreads), 0, stream, s, t, n_rows); };
+    if (s.q4) { if (s.D == 128) go(read_paged_kernel<MIXKV_BF16, 128, true>); else go(read_paged_kernel<MIXKV_BF16, 64, true>); }
+    else if (params->dtype == MIXKV_BF16) { if (s.D == 128) go(read_paged_kernel<MIXKV_BF16, 128, false>); else go(read_paged_kernel<MIXKV_BF16, 64, false>); }
+    else { if (s.D == 128) go(read_paged_kernel<MIXKV_F32, 128, false>); else go(read_paged_kernel<MIXKV_F32, 64, false>); }
+    if (hipGetLastError() != hipSuccess) return MIXKV_ERR_HIP;
+  }
+  return MIXKV_OK;
+}
