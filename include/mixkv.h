@@ -342,7 +342,7 @@ typedef struct {
   mixkv_dtype dtype;         /* element type of rows, queries, outputs and key bounds */
   mixkv_page_format format;  /* of the pages; 4BIT needs MIXKV_BF16 */
   int32_t batch;
-  int32_t n_q_heads;         /* multiple of n_kv_heads */
+  int32_t n_q_heads;         /* multiple of n_kv_heads; batch * n_q_heads <= 2^18 */
   int32_t n_kv_heads;
   int32_t head_dim;          /* 64 or 128 */
   int32_t page_rows;         /* 32, 64 or 128 */
@@ -409,6 +409,48 @@ mixkv_status mixkv_paged_append(const mixkv_paged_params *params, const mixkv_pa
  */
 mixkv_status mixkv_paged_read(const mixkv_paged_params *params, const mixkv_paged_cache *caches, const mixkv_paged_rows *rows,
                               int32_t n_layers, int32_t n_rows, int32_t max_count, void *hip_stream);
+
+/*
+ * Pages worth attending to: for the new token of every sequence and every KV head, the max_selected pages with the largest score
+ *     s_p = fp32(sum_d (Q+_d hi_pd + Q-_d lo_pd)),  Q+_d = sum_g max(q_gd, 0),  Q-_d = sum_g min(q_gd, 0)  over the head's G queries,
+ * in 64 bits, with lo and hi the page's K_bounds: the sum over the queries of the largest dot product that any key within
+ * the bounds can have (a bound that meets a zero counts nothing, infinite ones too).  The first keep_first and the last keep_last pages are always among them (keep_first + keep_last <=
+ * max_selected); equal scores go to the earlier page, places without a page
+ * come last; a head with no more pages than max_selected keeps all.  NaN is not supported.
+ * Writes selected [batch, n_kv_heads, max_selected] (places in the head's page table, ascending, then -1) and n_selected
+ * [batch, n_kv_heads].  K_pages and V_pages are not used and may be NULL; softmax_scale is not used.
+ * Workspace: mixkv_paged_select_workspace_size bytes, 256-byte aligned, no initialisation.
+ */
+typedef struct {
+  const void *Q;             /* [batch, n_q_heads, D] contiguous, 16-byte aligned */
+  int32_t *selected;         /* [batch, n_kv_heads, max_selected] */
+  int32_t *n_selected;       /* [batch, n_kv_heads] */
+} mixkv_paged_select_layer;
+mixkv_status mixkv_paged_select_workspace_size(const mixkv_paged_params *params, int32_t n_layers, size_t *bytes);
+mixkv_status mixkv_paged_select(const mixkv_paged_params *params, const mixkv_paged_cache *caches, const mixkv_paged_select_layer *layers,
+                                int32_t n_layers, int32_t max_selected, int32_t keep_first, int32_t keep_last, void *workspace,
+                                size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Attention of one new token per sequence over its pages (Sec. 3.1, as mixkv_decode_attention): out_g = sum_j
+ * softmax_j(softmax_scale * Q_g . k_j) v_j over the rows of KV head g / G, all lengths[b][h] of them or (selected given, for every
+ * layer or none) those in the pages selected[b][h][0 .. n_selected[b][h]): places in the page table, in any order; one that is no place
+ * in the table is passed over, a page that is listed twice counts twice.  A head without rows gets zeros.  fp32
+ * accumulation, out in the dtype.  With 4-bit pages, values and weights enter the second product as fp16.
+ * max_rows: the largest number of rows of a head (of selected pages, whole), as far as the host knows it (>= 1): with it the
+ * rows are dealt to workgroups; longer heads are served, slower.  Outputs repeat bit for bit for the same arguments, max_rows included.
+ * Workspace: mixkv_paged_attention_workspace_size bytes (0: NULL is accepted), 256-byte aligned, no initialisation.
+ */
+typedef struct {
+  const void *Q;             /* [batch, n_q_heads, D] contiguous, rows 16-byte aligned */
+  void *out;                 /* [batch, n_q_heads, D], 16-byte aligned */
+  const int32_t *selected;   /* [batch, n_kv_heads, max_selected] or NULL */
+  const int32_t *n_selected; /* [batch, n_kv_heads], with selected */
+} mixkv_paged_attention_layer;
+mixkv_status mixkv_paged_attention_workspace_size(const mixkv_paged_params *params, int32_t n_layers, int32_t max_rows, size_t *bytes);
+mixkv_status mixkv_paged_attention(const mixkv_paged_params *params, const mixkv_paged_cache *caches,
+                                   const mixkv_paged_attention_layer *layers, int32_t n_layers, int32_t max_selected, int32_t max_rows,
+                                   void *workspace, size_t workspace_bytes, void *hip_stream);
 
 const char *mixkv_status_string(mixkv_status status);
 int32_t mixkv_version(void);

@@ -187,7 +187,8 @@ def page_scores(Q, bounds, table, lengths, P, b, h):
     for i in range(len(out)):
         page = _page(table, b, h, i, len(bounds))
         if page >= 0:
-            out[i] = np.float32((bounds[page, 1] * up + bounds[page, 0] * down).sum())
+            hi, lo = np.where(up != 0, bounds[page, 1], 0.0), np.where(down != 0, bounds[page, 0], 0.0)
+            out[i] = np.float32((hi * up + lo * down).sum())
     return out
 
 

@@ -90,6 +90,14 @@ class MixkvRope(C.Structure):
                 ("sections", C.c_int32 * 3)]
 
 
+class MixkvPagedSelectLayer(C.Structure):
+    _fields_ = [("Q", C.c_void_p), ("selected", C.c_void_p), ("n_selected", C.c_void_p)]
+
+
+class MixkvPagedAttentionLayer(C.Structure):
+    _fields_ = [("Q", C.c_void_p), ("out", C.c_void_p), ("selected", C.c_void_p), ("n_selected", C.c_void_p)]
+
+
 class MixkvError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -139,6 +147,16 @@ def lib() -> C.CDLL:
         L.mixkv_paged_append.restype = C.c_int
         L.mixkv_paged_read.argtypes = [pg, pc, pr, C.c_int32, C.c_int32, C.c_int32, C.c_void_p]
         L.mixkv_paged_read.restype = C.c_int
+        L.mixkv_paged_select_workspace_size.argtypes = [pg, C.c_int32, C.POINTER(C.c_size_t)]
+        L.mixkv_paged_select_workspace_size.restype = C.c_int
+        L.mixkv_paged_select.argtypes = [pg, pc, C.POINTER(MixkvPagedSelectLayer), C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
+                                         C.c_size_t, C.c_void_p]
+        L.mixkv_paged_select.restype = C.c_int
+        L.mixkv_paged_attention_workspace_size.argtypes = [pg, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
+        L.mixkv_paged_attention_workspace_size.restype = C.c_int
+        L.mixkv_paged_attention.argtypes = [pg, pc, C.POINTER(MixkvPagedAttentionLayer), C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
+                                            C.c_size_t, C.c_void_p]
+        L.mixkv_paged_attention.restype = C.c_int
         L.mixkv_stage_name.argtypes = [C.c_int32]
         L.mixkv_stage_name.restype = C.c_char_p
         L.mixkv_status_string.argtypes = [C.c_int]
@@ -580,6 +598,102 @@ class PreparedPagedRead:
 
 def mixkv_paged_read(p: MixkvPagedParams, caches: Sequence[PagedCache], rows: Sequence[PagedRows], max_count: Optional[int] = None, stream=None):
     PreparedPagedRead(p, caches, rows, max_count).run(stream)
+
+
+def _paged_workspace(workspace, need: int, device):
+    if isinstance(workspace, str):                    # allocate what the shape needs (possibly nothing)
+        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    _need(workspace is None or workspace.is_contiguous() and workspace.device == device, f"the workspace has to be contiguous, on {device}")
+    return workspace
+
+
+def mixkv_paged_select_workspace_size(p: MixkvPagedParams, n_layers: int) -> int:
+    n = C.c_size_t(0)
+    _check(lib().mixkv_paged_select_workspace_size(C.byref(p), n_layers, C.byref(n)), "mixkv_paged_select_workspace_size")
+    return n.value
+
+
+class PreparedPagedSelect:
+    """The C arguments of one mixkv_paged_select call.  Qs: per layer [batch, Hq, D]; selected [batch, Hkv, max_selected] and n_selected
+    [batch, Hkv] i32 receive the places of the selected pages."""
+
+    def __init__(self, p: MixkvPagedParams, caches: Sequence[PagedCache], Qs, selected, n_selected, keep_first: int = 1, keep_last: int = 1,
+                 workspace="alloc"):
+        device = _paged_device(caches[0].lengths)
+        n = len(caches)
+        _need(n == len(Qs) == len(selected) == len(n_selected), "queries and selections for every cache")
+        self.p, self.n, self.caches, self.most = p, n, _paged_caches(p, caches, False, True, device), selected[0].shape[-1]
+        self.arr = (MixkvPagedSelectLayer * n)()
+        for i in range(n):
+            _tensor(Qs[i], "Q", TORCH_DTYPE[p.dtype], (p.batch, p.n_q_heads, p.head_dim), device)
+            _tensor(selected[i], "selected", torch.int32, (p.batch, p.n_kv_heads, self.most), device)
+            _tensor(n_selected[i], "n_selected", torch.int32, (p.batch, p.n_kv_heads), device)
+            self.arr[i] = MixkvPagedSelectLayer(_ptr(Qs[i]), _ptr(selected[i]), _ptr(n_selected[i]))
+        self.first, self.last = keep_first, keep_last
+        workspace = _paged_workspace(workspace, mixkv_paged_select_workspace_size(p, n) if isinstance(workspace, str) else 0, device)
+        self.wp, self.wb = _ws(workspace)
+        self._keep = (caches, Qs, selected, n_selected, workspace)
+        self._L = lib()
+
+    def run(self, stream=None):
+        _check(self._L.mixkv_paged_select(C.byref(self.p), self.caches, self.arr, self.n, self.most, self.first, self.last, self.wp, self.wb,
+                                          _stream(stream)), "mixkv_paged_select")
+
+
+def mixkv_paged_select(p: MixkvPagedParams, caches: Sequence[PagedCache], Qs, max_selected: int, keep_first: int = 1, keep_last: int = 1,
+                       workspace="alloc", stream=None):
+    """Returns per layer the places of the selected pages [batch, Hkv, max_selected] and their numbers [batch, Hkv]."""
+    dev, n = caches[0].lengths.device, len(caches)
+    selected = [torch.empty((p.batch, p.n_kv_heads, max_selected), dtype=torch.int32, device=dev) for _ in range(n)]
+    n_selected = [torch.empty((p.batch, p.n_kv_heads), dtype=torch.int32, device=dev) for _ in range(n)]
+    PreparedPagedSelect(p, caches, Qs, selected, n_selected, keep_first, keep_last, workspace).run(stream)
+    return selected, n_selected
+
+
+def mixkv_paged_attention_workspace_size(p: MixkvPagedParams, n_layers: int, max_rows: int) -> int:
+    n = C.c_size_t(0)
+    _check(lib().mixkv_paged_attention_workspace_size(C.byref(p), n_layers, max_rows, C.byref(n)), "mixkv_paged_attention_workspace_size")
+    return n.value
+
+
+class PreparedPagedAttention:
+    """The C arguments of one mixkv_paged_attention call.  Qs / outs: per layer [batch, Hq, D]; selected / n_selected: per layer the places
+    of the pages to attend to, or None for all; max_rows: the largest number of rows of a head as far as the host knows it (None:
+    what the page table, or the selection, can hold)."""
+
+    def __init__(self, p: MixkvPagedParams, caches: Sequence[PagedCache], Qs, outs, selected=None, n_selected=None,
+                 max_rows: Optional[int] = None, workspace="alloc"):
+        device = _paged_device(caches[0].lengths)
+        n, sparse = len(caches), selected is not None
+        _need(n == len(Qs) == len(outs) and (not sparse or n == len(selected) == len(n_selected)), "queries, outputs and selections for every cache")
+        self.p, self.n, self.caches = p, n, _paged_caches(p, caches, True, False, device)
+        self.most = selected[0].shape[-1] if sparse else 0
+        self.rows = max_rows if max_rows is not None else (min(self.most, p.max_pages) if sparse else p.max_pages) * p.page_rows
+        self.arr = (MixkvPagedAttentionLayer * n)()
+        for i in range(n):
+            for name, t in (("Q", Qs[i]), ("out", outs[i])):
+                _tensor(t, name, TORCH_DTYPE[p.dtype], (p.batch, p.n_q_heads, p.head_dim), device)
+            if sparse:
+                _tensor(selected[i], "selected", torch.int32, (p.batch, p.n_kv_heads, self.most), device)
+                _tensor(n_selected[i], "n_selected", torch.int32, (p.batch, p.n_kv_heads), device)
+            self.arr[i] = MixkvPagedAttentionLayer(_ptr(Qs[i]), _ptr(outs[i]), *((_ptr(selected[i]), _ptr(n_selected[i])) if sparse else (None, None)))
+        need = mixkv_paged_attention_workspace_size(p, n, self.rows) if isinstance(workspace, str) else 0
+        workspace = _paged_workspace(workspace, need, device)
+        self.wp, self.wb = _ws(workspace)
+        self._keep = (caches, Qs, outs, selected, n_selected, workspace)
+        self._L = lib()
+
+    def run(self, stream=None):
+        _check(self._L.mixkv_paged_attention(C.byref(self.p), self.caches, self.arr, self.n, self.most, self.rows, self.wp, self.wb,
+                                             _stream(stream)), "mixkv_paged_attention")
+
+
+def mixkv_paged_attention(p: MixkvPagedParams, caches: Sequence[PagedCache], Qs, selected=None, n_selected=None, max_rows: Optional[int] = None,
+                          workspace="alloc", stream=None):
+    """Returns per layer the attention output [batch, Hq, D] of the new token of every sequence."""
+    outs = [torch.empty_like(q) for q in Qs]
+    PreparedPagedAttention(p, caches, Qs, outs, selected, n_selected, max_rows, workspace).run(stream)
+    return outs
 
 
 def compacted_rows(p: MixkvParams, out: LayerOut) -> PagedRows:

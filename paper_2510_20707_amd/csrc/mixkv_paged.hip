@@ -368,7 +368,7 @@ mixkv_status make_pshape(const mixkv_paged_params *p, PShape *s) {
   if (p->page_rows != 32 && p->page_rows != 64 && p->page_rows != 128) return MIXKV_ERR_UNSUPPORTED;
   if (p->format == MIXKV_PAGE_4BIT && p->dtype != MIXKV_BF16) return MIXKV_ERR_UNSUPPORTED;
   if ((int64_t)p->max_pages * p->page_rows > (1 << 30)) return MIXKV_ERR_UNSUPPORTED;
-  if ((int64_t)p->batch * p->n_q_heads > (1 << 20)) return MIXKV_ERR_UNSUPPORTED;      // units and heads of a launch stay in 32 bits
+  if ((int64_t)p->batch * p->n_q_heads > (1 << 18)) return MIXKV_ERR_UNSUPPORTED;      // a launch has fewer than 2^32 threads
   s->batch = p->batch; s->hq = p->n_q_heads; s->hkv = p->n_kv_heads; s->G = p->n_q_heads / p->n_kv_heads; s->D = p->head_dim;
   s->P = p->page_rows; s->lp = p->page_rows == 32 ? 5 : p->page_rows == 64 ? 6 : 7;
   s->max_pages = p->max_pages; s->n_pages = p->n_pages;

@@ -40,9 +40,26 @@ def _rope(**kw):
     return B.MixkvRope(f["cos"], f["sin"], f["n_positions"], f["positions"], f["n_axes"], (C.c_int32 * 3)(*f["sections"]))
 
 
+def _select(p=None, caches=None, n=1, keep=8, first=1, last=1, ws=0x900000, size=1 << 40, null=False, **kw):
+    arr = (B.MixkvPagedSelectLayer * max(n, 1))()
+    for i in range(max(n, 1)):
+        arr[i] = B.MixkvPagedSelectLayer(*{**dict(Q=0x1000, selected=0x2000, n_selected=0x3000), **kw}.values())
+    return B.lib().mixkv_paged_select(C.byref(p or _params()), _caches(max(n, 1)) if caches is None else caches, None if null else arr, n, keep, first, last,
+                                      ws, size, None)
+
+
+def _attend(p=None, caches=None, n=1, most=8, rows=1000, ws=0x900000, size=1 << 40, null=False, second=None, **kw):
+    arr = (B.MixkvPagedAttentionLayer * max(n, 1))()
+    for i in range(max(n, 1)):
+        arr[i] = B.MixkvPagedAttentionLayer(*{**dict(Q=0x1000, out=0x2000, selected=0x3000, n_selected=0x4000), **kw, **(second or {} if i else {})}.values())
+    return B.lib().mixkv_paged_attention(C.byref(p or _params()), _caches(max(n, 1)) if caches is None else caches, None if null else arr, n, most, rows, ws,
+                                         size, None)
+
+
 def test_struct_layouts():
     assert C.sizeof(B.MixkvPagedParams) == 10 * 4 and C.sizeof(B.MixkvPagedCache) == 5 * 8 and C.sizeof(B.MixkvPagedRows) == 10 * 8
     assert C.sizeof(B.MixkvRope) == 16 + 8 + 8 + 16
+    assert C.sizeof(B.MixkvPagedSelectLayer) == 3 * 8 and C.sizeof(B.MixkvPagedAttentionLayer) == 4 * 8
 
 
 @pytest.mark.parametrize("kw,size", [(dict(), 64 * 128 * 5 // 8), (dict(head_dim=64, page_rows=32), 32 * 64 * 5 // 8),
@@ -56,7 +73,7 @@ def test_page_bytes(kw, size):
                                        (dict(dtype="f32"), UNSUPPORTED),                       # 4-bit pages of fp32 rows
                                        (dict(batch=0), INVALID), (dict(n_q_heads=30), INVALID), (dict(n_kv_heads=0), INVALID),
                                        (dict(max_pages=0), INVALID), (dict(n_pages=0), INVALID), (dict(max_pages=1 << 25), UNSUPPORTED),
-                                       (dict(batch=1 << 20), UNSUPPORTED),
+                                       (dict(batch=1 << 14), UNSUPPORTED),
                                        (dict(softmax_scale=0.0), INVALID), (dict(softmax_scale=float("nan")), INVALID),
                                        (dict(softmax_scale=float("inf")), INVALID), (dict(softmax_scale=-1.0), INVALID)])
 def test_bad_params_are_rejected_everywhere(kw, status):
@@ -66,6 +83,11 @@ def test_bad_params_are_rejected_everywhere(kw, status):
     assert e.value.status == status
     assert L.mixkv_paged_append(C.byref(p), _caches(), _rows(), 1, None, 10, 1, None) == status
     assert L.mixkv_paged_read(C.byref(p), _caches(), _rows(), 1, 10, 1, None) == status
+    assert _select(p=p) == _attend(p=p) == status
+    for size in (lambda: B.mixkv_paged_select_workspace_size(p, 1), lambda: B.mixkv_paged_attention_workspace_size(p, 1, 100)):
+        with pytest.raises(B.MixkvError) as e:
+            size()
+        assert e.value.status == status
 
 
 @pytest.mark.parametrize("field,value", [("dtype", 2), ("format", 2), ("format", -1)])
@@ -118,3 +140,41 @@ def test_bad_sizes_are_rejected():
     assert L.mixkv_paged_read(p, _caches(), None, 1, 10, 1, None) == INVALID
     same = _rows(V=0x100000)
     assert L.mixkv_paged_read(p, _caches(), same, 1, 10, 1, None) == INVALID
+
+
+@pytest.mark.parametrize("kw", [dict(Q=0), dict(Q=0x1008), dict(selected=0), dict(n_selected=0), dict(selected=0x2002), dict(n=0), dict(n=129), dict(null=True),
+                                dict(keep=0), dict(keep=-1), dict(first=-1), dict(last=-1), dict(first=5, last=4), dict(first=2 ** 31 - 1, last=2 ** 31 - 1),
+                                dict(ws=0), dict(ws=0x900010), dict(caches=_caches(K_bounds=0)), dict(caches=_caches(page_table=0))])
+def test_bad_selections_are_rejected(kw):
+    assert _select(**kw) == INVALID
+
+
+@pytest.mark.parametrize("kw", [dict(Q=0), dict(Q=0x1008), dict(out=0), dict(out=0x2004), dict(selected=0), dict(n_selected=0), dict(selected=0x3001),
+                                dict(n=0), dict(n=129), dict(null=True), dict(most=0), dict(most=1 << 25), dict(rows=0), dict(rows=-1),
+                                dict(n=2, second=dict(selected=0, n_selected=0)), dict(caches=_caches(K_pages=0)), dict(caches=_caches(lengths=0))])
+def test_bad_attention_arguments_are_rejected(kw):
+    assert _attend(**kw) == INVALID
+
+
+def test_workspaces():
+    p = _params(max_pages=4096, n_pages=9000)
+    n = B.mixkv_paged_select_workspace_size(p, 3)
+    assert n % 256 == 0 and n >= 3 * 2 * 4 * 4096 * 4
+    assert _select(p=p, n=3, size=n - 256) == B.MIXKV_ERR_WORKSPACE_TOO_SMALL
+    L, size = B.lib(), C.c_size_t(0)
+    assert L.mixkv_paged_select_workspace_size(C.byref(p), 0, C.byref(size)) == L.mixkv_paged_select_workspace_size(C.byref(p), 1, None) == INVALID
+    for n_layers, rows in ((0, 100), (1, 0), (129, 1)):
+        assert L.mixkv_paged_attention_workspace_size(C.byref(p), n_layers, rows, C.byref(size)) == INVALID
+    assert L.mixkv_paged_attention_workspace_size(C.byref(p), 1, 1, None) == INVALID
+    assert B.mixkv_paged_attention_workspace_size(p, 1, 32) == 0               # a tile is not split
+    n = B.mixkv_paged_attention_workspace_size(p, 1, 200000)
+    assert n % 256 == 0 and n > 0
+    assert _attend(p=p, rows=200000, size=n - 256) == B.MIXKV_ERR_WORKSPACE_TOO_SMALL
+    assert _attend(p=p, rows=200000, ws=0) == _attend(p=p, rows=200000, ws=0x900080) == INVALID
+    # rows beyond what the table holds do not count
+    assert B.mixkv_paged_attention_workspace_size(p, 1, 2 ** 31 - 1) == B.mixkv_paged_attention_workspace_size(p, 1, 4096 * 64)
+
+
+def test_launches_with_more_workgroups_than_a_grid_are_refused():
+    p = _params(batch=9000, max_pages=1 << 20, n_pages=1 << 20)
+    assert _attend(p=p, rows=1 << 26) == UNSUPPORTED
