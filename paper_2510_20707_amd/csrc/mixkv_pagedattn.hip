@@ -44,6 +44,9 @@ __device__ __forceinline__ void chunk_of(const AShape &a, int tiles, int ch, int
 }
 __device__ __forceinline__ int chunks_used(const AShape &a, int tiles) { return (int)min((int64_t)a.nchunks, ((int64_t)tiles + a.ctiles - 1) / a.ctiles); }
 
+// A weighted sum over its sum of weights; no rows give zeros, a NaN stays one.
+__device__ __forceinline__ float row_result(float acc, float tot) { return tot == 0.f ? 0.f : acc / tot; }
+
 // ------------------------------------------------------------------------------------------------
 // paged_plain_kernel: tiles of 32 rows as floats in LDS; 256 threads form the scores of up to 16 heads, then the weights, then the values.
 // ------------------------------------------------------------------------------------------------
@@ -140,9 +143,234 @@ __global__ __launch_bounds__(256) void paged_plain_kernel(PShape s, AShape a, At
       if (d == 0) { dst[D] = ms[g]; dst[D + 1] = ls[g]; }
       continue;
     }
-    const float res = ls[g] > 0.f ? o[j] / ls[g] : (ls[g] == 0.f ? 0.f : ls[g]);
+    const float res = row_result(o[j], ls[g]);
     if constexpr (EB == 2) reinterpret_cast<uint16_t *>(l.out)[(q0 + g) * D + d] = f32_to_bf16_rne(res);
     else reinterpret_cast<float *>(l.out)[(q0 + g) * D + d] = res;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// paged_q4_kernel (4-bit pages): a workgroup of four waves, every wave on 32-row tiles of its own.
+//   * An element is B + S u with u = 1 + code / 16, whose bits are those of 1.0 with the code on top of the mantissa: a shift and an
+//     and-or make two of them, in bf16 or fp16.
+//   * Scores: query heads on the output rows, keys on the columns of a 16 x 16 x 32 product for each group of 32 elements, on the u alone (exact
+//     in bf16, as the queries are); a lane then has one key and forms sum_g S_g acc_g + B_g sum(q_g) in fp32.  A key's words are stored in
+//     the order in which the lanes of a product want them, so they come from memory into the operand.
+//   * Weights as fp16 through the wave's LDS image (head, key): a lane holds two keys 16 rows apart, a word of the image.
+//   * Values: a word of a page holds eight rows' codes of one element, an operand of the second product; B + S u is formed by packed fp16
+//     multiply-adds with the strip's scales.  Fp16 rounds weights and values by 2^-11, an eighth of the output's own rounding; both are
+//     averaged over the rows.  The weights are relative to an offset that puts the largest near 2^8: fp16 then resolves weights down
+//     to 2^-32 of it.
+// ------------------------------------------------------------------------------------------------
+constexpr float kTopWeight = 8.f, kWeightLimit = 16384.f;     // log2 of the largest weight where an offset is chosen; where it moves
+
+template <int D>
+__global__ __launch_bounds__(256) void paged_q4_kernel(PShape s, AShape a, AttnTable tab, float *part, int64_t unit0) {
+  constexpr int NG = D / 32, NB = D / 16, NV = D / 64, H = kAttnHeads, W = 4;
+  constexpr int PROW = 20, VROW = 2 * NG + 1;                 // words of an image row of weights, 16-byte pieces of a strip's scales, padded
+  __shared__ float o_s[W][H][D];
+  __shared__ float m_s[W][H], l_s[W][H];
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int ch = blockIdx.x % a.nchunks, ug = blockIdx.x / a.nchunks, gc = ug % a.gchunks, ul = ug / a.gchunks;
+  const int layer = ul / s.units_per_layer, u = ul - layer * s.units_per_layer;
+  const int b = u / s.hkv, h = u - b * s.hkv, ng = min(H, s.G - gc * H);
+  const PCache c = tab.c[layer];
+  const AttnLayer l = tab.l[layer];
+  const int64_t q0 = (int64_t)b * s.hq + h * s.G + gc * H;   // first query row
+  // group of the words at place g' of a key row, and the queries in that order: lane (head, quad) holds elements 8 quad + e of the group
+  auto group_at = [](int pl) { return D == 128 ? (pl & 1) * 2 + (pl >> 1) : pl; };
+  u32x4 qf[NG];
+#pragma unroll
+  for (int pl = 0; pl < NG; ++pl)
+    qf[pl] = *reinterpret_cast<const u32x4 *>(l.Q + ((q0 + (l16 < ng ? l16 : 0)) * D + 32 * group_at(pl) + 8 * quad) * 2);
+  const int len = head_rows(s, c, u), tiles = head_tiles(s, a, c, l, u, len);
+  int t0, t1;
+  chunk_of(a, tiles, ch, t0, t1);
+  if (t0 >= t1 && ch > 0) return;
+#pragma unroll
+  for (int pl = 0; pl < NG; ++pl)
+    if (l16 >= ng) qf[pl] = u32x4{0u, 0u, 0u, 0u};           // heads past the group are zero rows
+  const int64_t codes = (int64_t)s.P * D / 2;                // bytes of codes in front of a page's scales
+  const float c2 = s.scale_log2e;
+
+  f32x4 qsum[NG], o[NB];
+  float nm[4] = {0.f, 0.f, 0.f, 0.f}, ls[4] = {0.f, 0.f, 0.f, 0.f};   // minus the offsets of heads 4 quad + i (0: none yet), sums of weights
+  bool has[4] = {false, false, false, false};
+  {
+    const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+#pragma unroll
+    for (int pl = 0; pl < NG; ++pl)
+      qsum[pl] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qf[pl]), ones, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+  }
+#pragma unroll
+  for (int i = 0; i < NB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  uint32_t *p_img = reinterpret_cast<uint32_t *>(o_s[wave]);           // the wave's own: weights, then the scales of its value strips
+  u32x4 *v_img = reinterpret_cast<u32x4 *>(p_img + H * PROW);
+  static_assert(H * PROW * 4 + 4 * VROW * 16 <= H * D * 4, "the images lie in the wave's share of the output");
+  bool fresh = true;                                           // some head has no offset yet
+
+  for (int first = t0 + wave; first < t1; first += 64 * W) {
+    // lane i: where the wave's i-th tile of the next 64 lies
+    const int mine = first + lane * W;
+    Tile x{0, 0, 0};
+    if (mine < t1) x = tile_at(s, a, c, l, u, len, mine);
+    const int x_page = max(x.page, 0), x_rows = x.row | (x.live << 8);
+    const int n = min((t1 - first + W - 1) / W, 64);
+
+    uint32_t kc[2][NG], ks[2][NG];
+    u32x4 vc[NV], vs;
+    auto load_keys = [&](int i) {
+      const char *p = c.K + (int64_t)__builtin_amdgcn_readlane(x_page, i) * s.page_bytes;
+      const int row = __builtin_amdgcn_readlane(x_rows, i) & 255;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int at = row + 16 * r + l16;
+        if constexpr (NG == 4) {
+          const u32x4 w = load_vec<true>(p + at * (D / 2) + quad * 16), z = load_vec<true>(p + codes + at * 16);
+#pragma unroll
+          for (int g = 0; g < 4; ++g) { kc[r][g] = w[g]; ks[r][g] = z[g]; }
+        } else {
+          const u32x2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(p + at * (D / 2) + quad * 8));
+          const u32x2 z = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(p + codes + at * 8));
+#pragma unroll
+          for (int g = 0; g < 2; ++g) { kc[r][g] = w[g]; ks[r][g] = z[g]; }
+        }
+      }
+    };
+    auto load_values = [&](int i) {
+      const char *p = c.V + (int64_t)__builtin_amdgcn_readlane(x_page, i) * s.page_bytes;
+      const int strip = (__builtin_amdgcn_readlane(x_rows, i) & 255) / 8 + quad;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) vc[j] = load_vec<true>(p + strip * (D * 4) + j * 256 + l16 * 16);
+      vs = load_vec<true>(p + codes + strip * (NG * 32) + (l16 & (2 * NG - 1)) * 16);
+    };
+    load_keys(0);
+    load_values(0);
+    for (int i = 0; i < n; ++i) {
+      const int live = __builtin_amdgcn_readlane(x_rows, i) >> 8;
+      // ---- scores of the keys l16 and 16 + l16 against the heads 4 quad + e
+      float x2[2][4];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x2[r][e] = 0.f;
+#pragma unroll
+        for (int pl = 0; pl < NG; ++pl) {
+          const uint32_t w = kc[r][pl];
+          u32x4 k;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) k[j] = ((j == 0 ? w << 3 : w >> (4 * j - 3)) & 0x00780078u) | 0x3f803f80u;
+          const f32x4 acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qf[pl]), __builtin_bit_cast(bf16x8, k),
+                                                                    f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+          const f16x2 sb = __builtin_bit_cast(f16x2, ks[r][pl]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x2[r][e] = fmaf((float)sb[1], qsum[pl][e], fmaf((float)sb[0], acc[e], x2[r][e]));
+        }
+      }
+      if (i + 1 < n) load_keys(i + 1);
+      if (live < 32) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x2[r][e] = 16 * r + l16 < live ? x2[r][e] : -INFINITY;
+      }
+      // ---- weights; the offsets move where a head has none yet or a weight leaves fp16's range
+      float p[2][4], top = 0.f;
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { p[r][e] = fast_exp2(fmaf(x2[r][e], c2, nm[e])); top = fmaxf(top, p[r][e]); }
+      if (fresh || __builtin_amdgcn_ballot_w64(!(top < kWeightLimit)) != 0) {
+        fresh = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float t = fmaxf(x2[0][e], x2[1][e]);
+#pragma unroll
+          for (int off = 1; off < 16; off <<= 1) t = fmaxf(t, __shfl_xor(t, off));
+          const float want = kTopWeight - t * c2;            // minus the offset that puts this tile's largest weight at 2^kTopWeight
+          if (t > -INFINITY && (!has[e] || want < nm[e])) {
+            const float f = has[e] ? fast_exp2(want - nm[e]) : 0.f;
+            nm[e] = want;
+            has[e] = true;
+            ls[e] *= f;
+#pragma unroll
+            for (int k = 0; k < NB; ++k) o[k][e] *= f;
+          }
+          fresh |= !has[e];
+#pragma unroll
+          for (int r = 0; r < 2; ++r) p[r][e] = fast_exp2(fmaf(x2[r][e], c2, nm[e]));
+        }
+        fresh = __builtin_amdgcn_ballot_w64(fresh) != 0;
+      }
+      // ---- images: weights (head, key pair), scales of the wave's strips; rows that do not exist get zeros
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        ls[e] += p[0][e] + p[1][e];
+        p_img[(4 * quad + e) * PROW + l16] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)p[0][e], (_Float16)p[1][e]});
+      }
+      if (live < 32) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          vs[k] &= (4 * quad + k < live ? 0xffffu : 0u) | (16 + 4 * quad + k < live ? 0xffff0000u : 0u);
+      }
+      if (l16 < 2 * NG) v_img[quad * VROW + l16] = vs;
+      wave_lds_fence();
+      const f16x8 pw = __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4 *>(p_img + l16 * PROW + 4 * quad));
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        const u32x4 st = v_img[quad * VROW + 2 * g], ba = v_img[quad * VROW + 2 * g + 1];
+#pragma unroll
+        for (int hb = 0; hb < 2; ++hb) {
+          const int blk = 2 * g + hb;
+          const uint32_t w = vc[blk >> 2][blk & 3];
+          u32x4 v;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t un = ((j < 2 ? w << (6 - 4 * j) : w >> (4 * j - 6)) & 0x03c003c0u) | 0x3c003c00u;
+            const f16x2 val = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, un), __builtin_bit_cast(f16x2, (uint32_t)st[j]),
+                                                        __builtin_bit_cast(f16x2, (uint32_t)ba[j]));
+            v[j] = __builtin_bit_cast(uint32_t, val);
+          }
+          o[blk] = __builtin_amdgcn_mfma_f32_16x16x32_f16(pw, __builtin_bit_cast(f16x8, v), o[blk], 0, 0, 0);
+        }
+      }
+      wave_lds_fence();
+      if (i + 1 < n) load_values(i + 1);
+    }
+  }
+
+  // ---- the waves' shares: offsets, sums over the 16 keys of a lane row, weighted values of head 4 quad + e, element 16 k + l16
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+#pragma unroll
+    for (int off = 1; off < 16; off <<= 1) ls[e] += __shfl_xor(ls[e], off);
+    if (l16 == 0) { m_s[wave][4 * quad + e] = has[e] ? -nm[e] : -INFINITY; l_s[wave][4 * quad + e] = ls[e]; }
+#pragma unroll
+    for (int k = 0; k < NB; ++k) o_s[wave][4 * quad + e][16 * k + l16] = o[k][e];
+  }
+  __syncthreads();
+  const bool whole = chunks_used(a, tiles) <= 1;
+  for (int idx = tid; idx < ng * D; idx += 256) {
+    const int g = idx / D, d = idx - g * D;
+    float mn = m_s[0][g];
+#pragma unroll
+    for (int w = 1; w < W; ++w) mn = fmaxf(mn, m_s[w][g]);
+    const float mu = mn == -INFINITY ? 0.f : mn;
+    float acc = 0.f, tot = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {                              // waves in order
+      const float f = fast_exp2(m_s[w][g] - mu);
+      acc = fmaf(o_s[w][g][d], f, acc);
+      tot = fmaf(l_s[w][g], f, tot);
+    }
+    if (!whole) {                                              // partial: weighted values, then (offset, sum)
+      float *dst = part + ((((unit0 + ul) * a.gchunks + gc) * a.nchunks + ch) * a.gt + g) * (D + 2);
+      dst[d] = acc;
+      if (d == 0) { dst[D] = mn; dst[D + 1] = tot; }
+      continue;
+    }
+    reinterpret_cast<uint16_t *>(l.out)[(q0 + g) * D + d] = f32_to_bf16_rne(row_result(acc, tot));
   }
 }
 
@@ -170,7 +398,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PShape s, AShape a, At
     acc = fmaf(src[i * step + d], f, acc);
     tot = fmaf(src[i * step + D + 1], f, tot);
   }
-  const float res = tot > 0.f ? acc / tot : (tot == 0.f ? 0.f : tot);
+  const float res = row_result(acc, tot);
   const int64_t at = ((int64_t)b * s.hq + h * s.G + gc * kAttnHeads + g) * D + d;
   if constexpr (DT == MIXKV_BF16) reinterpret_cast<uint16_t *>(l.out)[at] = f32_to_bf16_rne(res);
   else reinterpret_cast<float *>(l.out)[at] = res;
@@ -254,7 +482,7 @@ extern "C" mixkv_status mixkv_paged_attention(const mixkv_paged_params *params, 
         hipLaunchKernelGGL(merge, dim3((unsigned)groups, (unsigned)((a.gt * s.D + 255) / 256)), dim3(256), 0, stream, s, a, t, (const float *)part, unit0);
     };
     constexpr int B16 = MIXKV_BF16, F32 = MIXKV_F32;
-    if (s.q4) { if (s.D == 128) go(paged_plain_kernel<B16, 128, true>, paged_merge_kernel<B16, 128>); else go(paged_plain_kernel<B16, 64, true>, paged_merge_kernel<B16, 64>); }
+    if (s.q4) { if (s.D == 128) go(paged_q4_kernel<128>, paged_merge_kernel<B16, 128>); else go(paged_q4_kernel<64>, paged_merge_kernel<B16, 64>); }
     else if (params->dtype == B16) { if (s.D == 128) go(paged_plain_kernel<B16, 128, false>, paged_merge_kernel<B16, 128>); else go(paged_plain_kernel<B16, 64, false>, paged_merge_kernel<B16, 64>); }
     else { if (s.D == 128) go(paged_plain_kernel<F32, 128, false>, paged_merge_kernel<F32, 128>); else go(paged_plain_kernel<F32, 64, false>, paged_merge_kernel<F32, 64>); }
     if (hipGetLastError() != hipSuccess) return MIXKV_ERR_HIP;
