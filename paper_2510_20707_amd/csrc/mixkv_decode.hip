@@ -425,12 +425,6 @@ __global__ __launch_bounds__(D * 2, 2) void decode_mfma_kernel(DShape s, DecodeT
 // workgroups per compute unit (three spill, and were 5 % slower).
 // ------------------------------------------------------------------------------------------------
 constexpr int kDecWaveHeads = 16, kDecWaveThreads = 256;
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((__vector_size__(16)));
-
-// Rotation of the 16-byte pieces of a row in a value image: a transposed read takes two pieces of four neighbouring rows.
-template <int D>
-__device__ __forceinline__ int value_swz(int r) { return D == 128 ? (2 * r) & 15 : r & 6; }
 
 template <int D>
 __global__ __launch_bounds__(kDecWaveThreads, 2) void decode_wave_kernel(DShape s, DecodeTable tab, float *part) {

@@ -47,104 +47,33 @@ __device__ __forceinline__ int chunks_used(const AShape &a, int tiles) { return 
 // A weighted sum over its sum of weights; no rows give zeros, a NaN stays one.
 __device__ __forceinline__ float row_result(float acc, float tot) { return tot == 0.f ? 0.f : acc / tot; }
 
-// ------------------------------------------------------------------------------------------------
-// paged_plain_kernel: tiles of 32 rows as floats in LDS; 256 threads form the scores of up to 16 heads, then the weights, then the values.
-// ------------------------------------------------------------------------------------------------
-template <int DT, int D, bool Q4>
-__global__ __launch_bounds__(256) void paged_plain_kernel(PShape s, AShape a, AttnTable tab, float *part, int64_t unit0) {
-  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, H = kAttnHeads, NG = D / 32;
-  __shared__ float kt[32][D + 1], vt[32][D], qs[H][D + 1], ws[H][33], ms[H], ls[H], fs[H];
-  const int tid = threadIdx.x;
-  const int ch = blockIdx.x % a.nchunks, ug = blockIdx.x / a.nchunks, gc = ug % a.gchunks, ul = ug / a.gchunks;
-  const int layer = ul / s.units_per_layer, u = ul - layer * s.units_per_layer;
-  const int b = u / s.hkv, h = u - b * s.hkv, ng = min(H, s.G - gc * H);
-  const PCache c = tab.c[layer];
-  const AttnLayer l = tab.l[layer];
-  const int len = head_rows(s, c, u), tiles = head_tiles(s, a, c, l, u, len);
-  int t0, t1;
-  chunk_of(a, tiles, ch, t0, t1);
-  if (t0 >= t1 && ch > 0) return;
-  const int64_t q0 = (int64_t)b * s.hq + h * s.G + gc * H;           // first query row
-  auto value = [&](const char *p, int64_t i) -> float {
-    if constexpr (DT == MIXKV_BF16) return __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(p)[i] << 16);
-    else return reinterpret_cast<const float *>(p)[i];
-  };
-  for (int i = tid; i < H * D; i += 256) {
-    const int g = i / D, d = i - g * D;
-    qs[g][d] = g < ng ? value(l.Q, (q0 + g) * D + d) : 0.f;
-  }
-  if (tid < H) { ms[tid] = -INFINITY; ls[tid] = 0.f; }
-  constexpr int OWN = H * D / 256;
-  float o[OWN] = {};
-  for (int t = t0; t < t1; ++t) {
-    const Tile x = tile_at(s, a, c, l, u, len, t);
-    const char *kp = c.K + (int64_t)max(x.page, 0) * s.page_bytes, *vp = c.V + (int64_t)max(x.page, 0) * s.page_bytes;
-    const int64_t codes = (int64_t)s.P * D / 2;
-    __syncthreads();
-    for (int i = tid; i < 32 * D; i += 256) {
-      const int rr = i / D, d = i - rr * D, r = x.row + rr;
-      float k = 0.f, v = 0.f;
-      if (rr < x.live) {
-        if constexpr (Q4) {
-          const int g = d >> 5, pl = D == 128 ? (g & 1) * 2 + (g >> 1) : g;
-          const uint32_t kw = reinterpret_cast<const uint32_t *>(kp)[r * (D / 8) + ((d & 31) >> 3) * NG + pl];
-          const uint16_t *ks = reinterpret_cast<const uint16_t *>(kp + codes) + 2 * (r * NG + pl);
-          k = code_value((kw >> code_shift(d & 7)) & 15u, f16_value(ks[0]), f16_value(ks[1]));
-          const int strip = (r >> 5) * 4 + ((r & 15) >> 2), e = 2 * (r & 3) + ((r >> 4) & 1);
-          const uint32_t vw = reinterpret_cast<const uint32_t *>(vp)[strip * D + (d >> 6) * 64 + (d & 15) * 4 + ((d >> 4) & 3)];
-          const uint16_t *vs = reinterpret_cast<const uint16_t *>(vp + codes) + (strip * NG + g) * 16 + e;
-          v = code_value((vw >> code_shift(e)) & 15u, f16_value(vs[0]), f16_value(vs[8]));
-        } else {
-          k = value(kp, (int64_t)r * D + d);
-          v = value(vp, (int64_t)r * D + d);
-        }
-      }
-      kt[rr][d] = k; vt[rr][d] = v;
-    }
-    __syncthreads();
-    for (int i = tid; i < H * 32; i += 256) {
-      const int g = i >> 5, rr = i & 31;
-      float x2 = 0.f;
-      for (int d = 0; d < D; ++d) x2 = fmaf(qs[g][d], kt[rr][d], x2);
-      ws[g][rr] = rr < x.live ? x2 * s.scale_log2e : -INFINITY;
-    }
-    __syncthreads();
-    if (tid < H) {
-      float m = ms[tid], sum = 0.f;
-      for (int rr = 0; rr < 32; ++rr) m = fmaxf(m, ws[tid][rr]);
-      const float mu = m == -INFINITY ? 0.f : m;
-      for (int rr = 0; rr < 32; ++rr) {
-        const float p = fast_exp2(ws[tid][rr] - mu);
-        ws[tid][rr] = p;
-        sum += p;
-      }
-      fs[tid] = fast_exp2(ms[tid] - mu);
-      ls[tid] = ls[tid] * fs[tid] + sum;
-      ms[tid] = m;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < OWN; ++j) {
-      const int i = tid + 256 * j, g = i / D, d = i - g * D;
-      float acc = o[j] * fs[g];
-      for (int rr = 0; rr < 32; ++rr) acc = fmaf(ws[g][rr], vt[rr][d], acc);
-      o[j] = acc;
-    }
-  }
+// The workgroup's end: folds the waves' shares in order (o_s of head g holds element d at d ^ g) and writes the rows, or the chunk's partial: the
+// weighted values, then offset and sum.
+template <int DT, int D>
+__device__ __forceinline__ void finish_chunk(const PShape &s, const AShape &a, const AttnLayer &l, float (&o_s)[4][kAttnHeads][D], float (&m_s)[4][kAttnHeads],
+                                             float (&l_s)[4][kAttnHeads], float *part, int64_t slot, int64_t q0, int ng, bool whole) {
   __syncthreads();
-  const bool whole = chunks_used(a, tiles) <= 1;
+  for (int idx = threadIdx.x; idx < ng * D; idx += 256) {
+    const int g = idx / D, d = idx - g * D;
+    float mn = m_s[0][g];
 #pragma unroll
-  for (int j = 0; j < OWN; ++j) {
-    const int i = tid + 256 * j, g = i / D, d = i - g * D;
-    if (g >= ng) continue;
+    for (int w = 1; w < 4; ++w) mn = fmaxf(mn, m_s[w][g]);
+    const float mu = mn == -INFINITY ? 0.f : mn;
+    float acc = 0.f, tot = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = fast_exp2(m_s[w][g] - mu);
+      acc = fmaf(o_s[w][g][d ^ g], f, acc);
+      tot = fmaf(l_s[w][g], f, tot);
+    }
     if (!whole) {
-      float *dst = part + ((((unit0 + ul) * a.gchunks + gc) * a.nchunks + ch) * a.gt + g) * (D + 2);
-      dst[d] = o[j];
-      if (d == 0) { dst[D] = ms[g]; dst[D + 1] = ls[g]; }
+      float *dst = part + (slot + g) * (D + 2);
+      dst[d] = acc;
+      if (d == 0) { dst[D] = mn; dst[D + 1] = tot; }
       continue;
     }
-    const float res = row_result(o[j], ls[g]);
-    if constexpr (EB == 2) reinterpret_cast<uint16_t *>(l.out)[(q0 + g) * D + d] = f32_to_bf16_rne(res);
+    const float res = row_result(acc, tot);
+    if constexpr (DT == MIXKV_BF16) reinterpret_cast<uint16_t *>(l.out)[(q0 + g) * D + d] = f32_to_bf16_rne(res);
     else reinterpret_cast<float *>(l.out)[(q0 + g) * D + d] = res;
   }
 }
@@ -347,31 +276,177 @@ __global__ __launch_bounds__(256) void paged_q4_kernel(PShape s, AShape a, AttnT
     for (int off = 1; off < 16; off <<= 1) ls[e] += __shfl_xor(ls[e], off);
     if (l16 == 0) { m_s[wave][4 * quad + e] = has[e] ? -nm[e] : -INFINITY; l_s[wave][4 * quad + e] = ls[e]; }
 #pragma unroll
-    for (int k = 0; k < NB; ++k) o_s[wave][4 * quad + e][16 * k + l16] = o[k][e];
+    for (int k = 0; k < NB; ++k) o_s[wave][4 * quad + e][(16 * k + l16) ^ (4 * quad + e)] = o[k][e];
   }
-  __syncthreads();
-  const bool whole = chunks_used(a, tiles) <= 1;
-  for (int idx = tid; idx < ng * D; idx += 256) {
-    const int g = idx / D, d = idx - g * D;
-    float mn = m_s[0][g];
+  finish_chunk<MIXKV_BF16, D>(s, a, l, o_s, m_s, l_s, part, (((unit0 + ul) * a.gchunks + gc) * a.nchunks + ch) * a.gt, q0, ng, chunks_used(a, tiles) <= 1);
+}
+
+// ------------------------------------------------------------------------------------------------
+// paged_rows_kernel (full-precision pages): a workgroup of four waves, every wave on 32-row tiles of its own; keys come from memory into the
+// operand of the first product (lane (key, quad): every fourth 16-byte piece of its row), keys on the output rows, so that a lane (head,
+// quad) has its weights in the order in which they are the operand of the second.
+//   bf16  weights as a bf16 head and remainder; values through the wave's LDS image, read transposed.
+//   fp32  products of four elements' contraction; a lane takes four neighbouring elements of a value row at a time, which are four blocks'
+//         operands, the blocks' rows then being every fourth element: no image.
+// Offsets as in decode_mfma_kernel.
+// ------------------------------------------------------------------------------------------------
+template <int DT, int D>
+__global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, AttnTable tab, float *part, int64_t unit0) {
+  constexpr bool F32 = DT == MIXKV_F32;
+  constexpr int EB = F32 ? 4 : 2, RB = D * EB, PPR = RB / 16, NC = PPR / 4, NB = D / 16, H = kAttnHeads, W = 4;
+  constexpr int NV = F32 ? 8 * (D / 64) : 32 * PPR / 64, RPL = 64 / PPR;     // 16-byte loads of a lane for a tile of values
+  __shared__ float o_s[W][H][D];
+  __shared__ float m_s[W][H], l_s[W][H];
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int ch = blockIdx.x % a.nchunks, ug = blockIdx.x / a.nchunks, gc = ug % a.gchunks, ul = ug / a.gchunks;
+  const int layer = ul / s.units_per_layer, u = ul - layer * s.units_per_layer;
+  const int b = u / s.hkv, h = u - b * s.hkv, ng = min(H, s.G - gc * H);
+  const PCache c = tab.c[layer];
+  const AttnLayer l = tab.l[layer];
+  const int64_t q0 = (int64_t)b * s.hq + h * s.G + gc * H;   // first query row
+  u32x4 qf[NC];
 #pragma unroll
-    for (int w = 1; w < W; ++w) mn = fmaxf(mn, m_s[w][g]);
-    const float mu = mn == -INFINITY ? 0.f : mn;
-    float acc = 0.f, tot = 0.f;
+  for (int k = 0; k < NC; ++k) qf[k] = *reinterpret_cast<const u32x4 *>(l.Q + (q0 + (l16 < ng ? l16 : 0)) * RB + (4 * k + quad) * 16);
+  const int len = head_rows(s, c, u), tiles = head_tiles(s, a, c, l, u, len);
+  int t0, t1;
+  chunk_of(a, tiles, ch, t0, t1);
+  if (t0 >= t1 && ch > 0) return;
 #pragma unroll
-    for (int w = 0; w < W; ++w) {                              // waves in order
-      const float f = fast_exp2(m_s[w][g] - mu);
-      acc = fmaf(o_s[w][g][d], f, acc);
-      tot = fmaf(l_s[w][g], f, tot);
+  for (int k = 0; k < NC; ++k)
+    if (l16 >= ng) qf[k] = u32x4{0u, 0u, 0u, 0u};              // heads past the group are zero columns
+  const float c2 = s.scale_log2e;
+  float m = -INFINITY, sum = 0.f;                              // the head's offset, this lane's share of its sum of weights
+  f32x4 o[NB];
+#pragma unroll
+  for (int k = 0; k < NB; ++k) o[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+  char *img = reinterpret_cast<char *>(o_s[wave]);             // bf16: a tile of values, 32 rows
+  static_assert(F32 || 32 * RB <= H * D * 4, "the image lies in the wave's share of the output");
+  const uint32_t img_a = (uint32_t)(uintptr_t)(lds_void_t *)img;
+
+  for (int first = t0 + wave; first < t1; first += 64 * W) {
+    const int mine = first + lane * W;                         // lane i: where the wave's i-th tile of the next 64 lies
+    Tile x{0, 0, 0};
+    if (mine < t1) x = tile_at(s, a, c, l, u, len, mine);
+    const int x_page = max(x.page, 0), x_rows = x.row | (x.live << 8);
+    const int n = min((t1 - first + W - 1) / W, 64);
+    u32x4 kr[2][NC], vr[NV];
+    auto tile_of = [&](const char *pool, int i) {
+      return pool + (int64_t)__builtin_amdgcn_readlane(x_page, i) * s.page_bytes + (__builtin_amdgcn_readlane(x_rows, i) & 255) * RB;
+    };
+    auto load_keys = [&](int i) {
+      const char *p = tile_of(c.K, i) + l16 * RB + quad * 16;
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int k = 0; k < NC; ++k) kr[r][k] = load_vec<true>(p + r * 16 * RB + k * 64);
+    };
+    // value load j of a lane: bf16: piece lane % PPR of row RPL j + lane / PPR; fp32: elements 64 (j / 8) + 4 l16 + ... of row
+    // 16 (j / 4 % 2) + 4 quad + j % 4
+    auto value_row = [&](int j) { return F32 ? 16 * ((j >> 2) & 1) + 4 * quad + (j & 3) : RPL * j + lane / PPR; };
+    auto load_values = [&](int i) {
+      const char *p = tile_of(c.V, i);
+      const int live = __builtin_amdgcn_readlane(x_rows, i) >> 8;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const char *at = p + value_row(j) * RB + (F32 ? (j >> 3) * 256 + l16 * 16 : (lane % PPR) * 16);
+        if (live == 32) vr[j] = load_vec<true>(at);
+        else vr[j] = value_row(j) < live ? load_vec<true>(at) : u32x4{0u, 0u, 0u, 0u};   // rows that do not exist: zeros
+      }
+    };
+    load_keys(0);
+    load_values(0);
+    for (int i = 0; i < n; ++i) {
+      const int live = __builtin_amdgcn_readlane(x_rows, i) >> 8;
+      f32x4 acc[2];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+          if constexpr (F32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              acc[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[r][k][e]), __uint_as_float(qf[k][e]), acc[r], 0, 0, 0);
+          } else {
+            acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[r][k]), __builtin_bit_cast(bf16x8, qf[k]), acc[r], 0, 0, 0);
+          }
+        }
+      }
+      if (i + 1 < n) load_keys(i + 1);
+      float x8[8], p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float v = e < 4 ? acc[0][e & 3] : acc[1][e & 3];
+        x8[e] = 16 * (e >> 2) + 4 * quad + (e & 3) < live ? v : -INFINITY;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = fast_exp2(fmaf(x8[e], c2, -m));
+      float next = sum + (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])));
+      if (__builtin_amdgcn_ballot_w64(!(next < kSumLimit)) != 0) {
+        float t = fmaxf(fmaxf(fmaxf(x8[0], x8[1]), fmaxf(x8[2], x8[3])), fmaxf(fmaxf(x8[4], x8[5]), fmaxf(x8[6], x8[7])));
+        t = fmaxf(t, __shfl_xor(t, 16));
+        t = fmaxf(t, __shfl_xor(t, 32));
+        const float mn = fmaxf(m, t * c2), mu = mn == -INFINITY ? 0.f : mn;
+        const float f = fast_exp2(m - mu);                     // 0 while there is no offset yet
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = fast_exp2(fmaf(x8[e], c2, -mu));
+        next = sum * f + (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])));
+#pragma unroll
+        for (int k = 0; k < NB; ++k) o[k] *= f;
+        m = mn;
+      }
+      sum = next;
+      if constexpr (F32) {
+#pragma unroll
+        for (int k = 0; k < NB; ++k)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)                          // block k: elements 64 (k / 4) + 4 i + k % 4
+            o[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[(k >> 2) * 8 + e][k & 3]), p[e], o[k], 0, 0, 0);
+        if (i + 1 < n) load_values(i + 1);
+      } else {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          const int row = value_row(j);
+          reinterpret_cast<u32x4 *>(img)[row * PPR + ((lane % PPR) ^ value_swz<D>(row))] = vr[j];
+        }
+        if (i + 1 < n) load_values(i + 1);
+        wave_lds_fence();
+        bf16x8 ph, pl;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const __bf16 hi = (__bf16)p[e];
+          ph[e] = hi;
+          pl[e] = (__bf16)(p[e] - (float)hi);
+        }
+        const uint32_t r0 = 4 * quad + (l16 >> 2);             // rows 4 quad ... and 16 + 4 quad ... of block k of 16 elements
+#pragma unroll
+        for (int k = 0; k < NB; ++k) {
+          uint32_t at[2];
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+            at[r] = img_a + (r0 + 16 * r) * RB + ((2 * k + ((l16 & 3) >> 1)) ^ value_swz<D>(r0 + 16 * r)) * 16 + (l16 & 1) * 8;
+          const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)at[0]);
+          const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)at[1]);
+          const bf16x8 vv = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+          o[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, ph, o[k], 0, 0, 0);
+          o[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, pl, o[k], 0, 0, 0);
+        }
+        wave_lds_fence();
+      }
     }
-    if (!whole) {                                              // partial: weighted values, then (offset, sum)
-      float *dst = part + ((((unit0 + ul) * a.gchunks + gc) * a.nchunks + ch) * a.gt + g) * (D + 2);
-      dst[d] = acc;
-      if (d == 0) { dst[D] = mn; dst[D + 1] = tot; }
-      continue;
-    }
-    reinterpret_cast<uint16_t *>(l.out)[(q0 + g) * D + d] = f32_to_bf16_rne(row_result(acc, tot));
   }
+
+  // ---- the waves' shares: lane (head, quad) has rows 4 quad + e of every block
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  if (quad == 0) { m_s[wave][l16] = m; l_s[wave][l16] = sum; }
+#pragma unroll
+  for (int k = 0; k < NB; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      o_s[wave][l16][(F32 ? 64 * (k >> 2) + 4 * (4 * quad + e) + (k & 3) : 16 * k + 4 * quad + e) ^ l16] = o[k][e];
+  finish_chunk<DT, D>(s, a, l, o_s, m_s, l_s, part, (((unit0 + ul) * a.gchunks + gc) * a.nchunks + ch) * a.gt, q0, ng, chunks_used(a, tiles) <= 1);
 }
 
 // Folds the chunks of one (unit, group of query heads), in order: a thread per output element.
@@ -483,8 +558,8 @@ extern "C" mixkv_status mixkv_paged_attention(const mixkv_paged_params *params, 
     };
     constexpr int B16 = MIXKV_BF16, F32 = MIXKV_F32;
     if (s.q4) { if (s.D == 128) go(paged_q4_kernel<128>, paged_merge_kernel<B16, 128>); else go(paged_q4_kernel<64>, paged_merge_kernel<B16, 64>); }
-    else if (params->dtype == B16) { if (s.D == 128) go(paged_plain_kernel<B16, 128, false>, paged_merge_kernel<B16, 128>); else go(paged_plain_kernel<B16, 64, false>, paged_merge_kernel<B16, 64>); }
-    else { if (s.D == 128) go(paged_plain_kernel<F32, 128, false>, paged_merge_kernel<F32, 128>); else go(paged_plain_kernel<F32, 64, false>, paged_merge_kernel<F32, 64>); }
+    else if (params->dtype == B16) { if (s.D == 128) go(paged_rows_kernel<B16, 128>, paged_merge_kernel<B16, 128>); else go(paged_rows_kernel<B16, 64>, paged_merge_kernel<B16, 64>); }
+    else { if (s.D == 128) go(paged_rows_kernel<F32, 128>, paged_merge_kernel<F32, 128>); else go(paged_rows_kernel<F32, 64>, paged_merge_kernel<F32, 64>); }
     if (hipGetLastError() != hipSuccess) return MIXKV_ERR_HIP;
   }
   return MIXKV_OK;

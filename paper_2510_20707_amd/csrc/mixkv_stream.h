@@ -151,6 +151,12 @@ __device__ __forceinline__ u32x4 load_vec(const void *p) {
 // order, so this holds the compiler only and costs no instruction.
 __device__ __forceinline__ void wave_lds_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local"); }
 
+// Rotation of the 16-byte pieces of a row in a value image: a transposed read takes two pieces of four neighbouring rows.
+template <int D>
+__device__ __forceinline__ int value_swz(int r) { return D == 128 ? (2 * r) & 15 : r & 6; }
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((__vector_size__(16)));
 typedef __attribute__((address_space(3))) void lds_void_t;
 typedef short s16x4 __attribute__((__vector_size__(8)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
