@@ -91,13 +91,18 @@ __device__ __forceinline__ void finish_chunk(const PShape &s, const AShape &a, c
 //     averaged over the rows.  The weights are relative to an offset that puts the largest near 2^8: fp16 then resolves weights down
 //     to 2^-32 of it.
 // ------------------------------------------------------------------------------------------------
+constexpr int kQ4Ring = 3, kQ4Waves = 2;
 constexpr float kTopWeight = 8.f, kWeightLimit = 16384.f;     // log2 of the largest weight where an offset is chosen; where it moves
 
 template <int D>
-__global__ __launch_bounds__(256) void paged_q4_kernel(PShape s, AShape a, AttnTable tab, float *part, int64_t unit0) {
-  constexpr int NG = D / 32, NB = D / 16, NV = D / 64, H = kAttnHeads, W = 4;
-  constexpr int PROW = 20, VROW = 2 * NG + 1;                 // words of an image row of weights, 16-byte pieces of a strip's scales, padded
-  __shared__ float o_s[W][H][D];
+__global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShape a, AttnTable tab, float *part, int64_t unit0) {
+  constexpr int NG = D / 32, NB = D / 16, H = kAttnHeads, W = 4;
+  constexpr int CODES = 16 * D, SCALES = 32 * NG * 4, TILE = 2 * (CODES + SCALES);   // bytes of a tile: keys' codes, values', keys' scales, values'
+  constexpr int NL = CODES / 1024, LOADS = 2 * NL + 1, RING = kQ4Ring;
+  constexpr int PROW = 20;                                    // words of an image row of weights, padded
+  struct Share { float o[W][H][D]; };
+  struct Work { uint4 ring[W * RING * TILE / 16]; uint32_t p[W][H * PROW]; };
+  __shared__ union { Share share; Work work; } sh;
   __shared__ float m_s[W][H], l_s[W][H];
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -120,8 +125,12 @@ __global__ __launch_bounds__(256) void paged_q4_kernel(PShape s, AShape a, AttnT
 #pragma unroll
   for (int pl = 0; pl < NG; ++pl)
     if (l16 >= ng) qf[pl] = u32x4{0u, 0u, 0u, 0u};           // heads past the group are zero rows
-  const int64_t codes = (int64_t)s.P * D / 2;                // bytes of codes in front of a page's scales
+  const int codes = s.P * D / 2;                             // bytes of codes in front of a page's scales
   const float c2 = s.scale_log2e;
+  // an and-or takes one constant from a scalar register or the instruction; the other one lives in a vector register
+  uint32_t one_bf16, one_f16;
+  asm("v_mov_b32 %0, 0x3f803f80" : "=v"(one_bf16));
+  asm("v_mov_b32 %0, 0x3c003c00" : "=v"(one_f16));
 
   f32x4 qsum[NG], o[NB];
   float nm[4] = {0.f, 0.f, 0.f, 0.f}, ls[4] = {0.f, 0.f, 0.f, 0.f};   // minus the offsets of heads 4 quad + i (0: none yet), sums of weights
@@ -134,9 +143,16 @@ __global__ __launch_bounds__(256) void paged_q4_kernel(PShape s, AShape a, AttnT
   }
 #pragma unroll
   for (int i = 0; i < NB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  uint32_t *p_img = reinterpret_cast<uint32_t *>(o_s[wave]);           // the wave's own: weights, then the scales of its value strips
-  u32x4 *v_img = reinterpret_cast<u32x4 *>(p_img + H * PROW);
-  static_assert(H * PROW * 4 + 4 * VROW * 16 <= H * D * 4, "the images lie in the wave's share of the output");
+  const char *ring = reinterpret_cast<const char *>(sh.work.ring) + wave * (RING * TILE);
+  const uint32_t ring_a = lds_base_of(sh.work.ring) + wave * (RING * TILE);
+  uint32_t *p_img = sh.work.p[wave];
+  // what the lane fetches of a tile: a key row's four pieces lie rotated in the image by the row's number, so that 16 rows are read at once
+  // without conflict; the scales' 16-byte pieces are the keys' in the first half of the load, the values' in the second
+  constexpr int PPR = D / 32;                                 // 16-byte pieces of a key row's codes
+  const int krow = lane / PPR, kpiece = D == 128 ? (lane & 3) ^ ((krow >> 2) & 3) : lane % PPR;
+  const uint32_t k_off = krow * (D / 2) + kpiece * 16;
+  const bool s_keys = lane < SCALES / 16;
+  const uint32_t s_off = codes + (s_keys ? lane : lane - SCALES / 16) * 16;
   bool fresh = true;                                           // some head has no offset yet
 
   for (int first = t0 + wave; first < t1; first += 64 * W) {
@@ -146,58 +162,69 @@ __global__ __launch_bounds__(256) void paged_q4_kernel(PShape s, AShape a, AttnT
     if (mine < t1) x = tile_at(s, a, c, l, u, len, mine);
     const int x_page = max(x.page, 0), x_rows = x.row | (x.live << 8);
     const int n = min((t1 - first + W - 1) / W, 64);
-
-    uint32_t kc[2][NG], ks[2][NG];
-    u32x4 vc[NV], vs;
-    auto load_keys = [&](int i) {
-      const char *p = c.K + (int64_t)__builtin_amdgcn_readlane(x_page, i) * s.page_bytes;
+    // tile i into its image
+    auto request = [&](int i, uint32_t img) {
+      const int64_t page = (int64_t)__builtin_amdgcn_readlane(x_page, i) * s.page_bytes;
       const int row = __builtin_amdgcn_readlane(x_rows, i) & 255;
+      const char *kp = c.K + page, *vp = c.V + page;
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int at = row + 16 * r + l16;
-        if constexpr (NG == 4) {
-          const u32x4 w = load_vec<true>(p + at * (D / 2) + quad * 16), z = load_vec<true>(p + codes + at * 16);
+      for (int j = 0; j < NL; ++j) load_to_lds<true>(kp + (uint32_t)(row * (D / 2)) + (k_off + j * 1024), img + j * 1024);
 #pragma unroll
-          for (int g = 0; g < 4; ++g) { kc[r][g] = w[g]; ks[r][g] = z[g]; }
+      for (int j = 0; j < NL; ++j) load_to_lds<true>(vp + (uint32_t)(row * (D / 2)) + (uint32_t)(lane * 16 + j * 1024), img + CODES + j * 1024);
+      const char *sp = (s_keys ? kp : vp) + (uint32_t)(row * NG * 4) + s_off;
+      if (2 * SCALES / 16 == 64 || lane < 2 * SCALES / 16) load_to_lds<true>(sp, img + 2 * CODES);
+    };
+    wait_vm<0>();                                              // the loop counts its own requests
+#pragma unroll
+    for (int i = 0; i < RING - 1; ++i)
+      if (i < n) request(i, ring_a + i * TILE);
+    int slot = 0;
+    for (int i = 0; i < n; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      {
+        const int to = slot == 0 ? RING - 1 : slot - 1;        // the image that tile i - 1 has left
+        if (i + RING - 1 < n) {
+          request(i + RING - 1, ring_a + to * TILE);
+          wait_vm<(RING - 1) * LOADS>();
         } else {
-          const u32x2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(p + at * (D / 2) + quad * 8));
-          const u32x2 z = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(p + codes + at * 8));
-#pragma unroll
-          for (int g = 0; g < 2; ++g) { kc[r][g] = w[g]; ks[r][g] = z[g]; }
+          wait_vm<0>();
         }
       }
-    };
-    auto load_values = [&](int i) {
-      const char *p = c.V + (int64_t)__builtin_amdgcn_readlane(x_page, i) * s.page_bytes;
-      const int strip = (__builtin_amdgcn_readlane(x_rows, i) & 255) / 8 + quad;
-#pragma unroll
-      for (int j = 0; j < NV; ++j) vc[j] = load_vec<true>(p + strip * (D * 4) + j * 256 + l16 * 16);
-      vs = load_vec<true>(p + codes + strip * (NG * 32) + (l16 & (2 * NG - 1)) * 16);
-    };
-    load_keys(0);
-    load_values(0);
-    for (int i = 0; i < n; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      const char *img = ring + slot * TILE;
+      slot = slot == RING - 1 ? 0 : slot + 1;
       const int live = __builtin_amdgcn_readlane(x_rows, i) >> 8;
       // ---- scores of the keys l16 and 16 + l16 against the heads 4 quad + e
       float x2[2][4];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
+        const int row = 16 * r + l16;
+        uint32_t kc[NG], ks[NG];
+        if constexpr (NG == 4) {
+          const u32x4 w = *reinterpret_cast<const u32x4 *>(img + row * 64 + (quad ^ ((row >> 2) & 3)) * 16);
+          const u32x4 z = *reinterpret_cast<const u32x4 *>(img + 2 * CODES + row * 16);
+#pragma unroll
+          for (int g = 0; g < 4; ++g) { kc[g] = w[g]; ks[g] = z[g]; }
+        } else {
+          const u32x2 w = *reinterpret_cast<const u32x2 *>(img + row * 32 + quad * 8), z = *reinterpret_cast<const u32x2 *>(img + 2 * CODES + row * 8);
+#pragma unroll
+          for (int g = 0; g < 2; ++g) { kc[g] = w[g]; ks[g] = z[g]; }
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) x2[r][e] = 0.f;
 #pragma unroll
         for (int pl = 0; pl < NG; ++pl) {
-          const uint32_t w = kc[r][pl];
+          const uint32_t w = kc[pl];
           u32x4 k;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) k[j] = ((j == 0 ? w << 3 : w >> (4 * j - 3)) & 0x00780078u) | 0x3f803f80u;
+          for (int j = 0; j < 4; ++j) k[j] = ((j == 0 ? w << 3 : w >> (4 * j - 3)) & 0x00780078u) | one_bf16;
           const f32x4 acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qf[pl]), __builtin_bit_cast(bf16x8, k),
                                                                     f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-          const f16x2 sb = __builtin_bit_cast(f16x2, ks[r][pl]);
+          const f16x2 sb = __builtin_bit_cast(f16x2, ks[pl]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) x2[r][e] = fmaf((float)sb[1], qsum[pl][e], fmaf((float)sb[0], acc[e], x2[r][e]));
         }
       }
-      if (i + 1 < n) load_keys(i + 1);
       if (live < 32) {
 #pragma unroll
         for (int r = 0; r < 2; ++r)
@@ -218,45 +245,46 @@ __global__ __launch_bounds__(256) void paged_q4_kernel(PShape s, AShape a, AttnT
 #pragma unroll
           for (int off = 1; off < 16; off <<= 1) t = fmaxf(t, __shfl_xor(t, off));
           const float want = kTopWeight - t * c2;            // minus the offset that puts this tile's largest weight at 2^kTopWeight
-          if (t > -INFINITY && (!has[e] || want < nm[e])) {
-            const float f = has[e] ? fast_exp2(want - nm[e]) : 0.f;
-            nm[e] = want;
-            has[e] = true;
-            ls[e] *= f;
-#pragma unroll
-            for (int k = 0; k < NB; ++k) o[k][e] *= f;
-          }
+          const bool move = t > -INFINITY && (!has[e] || want < nm[e]);
+          const float f = move ? (has[e] ? fast_exp2(want - nm[e]) : 0.f) : 1.f;
+          nm[e] = move ? want : nm[e];
+          has[e] |= move;
           fresh |= !has[e];
+          ls[e] *= f;
+#pragma unroll
+          for (int k = 0; k < NB; ++k) o[k][e] *= f;
 #pragma unroll
           for (int r = 0; r < 2; ++r) p[r][e] = fast_exp2(fmaf(x2[r][e], c2, nm[e]));
         }
         fresh = __builtin_amdgcn_ballot_w64(fresh) != 0;
       }
-      // ---- images: weights (head, key pair), scales of the wave's strips; rows that do not exist get zeros
+      // ---- the image of the weights (head, key pair)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         ls[e] += p[0][e] + p[1][e];
         p_img[(4 * quad + e) * PROW + l16] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)p[0][e], (_Float16)p[1][e]});
       }
-      if (live < 32) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          vs[k] &= (4 * quad + k < live ? 0xffffu : 0u) | (16 + 4 * quad + k < live ? 0xffff0000u : 0u);
-      }
-      if (l16 < 2 * NG) v_img[quad * VROW + l16] = vs;
       wave_lds_fence();
       const f16x8 pw = __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4 *>(p_img + l16 * PROW + 4 * quad));
+      // ---- weighted values; scales of rows that do not exist count as zeros
+      u32x4 mask;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) mask[k] = (4 * quad + k < live ? 0xffffu : 0u) | (16 + 4 * quad + k < live ? 0xffff0000u : 0u);
+      const char *vimg = img + CODES + quad * (D * 4) + l16 * 16, *simg = img + 2 * CODES + SCALES + quad * (NG * 32);
+      u32x4 vc = {};
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        const u32x4 st = v_img[quad * VROW + 2 * g], ba = v_img[quad * VROW + 2 * g + 1];
+        if (g % 2 == 0) vc = *reinterpret_cast<const u32x4 *>(vimg + g / 2 * 256);
+        u32x4 st = *reinterpret_cast<const u32x4 *>(simg + g * 32), ba = *reinterpret_cast<const u32x4 *>(simg + g * 32 + 16);
+        if (live < 32) { st &= mask; ba &= mask; }
 #pragma unroll
         for (int hb = 0; hb < 2; ++hb) {
           const int blk = 2 * g + hb;
-          const uint32_t w = vc[blk >> 2][blk & 3];
+          const uint32_t w = vc[blk & 3];
           u32x4 v;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const uint32_t un = ((j < 2 ? w << (6 - 4 * j) : w >> (4 * j - 6)) & 0x03c003c0u) | 0x3c003c00u;
+            const uint32_t un = ((j < 2 ? w << (6 - 4 * j) : w >> (4 * j - 6)) & 0x03c003c0u) | one_f16;
             const f16x2 val = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, un), __builtin_bit_cast(f16x2, (uint32_t)st[j]),
                                                         __builtin_bit_cast(f16x2, (uint32_t)ba[j]));
             v[j] = __builtin_bit_cast(uint32_t, val);
@@ -265,20 +293,20 @@ __global__ __launch_bounds__(256) void paged_q4_kernel(PShape s, AShape a, AttnT
         }
       }
       wave_lds_fence();
-      if (i + 1 < n) load_values(i + 1);
     }
   }
 
   // ---- the waves' shares: offsets, sums over the 16 keys of a lane row, weighted values of head 4 quad + e, element 16 k + l16
+  __syncthreads();                                             // the shares take the rings' place
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
 #pragma unroll
     for (int off = 1; off < 16; off <<= 1) ls[e] += __shfl_xor(ls[e], off);
     if (l16 == 0) { m_s[wave][4 * quad + e] = has[e] ? -nm[e] : -INFINITY; l_s[wave][4 * quad + e] = ls[e]; }
 #pragma unroll
-    for (int k = 0; k < NB; ++k) o_s[wave][4 * quad + e][(16 * k + l16) ^ (4 * quad + e)] = o[k][e];
+    for (int k = 0; k < NB; ++k) sh.share.o[wave][4 * quad + e][(16 * k + l16) ^ (4 * quad + e)] = o[k][e];
   }
-  finish_chunk<MIXKV_BF16, D>(s, a, l, o_s, m_s, l_s, part, (((unit0 + ul) * a.gchunks + gc) * a.nchunks + ch) * a.gt, q0, ng, chunks_used(a, tiles) <= 1);
+  finish_chunk<MIXKV_BF16, D>(s, a, l, sh.share.o, m_s, l_s, part, (((unit0 + ul) * a.gchunks + gc) * a.nchunks + ch) * a.gt, q0, ng, chunks_used(a, tiles) <= 1);
 }
 
 // ------------------------------------------------------------------------------------------------
