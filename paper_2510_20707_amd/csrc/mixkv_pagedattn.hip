@@ -47,11 +47,11 @@ __device__ __forceinline__ int chunks_used(const AShape &a, int tiles) { return 
 // A weighted sum over its sum of weights; no rows give zeros, a NaN stays one.
 __device__ __forceinline__ float row_result(float acc, float tot) { return tot == 0.f ? 0.f : acc / tot; }
 
-// The workgroup's end: folds the waves' shares in order (o_s of head g holds element d at d ^ g) and writes the rows, or the chunk's partial: the
-// weighted values, then offset and sum.
+// The workgroup's end: folds the waves' shares in order (o_s of head g holds element d at d ^ g) and writes the rows, or the chunk's partial:
+// weighted values in `part`, offset and sum in `part_ml`.
 template <int DT, int D>
 __device__ __forceinline__ void finish_chunk(const PShape &s, const AShape &a, const AttnLayer &l, float (&o_s)[4][kAttnHeads][D], float (&m_s)[4][kAttnHeads],
-                                             float (&l_s)[4][kAttnHeads], float *part, int64_t slot, int64_t q0, int ng, bool whole) {
+                                             float (&l_s)[4][kAttnHeads], float *part, float *part_ml, int64_t slot, int64_t q0, int ng, bool whole) {
   __syncthreads();
   for (int idx = threadIdx.x; idx < ng * D; idx += 256) {
     const int g = idx / D, d = idx - g * D;
@@ -67,9 +67,8 @@ __device__ __forceinline__ void finish_chunk(const PShape &s, const AShape &a, c
       tot = fmaf(l_s[w][g], f, tot);
     }
     if (!whole) {
-      float *dst = part + (slot + g) * (D + 2);
-      dst[d] = acc;
-      if (d == 0) { dst[D] = mn; dst[D + 1] = tot; }
+      part[(slot + g) * D + d] = acc;
+      if (d == 0) reinterpret_cast<float2 *>(part_ml)[slot + g] = make_float2(mn, tot);
       continue;
     }
     const float res = row_result(acc, tot);
@@ -79,23 +78,25 @@ __device__ __forceinline__ void finish_chunk(const PShape &s, const AShape &a, c
 }
 
 // ------------------------------------------------------------------------------------------------
-// paged_q4_kernel (4-bit pages): a workgroup of four waves, every wave on 32-row tiles of its own.
-//   * An element is B + S u with u = 1 + code / 16, whose bits are those of 1.0 with the code on top of the mantissa: a shift and an
-//     and-or make two of them, in bf16 or fp16.
-//   * Scores: query heads on the output rows, keys on the columns of a 16 x 16 x 32 product for each group of 32 elements, on the u alone (exact
-//     in bf16, as the queries are); a lane then has one key and forms sum_g S_g acc_g + B_g sum(q_g) in fp32.  A key's words are stored in
-//     the order in which the lanes of a product want them, so they come from memory into the operand.
+// paged_q4_kernel (4-bit pages): a workgroup of four waves, every wave on 32-row tiles of its own, which travel through a ring of its
+// own in LDS (direct loads, the next tiles on their way while one is worked on; no barrier before the end).
+//   * Scores: query heads on the output rows, keys on the columns of a 16 x 16 x 32 fp16 product for each group of 32 elements.  A word's codes,
+//     masked in place, are fp16 subnormals, code 2^-24 and, one nibble up, code 2^-20 (the queries of those elements are taken by 16 less): no
+//     conversion, exact products.  Queries are brought to [2^13, 2^14) by a power of two per head, which makes bf16 exact in fp16 down to
+//     2^-37 of the largest.  With acc_g = sum q code of group g and element = B + S + S code / 16, a score is
+//     sum_g S_g acc_g / 16 + sum_g (B_g + S_g) sum(q_g): four multiply-adds, and one product of the key's raw (S, B) pairs with the sums of
+//     the queries in two fp16 parts.
 //   * Weights as fp16 through the wave's LDS image (head, key): a lane holds two keys 16 rows apart, a word of the image.
-//   * Values: a word of a page holds eight rows' codes of one element, an operand of the second product; B + S u is formed by packed fp16
-//     multiply-adds with the strip's scales.  Fp16 rounds weights and values by 2^-11, an eighth of the output's own rounding; both are
-//     averaged over the rows.  The weights are relative to an offset that puts the largest near 2^8: fp16 then resolves weights down
-//     to 2^-32 of it.
+//   * Values: a word of a page holds eight rows' codes of one element, an operand of the second product: the code on top of the mantissa of
+//     1.0 is u = 1 + code / 16, and B + S u a packed fp16 multiply-add with the strip's scales.  Fp16 rounds weights and values by 2^-11, an
+//     eighth of the output's own rounding; both are averaged over the rows.  The weights are relative to an offset that puts the
+//     largest near 2^8: fp16 then resolves weights down to 2^-32 of it.
 // ------------------------------------------------------------------------------------------------
-constexpr int kQ4Ring = 3, kQ4Waves = 2;
+constexpr int kQ4Ring = 2, kQ4Waves = 3;
 constexpr float kTopWeight = 8.f, kWeightLimit = 16384.f;     // log2 of the largest weight where an offset is chosen; where it moves
 
 template <int D>
-__global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShape a, AttnTable tab, float *part, int64_t unit0) {
+__global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShape a, AttnTable tab, float *part, float *part_ml, int64_t unit0) {
   constexpr int NG = D / 32, NB = D / 16, H = kAttnHeads, W = 4;
   constexpr int CODES = 16 * D, SCALES = 32 * NG * 4, TILE = 2 * (CODES + SCALES);   // bytes of a tile: keys' codes, values', keys' scales, values'
   constexpr int NL = CODES / 1024, LOADS = 2 * NL + 1, RING = kQ4Ring;
@@ -114,35 +115,15 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
   const int64_t q0 = (int64_t)b * s.hq + h * s.G + gc * H;   // first query row
   // group of the words at place g' of a key row, and the queries in that order: lane (head, quad) holds elements 8 quad + e of the group
   auto group_at = [](int pl) { return D == 128 ? (pl & 1) * 2 + (pl >> 1) : pl; };
-  u32x4 qf[NG];
+  u32x4 qr[NG];
 #pragma unroll
   for (int pl = 0; pl < NG; ++pl)
-    qf[pl] = *reinterpret_cast<const u32x4 *>(l.Q + ((q0 + (l16 < ng ? l16 : 0)) * D + 32 * group_at(pl) + 8 * quad) * 2);
+    qr[pl] = *reinterpret_cast<const u32x4 *>(l.Q + ((q0 + (l16 < ng ? l16 : 0)) * D + 32 * group_at(pl) + 8 * quad) * 2);
   const int len = head_rows(s, c, u), tiles = head_tiles(s, a, c, l, u, len);
   int t0, t1;
   chunk_of(a, tiles, ch, t0, t1);
   if (t0 >= t1 && ch > 0) return;
-#pragma unroll
-  for (int pl = 0; pl < NG; ++pl)
-    if (l16 >= ng) qf[pl] = u32x4{0u, 0u, 0u, 0u};           // heads past the group are zero rows
   const int codes = s.P * D / 2;                             // bytes of codes in front of a page's scales
-  const float c2 = s.scale_log2e;
-  // an and-or takes one constant from a scalar register or the instruction; the other one lives in a vector register
-  uint32_t one_bf16, one_f16;
-  asm("v_mov_b32 %0, 0x3f803f80" : "=v"(one_bf16));
-  asm("v_mov_b32 %0, 0x3c003c00" : "=v"(one_f16));
-
-  f32x4 qsum[NG], o[NB];
-  float nm[4] = {0.f, 0.f, 0.f, 0.f}, ls[4] = {0.f, 0.f, 0.f, 0.f};   // minus the offsets of heads 4 quad + i (0: none yet), sums of weights
-  bool has[4] = {false, false, false, false};
-  {
-    const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
-#pragma unroll
-    for (int pl = 0; pl < NG; ++pl)
-      qsum[pl] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qf[pl]), ones, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-  }
-#pragma unroll
-  for (int i = 0; i < NB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   const char *ring = reinterpret_cast<const char *>(sh.work.ring) + wave * (RING * TILE);
   const uint32_t ring_a = lds_base_of(sh.work.ring) + wave * (RING * TILE);
   uint32_t *p_img = sh.work.p[wave];
@@ -153,31 +134,84 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
   const uint32_t k_off = krow * (D / 2) + kpiece * 16;
   const bool s_keys = lane < SCALES / 16;
   const uint32_t s_off = codes + (s_keys ? lane : lane - SCALES / 16) * 16;
-  bool fresh = true;                                           // some head has no offset yet
-
-  for (int first = t0 + wave; first < t1; first += 64 * W) {
-    // lane i: where the wave's i-th tile of the next 64 lies
+  int x_page = 0, x_rows = 0, n = 0;                           // lane i: where the wave's i-th tile of a batch of 64 lies; tiles of the batch
+  auto batch = [&](int first) {
     const int mine = first + lane * W;
     Tile x{0, 0, 0};
     if (mine < t1) x = tile_at(s, a, c, l, u, len, mine);
-    const int x_page = max(x.page, 0), x_rows = x.row | (x.live << 8);
-    const int n = min((t1 - first + W - 1) / W, 64);
-    // tile i into its image
-    auto request = [&](int i, uint32_t img) {
-      const int64_t page = (int64_t)__builtin_amdgcn_readlane(x_page, i) * s.page_bytes;
-      const int row = __builtin_amdgcn_readlane(x_rows, i) & 255;
-      const char *kp = c.K + page, *vp = c.V + page;
+    x_page = max(x.page, 0);
+    x_rows = x.row | (x.live << 8);
+    n = min(max((t1 - first + W - 1) / W, 0), 64);
+  };
+  // tile i into its image
+  auto request = [&](int i, uint32_t img) {
+    const int64_t page = (int64_t)__builtin_amdgcn_readlane(x_page, i) * s.page_bytes;
+    const int row = __builtin_amdgcn_readlane(x_rows, i) & 255;
+    const char *kp = c.K + page, *vp = c.V + page;
 #pragma unroll
-      for (int j = 0; j < NL; ++j) load_to_lds<true>(kp + (uint32_t)(row * (D / 2)) + (k_off + j * 1024), img + j * 1024);
+    for (int j = 0; j < NL; ++j) load_to_lds<true>(kp + (uint32_t)(row * (D / 2)) + (k_off + j * 1024), img + j * 1024);
 #pragma unroll
-      for (int j = 0; j < NL; ++j) load_to_lds<true>(vp + (uint32_t)(row * (D / 2)) + (uint32_t)(lane * 16 + j * 1024), img + CODES + j * 1024);
-      const char *sp = (s_keys ? kp : vp) + (uint32_t)(row * NG * 4) + s_off;
-      if (2 * SCALES / 16 == 64 || lane < 2 * SCALES / 16) load_to_lds<true>(sp, img + 2 * CODES);
-    };
+    for (int j = 0; j < NL; ++j) load_to_lds<true>(vp + (uint32_t)(row * (D / 2)) + (uint32_t)(lane * 16 + j * 1024), img + CODES + j * 1024);
+    const char *sp = (s_keys ? kp : vp) + (uint32_t)(row * NG * 4) + s_off;
+    if (2 * SCALES / 16 == 64 || lane < 2 * SCALES / 16) load_to_lds<true>(sp, img + 2 * CODES);
+  };
+  auto begin = [&](int first) {                                // the batch's first tiles on their way
+    batch(first);
     wait_vm<0>();                                              // the loop counts its own requests
 #pragma unroll
     for (int i = 0; i < RING - 1; ++i)
       if (i < n) request(i, ring_a + i * TILE);
+  };
+  begin(t0 + wave);
+
+  // ---- the queries: to fp16, by a power of two per head; their sums over each group, in two parts, against a key's (S, B) pairs
+  f16x8 qf[NG], qs;
+  float c2[4];                                                 // heads 4 quad + e: what brings a score, times 2^-24 2^k, to the exponent of 2
+  {
+    uint32_t most = 0;
+#pragma unroll
+    for (int pl = 0; pl < NG; ++pl)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) most = max(most, max(qr[pl][j] & 0x7fffu, (qr[pl][j] >> 16) & 0x7fffu));
+    most = max(most, (uint32_t)__shfl_xor((int)most, 16));
+    most = max(most, (uint32_t)__shfl_xor((int)most, 32));
+    const int ex = min(max((int)(most >> 7), 1), 254) - 127, sh2 = l16 < ng ? 13 - ex : 0;   // 2^ex <= the largest < 2^(ex + 1); NaN and infinities stay what they are
+    const float back = ldexpf(s.scale_log2e * 1048576.f, -sh2);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c2[e] = __shfl(back, 4 * quad + e);
+    float hi[NG], lo[NG];
+#pragma unroll
+    for (int pl = 0; pl < NG; ++pl) {
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t w = qr[pl][e >> 1];
+        float q = ldexpf(__uint_as_float(e & 1 ? w & 0xffff0000u : w << 16), sh2);
+        if (l16 >= ng) q = 0.f;                                // heads past the group are zero rows
+        sum += q;
+        qf[pl][e] = (_Float16)((e >> 1) & 1 ? q * 0.0625f : q);
+      }
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      sum *= 0.00390625f;                                      // at most 32 2^14 2^-8
+      hi[pl] = (float)(_Float16)sum;
+      lo[pl] = sum - hi[pl];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) qs[e] = (_Float16)(e / 2 < NG ? (quad == 0 ? hi[e / 2 % NG] : (quad == 1 ? lo[e / 2 % NG] : 0.f)) : 0.f);
+  }
+  uint32_t one_f16;                                            // an and-or takes one scalar constant: the other one is kept in a register
+  asm("v_mov_b32 %0, 0x3c003c00" : "=v"(one_f16));
+
+  f32x4 o[NB];
+  float nm[4] = {0.f, 0.f, 0.f, 0.f}, ls[4] = {0.f, 0.f, 0.f, 0.f};   // minus the offsets of heads 4 quad + i (0: none yet), sums of weights
+  bool has[4] = {false, false, false, false};
+#pragma unroll
+  for (int i = 0; i < NB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  bool fresh = true;                                           // some head has no offset yet
+
+  for (int first = t0 + wave; first < t1; first += 64 * W) {
+    if (first != t0 + wave) begin(first);
     int slot = 0;
     for (int i = 0; i < n; ++i) {
       __builtin_amdgcn_sched_barrier(0);
@@ -192,51 +226,69 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
       }
       __builtin_amdgcn_sched_barrier(0);
       const char *img = ring + slot * TILE;
-      slot = slot == RING - 1 ? 0 : slot + 1;
       const int live = __builtin_amdgcn_readlane(x_rows, i) >> 8;
-      // ---- scores of the keys l16 and 16 + l16 against the heads 4 quad + e
-      float x2[2][4];
+      if (live < 32) {                                         // the values' scales of rows that do not exist: zeros
+        u32x4 *at = reinterpret_cast<u32x4 *>(const_cast<char *>(img) + 2 * CODES + SCALES) + lane;
+        if (lane < SCALES / 16) {
+          const int q = lane / (2 * NG);
+          u32x4 v = *at;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[k] &= (4 * q + k < live ? 0xffffu : 0u) | (16 + 4 * q + k < live ? 0xffff0000u : 0u);
+          *at = v;
+        }
+        wave_lds_fence();
+      }
+      slot = slot == RING - 1 ? 0 : slot + 1;
+      // ---- scores of the keys l16 and 16 + l16 against the heads 4 quad + e, by 2^-24 2^k
+      f32x4 acc[2][NG], x2[2];
+      uint32_t ks[2][NG];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
         const int row = 16 * r + l16;
-        uint32_t kc[NG], ks[NG];
+        uint32_t kc[NG];
+        u32x4 sb = {0u, 0u, 0u, 0u};
         if constexpr (NG == 4) {
           const u32x4 w = *reinterpret_cast<const u32x4 *>(img + row * 64 + (quad ^ ((row >> 2) & 3)) * 16);
-          const u32x4 z = *reinterpret_cast<const u32x4 *>(img + 2 * CODES + row * 16);
+          sb = *reinterpret_cast<const u32x4 *>(img + 2 * CODES + row * 16);
 #pragma unroll
-          for (int g = 0; g < 4; ++g) { kc[g] = w[g]; ks[g] = z[g]; }
+          for (int g = 0; g < 4; ++g) kc[g] = w[g];
         } else {
           const u32x2 w = *reinterpret_cast<const u32x2 *>(img + row * 32 + quad * 8), z = *reinterpret_cast<const u32x2 *>(img + 2 * CODES + row * 8);
 #pragma unroll
-          for (int g = 0; g < 2; ++g) { kc[g] = w[g]; ks[g] = z[g]; }
+          for (int g = 0; g < 2; ++g) { kc[g] = w[g]; sb[g] = z[g]; }
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x2[r][e] = 0.f;
+        x2[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(qs, __builtin_bit_cast(f16x8, sb), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
         for (int pl = 0; pl < NG; ++pl) {
-          const uint32_t w = kc[pl];
-          u32x4 k;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) k[j] = ((j == 0 ? w << 3 : w >> (4 * j - 3)) & 0x00780078u) | one_bf16;
-          const f32x4 acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qf[pl]), __builtin_bit_cast(bf16x8, k),
-                                                                    f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-          const f16x2 sb = __builtin_bit_cast(f16x2, ks[pl]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x2[r][e] = fmaf((float)sb[1], qsum[pl][e], fmaf((float)sb[0], acc[e], x2[r][e]));
+          ks[r][pl] = sb[pl];
+          const uint32_t w = kc[pl], w8 = w >> 8;
+          const u32x4 k = {w & 0x000f000fu, w & 0x00f000f0u, w8 & 0x000f000fu, w8 & 0x00f000f0u};
+          acc[r][pl] = __builtin_amdgcn_mfma_f32_16x16x32_f16(qf[pl], __builtin_bit_cast(f16x8, k), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
         }
       }
+#pragma unroll
+      for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float x = x2[r][e] * 0x1p-12f;                       // 2^8 2^-20
+#pragma unroll
+          for (int pl = 0; pl < NG; ++pl) x = fmaf((float)__builtin_bit_cast(f16x2, ks[r][pl])[0], acc[r][pl][e], x);
+          x2[r][e] = x;
+        }
       if (live < 32) {
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
           for (int e = 0; e < 4; ++e) x2[r][e] = 16 * r + l16 < live ? x2[r][e] : -INFINITY;
+        asm volatile("" : "+v"(x2[0]), "+v"(x2[1]));           // a branch, not selects in every tile
       }
       // ---- weights; the offsets move where a head has none yet or a weight leaves fp16's range
-      float p[2][4], top = 0.f;
+      float p[2][4];
 #pragma unroll
       for (int r = 0; r < 2; ++r)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { p[r][e] = fast_exp2(fmaf(x2[r][e], c2, nm[e])); top = fmaxf(top, p[r][e]); }
+        for (int e = 0; e < 4; ++e) p[r][e] = fast_exp2(fmaf(x2[r][e], c2[e], nm[e]));
+      const float top = fmaxf(fmaxf(fmaxf(p[0][0], p[0][1]), fmaxf(p[0][2], p[0][3])), fmaxf(fmaxf(p[1][0], p[1][1]), fmaxf(p[1][2], p[1][3])));
       if (fresh || __builtin_amdgcn_ballot_w64(!(top < kWeightLimit)) != 0) {
         fresh = false;
 #pragma unroll
@@ -244,7 +296,7 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
           float t = fmaxf(x2[0][e], x2[1][e]);
 #pragma unroll
           for (int off = 1; off < 16; off <<= 1) t = fmaxf(t, __shfl_xor(t, off));
-          const float want = kTopWeight - t * c2;            // minus the offset that puts this tile's largest weight at 2^kTopWeight
+          const float want = kTopWeight - t * c2[e];         // minus the offset that puts this tile's largest weight at 2^kTopWeight
           const bool move = t > -INFINITY && (!has[e] || want < nm[e]);
           const float f = move ? (has[e] ? fast_exp2(want - nm[e]) : 0.f) : 1.f;
           nm[e] = move ? want : nm[e];
@@ -254,7 +306,7 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
 #pragma unroll
           for (int k = 0; k < NB; ++k) o[k][e] *= f;
 #pragma unroll
-          for (int r = 0; r < 2; ++r) p[r][e] = fast_exp2(fmaf(x2[r][e], c2, nm[e]));
+          for (int r = 0; r < 2; ++r) p[r][e] = fast_exp2(fmaf(x2[r][e], c2[e], nm[e]));
         }
         fresh = __builtin_amdgcn_ballot_w64(fresh) != 0;
       }
@@ -266,17 +318,13 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
       }
       wave_lds_fence();
       const f16x8 pw = __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4 *>(p_img + l16 * PROW + 4 * quad));
-      // ---- weighted values; scales of rows that do not exist count as zeros
-      u32x4 mask;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) mask[k] = (4 * quad + k < live ? 0xffffu : 0u) | (16 + 4 * quad + k < live ? 0xffff0000u : 0u);
+      // ---- weighted values
       const char *vimg = img + CODES + quad * (D * 4) + l16 * 16, *simg = img + 2 * CODES + SCALES + quad * (NG * 32);
       u32x4 vc = {};
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
         if (g % 2 == 0) vc = *reinterpret_cast<const u32x4 *>(vimg + g / 2 * 256);
-        u32x4 st = *reinterpret_cast<const u32x4 *>(simg + g * 32), ba = *reinterpret_cast<const u32x4 *>(simg + g * 32 + 16);
-        if (live < 32) { st &= mask; ba &= mask; }
+        const u32x4 st = *reinterpret_cast<const u32x4 *>(simg + g * 32), ba = *reinterpret_cast<const u32x4 *>(simg + g * 32 + 16);
 #pragma unroll
         for (int hb = 0; hb < 2; ++hb) {
           const int blk = 2 * g + hb;
@@ -306,7 +354,7 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
 #pragma unroll
     for (int k = 0; k < NB; ++k) sh.share.o[wave][4 * quad + e][(16 * k + l16) ^ (4 * quad + e)] = o[k][e];
   }
-  finish_chunk<MIXKV_BF16, D>(s, a, l, sh.share.o, m_s, l_s, part, (((unit0 + ul) * a.gchunks + gc) * a.nchunks + ch) * a.gt, q0, ng, chunks_used(a, tiles) <= 1);
+  finish_chunk<MIXKV_BF16, D>(s, a, l, sh.share.o, m_s, l_s, part, part_ml, (((unit0 + ul) * a.gchunks + gc) * a.nchunks + ch) * a.gt, q0, ng, chunks_used(a, tiles) <= 1);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -319,7 +367,7 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
 // Offsets as in decode_mfma_kernel.
 // ------------------------------------------------------------------------------------------------
 template <int DT, int D>
-__global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, AttnTable tab, float *part, int64_t unit0) {
+__global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, AttnTable tab, float *part, float *part_ml, int64_t unit0) {
   constexpr bool F32 = DT == MIXKV_F32;
   constexpr int EB = F32 ? 4 : 2, RB = D * EB, PPR = RB / 16, NC = PPR / 4, NB = D / 16, H = kAttnHeads, W = 4;
   constexpr int NV = F32 ? 8 * (D / 64) : 32 * PPR / 64, RPL = 64 / PPR;     // 16-byte loads of a lane for a tile of values
@@ -474,37 +522,61 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Att
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       o_s[wave][l16][(F32 ? 64 * (k >> 2) + 4 * (4 * quad + e) + (k & 3) : 16 * k + 4 * quad + e) ^ l16] = o[k][e];
-  finish_chunk<DT, D>(s, a, l, o_s, m_s, l_s, part, (((unit0 + ul) * a.gchunks + gc) * a.nchunks + ch) * a.gt, q0, ng, chunks_used(a, tiles) <= 1);
+  finish_chunk<DT, D>(s, a, l, o_s, m_s, l_s, part, part_ml, (((unit0 + ul) * a.gchunks + gc) * a.nchunks + ch) * a.gt, q0, ng, chunks_used(a, tiles) <= 1);
 }
 
-// Folds the chunks of one (unit, group of query heads), in order: a thread per output element.
+// Folds the chunks of one query head: slices of D/4 threads take every S-th chunk, 16 bytes of its row a thread, and are summed in order.
 template <int DT, int D>
-__global__ __launch_bounds__(256) void paged_merge_kernel(PShape s, AShape a, AttnTable tab, const float *part, int64_t unit0) {
-  const int ug = blockIdx.x, gc = ug % a.gchunks, ul = ug / a.gchunks;
+__global__ __launch_bounds__(256) void paged_merge_kernel(PShape s, AShape a, AttnTable tab, const float *part, const float *part_ml, int64_t unit0) {
+  constexpr int T = D / 4, S = 256 / T;
+  __shared__ float red[4];
+  __shared__ f32x4 acc_s[S][T];
+  __shared__ float tot_s[S];
+  const int tid = threadIdx.x, t = tid % T, slice = tid / T;
+  const int ug = blockIdx.x, gc = ug % a.gchunks, ul = ug / a.gchunks, g = blockIdx.y;
   const int layer = ul / s.units_per_layer, u = ul - layer * s.units_per_layer;
-  const int b = u / s.hkv, h = u - b * s.hkv, ng = min(kAttnHeads, s.G - gc * kAttnHeads);
+  const int b = u / s.hkv, h = u - b * s.hkv;
+  if (g >= min(kAttnHeads, s.G - gc * kAttnHeads)) return;
   const PCache c = tab.c[layer];
   const AttnLayer l = tab.l[layer];
   const int used = chunks_used(a, head_tiles(s, a, c, l, u, head_rows(s, c, u)));
   if (used <= 1) return;
-  const int idx = blockIdx.y * 256 + threadIdx.x;
-  if (idx >= ng * D) return;
-  const int g = idx / D, d = idx - g * D;
-  const float *src = part + (((unit0 + ul) * a.gchunks + gc) * a.nchunks * a.gt + g) * (D + 2);
-  const int64_t step = (int64_t)a.gt * (D + 2);
+  const int64_t slot = (((unit0 + ul) * a.gchunks + gc) * a.nchunks) * a.gt + g;
+  const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + slot;
+  const float *rows = part + slot * D + 4 * t;
   float m = -INFINITY;
-  for (int i = 0; i < used; ++i) m = fmaxf(m, src[i * step + D]);
+  for (int i = tid; i < used; i += 256) m = fmaxf(m, ml[(int64_t)i * a.gt].x);
+  m = wave_reduce<WMax>(m, -INFINITY);
+  if ((tid & 63) == 0) red[tid >> 6] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
   const float mu = m == -INFINITY ? 0.f : m;
-  float acc = 0.f, tot = 0.f;
-  for (int i = 0; i < used; ++i) {
-    const float f = fast_exp2(src[i * step + D] - mu);
-    acc = fmaf(src[i * step + d], f, acc);
-    tot = fmaf(src[i * step + D + 1], f, tot);
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  float tot = 0.f;
+#pragma unroll 4
+  for (int i = slice; i < used; i += S) {
+    const float2 x = ml[(int64_t)i * a.gt];
+    const float f = fast_exp2(x.x - mu);
+    acc += *reinterpret_cast<const f32x4 *>(rows + (int64_t)i * a.gt * D) * f;
+    tot = fmaf(x.y, f, tot);
   }
-  const float res = row_result(acc, tot);
-  const int64_t at = ((int64_t)b * s.hq + h * s.G + gc * kAttnHeads + g) * D + d;
-  if constexpr (DT == MIXKV_BF16) reinterpret_cast<uint16_t *>(l.out)[at] = f32_to_bf16_rne(res);
-  else reinterpret_cast<float *>(l.out)[at] = res;
+  acc_s[slice][t] = acc;
+  if (t == 0) tot_s[slice] = tot;
+  __syncthreads();
+  if (tid >= T) return;
+#pragma unroll
+  for (int i = 1; i < S; ++i) { acc += acc_s[i][t]; tot += tot_s[i]; }
+  const int64_t at = ((int64_t)b * s.hq + h * s.G + gc * kAttnHeads + g) * D + 4 * t;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) acc[e] = row_result(acc[e], tot);
+  if constexpr (DT == MIXKV_BF16) {
+    u32x2 v;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) v[e] = (uint32_t)f32_to_bf16_rne(acc[2 * e]) | ((uint32_t)f32_to_bf16_rne(acc[2 * e + 1]) << 16);
+    *reinterpret_cast<u32x2 *>(reinterpret_cast<uint16_t *>(l.out) + at) = v;
+  } else {
+    *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(l.out) + at) = acc;
+  }
 }
 
 // Tiles of a chunk and chunks of a head, from nothing but the arguments.
@@ -517,10 +589,11 @@ static void attn_config(const PShape &s, int n_layers, int max_rows, AShape *a) 
   a->ctiles = (int)((ct + 3) / 4 * 4);
   a->nchunks = (int)std::max<int64_t>(1, (tiles + a->ctiles - 1) / a->ctiles);
 }
-static size_t attn_bytes(const PShape &s, const AShape &a, int n_layers) {
-  if (a.nchunks == 1) return 0;
-  return (size_t)n_layers * s.units_per_layer * a.gchunks * a.nchunks * a.gt * (s.D + 2) * sizeof(float);
+// Rows of partials; each has D floats, and behind them all each has two more.
+static size_t attn_slots(const PShape &s, const AShape &a, int n_layers) {
+  return a.nchunks == 1 ? 0 : (size_t)n_layers * s.units_per_layer * a.gchunks * a.nchunks * a.gt;
 }
+static size_t attn_bytes(const PShape &s, const AShape &a, int n_layers) { return attn_slots(s, a, n_layers) * (s.D + 2) * sizeof(float); }
 static int clamp_rows(const PShape &s, int max_rows) { return std::min(max_rows, s.max_pages * s.P); }
 
 }  // namespace mixkv
@@ -565,7 +638,7 @@ extern "C" mixkv_status mixkv_paged_attention(const mixkv_paged_params *params, 
     if (workspace_bytes < need) return MIXKV_ERR_WORKSPACE_TOO_SMALL;
   }
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
-  float *part = static_cast<float *>(workspace);
+  float *part = static_cast<float *>(workspace), *part_ml = need > 0 ? part + attn_slots(s, a, n_layers) * s.D : nullptr;
   for (int l0 = 0; l0 < n_layers; l0 += kLayersPerLaunch) {
     const int nl = n_layers - l0 < kLayersPerLaunch ? n_layers - l0 : kLayersPerLaunch;
     AttnTable t;
@@ -580,9 +653,9 @@ extern "C" mixkv_status mixkv_paged_attention(const mixkv_paged_params *params, 
     }
     const int64_t groups = (int64_t)nl * s.units_per_layer * a.gchunks, unit0 = (int64_t)l0 * s.units_per_layer;
     auto go = [&](auto kern, auto merge) {
-      hipLaunchKernelGGL(kern, dim3((unsigned)(groups * a.nchunks)), dim3(256), 0, stream, s, a, t, part, unit0);
+      hipLaunchKernelGGL(kern, dim3((unsigned)(groups * a.nchunks)), dim3(256), 0, stream, s, a, t, part, part_ml, unit0);
       if (a.nchunks > 1)
-        hipLaunchKernelGGL(merge, dim3((unsigned)groups, (unsigned)((a.gt * s.D + 255) / 256)), dim3(256), 0, stream, s, a, t, (const float *)part, unit0);
+        hipLaunchKernelGGL(merge, dim3((unsigned)groups, (unsigned)a.gt), dim3(256), 0, stream, s, a, t, (const float *)part, (const float *)part_ml, unit0);
     };
     constexpr int B16 = MIXKV_BF16, F32 = MIXKV_F32;
     if (s.q4) { if (s.D == 128) go(paged_q4_kernel<128>, paged_merge_kernel<B16, 128>); else go(paged_q4_kernel<64>, paged_merge_kernel<B16, 64>); }
