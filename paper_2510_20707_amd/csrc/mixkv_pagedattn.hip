@@ -22,30 +22,36 @@ struct AShape {
 constexpr int kAttnHeads = 16;
 
 // Tiles of unit u, and where a tile lies: its first row in the pool as (page, row of the page), and how many of its rows exist.
-__device__ __forceinline__ int head_tiles(const PShape &s, const AShape &a, const PCache &c, const AttnLayer &l, int u, int len) {
+__device__ __forceinline__ int head_tiles(const PShape &s, const AShape &a, const AttnLayer &l, int u, int len) {
   if (a.keep == 0) return (len + 31) >> 5;
   return min(max(l.nsel[u], 0), a.keep) << (s.lp - 5);
 }
+// The table entry of tile t (any number >= 0), and its place in the table.  No length is needed, so that the loads of both run side by side.
+__device__ __forceinline__ int tile_entry(const PShape &s, const AShape &a, const PCache &c, const AttnLayer &l, int u, int t, int &place) {
+  place = t >> (s.lp - 5);
+  if (a.keep) place = l.sel[(int64_t)u * a.keep + min(place, a.keep - 1)];
+  return c.table[(int64_t)u * s.max_pages + min(max(place, 0), s.max_pages - 1)];
+}
 struct Tile { int page, row, live; };
-__device__ __forceinline__ Tile tile_at(const PShape &s, const AShape &a, const PCache &c, const AttnLayer &l, int u, int len, int t) {
-  const int sub = s.lp - 5;
-  int place = t >> sub;
-  if (a.keep) place = l.sel[(int64_t)u * a.keep + place];
+__device__ __forceinline__ Tile tile_of_entry(const PShape &s, int len, int t, int place, int entry) {
   Tile x;
-  x.row = (t & ((1 << sub) - 1)) * 32;
-  x.page = page_at(s, c, u, place);
-  x.live = x.page < 0 ? 0 : min(max(len - ((place << s.lp) + x.row), 0), 32);   // a place with a page is one of the table
+  x.row = (t & ((1 << (s.lp - 5)) - 1)) * 32;
+  const bool on = (uint32_t)place < (uint32_t)s.max_pages && (uint32_t)entry < (uint32_t)s.n_pages;
+  x.page = on ? entry : 0;
+  x.live = on ? min(max(len - ((place << s.lp) + x.row), 0), 32) : 0;
   return x;
 }
-// The tiles [t0, t1) of chunk `ch`.
-__device__ __forceinline__ void chunk_of(const AShape &a, int tiles, int ch, int &t0, int &t1) {
-  t0 = min((int64_t)tiles, (int64_t)ch * a.ctiles);
-  t1 = ch == a.nchunks - 1 ? tiles : (int)min((int64_t)tiles, (int64_t)(ch + 1) * a.ctiles);
-}
-__device__ __forceinline__ int chunks_used(const AShape &a, int tiles) { return (int)min((int64_t)a.nchunks, ((int64_t)tiles + a.ctiles - 1) / a.ctiles); }
+// The first tile of chunk `ch`, which may lie behind the head's last, and the end of the chunk.
+__device__ __forceinline__ int chunk_end(const AShape &a, int tiles, int ch) { return ch == a.nchunks - 1 ? tiles : min(tiles, (ch + 1) * a.ctiles); }
+__device__ __forceinline__ int chunks_used(const AShape &a, int tiles) { return min(a.nchunks, (int)(((uint32_t)tiles + a.ctiles - 1) / (uint32_t)a.ctiles)); }
 
 // A weighted sum over its sum of weights; no rows give zeros, a NaN stays one.
 __device__ __forceinline__ float row_result(float acc, float tot) { return tot == 0.f ? 0.f : acc / tot; }
+
+// The first partial row of a chunk.
+__device__ __forceinline__ int64_t slot_of(const PShape &s, const AShape &a, int64_t unit0, int layer, int u, int gc, int ch) {
+  return (((unit0 + layer * s.units_per_layer + u) * a.gchunks + gc) * a.nchunks + ch) * a.gt;
+}
 
 // The workgroup's end: folds the waves' shares in order (o_s of head g holds element d at d ^ g) and writes the rows, or the chunk's partial:
 // weighted values in `part`, offset and sum in `part_ml`.
@@ -107,8 +113,7 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
   __shared__ float m_s[W][H], l_s[W][H];
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int ch = blockIdx.x % a.nchunks, ug = blockIdx.x / a.nchunks, gc = ug % a.gchunks, ul = ug / a.gchunks;
-  const int layer = ul / s.units_per_layer, u = ul - layer * s.units_per_layer;
+  const int u = blockIdx.x, ch = blockIdx.y, layer = blockIdx.z / a.gchunks, gc = blockIdx.z - layer * a.gchunks;
   const int b = u / s.hkv, h = u - b * s.hkv, ng = min(H, s.G - gc * H);
   const PCache c = tab.c[layer];
   const AttnLayer l = tab.l[layer];
@@ -119,9 +124,9 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
 #pragma unroll
   for (int pl = 0; pl < NG; ++pl)
     qr[pl] = *reinterpret_cast<const u32x4 *>(l.Q + ((q0 + (l16 < ng ? l16 : 0)) * D + 32 * group_at(pl) + 8 * quad) * 2);
-  const int len = head_rows(s, c, u), tiles = head_tiles(s, a, c, l, u, len);
-  int t0, t1;
-  chunk_of(a, tiles, ch, t0, t1);
+  const int t0 = ch * a.ctiles;
+  int place, entry = tile_entry(s, a, c, l, u, t0 + wave + lane * W, place);
+  const int len = head_rows(s, c, u), tiles = head_tiles(s, a, l, u, len), t1 = chunk_end(a, tiles, ch);
   if (t0 >= t1 && ch > 0) return;
   const int codes = s.P * D / 2;                             // bytes of codes in front of a page's scales
   const char *ring = reinterpret_cast<const char *>(sh.work.ring) + wave * (RING * TILE);
@@ -135,11 +140,9 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
   const bool s_keys = lane < SCALES / 16;
   const uint32_t s_off = codes + (s_keys ? lane : lane - SCALES / 16) * 16;
   int x_page = 0, x_rows = 0, n = 0;                           // lane i: where the wave's i-th tile of a batch of 64 lies; tiles of the batch
-  auto batch = [&](int first) {
-    const int mine = first + lane * W;
-    Tile x{0, 0, 0};
-    if (mine < t1) x = tile_at(s, a, c, l, u, len, mine);
-    x_page = max(x.page, 0);
+  auto batch = [&](int first) {                                // from the lanes' table entries
+    const Tile x = tile_of_entry(s, len, first + lane * W, place, entry);
+    x_page = x.page;
     x_rows = x.row | (x.live << 8);
     n = min(max((t1 - first + W - 1) / W, 0), 64);
   };
@@ -211,7 +214,10 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
   bool fresh = true;                                           // some head has no offset yet
 
   for (int first = t0 + wave; first < t1; first += 64 * W) {
-    if (first != t0 + wave) begin(first);
+    if (first != t0 + wave) {
+      entry = tile_entry(s, a, c, l, u, first + lane * W, place);
+      begin(first);
+    }
     int slot = 0;
     for (int i = 0; i < n; ++i) {
       __builtin_amdgcn_sched_barrier(0);
@@ -354,7 +360,7 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
 #pragma unroll
     for (int k = 0; k < NB; ++k) sh.share.o[wave][4 * quad + e][(16 * k + l16) ^ (4 * quad + e)] = o[k][e];
   }
-  finish_chunk<MIXKV_BF16, D>(s, a, l, sh.share.o, m_s, l_s, part, part_ml, (((unit0 + ul) * a.gchunks + gc) * a.nchunks + ch) * a.gt, q0, ng, chunks_used(a, tiles) <= 1);
+  finish_chunk<MIXKV_BF16, D>(s, a, l, sh.share.o, m_s, l_s, part, part_ml, slot_of(s, a, unit0, layer, u, gc, ch), q0, ng, chunks_used(a, tiles) <= 1);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -375,8 +381,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Att
   __shared__ float m_s[W][H], l_s[W][H];
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int ch = blockIdx.x % a.nchunks, ug = blockIdx.x / a.nchunks, gc = ug % a.gchunks, ul = ug / a.gchunks;
-  const int layer = ul / s.units_per_layer, u = ul - layer * s.units_per_layer;
+  const int u = blockIdx.x, ch = blockIdx.y, layer = blockIdx.z / a.gchunks, gc = blockIdx.z - layer * a.gchunks;
   const int b = u / s.hkv, h = u - b * s.hkv, ng = min(H, s.G - gc * H);
   const PCache c = tab.c[layer];
   const AttnLayer l = tab.l[layer];
@@ -384,9 +389,9 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Att
   u32x4 qf[NC];
 #pragma unroll
   for (int k = 0; k < NC; ++k) qf[k] = *reinterpret_cast<const u32x4 *>(l.Q + (q0 + (l16 < ng ? l16 : 0)) * RB + (4 * k + quad) * 16);
-  const int len = head_rows(s, c, u), tiles = head_tiles(s, a, c, l, u, len);
-  int t0, t1;
-  chunk_of(a, tiles, ch, t0, t1);
+  const int t0 = ch * a.ctiles;
+  int place, entry = tile_entry(s, a, c, l, u, t0 + wave + lane * W, place);   // lane i: where the wave's i-th tile of 64 lies
+  const int len = head_rows(s, c, u), tiles = head_tiles(s, a, l, u, len), t1 = chunk_end(a, tiles, ch);
   if (t0 >= t1 && ch > 0) return;
 #pragma unroll
   for (int k = 0; k < NC; ++k)
@@ -401,10 +406,9 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Att
   const uint32_t img_a = (uint32_t)(uintptr_t)(lds_void_t *)img;
 
   for (int first = t0 + wave; first < t1; first += 64 * W) {
-    const int mine = first + lane * W;                         // lane i: where the wave's i-th tile of the next 64 lies
-    Tile x{0, 0, 0};
-    if (mine < t1) x = tile_at(s, a, c, l, u, len, mine);
-    const int x_page = max(x.page, 0), x_rows = x.row | (x.live << 8);
+    if (first != t0 + wave) entry = tile_entry(s, a, c, l, u, first + lane * W, place);
+    const Tile x = tile_of_entry(s, len, first + lane * W, place, entry);
+    const int x_page = x.page, x_rows = x.row | (x.live << 8);
     const int n = min((t1 - first + W - 1) / W, 64);
     u32x4 kr[2][NC], vr[NV];
     auto tile_of = [&](const char *pool, int i) {
@@ -522,7 +526,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Att
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       o_s[wave][l16][(F32 ? 64 * (k >> 2) + 4 * (4 * quad + e) + (k & 3) : 16 * k + 4 * quad + e) ^ l16] = o[k][e];
-  finish_chunk<DT, D>(s, a, l, o_s, m_s, l_s, part, part_ml, (((unit0 + ul) * a.gchunks + gc) * a.nchunks + ch) * a.gt, q0, ng, chunks_used(a, tiles) <= 1);
+  finish_chunk<DT, D>(s, a, l, o_s, m_s, l_s, part, part_ml, slot_of(s, a, unit0, layer, u, gc, ch), q0, ng, chunks_used(a, tiles) <= 1);
 }
 
 // Folds the chunks of one query head: slices of D/4 threads take every S-th chunk, 16 bytes of its row a thread, and are summed in order.
@@ -533,15 +537,14 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PShape s, AShape a, At
   __shared__ f32x4 acc_s[S][T];
   __shared__ float tot_s[S];
   const int tid = threadIdx.x, t = tid % T, slice = tid / T;
-  const int ug = blockIdx.x, gc = ug % a.gchunks, ul = ug / a.gchunks, g = blockIdx.y;
-  const int layer = ul / s.units_per_layer, u = ul - layer * s.units_per_layer;
+  const int u = blockIdx.x, g = blockIdx.y, layer = blockIdx.z / a.gchunks, gc = blockIdx.z - layer * a.gchunks;
   const int b = u / s.hkv, h = u - b * s.hkv;
   if (g >= min(kAttnHeads, s.G - gc * kAttnHeads)) return;
   const PCache c = tab.c[layer];
   const AttnLayer l = tab.l[layer];
-  const int used = chunks_used(a, head_tiles(s, a, c, l, u, head_rows(s, c, u)));
+  const int used = chunks_used(a, head_tiles(s, a, l, u, head_rows(s, c, u)));
   if (used <= 1) return;
-  const int64_t slot = (((unit0 + ul) * a.gchunks + gc) * a.nchunks) * a.gt + g;
+  const int64_t slot = slot_of(s, a, unit0, layer, u, gc, 0) + g;
   const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + slot;
   const float *rows = part + slot * D + 4 * t;
   float m = -INFINITY;
@@ -584,10 +587,12 @@ static void attn_config(const PShape &s, int n_layers, int max_rows, AShape *a) 
   a->gchunks = (s.G + kAttnHeads - 1) / kAttnHeads;
   a->gt = std::min(s.G, kAttnHeads);
   const int64_t groups = (int64_t)n_layers * s.units_per_layer * a->gchunks, tiles = ((int64_t)max_rows + 31) / 32;
-  int64_t ct = (tiles * groups + 1023) / 1024;
-  ct = std::max<int64_t>(8, std::min<int64_t>(ct, 256));
+  int64_t ct = std::max<int64_t>(4, std::min<int64_t>((tiles * groups + 511) / 512, s.q4 ? 64 : 16));
+  if (tiles <= 12) ct = tiles;
   a->ctiles = (int)((ct + 3) / 4 * 4);
-  a->nchunks = (int)std::max<int64_t>(1, (tiles + a->ctiles - 1) / a->ctiles);
+  // a launch has at most 65535 chunks, and fewer than 2^32 threads; the last chunk of a head takes what is left
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 23) / (std::min(n_layers, kLayersPerLaunch) * s.units_per_layer * (int64_t)a->gchunks)));
+  a->nchunks = (int)std::min(most, std::max<int64_t>(1, (tiles + a->ctiles - 1) / a->ctiles));
 }
 // Rows of partials; each has D floats, and behind them all each has two more.
 static size_t attn_slots(const PShape &s, const AShape &a, int n_layers) {
@@ -630,8 +635,8 @@ extern "C" mixkv_status mixkv_paged_attention(const mixkv_paged_params *params, 
   }
   AShape a{};
   attn_config(s, n_layers, clamp_rows(s, max_rows), &a);
+  if ((int64_t)std::min(n_layers, kLayersPerLaunch) * a.gchunks > 65535) return MIXKV_ERR_UNSUPPORTED;
   a.keep = sparse ? max_selected : 0;
-  if ((int64_t)std::min(n_layers, kLayersPerLaunch) * s.units_per_layer * a.gchunks * a.nchunks >= (1 << 24)) return MIXKV_ERR_UNSUPPORTED;
   const size_t need = attn_bytes(s, a, n_layers);
   if (need > 0) {
     if (!workspace || misaligned(workspace, 256)) return MIXKV_ERR_INVALID_ARG;
@@ -651,11 +656,12 @@ extern "C" mixkv_status mixkv_paged_attention(const mixkv_paged_params *params, 
       t.c[l] = PCache{static_cast<char *>(c.K_pages), static_cast<char *>(c.V_pages), nullptr, c.page_table, c.lengths};
       t.l[l] = AttnLayer{static_cast<const char *>(d.Q), static_cast<char *>(d.out), d.selected, d.n_selected};
     }
-    const int64_t groups = (int64_t)nl * s.units_per_layer * a.gchunks, unit0 = (int64_t)l0 * s.units_per_layer;
+    const int64_t unit0 = (int64_t)l0 * s.units_per_layer;
+    const unsigned z = (unsigned)(nl * a.gchunks);
     auto go = [&](auto kern, auto merge) {
-      hipLaunchKernelGGL(kern, dim3((unsigned)(groups * a.nchunks)), dim3(256), 0, stream, s, a, t, part, part_ml, unit0);
+      hipLaunchKernelGGL(kern, dim3((unsigned)s.units_per_layer, (unsigned)a.nchunks, z), dim3(256), 0, stream, s, a, t, part, part_ml, unit0);
       if (a.nchunks > 1)
-        hipLaunchKernelGGL(merge, dim3((unsigned)groups, (unsigned)a.gt), dim3(256), 0, stream, s, a, t, (const float *)part, (const float *)part_ml, unit0);
+        hipLaunchKernelGGL(merge, dim3((unsigned)s.units_per_layer, (unsigned)a.gt, z), dim3(256), 0, stream, s, a, t, (const float *)part, (const float *)part_ml, unit0);
     };
     constexpr int B16 = MIXKV_BF16, F32 = MIXKV_F32;
     if (s.q4) { if (s.D == 128) go(paged_q4_kernel<128>, paged_merge_kernel<B16, 128>); else go(paged_q4_kernel<64>, paged_merge_kernel<B16, 64>); }

@@ -175,6 +175,6 @@ def test_workspaces():
     assert B.mixkv_paged_attention_workspace_size(p, 1, 2 ** 31 - 1) == B.mixkv_paged_attention_workspace_size(p, 1, 4096 * 64)
 
 
-def test_launches_with_more_workgroups_than_a_grid_are_refused():
-    p = _params(batch=9000, max_pages=1 << 20, n_pages=1 << 20)
-    assert _attend(p=p, rows=1 << 26) == UNSUPPORTED
+def test_more_layers_and_heads_than_a_grid_are_refused():
+    p = _params(batch=1, n_q_heads=1 << 18, n_kv_heads=1)            # 16384 groups of 16 query heads, in four layers
+    assert _attend(p=p, n=4) == UNSUPPORTED
