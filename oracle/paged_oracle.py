@@ -184,11 +184,14 @@ def page_scores(Q, bounds, table, lengths, P, b, h):
     up, down = np.maximum(q, 0).sum(0), np.minimum(q, 0).sum(0)
     n = min(max(int(lengths[b, h]), 0), table.shape[2] * P)
     out = np.full(-(-n // P), -np.inf, np.float32)
+    known = {}
     for i in range(len(out)):
         page = _page(table, b, h, i, len(bounds))
         if page >= 0:
-            hi, lo = np.where(up != 0, bounds[page, 1], 0.0), np.where(down != 0, bounds[page, 0], 0.0)
-            out[i] = np.float32((hi * up + lo * down).sum())
+            if page not in known:
+                hi, lo = np.where(up != 0, bounds[page, 1], 0.0), np.where(down != 0, bounds[page, 0], 0.0)
+                known[page] = np.float32((hi * up + lo * down).sum())
+            out[i] = known[page]
     return out
 
 

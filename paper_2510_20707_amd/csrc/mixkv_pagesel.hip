@@ -1,9 +1,12 @@
-// Pages worth attending to (mixkv_paged_select): scores of all pages from their key bounds, then the best of each head.
+// Pages worth attending to (mixkv_paged_select): order keys of all pages' scores from their key bounds, then the best of each head.
 //
 // With lo and hi a page's smallest and largest keys per element, max(q_d lo_d, q_d hi_d) = max(q_d, 0) hi_d + min(q_d, 0) lo_d, so the sum
 // over a group's queries is one product of 2 D elements with Q+ = sum max(q, 0) and Q- = sum min(q, 0): as cheap for 16 query heads as for
 // one.  It is formed in 64 bits, where the rounding to 32 bits that the pages are ranked by does not depend on the order of the sum.
+#include <algorithm>
+
 #include "mixkv_paged.h"
+#include "mixkv_topsel.h"
 
 namespace mixkv {
 
@@ -12,76 +15,153 @@ struct SelTable { PCache c[kLayersPerLaunch]; SelLayer l[kLayersPerLaunch]; };
 
 constexpr int kSelThreads = 256;
 
-// Order of the scores as unsigned numbers; the zeros are one.
-__device__ __forceinline__ uint32_t score_key(float x) {
-  const uint32_t b = __float_as_uint(x + 0.f);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+// Sums of eight doubles over aligned groups of L lanes: in every step a lane hands half of what it has to its partner and adds the partner's
+// other half, so that three steps leave it one of the eight (that of index 4 (lane & 1) + (lane & 2) + (lane / 4 & 1)).
+template <int L>
+__device__ __forceinline__ double scatter_sum(double (&v)[8], int lane) {
+#pragma unroll
+  for (int n = 4; n >= 1; n >>= 1) {
+    const int off = 4 / n;
+    const bool up = (lane & off) != 0;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const double keep = up ? v[n + i] : v[i], give = up ? v[i] : v[n + i];
+      v[i] = keep + __shfl_xor(give, off);
+    }
+  }
+  double x = v[0];
+#pragma unroll
+  for (int off = 8; off < L; off <<= 1) x += __shfl_xor(x, off);
+  return x;
 }
 
-template <int DT>
-__device__ __forceinline__ double element_of(const void *p, int64_t i) {
-  if constexpr (DT == MIXKV_BF16) return __uint_as_float((uint32_t)static_cast<const uint16_t *>(p)[i] << 16);
-  else return static_cast<const float *>(p)[i];
-}
-
-// One workgroup per (layer, sequence, KV head) and worker; a wave per page.
+// ------------------------------------------------------------------------------------------------
+// page_score_kernel: order keys of the pages' scores.  A page's bounds are 2 D neighbouring elements: L lanes take 16 bytes each and keep
+// their elements of (Q-, Q+) in registers; a wave has eight times 64 / L pages in flight.
+// ------------------------------------------------------------------------------------------------
 template <int DT, int D>
-__global__ __launch_bounds__(kSelThreads) void page_score_kernel(PShape s, SelTable tab, uint32_t *keys, int64_t unit0) {
-  __shared__ double up[D], down[D];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int layer = blockIdx.x / s.units_per_layer, u = blockIdx.x - layer * s.units_per_layer;
+__global__ __launch_bounds__(kSelThreads) void page_score_kernel(PShape s, SelTable tab, uint32_t *keys, int64_t unit0, int stride, int steps) {
+  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, E = 16 / EB, L = 2 * D * EB / 16, PPW = 64 / L, PAGES = 8 * PPW;
+  static_assert(L >= 16 && L <= 64, "a page's bounds are read by a group of lanes");
+  __shared__ double qsum[2][D];                           // Q-, Q+
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, u = blockIdx.x, layer = blockIdx.z;
   const int b = u / s.hkv, h = u - b * s.hkv;
   const PCache c = tab.c[layer];
-  const int np = (head_rows(s, c, u) + s.P - 1) >> s.lp;
-  for (int d = tid; d < D; d += kSelThreads) {
-    double p = 0., m = 0.;
+  int page0 = (blockIdx.y * steps * 4 + wave) * PAGES;    // the wave's first page of its first step
+  const int len = head_rows(s, c, u), np = (len + s.P - 1) >> s.lp;
+  if ((int64_t)blockIdx.y * steps * 4 * PAGES >= np) return;
+  for (int i = tid; i < 2 * D; i += kSelThreads) {
+    const int side = i / D, d = i - side * D;
+    const char *q = static_cast<const char *>(tab.l[layer].Q) + ((int64_t)(b * s.hq + h * s.G) * D + d) * EB;
+    double x = 0.;
     for (int g = 0; g < s.G; ++g) {
-      const double q = element_of<DT>(tab.l[layer].Q, (int64_t)(b * s.hq + h * s.G + g) * D + d);
-      p += q > 0. ? q : 0.;
-      m += q < 0. ? q : 0.;
+      float v;
+      if constexpr (DT == MIXKV_BF16) v = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(q + g * D * EB) << 16);
+      else v = *reinterpret_cast<const float *>(q + g * D * EB);
+      x += side ? fmaxf(v, 0.f) : fminf(v, 0.f);
     }
-    up[d] = p; down[d] = m;
+    qsum[side][d] = x;
   }
   __syncthreads();
-  uint32_t *out = keys + (unit0 + blockIdx.x) * s.max_pages;
-  for (int i = blockIdx.y * 4 + wave; i < np; i += gridDim.y * 4) {
-    const int id = page_at(s, c, u, i);
-    double x = 0.;
-    if (id >= 0)
-      for (int d = lane; d < D; d += 64)
-        x += (up[d] != 0. ? up[d] * element_of<DT>(c.bounds, ((int64_t)id * 2 + 1) * D + d) : 0.) +
-             (down[d] != 0. ? down[d] * element_of<DT>(c.bounds, (int64_t)id * 2 * D + d) : 0.);
+  const int part = lane % L, group = lane / L;
+  double q[E];
+  bool on[E];                                             // a bound that meets a zero counts nothing, whatever it is
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) x += __shfl_xor(x, off);
-    if (lane == 0) out[i] = id >= 0 ? score_key((float)x) : 0u;
+  for (int e = 0; e < E; ++e) { q[e] = (&qsum[0][0])[part * E + e]; on[e] = q[e] != 0.; }
+  uint32_t *out = keys + (unit0 + (int64_t)layer * s.units_per_layer + u) * stride;
+  for (int st = 0; st < steps && page0 < np; ++st, page0 += 4 * PAGES) {
+    const int entry = lane < PAGES ? page_at(s, c, u, min(page0 + lane, np - 1)) : -1;      // lane i: page i of the step
+    u32x4 r[8];
+    int id[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      id[j] = __shfl(entry, j * PPW + group);
+      r[j] = load_vec<true>(c.bounds + (int64_t)max(id[j], 0) * (2 * D * EB) + part * 16);
+    }
+    double v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      v[j] = 0.;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        float x;
+        if constexpr (DT == MIXKV_BF16) x = __uint_as_float(e & 1 ? r[j][e >> 1] & 0xffff0000u : r[j][e >> 1] << 16);
+        else x = __uint_as_float(r[j][e]);
+        v[j] = fma(q[e], (double)(on[e] ? x : 0.f), v[j]);
+      }
+      if (id[j] < 0) v[j] = -INFINITY;                    // a place without a page (its lanes agree)
+    }
+    const float x = (float)scatter_sum<L>(v, lane);
+    const int j = 4 * (lane & 1) + (lane & 2) + ((lane >> 2) & 1), i = page0 + j * PPW + group;
+    if (part < 8 && i < np) out[i] = order_key_u(x);
   }
 }
 
-// The best `keep` pages of a head: the pages in between the forced ones are counted by their key, eight bits at a time, until the
-// key of the last kept one is known; pages of that key are taken from the front.
-__global__ __launch_bounds__(kSelThreads) void page_top_kernel(PShape s, SelTable tab, const uint32_t *keys, int64_t unit0, int keep, int first, int last) {
-  __shared__ int count[256], wsum[4][2], found[2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int layer = blockIdx.x / s.units_per_layer, u = blockIdx.x - layer * s.units_per_layer;
+// The pages of a head that are kept whatever their score: [0, first) and [np - last, np) beside `need` of those in between; false: all are kept.
+__device__ __forceinline__ bool forced_pages(const PShape &s, const PCache &c, const SelLayer &L, int u, int keep, int first, int last, int *np,
+                                             int threads) {
+  *np = (head_rows(s, c, u) + s.P - 1) >> s.lp;
+  int32_t *sel = L.selected + (int64_t)u * keep;
+  if (threadIdx.x == 0) L.n_selected[u] = min(*np, keep);
+  if (*np <= keep) {
+    for (int i = threadIdx.x; i < keep; i += threads) sel[i] = i < *np ? i : -1;
+    return false;
+  }
+  for (int i = threadIdx.x; i < first; i += threads) sel[i] = i;
+  for (int i = threadIdx.x; i < last; i += threads) sel[keep - last + i] = *np - last + i;
+  return true;
+}
+
+// ------------------------------------------------------------------------------------------------
+// page_top_kernel: the best pages of a head by the threshold search of mixkv_topsel.h, a thread to EPT neighbouring pages.
+// ------------------------------------------------------------------------------------------------
+template <int THREADS, int EPT>
+__global__ __launch_bounds__(THREADS) void page_top_kernel(PShape s, SelTable tab, const uint32_t *keys, int64_t unit0, int stride, int keep, int first,
+                                                           int last) {
+  __shared__ MsScratch sc;
+  const int u = blockIdx.x, layer = blockIdx.z, base = threadIdx.x * EPT;
   const PCache c = tab.c[layer];
   const SelLayer L = tab.l[layer];
-  int32_t *sel = L.selected + (int64_t)u * keep;
-  const int np = (head_rows(s, c, u) + s.P - 1) >> s.lp, kept = min(np, keep);
-  if (tid == 0) L.n_selected[u] = kept;
-  if (np <= keep) {
-    for (int i = tid; i < keep; i += kSelThreads) sel[i] = i < np ? i : -1;
-    return;
+  const uint32_t *in = keys + (unit0 + (int64_t)layer * s.units_per_layer + u) * stride;
+  u32x4 raw[EPT / 4];
+#pragma unroll
+  for (int e = 0; e < EPT / 4; ++e) raw[e] = reinterpret_cast<const u32x4 *>(in)[min(base / 4 + e, stride / 4 - 1)];
+  int np;
+  if (!forced_pages(s, c, L, u, keep, first, last, &np, THREADS) || keep == first + last) return;
+  uint32_t key[EPT];
+  KeyRange range;
+#pragma unroll
+  for (int e = 0; e < EPT; ++e) {
+    const bool in_between = base + e >= first && base + e < np - last;
+    key[e] = in_between ? raw[e >> 2][e & 3] : 0u;
+    range.add_or_none(key[e], in_between);
   }
-  const uint32_t *in = keys + (unit0 + blockIdx.x) * s.max_pages;
+  thresholds_begin<THREADS>(range, sc);
+  __syncthreads();
+  top_select_keys<THREADS, EPT>(key, keep - first - last, L.selected + (int64_t)u * keep + first, nullptr, 0, sc, [&](int e) { return base + e; });
+}
+
+// The same for more pages than a workgroup holds in registers, counted by their key, eight bits at a time, until the key of the last
+// kept one is known; pages of that key are taken from the front.
+__global__ __launch_bounds__(kSelThreads) void page_top_long_kernel(PShape s, SelTable tab, const uint32_t *keys, int64_t unit0, int stride, int keep,
+                                                                    int first, int last) {
+  __shared__ int count[256], wsum[4][2], found[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, u = blockIdx.x, layer = blockIdx.z;
+  const PCache c = tab.c[layer];
+  const SelLayer L = tab.l[layer];
+  int np;
+  if (!forced_pages(s, c, L, u, keep, first, last, &np, kSelThreads) || keep == first + last) return;
+  const uint32_t *in = keys + (unit0 + (int64_t)layer * s.units_per_layer + u) * stride;
+  int32_t *sel = L.selected + (int64_t)u * keep + first;
   const int a = first, z = np - last;                  // pages [a, z) compete for `need` places
   int need = keep - first - last;
   uint32_t prefix = 0;
-  for (int shift = 24; shift >= 0 && need > 0; shift -= 8) {
-    for (int i = tid; i < 256; i += kSelThreads) count[i] = 0;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    count[tid] = 0;
     __syncthreads();
-    for (int i = a + tid; i < z; i += kSelThreads) {
-      const uint32_t k = in[i];
-      if (shift == 24 || k >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&count[(k >> shift) & 255], 1);
+    for (int i0 = a; i0 < z; i0 += kSelThreads) {
+      const uint32_t k = i0 + tid < z ? in[i0 + tid] : 0u;
+      hist_add(count, (k >> shift) & 255, i0 + tid < z && (shift == 24 || k >> (shift + 8) == prefix >> (shift + 8)));
     }
     __syncthreads();
     if (tid == 0) {
@@ -94,35 +174,29 @@ __global__ __launch_bounds__(kSelThreads) void page_top_kernel(PShape s, SelTabl
     need = found[1];
     __syncthreads();
   }
-  // need of the pages with key == prefix, and all above it
-  const bool any = keep > first + last;
-  int at = 0, ties = 0;
-  for (int i0 = 0; i0 < np; i0 += kSelThreads) {
-    const int i = i0 + tid;
-    bool take = i < np && (i < a || i >= z), tie = false;
-    if (!take && i < np && any) {
-      const uint32_t k = in[i];
-      take = k > prefix;
-      tie = k == prefix;
-    }
+  int at = 0, ties = 0;                                 // need of the pages with key == prefix, and all above it
+  for (int i0 = a; i0 < z; i0 += kSelThreads) {
+    const uint32_t k = i0 + tid < z ? in[i0 + tid] : 0u;
+    const bool tie = i0 + tid < z && k == prefix;
     const uint64_t tb = __builtin_amdgcn_ballot_w64(tie), below = ((uint64_t)1 << lane) - 1;
     if (lane == 0) wsum[wave][0] = __popcll(tb);
     __syncthreads();
     int t = ties + __popcll(tb & below), t_all = 0;
     for (int w = 0; w < 4; ++w) { t_all += wsum[w][0]; if (w < wave) t += wsum[w][0]; }
-    take |= tie && t < need;
+    const bool take = i0 + tid < z && (k > prefix || (tie && t < need));
     ties += t_all;
     const uint64_t kb = __builtin_amdgcn_ballot_w64(take);
     if (lane == 0) wsum[wave][1] = __popcll(kb);
     __syncthreads();
     int o = at + __popcll(kb & below), o_all = 0;
     for (int w = 0; w < 4; ++w) { o_all += wsum[w][1]; if (w < wave) o += wsum[w][1]; }
-    if (take) sel[o] = i;
+    if (take) sel[o] = i0 + tid;
     at += o_all;
   }
 }
 
-static size_t select_bytes(const PShape &s, int n_layers) { return (size_t)n_layers * s.units_per_layer * s.max_pages * 4; }
+static int key_stride(const PShape &s) { return (s.max_pages + 3) / 4 * 4; }
+static size_t select_bytes(const PShape &s, int n_layers) { return (size_t)n_layers * s.units_per_layer * key_stride(s) * 4; }
 
 }  // namespace mixkv
 
@@ -166,13 +240,22 @@ extern "C" mixkv_status mixkv_paged_select(const mixkv_paged_params *params, con
       t.l[l] = SelLayer{layers[l0 + l].Q, layers[l0 + l].selected, layers[l0 + l].n_selected};
     }
     const int64_t units = (int64_t)nl * s.units_per_layer, unit0 = (int64_t)l0 * s.units_per_layer;
-    int64_t w = (s.max_pages + 15) / 16, most = 8192 / units < 1 ? 1 : 8192 / units;
-    if (w > most) w = most;
-    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)units, (unsigned)w), dim3(kSelThreads), 0, stream, s, t, keys, unit0); };
-    if (params->dtype == MIXKV_BF16) { if (s.D == 128) go(page_score_kernel<MIXKV_BF16, 128>); else go(page_score_kernel<MIXKV_BF16, 64>); }
-    else { if (s.D == 128) go(page_score_kernel<MIXKV_F32, 128>); else go(page_score_kernel<MIXKV_F32, 64>); }
-    hipLaunchKernelGGL(page_top_kernel, dim3((unsigned)units), dim3(kSelThreads), 0, stream, s, t, (const uint32_t *)keys, unit0, max_selected, keep_first,
-                       keep_last);
+    const int stride = key_stride(s), eb = params->dtype == MIXKV_BF16 ? 2 : 4;
+    // a workgroup's pages a step, and steps, of which one costs less than the sums over the queries that come before them
+    const int pages = 4 * 8 * (64 / (2 * s.D * eb / 16));
+    const int64_t all = (s.max_pages + pages - 1) / pages;
+    const int64_t steps = std::min<int64_t>(std::max<int64_t>((all * units + 2047) / 2048, all / 65535 + 1), std::max<int64_t>(8, all / 65535 + 1));
+    const dim3 grid((unsigned)s.units_per_layer, (unsigned)((all + steps - 1) / steps), (unsigned)nl), one((unsigned)s.units_per_layer, 1, (unsigned)nl);
+    auto score = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(kSelThreads), 0, stream, s, t, keys, unit0, stride, (int)steps); };
+    if (params->dtype == MIXKV_BF16) { if (s.D == 128) score(page_score_kernel<MIXKV_BF16, 128>); else score(page_score_kernel<MIXKV_BF16, 64>); }
+    else { if (s.D == 128) score(page_score_kernel<MIXKV_F32, 128>); else score(page_score_kernel<MIXKV_F32, 64>); }
+    auto top = [&](auto kern, int threads) {
+      hipLaunchKernelGGL(kern, one, dim3(threads), 0, stream, s, t, (const uint32_t *)keys, unit0, stride, max_selected, keep_first, keep_last);
+    };
+    if (stride <= 1024) top(page_top_kernel<256, 4>, 256);
+    else if (stride <= 4096) top(page_top_kernel<512, 8>, 512);
+    else if (stride <= 16384) top(page_top_kernel<1024, 16>, 1024);
+    else top(page_top_long_kernel, kSelThreads);
     if (hipGetLastError() != hipSuccess) return MIXKV_ERR_HIP;
   }
   return MIXKV_OK;

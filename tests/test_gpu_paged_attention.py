@@ -375,3 +375,26 @@ def test_python_refuses_what_the_pointers_do_not_say():
         with pytest.raises(B.MixkvError) as e:
             bad()
         assert e.value.status == B.MIXKV_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("pages,distinct", [(1023, 1023), (1025, 40), (4100, 4100), (4096, 7), (16384, 3000), (16390, 500), (40001, 40001)])
+def test_selection_among_many_pages(dtype, D, pages, distinct):
+    # every kernel that ranks, with few and with many equal scores; a head of few pages beside the long one
+    rng = np.random.default_rng([24, pages])
+    P, G = 32, 3
+    lay = T.Layer(rng, "rows", dtype, D, P, [[P, P]], pages, spare=distinct - 2, bounds=True)
+    lay.lengths[0] = [pages * P - 5, 70]
+    lay.table[0] = rng.integers(0, lay.n_pages, (2, pages))
+    if pages < 5000:
+        lay.table[0, 0, 17:30] = -1
+    lay.bounds.sort(axis=1)
+    Q = _queries(rng, lay, 2 * G)
+    table, lengths, bounds = T.i32(lay.table), T.i32(lay.lengths), T.to_device(lay.bounds, dtype)
+    cache = B.PagedCache(None, None, table, lengths, bounds)
+    scores = [O.page_scores(Q, lay.bounds, lay.table, lay.lengths, P, 0, h) for h in range(2)]
+    for keep, first, last in ((16, 1, 1), (1000, 3, 4), (pages - 1, 0, 1), (2, 1, 1)):
+        (sel,), (n,) = B.mixkv_paged_select(lay.params(2 * G), [cache], [T.to_device(Q, dtype)], keep, first, last)
+        for h in range(2):
+            want = O.select(scores[h], keep, first, last)
+            assert n[0, h] == len(want) and sel[0, h].tolist() == want + [-1] * (keep - len(want)), (keep, h)
