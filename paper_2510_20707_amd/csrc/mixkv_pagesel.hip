@@ -17,18 +17,20 @@ constexpr int kSelThreads = 256;
 
 // Sums of eight doubles over aligned groups of L lanes: in every step a lane hands half of what it has to its partner and adds the partner's
 // other half, so that three steps leave it one of the eight (that of index 4 (lane & 1) + (lane & 2) + (lane / 4 & 1)).
+template <int N, int OFF>
+__device__ __forceinline__ void scatter_step(double (&v)[8], int lane) {
+  const bool up = (lane & OFF) != 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const double keep = up ? v[N + i] : v[i], give = up ? v[i] : v[N + i];
+    v[i] = keep + __shfl_xor(give, OFF);
+  }
+}
 template <int L>
 __device__ __forceinline__ double scatter_sum(double (&v)[8], int lane) {
-#pragma unroll
-  for (int n = 4; n >= 1; n >>= 1) {
-    const int off = 4 / n;
-    const bool up = (lane & off) != 0;
-#pragma unroll
-    for (int i = 0; i < n; ++i) {
-      const double keep = up ? v[n + i] : v[i], give = up ? v[i] : v[n + i];
-      v[i] = keep + __shfl_xor(give, off);
-    }
-  }
+  scatter_step<4, 1>(v, lane);
+  scatter_step<2, 2>(v, lane);
+  scatter_step<1, 4>(v, lane);
   double x = v[0];
 #pragma unroll
   for (int off = 8; off < L; off <<= 1) x += __shfl_xor(x, off);
@@ -47,13 +49,28 @@ __global__ __launch_bounds__(kSelThreads) void page_score_kernel(PShape s, SelTa
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, u = blockIdx.x, layer = blockIdx.z;
   const int b = u / s.hkv, h = u - b * s.hkv;
   const PCache c = tab.c[layer];
-  int page0 = (blockIdx.y * steps * 4 + wave) * PAGES;    // the wave's first page of its first step
+  const int64_t begin = (int64_t)blockIdx.y * steps * 4 * PAGES;
+  int page0 = (int)begin + wave * PAGES;                  // the wave's first page of its first step
+  // lane i: the table's entry of page i of a step, asked for a step ahead; the first one does not wait for the head's length
+  auto entry_of = [&](int first) { return lane < PAGES ? c.table[(int64_t)u * s.max_pages + min(first + lane, s.max_pages - 1)] : -1; };
+  int entry = entry_of(page0);
   const int len = head_rows(s, c, u), np = (len + s.P - 1) >> s.lp;
-  if ((int64_t)blockIdx.y * steps * 4 * PAGES >= np) return;
+  if (begin >= np) return;
+  const int part = lane % L, group = lane / L;
+  u32x4 r[8];
+  auto load = [&]() {
+    const int page = (uint32_t)entry < (uint32_t)s.n_pages ? entry : 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = load_vec<true>(c.bounds + (int64_t)__shfl(page, j * PPW + group) * (2 * D * EB) + part * 16);
+  };
+  load();
+  int loaded = entry;                                     // the entries of what is loaded
+  entry = entry_of(page0 + 4 * PAGES);
   for (int i = tid; i < 2 * D; i += kSelThreads) {
     const int side = i / D, d = i - side * D;
     const char *q = static_cast<const char *>(tab.l[layer].Q) + ((int64_t)(b * s.hq + h * s.G) * D + d) * EB;
     double x = 0.;
+#pragma unroll 8
     for (int g = 0; g < s.G; ++g) {
       float v;
       if constexpr (DT == MIXKV_BF16) v = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t *>(q + g * D * EB) << 16);
@@ -63,37 +80,41 @@ __global__ __launch_bounds__(kSelThreads) void page_score_kernel(PShape s, SelTa
     qsum[side][d] = x;
   }
   __syncthreads();
-  const int part = lane % L, group = lane / L;
   double q[E];
-  bool on[E];                                             // a bound that meets a zero counts nothing, whatever it is
 #pragma unroll
-  for (int e = 0; e < E; ++e) { q[e] = (&qsum[0][0])[part * E + e]; on[e] = q[e] != 0.; }
+  for (int e = 0; e < E; ++e) q[e] = (&qsum[0][0])[part * E + e];
+  auto bound_of = [&](int j, int e) {
+    if constexpr (DT == MIXKV_BF16) return __uint_as_float(e & 1 ? r[j][e >> 1] & 0xffff0000u : r[j][e >> 1] << 16);
+    else return __uint_as_float(r[j][e]);
+  };
   uint32_t *out = keys + (unit0 + (int64_t)layer * s.units_per_layer + u) * stride;
   for (int st = 0; st < steps && page0 < np; ++st, page0 += 4 * PAGES) {
-    const int entry = lane < PAGES ? page_at(s, c, u, min(page0 + lane, np - 1)) : -1;      // lane i: page i of the step
-    u32x4 r[8];
-    int id[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      id[j] = __shfl(entry, j * PPW + group);
-      r[j] = load_vec<true>(c.bounds + (int64_t)max(id[j], 0) * (2 * D * EB) + part * 16);
-    }
-    double v[8];
+    double v[8], all = 0.;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       v[j] = 0.;
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        float x;
-        if constexpr (DT == MIXKV_BF16) x = __uint_as_float(e & 1 ? r[j][e >> 1] & 0xffff0000u : r[j][e >> 1] << 16);
-        else x = __uint_as_float(r[j][e]);
-        v[j] = fma(q[e], (double)(on[e] ? x : 0.f), v[j]);
+      for (int e = 0; e < E; ++e) v[j] = fma(q[e], (double)bound_of(j, e), v[j]);
+      all += v[j];
+    }
+    if (__builtin_amdgcn_ballot_w64(all != all) != 0) {   // an infinity that may have met a zero: such a bound counts nothing
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        asm volatile("" : "+v"(r[j]));                      // not ahead of the branch
+        v[j] = 0.;
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[j] = fma(q[e], (double)(q[e] != 0. ? bound_of(j, e) : 0.f), v[j]);
       }
-      if (id[j] < 0) v[j] = -INFINITY;                    // a place without a page (its lanes agree)
+    }
+    const int j = 4 * (lane & 1) + (lane & 2) + ((lane >> 2) & 1), i = page0 + j * PPW + group;   // the sum that the lane is left with
+    const bool there = (uint32_t)__shfl(loaded, j * PPW + group) < (uint32_t)s.n_pages;
+    if (st + 1 < steps && page0 + 4 * PAGES < np) {
+      load();
+      loaded = entry;
+      entry = entry_of(page0 + 8 * PAGES);
     }
     const float x = (float)scatter_sum<L>(v, lane);
-    const int j = 4 * (lane & 1) + (lane & 2) + ((lane >> 2) & 1), i = page0 + j * PPW + group;
-    if (part < 8 && i < np) out[i] = order_key_u(x);
+    if (part < 8 && i < np) out[i] = order_key_u(there ? x : -INFINITY);
   }
 }
 
