@@ -377,7 +377,7 @@ typedef struct {
 } mixkv_paged_rows;
 
 /* Rotation of keys and queries to their positions: with the elements i and i + D/2 of a row as a pair (a, b), c and s the cosine and
- * sine of its angle, (a c - b s, b c + a s), in 64 bits, rounded once to the dtype.  The angle of pair i is that of
+ * sine of its angle, (a c - b s, b c + a s), in 64 bits, rounded to fp32 and from there to the dtype.  The angle of pair i is that of
  * positions[axis][r] for the row's index r: axis 0 everywhere (n_axes 1), or (n_axes 3) axis 0 for the first sections[0] pairs, 1 for
  * the next sections[1], 2 for the last sections[2] (time, height and width of vision-language models).  Positions are
  * clamped to the tables.  Shared by the layers of a call. */

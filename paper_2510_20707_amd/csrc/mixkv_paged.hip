@@ -1,14 +1,15 @@
 // The paged cache: rows into pages (mixkv_paged_append), and out of them (mixkv_paged_read).
 //
-// Both kernels give a workgroup the pages of one (layer, sequence, KV head), one page at a time, so that what a page's rows
-// share (the words of a 4-bit value strip, the key bounds) has one writer.  D/16 lanes hold a row: lane j the elements
-// [8 j, 8 j + 8) and [D/2 + 8 j, D/2 + 8 j + 8), the two halves of eight rotated pairs.
+// What the rows of a page share (the words of a 4-bit value strip, the key bounds) has one writer: the workgroup that has the page, or, where a
+// head gets a few rows, the lanes that walk them.  D/16 lanes hold a row: lane j the elements [8 j, 8 j + 8) and
+// [D/2 + 8 j, D/2 + 8 j + 8), the two halves of eight rotated pairs.
 #include "mixkv_paged.h"
 
 namespace mixkv {
 
 constexpr int kPagedLayers = 16;         // pointer-table entries of a launch: the dense rows' strides travel with them
 constexpr int kPagedThreads = 256;
+constexpr int kStepRows = 4;              // rows of a head up to which a few lanes walk them
 
 struct PRows {
   char *K, *V;
@@ -38,47 +39,34 @@ __device__ __forceinline__ RowRange row_range(const PShape &s, const PCache &c, 
   return x;
 }
 
-// Eight elements of a row.
-template <int DT>
-__device__ __forceinline__ void load_run(const char *p, float *x) {
-  if constexpr (DT == MIXKV_BF16) {
-    const u32x4 v = *reinterpret_cast<const u32x4 *>(p);
+// Eight elements of a row as memory has them, and as floats.
+template <int DT> struct Run;
+template <> struct Run<MIXKV_BF16> {
+  u32x4 v;
+  __device__ __forceinline__ void load(const char *p) { v = *reinterpret_cast<const u32x4 *>(p); }
+  __device__ __forceinline__ void store(char *p) const { *reinterpret_cast<u32x4 *>(p) = v; }
+  __device__ __forceinline__ float at(int i) const { return __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16); }
+  __device__ __forceinline__ void set(const float (&x)[8]) {            // rounded to nearest even
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(v[i] << 16);
-      x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
-    }
-  } else {
-    const f32x4 a = reinterpret_cast<const f32x4 *>(p)[0], b = reinterpret_cast<const f32x4 *>(p)[1];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
+    for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x[2 * i], (__bf16)x[2 * i + 1]});
   }
-}
-template <int DT>
-__device__ __forceinline__ void store_run(char *p, const float *x) {
-  if constexpr (DT == MIXKV_BF16) {
-    u32x4 v;
+};
+template <> struct Run<MIXKV_F32> {
+  f32x4 lo, hi;
+  __device__ __forceinline__ void load(const char *p) { lo = reinterpret_cast<const f32x4 *>(p)[0]; hi = reinterpret_cast<const f32x4 *>(p)[1]; }
+  __device__ __forceinline__ void store(char *p) const { reinterpret_cast<f32x4 *>(p)[0] = lo; reinterpret_cast<f32x4 *>(p)[1] = hi; }
+  __device__ __forceinline__ float at(int i) const { return i < 4 ? lo[i & 3] : hi[i & 3]; }
+  __device__ __forceinline__ void set(const float (&x)[8]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      v[i] = (uint32_t)f32_to_bf16_rne(x[2 * i]) | ((uint32_t)f32_to_bf16_rne(x[2 * i + 1]) << 16);
-    *reinterpret_cast<u32x4 *>(p) = v;
-  } else {
-    reinterpret_cast<f32x4 *>(p)[0] = f32x4{x[0], x[1], x[2], x[3]};
-    reinterpret_cast<f32x4 *>(p)[1] = f32x4{x[4], x[5], x[6], x[7]};
+    for (int i = 0; i < 4; ++i) { lo[i] = x[i]; hi[i] = x[4 + i]; }
   }
-}
-// A float as the dtype holds it.
-template <int DT>
-__device__ __forceinline__ float as_stored(float x) {
-  if constexpr (DT == MIXKV_BF16) return __uint_as_float((uint32_t)f32_to_bf16_rne(x) << 16);
-  return x;
-}
+};
 
-// Rotates the lane's eight pairs (a[i], b[i]), elements 8 j + i and D/2 + 8 j + i of dense row `row`.  In 64 bits: the products of
-// a table entry and an element are exact there, so the result is the rounded exact rotation whatever the order, and a row that is then
-// quantised gets the codes of its definition.  The operator is bound by memory; the 64-bit unit is idle otherwise.
-template <int DT, int D>
-__device__ __forceinline__ void rotate(const PRope &rp, int64_t row, int n_rows, int j, float *a, float *b) {
+// Cosines and sines of a lane's eight pairs, elements 8 j + i and D/2 + 8 j + i of dense row `row`.
+struct Angles { double c[8], s[8]; };
+template <int D>
+__device__ __forceinline__ void load_angles(const PRope &rp, int64_t row, int n_rows, int j, Angles &t) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {                           // four pairs at a time: 16 bytes of each table
     const int i0 = 8 * j + 4 * h;
@@ -99,12 +87,24 @@ __device__ __forceinline__ void rotate(const PRope &rp, int64_t row, int n_rows,
       }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const double x = a[4 * h + i], y = b[4 * h + i];
-      a[4 * h + i] = as_stored<DT>((float)(x * (double)c[i] - y * (double)s[i]));
-      b[4 * h + i] = as_stored<DT>((float)(y * (double)c[i] + x * (double)s[i]));
-    }
+    for (int i = 0; i < 4; ++i) { t.c[4 * h + i] = c[i]; t.s[4 * h + i] = s[i]; }
   }
+}
+// The pairs rotated.  In 64 bits: the products of a table entry and an element are exact there, so the result is the rounded exact rotation
+// whatever the order, and a row that is then quantised gets the codes of its definition.  The operator is bound by memory; the 64-bit
+// unit is idle otherwise.
+template <int DT>
+__device__ __forceinline__ void rotate(const Angles &t, Run<DT> &a, Run<DT> &b) {
+  float x[8], y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const double p = a.at(i), q = b.at(i);
+    x[i] = (float)(p * t.c[i] - q * t.s[i]);
+    y[i] = (float)(q * t.c[i] + p * t.s[i]);
+    asm("" : "+v"(x[i]), "+v"(y[i]));                     // by way of fp32: the two roundings to bf16 are not made one
+  }
+  a.set(x);
+  b.set(y);
 }
 
 // ---- 4 bits.  Step and base of a group from its extremes: the differences in 64 bits, rounded to fp32 and then to fp16.
@@ -122,13 +122,13 @@ __device__ __forceinline__ float clip(float x) { return fminf(fmaxf(x, -16384.f)
 
 // The codes of eight elements in a word.  (x - base - step) 16 / step in 32 bits is within 2^-15 of its value (the differences are at
 // most two steps and lose half a unit in the last place of that each); only where that could decide the rounding is it formed in 64 bits.
-__device__ __forceinline__ uint32_t run_codes(const float *x, const GroupScale &g) {
+__device__ __forceinline__ uint32_t run_codes(const Run<MIXKV_BF16> &x, const GroupScale &g) {
 #pragma clang fp contract(off)
   const float r = g.step > 0.f ? 16.f / g.step : 0.f;
   uint32_t w = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float v = clip(x[e]);
+    const float v = clip(x.at(e));
     const float t = ((v - g.base) - g.step) * r;
     float n = __builtin_rintf(t);
     if (fabsf(fabsf(t - n) - 0.5f) < 0x1p-12f && g.step > 0.f)
@@ -139,22 +139,162 @@ __device__ __forceinline__ uint32_t run_codes(const float *x, const GroupScale &
   return w;
 }
 
-// The extremes over the four lanes of a group.
-__device__ __forceinline__ void group_extremes(const float *x, float &lo, float &hi) {
-  lo = hi = clip(x[0]);
+// Step and base of a run's group, whose other runs lie in the neighbouring three lanes.
+__device__ __forceinline__ GroupScale run_scale(const Run<MIXKV_BF16> &x) {
+  float lo = clip(x.at(0)), hi = lo;
 #pragma unroll
-  for (int e = 1; e < 8; ++e) { const float v = clip(x[e]); lo = fminf(lo, v); hi = fmaxf(hi, v); }
+  for (int e = 1; e < 8; ++e) { const float v = clip(x.at(e)); lo = fminf(lo, v); hi = fmaxf(hi, v); }
 #pragma unroll
   for (int off = 1; off <= 2; off <<= 1) { lo = fminf(lo, __shfl_xor(lo, off)); hi = fmaxf(hi, __shfl_xor(hi, off)); }
+  return group_scale(lo, hi);
+}
+
+// Where things lie in a 4-bit page, for lane j of a row's D/16: the words of the lane's two runs in a key row and their groups' scales are
+// neighbours; a value row's element e of its strip.
+template <int D>
+struct Place4 {
+  static constexpr int NG = D / 32;
+  int j, r, e, strip;
+  int64_t codes;                                          // bytes of codes in front of the scales
+  __device__ __forceinline__ Place4(int j, int r, int P) : j(j), r(r), e(2 * (r & 3) + ((r >> 4) & 1)), strip((r >> 5) * 4 + ((r & 15) >> 2)), codes((int64_t)P * D / 2) {}
+  __device__ __forceinline__ int ga() const { return j >> 2; }              // groups of the first and the second run
+  __device__ __forceinline__ int gb() const { return (j >> 2) + NG / 2; }
+  __device__ __forceinline__ u32x2 *key_words(char *page) const { return reinterpret_cast<u32x2 *>(page + r * (D / 2) + (j & 3) * (NG * 4) + 8 * ga()); }
+  __device__ __forceinline__ u32x2 *key_scales(char *page) const { return reinterpret_cast<u32x2 *>(page + codes + (r * NG + 2 * ga()) * 4); }
+  __device__ __forceinline__ uint16_t *value_scale(char *page, int g) const { return reinterpret_cast<uint16_t *>(page + codes) + (strip * NG + g) * 16 + e; }
+  __device__ __forceinline__ uint32_t *strip_words(char *page) const { return reinterpret_cast<uint32_t *>(page) + strip * D; }
+  // the word of a strip that holds element d
+  __device__ __forceinline__ static int word_of(int d) { return (d >> 6) * 64 + (d & 15) * 4 + ((d >> 4) & 3); }
+  __device__ __forceinline__ void store_keys(char *page, const Run<MIXKV_BF16> &a, const Run<MIXKV_BF16> &b, const GroupScale &sa, const GroupScale &sb) const {
+    *key_words(page) = u32x2{run_codes(a, sa), run_codes(b, sb)};
+    if ((j & 3) == 0) *key_scales(page) = u32x2{sa.bits, sb.bits};
+  }
+  __device__ __forceinline__ void store_value_scales(char *page, const GroupScale &sa, const GroupScale &sb) const {
+    if ((j & 3) != 0) return;
+    uint16_t *a = value_scale(page, ga()), *b = value_scale(page, gb());
+    a[0] = (uint16_t)sa.bits; a[8] = (uint16_t)(sa.bits >> 16);
+    b[0] = (uint16_t)sb.bits; b[8] = (uint16_t)(sb.bits >> 16);
+  }
+};
+
+// ------------------------------------------------------------------------------------------------
+// append_step_kernel (few rows per head: a decoding step).  Every row of a (layer, sequence, KV head) that a call moves, key, value, or one of its
+// queries, is a task for D/16 lanes, which walk the head's new rows one after another: no barrier, and one writer for what rows share.
+// Bound: one chain of memory round trips (counts, table and positions, angles, the strip's old words).
+// ------------------------------------------------------------------------------------------------
+template <int DT, int D, bool Q4>
+__global__ __launch_bounds__(kPagedThreads) void append_step_kernel(PShape s, PTable tab, PRope rp, int n_rows, int tasks, int groups) {
+  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RB = D * EB;
+  const int at = blockIdx.x * (kPagedThreads / LPR) + threadIdx.x / LPR, j = threadIdx.x % LPR;
+  if (at >= groups) return;                                // whole groups of lanes
+  const int ul = at / tasks, task = at - ul * tasks;       // 0: the keys, 1: the values, then the queries
+  const int layer = ul / s.units_per_layer, u = ul - layer * s.units_per_layer, h = u % s.hkv;
+  const PCache c = tab.c[layer];
+  const PRows d = tab.r[layer];
+  const RowRange x = row_range(s, c, d, u, n_rows);
+  const bool turn = rp.cos != nullptr && task != 1;
+  for (int r = x.r0; r < x.r1; ++r) {
+    const int64_t row = r + x.shift;
+    const int place = r >> s.lp, in_page = r & (s.P - 1);
+    const int id = task < 2 ? page_at(s, c, u, place) : 0;
+    const char *src = task == 0 ? d.K + row * d.sn + h * d.sh : (task == 1 ? d.V + row * d.sn + h * d.sh : d.Q + row * d.qsn + (h * s.G + task - 2) * d.qsh);
+    Run<DT> a, b;
+    a.load(src + 8 * EB * j);
+    b.load(src + 8 * EB * (LPR + j));
+    if (turn) {
+      Angles t;
+      load_angles<D>(rp, row, n_rows, j, t);
+      rotate<DT>(t, a, b);
+    }
+    if (task >= 2) {
+      char *dst = d.Q_out + (row * s.hq + h * s.G + task - 2) * RB;
+      a.store(dst + 8 * EB * j);
+      b.store(dst + 8 * EB * (LPR + j));
+      continue;
+    }
+    if (id < 0) continue;                                  // the rows of no page are dropped
+    char *page = (task == 0 ? c.K : c.V) + (int64_t)id * s.page_bytes;
+    if constexpr (!Q4) {
+      a.store(page + (int64_t)in_page * RB + 8 * EB * j);
+      b.store(page + (int64_t)in_page * RB + 8 * EB * (LPR + j));
+    } else {
+      const Place4<D> pl(j, in_page, s.P);
+      const GroupScale sa = run_scale(a), sb = run_scale(b);
+      if (task == 0) {
+        pl.store_keys(page, a, b, sa, sb);
+      } else {
+        pl.store_value_scales(page, sa, sb);
+        const uint32_t wa = run_codes(a, sa), wb = run_codes(b, sb), sh = code_shift(pl.e);
+        uint32_t *words = pl.strip_words(page), old[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) old[i] = words[Place4<D>::word_of((i < 8 ? 0 : D / 2) + 8 * j + (i & 7))];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t code = ((i < 8 ? wa : wb) >> code_shift(i & 7)) & 15u;
+          words[Place4<D>::word_of((i < 8 ? 0 : D / 2) + 8 * j + (i & 7))] = (old[i] & ~(15u << sh)) | (code << sh);
+        }
+      }
+    }
+    if (task == 0 && c.bounds) {
+      char *lo = c.bounds + (int64_t)id * 2 * RB, *hi = lo + RB;
+      Run<DT> la = a, lb = b, ha = a, hb = b;
+      if (in_page > 0) {                                   // rows of before are in the page
+        Run<DT> o[4];
+        o[0].load(lo + 8 * EB * j); o[1].load(lo + 8 * EB * (LPR + j));
+        o[2].load(hi + 8 * EB * j); o[3].load(hi + 8 * EB * (LPR + j));
+        float v[4][8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          v[0][i] = fminf(o[0].at(i), a.at(i)); v[1][i] = fminf(o[1].at(i), b.at(i));
+          v[2][i] = fmaxf(o[2].at(i), a.at(i)); v[3][i] = fmaxf(o[3].at(i), b.at(i));
+        }
+        la.set(v[0]); lb.set(v[1]); ha.set(v[2]); hb.set(v[3]);
+      }
+      la.store(lo + 8 * EB * j); lb.store(lo + 8 * EB * (LPR + j));
+      ha.store(hi + 8 * EB * j); hb.store(hi + 8 * EB * (LPR + j));
+    }
+  }
 }
 
 // ------------------------------------------------------------------------------------------------
-// append_paged_kernel.  blockIdx.x: (layer, sequence, KV head); blockIdx.y: workers on the head's pages, then workers on its
-// query rows.
+// append_queries_kernel (many rows).  blockIdx.x: (layer, sequence, KV head); blockIdx.y: workers on its rows.  A group of lanes has a row's
+// angles, as 64-bit numbers, for all queries of the KV head's group.
+// ------------------------------------------------------------------------------------------------
+template <int DT, int D>
+__global__ __launch_bounds__(kPagedThreads) void append_queries_kernel(PShape s, PTable tab, PRope rp, int n_rows) {
+  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RS = kPagedThreads / LPR, RB = D * EB, U = 4;
+  const int j = threadIdx.x % LPR, slot = threadIdx.x / LPR;
+  const int layer = blockIdx.x / s.units_per_layer, u = blockIdx.x - layer * s.units_per_layer, h = u % s.hkv;
+  const PRows d = tab.r[layer];
+  const RowRange x = row_range(s, tab.c[layer], d, u, n_rows);
+  for (int r = x.r0 + (int)blockIdx.y * RS + slot; r < x.r1; r += (int)gridDim.y * RS) {
+    const int64_t row = r + x.shift;
+    const char *src = d.Q + row * d.qsn + (int64_t)h * s.G * d.qsh + 8 * EB * j;
+    char *dst = d.Q_out + (row * s.hq + h * s.G) * RB + 8 * EB * j;
+    Angles t;
+    if (rp.cos) load_angles<D>(rp, row, n_rows, j, t);
+    for (int g = 0; g < s.G; g += U) {
+      Run<DT> a[U], b[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (g + i < s.G) { a[i].load(src + (g + i) * d.qsh); b[i].load(src + (g + i) * d.qsh + RB / 2); }
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (g + i < s.G) {
+          if (rp.cos) rotate<DT>(t, a[i], b[i]);
+          a[i].store(dst + (g + i) * RB);
+          b[i].store(dst + (g + i) * RB + RB / 2);
+        }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------
+// append_pages_kernel (many rows).  blockIdx.x: (layer, sequence, KV head); blockIdx.y: workers on the head's pages.
 // ------------------------------------------------------------------------------------------------
 template <int DT, int D, bool Q4>
-__global__ __launch_bounds__(kPagedThreads) void append_paged_kernel(PShape s, PTable tab, PRope rp, int n_rows, int kv_workers) {
-  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RS = kPagedThreads / LPR, RB = D * EB, NG = D / 32, RUNS = D / 8;
+__global__ __launch_bounds__(kPagedThreads) void append_pages_kernel(PShape s, PTable tab, PRope rp, int n_rows) {
+  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RS = kPagedThreads / LPR, RB = D * EB, RUNS = D / 8;
   __shared__ uint32_t words[Q4 ? RS * RUNS : 1];           // codes of the value rows of a pass, a word per eight elements
   __shared__ float red[4][2][D];
   const int tid = threadIdx.x, j = tid % LPR, slot = tid / LPR, lane = tid & 63, wave = tid >> 6;
@@ -165,25 +305,7 @@ __global__ __launch_bounds__(kPagedThreads) void append_paged_kernel(PShape s, P
   const RowRange x = row_range(s, c, d, u, n_rows);
   const bool turn = rp.cos != nullptr;
 
-  if ((int)blockIdx.y >= kv_workers) {                     // ---- queries
-    const int w = blockIdx.y - kv_workers, nw = gridDim.y - kv_workers;
-    const int64_t items = (int64_t)(x.r1 - x.r0) * s.G;
-    for (int64_t i = (int64_t)w * RS + slot; i < items; i += (int64_t)nw * RS) {
-      const int t = (int)(i / s.G), g = h * s.G + (int)(i - (int64_t)t * s.G);
-      const int64_t row = x.r0 + t + x.shift;
-      const char *src = d.Q + row * d.qsn + g * d.qsh;
-      char *dst = d.Q_out + (row * s.hq + g) * RB;
-      float a[8], b[8];
-      load_run<DT>(src + 8 * EB * j, a);
-      load_run<DT>(src + 8 * EB * (LPR + j), b);
-      if (turn) rotate<DT, D>(rp, row, n_rows, j, a, b);
-      store_run<DT>(dst + 8 * EB * j, a);
-      store_run<DT>(dst + 8 * EB * (LPR + j), b);
-    }
-    return;
-  }
-
-  for (int pg = (x.r0 >> s.lp) + (int)blockIdx.y; pg << s.lp < x.r1; pg += kv_workers) {
+  for (int pg = (x.r0 >> s.lp) + (int)blockIdx.y; pg << s.lp < x.r1; pg += gridDim.y) {
     const int id = page_at(s, c, u, pg);
     if (id < 0) continue;                                  // uniform: the rows of no page are dropped
     const int first = pg << s.lp, lo_row = max(x.r0 - first, 0), hi_row = min(x.r1 - first, s.P);   // rows of the page to be written
@@ -196,53 +318,40 @@ __global__ __launch_bounds__(kPagedThreads) void append_paged_kernel(PShape s, P
       const int r = s0 + slot;
       const bool live = r >= lo_row && r < hi_row;
       const int64_t row = first + r + x.shift;
-      const char *ks = d.K + row * d.sn + h * d.sh, *vs = d.V + row * d.sn + h * d.sh;
-      float ka[8] = {}, kb[8] = {}, va[8] = {}, vb[8] = {};
+      const char *ks = d.K + row * d.sn + h * d.sh + 8 * EB * j, *vs = d.V + row * d.sn + h * d.sh + 8 * EB * j;
+      Run<DT> ka{}, kb{}, va{}, vb{};
       if (live) {
-        load_run<DT>(ks + 8 * EB * j, ka);
-        load_run<DT>(ks + 8 * EB * (LPR + j), kb);
-        load_run<DT>(vs + 8 * EB * j, va);
-        load_run<DT>(vs + 8 * EB * (LPR + j), vb);
-        if (turn) rotate<DT, D>(rp, row, n_rows, j, ka, kb);
+        ka.load(ks);
+        kb.load(ks + RB / 2);
+        va.load(vs);
+        vb.load(vs + RB / 2);
+        if (turn) {
+          Angles t;
+          load_angles<D>(rp, row, n_rows, j, t);
+          rotate<DT>(t, ka, kb);
+        }
         if (c.bounds) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            blo[i] = fminf(blo[i], ka[i]); bhi[i] = fmaxf(bhi[i], ka[i]);
-            blo[8 + i] = fminf(blo[8 + i], kb[i]); bhi[8 + i] = fmaxf(bhi[8 + i], kb[i]);
+            blo[i] = fminf(blo[i], ka.at(i)); bhi[i] = fmaxf(bhi[i], ka.at(i));
+            blo[8 + i] = fminf(blo[8 + i], kb.at(i)); bhi[8 + i] = fmaxf(bhi[8 + i], kb.at(i));
           }
         }
       }
       if constexpr (!Q4) {
         if (live) {
-          store_run<DT>(kp + (int64_t)r * RB + 8 * EB * j, ka);
-          store_run<DT>(kp + (int64_t)r * RB + 8 * EB * (LPR + j), kb);
-          store_run<DT>(vp + (int64_t)r * RB + 8 * EB * j, va);
-          store_run<DT>(vp + (int64_t)r * RB + 8 * EB * (LPR + j), vb);
+          const int64_t at = (int64_t)r * RB + 8 * EB * j;
+          ka.store(kp + at);
+          kb.store(kp + at + RB / 2);
+          va.store(vp + at);
+          vb.store(vp + at + RB / 2);
         }
       } else {
-        // group of the lane's first run is j / 4, of its second D/64 more: neighbours in a key row's words
-        const int ga = j >> 2, gb = ga + NG / 2;
-        float lo, hi;
-        group_extremes(ka, lo, hi);
-        const GroupScale ska = group_scale(lo, hi);
-        group_extremes(kb, lo, hi);
-        const GroupScale skb = group_scale(lo, hi);
-        group_extremes(va, lo, hi);
-        const GroupScale sva = group_scale(lo, hi);
-        group_extremes(vb, lo, hi);
-        const GroupScale svb = group_scale(lo, hi);
-        const int64_t codes = (int64_t)s.P * D / 2;        // bytes of codes in front of the scales
+        const GroupScale ska = run_scale(ka), skb = run_scale(kb), sva = run_scale(va), svb = run_scale(vb);
         if (live) {
-          uint32_t *kw = reinterpret_cast<uint32_t *>(kp) + r * RUNS + (j & 3) * NG + 2 * ga;
-          *reinterpret_cast<u32x2 *>(kw) = u32x2{run_codes(ka, ska), run_codes(kb, skb)};
-          if ((j & 3) == 0) {
-            *reinterpret_cast<u32x2 *>(kp + codes + (r * NG + 2 * ga) * 4) = u32x2{ska.bits, skb.bits};
-            // strip and place of the row among the strip's eight
-            const int strip = (r >> 5) * 4 + ((r & 15) >> 2), e = 2 * (r & 3) + ((r >> 4) & 1);
-            uint16_t *vsc = reinterpret_cast<uint16_t *>(vp + codes) + strip * NG * 16 + e;
-            vsc[ga * 16] = (uint16_t)sva.bits; vsc[ga * 16 + 8] = (uint16_t)(sva.bits >> 16);
-            vsc[gb * 16] = (uint16_t)svb.bits; vsc[gb * 16 + 8] = (uint16_t)(svb.bits >> 16);
-          }
+          const Place4<D> pl(j, r, s.P);
+          pl.store_keys(kp, ka, kb, ska, skb);
+          pl.store_value_scales(vp, sva, svb);
           words[slot * RUNS + j] = run_codes(va, sva);
           words[slot * RUNS + LPR + j] = run_codes(vb, svb);
         }
@@ -310,7 +419,7 @@ __global__ __launch_bounds__(kPagedThreads) void append_paged_kernel(PShape s, P
 // ------------------------------------------------------------------------------------------------
 template <int DT, int D, bool Q4>
 __global__ __launch_bounds__(kPagedThreads) void read_paged_kernel(PShape s, PTable tab, int n_rows) {
-  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RS = 32, RB = D * EB, NG = D / 32, RUNS = D / 8, THREADS = LPR * RS;
+  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RS = 32, RB = D * EB, THREADS = LPR * RS;
   const int tid = threadIdx.x, j = tid % LPR, slot = tid / LPR;
   const int layer = blockIdx.x / s.units_per_layer, u = blockIdx.x - layer * s.units_per_layer;
   const int h = u % s.hkv;
@@ -322,38 +431,36 @@ __global__ __launch_bounds__(kPagedThreads) void read_paged_kernel(PShape s, PTa
     const int id = page_at(s, c, u, (t0 * RS) >> s.lp);
     const int r = ((t0 * RS) & (s.P - 1)) + slot, at = t0 * RS + slot;   // row of the page, of the head
     if (id < 0 || at < x.r0 || at >= x.r1) continue;
-    const char *kp = c.K + (int64_t)id * s.page_bytes, *vp = c.V + (int64_t)id * s.page_bytes;
-    float ka[8], kb[8], va[8], vb[8];
+    char *kp = c.K + (int64_t)id * s.page_bytes, *vp = c.V + (int64_t)id * s.page_bytes;
+    Run<DT> ka, kb, va, vb;
     if constexpr (!Q4) {
-      load_run<DT>(kp + (int64_t)r * RB + 8 * EB * j, ka);
-      load_run<DT>(kp + (int64_t)r * RB + 8 * EB * (LPR + j), kb);
-      load_run<DT>(vp + (int64_t)r * RB + 8 * EB * j, va);
-      load_run<DT>(vp + (int64_t)r * RB + 8 * EB * (LPR + j), vb);
+      const int64_t from = (int64_t)r * RB + 8 * EB * j;
+      ka.load(kp + from);
+      kb.load(kp + from + RB / 2);
+      va.load(vp + from);
+      vb.load(vp + from + RB / 2);
     } else {
-      const int ga = j >> 2, gb = ga + NG / 2;
-      const int64_t codes = (int64_t)s.P * D / 2;
-      const u32x2 kw = *reinterpret_cast<const u32x2 *>(reinterpret_cast<const uint32_t *>(kp) + r * RUNS + (j & 3) * NG + 2 * ga);
-      const u32x2 ks = *reinterpret_cast<const u32x2 *>(kp + codes + (r * NG + 2 * ga) * 4);
-      const int strip = (r >> 5) * 4 + ((r & 15) >> 2), e = 2 * (r & 3) + ((r >> 4) & 1), sh = code_shift(e);
-      const uint16_t *vsc = reinterpret_cast<const uint16_t *>(vp + codes) + strip * NG * 16 + e;
-      const float sa = f16_value(vsc[ga * 16]), ba = f16_value(vsc[ga * 16 + 8]), sb = f16_value(vsc[gb * 16]), bb = f16_value(vsc[gb * 16 + 8]);
-      const uint32_t *vw = reinterpret_cast<const uint32_t *>(vp) + strip * D;
+      const Place4<D> pl(j, r, s.P);
+      const u32x2 kw = *pl.key_words(kp), ks = *pl.key_scales(kp);
+      const uint16_t *sa = pl.value_scale(vp, pl.ga()), *sb = pl.value_scale(vp, pl.gb());
+      const float s0 = f16_value(sa[0]), b0 = f16_value(sa[8]), s1 = f16_value(sb[0]), b1 = f16_value(sb[8]);
+      const uint32_t *vw = pl.strip_words(vp), sh = code_shift(pl.e);
+      float x0[8], x1[8], y0[8], y1[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        ka[i] = code_value((kw[0] >> code_shift(i)) & 15u, f16_value(ks[0] & 0xffffu), f16_value(ks[0] >> 16));
-        kb[i] = code_value((kw[1] >> code_shift(i)) & 15u, f16_value(ks[1] & 0xffffu), f16_value(ks[1] >> 16));
-        const int ea = 8 * j + i, eb = D / 2 + 8 * j + i;
-        const int wa = (ea >> 6) * 64 + (ea & 15) * 4 + ((ea >> 4) & 3), wb = (eb >> 6) * 64 + (eb & 15) * 4 + ((eb >> 4) & 3);
-        va[i] = code_value((vw[wa] >> sh) & 15u, sa, ba);
-        vb[i] = code_value((vw[wb] >> sh) & 15u, sb, bb);
+        x0[i] = code_value((kw[0] >> code_shift(i)) & 15u, f16_value(ks[0] & 0xffffu), f16_value(ks[0] >> 16));
+        x1[i] = code_value((kw[1] >> code_shift(i)) & 15u, f16_value(ks[1] & 0xffffu), f16_value(ks[1] >> 16));
+        y0[i] = code_value((vw[Place4<D>::word_of(8 * j + i)] >> sh) & 15u, s0, b0);
+        y1[i] = code_value((vw[Place4<D>::word_of(D / 2 + 8 * j + i)] >> sh) & 15u, s1, b1);
       }
+      ka.set(x0); kb.set(x1); va.set(y0); vb.set(y1);
     }
     const int64_t row = at + x.shift;
-    char *kd = d.K + row * d.sn + h * d.sh, *vd = d.V + row * d.sn + h * d.sh;
-    store_run<DT>(kd + 8 * EB * j, ka);
-    store_run<DT>(kd + 8 * EB * (LPR + j), kb);
-    store_run<DT>(vd + 8 * EB * j, va);
-    store_run<DT>(vd + 8 * EB * (LPR + j), vb);
+    char *kd = d.K + row * d.sn + h * d.sh + 8 * EB * j, *vd = d.V + row * d.sn + h * d.sh + 8 * EB * j;
+    ka.store(kd);
+    kb.store(kd + RB / 2);
+    va.store(vd);
+    vb.store(vd + RB / 2);
   }
 }
 
@@ -482,14 +589,27 @@ extern "C" mixkv_status mixkv_paged_append(const mixkv_paged_params *params, con
     const int nl = n_layers - l0 < kPagedLayers ? n_layers - l0 : kPagedLayers;
     const PTable t = table_of(caches + l0, rows + l0, nl, eb);
     const int64_t units = (int64_t)nl * s.units_per_layer;
-    const int kvw = workers(((int64_t)max_count + s.P - 2) / s.P + 1, units);
-    const int qw = rows[0].Q ? workers(((int64_t)max_count * s.G + 31) / 32, units) : 0;
-    auto go = [&](auto kern) {
-      hipLaunchKernelGGL(kern, dim3((unsigned)units, (unsigned)(kvw + qw)), dim3(kPagedThreads), 0, stream, s, t, rp, n_rows, kvw);
-    };
-    if (s.q4) { if (s.D == 128) go(append_paged_kernel<MIXKV_BF16, 128, true>); else go(append_paged_kernel<MIXKV_BF16, 64, true>); }
-    else if (params->dtype == MIXKV_BF16) { if (s.D == 128) go(append_paged_kernel<MIXKV_BF16, 128, false>); else go(append_paged_kernel<MIXKV_BF16, 64, false>); }
-    else { if (s.D == 128) go(append_paged_kernel<MIXKV_F32, 128, false>); else go(append_paged_kernel<MIXKV_F32, 64, false>); }
+    const bool queries = rows[0].Q != nullptr;
+    if (max_count <= kStepRows) {
+      const int tasks = 2 + (queries ? s.G : 0), per = kPagedThreads / (s.D / 16);
+      const int groups = (int)units * tasks;
+      auto go = [&](auto kern) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)((groups + per - 1) / per)), dim3(kPagedThreads), 0, stream, s, t, rp, n_rows, tasks, groups);
+      };
+      if (s.q4) { if (s.D == 128) go(append_step_kernel<MIXKV_BF16, 128, true>); else go(append_step_kernel<MIXKV_BF16, 64, true>); }
+      else if (params->dtype == MIXKV_BF16) { if (s.D == 128) go(append_step_kernel<MIXKV_BF16, 128, false>); else go(append_step_kernel<MIXKV_BF16, 64, false>); }
+      else { if (s.D == 128) go(append_step_kernel<MIXKV_F32, 128, false>); else go(append_step_kernel<MIXKV_F32, 64, false>); }
+    } else {
+      const int pw = workers(((int64_t)max_count + s.P - 2) / s.P + 1, units), qw = workers(((int64_t)max_count + 31) / 32, units);
+      auto go = [&](auto kern, auto qkern) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)units, (unsigned)pw), dim3(kPagedThreads), 0, stream, s, t, rp, n_rows);
+        if (queries) hipLaunchKernelGGL(qkern, dim3((unsigned)units, (unsigned)qw), dim3(kPagedThreads), 0, stream, s, t, rp, n_rows);
+      };
+      constexpr int B16 = MIXKV_BF16, F32 = MIXKV_F32;
+      if (s.q4) { if (s.D == 128) go(append_pages_kernel<B16, 128, true>, append_queries_kernel<B16, 128>); else go(append_pages_kernel<B16, 64, true>, append_queries_kernel<B16, 64>); }
+      else if (params->dtype == B16) { if (s.D == 128) go(append_pages_kernel<B16, 128, false>, append_queries_kernel<B16, 128>); else go(append_pages_kernel<B16, 64, false>, append_queries_kernel<B16, 64>); }
+      else { if (s.D == 128) go(append_pages_kernel<F32, 128, false>, append_queries_kernel<F32, 128>); else go(append_pages_kernel<F32, 64, false>, append_queries_kernel<F32, 64>); }
+    }
     if (hipGetLastError() != hipSuccess) return MIXKV_ERR_HIP;
   }
   return MIXKV_OK;
