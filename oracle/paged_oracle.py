@@ -41,7 +41,7 @@ def quantise(row):
     g = np.clip(row, -16384.0, 16384.0).reshape(-1, 32)
     lo, hi = g.min(1), g.max(1)
     step = ((hi - lo) * (16.0 / 15.0)).astype(np.float32).astype(np.float16)
-    base = (lo - step.astype(np.float64)).astype(np.float32).astype(np.float16)
+    base = ((lo - step.astype(np.float64)).astype(np.float32) + np.float32(0)).astype(np.float16)      # no negative zero
     s, b = step.astype(np.float64)[:, None], base.astype(np.float64)[:, None]
     with np.errstate(divide="ignore", invalid="ignore"):
         code = np.where(s > 0, np.clip(np.rint((g - b - s) * 16.0 / s), 0, 15), 0)

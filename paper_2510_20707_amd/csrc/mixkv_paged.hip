@@ -67,23 +67,25 @@ template <> struct Run<MIXKV_F32> {
 struct Angles { double c[8], s[8]; };
 template <int D>
 __device__ __forceinline__ void load_angles(const PRope &rp, int64_t row, int n_rows, int j, Angles &t) {
+  int64_t at[3];                                          // the row's place in the tables, for each axis
+#pragma unroll
+  for (int k = 0; k < 3; ++k) at[k] = k < rp.n_axes ? rp.positions[(int64_t)k * n_rows + row] : 0;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) at[k] = (int64_t)min(max((int)at[k], 0), rp.n_positions - 1) * (D / 2);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {                           // four pairs at a time: 16 bytes of each table
     const int i0 = 8 * j + 4 * h;
     f32x4 c, s;
-    if (rp.n_axes == 1 || i0 + 4 <= rp.s0 || (i0 >= rp.s0 && i0 + 4 <= rp.s1) || i0 >= rp.s1) {
-      const int axis = rp.n_axes == 1 || i0 + 4 <= rp.s0 ? 0 : (i0 >= rp.s1 ? 2 : 1);
-      const int pos = min(max(rp.positions[(int64_t)axis * n_rows + row], 0), rp.n_positions - 1);
-      const int64_t at = (int64_t)pos * (D / 2) + i0;
-      c = *reinterpret_cast<const f32x4 *>(rp.cos + at);
-      s = *reinterpret_cast<const f32x4 *>(rp.sin + at);
+    if (i0 + 4 <= rp.s0 || (i0 >= rp.s0 && i0 + 4 <= rp.s1) || i0 >= rp.s1) {
+      const int64_t p = (i0 + 4 <= rp.s0 ? at[0] : (i0 >= rp.s1 ? at[2] : at[1])) + i0;
+      c = *reinterpret_cast<const f32x4 *>(rp.cos + p);
+      s = *reinterpret_cast<const f32x4 *>(rp.sin + p);
     } else {                                              // an axis ends among the four
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int axis = i0 + i < rp.s0 ? 0 : (i0 + i < rp.s1 ? 1 : 2);
-        const int pos = min(max(rp.positions[(int64_t)axis * n_rows + row], 0), rp.n_positions - 1);
-        c[i] = rp.cos[(int64_t)pos * (D / 2) + i0 + i];
-        s[i] = rp.sin[(int64_t)pos * (D / 2) + i0 + i];
+        const int64_t p = (i0 + i < rp.s0 ? at[0] : (i0 + i < rp.s1 ? at[1] : at[2])) + i0 + i;
+        c[i] = rp.cos[p];
+        s[i] = rp.sin[p];
       }
     }
 #pragma unroll
@@ -107,46 +109,135 @@ __device__ __forceinline__ void rotate(const Angles &t, Run<DT> &a, Run<DT> &b) 
   b.set(y);
 }
 
+// Smallest and largest of each of a run's eight elements.  bf16 pairs as signed 16-bit numbers of the same order (all bits below the sign
+// turned over in negative ones), two elements an instruction.
+template <int DT> struct RunRange;
+template <> struct RunRange<MIXKV_BF16> {
+  typedef short s16x2 __attribute__((ext_vector_type(2)));
+  s16x2 lo[4], hi[4];
+  __device__ __forceinline__ static s16x2 turn(s16x2 x) { return x ^ ((x >> 15) & (short)0x7fff); }
+  __device__ __forceinline__ void none() {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { lo[i] = s16x2{0x7f80, 0x7f80}; hi[i] = turn(s16x2{(short)0xff80, (short)0xff80}); }   // the infinities
+  }
+  __device__ __forceinline__ void add(const Run<MIXKV_BF16> &x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const s16x2 v = turn(__builtin_bit_cast(s16x2, (uint32_t)x.v[i]));
+      lo[i] = __builtin_elementwise_min(lo[i], v);
+      hi[i] = __builtin_elementwise_max(hi[i], v);
+    }
+  }
+  __device__ __forceinline__ void lower(const Run<MIXKV_BF16> &x) {        // by smallest, by largest elements of before
+#pragma unroll
+    for (int i = 0; i < 4; ++i) lo[i] = __builtin_elementwise_min(lo[i], turn(__builtin_bit_cast(s16x2, (uint32_t)x.v[i])));
+  }
+  __device__ __forceinline__ void raise(const Run<MIXKV_BF16> &x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) hi[i] = __builtin_elementwise_max(hi[i], turn(__builtin_bit_cast(s16x2, (uint32_t)x.v[i])));
+  }
+  __device__ __forceinline__ void join(int off) {          // with the lane `off` away
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      lo[i] = __builtin_elementwise_min(lo[i], __builtin_bit_cast(s16x2, __shfl_xor(__builtin_bit_cast(int, lo[i]), off)));
+      hi[i] = __builtin_elementwise_max(hi[i], __builtin_bit_cast(s16x2, __shfl_xor(__builtin_bit_cast(int, hi[i]), off)));
+    }
+  }
+  __device__ __forceinline__ Run<MIXKV_BF16> low() const { return back(lo); }
+  __device__ __forceinline__ Run<MIXKV_BF16> high() const { return back(hi); }
+  __device__ __forceinline__ static Run<MIXKV_BF16> back(const s16x2 (&x)[4]) {
+    Run<MIXKV_BF16> r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.v[i] = __builtin_bit_cast(uint32_t, turn(x[i]));
+    return r;
+  }
+};
+template <> struct RunRange<MIXKV_F32> {
+  float lo[8], hi[8];
+  __device__ __forceinline__ void none() {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { lo[i] = INFINITY; hi[i] = -INFINITY; }
+  }
+  __device__ __forceinline__ void add(const Run<MIXKV_F32> &x) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { lo[i] = fminf(lo[i], x.at(i)); hi[i] = fmaxf(hi[i], x.at(i)); }
+  }
+  __device__ __forceinline__ void lower(const Run<MIXKV_F32> &x) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) lo[i] = fminf(lo[i], x.at(i));
+  }
+  __device__ __forceinline__ void raise(const Run<MIXKV_F32> &x) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) hi[i] = fmaxf(hi[i], x.at(i));
+  }
+  __device__ __forceinline__ void join(int off) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { lo[i] = fminf(lo[i], __shfl_xor(lo[i], off)); hi[i] = fmaxf(hi[i], __shfl_xor(hi[i], off)); }
+  }
+  __device__ __forceinline__ Run<MIXKV_F32> low() const { Run<MIXKV_F32> r; r.set(lo); return r; }
+  __device__ __forceinline__ Run<MIXKV_F32> high() const { Run<MIXKV_F32> r; r.set(hi); return r; }
+};
+
 // ---- 4 bits.  Step and base of a group from its extremes: the differences in 64 bits, rounded to fp32 and then to fp16.
-struct GroupScale { float step, base; uint32_t bits; };    // bits: step, and base above it
-__device__ __forceinline__ GroupScale group_scale(float lo, float hi) {
+struct GroupScale {
+  float step, base;
+  uint32_t bits;                                           // step, and base above it
+  bool wide;                                               // elements beyond the format's range
+};
+__device__ __forceinline__ float clip(float x) { return fminf(fmaxf(x, -16384.f), 16384.f); }
+__device__ __forceinline__ GroupScale group_scale(float least, float most) {
   GroupScale g;
+  const float lo = clip(least), hi = clip(most);
+  g.wide = lo != least || hi != most;
   const uint32_t sb = f16_bits((float)(((double)hi - (double)lo) * (16.0 / 15.0)));
   g.step = f16_value(sb);
-  const uint32_t bb = f16_bits((float)((double)lo - (double)g.step));
+  const uint32_t bb = f16_bits((float)((double)lo - (double)g.step) + 0.f);       // no negative zero
   g.base = f16_value(bb);
   g.bits = sb | (bb << 16);
   return g;
 }
-__device__ __forceinline__ float clip(float x) { return fminf(fmaxf(x, -16384.f), 16384.f); }
-
-// The codes of eight elements in a word.  (x - base - step) 16 / step in 32 bits is within 2^-15 of its value (the differences are at
-// most two steps and lose half a unit in the last place of that each); only where that could decide the rounding is it formed in 64 bits.
-__device__ __forceinline__ uint32_t run_codes(const Run<MIXKV_BF16> &x, const GroupScale &g) {
-#pragma clang fp contract(off)
-  const float r = g.step > 0.f ? 16.f / g.step : 0.f;
-  uint32_t w = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float v = clip(x.at(e));
-    const float t = ((v - g.base) - g.step) * r;
-    float n = __builtin_rintf(t);
-    if (fabsf(fabsf(t - n) - 0.5f) < 0x1p-12f && g.step > 0.f)
-      n = (float)__builtin_rint(((double)v - (double)g.base - (double)g.step) * 16.0 / (double)g.step);
-    const uint32_t code = (uint32_t)fminf(fmaxf(n, 0.f), 15.f);
-    w |= code << code_shift(e);
-  }
-  return w;
-}
-
 // Step and base of a run's group, whose other runs lie in the neighbouring three lanes.
 __device__ __forceinline__ GroupScale run_scale(const Run<MIXKV_BF16> &x) {
-  float lo = clip(x.at(0)), hi = lo;
+  typedef RunRange<MIXKV_BF16> R;
+  R::s16x2 v[4], lo, hi;
 #pragma unroll
-  for (int e = 1; e < 8; ++e) { const float v = clip(x.at(e)); lo = fminf(lo, v); hi = fmaxf(hi, v); }
+  for (int i = 0; i < 4; ++i) v[i] = R::turn(__builtin_bit_cast(R::s16x2, (uint32_t)x.v[i]));
+  lo = __builtin_elementwise_min(__builtin_elementwise_min(v[0], v[1]), __builtin_elementwise_min(v[2], v[3]));
+  hi = __builtin_elementwise_max(__builtin_elementwise_max(v[0], v[1]), __builtin_elementwise_max(v[2], v[3]));
 #pragma unroll
-  for (int off = 1; off <= 2; off <<= 1) { lo = fminf(lo, __shfl_xor(lo, off)); hi = fmaxf(hi, __shfl_xor(hi, off)); }
-  return group_scale(lo, hi);
+  for (int off = 1; off <= 2; off <<= 1) {
+    lo = __builtin_elementwise_min(lo, __builtin_bit_cast(R::s16x2, __shfl_xor(__builtin_bit_cast(int, lo), off)));
+    hi = __builtin_elementwise_max(hi, __builtin_bit_cast(R::s16x2, __shfl_xor(__builtin_bit_cast(int, hi), off)));
+  }
+  const R::s16x2 ends = R::turn(R::s16x2{lo[0] < lo[1] ? lo[0] : lo[1], hi[0] > hi[1] ? hi[0] : hi[1]});
+  const uint32_t w = __builtin_bit_cast(uint32_t, ends);
+  return group_scale(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+
+// The codes of eight elements in a word.  16 (x - base - step) / step as one multiply-add with 16 / step is off by at most 2^-22 of what its
+// product and its constant are together (the quotient, the constant and the sum are rounded by 2^-24 each); where that could decide a
+// rounding, or elements have to be clipped, the run's codes are formed in 64 bits: one run of some thousands.
+__device__ __forceinline__ uint32_t run_codes(const Run<MIXKV_BF16> &x, const GroupScale &g) {
+  const float r = g.step > 0.f ? 16.f / g.step : 0.f, k = -(g.base + g.step) * r;
+  uint32_t w = 0;
+  float off = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float t = fmaf(x.at(e), r, k), n = __builtin_rintf(t);
+    off = __builtin_fmaxf(off, __builtin_fabsf(t - n));
+    w |= (uint32_t)__builtin_amdgcn_fmed3f(n, 0.f, 15.f) << code_shift(e);
+  }
+  if ((g.wide || off > 0.5f - 0x1p-22f * (40.f + 2.f * fabsf(k))) && g.step > 0.f) {
+    w = 0;
+#pragma unroll 1
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t q = e < 2 ? x.v[0] : (e < 4 ? x.v[1] : (e < 6 ? x.v[2] : x.v[3]));
+      const double v = clip(__uint_as_float(e & 1 ? q & 0xffff0000u : q << 16));
+      const double n = __builtin_rint((v - (double)g.base - (double)g.step) * 16.0 / (double)g.step);
+      w |= (uint32_t)(n < 0. ? 0. : (n > 15. ? 15. : n)) << code_shift(e);
+    }
+  }
+  return w;
 }
 
 // Where things lie in a 4-bit page, for lane j of a row's D/16: the words of the lane's two runs in a key row and their groups' scales are
@@ -239,16 +330,15 @@ __global__ __launch_bounds__(kPagedThreads) void append_step_kernel(PShape s, PT
       char *lo = c.bounds + (int64_t)id * 2 * RB, *hi = lo + RB;
       Run<DT> la = a, lb = b, ha = a, hb = b;
       if (in_page > 0) {                                   // rows of before are in the page
+        RunRange<DT> ra, rb;
         Run<DT> o[4];
         o[0].load(lo + 8 * EB * j); o[1].load(lo + 8 * EB * (LPR + j));
         o[2].load(hi + 8 * EB * j); o[3].load(hi + 8 * EB * (LPR + j));
-        float v[4][8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          v[0][i] = fminf(o[0].at(i), a.at(i)); v[1][i] = fminf(o[1].at(i), b.at(i));
-          v[2][i] = fmaxf(o[2].at(i), a.at(i)); v[3][i] = fmaxf(o[3].at(i), b.at(i));
-        }
-        la.set(v[0]); lb.set(v[1]); ha.set(v[2]); hb.set(v[3]);
+        ra.none(); rb.none();
+        ra.add(a); rb.add(b);
+        ra.lower(o[0]); rb.lower(o[1]);
+        ra.raise(o[2]); rb.raise(o[3]);
+        la = ra.low(); lb = rb.low(); ha = ra.high(); hb = rb.high();
       }
       la.store(lo + 8 * EB * j); lb.store(lo + 8 * EB * (LPR + j));
       ha.store(hi + 8 * EB * j); hb.store(hi + 8 * EB * (LPR + j));
@@ -296,7 +386,7 @@ template <int DT, int D, bool Q4>
 __global__ __launch_bounds__(kPagedThreads) void append_pages_kernel(PShape s, PTable tab, PRope rp, int n_rows) {
   constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RS = kPagedThreads / LPR, RB = D * EB, RUNS = D / 8;
   __shared__ uint32_t words[Q4 ? RS * RUNS : 1];           // codes of the value rows of a pass, a word per eight elements
-  __shared__ float red[4][2][D];
+  __shared__ __align__(16) char red[4][2 * RB];
   const int tid = threadIdx.x, j = tid % LPR, slot = tid / LPR, lane = tid & 63, wave = tid >> 6;
   const int layer = blockIdx.x / s.units_per_layer, u = blockIdx.x - layer * s.units_per_layer;
   const int h = u % s.hkv;
@@ -311,9 +401,8 @@ __global__ __launch_bounds__(kPagedThreads) void append_pages_kernel(PShape s, P
     const int first = pg << s.lp, lo_row = max(x.r0 - first, 0), hi_row = min(x.r1 - first, s.P);   // rows of the page to be written
     if (lo_row >= hi_row) continue;
     char *kp = c.K + (int64_t)id * s.page_bytes, *vp = c.V + (int64_t)id * s.page_bytes;
-    float blo[16], bhi[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) { blo[i] = INFINITY; bhi[i] = -INFINITY; }
+    RunRange<DT> ra, rb;
+    ra.none(); rb.none();
     for (int s0 = lo_row / RS * RS; s0 < hi_row; s0 += RS) {
       const int r = s0 + slot;
       const bool live = r >= lo_row && r < hi_row;
@@ -330,13 +419,7 @@ __global__ __launch_bounds__(kPagedThreads) void append_pages_kernel(PShape s, P
           load_angles<D>(rp, row, n_rows, j, t);
           rotate<DT>(t, ka, kb);
         }
-        if (c.bounds) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            blo[i] = fminf(blo[i], ka.at(i)); bhi[i] = fmaxf(bhi[i], ka.at(i));
-            blo[8 + i] = fminf(blo[8 + i], kb.at(i)); bhi[8 + i] = fmaxf(bhi[8 + i], kb.at(i));
-          }
-        }
+        if (c.bounds) { ra.add(ka); rb.add(kb); }
       }
       if constexpr (!Q4) {
         if (live) {
@@ -356,22 +439,27 @@ __global__ __launch_bounds__(kPagedThreads) void append_pages_kernel(PShape s, P
           words[slot * RUNS + LPR + j] = run_codes(vb, svb);
         }
         __syncthreads();
-        // the strips' words: eight rows' codes of an element each; rows that are not written keep theirs
+        // the strips' words: eight rows' codes of an element each
+        const bool full = s0 >= lo_row && s0 + RS <= hi_row;
         for (int i = tid; i < RS / 8 * D; i += kPagedThreads) {
           const int sl = i / D, wi = i - sl * D, el = (wi >> 6) * 64 + (wi & 3) * 16 + ((wi >> 2) & 15);   // strip of the pass, word, element
           const int t0 = s0 + (sl >> 2) * 32 + (sl & 3) * 4;   // the strip's first row in the page
-          uint32_t w = 0, mask = 0;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int rr = t0 + (e >> 1) + 16 * (e & 1);
-            if (rr >= lo_row && rr < hi_row) {
-              w |= ((words[(rr - s0) * RUNS + (el >> 3)] >> code_shift(el & 7)) & 15u) << code_shift(e);
-              mask |= 15u << code_shift(e);
-            }
-          }
-          if (mask == 0) continue;
+          const uint32_t *from = words + (t0 - s0) * RUNS + (el >> 3);
           uint32_t *dst = reinterpret_cast<uint32_t *>(vp) + (t0 >> 5) * 4 * D + ((t0 & 15) >> 2) * D + wi;
-          if (mask != 0xffffffffu) w |= *dst & ~mask;
+          const uint32_t sh = code_shift(el & 7);
+          uint32_t w = 0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w |= ((from[((e >> 1) + 16 * (e & 1)) * RUNS] >> sh) & 15u) << code_shift(e);
+          if (!full) {                                     // rows of the pass that are not written keep their codes
+            uint32_t mask = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int rr = t0 + (e >> 1) + 16 * (e & 1);
+              mask |= rr >= lo_row && rr < hi_row ? 15u << code_shift(e) : 0u;
+            }
+            if (mask == 0) continue;
+            if (mask != 0xffffffffu) w = (w & mask) | (*dst & ~mask);
+          }
           *dst = w;
         }
         __syncthreads();
@@ -379,35 +467,23 @@ __global__ __launch_bounds__(kPagedThreads) void append_pages_kernel(PShape s, P
     }
     if (c.bounds) {                                        // uniform: over the lanes with the same elements, then the waves
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-#pragma unroll
-        for (int off = LPR; off < 64; off <<= 1) {
-          blo[i] = fminf(blo[i], __shfl_xor(blo[i], off));
-          bhi[i] = fmaxf(bhi[i], __shfl_xor(bhi[i], off));
-        }
+      for (int off = LPR; off < 64; off <<= 1) { ra.join(off); rb.join(off); }
       if (lane < LPR) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int el = (i < 8 ? 0 : D / 2) + 8 * j + (i & 7);
-          red[wave][0][el] = blo[i];
-          red[wave][1][el] = bhi[i];
-        }
+        char *at = red[wave] + 8 * EB * j;
+        ra.low().store(at); rb.low().store(at + RB / 2);
+        ra.high().store(at + RB); rb.high().store(at + RB + RB / 2);
       }
       __syncthreads();
-      for (int i = tid; i < 2 * D; i += kPagedThreads) {
-        const int side = i / D, el = i - side * D;
-        float v = red[0][side][el];
+      if (tid < 2 * RUNS) {                                // a run of the smallest, or of the largest elements
+        const int side = tid / RUNS, run = tid - side * RUNS;
+        RunRange<DT> m;
+        m.none();
+        Run<DT> v;
 #pragma unroll
-        for (int w = 1; w < 4; ++w) v = side ? fmaxf(v, red[w][side][el]) : fminf(v, red[w][side][el]);
-        char *dst = c.bounds + ((int64_t)id * 2 * D + i) * EB;
-        if (lo_row > 0) {                                  // rows of an earlier call are in the page
-          float old;
-          if constexpr (DT == MIXKV_BF16) old = __uint_as_float((uint32_t)*reinterpret_cast<uint16_t *>(dst) << 16);
-          else old = *reinterpret_cast<float *>(dst);
-          v = side ? fmaxf(v, old) : fminf(v, old);
-        }
-        if constexpr (DT == MIXKV_BF16) *reinterpret_cast<uint16_t *>(dst) = (uint16_t)(__float_as_uint(v) >> 16);
-        else *reinterpret_cast<float *>(dst) = v;
+        for (int w = 0; w < 4; ++w) { v.load(red[w] + side * RB + 8 * EB * run); m.add(v); }
+        char *dst = c.bounds + (int64_t)id * 2 * RB + side * RB + 8 * EB * run;
+        if (lo_row > 0) { v.load(dst); m.add(v); }         // rows of an earlier call are in the page
+        (side ? m.high() : m.low()).store(dst);
       }
       __syncthreads();
     }
@@ -418,33 +494,42 @@ __global__ __launch_bounds__(kPagedThreads) void append_pages_kernel(PShape s, P
 // read_paged_kernel.  blockIdx.x: (layer, sequence, KV head); blockIdx.y: workers on the head's passes of RS rows.
 // ------------------------------------------------------------------------------------------------
 template <int DT, int D, bool Q4>
-__global__ __launch_bounds__(kPagedThreads) void read_paged_kernel(PShape s, PTable tab, int n_rows) {
-  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RS = 32, RB = D * EB, THREADS = LPR * RS;
+__global__ __launch_bounds__(D * 2) void read_paged_kernel(PShape s, PTable tab, int n_rows) {
+  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RS = 32, RB = D * EB, STRIP = D + 8;   // (a strip's words, padded)
+  __shared__ __align__(16) uint32_t words[Q4 ? 4 * STRIP : 4];
   const int tid = threadIdx.x, j = tid % LPR, slot = tid / LPR;
   const int layer = blockIdx.x / s.units_per_layer, u = blockIdx.x - layer * s.units_per_layer;
   const int h = u % s.hkv;
   const PCache c = tab.c[layer];
   const PRows d = tab.r[layer];
   const RowRange x = row_range(s, c, d, u, n_rows);
-  if (tid >= THREADS) return;
   for (int t0 = x.r0 / RS + (int)blockIdx.y; t0 * RS < x.r1; t0 += gridDim.y) {
     const int id = page_at(s, c, u, (t0 * RS) >> s.lp);
-    const int r = ((t0 * RS) & (s.P - 1)) + slot, at = t0 * RS + slot;   // row of the page, of the head
-    if (id < 0 || at < x.r0 || at >= x.r1) continue;
+    if (id < 0) continue;                                  // uniform
+    const int r0 = (t0 * RS) & (s.P - 1), r = r0 + slot, at = t0 * RS + slot;   // the pass's first row of the page, the row of the page, of the head
+    const bool live = at >= x.r0 && at < x.r1;
     char *kp = c.K + (int64_t)id * s.page_bytes, *vp = c.V + (int64_t)id * s.page_bytes;
-    Run<DT> ka, kb, va, vb;
+    Run<DT> ka{}, kb{}, va{}, vb{};
     if constexpr (!Q4) {
       const int64_t from = (int64_t)r * RB + 8 * EB * j;
-      ka.load(kp + from);
-      kb.load(kp + from + RB / 2);
-      va.load(vp + from);
-      vb.load(vp + from + RB / 2);
+      if (live) {
+        ka.load(kp + from);
+        kb.load(kp + from + RB / 2);
+        va.load(vp + from);
+        vb.load(vp + from + RB / 2);
+      }
     } else {
       const Place4<D> pl(j, r, s.P);
+      // the pass's four strips through LDS: a word has eight rows' codes
+      u32x4 strip = {};
+      if (tid < D) strip = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const uint32_t *>(vp) + (r0 >> 5) * 4 * D + 4 * tid);
       const u32x2 kw = *pl.key_words(kp), ks = *pl.key_scales(kp);
       const uint16_t *sa = pl.value_scale(vp, pl.ga()), *sb = pl.value_scale(vp, pl.gb());
       const float s0 = f16_value(sa[0]), b0 = f16_value(sa[8]), s1 = f16_value(sb[0]), b1 = f16_value(sb[8]);
-      const uint32_t *vw = pl.strip_words(vp), sh = code_shift(pl.e);
+      __syncthreads();                                     // the pass before has read the strips
+      if (tid < D) *reinterpret_cast<u32x4 *>(words + (tid / (D / 4)) * STRIP + (tid % (D / 4)) * 4) = strip;
+      __syncthreads();
+      const uint32_t *vw = words + (pl.strip & 3) * STRIP, sh = code_shift(pl.e);
       float x0[8], x1[8], y0[8], y1[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -455,6 +540,7 @@ __global__ __launch_bounds__(kPagedThreads) void read_paged_kernel(PShape s, PTa
       }
       ka.set(x0); kb.set(x1); va.set(y0); vb.set(y1);
     }
+    if (!live) continue;
     const int64_t row = at + x.shift;
     char *kd = d.K + row * d.sn + h * d.sh + 8 * EB * j, *vd = d.V + row * d.sn + h * d.sh + 8 * EB * j;
     ka.store(kd);
@@ -632,7 +718,7 @@ extern "C" mixkv_status mixkv_paged_read(const mixkv_paged_params *params, const
     const PTable t = table_of(caches + l0, rows + l0, nl, eb);
     const int64_t units = (int64_t)nl * s.units_per_layer;
     const int w = workers(((int64_t)max_count + 30) / 32 + 1, units);
-    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)units, (unsigned)w), dim3(kPagedThreads), 0, stream, s, t, n_rows); };
+    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)units, (unsigned)w), dim3(2 * s.D), 0, stream, s, t, n_rows); };
     if (s.q4) { if (s.D == 128) go(read_paged_kernel<MIXKV_BF16, 128, true>); else go(read_paged_kernel<MIXKV_BF16, 64, true>); }
     else if (params->dtype == MIXKV_BF16) { if (s.D == 128) go(read_paged_kernel<MIXKV_BF16, 128, false>); else go(read_paged_kernel<MIXKV_BF16, 64, false>); }
     else { if (s.D == 128) go(read_paged_kernel<MIXKV_F32, 128, false>); else go(read_paged_kernel<MIXKV_F32, 64, false>); }
