@@ -45,6 +45,8 @@ template <> struct Run<MIXKV_BF16> {
   u32x4 v;
   __device__ __forceinline__ void load(const char *p) { v = *reinterpret_cast<const u32x4 *>(p); }
   __device__ __forceinline__ void store(char *p) const { *reinterpret_cast<u32x4 *>(p) = v; }
+  __device__ __forceinline__ void load_once(const char *p) { v = load_vec<true>(p); }
+  __device__ __forceinline__ void store_once(char *p) const { __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(p)); }
   __device__ __forceinline__ float at(int i) const { return __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16); }
   __device__ __forceinline__ void set(const float (&x)[8]) {            // rounded to nearest even
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -56,6 +58,14 @@ template <> struct Run<MIXKV_F32> {
   f32x4 lo, hi;
   __device__ __forceinline__ void load(const char *p) { lo = reinterpret_cast<const f32x4 *>(p)[0]; hi = reinterpret_cast<const f32x4 *>(p)[1]; }
   __device__ __forceinline__ void store(char *p) const { reinterpret_cast<f32x4 *>(p)[0] = lo; reinterpret_cast<f32x4 *>(p)[1] = hi; }
+  __device__ __forceinline__ void load_once(const char *p) {
+    lo = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p));
+    hi = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p) + 1);
+  }
+  __device__ __forceinline__ void store_once(char *p) const {
+    __builtin_nontemporal_store(lo, reinterpret_cast<f32x4 *>(p));
+    __builtin_nontemporal_store(hi, reinterpret_cast<f32x4 *>(p) + 1);
+  }
   __device__ __forceinline__ float at(int i) const { return i < 4 ? lo[i & 3] : hi[i & 3]; }
   __device__ __forceinline__ void set(const float (&x)[8]) {
 #pragma unroll
@@ -215,8 +225,10 @@ __device__ __forceinline__ GroupScale run_scale(const Run<MIXKV_BF16> &x) {
 }
 
 // The codes of eight elements in a word.  16 (x - base - step) / step as one multiply-add with 16 / step is off by at most 2^-22 of what its
-// product and its constant are together (the quotient, the constant and the sum are rounded by 2^-24 each); where that could decide a
-// rounding, or elements have to be clipped, the run's codes are formed in 64 bits: one run of some thousands.
+// product and its constant are together (the quotient, the constant and the sum are rounded by 2^-24 each).  Where that could decide a
+// rounding, and in bf16 rows exact ties between two codes are frequent (a run in some hundred), the side of the tie m + 1/2 is that of
+// 16 d - (m + 1/2) step, whose sign one multiply-add has exactly if d = x - base - step is; if it is not, or if elements have to be clipped, 64
+// bits decide.
 __device__ __forceinline__ uint32_t run_codes(const Run<MIXKV_BF16> &x, const GroupScale &g) {
   const float r = g.step > 0.f ? 16.f / g.step : 0.f, k = -(g.base + g.step) * r;
   uint32_t w = 0;
@@ -228,13 +240,29 @@ __device__ __forceinline__ uint32_t run_codes(const Run<MIXKV_BF16> &x, const Gr
     w |= (uint32_t)__builtin_amdgcn_fmed3f(n, 0.f, 15.f) << code_shift(e);
   }
   if ((g.wide || off > 0.5f - 0x1p-22f * (40.f + 2.f * fabsf(k))) && g.step > 0.f) {
+#pragma clang fp contract(off)
+    bool exact = !g.wide && fabsf(k) < 0x1p16f;
     w = 0;
-#pragma unroll 1
+#pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const uint32_t q = e < 2 ? x.v[0] : (e < 4 ? x.v[1] : (e < 6 ? x.v[2] : x.v[3]));
-      const double v = clip(__uint_as_float(e & 1 ? q & 0xffff0000u : q << 16));
-      const double n = __builtin_rint((v - (double)g.base - (double)g.step) * 16.0 / (double)g.step);
-      w |= (uint32_t)(n < 0. ? 0. : (n > 15. ? 15. : n)) << code_shift(e);
+      const float v = x.at(e), p = v - g.base, d = p - g.step;
+      const float vb = v - p, pb = p - d;                  // what the differences took off: base and step, if nothing was rounded
+      exact &= vb == g.base && p + vb == v && pb == g.step && d + pb == p;
+      const float m = __builtin_floorf(fminf(fmaxf(d * r, -1.f), 16.f));   // the rounded quotient may be past m or m + 1 by a little: then the tie is far
+      const float side = fmaf(-(m + 0.5f), g.step, 16.f * d);
+      const bool odd = ((int)m & 1) != 0;
+      const float n = m + (side > 0.f || (side == 0.f && odd) ? 1.f : 0.f);
+      w |= (uint32_t)fminf(fmaxf(n, 0.f), 15.f) << code_shift(e);
+    }
+    if (!exact) {
+      w = 0;
+#pragma unroll 1
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t q = e < 2 ? x.v[0] : (e < 4 ? x.v[1] : (e < 6 ? x.v[2] : x.v[3]));
+        const double v = clip(__uint_as_float(e & 1 ? q & 0xffff0000u : q << 16));
+        const double n = __builtin_rint((v - (double)g.base - (double)g.step) * 16.0 / (double)g.step);
+        w |= (uint32_t)(n < 0. ? 0. : (n > 15. ? 15. : n)) << code_shift(e);
+      }
     }
   }
   return w;
@@ -347,34 +375,45 @@ __global__ __launch_bounds__(kPagedThreads) void append_step_kernel(PShape s, PT
 }
 
 // ------------------------------------------------------------------------------------------------
-// append_queries_kernel (many rows).  blockIdx.x: (layer, sequence, KV head); blockIdx.y: workers on its rows.  A group of lanes has a row's
-// angles, as 64-bit numbers, for all queries of the KV head's group.
+// append_queries_kernel (many rows).  blockIdx.x: (layer, sequence); blockIdx.y: workers on its rows.  A group of lanes has a row's angles, as
+// 64-bit numbers, for all of its queries, or, where the KV heads do not have the same rows, for those of one KV head at a time.
+// Bound: memory; loads and stores pass the caches by (a prompt's queries are more than they keep).  Four prompts of 72 thousand
+// tokens together, 28 heads of 128, 1.03 GB, positions at random: plain 293 us, past the caches 277, eight heads in flight instead of four 268.
 // ------------------------------------------------------------------------------------------------
 template <int DT, int D>
 __global__ __launch_bounds__(kPagedThreads) void append_queries_kernel(PShape s, PTable tab, PRope rp, int n_rows) {
-  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RS = kPagedThreads / LPR, RB = D * EB, U = 4;
+  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RS = kPagedThreads / LPR, RB = D * EB, U = DT == MIXKV_BF16 ? 8 : 4;
   const int j = threadIdx.x % LPR, slot = threadIdx.x / LPR;
-  const int layer = blockIdx.x / s.units_per_layer, u = blockIdx.x - layer * s.units_per_layer, h = u % s.hkv;
+  const int layer = blockIdx.x / s.batch, b = blockIdx.x - layer * s.batch;
   const PRows d = tab.r[layer];
-  const RowRange x = row_range(s, tab.c[layer], d, u, n_rows);
-  for (int r = x.r0 + (int)blockIdx.y * RS + slot; r < x.r1; r += (int)gridDim.y * RS) {
-    const int64_t row = r + x.shift;
-    const char *src = d.Q + row * d.qsn + (int64_t)h * s.G * d.qsh + 8 * EB * j;
-    char *dst = d.Q_out + (row * s.hq + h * s.G) * RB + 8 * EB * j;
-    Angles t;
-    if (rp.cos) load_angles<D>(rp, row, n_rows, j, t);
-    for (int g = 0; g < s.G; g += U) {
-      Run<DT> a[U], b[U];
+  const RowRange x0 = row_range(s, tab.c[layer], d, b * s.hkv, n_rows);
+  bool same = true;
+  for (int h = 1; h < s.hkv; ++h) {
+    const RowRange y = row_range(s, tab.c[layer], d, b * s.hkv + h, n_rows);
+    same &= y.r1 - y.r0 == x0.r1 - x0.r0 && y.r0 + y.shift == x0.r0 + x0.shift;
+  }
+  for (int h = 0; h < s.hkv; h += same ? s.hkv : 1) {
+    const RowRange x = h == 0 ? x0 : row_range(s, tab.c[layer], d, b * s.hkv + h, n_rows);
+    const int heads = same ? s.hq : s.G;
+    for (int r = x.r0 + (int)blockIdx.y * RS + slot; r < x.r1; r += (int)gridDim.y * RS) {
+      const int64_t row = r + x.shift;
+      const char *src = d.Q + row * d.qsn + (int64_t)h * s.G * d.qsh + 8 * EB * j;
+      char *dst = d.Q_out + (row * s.hq + h * s.G) * RB + 8 * EB * j;
+      Angles t;
+      if (rp.cos) load_angles<D>(rp, row, n_rows, j, t);
+      for (int g = 0; g < heads; g += U) {
+        Run<DT> p[U], q[U];
 #pragma unroll
-      for (int i = 0; i < U; ++i)
-        if (g + i < s.G) { a[i].load(src + (g + i) * d.qsh); b[i].load(src + (g + i) * d.qsh + RB / 2); }
+        for (int i = 0; i < U; ++i)
+          if (g + i < heads) { p[i].load_once(src + (g + i) * d.qsh); q[i].load_once(src + (g + i) * d.qsh + RB / 2); }
 #pragma unroll
-      for (int i = 0; i < U; ++i)
-        if (g + i < s.G) {
-          if (rp.cos) rotate<DT>(t, a[i], b[i]);
-          a[i].store(dst + (g + i) * RB);
-          b[i].store(dst + (g + i) * RB + RB / 2);
-        }
+        for (int i = 0; i < U; ++i)
+          if (g + i < heads) {
+            if (rp.cos) rotate<DT>(t, p[i], q[i]);
+            p[i].store_once(dst + (int64_t)(g + i) * RB);
+            q[i].store_once(dst + (int64_t)(g + i) * RB + RB / 2);
+          }
+      }
     }
   }
 }
@@ -686,10 +725,10 @@ extern "C" mixkv_status mixkv_paged_append(const mixkv_paged_params *params, con
       else if (params->dtype == MIXKV_BF16) { if (s.D == 128) go(append_step_kernel<MIXKV_BF16, 128, false>); else go(append_step_kernel<MIXKV_BF16, 64, false>); }
       else { if (s.D == 128) go(append_step_kernel<MIXKV_F32, 128, false>); else go(append_step_kernel<MIXKV_F32, 64, false>); }
     } else {
-      const int pw = workers(((int64_t)max_count + s.P - 2) / s.P + 1, units), qw = workers(((int64_t)max_count + 31) / 32, units);
+      const int pw = workers(((int64_t)max_count + s.P - 2) / s.P + 1, units), qw = workers(((int64_t)max_count + 31) / 32, (int64_t)nl * s.batch);
       auto go = [&](auto kern, auto qkern) {
         hipLaunchKernelGGL(kern, dim3((unsigned)units, (unsigned)pw), dim3(kPagedThreads), 0, stream, s, t, rp, n_rows);
-        if (queries) hipLaunchKernelGGL(qkern, dim3((unsigned)units, (unsigned)qw), dim3(kPagedThreads), 0, stream, s, t, rp, n_rows);
+        if (queries) hipLaunchKernelGGL(qkern, dim3((unsigned)(nl * s.batch), (unsigned)qw), dim3(kPagedThreads), 0, stream, s, t, rp, n_rows);
       };
       constexpr int B16 = MIXKV_BF16, F32 = MIXKV_F32;
       if (s.q4) { if (s.D == 128) go(append_pages_kernel<B16, 128, true>, append_queries_kernel<B16, 128>); else go(append_pages_kernel<B16, 64, true>, append_queries_kernel<B16, 64>); }
