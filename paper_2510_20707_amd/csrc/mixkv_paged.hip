@@ -45,8 +45,6 @@ template <> struct Run<MIXKV_BF16> {
   u32x4 v;
   __device__ __forceinline__ void load(const char *p) { v = *reinterpret_cast<const u32x4 *>(p); }
   __device__ __forceinline__ void store(char *p) const { *reinterpret_cast<u32x4 *>(p) = v; }
-  __device__ __forceinline__ void load_once(const char *p) { v = load_vec<true>(p); }
-  __device__ __forceinline__ void store_once(char *p) const { __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(p)); }
   __device__ __forceinline__ float at(int i) const { return __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16); }
   __device__ __forceinline__ void set(const float (&x)[8]) {            // rounded to nearest even
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -58,14 +56,6 @@ template <> struct Run<MIXKV_F32> {
   f32x4 lo, hi;
   __device__ __forceinline__ void load(const char *p) { lo = reinterpret_cast<const f32x4 *>(p)[0]; hi = reinterpret_cast<const f32x4 *>(p)[1]; }
   __device__ __forceinline__ void store(char *p) const { reinterpret_cast<f32x4 *>(p)[0] = lo; reinterpret_cast<f32x4 *>(p)[1] = hi; }
-  __device__ __forceinline__ void load_once(const char *p) {
-    lo = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p));
-    hi = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p) + 1);
-  }
-  __device__ __forceinline__ void store_once(char *p) const {
-    __builtin_nontemporal_store(lo, reinterpret_cast<f32x4 *>(p));
-    __builtin_nontemporal_store(hi, reinterpret_cast<f32x4 *>(p) + 1);
-  }
   __device__ __forceinline__ float at(int i) const { return i < 4 ? lo[i & 3] : hi[i & 3]; }
   __device__ __forceinline__ void set(const float (&x)[8]) {
 #pragma unroll
@@ -73,46 +63,47 @@ template <> struct Run<MIXKV_F32> {
   }
 };
 
-// Cosines and sines of a lane's eight pairs, elements 8 j + i and D/2 + 8 j + i of dense row `row`.
-struct Angles { double c[8], s[8]; };
-template <int D>
-__device__ __forceinline__ void load_angles(const PRope &rp, int64_t row, int n_rows, int j, Angles &t) {
+// Cosines and sines of the N pairs from pair i0 on (elements i and D/2 + i), of dense row `row`.
+template <int N> struct Angles { float c[N], s[N]; };
+template <int D, int N>
+__device__ __forceinline__ void load_angles(const PRope &rp, int64_t row, int n_rows, int i0, Angles<N> &t) {
   int64_t at[3];                                          // the row's place in the tables, for each axis
 #pragma unroll
   for (int k = 0; k < 3; ++k) at[k] = k < rp.n_axes ? rp.positions[(int64_t)k * n_rows + row] : 0;
 #pragma unroll
   for (int k = 0; k < 3; ++k) at[k] = (int64_t)min(max((int)at[k], 0), rp.n_positions - 1) * (D / 2);
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {                           // four pairs at a time: 16 bytes of each table
-    const int i0 = 8 * j + 4 * h;
+  for (int h = 0; h < N; h += 4) {                        // four pairs at a time: 16 bytes of each table
+    const int p0 = i0 + h;
     f32x4 c, s;
-    if (i0 + 4 <= rp.s0 || (i0 >= rp.s0 && i0 + 4 <= rp.s1) || i0 >= rp.s1) {
-      const int64_t p = (i0 + 4 <= rp.s0 ? at[0] : (i0 >= rp.s1 ? at[2] : at[1])) + i0;
+    if (p0 + 4 <= rp.s0 || (p0 >= rp.s0 && p0 + 4 <= rp.s1) || p0 >= rp.s1) {
+      const int64_t p = (p0 + 4 <= rp.s0 ? at[0] : (p0 >= rp.s1 ? at[2] : at[1])) + p0;
       c = *reinterpret_cast<const f32x4 *>(rp.cos + p);
       s = *reinterpret_cast<const f32x4 *>(rp.sin + p);
     } else {                                              // an axis ends among the four
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int64_t p = (i0 + i < rp.s0 ? at[0] : (i0 + i < rp.s1 ? at[1] : at[2])) + i0 + i;
+        const int64_t p = (p0 + i < rp.s0 ? at[0] : (p0 + i < rp.s1 ? at[1] : at[2])) + p0 + i;
         c[i] = rp.cos[p];
         s[i] = rp.sin[p];
       }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { t.c[4 * h + i] = c[i]; t.s[4 * h + i] = s[i]; }
+    for (int i = 0; i < 4; ++i) { t.c[h + i] = c[i]; t.s[h + i] = s[i]; }
   }
 }
 // The pairs rotated.  In 64 bits: the products of a table entry and an element are exact there, so the result is the rounded exact rotation
 // whatever the order, and a row that is then quantised gets the codes of its definition.  The operator is bound by memory; the 64-bit
 // unit is idle otherwise.
 template <int DT>
-__device__ __forceinline__ void rotate(const Angles &t, Run<DT> &a, Run<DT> &b) {
+__device__ __forceinline__ void rotate(const Angles<8> &t, Run<DT> &a, Run<DT> &b) {
   float x[8], y[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const double p = a.at(i), q = b.at(i);
-    x[i] = (float)(p * t.c[i] - q * t.s[i]);
-    y[i] = (float)(q * t.c[i] + p * t.s[i]);
+    const double c = t.c[i], s = t.s[i];
+    x[i] = (float)(p * c - q * s);
+    y[i] = (float)(q * c + p * s);
     asm("" : "+v"(x[i]), "+v"(y[i]));                     // by way of fp32: the two roundings to bf16 are not made one
   }
   a.set(x);
@@ -321,8 +312,8 @@ __global__ __launch_bounds__(kPagedThreads) void append_step_kernel(PShape s, PT
     a.load(src + 8 * EB * j);
     b.load(src + 8 * EB * (LPR + j));
     if (turn) {
-      Angles t;
-      load_angles<D>(rp, row, n_rows, j, t);
+      Angles<8> t;
+      load_angles<D>(rp, row, n_rows, 8 * j, t);
       rotate<DT>(t, a, b);
     }
     if (task >= 2) {
@@ -375,15 +366,26 @@ __global__ __launch_bounds__(kPagedThreads) void append_step_kernel(PShape s, PT
 }
 
 // ------------------------------------------------------------------------------------------------
-// append_queries_kernel (many rows).  blockIdx.x: (layer, sequence); blockIdx.y: workers on its rows.  A group of lanes has a row's angles, as
-// 64-bit numbers, for all of its queries, or, where the KV heads do not have the same rows, for those of one KV head at a time.
-// Bound: memory; loads and stores pass the caches by (a prompt's queries are more than they keep).  Four prompts of 72 thousand
-// tokens together, 28 heads of 128, 1.03 GB, positions at random: plain 293 us, past the caches 277, eight heads in flight instead of four 268.
+// append_queries_kernel (many rows).  blockIdx.x: (layer, sequence); blockIdx.y: workers on its rows, a wave to a row.  A lane has 16 bytes of every
+// 64 / LR-th head (neighbouring lanes neighbouring bytes: an instruction takes a kilobyte of the row), its elements' partners are in the lane
+// LR / 2 away, and it keeps its angles for all heads, or, where the KV heads do not have the same rows, for those of
+// one KV head at a time.
+// Bound: memory; loads and stores pass the caches by (a prompt's queries are more than they keep).  us for four prompts of 72 thousand
+// tokens together, 28 heads of 128, 1.03 GB, where torch's copy of the same strided rows takes 199: 254 (with angles held as 64-bit numbers 277, in 16 384
+// workgroups instead of 4096 293); with eight lanes to a head and eight
+// heads' halves in flight, 128 bytes at a place, 268 (through the caches 287).
 // ------------------------------------------------------------------------------------------------
+template <int OFF>
+__device__ __forceinline__ uint32_t from_lane_xor(uint32_t x) {
+  if constexpr (OFF == 8) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, true);      // row_ror:8
+  else return (uint32_t)__shfl_xor((int)x, OFF);
+}
+
 template <int DT, int D>
 __global__ __launch_bounds__(kPagedThreads) void append_queries_kernel(PShape s, PTable tab, PRope rp, int n_rows) {
-  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RS = kPagedThreads / LPR, RB = D * EB, U = DT == MIXKV_BF16 ? 8 : 4;
-  const int j = threadIdx.x % LPR, slot = threadIdx.x / LPR;
+  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, E = 16 / EB, RB = D * EB, LR = RB / 16, HPI = 64 / LR, U = 8;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane % LR, sub = lane / LR;
+  const bool upper = l >= LR / 2;
   const int layer = blockIdx.x / s.batch, b = blockIdx.x - layer * s.batch;
   const PRows d = tab.r[layer];
   const RowRange x0 = row_range(s, tab.c[layer], d, b * s.hkv, n_rows);
@@ -395,24 +397,56 @@ __global__ __launch_bounds__(kPagedThreads) void append_queries_kernel(PShape s,
   for (int h = 0; h < s.hkv; h += same ? s.hkv : 1) {
     const RowRange x = h == 0 ? x0 : row_range(s, tab.c[layer], d, b * s.hkv + h, n_rows);
     const int heads = same ? s.hq : s.G;
-    for (int r = x.r0 + (int)blockIdx.y * RS + slot; r < x.r1; r += (int)gridDim.y * RS) {
+    for (int r = x.r0 + (int)blockIdx.y * 4 + wave; r < x.r1; r += (int)gridDim.y * 4) {
       const int64_t row = r + x.shift;
-      const char *src = d.Q + row * d.qsn + (int64_t)h * s.G * d.qsh + 8 * EB * j;
-      char *dst = d.Q_out + (row * s.hq + h * s.G) * RB + 8 * EB * j;
-      Angles t;
-      if (rp.cos) load_angles<D>(rp, row, n_rows, j, t);
-      for (int g = 0; g < heads; g += U) {
-        Run<DT> p[U], q[U];
+      const char *src = d.Q + row * d.qsn + (int64_t)h * s.G * d.qsh + l * 16;
+      char *dst = d.Q_out + (row * s.hq + h * s.G) * RB + l * 16;
+      Angles<E> t;
+      for (int g0 = 0; g0 < heads; g0 += U * HPI) {
+        u32x4 v[U];
 #pragma unroll
-        for (int i = 0; i < U; ++i)
-          if (g + i < heads) { p[i].load_once(src + (g + i) * d.qsh); q[i].load_once(src + (g + i) * d.qsh + RB / 2); }
+        for (int i = 0; i < U; ++i) {
+          const int g = g0 + i * HPI + sub;
+          v[i] = u32x4{0u, 0u, 0u, 0u};
+          if (g < heads) v[i] = load_vec<true>(src + g * d.qsh);
+        }
+        if (g0 == 0 && rp.cos) {
+          load_angles<D>(rp, row, n_rows, E * (l % (LR / 2)), t);
 #pragma unroll
-        for (int i = 0; i < U; ++i)
-          if (g + i < heads) {
-            if (rp.cos) rotate<DT>(t, p[i], q[i]);
-            p[i].store_once(dst + (int64_t)(g + i) * RB);
-            q[i].store_once(dst + (int64_t)(g + i) * RB + RB / 2);
+          for (int e = 0; e < E; ++e) t.s[e] = upper ? t.s[e] : -t.s[e];
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const int g = g0 + i * HPI + sub;
+          if (rp.cos) {                                    // (all lanes take part in the exchange)
+            u32x4 o;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o[k] = from_lane_xor<LR / 2>(v[i][k]);
+            float y[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              float mine, other;
+              if constexpr (EB == 2) {
+                mine = __uint_as_float(e & 1 ? v[i][e >> 1] & 0xffff0000u : v[i][e >> 1] << 16);
+                other = __uint_as_float(e & 1 ? o[e >> 1] & 0xffff0000u : o[e >> 1] << 16);
+              } else {
+                mine = __uint_as_float(v[i][e]);
+                other = __uint_as_float(o[e]);
+              }
+              y[e] = (float)((double)mine * (double)t.c[e] + (double)other * (double)t.s[e]);
+              asm("" : "+v"(y[e]));                        // by way of fp32, as in rotate()
+            }
+            if constexpr (EB == 2) {
+              Run<MIXKV_BF16> z;
+              z.set(y);
+              v[i] = z.v;
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[i][e] = __float_as_uint(y[e]);
+            }
           }
+          if (g < heads) __builtin_nontemporal_store(v[i], reinterpret_cast<u32x4 *>(dst + (int64_t)g * RB));
+        }
       }
     }
   }
@@ -454,8 +488,8 @@ __global__ __launch_bounds__(kPagedThreads) void append_pages_kernel(PShape s, P
         va.load(vs);
         vb.load(vs + RB / 2);
         if (turn) {
-          Angles t;
-          load_angles<D>(rp, row, n_rows, j, t);
+          Angles<8> t;
+          load_angles<D>(rp, row, n_rows, 8 * j, t);
           rotate<DT>(t, ka, kb);
         }
         if (c.bounds) { ra.add(ka); rb.add(kb); }
@@ -668,8 +702,8 @@ static PTable table_of(const mixkv_paged_cache *c, const mixkv_paged_rows *r, in
 
 // Workers of a unit: one for every `per` rows or pages that it may touch, as long as a launch has no more workgroups than keep the
 // chip busy several times over; the workers then walk.
-static int workers(int64_t wanted, int64_t units) {
-  const int64_t most = 16384 / units < 1 ? 1 : 16384 / units;
+static int workers(int64_t wanted, int64_t units, int64_t groups = 16384) {
+  const int64_t most = groups / units < 1 ? 1 : groups / units;
   return (int)(wanted < most ? wanted : most);
 }
 
@@ -725,7 +759,7 @@ extern "C" mixkv_status mixkv_paged_append(const mixkv_paged_params *params, con
       else if (params->dtype == MIXKV_BF16) { if (s.D == 128) go(append_step_kernel<MIXKV_BF16, 128, false>); else go(append_step_kernel<MIXKV_BF16, 64, false>); }
       else { if (s.D == 128) go(append_step_kernel<MIXKV_F32, 128, false>); else go(append_step_kernel<MIXKV_F32, 64, false>); }
     } else {
-      const int pw = workers(((int64_t)max_count + s.P - 2) / s.P + 1, units), qw = workers(((int64_t)max_count + 31) / 32, (int64_t)nl * s.batch);
+      const int pw = workers(((int64_t)max_count + s.P - 2) / s.P + 1, units), qw = workers(((int64_t)max_count + 3) / 4, (int64_t)nl * s.batch, 4096);
       auto go = [&](auto kern, auto qkern) {
         hipLaunchKernelGGL(kern, dim3((unsigned)units, (unsigned)pw), dim3(kPagedThreads), 0, stream, s, t, rp, n_rows);
         if (queries) hipLaunchKernelGGL(qkern, dim3((unsigned)(nl * s.batch), (unsigned)qw), dim3(kPagedThreads), 0, stream, s, t, rp, n_rows);
