@@ -101,6 +101,22 @@ __device__ __forceinline__ void finish_chunk(const PShape &s, const AShape &a, c
 constexpr int kQ4Ring = 2, kQ4Waves = 3;
 constexpr float kTopWeight = 8.f, kWeightLimit = 16384.f;     // log2 of the largest weight where an offset is chosen; where it moves
 
+// Over the 16 lanes of a row, in every one of them: rotations in the vector ALU.
+template <int CTRL>
+__device__ __forceinline__ float row_turned(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true)); }
+__device__ __forceinline__ float row_max(float x) {
+  x = fmaxf(x, row_turned<0x128>(x));                         // row_ror:8, 4, 2, 1
+  x = fmaxf(x, row_turned<0x124>(x));
+  x = fmaxf(x, row_turned<0x122>(x));
+  return fmaxf(x, row_turned<0x121>(x));
+}
+__device__ __forceinline__ float row_sum(float x) {
+  x += row_turned<0x128>(x);
+  x += row_turned<0x124>(x);
+  x += row_turned<0x122>(x);
+  return x + row_turned<0x121>(x);
+}
+
 template <int D>
 __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShape a, AttnTable tab, float *part, float *part_ml, int64_t unit0) {
   constexpr int NG = D / 32, NB = D / 16, H = kAttnHeads, W = 4;
@@ -300,8 +316,7 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float t = fmaxf(x2[0][e], x2[1][e]);
-#pragma unroll
-          for (int off = 1; off < 16; off <<= 1) t = fmaxf(t, __shfl_xor(t, off));
+          t = row_max(t);
           const float want = kTopWeight - t * c2[e];         // minus the offset that puts this tile's largest weight at 2^kTopWeight
           const bool move = t > -INFINITY && (!has[e] || want < nm[e]);
           const float f = move ? (has[e] ? fast_exp2(want - nm[e]) : 0.f) : 1.f;
@@ -354,8 +369,7 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
   __syncthreads();                                             // the shares take the rings' place
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-#pragma unroll
-    for (int off = 1; off < 16; off <<= 1) ls[e] += __shfl_xor(ls[e], off);
+    ls[e] = row_sum(ls[e]);
     if (l16 == 0) { m_s[wave][4 * quad + e] = has[e] ? -nm[e] : -INFINITY; l_s[wave][4 * quad + e] = ls[e]; }
 #pragma unroll
     for (int k = 0; k < NB; ++k) sh.share.o[wave][4 * quad + e][(16 * k + l16) ^ (4 * quad + e)] = o[k][e];
@@ -582,12 +596,18 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PShape s, AShape a, At
   }
 }
 
-// Tiles of a chunk and chunks of a head, from nothing but the arguments.
+// Tiles of a chunk and chunks of a head, from nothing but the arguments.  A workgroup costs some 4 us before and after its tiles (its chain of
+// loads, the queries, the fold of its waves), a tile some 1 us of a wave, the merge 4 us with the gap before it: as many workgroups as
+// there are compute units as soon as there are tiles for them, then longer chunks, up to two rounds of a few workgroups on every unit, then, in 4 bits, up
+// to 64 tiles (full-precision tiles take three times the bytes: 16).  us in chunks of 4, 8, 16, 32, 64, 128 tiles, 4-bit rows of 128: 4 heads of 2048
+// rows 10 11 13 17 23 21; 4 of 32 768 22 16 15 18 25 39; 4 of 131 072 59 41 32 26 27 40; 64 of 4096 25 19 16 17 24 37; 64 of 64 pages of 64
+// 28 22 17 19 25 37; 512 of up to 16 384 336 223 172 149 138 140; bf16 rows, 128 heads of up to 8192 100 79 73 78 80 87, 4 of 8192 12 12 16 23 38
+// 69; fp32, 128 of up to 8192 97 86 88 85 85 138.  Heads of up to 12 tiles stay whole: 4 of 260 rows 8.4 against 9.5 in chunks of 4.
 static void attn_config(const PShape &s, int n_layers, int max_rows, AShape *a) {
   a->gchunks = (s.G + kAttnHeads - 1) / kAttnHeads;
   a->gt = std::min(s.G, kAttnHeads);
-  const int64_t groups = (int64_t)n_layers * s.units_per_layer * a->gchunks, tiles = ((int64_t)max_rows + 31) / 32;
-  int64_t ct = std::max<int64_t>(4, std::min<int64_t>((tiles * groups + 511) / 512, s.q4 ? 64 : 16));
+  const int64_t groups = (int64_t)n_layers * s.units_per_layer * a->gchunks, tiles = ((int64_t)max_rows + 31) / 32, all = tiles * groups;
+  int64_t ct = std::max<int64_t>(4, std::max(std::min<int64_t>((all + 255) / 256, 16), std::min<int64_t>((all + 511) / 512, s.q4 ? 64 : 16)));
   if (tiles <= 12) ct = tiles;
   a->ctiles = (int)((ct + 3) / 4 * 4);
   // a launch has at most 65535 chunks, and fewer than 2^32 threads; the last chunk of a head takes what is left
