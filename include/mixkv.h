@@ -331,7 +331,7 @@ mixkv_status mixkv_append(const mixkv_params *params, const mixkv_append_layer *
  *           Word (4 t + q) D + 64 j + 4 m + w: the codes of the element 64 j + 16 w + m of the strip's rows; then S of the strip's
  *           row e and group g at fp16 ((4 t + q) D/32 + g) 16 + e, B eight further.
  * A program that builds pages itself may write them in this form.  Pages need no initialisation; rows of a page that have not
- * been written are never used.  Pages written by one call must be written for one (sequence, head) only.
+ * been written are never used.  A page that a call writes to must be written to for one place of one (sequence, head) only.
  *
  * lengths[b][h] counts the rows of a head, those that a call appends among them: a program adds the new rows to the
  * lengths first.  Lengths are clamped to [0, max_pages * page_rows].

@@ -501,13 +501,14 @@ def _tensor(t: torch.Tensor, name: str, dtype, shape, device, contiguous=True) -
     return t
 
 
-def _paged_device(t: torch.Tensor) -> torch.device:
+def _paged_device(caches: Sequence[PagedCache]) -> torch.device:
+    _need(len(caches) > 0, "no layers")
+    t = caches[0].lengths
     _need(t.is_cuda and t.device.index == torch.cuda.current_device(), "the tensors have to be on the current device")
     return t.device
 
 
 def _paged_caches(p: MixkvPagedParams, caches: Sequence[PagedCache], pages: bool, bounds: bool, device):
-    _need(len(caches) > 0, "no layers")
     units, pool = (p.batch, p.n_kv_heads), 0
     if pages:
         pool = p.n_pages * mixkv_page_bytes(p)
@@ -551,7 +552,7 @@ class PreparedPagedAppend:
 
     def __init__(self, p: MixkvPagedParams, caches: Sequence[PagedCache], rows: Sequence[PagedRows], rope: Optional[Rope] = None,
                  max_count: Optional[int] = None):
-        device = _paged_device(caches[0].lengths)
+        device = _paged_device(caches)
         _need(len(caches) == len(rows), "a rows entry for every cache")
         self.p, self.n, self.caches = p, len(caches), _paged_caches(p, caches, True, False, device)
         self.rows, self.n_rows = _paged_rows(p, rows, True, device)
@@ -565,12 +566,12 @@ class PreparedPagedAppend:
             self.rope = MixkvRope(_ptr(rope.cos), _ptr(rope.sin), rope.cos.shape[0], _ptr(rope.positions), axes,
                                   (C.c_int32 * 3)(*(rope.sections if axes == 3 else (0, 0, 0))))
         self._keep = (caches, rows, rope)
-        self._rope_arg = None if self.rope is None else C.byref(self.rope)
-        self._L = lib()
+        self._args = (C.byref(self.p), self.caches, self.rows, self.n, None if self.rope is None else C.byref(self.rope), self.n_rows,
+                      self.max_count)
+        self._call = lib().mixkv_paged_append
 
     def run(self, stream=None):
-        _check(self._L.mixkv_paged_append(C.byref(self.p), self.caches, self.rows, self.n, self._rope_arg, self.n_rows, self.max_count,
-                                          _stream(stream)), "mixkv_paged_append")
+        _check(self._call(*self._args, _stream(stream)), "mixkv_paged_append")
 
 
 def mixkv_paged_append(p: MixkvPagedParams, caches: Sequence[PagedCache], rows: Sequence[PagedRows], rope: Optional[Rope] = None,
@@ -583,17 +584,17 @@ class PreparedPagedRead:
     """The C arguments of one mixkv_paged_read call: rows[i].K and .V receive the newest row_count rows of every head."""
 
     def __init__(self, p: MixkvPagedParams, caches: Sequence[PagedCache], rows: Sequence[PagedRows], max_count: Optional[int] = None):
-        device = _paged_device(caches[0].lengths)
+        device = _paged_device(caches)
         _need(len(caches) == len(rows), "a rows entry for every cache")
         self.p, self.n, self.caches = p, len(caches), _paged_caches(p, caches, True, False, device)
         self.rows, self.n_rows = _paged_rows(p, rows, False, device)
         self.max_count = self.n_rows if max_count is None else max_count
         self._keep = (caches, rows)
-        self._L = lib()
+        self._args = (C.byref(self.p), self.caches, self.rows, self.n, self.n_rows, self.max_count)
+        self._call = lib().mixkv_paged_read
 
     def run(self, stream=None):
-        _check(self._L.mixkv_paged_read(C.byref(self.p), self.caches, self.rows, self.n, self.n_rows, self.max_count, _stream(stream)),
-               "mixkv_paged_read")
+        _check(self._call(*self._args, _stream(stream)), "mixkv_paged_read")
 
 
 def mixkv_paged_read(p: MixkvPagedParams, caches: Sequence[PagedCache], rows: Sequence[PagedRows], max_count: Optional[int] = None, stream=None):
@@ -619,7 +620,7 @@ class PreparedPagedSelect:
 
     def __init__(self, p: MixkvPagedParams, caches: Sequence[PagedCache], Qs, selected, n_selected, keep_first: int = 1, keep_last: int = 1,
                  workspace="alloc"):
-        device = _paged_device(caches[0].lengths)
+        device = _paged_device(caches)
         n = len(caches)
         _need(n == len(Qs) == len(selected) == len(n_selected), "queries and selections for every cache")
         self.p, self.n, self.caches, self.most = p, n, _paged_caches(p, caches, False, True, device), selected[0].shape[-1]
@@ -633,11 +634,11 @@ class PreparedPagedSelect:
         workspace = _paged_workspace(workspace, mixkv_paged_select_workspace_size(p, n) if isinstance(workspace, str) else 0, device)
         self.wp, self.wb = _ws(workspace)
         self._keep = (caches, Qs, selected, n_selected, workspace)
-        self._L = lib()
+        self._args = (C.byref(self.p), self.caches, self.arr, self.n, self.most, self.first, self.last, self.wp, self.wb)
+        self._call = lib().mixkv_paged_select
 
     def run(self, stream=None):
-        _check(self._L.mixkv_paged_select(C.byref(self.p), self.caches, self.arr, self.n, self.most, self.first, self.last, self.wp, self.wb,
-                                          _stream(stream)), "mixkv_paged_select")
+        _check(self._call(*self._args, _stream(stream)), "mixkv_paged_select")
 
 
 def mixkv_paged_select(p: MixkvPagedParams, caches: Sequence[PagedCache], Qs, max_selected: int, keep_first: int = 1, keep_last: int = 1,
@@ -663,7 +664,7 @@ class PreparedPagedAttention:
 
     def __init__(self, p: MixkvPagedParams, caches: Sequence[PagedCache], Qs, outs, selected=None, n_selected=None,
                  max_rows: Optional[int] = None, workspace="alloc"):
-        device = _paged_device(caches[0].lengths)
+        device = _paged_device(caches)
         n, sparse = len(caches), selected is not None
         _need(n == len(Qs) == len(outs) and (not sparse or n == len(selected) == len(n_selected)), "queries, outputs and selections for every cache")
         self.p, self.n, self.caches = p, n, _paged_caches(p, caches, True, False, device)
@@ -681,11 +682,11 @@ class PreparedPagedAttention:
         workspace = _paged_workspace(workspace, need, device)
         self.wp, self.wb = _ws(workspace)
         self._keep = (caches, Qs, outs, selected, n_selected, workspace)
-        self._L = lib()
+        self._args = (C.byref(self.p), self.caches, self.arr, self.n, self.most, self.rows, self.wp, self.wb)
+        self._call = lib().mixkv_paged_attention
 
     def run(self, stream=None):
-        _check(self._L.mixkv_paged_attention(C.byref(self.p), self.caches, self.arr, self.n, self.most, self.rows, self.wp, self.wb,
-                                             _stream(stream)), "mixkv_paged_attention")
+        _check(self._call(*self._args, _stream(stream)), "mixkv_paged_attention")
 
 
 def mixkv_paged_attention(p: MixkvPagedParams, caches: Sequence[PagedCache], Qs, selected=None, n_selected=None, max_rows: Optional[int] = None,

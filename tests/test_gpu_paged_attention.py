@@ -398,3 +398,102 @@ def test_selection_among_many_pages(dtype, D, pages, distinct):
         for h in range(2):
             want = O.select(scores[h], keep, first, last)
             assert n[0, h] == len(want) and sel[0, h].tolist() == want + [-1] * (keep - len(want)), (keep, h)
+
+
+@pytest.mark.parametrize("fmt,page_bytes", [("rows", 32768), ("4bit", 10240)])
+def test_pages_and_rows_beyond_four_gigabytes(fmt, page_bytes):
+    """The same rows through a small pool and at the end of one of more than 2^32 bytes, from the end of a dense tensor of more than 2^32
+    bytes: every output agrees bit for bit."""
+    D, P, n, batch = 128, 128, 300, 1
+    far_pages, far_rows = (1 << 32) // page_bytes + 40, (1 << 32) // (2 * D) + 5000
+    g = torch.Generator(device=T.DEV).manual_seed(25)
+    K, V, Q = (torch.randn((n, 1, D), generator=g, device=T.DEV).bfloat16() for _ in range(3))
+    angle = torch.rand((400, D // 2), generator=g, device=T.DEV) * 6
+    pos = torch.randint(0, 400, (1, n), generator=g, device=T.DEV).int()
+    got = []
+    for pages, rows in ((8, n), (far_pages, far_rows)):
+        p = B.make_paged_params("bf16", fmt, batch, 1, 1, D, P, 3, pages, 0.2)
+        cache = B.alloc_paged_cache(p, T.DEV, bounds=True)
+        assert pages == 8 or cache.K_pages.numel() * cache.K_pages.element_size() > 1 << 32
+        cache.page_table[0, 0] = torch.arange(pages - 3, pages, device=T.DEV)
+        cache.lengths.fill_(n)
+        at = rows - n
+        dense = [torch.empty((rows, 1, D), dtype=torch.bfloat16, device=T.DEV) for _ in range(4)]
+        for t, x in zip(dense, (K, V, Q)):
+            t[at:] = x
+        where = torch.zeros((1, rows), dtype=torch.int32, device=T.DEV)
+        where[:, at:] = pos
+        one = lambda x: torch.full((1, 1), x, dtype=torch.int32, device=T.DEV)  # noqa: E731
+        B.mixkv_paged_append(p, [cache], [B.PagedRows(dense[0], dense[1], one(at), one(n), dense[2], dense[3])], B.Rope(angle.cos(), angle.sin(), where), n)
+        q = dense[3][-1:].contiguous().view(1, 1, D)
+        dense[0][at:] = 0
+        dense[1][at:] = 0
+        B.mixkv_paged_read(p, [cache], [B.PagedRows(dense[0], dense[1], one(at), one(n))], n)
+        (sel,), (m,) = B.mixkv_paged_select(p, [cache], [q], 2)
+        outs = [t[at:].clone() for t in (dense[3], dense[0], dense[1])] + [sel, m, cache.K_bounds[pages - 3:].clone()]
+        outs += [B.mixkv_paged_attention(p, [cache], [q])[0], B.mixkv_paged_attention(p, [cache], [q], [sel], [m])[0]]
+        # a step of one row more, by the kernel for few rows
+        cache.lengths.fill_(n + 1)
+        B.mixkv_paged_append(p, [cache], [B.PagedRows(dense[3], dense[2], one(rows - 1), one(1), dense[2], torch.empty_like(dense[2]))], None, 1)
+        outs += [cache.K_pages[pages - 3:].clone(), cache.V_pages[pages - 3:].clone()] if fmt == "rows" else []
+        outs.append(B.mixkv_paged_attention(p, [cache], [q])[0])
+        torch.cuda.synchronize()
+        got.append([t.cpu() for t in outs])
+        del dense, cache, outs
+        torch.cuda.empty_cache()
+    for a, b in zip(*got):
+        live = a.shape == b.shape and torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
+        # (rows of the last page that were never written are whatever the allocation held)
+        if not live and a.dim() == 3 and a.shape[0] == 3 and fmt == "rows" and a.shape[1] == P:
+            flat = lambda t: t.reshape(-1, D)[:n + 1].contiguous().view(torch.uint8)  # noqa: E731
+            live = torch.equal(flat(a), flat(b))
+        assert live
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS)
+def test_more_layers_than_one_launch_takes(fmt, dtype):
+    D, P, L = 64, 32, 35
+    rng = np.random.default_rng(26)
+    lens = [np.array([[5 + 7 * l, 300 - 8 * l]]) for l in range(L)]
+    lays = [T.Layer(rng, fmt, dtype, D, P, n, 10, spare=0, bounds=True, fill=True) for n in lens]
+    most = max(l.n_pages for l in lays)
+    for l in lays:                                                       # pools of one size
+        pad = most - l.n_pages
+        l.K, l.V = (np.concatenate([x, np.zeros((pad, x.shape[1]), np.uint8)]) for x in (l.K, l.V))
+        l.bounds = np.sort(np.concatenate([l.bounds, np.zeros((pad, 2, D))]), axis=1)
+        l.n_pages = most
+    Qs = [_queries(rng, l, 6) for l in lays]
+    p, caches, q = lays[0].params(6), [l.device() for l in lays], [T.to_device(x, dtype) for x in Qs]
+    sel, n = B.mixkv_paged_select(p, caches, q, 4)
+    outs = B.mixkv_paged_attention(p, caches, q), B.mixkv_paged_attention(p, caches, q, sel, n)
+    for l, lay in enumerate(lays):
+        for h in range(2):
+            places = O.select(O.page_scores(Qs[l], lay.bounds, lay.table, lay.lengths, P, 0, h), 4, 1, 1)
+            assert sel[l][0, h, :len(places)].tolist() == places and n[l][0, h] == len(places)
+            for out, which in zip(outs, (None, places)):
+                k, v = O.head(*lay.args(), lay.table, lay.lengths, 0, h, which)
+                want = O.attention(Qs[l][0, 3 * h:3 * h + 3], k, v, 1.0)
+                err = np.abs(T.values(out[l])[0, 3 * h:3 * h + 3] - want).max(1)
+                assert (err <= TOL[dtype] * np.abs(want).max(1) + (2.0 ** -10 * np.abs(v).max() if fmt == "4bit" else 0)).all(), (l, h)
+
+
+def test_calls_on_two_streams_with_workspaces_of_their_own():
+    rng = np.random.default_rng(27)
+    lays = [T.Layer(rng, fmt, "bf16", 128, 32, [[900, 30], [1, 400]], 30, fill=True, bounds=True) for fmt in ("4bit", "rows")]
+    jobs = []
+    for lay in lays:
+        c, q, p = lay.device(), T.to_device(_queries(rng, lay, 8), "bf16"), lay.params(8)
+        alone = B.mixkv_paged_attention(p, [c], [q])[0], B.mixkv_paged_select(p, [c], [q], 5)[0][0]
+        out, sel, n = torch.empty_like(q), torch.empty((2, 2, 5), dtype=torch.int32, device=T.DEV), torch.empty((2, 2), dtype=torch.int32, device=T.DEV)
+        jobs.append((torch.cuda.Stream(), (B.PreparedPagedAttention(p, [c], [q], [out]), B.PreparedPagedSelect(p, [c], [q], [sel], [n])), alone, (out, sel)))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for stream, calls, _, got in jobs:
+            with torch.cuda.stream(stream):
+                for t in got:
+                    t.zero_()
+            for call in calls:
+                call.run(stream)
+        torch.cuda.synchronize()
+        for _, _, alone, got in jobs:
+            assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(alone, got))
