@@ -330,8 +330,10 @@ mixkv_status mixkv_append(const mixkv_params *params, const mixkv_append_layer *
  *   values  strip q of the 32 rows from row 32 t: the rows 32 t + 4 q + i and 32 t + 16 + 4 q + i, i = 0 ... 3, as e = 2 i and 2 i + 1.
  *           Word (4 t + q) D + 64 j + 4 m + w: the codes of the element 64 j + 16 w + m of the strip's rows; then S of the strip's
  *           row e and group g at fp16 ((4 t + q) D/32 + g) 16 + e, B eight further.
+ * NaN is not supported in rows that go into 4-bit pages, nor in keys where K_bounds are kept.
  * A program that builds pages itself may write them in this form.  Pages need no initialisation; rows of a page that have not
  * been written are never used.  A page that a call writes to must be written to for one place of one (sequence, head) only.
+ * Pages, bounds, dense rows and outputs of a call may not overlap one another where any of them is written.
  *
  * lengths[b][h] counts the rows of a head, those that a call appends among them: a program adds the new rows to the
  * lengths first.  Lengths are clamped to [0, max_pages * page_rows].
@@ -416,7 +418,7 @@ mixkv_status mixkv_paged_read(const mixkv_paged_params *params, const mixkv_page
  * in 64 bits, with lo and hi the page's K_bounds: the sum over the queries of the largest dot product that any key within
  * the bounds can have (a bound that meets a zero counts nothing, infinite ones too).  The first keep_first and the last keep_last pages are always among them (keep_first + keep_last <=
  * max_selected); equal scores go to the earlier page, a place without a
- * page scores -infinity; a head with no more pages than max_selected keeps all.  NaN is not supported.
+ * page scores -infinity, and so does one whose score is NaN (queries hold none); a head with no more pages than max_selected keeps all.
  * Writes selected [batch, n_kv_heads, max_selected] (places in the head's page table, ascending, then -1) and n_selected
  * [batch, n_kv_heads].  K_pages and V_pages are not used and may be NULL; softmax_scale is not used.
  * Workspace: mixkv_paged_select_workspace_size bytes, 256-byte aligned, no initialisation.

@@ -27,7 +27,7 @@ __host__ __device__ constexpr int64_t page_bytes_of(bool q4, int dtype, int P, i
 }
 
 mixkv_status make_pshape(const mixkv_paged_params *p, PShape *s);
-mixkv_status check_caches(const mixkv_paged_params *p, const mixkv_paged_cache *c, int n_layers, bool pages, bool bounds);
+mixkv_status check_caches(const mixkv_paged_cache *c, int n_layers, bool pages, bool bounds);
 inline bool misaligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
 // Rows of unit u (sequence, head) of a layer.

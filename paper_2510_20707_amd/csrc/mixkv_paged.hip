@@ -9,7 +9,13 @@ namespace mixkv {
 
 constexpr int kPagedLayers = 16;         // pointer-table entries of a launch: the dense rows' strides travel with them
 constexpr int kPagedThreads = 256;
-constexpr int kStepRows = 4;              // rows of a head up to which a few lanes walk them
+
+// Rows of a head up to which a few lanes walk them (append_step_kernel) instead of a workgroup to a page (append_pages_kernel and
+// append_queries_kernel: 9 us of launches, shared memory and barriers whatever the count).  us for 1, 2, 3, 4, 6, 8 rows of 8 heads of 128 with 32 query heads,
+// bounds kept, walked | by pages: bf16 rows, one sequence 3.7 5.0 6.3 7.3 9.9 12.6 | 9.4 9.5 9.4 9.2 9.5 9.4, 64 sequences 3.9 5.3 6.8 8.2 11.5 16.5 | 10.8
+// 10.9 11.1 11.4 11.5 12.5; 4-bit with the rows read back, one sequence 9.7 13.5 17.3 21.6 29.0 36.6 | 15.8 16.3 16.7 17.0 17.4 17.4, 64
+// sequences 11.1 14.9 18.7 23.3 31.7 40.8 | 19.1 20.7 21.0 23.9 25.4 26.3.
+static int step_rows(bool q4) { return q4 ? 3 : 5; }
 
 struct PRows {
   char *K, *V;
@@ -290,7 +296,8 @@ struct Place4 {
 // ------------------------------------------------------------------------------------------------
 // append_step_kernel (few rows per head: a decoding step).  Every row of a (layer, sequence, KV head) that a call moves, key, value, or one of its
 // queries, is a task for D/16 lanes, which walk the head's new rows one after another: no barrier, and one writer for what rows share.
-// Bound: one chain of memory round trips (counts, table and positions, angles, the strip's old words).
+// Bound: one chain of memory round trips (counts, table and positions, angles, the strip's old words): 3.5 us for one sequence's row into bf16
+// pages, 8 us for 64 sequences into 4-bit ones.
 // ------------------------------------------------------------------------------------------------
 template <int DT, int D, bool Q4>
 __global__ __launch_bounds__(kPagedThreads) void append_step_kernel(PShape s, PTable tab, PRope rp, int n_rows, int tasks, int groups) {
@@ -453,7 +460,10 @@ __global__ __launch_bounds__(kPagedThreads) void append_queries_kernel(PShape s,
 }
 
 // ------------------------------------------------------------------------------------------------
-// append_pages_kernel (many rows).  blockIdx.x: (layer, sequence, KV head); blockIdx.y: workers on the head's pages.
+// append_pages_kernel (many rows).  blockIdx.x: (layer, sequence, KV head); blockIdx.y: workers on the head's pages, a workgroup to a page: D/16 lanes
+// to a row, codes of values turned into the strips' words through LDS, bounds folded over the page's passes.
+// Bound: in 4 bits the quantiser's and the rotation's arithmetic.  us for four prompts of 72 thousand tokens together, 4 KV heads of 128, 147 MB in: 175
+// (in 1024 workgroups 194, 512 260, with 512 threads 214); without rotation 139; bf16 pages without rotation 84, which is memory.
 // ------------------------------------------------------------------------------------------------
 template <int DT, int D, bool Q4>
 __global__ __launch_bounds__(kPagedThreads) void append_pages_kernel(PShape s, PTable tab, PRope rp, int n_rows) {
@@ -565,6 +575,7 @@ __global__ __launch_bounds__(kPagedThreads) void append_pages_kernel(PShape s, P
 
 // ------------------------------------------------------------------------------------------------
 // read_paged_kernel.  blockIdx.x: (layer, sequence, KV head); blockIdx.y: workers on the head's passes of RS rows.
+// Bound: memory, the dense rows' stores first: the same four prompts, 46 MB of 4-bit pages to 147 MB of rows, in 56 us.
 // ------------------------------------------------------------------------------------------------
 template <int DT, int D, bool Q4>
 __global__ __launch_bounds__(D * 2) void read_paged_kernel(PShape s, PTable tab, int n_rows) {
@@ -645,7 +656,7 @@ mixkv_status make_pshape(const mixkv_paged_params *p, PShape *s) {
   return MIXKV_OK;
 }
 
-mixkv_status check_caches(const mixkv_paged_params *, const mixkv_paged_cache *c, int n_layers, bool pages, bool bounds) {
+mixkv_status check_caches(const mixkv_paged_cache *c, int n_layers, bool pages, bool bounds) {
   if (!c || n_layers < 1 || n_layers > MIXKV_MAX_LAYERS) return MIXKV_ERR_INVALID_ARG;
   for (int l = 0; l < n_layers; ++l) {
     if (pages && (!c[l].K_pages || !c[l].V_pages || c[l].K_pages == c[l].V_pages)) return MIXKV_ERR_INVALID_ARG;
@@ -700,8 +711,8 @@ static PTable table_of(const mixkv_paged_cache *c, const mixkv_paged_rows *r, in
   return t;
 }
 
-// Workers of a unit: one for every `per` rows or pages that it may touch, as long as a launch has no more workgroups than keep the
-// chip busy several times over; the workers then walk.
+// Workers of a unit: those that are wanted, one to a page or a few rows, as long as a launch has no more workgroups than `groups`; the workers
+// then walk.
 static int workers(int64_t wanted, int64_t units, int64_t groups = 16384) {
   const int64_t most = groups / units < 1 ? 1 : groups / units;
   return (int)(wanted < most ? wanted : most);
@@ -726,7 +737,7 @@ extern "C" mixkv_status mixkv_paged_append(const mixkv_paged_params *params, con
   mixkv_status st = make_pshape(params, &s);
   if (st != MIXKV_OK) return st;
   if (n_rows < 1 || max_count < 1) return MIXKV_ERR_INVALID_ARG;
-  if ((st = check_caches(params, caches, n_layers, true, false)) != MIXKV_OK) return st;
+  if ((st = check_caches(caches, n_layers, true, false)) != MIXKV_OK) return st;
   const int eb = params->dtype == MIXKV_BF16 ? 2 : 4;
   if ((st = check_rows(s, eb, rows, n_layers, n_rows, true)) != MIXKV_OK) return st;
   PRope rp{};
@@ -749,7 +760,7 @@ extern "C" mixkv_status mixkv_paged_append(const mixkv_paged_params *params, con
     const PTable t = table_of(caches + l0, rows + l0, nl, eb);
     const int64_t units = (int64_t)nl * s.units_per_layer;
     const bool queries = rows[0].Q != nullptr;
-    if (max_count <= kStepRows) {
+    if (max_count <= step_rows(s.q4)) {
       const int tasks = 2 + (queries ? s.G : 0), per = kPagedThreads / (s.D / 16);
       const int groups = (int)units * tasks;
       auto go = [&](auto kern) {
@@ -781,7 +792,7 @@ extern "C" mixkv_status mixkv_paged_read(const mixkv_paged_params *params, const
   mixkv_status st = make_pshape(params, &s);
   if (st != MIXKV_OK) return st;
   if (n_rows < 1 || max_count < 1) return MIXKV_ERR_INVALID_ARG;
-  if ((st = check_caches(params, caches, n_layers, true, false)) != MIXKV_OK) return st;
+  if ((st = check_caches(caches, n_layers, true, false)) != MIXKV_OK) return st;
   const int eb = params->dtype == MIXKV_BF16 ? 2 : 4;
   if ((st = check_rows(s, eb, rows, n_layers, n_rows, false)) != MIXKV_OK) return st;
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);

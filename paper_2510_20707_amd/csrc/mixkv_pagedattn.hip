@@ -97,7 +97,10 @@ __device__ __forceinline__ void finish_chunk(const PShape &s, const AShape &a, c
 //     1.0 is u = 1 + code / 16, and B + S u a packed fp16 multiply-add with the strip's scales.  Fp16 rounds weights and values by 2^-11, an
 //     eighth of the output's own rounding; both are averaged over the rows.  The weights are relative to an offset that puts the
 //     largest near 2^8: fp16 then resolves weights down to 2^-32 of it.
+// Bound: memory for long heads: 64 sequences of 8192 rows, 8 heads of 128, 671 MB in 114 us, 5.9 TB/s, and the merge behind it; for
+// few rows the workgroup's own beginning and end (4 heads of 260 rows: 7.8 us).
 // ------------------------------------------------------------------------------------------------
+// Images of a wave's ring and waves per SIMD, as LDS holds them; us for 64 sequences of 8192 rows, 8 heads of 128: 2 and 3 125, 3 and 2 139.
 constexpr int kQ4Ring = 2, kQ4Waves = 3;
 constexpr float kTopWeight = 8.f, kWeightLimit = 16384.f;     // log2 of the largest weight where an offset is chosen; where it moves
 
@@ -117,7 +120,7 @@ __device__ __forceinline__ float row_sum(float x) {
   return x + row_turned<0x121>(x);
 }
 
-template <int D>
+template <int D, bool ONCE>
 __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShape a, AttnTable tab, float *part, float *part_ml, int64_t unit0) {
   constexpr int NG = D / 32, NB = D / 16, H = kAttnHeads, W = 4;
   constexpr int CODES = 16 * D, SCALES = 32 * NG * 4, TILE = 2 * (CODES + SCALES);   // bytes of a tile: keys' codes, values', keys' scales, values'
@@ -168,11 +171,11 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
     const int row = __builtin_amdgcn_readlane(x_rows, i) & 255;
     const char *kp = c.K + page, *vp = c.V + page;
 #pragma unroll
-    for (int j = 0; j < NL; ++j) load_to_lds<true>(kp + (uint32_t)(row * (D / 2)) + (k_off + j * 1024), img + j * 1024);
+    for (int j = 0; j < NL; ++j) load_to_lds<ONCE>(kp + (uint32_t)(row * (D / 2)) + (k_off + j * 1024), img + j * 1024);
 #pragma unroll
-    for (int j = 0; j < NL; ++j) load_to_lds<true>(vp + (uint32_t)(row * (D / 2)) + (uint32_t)(lane * 16 + j * 1024), img + CODES + j * 1024);
+    for (int j = 0; j < NL; ++j) load_to_lds<ONCE>(vp + (uint32_t)(row * (D / 2)) + (uint32_t)(lane * 16 + j * 1024), img + CODES + j * 1024);
     const char *sp = (s_keys ? kp : vp) + (uint32_t)(row * NG * 4) + s_off;
-    if (2 * SCALES / 16 == 64 || lane < 2 * SCALES / 16) load_to_lds<true>(sp, img + 2 * CODES);
+    if (2 * SCALES / 16 == 64 || lane < 2 * SCALES / 16) load_to_lds<ONCE>(sp, img + 2 * CODES);
   };
   auto begin = [&](int first) {                                // the batch's first tiles on their way
     batch(first);
@@ -385,8 +388,9 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
 //   fp32  products of four elements' contraction; a lane takes four neighbouring elements of a value row at a time, which are four blocks'
 //         operands, the blocks' rows then being every fourth element: no image.
 // Offsets as in decode_mfma_kernel.
+// Bound: memory, one tile of each wave in flight: bf16, 16 sequences of 8192 rows, 8 heads of 128, 537 MB in 94 us, 5.7 TB/s.
 // ------------------------------------------------------------------------------------------------
-template <int DT, int D>
+template <int DT, int D, bool ONCE>
 __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, AttnTable tab, float *part, float *part_ml, int64_t unit0) {
   constexpr bool F32 = DT == MIXKV_F32;
   constexpr int EB = F32 ? 4 : 2, RB = D * EB, PPR = RB / 16, NC = PPR / 4, NB = D / 16, H = kAttnHeads, W = 4;
@@ -433,7 +437,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Att
 #pragma unroll
       for (int r = 0; r < 2; ++r)
 #pragma unroll
-        for (int k = 0; k < NC; ++k) kr[r][k] = load_vec<true>(p + r * 16 * RB + k * 64);
+        for (int k = 0; k < NC; ++k) kr[r][k] = load_vec<ONCE>(p + r * 16 * RB + k * 64);
     };
     // value load j of a lane: bf16: piece lane % PPR of row RPL j + lane / PPR; fp32: elements 64 (j / 8) + 4 l16 + ... of row
     // 16 (j / 4 % 2) + 4 quad + j % 4
@@ -444,8 +448,8 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Att
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         const char *at = p + value_row(j) * RB + (F32 ? (j >> 3) * 256 + l16 * 16 : (lane % PPR) * 16);
-        if (live == 32) vr[j] = load_vec<true>(at);
-        else vr[j] = value_row(j) < live ? load_vec<true>(at) : u32x4{0u, 0u, 0u, 0u};   // rows that do not exist: zeros
+        if (live == 32) vr[j] = load_vec<ONCE>(at);
+        else vr[j] = value_row(j) < live ? load_vec<ONCE>(at) : u32x4{0u, 0u, 0u, 0u};   // rows that do not exist: zeros
       }
     };
     load_keys(0);
@@ -619,6 +623,17 @@ static size_t attn_slots(const PShape &s, const AShape &a, int n_layers) {
   return a.nchunks == 1 ? 0 : (size_t)n_layers * s.units_per_layer * a.gchunks * a.nchunks * a.gt;
 }
 static size_t attn_bytes(const PShape &s, const AShape &a, int n_layers) { return attn_slots(s, a, n_layers) * (s.D + 2) * sizeof(float); }
+// ONCE: the rows pass the caches by.  With more query heads to a KV head than a workgroup takes, several workgroups read the same rows, and they go
+// through the caches.  us by the caches and through them, rows of 128: 4-bit, 64 sequences of 8192, 4 query heads to a KV head 125 and 138, 48 heads
+// to one KV head 60 and 51; bf16, 16 of 8192, 4 to a head 94 and 107, 32 to a head 56 and 54; fp32, 32 to a head 103 and 98.
+template <bool ONCE, typename Go>
+static void launch_attention(const PShape &s, int dtype, Go &&go) {
+  constexpr int B16 = MIXKV_BF16, F32 = MIXKV_F32;
+  if (s.q4) { if (s.D == 128) go(paged_q4_kernel<128, ONCE>, paged_merge_kernel<B16, 128>); else go(paged_q4_kernel<64, ONCE>, paged_merge_kernel<B16, 64>); }
+  else if (dtype == B16) { if (s.D == 128) go(paged_rows_kernel<B16, 128, ONCE>, paged_merge_kernel<B16, 128>); else go(paged_rows_kernel<B16, 64, ONCE>, paged_merge_kernel<B16, 64>); }
+  else { if (s.D == 128) go(paged_rows_kernel<F32, 128, ONCE>, paged_merge_kernel<F32, 128>); else go(paged_rows_kernel<F32, 64, ONCE>, paged_merge_kernel<F32, 64>); }
+}
+
 static int clamp_rows(const PShape &s, int max_rows) { return std::min(max_rows, s.max_pages * s.P); }
 
 }  // namespace mixkv
@@ -643,7 +658,7 @@ extern "C" mixkv_status mixkv_paged_attention(const mixkv_paged_params *params, 
   mixkv_status st = make_pshape(params, &s);
   if (st != MIXKV_OK) return st;
   if (max_rows < 1) return MIXKV_ERR_INVALID_ARG;
-  if ((st = check_caches(params, caches, n_layers, true, false)) != MIXKV_OK) return st;
+  if ((st = check_caches(caches, n_layers, true, false)) != MIXKV_OK) return st;
   if (!layers) return MIXKV_ERR_INVALID_ARG;
   const bool sparse = layers[0].selected != nullptr;
   if (sparse && (max_selected < 1 || (int64_t)max_selected * s.P > (1 << 30))) return MIXKV_ERR_INVALID_ARG;
@@ -683,10 +698,8 @@ extern "C" mixkv_status mixkv_paged_attention(const mixkv_paged_params *params, 
       if (a.nchunks > 1)
         hipLaunchKernelGGL(merge, dim3((unsigned)s.units_per_layer, (unsigned)a.gt, z), dim3(256), 0, stream, s, a, t, (const float *)part, (const float *)part_ml, unit0);
     };
-    constexpr int B16 = MIXKV_BF16, F32 = MIXKV_F32;
-    if (s.q4) { if (s.D == 128) go(paged_q4_kernel<128>, paged_merge_kernel<B16, 128>); else go(paged_q4_kernel<64>, paged_merge_kernel<B16, 64>); }
-    else if (params->dtype == B16) { if (s.D == 128) go(paged_rows_kernel<B16, 128>, paged_merge_kernel<B16, 128>); else go(paged_rows_kernel<B16, 64>, paged_merge_kernel<B16, 64>); }
-    else { if (s.D == 128) go(paged_rows_kernel<F32, 128>, paged_merge_kernel<F32, 128>); else go(paged_rows_kernel<F32, 64>, paged_merge_kernel<F32, 64>); }
+    if (a.gchunks == 1) launch_attention<true>(s, params->dtype, go);
+    else launch_attention<false>(s, params->dtype, go);
     if (hipGetLastError() != hipSuccess) return MIXKV_ERR_HIP;
   }
   return MIXKV_OK;

@@ -243,6 +243,33 @@ def test_selection_of_equal_scores(what):
             assert sel[0, h].tolist() == O.select(s, keep, 1, 1), (keep, h)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pages", [500, 3000, 17000])
+def test_pages_whose_score_is_nan_come_last(dtype, pages):
+    D, P = 64, 32
+    rng = np.random.default_rng([23, pages])
+    lay = T.Layer(rng, "rows", dtype, D, P, [[pages * P]], pages, spare=0, bounds=True)
+    lay.K, lay.V = lay.K[:1], lay.V[:1]
+    cache = lay.device()
+    bad = rng.random(pages) < 0.5                                        # by place in the table
+    bits = cache.K_bounds.view(torch.int32 if dtype == "f32" else torch.int16)
+    ids = cache.page_table[0, 0, :pages].long()
+    bits[ids[torch.from_numpy(bad).to(ids.device)], 0, 5] = -1           # all bits of a smallest key set: a NaN of negative sign
+    Q = np.full((1, 1, D), -1.0)
+    good = int((~bad).sum())
+    for keep in (good - 3, good + 20):
+        (sel,), (n,) = B.mixkv_paged_select(lay.params(1), [B.PagedCache(None, None, cache.page_table, cache.lengths, cache.K_bounds)],
+                                            [T.to_device(Q, dtype)], keep, 0, 0)
+        got = sel[0, 0].cpu().numpy()
+        assert n.item() == keep and np.all(np.diff(got) > 0) and got[0] >= 0 and got[-1] < pages
+        taken = np.zeros(pages, bool)
+        taken[got] = True
+        if keep < good:
+            assert not np.any(taken & bad)
+        else:                                                            # the earliest ones of them
+            assert np.all(taken[~bad]) and np.array_equal(np.flatnonzero(taken & bad), np.flatnonzero(bad)[:keep - good])
+
+
 @pytest.mark.parametrize("fmt,dtype", KINDS)
 def test_a_decoding_loop(fmt, dtype):
     """A prompt, then eight tokens: rotated rows appended, pages selected, attention over those and over all, against the oracle's own
