@@ -45,6 +45,10 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
+// The unit (of gridDim.x) of a workgroup.  Workgroups go to the chip's eight dies in turn by their number, so a
+// multiple of eight units would leave each of a unit's workgroups to one die, and units are of unequal length: the units turn with blockIdx.y.
+__device__ __forceinline__ int dealt_unit() { return (int)((blockIdx.x + blockIdx.y + (blockIdx.y >> 1)) % gridDim.x); }
+
 __device__ __forceinline__ float f16_value(uint32_t bits) { return (float)__builtin_bit_cast(_Float16, (uint16_t)bits); }
 __device__ __forceinline__ uint32_t f16_bits(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }
 // Bit position of element e of a word of eight codes.

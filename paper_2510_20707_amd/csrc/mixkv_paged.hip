@@ -45,6 +45,10 @@ __device__ __forceinline__ RowRange row_range(const PShape &s, const PCache &c, 
   return x;
 }
 
+// What another lane of the row of 16 has, by a move of the vector ALU (DPP control CTRL).
+template <int CTRL>
+__device__ __forceinline__ int lane_moved(int x) { return __builtin_amdgcn_mov_dpp(x, CTRL, 0xf, 0xf, true); }
+
 // Eight elements of a row as memory has them, and as floats.
 template <int DT> struct Run;
 template <> struct Run<MIXKV_BF16> {
@@ -211,23 +215,21 @@ __device__ __forceinline__ GroupScale run_scale(const Run<MIXKV_BF16> &x) {
   for (int i = 0; i < 4; ++i) v[i] = R::turn(__builtin_bit_cast(R::s16x2, (uint32_t)x.v[i]));
   lo = __builtin_elementwise_min(__builtin_elementwise_min(v[0], v[1]), __builtin_elementwise_min(v[2], v[3]));
   hi = __builtin_elementwise_max(__builtin_elementwise_max(v[0], v[1]), __builtin_elementwise_max(v[2], v[3]));
-#pragma unroll
-  for (int off = 1; off <= 2; off <<= 1) {
-    lo = __builtin_elementwise_min(lo, __builtin_bit_cast(R::s16x2, __shfl_xor(__builtin_bit_cast(int, lo), off)));
-    hi = __builtin_elementwise_max(hi, __builtin_bit_cast(R::s16x2, __shfl_xor(__builtin_bit_cast(int, hi), off)));
-  }
+  lo = __builtin_elementwise_min(lo, __builtin_bit_cast(R::s16x2, lane_moved<0xb1>(__builtin_bit_cast(int, lo))));   // lane ^ 1
+  hi = __builtin_elementwise_max(hi, __builtin_bit_cast(R::s16x2, lane_moved<0xb1>(__builtin_bit_cast(int, hi))));
+  lo = __builtin_elementwise_min(lo, __builtin_bit_cast(R::s16x2, lane_moved<0x4e>(__builtin_bit_cast(int, lo))));   // lane ^ 2
+  hi = __builtin_elementwise_max(hi, __builtin_bit_cast(R::s16x2, lane_moved<0x4e>(__builtin_bit_cast(int, hi))));
   const R::s16x2 ends = R::turn(R::s16x2{lo[0] < lo[1] ? lo[0] : lo[1], hi[0] > hi[1] ? hi[0] : hi[1]});
   const uint32_t w = __builtin_bit_cast(uint32_t, ends);
   return group_scale(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
 }
 
-// The codes of eight elements in a word.  16 (x - base - step) / step as one multiply-add with 16 / step is off by at most 2^-22 of what its
-// product and its constant are together (the quotient, the constant and the sum are rounded by 2^-24 each).  Where that could decide a
-// rounding, and in bf16 rows exact ties between two codes are frequent (a run in some hundred), the side of the tie m + 1/2 is that of
-// 16 d - (m + 1/2) step, whose sign one multiply-add has exactly if d = x - base - step is; if it is not, or if elements have to be clipped, 64
-// bits decide.
+// The codes of eight elements in a word.  16 (x - base - step) / step as one multiply-add with 16 / step is off by less than 2^-21 of what its
+// product and its constant are together (the reciprocal by 2^-23, the constant and the sum by another 2^-24 each, and the constant holds the
+// reciprocal).  An element for which that could decide the rounding, and in bf16 rows exact ties between two codes are frequent (a run in some
+// hundred), is taken again in 64 bits, one after another, as are those of a group with elements to be clipped.
 __device__ __forceinline__ uint32_t run_codes(const Run<MIXKV_BF16> &x, const GroupScale &g) {
-  const float r = g.step > 0.f ? 16.f / g.step : 0.f, k = -(g.base + g.step) * r;
+  const float r = g.step > 0.f ? 16.f * __builtin_amdgcn_rcpf(g.step) : 0.f, k = -(g.base + g.step) * r;
   uint32_t w = 0;
   float off = 0.f;
 #pragma unroll
@@ -236,30 +238,22 @@ __device__ __forceinline__ uint32_t run_codes(const Run<MIXKV_BF16> &x, const Gr
     off = __builtin_fmaxf(off, __builtin_fabsf(t - n));
     w |= (uint32_t)__builtin_amdgcn_fmed3f(n, 0.f, 15.f) << code_shift(e);
   }
-  if ((g.wide || off > 0.5f - 0x1p-22f * (40.f + 2.f * fabsf(k))) && g.step > 0.f) {
-#pragma clang fp contract(off)
-    bool exact = !g.wide && fabsf(k) < 0x1p16f;
-    w = 0;
+  const float far = 0.5f - 0x1p-21f * (40.f + 2.f * fabsf(k));
+  if ((g.wide || off > far) && g.step > 0.f) {
+    uint32_t again = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float v = x.at(e), p = v - g.base, d = p - g.step;
-      const float vb = v - p, pb = p - d;                  // what the differences took off: base and step, if nothing was rounded
-      exact &= vb == g.base && p + vb == v && pb == g.step && d + pb == p;
-      const float m = __builtin_floorf(fminf(fmaxf(d * r, -1.f), 16.f));   // the rounded quotient may be past m or m + 1 by a little: then the tie is far
-      const float side = fmaf(-(m + 0.5f), g.step, 16.f * d);
-      const bool odd = ((int)m & 1) != 0;
-      const float n = m + (side > 0.f || (side == 0.f && odd) ? 1.f : 0.f);
-      w |= (uint32_t)fminf(fmaxf(n, 0.f), 15.f) << code_shift(e);
+      const float t = fmaf(x.at(e), r, k);
+      again |= g.wide || __builtin_fabsf(t - __builtin_rintf(t)) > far ? 1u << e : 0u;
     }
-    if (!exact) {
-      w = 0;
 #pragma unroll 1
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t q = e < 2 ? x.v[0] : (e < 4 ? x.v[1] : (e < 6 ? x.v[2] : x.v[3]));
-        const double v = clip(__uint_as_float(e & 1 ? q & 0xffff0000u : q << 16));
-        const double n = __builtin_rint((v - (double)g.base - (double)g.step) * 16.0 / (double)g.step);
-        w |= (uint32_t)(n < 0. ? 0. : (n > 15. ? 15. : n)) << code_shift(e);
-      }
+    while (again != 0) {
+      const int e = __builtin_ctz(again);
+      again &= again - 1;
+      const uint32_t q = e < 4 ? (e < 2 ? x.v[0] : x.v[1]) : (e < 6 ? x.v[2] : x.v[3]), sh = code_shift(e);
+      const double v = clip(__uint_as_float(e & 1 ? q & 0xffff0000u : q << 16));
+      const double n = __builtin_rint((v - (double)g.base - (double)g.step) * 16.0 / (double)g.step);
+      w = (w & ~(15u << sh)) | ((uint32_t)(n < 0. ? 0. : (n > 15. ? 15. : n)) << sh);
     }
   }
   return w;
@@ -373,14 +367,14 @@ __global__ __launch_bounds__(kPagedThreads) void append_step_kernel(PShape s, PT
 }
 
 // ------------------------------------------------------------------------------------------------
-// append_queries_kernel (many rows).  blockIdx.x: (layer, sequence); blockIdx.y: workers on its rows, a wave to a row.  A lane has 16 bytes of every
-// 64 / LR-th head (neighbouring lanes neighbouring bytes: an instruction takes a kilobyte of the row), its elements' partners are in the lane
+// append_queries_kernel (many rows).  Workers on the rows of a (layer, sequence), a wave to a row, the sequences one after another.  A lane has 16 bytes of
+// every 64 / LR-th head (neighbouring lanes neighbouring bytes: an instruction takes a kilobyte of the row), its elements' partners are in the lane
 // LR / 2 away, and it keeps its angles for all heads, or, where the KV heads do not have the same rows, for those of
 // one KV head at a time.
 // Bound: memory; loads and stores pass the caches by (a prompt's queries are more than they keep).  us for four prompts of 72 thousand
-// tokens together, 28 heads of 128, 1.03 GB, where torch's copy of the same strided rows takes 199: 254 (with angles held as 64-bit numbers 277, in 16 384
-// workgroups instead of 4096 293); with eight lanes to a head and eight
-// heads' halves in flight, 128 bytes at a place, 268 (through the caches 287).
+// tokens together, 28 heads of 128, 1.03 GB, where torch's copy of the same strided rows takes 199: 208, 5 TB/s; with workgroups that follow each other on
+// different sequences 254, for DRAM then has four places to read from and to write to; in 1024, 2048, 8192 and 16 384 workgroups instead of 4096 218, 211,
+// 209, 228; with the next row's positions fetched ahead and a third of the instructions less 218.
 // ------------------------------------------------------------------------------------------------
 template <int OFF>
 __device__ __forceinline__ uint32_t from_lane_xor(uint32_t x) {
@@ -389,11 +383,11 @@ __device__ __forceinline__ uint32_t from_lane_xor(uint32_t x) {
 }
 
 template <int DT, int D>
-__global__ __launch_bounds__(kPagedThreads) void append_queries_kernel(PShape s, PTable tab, PRope rp, int n_rows) {
+__global__ __launch_bounds__(kPagedThreads) void append_queries_kernel(PShape s, PTable tab, PRope rp, int n_rows, int workers) {
   constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, E = 16 / EB, RB = D * EB, LR = RB / 16, HPI = 64 / LR, U = 8;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane % LR, sub = lane / LR;
   const bool upper = l >= LR / 2;
-  const int layer = blockIdx.x / s.batch, b = blockIdx.x - layer * s.batch;
+  const int lb = blockIdx.x / workers, worker = blockIdx.x - lb * workers, layer = lb / s.batch, b = lb - layer * s.batch;
   const PRows d = tab.r[layer];
   const RowRange x0 = row_range(s, tab.c[layer], d, b * s.hkv, n_rows);
   bool same = true;
@@ -404,7 +398,7 @@ __global__ __launch_bounds__(kPagedThreads) void append_queries_kernel(PShape s,
   for (int h = 0; h < s.hkv; h += same ? s.hkv : 1) {
     const RowRange x = h == 0 ? x0 : row_range(s, tab.c[layer], d, b * s.hkv + h, n_rows);
     const int heads = same ? s.hq : s.G;
-    for (int r = x.r0 + (int)blockIdx.y * 4 + wave; r < x.r1; r += (int)gridDim.y * 4) {
+    for (int r = x.r0 + worker * 4 + wave; r < x.r1; r += workers * 4) {
       const int64_t row = r + x.shift;
       const char *src = d.Q + row * d.qsn + (int64_t)h * s.G * d.qsh + l * 16;
       char *dst = d.Q_out + (row * s.hq + h * s.G) * RB + l * 16;
@@ -462,8 +456,8 @@ __global__ __launch_bounds__(kPagedThreads) void append_queries_kernel(PShape s,
 // ------------------------------------------------------------------------------------------------
 // append_pages_kernel (many rows).  blockIdx.x: (layer, sequence, KV head); blockIdx.y: workers on the head's pages, a workgroup to a page: D/16 lanes
 // to a row, codes of values turned into the strips' words through LDS, bounds folded over the page's passes.
-// Bound: in 4 bits the quantiser's and the rotation's arithmetic.  us for four prompts of 72 thousand tokens together, 4 KV heads of 128, 147 MB in: 175
-// (in 1024 workgroups 194, 512 260, with 512 threads 214); without rotation 139; bf16 pages without rotation 84, which is memory.
+// Bound: in 4 bits the quantiser's and the rotation's arithmetic.  us for four prompts of 5 to 32 thousand tokens, 4 KV heads of 128, 147 MB in: 118 (without
+// the units dealt to the dies in turn 158, and in at most 4096 workgroups 121).
 // ------------------------------------------------------------------------------------------------
 template <int DT, int D, bool Q4>
 __global__ __launch_bounds__(kPagedThreads) void append_pages_kernel(PShape s, PTable tab, PRope rp, int n_rows) {
@@ -471,7 +465,7 @@ __global__ __launch_bounds__(kPagedThreads) void append_pages_kernel(PShape s, P
   __shared__ uint32_t words[Q4 ? RS * RUNS : 1];           // codes of the value rows of a pass, a word per eight elements
   __shared__ __align__(16) char red[4][2 * RB];
   const int tid = threadIdx.x, j = tid % LPR, slot = tid / LPR, lane = tid & 63, wave = tid >> 6;
-  const int layer = blockIdx.x / s.units_per_layer, u = blockIdx.x - layer * s.units_per_layer;
+  const int ul = dealt_unit(), layer = ul / s.units_per_layer, u = ul - layer * s.units_per_layer;
   const int h = u % s.hkv;
   const PCache c = tab.c[layer];
   const PRows d = tab.r[layer];
@@ -575,14 +569,15 @@ __global__ __launch_bounds__(kPagedThreads) void append_pages_kernel(PShape s, P
 
 // ------------------------------------------------------------------------------------------------
 // read_paged_kernel.  blockIdx.x: (layer, sequence, KV head); blockIdx.y: workers on the head's passes of RS rows.
-// Bound: memory, the dense rows' stores first: the same four prompts, 46 MB of 4-bit pages to 147 MB of rows, in 56 us.
+// Bound: memory, the dense rows' stores first: the same four prompts, 46 MB of 4-bit pages to 147 MB of rows, in 47 us
+// (without the units dealt to the dies in turn 55).
 // ------------------------------------------------------------------------------------------------
 template <int DT, int D, bool Q4>
 __global__ __launch_bounds__(D * 2) void read_paged_kernel(PShape s, PTable tab, int n_rows) {
   constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RS = 32, RB = D * EB, STRIP = D + 8;   // (a strip's words, padded)
   __shared__ __align__(16) uint32_t words[Q4 ? 4 * STRIP : 4];
   const int tid = threadIdx.x, j = tid % LPR, slot = tid / LPR;
-  const int layer = blockIdx.x / s.units_per_layer, u = blockIdx.x - layer * s.units_per_layer;
+  const int ul = dealt_unit(), layer = ul / s.units_per_layer, u = ul - layer * s.units_per_layer;
   const int h = u % s.hkv;
   const PCache c = tab.c[layer];
   const PRows d = tab.r[layer];
@@ -773,7 +768,7 @@ extern "C" mixkv_status mixkv_paged_append(const mixkv_paged_params *params, con
       const int pw = workers(((int64_t)max_count + s.P - 2) / s.P + 1, units), qw = workers(((int64_t)max_count + 3) / 4, (int64_t)nl * s.batch, 4096);
       auto go = [&](auto kern, auto qkern) {
         hipLaunchKernelGGL(kern, dim3((unsigned)units, (unsigned)pw), dim3(kPagedThreads), 0, stream, s, t, rp, n_rows);
-        if (queries) hipLaunchKernelGGL(qkern, dim3((unsigned)(nl * s.batch), (unsigned)qw), dim3(kPagedThreads), 0, stream, s, t, rp, n_rows);
+        if (queries) hipLaunchKernelGGL(qkern, dim3((unsigned)(nl * s.batch * qw)), dim3(kPagedThreads), 0, stream, s, t, rp, n_rows, qw);
       };
       constexpr int B16 = MIXKV_BF16, F32 = MIXKV_F32;
       if (s.q4) { if (s.D == 128) go(append_pages_kernel<B16, 128, true>, append_queries_kernel<B16, 128>); else go(append_pages_kernel<B16, 64, true>, append_queries_kernel<B16, 64>); }
