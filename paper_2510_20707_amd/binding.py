@@ -508,6 +508,13 @@ def _paged_device(caches: Sequence[PagedCache]) -> torch.device:
     return t.device
 
 
+def _paged_stream(device: torch.device, stream) -> C.c_void_p:
+    """The stream of a call prepared on `device`, which has to be the current one then too."""
+    current = torch.cuda.current_device()
+    _need(current == device.index and (stream is None or stream.device_index == current), "the call was prepared on another device")
+    return C.c_void_p(torch._C._cuda_getCurrentRawStream(current) if stream is None else stream.cuda_stream)
+
+
 def _paged_caches(p: MixkvPagedParams, caches: Sequence[PagedCache], pages: bool, bounds: bool, device):
     units, pool = (p.batch, p.n_kv_heads), 0
     if pages:
@@ -547,12 +554,13 @@ def _paged_rows(p: MixkvPagedParams, rows: Sequence[PagedRows], queries: bool, d
 
 
 class PreparedPagedAppend:
-    """The C arguments of one mixkv_paged_append call, built once over buffers that a serving loop keeps.  `max_count`: the largest
+    """The C arguments of one mixkv_paged_append call, built once over buffers that a serving loop keeps (a workspace that a prepared call allocates is
+    the current stream's: a run on another stream has to wait for that one, as for any tensor).  `max_count`: the largest
     row_count as far as the host knows it (None: the dense tensor's rows)."""
 
     def __init__(self, p: MixkvPagedParams, caches: Sequence[PagedCache], rows: Sequence[PagedRows], rope: Optional[Rope] = None,
                  max_count: Optional[int] = None):
-        device = _paged_device(caches)
+        self.device = device = _paged_device(caches)
         _need(len(caches) == len(rows), "a rows entry for every cache")
         self.p, self.n, self.caches = p, len(caches), _paged_caches(p, caches, True, False, device)
         self.rows, self.n_rows = _paged_rows(p, rows, True, device)
@@ -571,7 +579,7 @@ class PreparedPagedAppend:
         self._call = lib().mixkv_paged_append
 
     def run(self, stream=None):
-        _check(self._call(*self._args, _stream(stream)), "mixkv_paged_append")
+        _check(self._call(*self._args, _paged_stream(self.device, stream)), "mixkv_paged_append")
 
 
 def mixkv_paged_append(p: MixkvPagedParams, caches: Sequence[PagedCache], rows: Sequence[PagedRows], rope: Optional[Rope] = None,
@@ -584,7 +592,7 @@ class PreparedPagedRead:
     """The C arguments of one mixkv_paged_read call: rows[i].K and .V receive the newest row_count rows of every head."""
 
     def __init__(self, p: MixkvPagedParams, caches: Sequence[PagedCache], rows: Sequence[PagedRows], max_count: Optional[int] = None):
-        device = _paged_device(caches)
+        self.device = device = _paged_device(caches)
         _need(len(caches) == len(rows), "a rows entry for every cache")
         self.p, self.n, self.caches = p, len(caches), _paged_caches(p, caches, True, False, device)
         self.rows, self.n_rows = _paged_rows(p, rows, False, device)
@@ -594,7 +602,7 @@ class PreparedPagedRead:
         self._call = lib().mixkv_paged_read
 
     def run(self, stream=None):
-        _check(self._call(*self._args, _stream(stream)), "mixkv_paged_read")
+        _check(self._call(*self._args, _paged_stream(self.device, stream)), "mixkv_paged_read")
 
 
 def mixkv_paged_read(p: MixkvPagedParams, caches: Sequence[PagedCache], rows: Sequence[PagedRows], max_count: Optional[int] = None, stream=None):
@@ -620,7 +628,7 @@ class PreparedPagedSelect:
 
     def __init__(self, p: MixkvPagedParams, caches: Sequence[PagedCache], Qs, selected, n_selected, keep_first: int = 1, keep_last: int = 1,
                  workspace="alloc"):
-        device = _paged_device(caches)
+        self.device = device = _paged_device(caches)
         n = len(caches)
         _need(n == len(Qs) == len(selected) == len(n_selected), "queries and selections for every cache")
         self.p, self.n, self.caches, self.most = p, n, _paged_caches(p, caches, False, True, device), selected[0].shape[-1]
@@ -638,16 +646,17 @@ class PreparedPagedSelect:
         self._call = lib().mixkv_paged_select
 
     def run(self, stream=None):
-        _check(self._call(*self._args, _stream(stream)), "mixkv_paged_select")
+        _check(self._call(*self._args, _paged_stream(self.device, stream)), "mixkv_paged_select")
 
 
 def mixkv_paged_select(p: MixkvPagedParams, caches: Sequence[PagedCache], Qs, max_selected: int, keep_first: int = 1, keep_last: int = 1,
                        workspace="alloc", stream=None):
-    """Returns per layer the places of the selected pages [batch, Hkv, max_selected] and their numbers [batch, Hkv]."""
-    dev, n = caches[0].lengths.device, len(caches)
-    selected = [torch.empty((p.batch, p.n_kv_heads, max_selected), dtype=torch.int32, device=dev) for _ in range(n)]
-    n_selected = [torch.empty((p.batch, p.n_kv_heads), dtype=torch.int32, device=dev) for _ in range(n)]
-    PreparedPagedSelect(p, caches, Qs, selected, n_selected, keep_first, keep_last, workspace).run(stream)
+    """Returns per layer the places of the selected pages [batch, Hkv, max_selected] and their numbers [batch, Hkv], allocated on the call's stream."""
+    dev, n = _paged_device(caches), len(caches)
+    with torch.cuda.stream(stream):                   # what is allocated here is the stream's (None: the current one's)
+        selected = [torch.empty((p.batch, p.n_kv_heads, max_selected), dtype=torch.int32, device=dev) for _ in range(n)]
+        n_selected = [torch.empty((p.batch, p.n_kv_heads), dtype=torch.int32, device=dev) for _ in range(n)]
+        PreparedPagedSelect(p, caches, Qs, selected, n_selected, keep_first, keep_last, workspace).run(stream)
     return selected, n_selected
 
 
@@ -664,7 +673,7 @@ class PreparedPagedAttention:
 
     def __init__(self, p: MixkvPagedParams, caches: Sequence[PagedCache], Qs, outs, selected=None, n_selected=None,
                  max_rows: Optional[int] = None, workspace="alloc"):
-        device = _paged_device(caches)
+        self.device = device = _paged_device(caches)
         n, sparse = len(caches), selected is not None
         _need(n == len(Qs) == len(outs) and (not sparse or n == len(selected) == len(n_selected)), "queries, outputs and selections for every cache")
         self.p, self.n, self.caches = p, n, _paged_caches(p, caches, True, False, device)
@@ -686,14 +695,16 @@ class PreparedPagedAttention:
         self._call = lib().mixkv_paged_attention
 
     def run(self, stream=None):
-        _check(self._call(*self._args, _stream(stream)), "mixkv_paged_attention")
+        _check(self._call(*self._args, _paged_stream(self.device, stream)), "mixkv_paged_attention")
 
 
 def mixkv_paged_attention(p: MixkvPagedParams, caches: Sequence[PagedCache], Qs, selected=None, n_selected=None, max_rows: Optional[int] = None,
                           workspace="alloc", stream=None):
-    """Returns per layer the attention output [batch, Hq, D] of the new token of every sequence."""
-    outs = [torch.empty_like(q) for q in Qs]
-    PreparedPagedAttention(p, caches, Qs, outs, selected, n_selected, max_rows, workspace).run(stream)
+    """Returns per layer the attention output [batch, Hq, D] of the new token of every sequence, allocated on the call's stream."""
+    _paged_device(caches)
+    with torch.cuda.stream(stream):                   # what is allocated here is the stream's (None: the current one's)
+        outs = [torch.empty_like(q) for q in Qs]
+        PreparedPagedAttention(p, caches, Qs, outs, selected, n_selected, max_rows, workspace).run(stream)
     return outs
 
 

@@ -524,3 +524,36 @@ def test_calls_on_two_streams_with_workspaces_of_their_own():
         torch.cuda.synchronize()
         for _, _, alone, got in jobs:
             assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(alone, got))
+
+
+def test_a_call_on_a_stream_of_its_own_allocates_there():
+    """Outputs and workspace of a call on another stream are that stream's: work that still runs on the current one does not share their memory."""
+    rng = np.random.default_rng(28)
+    lay = T.Layer(rng, "4bit", "bf16", 128, 32, [[700, 900], [30, 400]], 30, fill=True, bounds=True)
+    c, q, p = lay.device(), T.to_device(_queries(rng, lay, 8), "bf16"), lay.params(8)
+    want, (sel,), side = B.mixkv_paged_attention(p, [c], [q])[0], B.mixkv_paged_select(p, [c], [q], 5)[0], torch.cuda.Stream()
+    torch.cuda.synchronize()
+    busy = torch.zeros(1 << 26, device=T.DEV)
+    for _ in range(5):
+        for _ in range(4):
+            busy.add_(1)
+        trash = [torch.full((1 << n,), 127, dtype=torch.uint8, device=T.DEV) for n in range(9, 20)]
+        del trash                                                        # free for the current stream, still to be written to there
+        out = B.mixkv_paged_attention(p, [c], [q], stream=side)[0]
+        picked = B.mixkv_paged_select(p, [c], [q], 5, stream=side)[0][0]
+        torch.cuda.synchronize()
+        assert torch.equal(out.view(torch.int16), want.view(torch.int16)) and torch.equal(picked, sel)
+
+
+def test_a_prepared_call_belongs_to_its_device(monkeypatch):
+    rng = np.random.default_rng(29)
+    lay = T.Layer(rng, "rows", "f32", 64, 32, [[40, 7]], 2, fill=True, bounds=True)
+    c, q, p = lay.device(), torch.zeros((1, 2, 64), device=T.DEV), lay.params(2)
+    call = B.PreparedPagedAttention(p, [c], [q], [torch.empty_like(q)])
+    call.run()
+    torch.cuda.synchronize()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)         # as a program that has gone on to another device
+    with pytest.raises(ValueError):
+        call.run()
+    with pytest.raises(ValueError):
+        B.PreparedPagedAttention(p, [c], [q], [torch.empty_like(q)])
