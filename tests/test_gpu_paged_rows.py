@@ -123,6 +123,27 @@ def test_heads_of_unequal_length_from_one_block(fmt, dtype, D):
 
 
 @pytest.mark.parametrize("fmt,dtype", KINDS)
+@pytest.mark.parametrize("D,hkv", [(128, 1), (128, 2), (64, 2)])
+@pytest.mark.parametrize("equal", [True, False])
+def test_many_query_heads(fmt, dtype, D, hkv, equal):
+    # more query heads than a wave takes at once; KV heads with the same rows, or each with its own and their queries alone
+    P, hq = 32, 74
+    print(f"[case] append queries {fmt} {dtype} D={D} Hkv={hkv} equal={equal}", flush=True)
+    rng = np.random.default_rng([30, D, hkv])
+    lens = np.array([[70] * hkv, [41] * hkv])
+    count = np.array([[37] * hkv, [9] * hkv])
+    start = np.array([[0] * hkv, [37] * hkv])
+    if not equal:
+        count[:, -1] -= 8
+        start[:, -1] += 3
+    lay = T.Layer(rng, fmt, dtype, D, P, lens, 3, bounds=True)
+    K, V, Q = (O.as_dtype(rng.standard_normal((50, h, D)) * 2, dtype) for h in (hkv, hkv, hq))
+    rope = (*_tables(rng, 90, D // 2), rng.integers(0, 90, (3, 50)).astype(np.int32), (D // 8, 3 * D // 16, 3 * D // 16))
+    _append_and_check(rng, lay, hq, K, V, start, count, Q, rope)
+    _append_and_check(rng, lay, hq, K, V, start, count, Q, rope, max_count=2)
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS)
 def test_rows_and_pages_that_do_not_exist_are_left_out(fmt, dtype):
     # dense rows before the first and behind the last, more rows than the head is long, lengths beyond the table, table entries that are
     # no pages of the pool
@@ -157,6 +178,20 @@ def test_every_code_of_ordinary_rows():
     rng = np.random.default_rng(7)
     lay = T.Layer(rng, "4bit", "bf16", D, P, [[n]], 16)
     K, V = (O.as_dtype(rng.standard_normal((n, 1, D)) * np.exp(rng.standard_normal((n, 1, 1)) * 3) + rng.standard_normal((n, 1, 1)), "bf16") for _ in range(2))
+    _append_and_check(rng, lay, 1, K, V, [[0]], [[n]])
+
+
+def test_codes_of_rows_far_from_zero_and_on_grids():
+    # offsets up to 2^12 times the spread, elements on grids of powers of two (exact ties between codes), a few tiny ones among them,
+    # groups with elements beyond the format's range
+    D, P, n = 128, 128, 2000
+    rng = np.random.default_rng(31)
+    lay = T.Layer(rng, "4bit", "bf16", D, P, [[n]], 16)
+    scale = lambda lo, hi: 2.0 ** rng.integers(lo, hi, (n, 1, 1))  # noqa: E731
+    grid = np.round(rng.standard_normal((n, 1, D)) * 16) * scale(-12, 9) + np.round(rng.standard_normal((n, 1, 1)) * 8) * scale(-6, 4)
+    K = np.where(rng.random((n, 1, D)) < 0.02, rng.standard_normal((n, 1, D)) * 1e-20, grid)
+    V = rng.standard_normal((n, 1, D)) * scale(-14, 13) + rng.standard_normal((n, 1, 1)) * scale(-8, 13)
+    K, V = O.as_dtype(K, "bf16"), O.as_dtype(V, "bf16")
     _append_and_check(rng, lay, 1, K, V, [[0]], [[n]])
 
 
