@@ -560,13 +560,18 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PShape s, AShape a, At
   if (g >= min(kAttnHeads, s.G - gc * kAttnHeads)) return;
   const PCache c = tab.c[layer];
   const AttnLayer l = tab.l[layer];
-  const int used = chunks_used(a, head_tiles(s, a, l, u, head_rows(s, c, u)));
-  if (used <= 1) return;
   const int64_t slot = slot_of(s, a, unit0, layer, u, gc, 0) + g;
   const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + slot;
   const float *rows = part + slot * D + 4 * t;
-  float m = -INFINITY;
-  for (int i = tid; i < used; i += 256) m = fmaxf(m, ml[(int64_t)i * a.gt].x);
+  // the thread's first chunks, asked for beside the head's length: in bounds, and of no use where the head has fewer
+  const int64_t i0 = (int64_t)min(slice, a.nchunks - 1) * a.gt;
+  const float m0 = ml[(int64_t)min(tid, a.nchunks - 1) * a.gt].x;
+  const float2 x0 = ml[i0];
+  const f32x4 r0 = *reinterpret_cast<const f32x4 *>(rows + i0 * D);
+  const int used = chunks_used(a, head_tiles(s, a, l, u, head_rows(s, c, u)));
+  if (used <= 1) return;
+  float m = tid < used ? m0 : -INFINITY;
+  for (int i = tid + 256; i < used; i += 256) m = fmaxf(m, ml[(int64_t)i * a.gt].x);
   m = wave_reduce<WMax>(m, -INFINITY);
   if ((tid & 63) == 0) red[tid >> 6] = m;
   __syncthreads();
@@ -574,8 +579,13 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PShape s, AShape a, At
   const float mu = m == -INFINITY ? 0.f : m;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   float tot = 0.f;
+  if (slice < used) {
+    const float f = fast_exp2(x0.x - mu);
+    acc = r0 * f;
+    tot = x0.y * f;
+  }
 #pragma unroll 4
-  for (int i = slice; i < used; i += S) {
+  for (int i = slice + S; i < used; i += S) {
     const float2 x = ml[(int64_t)i * a.gt];
     const float f = fast_exp2(x.x - mu);
     acc += *reinterpret_cast<const f32x4 *>(rows + (int64_t)i * a.gt * D) * f;
