@@ -45,9 +45,9 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// The unit (of gridDim.x) of a workgroup.  Workgroups go to the chip's eight dies in turn by their number, so a
-// multiple of eight units would leave each of a unit's workgroups to one die, and units are of unequal length: the units turn with blockIdx.y.
-__device__ __forceinline__ int dealt_unit() { return (int)((blockIdx.x + blockIdx.y + (blockIdx.y >> 1)) % gridDim.x); }
+// The unit of the workgroup number x + units * turn, x < units.  Workgroups go to the chip's eight dies in turn by their number, so a
+// multiple of eight units would leave each of a unit's workgroups to one die, and units are of unequal length: the units move on with the turns.
+__device__ __forceinline__ int dealt_unit(int x, int turn, int units) { return (int)(((uint32_t)x + (uint32_t)turn + ((uint32_t)turn >> 1)) % (uint32_t)units); }
 
 __device__ __forceinline__ float f16_value(uint32_t bits) { return (float)__builtin_bit_cast(_Float16, (uint16_t)bits); }
 __device__ __forceinline__ uint32_t f16_bits(float x) { return __builtin_bit_cast(uint16_t, (_Float16)x); }

@@ -10,12 +10,12 @@ namespace mixkv {
 constexpr int kPagedLayers = 16;         // pointer-table entries of a launch: the dense rows' strides travel with them
 constexpr int kPagedThreads = 256;
 
-// Rows of a head up to which a few lanes walk them (append_step_kernel) instead of a workgroup to a page (append_pages_kernel and
-// append_queries_kernel: 9 us of launches, shared memory and barriers whatever the count).  us for 1, 2, 3, 4, 6, 8 rows of 8 heads of 128 with 32 query heads,
-// bounds kept, walked | by pages: bf16 rows, one sequence 3.7 5.0 6.3 7.3 9.9 12.6 | 9.4 9.5 9.4 9.2 9.5 9.4, 64 sequences 3.9 5.3 6.8 8.2 11.5 16.5 | 10.8
-// 10.9 11.1 11.4 11.5 12.5; 4-bit with the rows read back, one sequence 9.7 13.5 17.3 21.6 29.0 36.6 | 15.8 16.3 16.7 17.0 17.4 17.4, 64
-// sequences 11.1 14.9 18.7 23.3 31.7 40.8 | 19.1 20.7 21.0 23.9 25.4 26.3.
-static int step_rows(bool q4) { return q4 ? 3 : 5; }
+// Rows of a head up to which a few lanes walk them (append_step_kernel) instead of a workgroup to a page and a wave to a row of queries
+// (append_many_kernel: shared memory and barriers whatever the count).  us for 1, 2, 3, 4, 6, 8 rows of 8 heads of 128 with 32 query heads, bounds
+// kept, walked | by pages: bf16 rows, one sequence 3.7 5.0 6.4 7.3 10.0 12.7 | 6.1 6.3 6.3 6.5 6.6 6.6, 64 sequences 4.0 5.4 6.8 8.2 11.5 17.4 | 7.7 8.9
+// 9.1 9.2 9.4 9.8; 4-bit with the rows read back, one sequence 8.9 12.1 15.8 18.8 26.1 33.1 | 10.3 10.3 10.4 10.4 10.5 10.6, 64 sequences
+// 9.7 12.9 16.4 20.1 28.0 35.9 | 12.5 14.1 15.0 16.7 17.7 18.6.
+static int step_rows(bool q4) { return q4 ? 1 : 3; }
 
 struct PRows {
   char *K, *V;
@@ -367,7 +367,7 @@ __global__ __launch_bounds__(kPagedThreads) void append_step_kernel(PShape s, PT
 }
 
 // ------------------------------------------------------------------------------------------------
-// append_queries_kernel (many rows).  Workers on the rows of a (layer, sequence), a wave to a row, the sequences one after another.  A lane has 16 bytes of
+// append_queries (many rows).  Workers on the rows of a (layer, sequence), a wave to a row, the sequences one after another.  A lane has 16 bytes of
 // every 64 / LR-th head (neighbouring lanes neighbouring bytes: an instruction takes a kilobyte of the row), its elements' partners are in the lane
 // LR / 2 away, and it keeps its angles for all heads, or, where the KV heads do not have the same rows, for those of
 // one KV head at a time.
@@ -383,11 +383,11 @@ __device__ __forceinline__ uint32_t from_lane_xor(uint32_t x) {
 }
 
 template <int DT, int D>
-__global__ __launch_bounds__(kPagedThreads) void append_queries_kernel(PShape s, PTable tab, PRope rp, int n_rows, int workers) {
+__device__ __forceinline__ void append_queries(const PShape &s, const PTable &tab, const PRope &rp, int n_rows, int lb, int worker, int workers) {
   constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, E = 16 / EB, RB = D * EB, LR = RB / 16, HPI = 64 / LR, U = 8;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane % LR, sub = lane / LR;
   const bool upper = l >= LR / 2;
-  const int lb = blockIdx.x / workers, worker = blockIdx.x - lb * workers, layer = lb / s.batch, b = lb - layer * s.batch;
+  const int layer = lb / s.batch, b = lb - layer * s.batch;
   const PRows d = tab.r[layer];
   const RowRange x0 = row_range(s, tab.c[layer], d, b * s.hkv, n_rows);
   bool same = true;
@@ -454,25 +454,25 @@ __global__ __launch_bounds__(kPagedThreads) void append_queries_kernel(PShape s,
 }
 
 // ------------------------------------------------------------------------------------------------
-// append_pages_kernel (many rows).  blockIdx.x: (layer, sequence, KV head); blockIdx.y: workers on the head's pages, a workgroup to a page: D/16 lanes
+// append_pages (many rows).  Workers on the pages of a (layer, sequence, KV head), a workgroup to a page: D/16 lanes
 // to a row, codes of values turned into the strips' words through LDS, bounds folded over the page's passes.
-// Bound: in 4 bits the quantiser's and the rotation's arithmetic.  us for four prompts of 5 to 32 thousand tokens, 4 KV heads of 128, 147 MB in: 118 (without
-// the units dealt to the dies in turn 158, and in at most 4096 workgroups 121).
+// Bound: in 4 bits the quantiser's and the rotation's arithmetic.  us for four prompts of 5 to 32 thousand tokens, 4 KV heads of 128, 147 MB in,
+// in a launch of their own: 118 (without the units dealt to the dies in turn 158, and in at most 4096 workgroups 121).
 // ------------------------------------------------------------------------------------------------
 template <int DT, int D, bool Q4>
-__global__ __launch_bounds__(kPagedThreads) void append_pages_kernel(PShape s, PTable tab, PRope rp, int n_rows) {
+__device__ __forceinline__ void append_pages(const PShape &s, const PTable &tab, const PRope &rp, int n_rows, int ul, int worker, int workers) {
   constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RS = kPagedThreads / LPR, RB = D * EB, RUNS = D / 8;
   __shared__ uint32_t words[Q4 ? RS * RUNS : 1];           // codes of the value rows of a pass, a word per eight elements
   __shared__ __align__(16) char red[4][2 * RB];
   const int tid = threadIdx.x, j = tid % LPR, slot = tid / LPR, lane = tid & 63, wave = tid >> 6;
-  const int ul = dealt_unit(), layer = ul / s.units_per_layer, u = ul - layer * s.units_per_layer;
+  const int layer = ul / s.units_per_layer, u = ul - layer * s.units_per_layer;
   const int h = u % s.hkv;
   const PCache c = tab.c[layer];
   const PRows d = tab.r[layer];
   const RowRange x = row_range(s, c, d, u, n_rows);
   const bool turn = rp.cos != nullptr;
 
-  for (int pg = (x.r0 >> s.lp) + (int)blockIdx.y; pg << s.lp < x.r1; pg += gridDim.y) {
+  for (int pg = (x.r0 >> s.lp) + worker; pg << s.lp < x.r1; pg += workers) {
     const int id = page_at(s, c, u, pg);
     if (id < 0) continue;                                  // uniform: the rows of no page are dropped
     const int first = pg << s.lp, lo_row = max(x.r0 - first, 0), hi_row = min(x.r1 - first, s.P);   // rows of the page to be written
@@ -567,6 +567,25 @@ __global__ __launch_bounds__(kPagedThreads) void append_pages_kernel(PShape s, P
   }
 }
 
+// append_many_kernel.  The pages' workgroups, then (QUERIES) the queries' in one launch.  us against two launches: 17 rows of 33 sequences (12 query
+// heads, read back) 15.3 and 19.6, a prompt of 4000 tokens 28.3 and 32.7, one of 32 768 into bf16 pages 118 and 121, four of 72 thousand together
+// 374 and 369; with the queries first 15.1, 31.9, 118, 380.
+template <int DT, int D, bool Q4, bool QUERIES>
+__global__ __launch_bounds__(kPagedThreads) void append_many_kernel(PShape s, PTable tab, PRope rp, int n_rows, int units, int page_workers, int query_workers) {
+  const int i = blockIdx.x, q = i - units * page_workers;
+  if (!QUERIES || q < 0) {
+    const int turn = i / units;
+    append_pages<DT, D, Q4>(s, tab, rp, n_rows, dealt_unit(i - turn * units, turn, units), turn, page_workers);
+  } else if constexpr (QUERIES) {
+    const int lb = q / query_workers;
+    append_queries<DT, D>(s, tab, rp, n_rows, lb, q - lb * query_workers, query_workers);
+  }
+}
+
+// The kernels of a page's format: for a few rows, for many of keys and values, and of queries beside them.
+template <int DT, int D, bool Q4, typename Go>
+static void append_kernels(Go &&go) { go(append_step_kernel<DT, D, Q4>, append_many_kernel<DT, D, Q4, false>, append_many_kernel<DT, D, Q4, true>); }
+
 // ------------------------------------------------------------------------------------------------
 // read_paged_kernel.  blockIdx.x: (layer, sequence, KV head); blockIdx.y: workers on the head's passes of RS rows.
 // Bound: memory, the dense rows' stores first: the same four prompts, 46 MB of 4-bit pages to 147 MB of rows, in 47 us
@@ -577,7 +596,7 @@ __global__ __launch_bounds__(D * 2) void read_paged_kernel(PShape s, PTable tab,
   constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RS = 32, RB = D * EB, STRIP = D + 8;   // (a strip's words, padded)
   __shared__ __align__(16) uint32_t words[Q4 ? 4 * STRIP : 4];
   const int tid = threadIdx.x, j = tid % LPR, slot = tid / LPR;
-  const int ul = dealt_unit(), layer = ul / s.units_per_layer, u = ul - layer * s.units_per_layer;
+  const int ul = dealt_unit(blockIdx.x, blockIdx.y, gridDim.x), layer = ul / s.units_per_layer, u = ul - layer * s.units_per_layer;
   const int h = u % s.hkv;
   const PCache c = tab.c[layer];
   const PRows d = tab.r[layer];
@@ -755,26 +774,20 @@ extern "C" mixkv_status mixkv_paged_append(const mixkv_paged_params *params, con
     const PTable t = table_of(caches + l0, rows + l0, nl, eb);
     const int64_t units = (int64_t)nl * s.units_per_layer;
     const bool queries = rows[0].Q != nullptr;
-    if (max_count <= step_rows(s.q4)) {
-      const int tasks = 2 + (queries ? s.G : 0), per = kPagedThreads / (s.D / 16);
-      const int groups = (int)units * tasks;
-      auto go = [&](auto kern) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)((groups + per - 1) / per)), dim3(kPagedThreads), 0, stream, s, t, rp, n_rows, tasks, groups);
-      };
-      if (s.q4) { if (s.D == 128) go(append_step_kernel<MIXKV_BF16, 128, true>); else go(append_step_kernel<MIXKV_BF16, 64, true>); }
-      else if (params->dtype == MIXKV_BF16) { if (s.D == 128) go(append_step_kernel<MIXKV_BF16, 128, false>); else go(append_step_kernel<MIXKV_BF16, 64, false>); }
-      else { if (s.D == 128) go(append_step_kernel<MIXKV_F32, 128, false>); else go(append_step_kernel<MIXKV_F32, 64, false>); }
-    } else {
+    auto go = [&](auto step, auto many, auto many_queries) {
+      if (max_count <= step_rows(s.q4)) {
+        const int tasks = 2 + (queries ? s.G : 0), per = kPagedThreads / (s.D / 16), groups = (int)units * tasks;
+        hipLaunchKernelGGL(step, dim3((unsigned)((groups + per - 1) / per)), dim3(kPagedThreads), 0, stream, s, t, rp, n_rows, tasks, groups);
+        return;
+      }
       const int pw = workers(((int64_t)max_count + s.P - 2) / s.P + 1, units), qw = workers(((int64_t)max_count + 3) / 4, (int64_t)nl * s.batch, 4096);
-      auto go = [&](auto kern, auto qkern) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)units, (unsigned)pw), dim3(kPagedThreads), 0, stream, s, t, rp, n_rows);
-        if (queries) hipLaunchKernelGGL(qkern, dim3((unsigned)(nl * s.batch * qw)), dim3(kPagedThreads), 0, stream, s, t, rp, n_rows, qw);
-      };
-      constexpr int B16 = MIXKV_BF16, F32 = MIXKV_F32;
-      if (s.q4) { if (s.D == 128) go(append_pages_kernel<B16, 128, true>, append_queries_kernel<B16, 128>); else go(append_pages_kernel<B16, 64, true>, append_queries_kernel<B16, 64>); }
-      else if (params->dtype == B16) { if (s.D == 128) go(append_pages_kernel<B16, 128, false>, append_queries_kernel<B16, 128>); else go(append_pages_kernel<B16, 64, false>, append_queries_kernel<B16, 64>); }
-      else { if (s.D == 128) go(append_pages_kernel<F32, 128, false>, append_queries_kernel<F32, 128>); else go(append_pages_kernel<F32, 64, false>, append_queries_kernel<F32, 64>); }
-    }
+      const dim3 grid((unsigned)(units * pw + (queries ? (int64_t)nl * s.batch * qw : 0)));
+      if (queries) hipLaunchKernelGGL(many_queries, grid, dim3(kPagedThreads), 0, stream, s, t, rp, n_rows, (int)units, pw, qw);
+      else hipLaunchKernelGGL(many, grid, dim3(kPagedThreads), 0, stream, s, t, rp, n_rows, (int)units, pw, qw);
+    };
+    if (s.q4) { if (s.D == 128) append_kernels<MIXKV_BF16, 128, true>(go); else append_kernels<MIXKV_BF16, 64, true>(go); }
+    else if (params->dtype == MIXKV_BF16) { if (s.D == 128) append_kernels<MIXKV_BF16, 128, false>(go); else append_kernels<MIXKV_BF16, 64, false>(go); }
+    else { if (s.D == 128) append_kernels<MIXKV_F32, 128, false>(go); else append_kernels<MIXKV_F32, 64, false>(go); }
     if (hipGetLastError() != hipSuccess) return MIXKV_ERR_HIP;
   }
   return MIXKV_OK;
