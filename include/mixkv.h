@@ -350,7 +350,7 @@ typedef struct {
   int32_t page_rows;         /* 32, 64 or 128 */
   int32_t max_pages;         /* entries of a head in the page table; max_pages * page_rows <= 2^30 */
   int32_t n_pages;           /* pages in a layer's K_pages and V_pages */
-  float softmax_scale;       /* finite, > 0 */
+  float softmax_scale;       /* > 0, at most 2^127 */
 } mixkv_paged_params;
 
 /* One layer's pages.  DEVICE pointers owned by the caller, K_pages, V_pages and K_bounds 16-byte aligned. */

@@ -654,7 +654,7 @@ mixkv_status make_pshape(const mixkv_paged_params *p, PShape *s) {
   if (p->format != MIXKV_PAGE_ROWS && p->format != MIXKV_PAGE_4BIT) return MIXKV_ERR_INVALID_ARG;
   if (p->batch < 1 || p->n_q_heads < 1 || p->n_kv_heads < 1 || p->n_q_heads % p->n_kv_heads != 0) return MIXKV_ERR_INVALID_ARG;
   if (p->max_pages < 1 || p->n_pages < 1) return MIXKV_ERR_INVALID_ARG;
-  if (!(p->softmax_scale > 0.f) || p->softmax_scale > 3e38f) return MIXKV_ERR_INVALID_ARG;
+  if (!(p->softmax_scale > 0.f) || p->softmax_scale > 0x1p127f) return MIXKV_ERR_INVALID_ARG;   // times log2(e) it has to be finite
   if (p->head_dim != 64 && p->head_dim != 128) return MIXKV_ERR_UNSUPPORTED;
   if (p->page_rows != 32 && p->page_rows != 64 && p->page_rows != 128) return MIXKV_ERR_UNSUPPORTED;
   if (p->format == MIXKV_PAGE_4BIT && p->dtype != MIXKV_BF16) return MIXKV_ERR_UNSUPPORTED;

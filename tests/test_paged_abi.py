@@ -178,3 +178,12 @@ def test_workspaces():
 def test_more_layers_and_heads_than_a_grid_are_refused():
     p = _params(batch=1, n_q_heads=1 << 18, n_kv_heads=1)            # 16384 groups of 16 query heads, in four layers
     assert _attend(p=p, n=4) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 127 * 1.01, 2.9e38])
+def test_scales_that_overflow_in_the_exponent_of_two_are_rejected(scale):
+    with pytest.raises(B.MixkvError) as e:
+        B.mixkv_page_bytes(_params(softmax_scale=scale))
+    assert e.value.status == INVALID
+    for fits in (2.0 ** 127, 1e-40):
+        assert B.mixkv_page_bytes(_params(softmax_scale=fits)) > 0
