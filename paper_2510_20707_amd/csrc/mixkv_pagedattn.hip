@@ -198,7 +198,9 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
     most = max(most, (uint32_t)__shfl_xor((int)most, 16));
     most = max(most, (uint32_t)__shfl_xor((int)most, 32));
     const int ex = min(max((int)(most >> 7), 1), 254) - 127, sh2 = l16 < ng ? 13 - ex : 0;   // 2^ex <= the largest < 2^(ex + 1); NaN and infinities stay what they are
-    const float back = ldexpf(s.scale_log2e * 1048576.f, -sh2);
+    // (Between 2^-126 and 2^100: a factor of zero or infinity would make NaNs of rows that do not exist or of scores of zero.  Below, the scores, under 2^18
+    // here, make no difference to a weight; above, any score but zero, at least 2^-72, is a logit of 2^28 or more.)
+    const float back = fminf(fmaxf(ldexpf(s.scale_log2e, 20 - sh2), 0x1p-126f), 0x1p100f);
 #pragma unroll
     for (int e = 0; e < 4; ++e) c2[e] = __shfl(back, 4 * quad + e);
     float hi[NG], lo[NG];

@@ -557,3 +557,24 @@ def test_a_prepared_call_belongs_to_its_device(monkeypatch):
         call.run()
     with pytest.raises(ValueError):
         B.PreparedPagedAttention(p, [c], [q], [torch.empty_like(q)])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("size,scale", [(0.0, 1e-12), (0.0, 1e-40), (2.0 ** 125, 1.0), (2.0 ** 100, 2.0 ** -100), (2.0 ** -118, 2.0 ** 120)])
+def test_4bit_scores_at_the_ends_of_the_exponents(D, size, scale):
+    """Queries and softmax scales far from one whose logits are ordinary: queries of zero, queries that meet nothing but zeros in the keys, a size
+    and a scale that make up for one another.  The heads end inside a tile, so rows that do not exist are among the scores."""
+    rng = np.random.default_rng([40, D])
+    P = 32
+    lay = T.Layer(rng, "4bit", "bf16", D, P, [[40, 1], [33, 70]], 3, fill=True)
+    Q = _queries(rng, lay, 6)
+    if size == 2.0 ** 125:                                               # all of the queries in the first 32 elements, where the keys have zeros
+        Q[..., 32:] = 0.0
+        for b, h in np.ndindex(2, 2):
+            for r in range(int(lay.lengths[b, h])):
+                page = lay.K[lay.table[b, h, r // P]]
+                row = O.as_dtype(rng.standard_normal(D), "bf16")
+                row[:32] = 0.0
+                O.write_row(page, "4bit", "bf16", True, P, r % P, row)
+    got = _attend_and_check(lay, Q * size, scale=scale)
+    assert np.isfinite(got).all()
