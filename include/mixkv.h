@@ -439,7 +439,7 @@ mixkv_status mixkv_paged_select(const mixkv_paged_params *params, const mixkv_pa
  * layer or none) those in the pages selected[b][h][0 .. n_selected[b][h]): places in the page table, in any order; one that is no place
  * in the table is passed over, a page that is listed twice counts twice.  A head without rows gets zeros.  fp32
  * accumulation, out in the dtype.  With 4-bit pages, values and weights enter the second product as fp16.
- * Logits are to stay below 2^25 in magnitude, beyond which fp32 has no differences of one left between them.
+ * Logits are to stay below 2^25 in magnitude, beyond which fp32 has no differences of one left between them, values below 2^100.
  * max_rows: the largest number of rows of a head (of selected pages, whole), as far as the host knows it (>= 1): with it the
  * rows are dealt to workgroups; longer heads are served, slower.  Outputs repeat bit for bit for the same arguments, max_rows included.
  * Workspace: mixkv_paged_attention_workspace_size bytes (0: NULL is accepted), 256-byte aligned, no initialisation.

@@ -389,9 +389,13 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
 //   bf16  weights as a bf16 head and remainder; values through the wave's LDS image, read transposed.
 //   fp32  products of four elements' contraction; a lane takes four neighbouring elements of a value row at a time, which are four blocks'
 //         operands, the blocks' rows then being every fourth element: no image.
-// Offsets as in decode_mfma_kernel.
+// Offsets as in decode_mfma_kernel, with a limit of their own.
 // Bound: memory, one tile of each wave in flight: bf16, 16 sequences of 8192 rows, 8 heads of 128, 537 MB in 94 us, 5.7 TB/s.
 // ------------------------------------------------------------------------------------------------
+// A lane's sum of weights that reaches this moves the head's offset.  The weighted values stay below it times the largest value: values of up to 2^100
+// do not overflow, whatever the logits behind them.
+constexpr float kRowsSumLimit = 0x1p20f;
+
 template <int DT, int D, bool ONCE>
 __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, AttnTable tab, float *part, float *part_ml, int64_t unit0) {
   constexpr bool F32 = DT == MIXKV_F32;
@@ -483,7 +487,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Att
 #pragma unroll
       for (int e = 0; e < 8; ++e) p[e] = fast_exp2(fmaf(x8[e], c2, -m));
       float next = sum + (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])));
-      if (__builtin_amdgcn_ballot_w64(!(next < kSumLimit)) != 0) {
+      if (__builtin_amdgcn_ballot_w64(!(next < kRowsSumLimit)) != 0) {
         float t = fmaxf(fmaxf(fmaxf(x8[0], x8[1]), fmaxf(x8[2], x8[3])), fmaxf(fmaxf(x8[4], x8[5]), fmaxf(x8[6], x8[7])));
         t = fmaxf(t, __shfl_xor(t, 16));
         t = fmaxf(t, __shfl_xor(t, 32));

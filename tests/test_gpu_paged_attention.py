@@ -578,3 +578,36 @@ def test_4bit_scores_at_the_ends_of_the_exponents(D, size, scale):
                 O.write_row(page, "4bit", "bf16", True, P, r % P, row)
     got = _attend_and_check(lay, Q * size, scale=scale)
     assert np.isfinite(got).all()
+
+
+def _terms(lay, Q):
+    """The largest sum of the magnitudes of a logit's terms (4-bit keys: S sum(q u) + B sum(q) with u in [1, 2), up to 8 max |k| times |q|)."""
+    G, most = Q.shape[1] // lay.lengths.shape[1], 0.0
+    for b, h in np.ndindex(*lay.lengths.shape):
+        q, k = np.abs(Q[b, h * G:(h + 1) * G]), np.abs(O.head(*lay.args(), lay.table, lay.lengths, b, h)[0])
+        k = k[np.isfinite(k).all(1)]
+        if len(k):
+            most = max(most, float(q.sum(1).max() * 8 * k.max() if lay.fmt == "4bit" else (q @ k.T).max()))
+    return most
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D,size", [(64, 1e20), (128, 1e30)])
+def test_large_values_behind_rising_logits(dtype, D, size):
+    """Logits that rise by 40 powers of two from one of a wave's tiles to its next, twice, and large values: a weight is at most a power of two above
+    the first tile's, times a value of 1e30 no infinity."""
+    rng = np.random.default_rng([41, D])
+    P, n = 32, 300
+    lay = T.Layer(rng, "rows", dtype, D, P, [[n, n - 13]], 10, fill=True)
+    Q = _queries(rng, lay, 4)
+    Q[..., 0] = 1.0
+    for h in range(2):
+        for r in range(int(lay.lengths[0, h])):
+            page = lay.table[0, h, r // P]
+            row = O.read_rows(lay.K[page], "rows", dtype, True, P, D)[r % P]
+            row[0] = 28.0 * (r // 128)                                   # tile t is wave t % 4's
+            O.write_row(lay.K[page], "rows", dtype, True, P, r % P, row)
+            O.write_row(lay.V[page], "rows", dtype, False, P, r % P, O.as_dtype(rng.standard_normal(D) * size, dtype))
+    got = _attend_and_check(lay, Q, logit_error=D * 2.0 ** -24 * _terms(lay, Q))
+    assert np.isfinite(got).all()
+    print(f"[case] large values {dtype} D={D}", flush=True)
