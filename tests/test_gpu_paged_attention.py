@@ -611,3 +611,126 @@ def test_large_values_behind_rising_logits(dtype, D, size):
     got = _attend_and_check(lay, Q, logit_error=D * 2.0 ** -24 * _terms(lay, Q))
     assert np.isfinite(got).all()
     print(f"[case] large values {dtype} D={D}", flush=True)
+
+
+def _chunks_are_several(lay, hq, max_rows):
+    rows = lay.table.shape[2] * lay.P if max_rows is None else max_rows
+    assert B.mixkv_paged_attention_workspace_size(lay.params(hq), 1, rows) > 0
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS)
+@pytest.mark.parametrize("D,P,G", [(128, 64, 7), (64, 32, 1), (128, 32, 19)])
+def test_heads_of_several_chunks(fmt, dtype, D, P, G):
+    """Lengths around the borders of chunks of 128 rows, and the last chunk longer than the others."""
+    print(f"[case] attention chunks {fmt} {dtype} D={D} P={P} G={G}", flush=True)
+    rng = np.random.default_rng([42, D, P, G])
+    lay = T.Layer(rng, fmt, dtype, D, P, [[127, 128, 129], [640, 513, 0], [255, 1, 400]], 640 // P, fill=True)
+    Q = _queries(rng, lay, 3 * G)
+    for most in (None, 385, 500):
+        _chunks_are_several(lay, 3 * G, most)
+        got = _attend_and_check(lay, Q, max_rows=most)
+        assert np.array_equal(got, _attend_and_check(lay, Q, max_rows=most)) and (got[1, 2 * G:] == 0).all()
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS)
+@pytest.mark.parametrize("gone", ["first", "last", "between", "all but one", "all"])
+def test_chunks_without_rows_or_weight(fmt, dtype, gone):
+    """Whole chunks whose pages do not exist, and in full precision whole chunks of keys of minus infinity: their partial results have no offset."""
+    D, P, n = 128, 32, 620
+    for masked in (False, True):
+        if masked and fmt == "4bit":
+            continue
+        rng = np.random.default_rng(43)
+        lay = T.Layer(rng, fmt, dtype, D, P, [[n, n]], 20, fill=True)
+        Q = _queries(rng, lay, 6)
+        Q[..., 7] = O.as_dtype(np.abs(Q[..., 7]) + 0.5, dtype)
+        chunk = np.arange(20) // 4
+        off = {"first": chunk < 2, "last": chunk >= 3, "between": (chunk == 1) | (chunk == 3), "all but one": chunk != 2, "all": chunk >= 0}[gone]
+        if not masked:
+            lay.table[0, 0, off] = -1
+        else:
+            for place in np.nonzero(off)[0]:
+                for r in range(P):
+                    row = O.read_rows(lay.K[lay.table[0, 0, place]], fmt, dtype, True, P, D)[r]
+                    row[7] = -np.inf
+                    O.write_row(lay.K[lay.table[0, 0, place]], fmt, dtype, True, P, r, row)
+        for most in (None, 400):
+            _chunks_are_several(lay, 6, most)
+            got = _attend_and_check(lay, Q, max_rows=most)
+            assert np.isfinite(got).all() and (gone != "all" or (got[0, :3] == 0).all())
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS)
+@pytest.mark.parametrize("spread,scale", [(60.0, 1.0), (2.0, 30.0), (500.0, 3.0)])
+def test_chunks_with_logits_far_apart(fmt, dtype, spread, scale):
+    rng = np.random.default_rng([44, int(spread)])
+    lay = T.Layer(rng, fmt, dtype, 128, 32, [[640, 390]], 20, fill=True)
+    Q = _queries(rng, lay, 6, spread)
+    _chunks_are_several(lay, 6, None)
+    _attend_and_check(lay, Q, scale=scale, logit_error=128 * 2.0 ** -24 * _terms(lay, Q) * scale)
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS)
+@pytest.mark.parametrize("D", [64, 128])
+def test_chunks_of_more_tiles_than_a_wave_has_lanes_for(fmt, dtype, D):
+    """A wave asks for the table entries of 64 tiles at a time: heads of 9001 and 17 000 rows as one chunk each, all their pages and listed ones."""
+    print(f"[case] attention long chunks {fmt} {dtype} D={D}", flush=True)
+    rng = np.random.default_rng([45, D])
+    P = 32
+    lay = T.Layer(rng, fmt, dtype, D, P, [[8 * P, 8 * P]], 600, spare=0, fill=True)
+    lay.table[:] = rng.integers(0, lay.n_pages, lay.table.shape)
+    lay.table[0, :, 300:303] = -1
+    lay.lengths[0] = 17000, 9001
+    Q = _queries(rng, lay, 6)
+    error = D * 2.0 ** -24 * _terms(lay, Q)
+    _attend_and_check(lay, Q, max_rows=1, logit_error=error)
+    _attend_and_check(lay, Q, max_rows=1, lists=[[rng.permutation(600).tolist(), rng.integers(0, 282, 600).tolist()]], logit_error=error)
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS)
+def test_more_chunks_than_a_workgroup_has_threads(fmt, dtype):
+    """264 chunks of 16 tiles: the threads that fold them take a second one each."""
+    print(f"[case] attention many chunks {fmt} {dtype}", flush=True)
+    rng = np.random.default_rng(46)
+    D, P, n = 64, 128, 135000
+    lay = T.Layer(rng, fmt, dtype, D, P, [[16 * P]], -(-n // P), spare=0, fill=True)
+    lay.table[:] = rng.integers(0, lay.n_pages, lay.table.shape)
+    lay.lengths[0] = n
+    Q = _queries(rng, lay, 3)
+    p = lay.params(3)
+    assert B.mixkv_paged_attention_workspace_size(p, 1, n) >= 257 * 3 * (D + 2) * 4
+    _attend_and_check(lay, Q, logit_error=D * 2.0 ** -24 * _terms(lay, Q))
+    lay.lengths[0] = 300                                                 # most of them without rows
+    _attend_and_check(lay, Q, logit_error=D * 2.0 ** -24 * _terms(lay, Q))
+
+
+@pytest.mark.parametrize("dtype,D,pages", [("bf16", 64, 600), ("bf16", 128, 600), ("f32", 64, 600), ("f32", 128, 600), ("f32", 128, 1200)])
+def test_selection_in_several_steps(dtype, D, pages):
+    """Many heads: a workgroup scores several steps of 32 to 128 pages, the last case more than the eight that it takes at most.  Heads end before, at
+    and behind the borders of steps and of workgroups, and entries that are no page lie in all of them."""
+    print(f"[case] select steps {dtype} D={D} pages={pages}", flush=True)
+    rng = np.random.default_rng([47, D, pages])
+    P, batch, hkv, G = 32, 64, 8, 2
+    step = 4 * 8 * (64 // (2 * D * (2 if dtype == "bf16" else 4) // 16))       # pages of a workgroup's step
+    assert -(-pages // step) * batch * hkv > 2048
+    n_pages = 150
+    ends = [0, 1, step - 1, step, step + 1, 2 * step, 2 * step + 1, 3 * step, 8 * step - 1, 8 * step, 8 * step + 1, 9 * step, pages - 1, pages]
+    n = rng.choice([min(x, pages) for x in ends], (batch, hkv))
+    lengths = np.maximum(n * P - rng.integers(0, P, (batch, hkv)), 0).astype(np.int32)
+    table = rng.integers(0, n_pages, (batch, hkv, pages)).astype(np.int32)
+    table[rng.random(table.shape) < 0.05] = -1
+    table[rng.random(table.shape) < 0.01] = n_pages
+    bounds = np.sort(O.as_dtype(rng.standard_normal((n_pages, 2, D)), dtype), axis=1)
+    Q = O.as_dtype(rng.standard_normal((batch, hkv * G, D)), dtype)
+    p = B.make_paged_params(dtype, "rows", batch, hkv * G, hkv, D, P, pages, n_pages)
+    cache = B.PagedCache(None, None, T.i32(table), T.i32(lengths), T.to_device(bounds, dtype))
+    q = Q.reshape(batch, hkv, G, D)
+    scores = (np.maximum(q, 0).sum(2) @ bounds[:, 1].T + np.minimum(q, 0).sum(2) @ bounds[:, 0].T).astype(np.float32)      # [batch, Hkv, pages of the pool]
+    scores = np.concatenate([scores, np.full((batch, hkv, 1), -np.inf, np.float32)], 2)
+    for keep, first, last in ((20, 1, 1), (500, 0, 3)):
+        (sel,), (got_n,) = B.mixkv_paged_select(p, [cache], [T.to_device(Q, dtype)], keep, first, last)
+        sel, got_n = sel.cpu().numpy(), got_n.cpu().numpy()
+        for b, h in np.ndindex(batch, hkv):
+            row = table[b, h, :-(-int(lengths[b, h]) // P)]
+            want = O.select(scores[b, h][np.where((row >= 0) & (row < n_pages), row, n_pages)], keep, first, last)
+            assert got_n[b, h] == len(want) and sel[b, h].tolist() == want + [-1] * (keep - len(want)), (b, h, len(row))
