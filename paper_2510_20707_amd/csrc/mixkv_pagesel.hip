@@ -255,6 +255,7 @@ extern "C" mixkv_status mixkv_paged_select(const mixkv_paged_params *params, con
   mixkv_status st = make_pshape(params, &s);
   if (st != MIXKV_OK) return st;
   if (max_selected < 1 || keep_first < 0 || keep_last < 0 || (int64_t)keep_first + keep_last > max_selected) return MIXKV_ERR_INVALID_ARG;
+  if ((int64_t)max_selected * s.P > (1 << 30)) return MIXKV_ERR_INVALID_ARG;             // as mixkv_paged_attention, which takes the list
   if ((st = check_caches(caches, n_layers, false, true)) != MIXKV_OK) return st;
   if (!layers) return MIXKV_ERR_INVALID_ARG;
   for (int l = 0; l < n_layers; ++l) {

@@ -187,3 +187,9 @@ def test_scales_that_overflow_in_the_exponent_of_two_are_rejected(scale):
     assert e.value.status == INVALID
     for fits in (2.0 ** 127, 1e-40):
         assert B.mixkv_page_bytes(_params(softmax_scale=fits)) > 0
+
+
+@pytest.mark.parametrize("keep", [(1 << 24) + 1, 2 ** 31 - 1])
+def test_selections_longer_than_any_table_are_rejected(keep):
+    """As attention refuses such lists (64-row pages here): a thread's walk over 2^31 - 1 places would pass what 32 bits hold."""
+    assert _select(keep=keep, first=0, last=0) == INVALID
