@@ -11,7 +11,7 @@ import ctypes as C
 import operator
 import os
 from array import array
-from dataclasses import dataclass
+from dataclasses import dataclass, is_dataclass
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -501,6 +501,12 @@ def _tensor(t: torch.Tensor, name: str, dtype, shape, device, contiguous=True) -
     return t
 
 
+def _held(*xs) -> list:
+    """The tensors of what a call was prepared over.  Themselves: the call has their addresses, and a program may give a field or a list's place a new one."""
+    return [t for x in xs if x is not None for t in
+            ([x] if isinstance(x, torch.Tensor) else _held(*vars(x).values()) if is_dataclass(x) else _held(*x) if hasattr(x, "__iter__") else ())]
+
+
 def _paged_device(caches: Sequence[PagedCache]) -> torch.device:
     _need(len(caches) > 0, "no layers")
     t = caches[0].lengths
@@ -555,8 +561,8 @@ def _paged_rows(p: MixkvPagedParams, rows: Sequence[PagedRows], queries: bool, d
 
 class PreparedPagedAppend:
     """The C arguments of one mixkv_paged_append call, built once over buffers that a serving loop keeps (a workspace that a prepared call allocates is
-    the current stream's: a run on another stream has to wait for that one, as for any tensor).  `max_count`: the largest
-    row_count as far as the host knows it (None: the dense tensor's rows)."""
+    the current stream's: a run on another stream has to wait for that one, as for any tensor).  The call is about the tensors that it was prepared over, and holds
+    them: after a field has got another one, prepare again.  `max_count`: the largest row_count as far as the host knows it (None: the dense tensor's rows)."""
 
     def __init__(self, p: MixkvPagedParams, caches: Sequence[PagedCache], rows: Sequence[PagedRows], rope: Optional[Rope] = None,
                  max_count: Optional[int] = None):
@@ -573,7 +579,7 @@ class PreparedPagedAppend:
             _need(axes != 3 or rope.sections is not None and len(rope.sections) == 3, "three axes need three sections")
             self.rope = MixkvRope(_ptr(rope.cos), _ptr(rope.sin), rope.cos.shape[0], _ptr(rope.positions), axes,
                                   (C.c_int32 * 3)(*(rope.sections if axes == 3 else (0, 0, 0))))
-        self._keep = (caches, rows, rope)
+        self._keep = _held(caches, rows, rope)
         self._args = (C.byref(self.p), self.caches, self.rows, self.n, None if self.rope is None else C.byref(self.rope), self.n_rows,
                       self.max_count)
         self._call = lib().mixkv_paged_append
@@ -597,7 +603,7 @@ class PreparedPagedRead:
         self.p, self.n, self.caches = p, len(caches), _paged_caches(p, caches, True, False, device)
         self.rows, self.n_rows = _paged_rows(p, rows, False, device)
         self.max_count = self.n_rows if max_count is None else max_count
-        self._keep = (caches, rows)
+        self._keep = _held(caches, rows)
         self._args = (C.byref(self.p), self.caches, self.rows, self.n, self.n_rows, self.max_count)
         self._call = lib().mixkv_paged_read
 
@@ -641,7 +647,7 @@ class PreparedPagedSelect:
         self.first, self.last = keep_first, keep_last
         workspace = _paged_workspace(workspace, mixkv_paged_select_workspace_size(p, n) if isinstance(workspace, str) else 0, device)
         self.wp, self.wb = _ws(workspace)
-        self._keep = (caches, Qs, selected, n_selected, workspace)
+        self._keep = _held(caches, Qs, selected, n_selected, workspace)
         self._args = (C.byref(self.p), self.caches, self.arr, self.n, self.most, self.first, self.last, self.wp, self.wb)
         self._call = lib().mixkv_paged_select
 
@@ -690,7 +696,7 @@ class PreparedPagedAttention:
         need = mixkv_paged_attention_workspace_size(p, n, self.rows) if isinstance(workspace, str) else 0
         workspace = _paged_workspace(workspace, need, device)
         self.wp, self.wb = _ws(workspace)
-        self._keep = (caches, Qs, outs, selected, n_selected, workspace)
+        self._keep = _held(caches, Qs, outs, selected, n_selected, workspace)
         self._args = (C.byref(self.p), self.caches, self.arr, self.n, self.most, self.rows, self.wp, self.wb)
         self._call = lib().mixkv_paged_attention
 
