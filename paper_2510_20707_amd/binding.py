@@ -507,6 +507,11 @@ def _held(*xs) -> list:
             ([x] if isinstance(x, torch.Tensor) else _held(*vars(x).values()) if is_dataclass(x) else _held(*x) if hasattr(x, "__iter__") else ())]
 
 
+def _own(p: MixkvPagedParams) -> MixkvPagedParams:
+    """A prepared call's own params: the sizes that its buffers were checked against."""
+    return MixkvPagedParams.from_buffer_copy(p)
+
+
 def _paged_device(caches: Sequence[PagedCache]) -> torch.device:
     _need(len(caches) > 0, "no layers")
     t = caches[0].lengths
@@ -568,7 +573,7 @@ class PreparedPagedAppend:
                  max_count: Optional[int] = None):
         self.device = device = _paged_device(caches)
         _need(len(caches) == len(rows), "a rows entry for every cache")
-        self.p, self.n, self.caches = p, len(caches), _paged_caches(p, caches, True, False, device)
+        self.p, self.n, self.caches = _own(p), len(caches), _paged_caches(p, caches, True, False, device)
         self.rows, self.n_rows = _paged_rows(p, rows, True, device)
         self.max_count, self.rope = self.n_rows if max_count is None else max_count, None
         if rope is not None:
@@ -600,7 +605,7 @@ class PreparedPagedRead:
     def __init__(self, p: MixkvPagedParams, caches: Sequence[PagedCache], rows: Sequence[PagedRows], max_count: Optional[int] = None):
         self.device = device = _paged_device(caches)
         _need(len(caches) == len(rows), "a rows entry for every cache")
-        self.p, self.n, self.caches = p, len(caches), _paged_caches(p, caches, True, False, device)
+        self.p, self.n, self.caches = _own(p), len(caches), _paged_caches(p, caches, True, False, device)
         self.rows, self.n_rows = _paged_rows(p, rows, False, device)
         self.max_count = self.n_rows if max_count is None else max_count
         self._keep = _held(caches, rows)
@@ -637,7 +642,7 @@ class PreparedPagedSelect:
         self.device = device = _paged_device(caches)
         n = len(caches)
         _need(n == len(Qs) == len(selected) == len(n_selected), "queries and selections for every cache")
-        self.p, self.n, self.caches, self.most = p, n, _paged_caches(p, caches, False, True, device), selected[0].shape[-1]
+        self.p, self.n, self.caches, self.most = _own(p), n, _paged_caches(p, caches, False, True, device), selected[0].shape[-1]
         self.arr = (MixkvPagedSelectLayer * n)()
         for i in range(n):
             _tensor(Qs[i], "Q", TORCH_DTYPE[p.dtype], (p.batch, p.n_q_heads, p.head_dim), device)
@@ -682,7 +687,7 @@ class PreparedPagedAttention:
         self.device = device = _paged_device(caches)
         n, sparse = len(caches), selected is not None
         _need(n == len(Qs) == len(outs) and (not sparse or n == len(selected) == len(n_selected)), "queries, outputs and selections for every cache")
-        self.p, self.n, self.caches = p, n, _paged_caches(p, caches, True, False, device)
+        self.p, self.n, self.caches = _own(p), n, _paged_caches(p, caches, True, False, device)
         self.most = selected[0].shape[-1] if sparse else 0
         self.rows = max_rows if max_rows is not None else (min(self.most, p.max_pages) if sparse else p.max_pages) * p.page_rows
         self.arr = (MixkvPagedAttentionLayer * n)()

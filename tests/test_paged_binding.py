@@ -53,3 +53,14 @@ def test_rebound_fields_leave_a_prepared_calls_tensors_alive(monkeypatch, kind):
     assert [name for name, r in refs.items() if r() is None] == []
     del call
     assert [name for name, r in refs.items() if r() is not None] == []
+
+
+@pytest.mark.parametrize("kind", list(CALLS))
+def test_changed_params_do_not_reach_a_prepared_call(monkeypatch, kind):
+    """The sizes that the buffers were checked against are those of every run."""
+    monkeypatch.setattr(B, "_paged_device", lambda caches: CPU)
+    parts = _parts()
+    call = CALLS[kind](*parts)
+    parts[0].batch, parts[0].n_pages, parts[0].max_pages = 7, 1000, 500
+    given = call._args[0]._obj
+    assert (given.batch, given.n_pages, given.max_pages) == (1, 5, 3)
