@@ -284,6 +284,12 @@ def _ws(workspace: Optional[torch.Tensor]):
     return C.c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size()
 
 
+def _held(*xs) -> list:
+    """The tensors of what a call was prepared over.  Themselves: the call has their addresses, and a program may give a field or a list's place a new one."""
+    return [t for x in xs if x is not None for t in
+            ([x] if isinstance(x, torch.Tensor) else _held(*vars(x).values()) if is_dataclass(x) else _held(*x) if hasattr(x, "__iter__") else ())]
+
+
 def mixkv_score(p: MixkvParams, Ks, Vs, Qs, outs: Sequence[LayerOut], workspace: torch.Tensor, stream=None,
                 r_given=None, window_lse=None):
     wp, wb = _ws(workspace)
@@ -332,7 +338,7 @@ class PreparedSimilarity:
             self.outs[i] = MixkvSimilarityOut(_ptr(None if redundancy is None else redundancy[i]),
                                               _ptr(None if block_maps is None else block_maps[i]))
         self.wp, self.wb = _ws(workspace)
-        self._keep = (Xs, redundancy, block_maps, workspace)
+        self._keep = _held(Xs, redundancy, block_maps, workspace)
         self._L = lib()
 
     def run(self, stream=None):
@@ -368,13 +374,13 @@ class PreparedDecode:
         self._ws_keep = workspace
         self.p, self.n, self.tail_len = p, n, tail_len
         self.tail_cap = 0 if tails is None else tails[0][0].shape[2]
-        self.arr = (MixkvDecodeLayer * n)()
+        self.arr, self._keep = (MixkvDecodeLayer * n)(), []
         for i, c in enumerate(caches):
             kt, vt = (None, None) if tails is None else tails[i]
             assert Qs[i].is_contiguous() and outs[i].is_contiguous() and (kt is None or kt.is_contiguous())
             self.arr[i] = MixkvDecodeLayer(_ptr(c.K_out), _ptr(c.V_out), _ptr(c.counts), _ptr(c.offsets), _ptr(kt), _ptr(vt),
                                            _ptr(Qs[i]), _ptr(outs[i]))
-        self._keep = (caches, tails, Qs, outs)
+            self._keep += (c.K_out, c.V_out, c.counts, c.offsets, kt, vt, Qs[i], outs[i])
         self._L = lib()
 
     def run(self, stream=None):
@@ -415,7 +421,7 @@ class PreparedCall:
         self.p, self.n = p, len(outs)
         self.ins, self.outs = _in_array(Ks, Vs, Qs, r_given, window_lse), _out_array(outs)
         self.wp, self.wb = _ws(workspace)
-        self._keep = (Ks, Vs, Qs, outs, workspace, r_given, window_lse)
+        self._keep = _held(Ks, Vs, Qs, outs, workspace, r_given, window_lse)
         self._L = lib()
 
     def compress(self, stream=None):
@@ -499,12 +505,6 @@ def _tensor(t: torch.Tensor, name: str, dtype, shape, device, contiguous=True) -
     _need(not contiguous or t.is_contiguous(), f"{name} has to be contiguous")
     _need(t.device == device, f"{name} is on {t.device}, expected {device}")
     return t
-
-
-def _held(*xs) -> list:
-    """The tensors of what a call was prepared over.  Themselves: the call has their addresses, and a program may give a field or a list's place a new one."""
-    return [t for x in xs if x is not None for t in
-            ([x] if isinstance(x, torch.Tensor) else _held(*vars(x).values()) if is_dataclass(x) else _held(*x) if hasattr(x, "__iter__") else ())]
 
 
 def _own(p: MixkvPagedParams) -> MixkvPagedParams:

@@ -64,3 +64,18 @@ def test_changed_params_do_not_reach_a_prepared_call(monkeypatch, kind):
     parts[0].batch, parts[0].n_pages, parts[0].max_pages = 7, 1000, 500
     given = call._args[0]._obj
     assert (given.batch, given.n_pages, given.max_pages) == (1, 5, 3)
+
+
+def test_the_other_prepared_calls_hold_their_tensors():
+    p = B.make_params("bf16", 1, 4, 2, 64, 40, 8, 10, budget_mode="adaptive")
+    t = lambda *shape: torch.zeros(shape, dtype=torch.bfloat16)  # noqa: E731
+    Ks, Vs, Qs, outs, ws = [t(1, 2, 40, 64)], [t(1, 2, 40, 64)], [t(1, 4, 8, 64)], [B.alloc_layer_out(p, CPU)], torch.zeros(1 << 10, dtype=torch.uint8)
+    red, q, out, tails = [torch.zeros(1, 2)], [t(1, 4, 64)], [t(1, 4, 64)], [(t(1, 2, 3, 64), t(1, 2, 3, 64))]
+    calls = [B.PreparedCall(p, Ks, Vs, Qs, outs, ws), B.PreparedDecode(p, outs, tails, q, out, 1), B.PreparedSimilarity(p, Ks, red, None, 8, ws)]
+    refs = [weakref.ref(x) for x in (Ks[0], Vs[0], Qs[0], outs[0].K_out, outs[0].counts, outs[0].offsets, tails[0][0], tails[0][1], q[0], out[0], red[0])]
+    for x in (Ks, Vs, Qs, red, q, out, tails):
+        x[0] = None
+    outs[0].K_out = outs[0].counts = outs[0].offsets = None
+    assert all(r() is not None for r in refs)
+    del calls
+    assert all(r() is None for r in refs)
