@@ -734,3 +734,20 @@ def test_selection_in_several_steps(dtype, D, pages):
             row = table[b, h, :-(-int(lengths[b, h]) // P)]
             want = O.select(scores[b, h][np.where((row >= 0) & (row < n_pages), row, n_pages)], keep, first, last)
             assert got_n[b, h] == len(want) and sel[b, h].tolist() == want + [-1] * (keep - len(want)), (b, h, len(row))
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS)
+@pytest.mark.parametrize("D,max_rows", [(64, None), (128, 400)])
+def test_logits_of_nearly_two_to_the_25(fmt, dtype, D, max_rows):
+    """The largest that the operator is for: fp32 leaves steps of 2 between such logits, so an output is a mean of a few values, and no more than that is
+    asked of it here: it is finite, and no larger than they are."""
+    rng = np.random.default_rng([48, D])
+    lay = T.Layer(rng, fmt, dtype, D, 32, [[620, 500]], 20, fill=True)
+    Q = _queries(rng, lay, 6)
+    most = max(float(np.abs(Q[0, 3 * h:3 * h + 3] @ O.head(*lay.args(), lay.table, lay.lengths, 0, h)[0].T).max()) for h in range(2))
+    for q, scale in ((Q, 0.97 * 2.0 ** 25 / most), (Q * 2.0 ** 25, 0.97 / most)):
+        got = T.values(B.mixkv_paged_attention(lay.params(6, scale), [lay.device()], [T.to_device(q, dtype)], max_rows=max_rows)[0])
+        for h in range(2):
+            v = np.abs(O.head(*lay.args(), lay.table, lay.lengths, 0, h)[1]).max()
+            x = got[0, 3 * h:3 * h + 3]
+            assert np.isfinite(x).all() and (np.abs(x) <= v * (1 + 2.0 ** -7)).all() and (np.abs(x).max(1) > 0).all()
