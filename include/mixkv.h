@@ -416,7 +416,9 @@ mixkv_status mixkv_paged_read(const mixkv_paged_params *params, const mixkv_page
  * Pages worth attending to: for the new token of every sequence and every KV head, the max_selected pages with the largest score
  *     s_p = fp32(sum_d (Q+_d hi_pd + Q-_d lo_pd)),  Q+_d = sum_g max(q_gd, 0),  Q-_d = sum_g min(q_gd, 0)  over the head's G queries,
  * in 64 bits, with lo and hi the page's K_bounds: the sum over the queries of the largest dot product that any key within
- * the bounds can have (a bound that meets a zero counts nothing, infinite ones too).  The first keep_first and the last keep_last pages are always among them (keep_first + keep_last <=
+ * the bounds can have (a bound that meets a zero counts nothing, infinite ones too).  The bounds are those of the rows as
+ * appended: elements of 4-bit pages, which attention takes, lie up to half a code and the fp16 rounding of their base outside them.  The first keep_first and
+ * the last keep_last pages are always among them (keep_first + keep_last <=
  * max_selected, and max_selected * page_rows <= 2^30 here and in mixkv_paged_attention); equal scores go to the earlier page, a place without a
  * page scores -infinity, and so does one whose score is NaN (queries hold none); a head with no more pages than max_selected keeps all.
  * Writes selected [batch, n_kv_heads, max_selected] (places in the head's page table, ascending, then -1) and n_selected

@@ -14,7 +14,8 @@ constexpr int kPagedThreads = 256;
 // (append_many_kernel: shared memory and barriers whatever the count).  us for 1, 2, 3, 4, 6, 8 rows of 8 heads of 128 with 32 query heads, bounds
 // kept, walked | by pages: bf16 rows, one sequence 3.7 5.0 6.4 7.3 10.0 12.7 | 6.1 6.3 6.3 6.5 6.6 6.6, 64 sequences 4.0 5.4 6.8 8.2 11.5 17.4 | 7.7 8.9
 // 9.1 9.2 9.4 9.8; 4-bit with the rows read back, one sequence 8.9 12.1 15.8 18.8 26.1 33.1 | 10.3 10.3 10.4 10.4 10.5 10.6, 64 sequences
-// 9.7 12.9 16.4 20.1 28.0 35.9 | 12.5 14.1 15.0 16.7 17.7 18.6.
+// 9.7 12.9 16.4 20.1 28.0 35.9 | 12.5 14.1 15.0 16.7 17.7 18.6.  The rule goes by the format alone, as one sequence has it: with 64 of them two rows in
+// 4 bits and four in full precision would be a tenth faster walked.
 static int step_rows(bool q4) { return q4 ? 1 : 3; }
 
 struct PRows {
@@ -290,8 +291,9 @@ struct Place4 {
 // ------------------------------------------------------------------------------------------------
 // append_step_kernel (few rows per head: a decoding step).  Every row of a (layer, sequence, KV head) that a call moves, key, value, or one of its
 // queries, is a task for D/16 lanes, which walk the head's new rows one after another: no barrier, and one writer for what rows share.
-// Bound: one chain of memory round trips (counts, table and positions, angles, the strip's old words): 3.5 us for one sequence's row into bf16
-// pages, 8 us for 64 sequences into 4-bit ones.
+// Bound: a chain of some eight memory round trips, for lanes of one wave may be of different layers: the layer's pointers, its lengths and counts, the table's entry, the row,
+// the positions axis by axis, the angles, then the strip's old words or the page's bounds.  3.5 us for one sequence's row into bf16 pages, 6.5 us
+// for 64 sequences into 4-bit ones.
 // ------------------------------------------------------------------------------------------------
 template <int DT, int D, bool Q4>
 __global__ __launch_bounds__(kPagedThreads) void append_step_kernel(PShape s, PTable tab, PRope rp, int n_rows, int tasks, int groups) {

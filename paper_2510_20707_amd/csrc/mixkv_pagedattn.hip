@@ -26,7 +26,8 @@ __device__ __forceinline__ int head_tiles(const PShape &s, const AShape &a, cons
   if (a.keep == 0) return (len + 31) >> 5;
   return min(max(l.nsel[u], 0), a.keep) << (s.lp - 5);
 }
-// The table entry of tile t (any number >= 0), and its place in the table.  No length is needed, so that the loads of both run side by side.
+// The table entry of tile t (any number >= 0), and its place in the table.  No length is needed.  (The optional list makes a branch, before which the compiler waits for
+// what was asked for earlier: in both kernels entry and length are asked for once the queries are there.)
 __device__ __forceinline__ int tile_entry(const PShape &s, const AShape &a, const PCache &c, const AttnLayer &l, int u, int t, int &place) {
   place = t >> (s.lp - 5);
   if (a.keep) place = l.sel[(int64_t)u * a.keep + min(place, a.keep - 1)];
@@ -89,13 +90,15 @@ __device__ __forceinline__ void finish_chunk(const PShape &s, const AShape &a, c
 //   * Scores: query heads on the output rows, keys on the columns of a 16 x 16 x 32 fp16 product for each group of 32 elements.  A word's codes,
 //     masked in place, are fp16 subnormals, code 2^-24 and, one nibble up, code 2^-20 (the queries of those elements are taken by 16 less): no
 //     conversion, exact products.  Queries are brought to [2^13, 2^14) by a power of two per head, which makes bf16 exact in fp16 down to
-//     2^-37 of the largest.  With acc_g = sum q code of group g and element = B + S + S code / 16, a score is
+//     2^-26 of the largest, smaller ones off by at most 2^-34 of it.  With acc_g = sum q code of group g and element = B + S + S code / 16, a score is
 //     sum_g S_g acc_g / 16 + sum_g (B_g + S_g) sum(q_g): four multiply-adds, and one product of the key's raw (S, B) pairs with the sums of
 //     the queries in two fp16 parts.
 //   * Weights as fp16 through the wave's LDS image (head, key): a lane holds two keys 16 rows apart, a word of the image.
 //   * Values: a word of a page holds eight rows' codes of one element, an operand of the second product: the code on top of the mantissa of
 //     1.0 is u = 1 + code / 16, and B + S u a packed fp16 multiply-add with the strip's scales.  Fp16 rounds weights and values by 2^-11, an
-//     eighth of the output's own rounding; both are averaged over the rows.  The weights are relative to an offset that puts the
+//     eighth of the output's own rounding; both are averaged over the rows: 1.681e-3 off from 64 bits (2-norms, 64 sequences of up to 16 384 rows), where the
+//     output's rounding alone is 1.664e-3.  That is what this costs to avoid: with the codes as exact operands and the products of weights and steps in two bf16
+//     parts, the bases by a product of their own, 1.664e-3 in 177 us instead of 138 (the vector unit then bounds it).  The weights are relative to an offset that puts the
 //     largest near 2^8: fp16 then resolves weights down to 2^-32 of it.
 // Bound: memory for long heads: 64 sequences of 8192 rows, 8 heads of 128, 671 MB in 114 us, 5.9 TB/s, and the merge behind it; for
 // few rows the workgroup's own beginning and end (4 heads of 260 rows: 7.8 us).
@@ -390,7 +393,8 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
 //   fp32  products of four elements' contraction; a lane takes four neighbouring elements of a value row at a time, which are four blocks'
 //         operands, the blocks' rows then being every fourth element: no image.
 // Offsets as in decode_mfma_kernel, with a limit of their own.
-// Bound: memory, one tile of each wave in flight: bf16, 16 sequences of 8192 rows, 8 heads of 128, 537 MB in 94 us, 5.7 TB/s.
+// Bound: memory, a tile of each wave in flight and not always whole: value loads are branches (rows that may not exist), so that a tile's values are waited for
+// before its last score product, and the next tile's keys alone are on their way during the weights.  bf16, 16 sequences of 8192 rows, 8 heads of 128, 537 MB in 94 us, 5.7 TB/s.
 // ------------------------------------------------------------------------------------------------
 // A lane's sum of weights that reaches this moves the head's offset.  The weighted values stay below it times the largest value: values of up to 2^100
 // do not overflow, whatever the logits behind them.
@@ -618,8 +622,8 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PShape s, AShape a, At
 
 // Tiles of a chunk and chunks of a head, from nothing but the arguments.  A workgroup costs some 4 us before and after its tiles (its chain of
 // loads, the queries, the fold of its waves), a tile some 1 us of a wave, the merge 4 us with the gap before it: as many workgroups as
-// there are compute units as soon as there are tiles for them, then longer chunks, up to two rounds of a few workgroups on every unit, then, in 4 bits, up
-// to 64 tiles (full-precision tiles take three times the bytes: 16).  us in chunks of 4, 8, 16, 32, 64, 128 tiles, 4-bit rows of 128: 4 heads of 2048
+// there are compute units as soon as there are tiles for them, then longer chunks, up to two workgroups for every unit (all of them at once: LDS and registers hold three in 4 bits, four at
+// 64 elements), then, in 4 bits, up to 64 tiles (full-precision tiles take three times the bytes: 16).  us in chunks of 4, 8, 16, 32, 64, 128 tiles, 4-bit rows of 128: 4 heads of 2048
 // rows 10 11 13 17 23 21; 4 of 32 768 22 16 15 18 25 39; 4 of 131 072 59 41 32 26 27 40; 64 of 4096 25 19 16 17 24 37; 64 of 64 pages of 64
 // 28 22 17 19 25 37; 512 of up to 16 384 336 223 172 149 138 140; bf16 rows, 128 heads of up to 8192 100 79 73 78 80 87, 4 of 8192 12 12 16 23 38
 // 69; fp32, 128 of up to 8192 97 86 88 85 85 138.  Heads of up to 12 tiles stay whole: 4 of 260 rows 8.4 against 9.5 in chunks of 4.

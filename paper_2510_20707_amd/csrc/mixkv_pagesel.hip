@@ -2,7 +2,8 @@
 //
 // With lo and hi a page's smallest and largest keys per element, max(q_d lo_d, q_d hi_d) = max(q_d, 0) hi_d + min(q_d, 0) lo_d, so the sum
 // over a group's queries is one product of 2 D elements with Q+ = sum max(q, 0) and Q- = sum min(q, 0): as cheap for 16 query heads as for
-// one.  It is formed in 64 bits, where the rounding to 32 bits that the pages are ranked by does not depend on the order of the sum.
+// one.  It is formed in 64 bits: the order of the sum decides the rounding to 32 bits, by which pages are ranked, only within some 2^-45 of a tie, and it is the
+// same order for every page, so that equal bounds have equal scores.
 #include <algorithm>
 
 #include "mixkv_paged.h"
@@ -40,7 +41,8 @@ __device__ __forceinline__ double scatter_sum(double (&v)[8], int lane) {
 // ------------------------------------------------------------------------------------------------
 // page_score_kernel: order keys of the pages' scores.  A page's bounds are 2 D neighbouring elements: L lanes take 16 bytes each and keep
 // their elements of (Q-, Q+) in registers; a wave has eight times 64 / L pages in flight.
-// Bound: memory in long launches, the chain table entry, bounds, sums in short ones (4 heads of 2048 pages: 9.3 us with the choice).
+// Bound: memory in long launches; in short ones the chain of table entry, bounds, the queries (fewer than eight to a KV head are loaded and waited for one
+// after another), sums (4 heads of 2048 pages: 9.3 us with the choice).
 // ------------------------------------------------------------------------------------------------
 template <int DT, int D>
 __global__ __launch_bounds__(kSelThreads) void page_score_kernel(PShape s, SelTable tab, uint32_t *keys, int64_t unit0, int stride, int steps) {
