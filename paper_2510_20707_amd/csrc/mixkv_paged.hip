@@ -373,8 +373,8 @@ __global__ __launch_bounds__(kPagedThreads) void append_step_kernel(PShape s, PT
 // every 64 / LR-th head (neighbouring lanes neighbouring bytes: an instruction takes a kilobyte of the row), its elements' partners are in the lane
 // LR / 2 away, and it keeps its angles for all heads, or, where the KV heads do not have the same rows, for those of
 // one KV head at a time.
-// Bound: memory; loads and stores pass the caches by (a prompt's queries are more than they keep).  us for four prompts of 72 thousand
-// tokens together, 28 heads of 128, 1.03 GB, where torch's copy of the same strided rows takes 199: 208, 5 TB/s; with workgroups that follow each other on
+// Bound: memory; loads and stores pass the caches by (a prompt's queries are more than they keep).  us for four prompts of 84 thousand
+// tokens together, 28 heads of 128, 1.20 GB, where torch's copy of the same strided rows takes 211: 208, 5.8 TB/s; with workgroups that follow each other on
 // different sequences 254, for DRAM then has four places to read from and to write to; in 1024, 2048, 8192 and 16 384 workgroups instead of 4096 218, 211,
 // 209, 228; with the next row's positions fetched ahead and a third of the instructions less 218.
 // ------------------------------------------------------------------------------------------------
@@ -458,7 +458,7 @@ __device__ __forceinline__ void append_queries(const PShape &s, const PTable &ta
 // ------------------------------------------------------------------------------------------------
 // append_pages (many rows).  Workers on the pages of a (layer, sequence, KV head), a workgroup to a page: D/16 lanes
 // to a row, codes of values turned into the strips' words through LDS, bounds folded over the page's passes.
-// Bound: in 4 bits the quantiser's and the rotation's arithmetic.  us for four prompts of 5 to 32 thousand tokens, 4 KV heads of 128, 147 MB in,
+// Bound: in 4 bits the quantiser's and the rotation's arithmetic.  us for four prompts of 5 to 32 thousand tokens, 4 KV heads of 128, 171 MB in,
 // in a launch of their own: 118 (without the units dealt to the dies in turn 158, and in at most 4096 workgroups 121).
 // ------------------------------------------------------------------------------------------------
 template <int DT, int D, bool Q4>
@@ -570,7 +570,7 @@ __device__ __forceinline__ void append_pages(const PShape &s, const PTable &tab,
 }
 
 // append_many_kernel.  The pages' workgroups, then (QUERIES) the queries' in one launch.  us against two launches: 17 rows of 33 sequences (12 query
-// heads, read back) 15.3 and 19.6, a prompt of 4000 tokens 28.3 and 32.7, one of 32 768 into bf16 pages 118 and 121, four of 72 thousand together
+// heads, read back) 15.3 and 19.6, a prompt of 4000 tokens 28.3 and 32.7, one of 32 768 into bf16 pages 118 and 121, four of 84 thousand together
 // 374 and 369; with the queries first 15.1, 31.9, 118, 380.
 template <int DT, int D, bool Q4, bool QUERIES>
 __global__ __launch_bounds__(kPagedThreads) void append_many_kernel(PShape s, PTable tab, PRope rp, int n_rows, int units, int page_workers, int query_workers) {
@@ -590,7 +590,7 @@ static void append_kernels(Go &&go) { go(append_step_kernel<DT, D, Q4>, append_m
 
 // ------------------------------------------------------------------------------------------------
 // read_paged_kernel.  blockIdx.x: (layer, sequence, KV head); blockIdx.y: workers on the head's passes of RS rows.
-// Bound: memory, the dense rows' stores first: the same four prompts, 46 MB of 4-bit pages to 147 MB of rows, in 47 us
+// Bound: memory, the dense rows' stores first: the same four prompts, 54 MB of 4-bit pages to 171 MB of rows, in 46 us
 // (without the units dealt to the dies in turn 55).
 // ------------------------------------------------------------------------------------------------
 template <int DT, int D, bool Q4>
