@@ -39,7 +39,7 @@
 extern "C" {
 #endif
 
-#define MIXKV_VERSION 11
+#define MIXKV_VERSION 12
 #define MIXKV_MAX_LAYERS 128      /* layers per call */
 #define MIXKV_MAX_WINDOW 64
 #define MIXKV_MAX_GROUP_ROWS 512  /* G * W */
@@ -456,6 +456,81 @@ mixkv_status mixkv_paged_attention_workspace_size(const mixkv_paged_params *para
 mixkv_status mixkv_paged_attention(const mixkv_paged_params *params, const mixkv_paged_cache *caches,
                                    const mixkv_paged_attention_layer *layers, int32_t n_layers, int32_t max_selected, int32_t max_rows,
                                    void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Queries of new rows: a prompt's, a few drafted tokens', a step's single ones, of ragged sequences one after another with unused rows
+ * behind them.  The rows of (b, h) are [row_start[b][h], row_start[b][h] + row_count[b][h]), for each the G query heads that KV head h
+ * serves; those outside [0, n_rows) are left out.  Their keys and values are in the cache already (mixkv_paged_append, which takes the same
+ * row_start and row_count, and whose Q_out is Q here): row t of a head's row_count[b][h] rows has the place p = lengths[b][h] - row_count[b][h] + t,
+ * and sees the places j <= p with
+ *     j > p - window   or   j < keep_first:
+ * the newest `window` rows, its own among them, and the first keep_first ones (sinks).  A window of max_pages * page_rows or more
+ * leaves nothing out.  A row whose p is below 0 sees nothing.  Places are counted in rows of the cache; heads of one sequence may have different lengths.
+ * What a place that a row does not see holds, infinities and NaN too, does not reach that row's results.
+ */
+typedef struct {
+  const void *Q;             /* head g of row r at element r * q_stride_n + g * q_stride_h; 16-byte aligned, rows and heads too */
+  int64_t q_stride_n, q_stride_h;
+  const int32_t *row_start, *row_count;  /* DEVICE [batch, n_kv_heads] */
+  void *out;                 /* mixkv_paged_window_attention only: [n_rows, n_q_heads, D] contiguous, 16-byte aligned, may not overlap Q */
+  float *lse;                /* [n_rows, n_q_heads]: written by mixkv_paged_window_attention (may be NULL there), read by mixkv_paged_weights */
+} mixkv_paged_queries;
+
+/*
+ * Attention of new rows over the rows that each of them sees (Sec. 3.1: the prefill in front of the compression, and decoding behind it):
+ * out = sum_j softmax_j(softmax_scale * q . k_j) v_j, and lse = log sum_j exp(softmax_scale * q . k_j), the natural logarithm (for the last
+ * W rows of a prompt what mixkv_layer_in.window_lse asks for, with causal_window and a window that leaves nothing out).  A row that sees nothing gets zeros
+ * and -infinity.  Rows of out and lse that belong to no (sequence, head) keep their contents.  fp32 accumulation, out in the dtype.  With
+ * many new rows of bf16 the weights enter the second product as bf16; with 4-bit pages values and weights enter it as fp16, and with many
+ * new rows the keys' elements enter the first one as fp16.  Logits and values as for mixkv_paged_attention.
+ * max_count: the largest row_count; a head's rows beyond max_count are not served (their outputs keep their contents).  max_rows: the largest length, as
+ * far as the host knows it (>= 1): longer heads are served, slower.  Outputs repeat bit for bit for the same arguments, max_count and max_rows
+ * included.  n_rows * n_q_heads <= 2^31 - 1.  Workspace: mixkv_paged_window_attention_workspace_size bytes (0: NULL is accepted), 256-byte
+ * aligned, no initialisation.
+ */
+mixkv_status mixkv_paged_window_attention_workspace_size(const mixkv_paged_params *params, int32_t n_layers, int32_t n_rows, int32_t window,
+                                                         int32_t keep_first, int32_t max_count, int32_t max_rows, size_t *bytes);
+mixkv_status mixkv_paged_window_attention(const mixkv_paged_params *params, const mixkv_paged_cache *caches, const mixkv_paged_queries *queries,
+                                          int32_t n_layers, int32_t n_rows, int32_t window, int32_t keep_first, int32_t max_count, int32_t max_rows,
+                                          void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * The attention that cached rows have been given, summed up: with the lse that mixkv_paged_window_attention left for the same queries, window and
+ * keep_first (or any other normaliser), row j of KV head h has its weight raised by
+ *     sum over the new rows that see j, and over the G query heads, of exp(softmax_scale * q . k_j - lse),
+ * in fp32; the weights of the new rows themselves begin at zero.  A place's weight lies beside its page: weights[page][row of the page].  Rows
+ * whose lse is -infinity give nothing.  Weights of rows that do not exist, and of old rows that no new row sees, keep their contents.  A head's
+ * rows beyond max_count are not served; max_rows as above.  V_pages are not used and may be NULL.  Sums repeat bit for bit for the same
+ * arguments.  Workspace: mixkv_paged_weights_workspace_size bytes (0: NULL is accepted), 256-byte aligned, no initialisation.
+ */
+mixkv_status mixkv_paged_weights_workspace_size(const mixkv_paged_params *params, int32_t n_layers, int32_t n_rows, int32_t window, int32_t keep_first,
+                                                int32_t max_count, int32_t max_rows, size_t *bytes);
+mixkv_status mixkv_paged_weights(const mixkv_paged_params *params, const mixkv_paged_cache *caches, const mixkv_paged_queries *queries, float *const *weights,
+                                 int32_t n_layers, int32_t n_rows, int32_t window, int32_t keep_first, int32_t max_count, int32_t max_rows, void *workspace,
+                                 size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Eviction by weight: head (b, h) keeps min(lengths[b][h], keep[b][h]) of its rows, those with the largest weight (equal ones: the earlier
+ * row; NaN counts as -infinity); the first keep_first and the last keep_last rows of a head count as infinite.  Rows whose page is none do not
+ * exist: they are not kept.  The kept rows move in order, bit for bit, into the pages of `into` (whose page table has the same shape, and
+ * whose pools may be the caches' own), with their weights; a place of `into` without a page is left out.  kept receives the places they
+ * come from, n_kept how many they are: the lengths of `into` from then on (into[l].lengths is not used).  K_bounds, if both have them, become the bounds of the rows that a page
+ * of `into` now holds (4-bit elements rounded to the dtype).  The pages that `into` lists may be none of those that the caches list; these are not
+ * written, and free afterwards.
+ * max_keep: the largest keep, and the width of kept; larger ones are taken as it.  max_rows: the largest length, as far as the host knows
+ * it (>= 1): longer heads are served, slower.  Workspace: mixkv_paged_evict_workspace_size bytes (0: NULL is accepted), 256-byte aligned, no initialisation.
+ */
+typedef struct {
+  const float *weights;      /* [n_pages, page_rows], of the caches' pages */
+  float *weights_into;       /* the same of the pages of `into` (may be the same array), or NULL */
+  const int32_t *keep;       /* [batch, n_kv_heads]; below 0: none */
+  int32_t *kept;             /* [batch, n_kv_heads, max_keep] places, ascending, then -1 */
+  int32_t *n_kept;           /* [batch, n_kv_heads] */
+} mixkv_paged_evict_layer;
+mixkv_status mixkv_paged_evict_workspace_size(const mixkv_paged_params *params, int32_t n_layers, int32_t max_rows, size_t *bytes);
+mixkv_status mixkv_paged_evict(const mixkv_paged_params *params, const mixkv_paged_cache *caches, const mixkv_paged_cache *into,
+                               const mixkv_paged_evict_layer *layers, int32_t n_layers, int32_t max_keep, int32_t keep_first, int32_t keep_last,
+                               int32_t max_rows, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 const char *mixkv_status_string(mixkv_status status);
 int32_t mixkv_version(void);

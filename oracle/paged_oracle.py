@@ -216,3 +216,111 @@ def attention(Q, k, v, scale):
     w = np.exp(x - top)
     total = w.sum(1, keepdims=True)
     return np.where(total > 0, (w @ v) / np.where(total > 0, total, 1.0), 0.0)
+
+
+# ---- queries of new rows within a window, the weights they give, eviction by them
+def sees(place, n, window, first):
+    """Which of the places 0 ... n - 1 a row at `place` sees."""
+    j = np.arange(n)
+    return (j <= place) & ((j > place - window) | (j < first))
+
+
+def rows_of(fmt, dtype, P, D, K_pages, V_pages, table, lengths, b, h):
+    """Keys and values of a head by place, and which of the places have a page."""
+    n = min(max(int(lengths[b, h]), 0), table.shape[2] * P)
+    k, v, there = np.zeros((n, D)), np.zeros((n, D)), np.zeros(n, bool)
+    for i in range(-(-n // P)):
+        page, live = _page(table, b, h, i, len(K_pages)), min(P, n - i * P)
+        if page >= 0:
+            at = slice(i * P, i * P + live)
+            k[at], v[at] = (read_rows(x[page], fmt, dtype, keys, P, D)[:live] for x, keys in ((K_pages, True), (V_pages, False)))
+            there[at] = True
+    return k, v, there
+
+
+def new_rows(lengths, row_start, row_count, b, h, n, n_rows, max_count):
+    """(row among the queries, place) of a head's new rows that are served."""
+    count, start = max(int(row_count[b, h]), 0), int(row_start[b, h])
+    return [(start + t, n - count + t) for t in range(min(count, max_count)) if 0 <= start + t < n_rows]
+
+
+def window_attention(args, table, lengths, Q, row_start, row_count, window, first, max_count, scale, out, lse):
+    """In place: out [n_rows, Hq, D], lse [n_rows, Hq] float64.  args: format, dtype, P, D and the pools."""
+    G = Q.shape[1] // lengths.shape[1]
+    for b, h in np.ndindex(*lengths.shape):
+        k, v, there = rows_of(*args, table, lengths, b, h)
+        for row, place in new_rows(lengths, row_start, row_count, b, h, len(k), len(Q), max_count):
+            at = sees(place, len(k), window, first) & there
+            heads = slice(h * G, (h + 1) * G)
+            x = scale * (Q[row, heads] @ k[at].T)
+            out[row, heads] = attention(Q[row, heads], k[at], v[at], scale)
+            top = x.max(1, initial=-np.inf)
+            safe = np.where(np.isneginf(top), 0.0, top)
+            with np.errstate(divide="ignore"):
+                lse[row, heads] = safe + np.log(np.exp(x - safe[:, None]).sum(1))
+
+
+def window_weights(args, table, lengths, Q, row_start, row_count, window, first, max_count, scale, lse, weights):
+    """In place: weights [n_pages, P] float64."""
+    P = args[2]
+    G = Q.shape[1] // lengths.shape[1]
+    for b, h in np.ndindex(*lengths.shape):
+        k, _, there = rows_of(*args, table, lengths, b, h)
+        got = np.zeros(len(k))
+        for row, place in new_rows(lengths, row_start, row_count, b, h, len(k), len(Q), max_count):
+            at = sees(place, len(k), window, first) & there
+            for g in range(h * G, (h + 1) * G):
+                if not np.isneginf(lse[row, g]):
+                    got[at] += np.exp(scale * (k[at] @ Q[row, g]) - lse[row, g])
+        for j in np.nonzero(there)[0]:
+            page = table[b, h, j // P]
+            weights[page, j % P] = (0.0 if j >= len(k) - max(int(row_count[b, h]), 0) else weights[page, j % P]) + got[j]
+
+
+def evicted(weights, there, keep, first, last):
+    """Places of one head that are kept, ascending; weights and there by place."""
+    n = len(weights)
+    x = np.where(np.isnan(weights), -np.inf, weights)
+    x[np.arange(n) < first] = np.inf
+    x[np.arange(n) >= n - last] = np.inf
+    best = sorted((j for j in range(n) if there[j]), key=lambda j: (-x[j], j))
+    return sorted(best[:max(keep, 0)])
+
+
+def evict(args, table, lengths, into, weights, weights_into, keep, max_keep, first, last, K_into, V_into, bounds_into):
+    """In place: the pools (uint8) and weights that the rows go to, bounds [n_pages, 2, D] or None.  Returns (kept, n_kept)."""
+    fmt, dtype, P, D, K, V = args
+    kept, n_kept = np.full(lengths.shape + (max_keep,), -1, np.int32), np.zeros(lengths.shape, np.int32)
+    for b, h in np.ndindex(*lengths.shape):
+        n = min(max(int(lengths[b, h]), 0), table.shape[2] * P)
+        there = np.array([_page(table, b, h, j // P, len(K)) >= 0 for j in range(n)], bool)
+        w = np.array([weights[table[b, h, j // P], j % P] if there[j] else 0.0 for j in range(n)])
+        at = evicted(w, there, min(int(keep[b, h]), max_keep), first, last)
+        kept[b, h, :len(at)], n_kept[b, h] = at, len(at)
+        for i, j in enumerate(at):
+            src, dst = table[b, h, j // P], _page(into, b, h, i // P, len(K_into))
+            if dst < 0:
+                continue
+            if weights_into is not None:
+                weights_into[dst, i % P] = w[j]
+            for pool, to, keys in ((K, K_into, True), (V, V_into, False)):
+                move_row(pool[src], j % P, to[dst], i % P, fmt, dtype, keys, P, D)
+            if bounds_into is not None:
+                row = as_dtype(read_rows(K[src], fmt, dtype, True, P, D)[j % P], dtype)
+                bounds_into[dst] = row if i % P == 0 else [np.minimum(bounds_into[dst, 0], row), np.maximum(bounds_into[dst, 1], row)]
+    return kept, n_kept
+
+
+def move_row(src, r, dst, i, fmt, dtype, keys, P, D):
+    """Row r of one page becomes row i of another, bit for bit."""
+    if fmt == "rows":
+        w = D * (2 if dtype == "bf16" else 4)
+        dst[i * w:(i + 1) * w] = src[r * w:(r + 1) * w]
+        return
+    a, z = _Places(keys, P, D)[r], _Places(keys, P, D)[i]
+    sw, dw = src[:P * D // 2].view(np.uint32), dst[:P * D // 2].view(np.uint32)
+    sh, dh = src[P * D // 2:].view(np.uint16), dst[P * D // 2:].view(np.uint16)
+    for d in range(D):
+        code = int(sw[a[d, 0]]) >> int(4 * a[d, 1]) & 15
+        dw[z[d, 0]] = int(dw[z[d, 0]]) & ~(15 << int(4 * z[d, 1])) & 0xFFFFFFFF | code << int(4 * z[d, 1])
+        dh[z[d, 2]], dh[z[d, 3]] = sh[a[d, 2]], sh[a[d, 3]]

@@ -98,6 +98,15 @@ class MixkvPagedAttentionLayer(C.Structure):
     _fields_ = [("Q", C.c_void_p), ("out", C.c_void_p), ("selected", C.c_void_p), ("n_selected", C.c_void_p)]
 
 
+class MixkvPagedQueries(C.Structure):
+    _fields_ = [("Q", C.c_void_p), ("q_stride_n", C.c_int64), ("q_stride_h", C.c_int64), ("row_start", C.c_void_p), ("row_count", C.c_void_p),
+                ("out", C.c_void_p), ("lse", C.c_void_p)]
+
+
+class MixkvPagedEvictLayer(C.Structure):
+    _fields_ = [("weights", C.c_void_p), ("weights_into", C.c_void_p), ("keep", C.c_void_p), ("kept", C.c_void_p), ("n_kept", C.c_void_p)]
+
+
 class MixkvError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -157,6 +166,18 @@ def lib() -> C.CDLL:
         L.mixkv_paged_attention.argtypes = [pg, pc, C.POINTER(MixkvPagedAttentionLayer), C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
                                             C.c_size_t, C.c_void_p]
         L.mixkv_paged_attention.restype = C.c_int
+        pq, pe, ints = C.POINTER(MixkvPagedQueries), C.POINTER(MixkvPagedEvictLayer), [C.c_int32] * 6
+        for name in ("mixkv_paged_window_attention_workspace_size", "mixkv_paged_weights_workspace_size"):
+            getattr(L, name).argtypes = [pg, *ints, C.POINTER(C.c_size_t)]
+            getattr(L, name).restype = C.c_int
+        L.mixkv_paged_window_attention.argtypes = [pg, pc, pq, *ints, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.mixkv_paged_window_attention.restype = C.c_int
+        L.mixkv_paged_weights.argtypes = [pg, pc, pq, C.POINTER(C.c_void_p), *ints, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.mixkv_paged_weights.restype = C.c_int
+        L.mixkv_paged_evict_workspace_size.argtypes = [pg, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
+        L.mixkv_paged_evict_workspace_size.restype = C.c_int
+        L.mixkv_paged_evict.argtypes = [pg, pc, pc, pe, *[C.c_int32] * 5, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.mixkv_paged_evict.restype = C.c_int
         L.mixkv_stage_name.argtypes = [C.c_int32]
         L.mixkv_stage_name.restype = C.c_char_p
         L.mixkv_status_string.argtypes = [C.c_int]
@@ -717,6 +738,170 @@ def mixkv_paged_attention(p: MixkvPagedParams, caches: Sequence[PagedCache], Qs,
         outs = [torch.empty_like(q) for q in Qs]
         PreparedPagedAttention(p, caches, Qs, outs, selected, n_selected, max_rows, workspace).run(stream)
     return outs
+
+
+@dataclass
+class PagedQueries:
+    """One layer's queries of new rows, as mixkv_paged_append rotated them, and what the attention makes of them."""
+    Q: torch.Tensor                              # [n_rows, Hq, D], stride 1 along D
+    row_start: torch.Tensor                      # [batch, Hkv] i32
+    row_count: torch.Tensor
+    out: Optional[torch.Tensor] = None           # [n_rows, Hq, D] contiguous (attention)
+    lse: Optional[torch.Tensor] = None           # [n_rows, Hq] f32 contiguous (attention: if wanted; weights: needed)
+
+
+EVERY_ROW = 1 << 30                              # a window that leaves nothing out
+
+
+def _paged_queries(p: MixkvPagedParams, queries: Sequence[PagedQueries], attention: bool, device):
+    arr, n_rows, dt = (MixkvPagedQueries * len(queries))(), queries[0].Q.shape[0], TORCH_DTYPE[p.dtype]
+    for i, q in enumerate(queries):
+        shape = (n_rows, p.n_q_heads, p.head_dim)
+        _tensor(q.Q, "Q", dt, shape, device, contiguous=False)
+        _need(q.Q.stride(2) == 1, "Q needs stride 1 along a row")
+        for name, t in (("row_start", q.row_start), ("row_count", q.row_count)):
+            _tensor(t, name, torch.int32, (p.batch, p.n_kv_heads), device)
+        _need(q.out is not None if attention else q.lse is not None, "out is needed" if attention else "lse is needed")
+        if attention:
+            _tensor(q.out, "out", dt, shape, device)
+        if q.lse is not None:
+            _tensor(q.lse, "lse", torch.float32, shape[:2], device)
+        arr[i] = MixkvPagedQueries(_ptr(q.Q), q.Q.stride(0), q.Q.stride(1), _ptr(q.row_start), _ptr(q.row_count), _ptr(q.out), _ptr(q.lse))
+    return arr, n_rows
+
+
+def mixkv_paged_window_attention_workspace_size(p: MixkvPagedParams, n_layers: int, n_rows: int, window: int, keep_first: int, max_count: int,
+                                                max_rows: int) -> int:
+    n = C.c_size_t(0)
+    _check(lib().mixkv_paged_window_attention_workspace_size(C.byref(p), n_layers, n_rows, window, keep_first, max_count, max_rows, C.byref(n)),
+           "mixkv_paged_window_attention_workspace_size")
+    return n.value
+
+
+def mixkv_paged_weights_workspace_size(p: MixkvPagedParams, n_layers: int, n_rows: int, window: int, keep_first: int, max_count: int, max_rows: int) -> int:
+    n = C.c_size_t(0)
+    _check(lib().mixkv_paged_weights_workspace_size(C.byref(p), n_layers, n_rows, window, keep_first, max_count, max_rows, C.byref(n)),
+           "mixkv_paged_weights_workspace_size")
+    return n.value
+
+
+class PreparedPagedWindowAttention:
+    """The C arguments of one mixkv_paged_window_attention call.  queries: per layer a PagedQueries with `out` (and `lse`, if wanted); max_count: the
+    largest row_count, a bound that is kept to (None: the queries' rows); max_rows: the largest length as far as the host knows it (None: what the page table can hold)."""
+
+    def __init__(self, p: MixkvPagedParams, caches: Sequence[PagedCache], queries: Sequence[PagedQueries], window: int = EVERY_ROW, keep_first: int = 0,
+                 max_count: Optional[int] = None, max_rows: Optional[int] = None, workspace="alloc"):
+        self.device = device = _paged_device(caches)
+        _need(len(caches) == len(queries), "queries for every cache")
+        self.p, self.n, self.caches = _own(p), len(caches), _paged_caches(p, caches, True, False, device)
+        self.queries, n_rows = _paged_queries(p, queries, True, device)
+        sizes = (n_rows, window, keep_first, n_rows if max_count is None else max_count, p.max_pages * p.page_rows if max_rows is None else max_rows)
+        workspace = _paged_workspace(workspace, mixkv_paged_window_attention_workspace_size(p, self.n, *sizes) if isinstance(workspace, str) else 0, device)
+        self.wp, self.wb = _ws(workspace)
+        self._keep = _held(caches, queries, workspace)
+        self._args = (C.byref(self.p), self.caches, self.queries, self.n, *sizes, self.wp, self.wb)
+        self._call = lib().mixkv_paged_window_attention
+
+    def run(self, stream=None):
+        _check(self._call(*self._args, _paged_stream(self.device, stream)), "mixkv_paged_window_attention")
+
+
+def mixkv_paged_window_attention(p: MixkvPagedParams, caches: Sequence[PagedCache], queries: Sequence[PagedQueries], window: int = EVERY_ROW, keep_first: int = 0,
+                                 max_count: Optional[int] = None, max_rows: Optional[int] = None, workspace="alloc", stream=None):
+    """Attention of the new rows into queries[i].out (and .lse)."""
+    with torch.cuda.stream(stream):                   # what is allocated here is the stream's (None: the current one's)
+        PreparedPagedWindowAttention(p, caches, queries, window, keep_first, max_count, max_rows, workspace).run(stream)
+
+
+def _weight_pool(p: MixkvPagedParams, t: torch.Tensor, name: str, device) -> torch.Tensor:
+    return _tensor(t, name, torch.float32, (p.n_pages, p.page_rows), device)
+
+
+class PreparedPagedWeights:
+    """The C arguments of one mixkv_paged_weights call.  queries: per layer a PagedQueries with the `lse` of the attention; weights: per layer
+    [n_pages, page_rows] f32, raised in place."""
+
+    def __init__(self, p: MixkvPagedParams, caches: Sequence[PagedCache], queries: Sequence[PagedQueries], weights: Sequence[torch.Tensor],
+                 window: int = EVERY_ROW, keep_first: int = 0, max_count: Optional[int] = None, max_rows: Optional[int] = None, workspace="alloc"):
+        self.device = device = _paged_device(caches)
+        _need(len(caches) == len(queries) == len(weights), "queries and weights for every cache")
+        self.p, self.n, self.caches = _own(p), len(caches), _paged_caches(p, caches, False, False, device)
+        _key_pages(p, caches, device)
+        self.queries, n_rows = _paged_queries(p, queries, False, device)
+        self.weights = (C.c_void_p * self.n)(*(_weight_pool(p, w, "weights", device).data_ptr() for w in weights))
+        sizes = (n_rows, window, keep_first, n_rows if max_count is None else max_count, p.max_pages * p.page_rows if max_rows is None else max_rows)
+        workspace = _paged_workspace(workspace, mixkv_paged_weights_workspace_size(p, self.n, *sizes) if isinstance(workspace, str) else 0, device)
+        self.wp, self.wb = _ws(workspace)
+        self._keep = _held(caches, queries, weights, workspace)
+        self._args = (C.byref(self.p), self.caches, self.queries, self.weights, self.n, *sizes, self.wp, self.wb)
+        self._call = lib().mixkv_paged_weights
+
+    def run(self, stream=None):
+        _check(self._call(*self._args, _paged_stream(self.device, stream)), "mixkv_paged_weights")
+
+
+def _key_pages(p: MixkvPagedParams, caches: Sequence[PagedCache], device):
+    pool = p.n_pages * mixkv_page_bytes(p)
+    for c in caches:
+        t = c.K_pages
+        _need(t is not None and t.is_contiguous() and t.device == device and t.numel() * t.element_size() == pool, f"K_pages has to be {pool} contiguous bytes on {device}")
+
+
+def mixkv_paged_weights(p: MixkvPagedParams, caches: Sequence[PagedCache], queries: Sequence[PagedQueries], weights: Sequence[torch.Tensor],
+                        window: int = EVERY_ROW, keep_first: int = 0, max_count: Optional[int] = None, max_rows: Optional[int] = None, workspace="alloc",
+                        stream=None):
+    """The weights that the new rows give to the cached ones, added to `weights` in place."""
+    with torch.cuda.stream(stream):                   # what is allocated here is the stream's (None: the current one's)
+        PreparedPagedWeights(p, caches, queries, weights, window, keep_first, max_count, max_rows, workspace).run(stream)
+
+
+def mixkv_paged_evict_workspace_size(p: MixkvPagedParams, n_layers: int, max_rows: int) -> int:
+    n = C.c_size_t(0)
+    _check(lib().mixkv_paged_evict_workspace_size(C.byref(p), n_layers, max_rows, C.byref(n)), "mixkv_paged_evict_workspace_size")
+    return n.value
+
+
+class PreparedPagedEvict:
+    """The C arguments of one mixkv_paged_evict call.  into: per layer the cache that the kept rows go to (pools of the same size, the caches' own or others; its
+    page_table lists free pages, its lengths are written); weights, weights_into: [n_pages, page_rows] f32 of the one's and the other's pages; keep: per layer
+    [batch, Hkv] i32; kept: [batch, Hkv, max_keep] i32 receives the places that the rows come from."""
+
+    def __init__(self, p: MixkvPagedParams, caches: Sequence[PagedCache], into: Sequence[PagedCache], weights: Sequence[torch.Tensor], keep, kept,
+                 keep_first: int = 0, keep_last: int = 0, weights_into: Optional[Sequence[torch.Tensor]] = None, max_rows: Optional[int] = None, workspace="alloc"):
+        self.device = device = _paged_device(caches)
+        n = len(caches)
+        _need(n == len(into) == len(weights) == len(keep) == len(kept) and (weights_into is None or n == len(weights_into)), "one of each for every cache")
+        self.p, self.n, self.caches, self.into = _own(p), n, _paged_caches(p, caches, True, False, device), _paged_caches(p, into, True, False, device)
+        most = kept[0].shape[-1]
+        self.arr = (MixkvPagedEvictLayer * n)()
+        for i in range(n):
+            _weight_pool(p, weights[i], "weights", device)
+            if weights_into is not None:
+                _weight_pool(p, weights_into[i], "weights_into", device)
+            _tensor(keep[i], "keep", torch.int32, (p.batch, p.n_kv_heads), device)
+            _tensor(kept[i], "kept", torch.int32, (p.batch, p.n_kv_heads, most), device)
+            self.arr[i] = MixkvPagedEvictLayer(_ptr(weights[i]), _ptr(None if weights_into is None else weights_into[i]), _ptr(keep[i]), _ptr(kept[i]),
+                                               _ptr(into[i].lengths))
+        rows = p.max_pages * p.page_rows if max_rows is None else max_rows
+        workspace = _paged_workspace(workspace, mixkv_paged_evict_workspace_size(p, n, rows) if isinstance(workspace, str) else 0, device)
+        self.wp, self.wb = _ws(workspace)
+        self._keep = _held(caches, into, weights, weights_into, keep, kept, workspace)
+        self._args = (C.byref(self.p), self.caches, self.into, self.arr, n, most, keep_first, keep_last, rows, self.wp, self.wb)
+        self._call = lib().mixkv_paged_evict
+
+    def run(self, stream=None):
+        _check(self._call(*self._args, _paged_stream(self.device, stream)), "mixkv_paged_evict")
+
+
+def mixkv_paged_evict(p: MixkvPagedParams, caches: Sequence[PagedCache], into: Sequence[PagedCache], weights: Sequence[torch.Tensor], keep, max_keep: int,
+                      keep_first: int = 0, keep_last: int = 0, weights_into: Optional[Sequence[torch.Tensor]] = None, max_rows: Optional[int] = None,
+                      workspace="alloc", stream=None):
+    """Moves what is kept into the pages of `into`; returns per layer the places [batch, Hkv, max_keep] that the rows come from, allocated on the call's stream."""
+    dev = _paged_device(caches)
+    with torch.cuda.stream(stream):                   # what is allocated here is the stream's (None: the current one's)
+        kept = [torch.empty((p.batch, p.n_kv_heads, max_keep), dtype=torch.int32, device=dev) for _ in caches]
+        PreparedPagedEvict(p, caches, into, weights, keep, kept, keep_first, keep_last, weights_into, max_rows, workspace).run(stream)
+    return kept
 
 
 def compacted_rows(p: MixkvParams, out: LayerOut) -> PagedRows:

@@ -29,6 +29,15 @@ __host__ __device__ constexpr int64_t page_bytes_of(bool q4, int dtype, int P, i
 mixkv_status make_pshape(const mixkv_paged_params *p, PShape *s);
 mixkv_status check_caches(const mixkv_paged_cache *c, int n_layers, bool pages, bool bounds);
 inline bool misaligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+// Dense rows with strides n (rows) and h (heads) in elements of eb bytes: whether the strides are none, the bytes from the first to the last.
+inline bool bad_row_strides(const PShape &s, int eb, int64_t n_rows, int64_t n, int64_t h) {
+  return n < s.D || h < 0 || n > INT64_MAX / 16 / (n_rows + 1) || h > (INT64_MAX >> 30) || (n * eb) % 16 || (h * eb) % 16;
+}
+inline uint64_t row_span(const PShape &s, int eb, int64_t n_rows, int64_t n, int64_t h, int heads) { return (uint64_t)((n_rows - 1) * n + (heads - 1) * h + s.D) * eb; }
+inline bool regions_overlap(const void *a, uint64_t na, const void *b, uint64_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
 
 // Rows of unit u (sequence, head) of a layer.
 __device__ __forceinline__ int head_rows(const PShape &s, const PCache &c, int u) {

@@ -1,4 +1,6 @@
-// Attention of one new token per sequence over the pages of its cache (mixkv_paged_attention).
+// Attention of one new token per sequence over the pages of its cache (mixkv_paged_attention), and of the new rows of every sequence,
+// each within its window and among the first rows (mixkv_paged_window_attention), where a unit has few of them (WIN: the kernels' row i of a unit
+// is query head i % G of new row i / G, and a tile's rows are seen by some of the rows only).
 //
 // A head's rows are dealt to workgroups in chunks of whole 32-row tiles.  The number of chunks of a launch comes from the host's bound on
 // the lengths, the chunks that a head has from its own length, so short heads of a ragged batch cost workgroups that end at once; the
@@ -6,7 +8,7 @@
 // unless its head has one chunk, and paged_merge_kernel folds the chunks in order.
 #include <algorithm>
 
-#include "mixkv_paged.h"
+#include "mixkv_pagedwin.h"
 
 namespace mixkv {
 
@@ -15,11 +17,16 @@ struct AttnTable { PCache c[kLayersPerLaunch]; AttnLayer l[kLayersPerLaunch]; };
 
 struct AShape {
   int32_t nchunks, ctiles;     // chunks of a head in the launch, tiles of a chunk
-  int32_t gchunks, gt;         // groups of up to kAttnHeads query heads, and the heads of a full one
+  int32_t gchunks, gt;         // groups of up to kAttnHeads rows (query heads, with WIN of all new rows), and the rows of a full one
   int32_t keep;                // entries of a head's list of selected pages, 0: all pages
+  int32_t gc0, gcn;            // WIN: groups of the launch
+  PWindow w;                   // WIN
 };
 
 constexpr int kAttnHeads = 16;
+
+template <bool WIN> using Table = std::conditional_t<WIN, WinTable, AttnTable>;
+template <bool WIN> using Layer = std::conditional_t<WIN, WinLayer, AttnLayer>;
 
 // Tiles of unit u, and where a tile lies: its first row in the pool as (page, row of the page), and how many of its rows exist.
 __device__ __forceinline__ int head_tiles(const PShape &s, const AShape &a, const AttnLayer &l, int u, int len) {
@@ -46,8 +53,16 @@ __device__ __forceinline__ Tile tile_of_entry(const PShape &s, int len, int t, i
 __device__ __forceinline__ int chunk_end(const AShape &a, int tiles, int ch) { return ch == a.nchunks - 1 ? tiles : min(tiles, (ch + 1) * a.ctiles); }
 __device__ __forceinline__ int chunks_used(const AShape &a, int tiles) { return min(a.nchunks, (int)(((uint32_t)tiles + a.ctiles - 1) / (uint32_t)a.ctiles)); }
 
-// A weighted sum over its sum of weights; no rows give zeros, a NaN stays one.
-__device__ __forceinline__ float row_result(float acc, float tot) { return tot == 0.f ? 0.f : acc / tot; }
+// A tile of a group with a window: where it lies, its first row's place in the head, and whether every row of the group sees all of it.
+__device__ __forceinline__ bool whole_tile(const PWindow &w, const View &v, int row0, int live) {
+  return live == 32 && row0 + 31 <= v.pa && (row0 > v.pb - w.window || row0 + 31 < w.first);
+}
+// The table's entry of a group's tile t (any number >= 0) and its number in the head.
+__device__ __forceinline__ int view_entry(const PShape &s, const PCache &c, const View &v, int u, int t, int &tile, int &place) {
+  tile = v.tile(t);
+  place = tile >> (s.lp - 5);
+  return c.table[(int64_t)u * s.max_pages + min(place, s.max_pages - 1)];
+}
 
 // The first partial row of a chunk.
 __device__ __forceinline__ int64_t slot_of(const PShape &s, const AShape &a, int64_t unit0, int layer, int u, int gc, int ch) {
@@ -56,9 +71,10 @@ __device__ __forceinline__ int64_t slot_of(const PShape &s, const AShape &a, int
 
 // The workgroup's end: folds the waves' shares in order (o_s of head g holds element d at d ^ g) and writes the rows, or the chunk's partial:
 // weighted values in `part`, offset and sum in `part_ml`.
-template <int DT, int D>
-__device__ __forceinline__ void finish_chunk(const PShape &s, const AShape &a, const AttnLayer &l, float (&o_s)[4][kAttnHeads][D], float (&m_s)[4][kAttnHeads],
-                                             float (&l_s)[4][kAttnHeads], float *part, float *part_ml, int64_t slot, int64_t q0, int ng, bool whole) {
+template <int DT, int D, bool WIN>
+__device__ __forceinline__ void finish_chunk(const PShape &s, const AShape &a, const Layer<WIN> &l, float (&o_s)[4][kAttnHeads][D], float (&m_s)[4][kAttnHeads],
+                                             float (&l_s)[4][kAttnHeads], float *part, float *part_ml, int64_t slot, int64_t q0, int ng, bool whole,
+                                             const View &v, int h) {
   __syncthreads();
   for (int idx = threadIdx.x; idx < ng * D; idx += 256) {
     const int g = idx / D, d = idx - g * D;
@@ -79,8 +95,14 @@ __device__ __forceinline__ void finish_chunk(const PShape &s, const AShape &a, c
       continue;
     }
     const float res = row_result(acc, tot);
-    if constexpr (DT == MIXKV_BF16) reinterpret_cast<uint16_t *>(l.out)[(q0 + g) * D + d] = f32_to_bf16_rne(res);
-    else reinterpret_cast<float *>(l.out)[(q0 + g) * D + d] = res;
+    int64_t row = q0 + g;
+    if constexpr (WIN) {
+      row = v.out_row(s, a.w, h, g);
+      if (row < 0) continue;
+      if (d == 0 && l.lse) l.lse[row] = row_lse(mu, tot);
+    }
+    if constexpr (DT == MIXKV_BF16) reinterpret_cast<uint16_t *>(l.out)[row * D + d] = f32_to_bf16_rne(res);
+    else reinterpret_cast<float *>(l.out)[row * D + d] = res;
   }
 }
 
@@ -123,8 +145,8 @@ __device__ __forceinline__ float row_sum(float x) {
   return x + row_turned<0x121>(x);
 }
 
-template <int D, bool ONCE>
-__global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShape a, AttnTable tab, float *part, float *part_ml, int64_t unit0) {
+template <int D, bool ONCE, bool WIN>
+__global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShape a, Table<WIN> tab, float *part, float *part_ml, int64_t unit0) {
   constexpr int NG = D / 32, NB = D / 16, H = kAttnHeads, W = 4;
   constexpr int CODES = 16 * D, SCALES = 32 * NG * 4, TILE = 2 * (CODES + SCALES);   // bytes of a tile: keys' codes, values', keys' scales, values'
   constexpr int NL = CODES / 1024, LOADS = 2 * NL + 1, RING = kQ4Ring;
@@ -135,20 +157,39 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
   __shared__ float m_s[W][H], l_s[W][H];
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int u = blockIdx.x, ch = blockIdx.y, layer = blockIdx.z / a.gchunks, gc = blockIdx.z - layer * a.gchunks;
-  const int b = u / s.hkv, h = u - b * s.hkv, ng = min(H, s.G - gc * H);
+  const int gcs = WIN ? a.gcn : a.gchunks;
+  const int u = blockIdx.x, ch = blockIdx.y, layer = blockIdx.z / gcs, gc = blockIdx.z - layer * gcs + (WIN ? a.gc0 : 0);
+  const int b = u / s.hkv, h = u - b * s.hkv;
   const PCache c = tab.c[layer];
-  const AttnLayer l = tab.l[layer];
+  const Layer<WIN> l = tab.l[layer];
+  View v;
+  if constexpr (WIN) {
+    v = view_of(s, a.w, c, l, u, gc * H, H);
+    if (v.ng <= 0) return;
+  }
+  const int ng = WIN ? v.ng : min(H, s.G - gc * H);
   const int64_t q0 = (int64_t)b * s.hq + h * s.G + gc * H;   // first query row
+  auto q_row = [&](int i) {
+    if constexpr (WIN) return v.query(s, a.w, l, h, i);
+    else return l.Q + (q0 + i) * D * 2;
+  };
   // group of the words at place g' of a key row, and the queries in that order: lane (head, quad) holds elements 8 quad + e of the group
   auto group_at = [](int pl) { return D == 128 ? (pl & 1) * 2 + (pl >> 1) : pl; };
   u32x4 qr[NG];
 #pragma unroll
   for (int pl = 0; pl < NG; ++pl)
-    qr[pl] = *reinterpret_cast<const u32x4 *>(l.Q + ((q0 + (l16 < ng ? l16 : 0)) * D + 32 * group_at(pl) + 8 * quad) * 2);
+    qr[pl] = *reinterpret_cast<const u32x4 *>(q_row(l16 < ng ? l16 : 0) + (32 * group_at(pl) + 8 * quad) * 2);
   const int t0 = ch * a.ctiles;
-  int place, entry = tile_entry(s, a, c, l, u, t0 + wave + lane * W, place);
-  const int len = head_rows(s, c, u), tiles = head_tiles(s, a, l, u, len), t1 = chunk_end(a, tiles, ch);
+  int place, tile = 0;
+  auto entry_of = [&](int t) {
+    if constexpr (WIN) return view_entry(s, c, v, u, t, tile, place);
+    else return tile_entry(s, a, c, l, u, t, place);
+  };
+  int entry = entry_of(t0 + wave + lane * W);
+  int len, tiles;
+  if constexpr (WIN) { len = v.len; tiles = v.tiles; }
+  else { len = head_rows(s, c, u); tiles = head_tiles(s, a, l, u, len); }
+  const int t1 = chunk_end(a, tiles, ch);
   if (t0 >= t1 && ch > 0) return;
   const int codes = s.P * D / 2;                             // bytes of codes in front of a page's scales
   const char *ring = reinterpret_cast<const char *>(sh.work.ring) + wave * (RING * TILE);
@@ -161,11 +202,17 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
   const uint32_t k_off = krow * (D / 2) + kpiece * 16;
   const bool s_keys = lane < SCALES / 16;
   const uint32_t s_off = codes + (s_keys ? lane : lane - SCALES / 16) * 16;
-  int x_page = 0, x_rows = 0, n = 0;                           // lane i: where the wave's i-th tile of a batch of 64 lies; tiles of the batch
+  int seen[4] = {};                                            // WIN: the last place that the rows 4 quad + e see
+  if constexpr (WIN) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) seen[e] = v.place(s, min(4 * quad + e, ng - 1));
+  }
+  int x_page = 0, x_rows = 0, x_row0 = 0, n = 0;               // lane i: where the wave's i-th tile of a batch of 64 lies; tiles of the batch
   auto batch = [&](int first) {                                // from the lanes' table entries
-    const Tile x = tile_of_entry(s, len, first + lane * W, place, entry);
+    const Tile x = tile_of_entry(s, len, WIN ? tile : first + lane * W, place, entry);
     x_page = x.page;
     x_rows = x.row | (x.live << 8);
+    if constexpr (WIN) x_row0 = tile * 32;
     n = min(max((t1 - first + W - 1) / W, 0), 64);
   };
   // tile i into its image
@@ -239,7 +286,7 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
 
   for (int first = t0 + wave; first < t1; first += 64 * W) {
     if (first != t0 + wave) {
-      entry = tile_entry(s, a, c, l, u, first + lane * W, place);
+      entry = entry_of(first + lane * W);
       begin(first);
     }
     int slot = 0;
@@ -305,7 +352,18 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
           for (int pl = 0; pl < NG; ++pl) x = fmaf((float)__builtin_bit_cast(f16x2, ks[r][pl])[0], acc[r][pl][e], x);
           x2[r][e] = x;
         }
-      if (live < 32) {
+      bool part_seen = live < 32;
+      if constexpr (WIN) {                                     // (rows that exist and are not seen: their weights of zero meet finite values)
+        const int row0 = __builtin_amdgcn_readlane(x_row0, i);
+        part_seen = !whole_tile(a.w, v, row0, live);
+        if (part_seen) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x2[r][e] = sees(a.w, seen[e], row0 + 16 * r + l16) ? x2[r][e] : -INFINITY;
+        }
+      }
+      if (part_seen) {
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
@@ -382,7 +440,7 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
 #pragma unroll
     for (int k = 0; k < NB; ++k) sh.share.o[wave][4 * quad + e][(16 * k + l16) ^ (4 * quad + e)] = o[k][e];
   }
-  finish_chunk<MIXKV_BF16, D>(s, a, l, sh.share.o, m_s, l_s, part, part_ml, slot_of(s, a, unit0, layer, u, gc, ch), q0, ng, chunks_used(a, tiles) <= 1);
+  finish_chunk<MIXKV_BF16, D, WIN>(s, a, l, sh.share.o, m_s, l_s, part, part_ml, slot_of(s, a, unit0, layer, u, gc, ch), q0, ng, chunks_used(a, tiles) <= 1, v, h);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -400,8 +458,8 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
 // do not overflow, whatever the logits behind them.
 constexpr float kRowsSumLimit = 0x1p20f;
 
-template <int DT, int D, bool ONCE>
-__global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, AttnTable tab, float *part, float *part_ml, int64_t unit0) {
+template <int DT, int D, bool ONCE, bool WIN>
+__global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Table<WIN> tab, float *part, float *part_ml, int64_t unit0) {
   constexpr bool F32 = DT == MIXKV_F32;
   constexpr int EB = F32 ? 4 : 2, RB = D * EB, PPR = RB / 16, NC = PPR / 4, NB = D / 16, H = kAttnHeads, W = 4;
   constexpr int NV = F32 ? 8 * (D / 64) : 32 * PPR / 64, RPL = 64 / PPR;     // 16-byte loads of a lane for a tile of values
@@ -409,17 +467,39 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Att
   __shared__ float m_s[W][H], l_s[W][H];
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int u = blockIdx.x, ch = blockIdx.y, layer = blockIdx.z / a.gchunks, gc = blockIdx.z - layer * a.gchunks;
-  const int b = u / s.hkv, h = u - b * s.hkv, ng = min(H, s.G - gc * H);
+  const int gcs = WIN ? a.gcn : a.gchunks;
+  const int u = blockIdx.x, ch = blockIdx.y, layer = blockIdx.z / gcs, gc = blockIdx.z - layer * gcs + (WIN ? a.gc0 : 0);
+  const int b = u / s.hkv, h = u - b * s.hkv;
   const PCache c = tab.c[layer];
-  const AttnLayer l = tab.l[layer];
+  const Layer<WIN> l = tab.l[layer];
+  View v;
+  if constexpr (WIN) {
+    v = view_of(s, a.w, c, l, u, gc * H, H);
+    if (v.ng <= 0) return;
+  }
+  const int ng = WIN ? v.ng : min(H, s.G - gc * H);
   const int64_t q0 = (int64_t)b * s.hq + h * s.G + gc * H;   // first query row
+  auto q_row = [&](int i) {
+    if constexpr (WIN) return v.query(s, a.w, l, h, i);
+    else return l.Q + (q0 + i) * RB;
+  };
   u32x4 qf[NC];
+  {
+    const char *q = q_row(l16 < ng ? l16 : 0);
 #pragma unroll
-  for (int k = 0; k < NC; ++k) qf[k] = *reinterpret_cast<const u32x4 *>(l.Q + (q0 + (l16 < ng ? l16 : 0)) * RB + (4 * k + quad) * 16);
+    for (int k = 0; k < NC; ++k) qf[k] = *reinterpret_cast<const u32x4 *>(q + (4 * k + quad) * 16);
+  }
   const int t0 = ch * a.ctiles;
-  int place, entry = tile_entry(s, a, c, l, u, t0 + wave + lane * W, place);   // lane i: where the wave's i-th tile of 64 lies
-  const int len = head_rows(s, c, u), tiles = head_tiles(s, a, l, u, len), t1 = chunk_end(a, tiles, ch);
+  int place, tile = 0;
+  auto entry_of = [&](int t) {
+    if constexpr (WIN) return view_entry(s, c, v, u, t, tile, place);
+    else return tile_entry(s, a, c, l, u, t, place);
+  };
+  int entry = entry_of(t0 + wave + lane * W);                  // lane i: where the wave's i-th tile of 64 lies
+  int len, tiles, seen = 0;                                    // WIN: the last place that row l16 sees
+  if constexpr (WIN) { len = v.len; tiles = v.tiles; seen = v.place(s, min(l16, ng - 1)); }
+  else { len = head_rows(s, c, u); tiles = head_tiles(s, a, l, u, len); }
+  const int t1 = chunk_end(a, tiles, ch);
   if (t0 >= t1 && ch > 0) return;
 #pragma unroll
   for (int k = 0; k < NC; ++k)
@@ -434,9 +514,9 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Att
   const uint32_t img_a = (uint32_t)(uintptr_t)(lds_void_t *)img;
 
   for (int first = t0 + wave; first < t1; first += 64 * W) {
-    if (first != t0 + wave) entry = tile_entry(s, a, c, l, u, first + lane * W, place);
-    const Tile x = tile_of_entry(s, len, first + lane * W, place, entry);
-    const int x_page = x.page, x_rows = x.row | (x.live << 8);
+    if (first != t0 + wave) entry = entry_of(first + lane * W);
+    const Tile x = tile_of_entry(s, len, WIN ? tile : first + lane * W, place, entry);
+    const int x_page = x.page, x_rows = x.row | (x.live << 8), x_row0 = tile * 32;
     const int n = min((t1 - first + W - 1) / W, 64);
     u32x4 kr[2][NC], vr[NV];
     auto tile_of = [&](const char *pool, int i) {
@@ -455,11 +535,34 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Att
     auto load_values = [&](int i) {
       const char *p = tile_of(c.V, i);
       const int live = __builtin_amdgcn_readlane(x_rows, i) >> 8;
+      bool all = live == 32;
+      int row0 = 0;
+      if constexpr (WIN) { row0 = __builtin_amdgcn_readlane(x_row0, i); all = whole_tile(a.w, v, row0, live); }
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         const char *at = p + value_row(j) * RB + (F32 ? (j >> 3) * 256 + l16 * 16 : (lane % PPR) * 16);
-        if (live == 32) vr[j] = load_vec<ONCE>(at);
-        else vr[j] = value_row(j) < live ? load_vec<ONCE>(at) : u32x4{0u, 0u, 0u, 0u};   // rows that do not exist: zeros
+        bool there = value_row(j) < live;
+        if constexpr (WIN) there = there && v.any_sees(a.w, row0 + value_row(j));
+        if (all) vr[j] = load_vec<ONCE>(at);
+        else vr[j] = there ? load_vec<ONCE>(at) : u32x4{0u, 0u, 0u, 0u};   // rows that do not exist, or that no row of the group sees: zeros
+      }
+    };
+    // (WIN) Values that are no numbers and went into the product as zeros, added where their rows are seen: a weight of zero does not make NaN of them.
+    auto add_odd = [&](int i) {
+      const char *p = tile_of(c.V, i);
+      const int live = __builtin_amdgcn_readlane(x_rows, i) >> 8, row0 = __builtin_amdgcn_readlane(x_row0, i);
+#pragma unroll 1
+      for (int r = 0; r < live; ++r) {
+        if (!sees(a.w, seen, row0 + r)) continue;
+#pragma unroll
+        for (int k = 0; k < NB; ++k)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float x;
+            if constexpr (F32) x = reinterpret_cast<const float *>(p + r * RB)[64 * (k >> 2) + 4 * (4 * quad + e) + (k & 3)];
+            else x = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(p + r * RB)[16 * k + 4 * quad + e] << 16);
+            if (no_number<MIXKV_F32>(__float_as_uint(x))) o[k][e] += x;
+          }
       }
     };
     load_keys(0);
@@ -488,6 +591,28 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Att
         const float v = e < 4 ? acc[0][e & 3] : acc[1][e & 3];
         x8[e] = 16 * (e >> 2) + 4 * quad + (e & 3) < live ? v : -INFINITY;
       }
+      bool mixed = false;                                      // values that are no numbers, in rows that only some of the group's rows see
+      if constexpr (WIN) {
+        const int row0 = __builtin_amdgcn_readlane(x_row0, i);
+        if (!whole_tile(a.w, v, row0, live)) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x8[e] = sees(a.w, seen, row0 + 16 * (e >> 2) + 4 * quad + (e & 3)) ? x8[e] : -INFINITY;
+          if (v.pa != v.pb) {
+            bool odd = false;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+              for (int w = 0; w < 4; ++w) odd |= no_number<DT>(vr[j][w]);
+            mixed = __builtin_amdgcn_ballot_w64(odd) != 0;
+            if (mixed) {
+#pragma unroll
+              for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) vr[j][w] = numbers_only<DT>(vr[j][w]);
+            }
+          }
+        }
+      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) p[e] = fast_exp2(fmaf(x8[e], c2, -m));
       float next = sum + (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])));
@@ -512,6 +637,9 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Att
           for (int e = 0; e < 8; ++e)                          // block k: elements 64 (k / 4) + 4 i + k % 4
             o[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[(k >> 2) * 8 + e][k & 3]), p[e], o[k], 0, 0, 0);
         if (i + 1 < n) load_values(i + 1);
+        if constexpr (WIN) {
+          if (mixed) add_odd(i);
+        }
       } else {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -541,6 +669,9 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Att
           o[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, pl, o[k], 0, 0, 0);
         }
         wave_lds_fence();
+        if constexpr (WIN) {
+          if (mixed) add_odd(i);
+        }
       }
     }
   }
@@ -554,22 +685,25 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Att
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       o_s[wave][l16][(F32 ? 64 * (k >> 2) + 4 * (4 * quad + e) + (k & 3) : 16 * k + 4 * quad + e) ^ l16] = o[k][e];
-  finish_chunk<DT, D>(s, a, l, o_s, m_s, l_s, part, part_ml, slot_of(s, a, unit0, layer, u, gc, ch), q0, ng, chunks_used(a, tiles) <= 1);
+  finish_chunk<DT, D, WIN>(s, a, l, o_s, m_s, l_s, part, part_ml, slot_of(s, a, unit0, layer, u, gc, ch), q0, ng, chunks_used(a, tiles) <= 1, v, h);
 }
 
 // Folds the chunks of one query head: slices of D/4 threads take every S-th chunk, 16 bytes of its row a thread, and are summed in order.
-template <int DT, int D>
-__global__ __launch_bounds__(256) void paged_merge_kernel(PShape s, AShape a, AttnTable tab, const float *part, const float *part_ml, int64_t unit0) {
+template <int DT, int D, bool WIN>
+__global__ __launch_bounds__(256) void paged_merge_kernel(PShape s, AShape a, Table<WIN> tab, const float *part, const float *part_ml, int64_t unit0) {
   constexpr int T = D / 4, S = 256 / T;
   __shared__ float red[4];
   __shared__ f32x4 acc_s[S][T];
   __shared__ float tot_s[S];
   const int tid = threadIdx.x, t = tid % T, slice = tid / T;
-  const int u = blockIdx.x, g = blockIdx.y, layer = blockIdx.z / a.gchunks, gc = blockIdx.z - layer * a.gchunks;
+  const int gcs = WIN ? a.gcn : a.gchunks;
+  const int u = blockIdx.x, g = blockIdx.y, layer = blockIdx.z / gcs, gc = blockIdx.z - layer * gcs + (WIN ? a.gc0 : 0);
   const int b = u / s.hkv, h = u - b * s.hkv;
-  if (g >= min(kAttnHeads, s.G - gc * kAttnHeads)) return;
   const PCache c = tab.c[layer];
-  const AttnLayer l = tab.l[layer];
+  const Layer<WIN> l = tab.l[layer];
+  View v;
+  if constexpr (WIN) v = view_of(s, a.w, c, l, u, gc * kAttnHeads, kAttnHeads);
+  if (g >= (WIN ? v.ng : min(kAttnHeads, s.G - gc * kAttnHeads))) return;
   const int64_t slot = slot_of(s, a, unit0, layer, u, gc, 0) + g;
   const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + slot;
   const float *rows = part + slot * D + 4 * t;
@@ -578,7 +712,9 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PShape s, AShape a, At
   const float m0 = ml[(int64_t)min(tid, a.nchunks - 1) * a.gt].x;
   const float2 x0 = ml[i0];
   const f32x4 r0 = *reinterpret_cast<const f32x4 *>(rows + i0 * D);
-  const int used = chunks_used(a, head_tiles(s, a, l, u, head_rows(s, c, u)));
+  int used;
+  if constexpr (WIN) used = chunks_used(a, v.tiles);
+  else used = chunks_used(a, head_tiles(s, a, l, u, head_rows(s, c, u)));
   if (used <= 1) return;
   float m = tid < used ? m0 : -INFINITY;
   for (int i = tid + 256; i < used; i += 256) m = fmaxf(m, ml[(int64_t)i * a.gt].x);
@@ -607,7 +743,13 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PShape s, AShape a, At
   if (tid >= T) return;
 #pragma unroll
   for (int i = 1; i < S; ++i) { acc += acc_s[i][t]; tot += tot_s[i]; }
-  const int64_t at = ((int64_t)b * s.hq + h * s.G + gc * kAttnHeads + g) * D + 4 * t;
+  int64_t row = (int64_t)b * s.hq + h * s.G + gc * kAttnHeads + g;
+  if constexpr (WIN) {
+    row = v.out_row(s, a.w, h, g);
+    if (row < 0) return;
+    if (t == 0 && l.lse) l.lse[row] = row_lse(mu, tot);
+  }
+  const int64_t at = row * D + 4 * t;
 #pragma unroll
   for (int e = 0; e < 4; ++e) acc[e] = row_result(acc[e], tot);
   if constexpr (DT == MIXKV_BF16) {
@@ -646,12 +788,19 @@ static size_t attn_bytes(const PShape &s, const AShape &a, int n_layers) { retur
 // ONCE: the rows pass the caches by.  With more query heads to a KV head than a workgroup takes, several workgroups read the same rows, and they go
 // through the caches.  us by the caches and through them, rows of 128: 4-bit, 64 sequences of 8192, 4 query heads to a KV head 125 and 138, 48 heads
 // to one KV head 60 and 51; bf16, 16 of 8192, 4 to a head 94 and 107, 32 to a head 56 and 54; fp32, 32 to a head 103 and 98.
-template <bool ONCE, typename Go>
+template <bool ONCE, bool WIN, typename Go>
 static void launch_attention(const PShape &s, int dtype, Go &&go) {
   constexpr int B16 = MIXKV_BF16, F32 = MIXKV_F32;
-  if (s.q4) { if (s.D == 128) go(paged_q4_kernel<128, ONCE>, paged_merge_kernel<B16, 128>); else go(paged_q4_kernel<64, ONCE>, paged_merge_kernel<B16, 64>); }
-  else if (dtype == B16) { if (s.D == 128) go(paged_rows_kernel<B16, 128, ONCE>, paged_merge_kernel<B16, 128>); else go(paged_rows_kernel<B16, 64, ONCE>, paged_merge_kernel<B16, 64>); }
-  else { if (s.D == 128) go(paged_rows_kernel<F32, 128, ONCE>, paged_merge_kernel<F32, 128>); else go(paged_rows_kernel<F32, 64, ONCE>, paged_merge_kernel<F32, 64>); }
+  if (s.q4) {
+    if (s.D == 128) go(paged_q4_kernel<128, ONCE, WIN>, paged_merge_kernel<B16, 128, WIN>);
+    else go(paged_q4_kernel<64, ONCE, WIN>, paged_merge_kernel<B16, 64, WIN>);
+  } else if (dtype == B16) {
+    if (s.D == 128) go(paged_rows_kernel<B16, 128, ONCE, WIN>, paged_merge_kernel<B16, 128, WIN>);
+    else go(paged_rows_kernel<B16, 64, ONCE, WIN>, paged_merge_kernel<B16, 64, WIN>);
+  } else {
+    if (s.D == 128) go(paged_rows_kernel<F32, 128, ONCE, WIN>, paged_merge_kernel<F32, 128, WIN>);
+    else go(paged_rows_kernel<F32, 64, ONCE, WIN>, paged_merge_kernel<F32, 64, WIN>);
+  }
 }
 
 static int clamp_rows(const PShape &s, int max_rows) { return std::min(max_rows, s.max_pages * s.P); }
@@ -718,9 +867,127 @@ extern "C" mixkv_status mixkv_paged_attention(const mixkv_paged_params *params, 
       if (a.nchunks > 1)
         hipLaunchKernelGGL(merge, dim3((unsigned)s.units_per_layer, (unsigned)a.gt, z), dim3(256), 0, stream, s, a, t, (const float *)part, (const float *)part_ml, unit0);
     };
-    if (a.gchunks == 1) launch_attention<true>(s, params->dtype, go);
-    else launch_attention<false>(s, params->dtype, go);
+    if (a.gchunks == 1) launch_attention<true, false>(s, params->dtype, go);
+    else launch_attention<false, false>(s, params->dtype, go);
     if (hipGetLastError() != hipSuccess) return MIXKV_ERR_HIP;
+  }
+  return MIXKV_OK;
+}
+
+// ------------------------------------------------------------------------------------------------
+// mixkv_paged_window_attention
+// ------------------------------------------------------------------------------------------------
+namespace mixkv {
+
+mixkv_status make_window(const PShape &s, int n_rows, int window, int first, int max_count, int max_rows, PWindow *w) {
+  if (n_rows < 1 || window < 1 || first < 0 || max_count < 1 || max_rows < 1) return MIXKV_ERR_INVALID_ARG;
+  if ((int64_t)n_rows * s.hq > INT32_MAX) return MIXKV_ERR_UNSUPPORTED;
+  const int every = 1 << 30;             // no head has more rows
+  *w = PWindow{std::min(window, every), std::min(first, every), std::min(max_count, n_rows), n_rows};
+  return MIXKV_OK;
+}
+
+mixkv_status check_queries(const PShape &s, int eb, const mixkv_paged_queries *q, int n_layers, int64_t n_rows, bool outputs) {
+  if (!q) return MIXKV_ERR_INVALID_ARG;
+  for (int l = 0; l < n_layers; ++l) {
+    const mixkv_paged_queries &d = q[l];
+    if (!d.Q || misaligned(d.Q, 16) || bad_row_strides(s, eb, n_rows, d.q_stride_n, d.q_stride_h)) return MIXKV_ERR_INVALID_ARG;
+    if (!d.row_start || !d.row_count || misaligned(d.row_start, 4) || misaligned(d.row_count, 4) || misaligned(d.lse, 4)) return MIXKV_ERR_INVALID_ARG;
+    if (!outputs) {
+      if (!d.lse) return MIXKV_ERR_INVALID_ARG;
+      continue;
+    }
+    if (!d.out || misaligned(d.out, 16)) return MIXKV_ERR_INVALID_ARG;
+    const uint64_t out = (uint64_t)n_rows * s.hq * s.D * eb, in = row_span(s, eb, n_rows, d.q_stride_n, d.q_stride_h, s.hq), sums = (uint64_t)n_rows * s.hq * 4;
+    if (regions_overlap(d.out, out, d.Q, in) || (d.lse && (regions_overlap(d.lse, sums, d.Q, in) || regions_overlap(d.lse, sums, d.out, out)))) return MIXKV_ERR_INVALID_ARG;
+  }
+  return MIXKV_OK;
+}
+
+WinTable window_table(const mixkv_paged_cache *c, const mixkv_paged_queries *q, int nl, int eb) {
+  WinTable t;
+  for (int l = 0; l < kLayersPerLaunch; ++l) {
+    t.c[l] = PCache{};
+    t.l[l] = WinLayer{};
+    if (l >= nl) continue;
+    t.c[l] = PCache{static_cast<char *>(c[l].K_pages), static_cast<char *>(c[l].V_pages), nullptr, c[l].page_table, c[l].lengths};
+    t.l[l] = WinLayer{static_cast<const char *>(q[l].Q), q[l].q_stride_n * eb, q[l].q_stride_h * eb, q[l].row_start, q[l].row_count, static_cast<char *>(q[l].out), q[l].lse};
+  }
+  return t;
+}
+
+// The same dealing for groups of rows with a window: the tiles that a group may see, at most.  Chunks grow without end where there are groups enough, as
+// there are for prompts.
+static void window_config(const PShape &s, const PWindow &w, int n_layers, int max_rows, AShape *a) {
+  const int64_t rows = (int64_t)w.max_count * s.G;
+  a->gchunks = (int)((rows + kAttnHeads - 1) / kAttnHeads);
+  a->gt = (int)std::min<int64_t>(rows, kAttnHeads);
+  const int64_t groups = (int64_t)n_layers * s.units_per_layer * a->gchunks, tiles = most_tiles(s, w, max_rows, kAttnHeads), all = tiles * groups;
+  int64_t ct = std::max<int64_t>(4, std::max(std::min<int64_t>((all + 255) / 256, 16), (all + 511) / 512));
+  if (tiles <= 12) ct = tiles;
+  a->ctiles = (int)((std::min(ct, tiles) + 3) / 4 * 4);
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 23) / s.units_per_layer));
+  a->nchunks = (int)std::min(most, std::max<int64_t>(1, (tiles + a->ctiles - 1) / a->ctiles));
+  a->w = w;
+}
+
+}  // namespace mixkv
+
+extern "C" mixkv_status mixkv_paged_window_attention_workspace_size(const mixkv_paged_params *params, int32_t n_layers, int32_t n_rows, int32_t window,
+                                                                    int32_t keep_first, int32_t max_count, int32_t max_rows, size_t *bytes) {
+  using namespace mixkv;
+  PShape s;
+  PWindow w;
+  mixkv_status st = make_pshape(params, &s);
+  if (st != MIXKV_OK) return st;
+  if ((st = make_window(s, n_rows, window, keep_first, max_count, max_rows, &w)) != MIXKV_OK) return st;
+  if (!bytes || n_layers < 1 || n_layers > MIXKV_MAX_LAYERS) return MIXKV_ERR_INVALID_ARG;
+  AShape a{};
+  window_config(s, w, n_layers, clamp_rows(s, max_rows), &a);
+  *bytes = (attn_bytes(s, a, n_layers) + 255) / 256 * 256;
+  return MIXKV_OK;
+}
+
+extern "C" mixkv_status mixkv_paged_window_attention(const mixkv_paged_params *params, const mixkv_paged_cache *caches, const mixkv_paged_queries *queries,
+                                                     int32_t n_layers, int32_t n_rows, int32_t window, int32_t keep_first, int32_t max_count, int32_t max_rows,
+                                                     void *workspace, size_t workspace_bytes, void *hip_stream) {
+  using namespace mixkv;
+  PShape s;
+  PWindow w;
+  mixkv_status st = make_pshape(params, &s);
+  if (st != MIXKV_OK) return st;
+  if ((st = make_window(s, n_rows, window, keep_first, max_count, max_rows, &w)) != MIXKV_OK) return st;
+  if ((st = check_caches(caches, n_layers, true, false)) != MIXKV_OK) return st;
+  const int eb = params->dtype == MIXKV_BF16 ? 2 : 4;
+  if ((st = check_queries(s, eb, queries, n_layers, n_rows, true)) != MIXKV_OK) return st;
+  AShape a{};
+  window_config(s, w, n_layers, clamp_rows(s, max_rows), &a);
+  const size_t need = attn_bytes(s, a, n_layers);
+  if (need > 0) {
+    if (!workspace || misaligned(workspace, 256)) return MIXKV_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return MIXKV_ERR_WORKSPACE_TOO_SMALL;
+  }
+  hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+  float *part = static_cast<float *>(workspace), *part_ml = need > 0 ? part + attn_slots(s, a, n_layers) * s.D : nullptr;
+  // a launch has at most 65535 groups, and fewer than 2^32 threads
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 23) / ((int64_t)s.units_per_layer * std::max(a.nchunks, a.gt))));
+  for (int l0 = 0; l0 < n_layers;) {
+    const int nl = (int)std::min<int64_t>(std::min(n_layers - l0, kLayersPerLaunch), std::max<int64_t>(1, most / a.gchunks));
+    const WinTable t = window_table(caches + l0, queries + l0, nl, eb);
+    const int64_t unit0 = (int64_t)l0 * s.units_per_layer;
+    for (a.gc0 = 0; a.gc0 < a.gchunks; a.gc0 += a.gcn) {
+      a.gcn = (int)std::min<int64_t>(a.gchunks - a.gc0, std::max<int64_t>(1, most / nl));
+      const unsigned z = (unsigned)(nl * a.gcn);
+      auto go = [&](auto kern, auto merge) {
+        hipLaunchKernelGGL(kern, dim3((unsigned)s.units_per_layer, (unsigned)a.nchunks, z), dim3(256), 0, stream, s, a, t, part, part_ml, unit0);
+        if (a.nchunks > 1)
+          hipLaunchKernelGGL(merge, dim3((unsigned)s.units_per_layer, (unsigned)a.gt, z), dim3(256), 0, stream, s, a, t, (const float *)part, (const float *)part_ml, unit0);
+      };
+      if (a.gchunks == 1) launch_attention<true, true>(s, params->dtype, go);
+      else launch_attention<false, true>(s, params->dtype, go);
+      if (hipGetLastError() != hipSuccess) return MIXKV_ERR_HIP;
+    }
+    l0 += nl;
   }
   return MIXKV_OK;
 }
