@@ -942,9 +942,11 @@ extern "C" mixkv_status mixkv_paged_window_attention_workspace_size(const mixkv_
   if (st != MIXKV_OK) return st;
   if ((st = make_window(s, n_rows, window, keep_first, max_count, max_rows, &w)) != MIXKV_OK) return st;
   if (!bytes || n_layers < 1 || n_layers > MIXKV_MAX_LAYERS) return MIXKV_ERR_INVALID_ARG;
+  max_rows = clamp_rows(s, max_rows);
   AShape a{};
-  window_config(s, w, n_layers, clamp_rows(s, max_rows), &a);
-  *bytes = (attn_bytes(s, a, n_layers) + 255) / 256 * 256;
+  const bool many = many_rows(s, params->dtype, w);
+  if (!many) window_config(s, w, n_layers, max_rows, &a);
+  *bytes = ((many ? prompt_bytes(s, w, n_layers, max_rows) : attn_bytes(s, a, n_layers)) + 255) / 256 * 256;
   return MIXKV_OK;
 }
 
@@ -960,14 +962,17 @@ extern "C" mixkv_status mixkv_paged_window_attention(const mixkv_paged_params *p
   if ((st = check_caches(caches, n_layers, true, false)) != MIXKV_OK) return st;
   const int eb = params->dtype == MIXKV_BF16 ? 2 : 4;
   if ((st = check_queries(s, eb, queries, n_layers, n_rows, true)) != MIXKV_OK) return st;
+  max_rows = clamp_rows(s, max_rows);
   AShape a{};
-  window_config(s, w, n_layers, clamp_rows(s, max_rows), &a);
-  const size_t need = attn_bytes(s, a, n_layers);
+  const bool many = many_rows(s, params->dtype, w);
+  if (!many) window_config(s, w, n_layers, max_rows, &a);
+  const size_t need = many ? prompt_bytes(s, w, n_layers, max_rows) : attn_bytes(s, a, n_layers);
   if (need > 0) {
     if (!workspace || misaligned(workspace, 256)) return MIXKV_ERR_INVALID_ARG;
     if (workspace_bytes < need) return MIXKV_ERR_WORKSPACE_TOO_SMALL;
   }
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+  if (many) return launch_prompt(s, w, caches, queries, n_layers, max_rows, workspace, stream);
   float *part = static_cast<float *>(workspace), *part_ml = need > 0 ? part + attn_slots(s, a, n_layers) * s.D : nullptr;
   // a launch has at most 65535 groups, and fewer than 2^32 threads
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 23) / ((int64_t)s.units_per_layer * std::max(a.nchunks, a.gt))));

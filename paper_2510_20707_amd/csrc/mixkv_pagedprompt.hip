@@ -1,0 +1,408 @@
+// Attention of many new rows (prompts, chunks of them) over the pages of a cache: mixkv_paged_window_attention where a unit has more rows than a few.
+//
+// A workgroup has kPromptRows rows of a unit (new rows times the G query heads of a KV head, row i being query head i % G of new row i / G, so that a tile of
+// keys serves all of them), a wave 32 of them, and goes through the 32-row tiles that they see, two at a time, which travel through LDS.
+//   * Scores: S' = K Q', keys on the output rows of 32 x 32 x 16 products: a lane has 16 keys of one row, its neighbour 32 lanes on the other 16, so that the
+//     softmax stays in the lane.
+//   * The second product is O' = V' P': the weights are its second operand as they lie in the lane, because the order of its contraction is free: slot 8 h + j of 16
+//     keys is what the lane's registers hold.
+//   * The offset of a row's exponents moves only where a sum of weights reaches a limit: no maximum is taken otherwise.
+#include "mixkv_pagedwin.h"
+
+namespace mixkv {
+
+constexpr int kPromptWaves = 4, kPromptRows = 32 * kPromptWaves;
+// bf16 weights: a lane's sum of weights that reaches this moves the row's offset (the weighted values stay below it times the largest value).  fp16 weights: a
+// tile's sum of weights in a lane does, and the offset puts the largest weight at 2^8: fp16 then resolves weights down to 2^-32 of it.
+constexpr float kPromptSum = 0x1p20f, kPromptSum16 = 0x1p14f;
+
+struct PromptShape {
+  PWindow w;
+  int32_t qtiles;                        // groups of rows of a unit
+  int32_t q0, qn;                        // those of the launch
+  int32_t nchunks, ctiles;               // chunks of a group's tiles, tiles of a chunk (even)
+};
+
+// What a word's codes i and i + 4 stand for, two fp16: the code on top of the mantissa of 1.0, times the step, plus the base.
+__device__ __forceinline__ uint32_t half_pair(uint32_t w, int i, uint32_t step, uint32_t base) {
+  const uint32_t u = ((i < 2 ? w << (6 - 4 * i) : w >> (4 * i - 6)) & 0x03c003c0u) | 0x3c003c00u;
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, u), __builtin_bit_cast(f16x2, step), __builtin_bit_cast(f16x2, base)));
+}
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+__device__ __forceinline__ u32x4 lds_vec(uint32_t at) { return *(const lds_u32x4 *)(uintptr_t)at; }
+__device__ __forceinline__ void store_lds(uint32_t at, u32x4 x) { *(lds_u32x4 *)(uintptr_t)at = x; }
+
+template <int D, bool Q4>
+__global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(PShape s, PromptShape a, WinTable tab, float *part, float *part_ml, int64_t unit0) {
+  constexpr int RB = D * 2, PPR = RB / 16, KS = D / 16, NB = D / 32, W = kPromptWaves, R = kPromptRows;
+  constexpr int TILE = 32 * RB, IMG = 2 * TILE;              // a tile of 32 rows; two of them
+  __shared__ __align__(16) char img[2][2][IMG];              // turn, keys and values
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int units = s.units_per_layer, turn = a.q0 + a.qn - 1 - (int)blockIdx.y, ch = blockIdx.x / units;     // the rows that see most come first
+  const int u = dealt_unit((int)blockIdx.x - ch * units, blockIdx.y, units), layer = blockIdx.z, b = u / s.hkv, h = u - b * s.hkv;
+  const PCache c = tab.c[layer];
+  const WinLayer l = tab.l[layer];
+  const View v = view_of(s, a.w, c, l, u, turn * R, R);
+  if (v.ng <= 0) return;
+  const int t0 = ch * a.ctiles, t1 = ch == a.nchunks - 1 ? v.tiles : min(v.tiles, t0 + a.ctiles);
+  if (t0 >= t1 && ch > 0) return;
+
+  // ---- the lane's row: its query as the second operand, and its place
+  const int mine = 32 * wave + l32, i_row = min(mine, v.ng - 1), place = v.place(s, i_row);
+  const bool busy = 32 * wave < v.ng;                        // the wave has rows
+  const int wpa = v.place(s, min(32 * wave, v.ng - 1)), wpb = v.place(s, min(32 * wave + 31, v.ng - 1));
+  u32x4 qf[KS];
+  float c2 = s.scale_log2e;
+  {
+    const char *q = v.query(s, a.w, l, h, i_row) + half * 16;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) qf[k] = *reinterpret_cast<const u32x4 *>(q + k * 32);
+    if constexpr (Q4) {                                      // to fp16, by a power of two that brings the row's largest element to [2^13, 2^14)
+      uint32_t most = 0;
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) most = max(most, max(qf[k][j] & 0x7fffu, (qf[k][j] >> 16) & 0x7fffu));
+      most = max(most, (uint32_t)__shfl_xor((int)most, 32));
+      const int up = 13 - (min(max((int)(most >> 7), 1), 254) - 127);
+      c2 = fminf(fmaxf(ldexpf(c2, -up), 0x1p-126f), 0x1p100f);
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          qf[k][j] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)ldexpf(__uint_as_float(qf[k][j] << 16), up), (_Float16)ldexpf(__uint_as_float(qf[k][j] & 0xffff0000u), up)});
+    }
+  }
+
+  // ---- tiles: lane i knows where the i-th tile of a batch of 64 lies
+  int x_page = 0, x_row = 0, x_row0 = 0, x_live = 0;
+  auto batch = [&](int first) {
+    const int t = first + lane, tile = v.tile(t), at = tile >> (s.lp - 5);
+    const int id = t < t1 ? page_at(s, c, u, at) : -1;
+    x_page = max(id, 0);
+    x_row0 = tile * 32;
+    x_row = x_row0 & (s.P - 1);
+    x_live = id >= 0 ? min(max(v.len - x_row0, 0), 32) : 0;
+  };
+  const uint32_t img_a = lds_base_of(img);
+  // bf16: a wave fetches half of one tile's rows, directly.  4 bits: a thread's words and scales, turned into fp16 on their way.
+  constexpr int NG = D / 32, VT = D == 128 ? 128 : 64;       // groups of a row; threads with values of a tile
+  uint32_t kw[NG], ksb[NG];
+  u32x4 vw, vst[2], vba[2];
+  const int side = wave >> 1, r128 = tid & 127;              // which of the two tiles
+  const int krow = r128 >> 2, krun = r128 & 3;               // 4 bits: the thread's key row and run; strip and words of the values
+  const int vq = r128 / (VT / 4), vj = (r128 % (VT / 4)) >> 4, vm = r128 & 15;
+  auto request = [&](int i, int to) {                        // tiles i and i + 1 of the batch
+    const int64_t page = (int64_t)__builtin_amdgcn_readlane(x_page, i + side) * s.page_bytes;
+    const int row = __builtin_amdgcn_readlane(x_row, i + side);
+    if constexpr (!Q4) {
+      constexpr int RPL = 64 / PPR, LOADS = 16 / RPL;        // rows of a load, loads of a wave
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        const char *base = (kv ? c.V : c.K) + page + (int64_t)(row + 16 * (wave & 1)) * RB;
+        const uint32_t dst = img_a + to * (2 * IMG) + kv * IMG + side * TILE + (wave & 1) * (16 * RB);
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+          const int r = 16 * (wave & 1) + j * RPL + lane / PPR, sw = kv ? value_swz<D>(r) : tile_swz<MIXKV_BF16, D>(r);
+          load_to_lds<false>(base + (uint32_t)((j * RPL + lane / PPR) * RB + ((lane % PPR) ^ sw) * 16), dst + j * 1024);
+        }
+      }
+    } else {
+      const char *kp = c.K + page, *vp = c.V + page;
+      const int codes = s.P * (D / 2);
+      const uint32_t *kc = reinterpret_cast<const uint32_t *>(kp + (row + krow) * (D / 2) + krun * (NG * 4));
+      const uint32_t *kz = reinterpret_cast<const uint32_t *>(kp + codes + (row + krow) * (NG * 4));
+#pragma unroll
+      for (int g = 0; g < NG; ++g) { kw[g] = kc[g]; ksb[g] = kz[g]; }
+      if (VT == 128 || r128 < VT) {
+        const int strip = (row >> 5) * 4 + vq;
+        vw = *reinterpret_cast<const u32x4 *>(vp + (strip * D + 64 * vj + 4 * vm) * 4);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const char *z = vp + codes + (strip * NG + 2 * vj + g) * 32;
+          vst[g] = *reinterpret_cast<const u32x4 *>(z);
+          vba[g] = *reinterpret_cast<const u32x4 *>(z + 16);
+        }
+      }
+    }
+  };
+  // 4 bits: what was requested, in fp16, into an image; rows that do not exist are zeros among the values
+  auto unpack = [&](int live, int to) {
+    const uint32_t k_a = img_a + to * (2 * IMG) + side * TILE, v_a = k_a + IMG;
+#pragma unroll
+    for (int pl = 0; pl < NG; ++pl) {
+      const int g = D == 128 ? (pl & 1) * 2 + (pl >> 1) : pl;
+      const uint32_t step = (ksb[pl] & 0xffffu) * 0x10001u, base = (ksb[pl] >> 16) * 0x10001u;
+      u32x4 x;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = half_pair(kw[pl], j, step, base);
+      store_lds(k_a + krow * RB + ((4 * g + krun) ^ tile_swz<MIXKV_BF16, D>(krow)) * 16, x);
+    }
+    if (VT == 128 || r128 < VT) {
+      uint32_t on[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) on[j] = (4 * vq + j < live ? 0xffffu : 0u) | (16 + 4 * vq + j < live ? 0xffff0000u : 0u);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        u32x4 x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = half_pair(vw[w], j, vst[w >> 1][j] & on[j], vba[w >> 1][j] & on[j]);
+        store_lds(v_a + (vq * D + 64 * vj + 16 * w + vm) * 16, x);
+      }
+    }
+  };
+
+  f32x16 o[NB];
+#pragma unroll
+  for (int k = 0; k < NB; ++k)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[k][e] = 0.f;
+  float m = -INFINITY, sum = 0.f;                            // the row's offset, this lane's share of its sum of weights
+
+  const int n = t1 - t0;
+  batch(t0);
+  request(0, 0);
+  if constexpr (Q4) unpack(__builtin_amdgcn_readlane(x_live, side), 0);
+  for (int i = 0; i < n; i += 2) {
+    const int at = i & 63, to = (i >> 1) & 1;
+    if constexpr (!Q4) wait_vm<0>();
+    lds_barrier();
+    const int row0[2] = {__builtin_amdgcn_readlane(x_row0, at), __builtin_amdgcn_readlane(x_row0, at + 1)};
+    const int live[2] = {__builtin_amdgcn_readlane(x_live, at), __builtin_amdgcn_readlane(x_live, at + 1)};
+    const int page[2] = {__builtin_amdgcn_readlane(x_page, at), __builtin_amdgcn_readlane(x_page, at + 1)};
+    int next_live = 0;
+    if (i + 2 < n) {
+      if (((i + 2) & 63) == 0) batch(t0 + i + 2);
+      request((i + 2) & 63, to ^ 1);
+      next_live = __builtin_amdgcn_readlane(x_live, ((i + 2) & 63) + side);
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      if (!busy) continue;
+      const int r0 = row0[x];
+      if (live[x] == 0 || r0 > wpb || (r0 + 31 <= wpa - a.w.window && r0 >= a.w.first)) continue;
+      const bool whole = live[x] == 32 && r0 + 31 <= wpa && (r0 > wpb - a.w.window || r0 + 31 < a.w.first);
+      // ---- scores
+      f32x16 acc;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+      const uint32_t k_a = img_a + to * (2 * IMG) + x * TILE, v_a = k_a + IMG;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const u32x4 kf = lds_vec(k_a + l32 * RB + ((2 * k + half) ^ tile_swz<MIXKV_BF16, D>(l32)) * 16);
+        if constexpr (Q4) acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kf), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
+        else acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[k]), acc, 0, 0, 0);
+      }
+      // ---- weights: register e is key 8 (e / 4) + 4 half + e % 4
+      if (!whole) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int key = 8 * (e >> 2) + 4 * half + (e & 3);
+          acc[e] = key < live[x] && sees(a.w, place, r0 + key) ? acc[e] : -INFINITY;
+        }
+      }
+      float p[16], next = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) { p[e] = fast_exp2(fmaf(acc[e], c2, -m)); next += p[e]; }
+      if (__builtin_amdgcn_ballot_w64(!((Q4 ? next : sum + next) < (Q4 ? kPromptSum16 : kPromptSum))) != 0) {
+        float t = acc[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) t = fmaxf(t, acc[e]);
+        t = fmaxf(t, __shfl_xor(t, 32));
+        const float mn = fmaxf(m, t * c2 - (Q4 ? 8.f : 0.f)), mu = mn == -INFINITY ? 0.f : mn, f = fast_exp2(m - mu);
+        next = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) { p[e] = fast_exp2(fmaf(acc[e], c2, -mu)); next += p[e]; }
+        sum *= f;
+#pragma unroll
+        for (int k = 0; k < NB; ++k)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[k][e] *= f;
+        m = mn;
+      }
+      sum += next;
+      // ---- weighted values
+      u32x4 pw[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (Q4) pw[k][j] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)p[4 * k + j], (_Float16)p[8 + 4 * k + j]});
+          else pw[k][j] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)p[8 * k + 2 * j], (__bf16)p[8 * k + 2 * j + 1]});
+        }
+      auto value = [&](int k, int blk) {
+        if constexpr (Q4) {
+          return lds_vec(v_a + ((2 * k + half) * D + 32 * blk + l32) * 16);
+        } else {
+          const int l16 = lane & 15, sub = (lane >> 4) & 1;
+          uint32_t at2[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int r = 16 * k + 8 * j + 4 * half + (l16 >> 2);
+            at2[j] = v_a + r * RB + ((4 * blk + 2 * sub + ((l16 & 3) >> 1)) ^ value_swz<D>(r)) * 16 + (l16 & 1) * 8;
+          }
+          const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)at2[0]);
+          const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)at2[1]);
+          return __builtin_bit_cast(u32x4, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+      };
+      bool mixed = false;                                    // values that are no numbers, in a tile that not all of the wave's rows see all of
+      if constexpr (!Q4) {
+        if (!whole) {
+          bool odd = false;
+#pragma unroll
+          for (int j = 0; j < TILE / 1024; ++j) {
+            const u32x4 w = lds_vec(v_a + j * 1024 + lane * 16);
+#pragma unroll
+            for (int z = 0; z < 4; ++z) odd |= no_number<MIXKV_BF16>(w[z]);
+          }
+          mixed = __builtin_amdgcn_ballot_w64(odd) != 0;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int blk = 0; blk < NB; ++blk) {
+          u32x4 vf = value(k, blk);
+          if constexpr (Q4) {
+            o[blk] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, vf), __builtin_bit_cast(f16x8, pw[k]), o[blk], 0, 0, 0);
+          } else {
+            if (mixed) {
+#pragma unroll
+              for (int z = 0; z < 4; ++z) vf[z] = numbers_only<MIXKV_BF16>(vf[z]);
+            }
+            o[blk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pw[k]), o[blk], 0, 0, 0);
+          }
+        }
+      if (mixed) {                                           // what went into the product as zeros, where its row is seen: a weight of zero does not make NaN of it
+        const char *from = c.V + (int64_t)page[x] * s.page_bytes + (int64_t)(r0 & (s.P - 1)) * RB;
+#pragma unroll 1
+        for (int r = 0; r < live[x]; ++r) {
+          if (!sees(a.w, place, r0 + r)) continue;
+#pragma unroll
+          for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float y = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(from + r * RB)[32 * blk + 8 * (e >> 2) + 4 * half + (e & 3)] << 16);
+              if (no_number<MIXKV_F32>(__float_as_uint(y))) o[blk][e] += y;
+            }
+        }
+      }
+    }
+    if constexpr (Q4) {
+      if (i + 2 < n) unpack(next_live, to ^ 1);
+    }
+  }
+
+  // ---- lane (row, half) has the elements 32 blk + 8 (e / 4) + 4 half + e % 4
+  if (!busy || mine >= v.ng) return;
+  sum += __shfl_xor(sum, 32);
+  if (a.nchunks > 1) {
+    const int64_t slot = (((unit0 + (int64_t)layer * units + u) * a.qtiles + turn) * a.nchunks + ch) * R + mine;
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4 *>(part + slot * D + 32 * blk + 8 * q + 4 * half) = f32x4{o[blk][4 * q], o[blk][4 * q + 1], o[blk][4 * q + 2], o[blk][4 * q + 3]};
+    if (half == 0) reinterpret_cast<float2 *>(part_ml)[slot] = make_float2(m, sum);
+    return;
+  }
+  const int64_t row = v.out_row(s, a.w, h, mine);
+  if (row < 0) return;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+  for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      u32x2 w;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) w[j] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)(o[blk][4 * q + 2 * j] * inv), (__bf16)(o[blk][4 * q + 2 * j + 1] * inv)});
+      *reinterpret_cast<u32x2 *>(l.out + row * RB + (32 * blk + 8 * q + 4 * half) * 2) = w;
+    }
+  if (half == 0 && l.lse) l.lse[row] = row_lse(m == -INFINITY ? 0.f : m, sum);
+}
+
+// Folds the chunks of a group's rows: D/4 threads to a row, in the order of the chunks.
+template <int D>
+__global__ __launch_bounds__(256) void prompt_merge_kernel(PShape s, PromptShape a, WinTable tab, const float *part, const float *part_ml, int64_t unit0) {
+  constexpr int T = D / 4, ROWS = 256 / T, R = kPromptRows;
+  const int t = threadIdx.x % T, i = blockIdx.y * ROWS + threadIdx.x / T, turn = a.q0 + blockIdx.z % a.qn, layer = blockIdx.z / a.qn, u = blockIdx.x;
+  const int h = u % s.hkv;
+  const WinLayer l = tab.l[layer];
+  const View v = view_of(s, a.w, tab.c[layer], l, u, turn * R, R);
+  if (i >= v.ng) return;
+  const int64_t row = v.out_row(s, a.w, h, i);
+  if (row < 0) return;
+  const int used = max(1, min(a.nchunks, (v.tiles + a.ctiles - 1) / a.ctiles));
+  const int64_t slot = ((unit0 + (int64_t)layer * s.units_per_layer + u) * a.qtiles + turn) * a.nchunks * R + i;
+  const float2 *ml = reinterpret_cast<const float2 *>(part_ml);
+  float m = -INFINITY, tot = 0.f;
+  for (int k = 0; k < used; ++k) m = fmaxf(m, ml[slot + (int64_t)k * R].x);
+  const float mu = m == -INFINITY ? 0.f : m;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int k = 0; k < used; ++k) {
+    const float2 x = ml[slot + (int64_t)k * R];
+    const float f = fast_exp2(x.x - mu);
+    acc += *reinterpret_cast<const f32x4 *>(part + (slot + (int64_t)k * R) * D + 4 * t) * f;
+    tot = fmaf(x.y, f, tot);
+  }
+  u32x2 w;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) w[j] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)row_result(acc[2 * j], tot), (__bf16)row_result(acc[2 * j + 1], tot)});
+  *reinterpret_cast<u32x2 *>(l.out + (row * D + 4 * t) * 2) = w;
+  if (t == 0 && l.lse) l.lse[row] = row_lse(mu, tot);
+}
+
+// Chunks of a group's tiles: one, unless the groups are fewer than the chip takes at once; then as many as fill it, of at least eight tiles.
+static PromptShape prompt_config(const PShape &s, const PWindow &w, int n_layers, int max_rows) {
+  PromptShape a{};
+  a.w = w;
+  a.qtiles = (int)(((int64_t)w.max_count * s.G + kPromptRows - 1) / kPromptRows);
+  const int64_t groups = (int64_t)n_layers * s.units_per_layer * a.qtiles, tiles = most_tiles(s, w, max_rows, kPromptRows);
+  int64_t chunks = std::max<int64_t>(1, std::min<int64_t>(512 / groups, (tiles + 7) / 8));
+  a.ctiles = (int)(((tiles + chunks - 1) / chunks + 1) / 2 * 2);
+  a.nchunks = (int)((tiles + a.ctiles - 1) / a.ctiles);
+  return a;
+}
+static size_t prompt_slots(const PShape &s, const PromptShape &a, int n_layers) {
+  return a.nchunks == 1 ? 0 : (size_t)n_layers * s.units_per_layer * a.qtiles * a.nchunks * kPromptRows;
+}
+
+size_t prompt_bytes(const PShape &s, const PWindow &w, int n_layers, int max_rows) {
+  return prompt_slots(s, prompt_config(s, w, n_layers, max_rows), n_layers) * (s.D + 2) * sizeof(float);
+}
+
+mixkv_status launch_prompt(const PShape &s, const PWindow &w, const mixkv_paged_cache *caches, const mixkv_paged_queries *queries, int n_layers, int max_rows,
+                           void *workspace, hipStream_t stream) {
+  PromptShape a = prompt_config(s, w, n_layers, max_rows);
+  const size_t slots = prompt_slots(s, a, n_layers);
+  float *part = static_cast<float *>(workspace), *part_ml = slots ? part + slots * s.D : nullptr;
+  // a launch has at most 65535 groups of rows, and fewer than 2^32 threads
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 23) / ((int64_t)s.units_per_layer * std::max(a.nchunks, kPromptRows))));
+  for (int l0 = 0; l0 < n_layers;) {
+    const int nl = (int)std::min<int64_t>(std::min(n_layers - l0, kLayersPerLaunch), std::max<int64_t>(1, most / a.qtiles));
+    const WinTable t = window_table(caches + l0, queries + l0, nl, 2);
+    const int64_t unit0 = (int64_t)l0 * s.units_per_layer;
+    for (a.q0 = 0; a.q0 < a.qtiles; a.q0 += a.qn) {
+      a.qn = (int)std::min<int64_t>(a.qtiles - a.q0, std::max<int64_t>(1, most / nl));
+      const dim3 grid((unsigned)(s.units_per_layer * a.nchunks), (unsigned)a.qn, (unsigned)nl);
+      auto go = [&](auto kern, auto merge, int rows) {
+        hipLaunchKernelGGL(kern, grid, dim3(64 * kPromptWaves), 0, stream, s, a, t, part, part_ml, unit0);
+        if (a.nchunks > 1)
+          hipLaunchKernelGGL(merge, dim3((unsigned)s.units_per_layer, (unsigned)(kPromptRows / rows), (unsigned)(nl * a.qn)), dim3(256), 0, stream, s, a, t, (const float *)part,
+                             (const float *)part_ml, unit0);
+      };
+      if (s.q4) { if (s.D == 128) go(paged_prompt_kernel<128, true>, prompt_merge_kernel<128>, 8); else go(paged_prompt_kernel<64, true>, prompt_merge_kernel<64>, 16); }
+      else { if (s.D == 128) go(paged_prompt_kernel<128, false>, prompt_merge_kernel<128>, 8); else go(paged_prompt_kernel<64, false>, prompt_merge_kernel<64>, 16); }
+      if (hipGetLastError() != hipSuccess) return MIXKV_ERR_HIP;
+    }
+    l0 += nl;
+  }
+  return MIXKV_OK;
+}
+
+}  // namespace mixkv

@@ -92,6 +92,12 @@ __device__ __forceinline__ uint32_t numbers_only(uint32_t w) {
 
 mixkv_status make_window(const PShape &s, int n_rows, int window, int first, int max_count, int max_rows, PWindow *w);
 mixkv_status check_queries(const PShape &s, int eb, const mixkv_paged_queries *q, int n_layers, int64_t n_rows, bool outputs);
+// Whether rows go to the kernel of prompts (mixkv_pagedprompt.hip), its workspace and its launches.
+constexpr int kFewRows = 64;
+inline bool many_rows(const PShape &s, int dtype, const PWindow &w) { return dtype == MIXKV_BF16 && (int64_t)w.max_count * s.G > kFewRows; }
+size_t prompt_bytes(const PShape &s, const PWindow &w, int n_layers, int max_rows);
+mixkv_status launch_prompt(const PShape &s, const PWindow &w, const mixkv_paged_cache *caches, const mixkv_paged_queries *queries, int n_layers, int max_rows,
+                           void *workspace, hipStream_t stream);
 WinTable window_table(const mixkv_paged_cache *c, const mixkv_paged_queries *q, int nl, int eb);
 
 }  // namespace mixkv
