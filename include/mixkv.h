@@ -481,8 +481,7 @@ typedef struct {
  * out = sum_j softmax_j(softmax_scale * q . k_j) v_j, and lse = log sum_j exp(softmax_scale * q . k_j), the natural logarithm (for the last
  * W rows of a prompt what mixkv_layer_in.window_lse asks for, with causal_window and a window that leaves nothing out).  A row that sees nothing gets zeros
  * and -infinity.  Rows of out and lse that belong to no (sequence, head) keep their contents.  fp32 accumulation, out in the dtype.  With
- * many new rows of bf16 the weights enter the second product as bf16; with 4-bit pages values and weights enter it as fp16, and with many
- * new rows the keys' elements enter the first one as fp16.  Logits and values as for mixkv_paged_attention.
+ * many new rows of bf16 the weights enter the second product as bf16; with 4-bit pages values and weights enter it as fp16.  Logits and values as for mixkv_paged_attention.
  * max_count: the largest row_count; a head's rows beyond max_count are not served (their outputs keep their contents).  max_rows: the largest length, as
  * far as the host knows it (>= 1): longer heads are served, slower.  Outputs repeat bit for bit for the same arguments, max_count and max_rows
  * included.  n_rows * n_q_heads <= 2^31 - 1.  Workspace: mixkv_paged_window_attention_workspace_size bytes (0: NULL is accepted), 256-byte
@@ -498,7 +497,7 @@ mixkv_status mixkv_paged_window_attention(const mixkv_paged_params *params, cons
  * The attention that cached rows have been given, summed up: with the lse that mixkv_paged_window_attention left for the same queries, window and
  * keep_first (or any other normaliser), row j of KV head h has its weight raised by
  *     sum over the new rows that see j, and over the G query heads, of exp(softmax_scale * q . k_j - lse),
- * in fp32; the weights of the new rows themselves begin at zero.  A place's weight lies beside its page: weights[page][row of the page].  Rows
+ * in fp32; the weights of the new rows themselves begin at zero.  A place's weight lies beside its page: weights[l][page][row of the page], 16-byte aligned.  Rows
  * whose lse is -infinity give nothing.  Weights of rows that do not exist, and of old rows that no new row sees, keep their contents.  A head's
  * rows beyond max_count are not served; max_rows as above.  V_pages are not used and may be NULL.  Sums repeat bit for bit for the same
  * arguments.  Workspace: mixkv_paged_weights_workspace_size bytes (0: NULL is accepted), 256-byte aligned, no initialisation.

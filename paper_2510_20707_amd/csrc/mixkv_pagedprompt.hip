@@ -1,6 +1,6 @@
 // Attention of many new rows (prompts, chunks of them) over the pages of a cache: mixkv_paged_window_attention where a unit has more rows than a few.
 //
-// A workgroup has kPromptRows rows of a unit (new rows times the G query heads of a KV head, row i being query head i % G of new row i / G, so that a tile of
+// A workgroup has 128 or 256 rows of a unit (new rows times the G query heads of a KV head, row i being query head i % G of new row i / G, so that a tile of
 // keys serves all of them), a wave 32 of them, and goes through the 32-row tiles that they see, two at a time, which travel through LDS.
 //   * Scores: S' = K Q', keys on the output rows of 32 x 32 x 16 products: a lane has 16 keys of one row, its neighbour 32 lanes on the other 16, so that the
 //     softmax stays in the lane.
@@ -11,7 +11,9 @@
 
 namespace mixkv {
 
-constexpr int kPromptWaves = 4, kPromptRows = 32 * kPromptWaves;
+// Waves of a workgroup.  4-bit tiles are turned into fp16 once for all of its rows, and take half as much of LDS again.
+constexpr int prompt_waves(bool q4) { return q4 ? 8 : 4; }
+constexpr int prompt_rows(bool q4) { return 32 * prompt_waves(q4); }
 // bf16 weights: a lane's sum of weights that reaches this moves the row's offset (the weighted values stay below it times the largest value).  fp16 weights: a
 // tile's sum of weights in a lane does, and the offset puts the largest weight at 2^8: fp16 then resolves weights down to 2^-32 of it.
 constexpr float kPromptSum = 0x1p20f, kPromptSum16 = 0x1p14f;
@@ -23,10 +25,9 @@ struct PromptShape {
   int32_t nchunks, ctiles;               // chunks of a group's tiles, tiles of a chunk (even)
 };
 
-// What a word's codes i and i + 4 stand for, two fp16: the code on top of the mantissa of 1.0, times the step, plus the base.
-__device__ __forceinline__ uint32_t half_pair(uint32_t w, int i, uint32_t step, uint32_t base) {
-  const uint32_t u = ((i < 2 ? w << (6 - 4 * i) : w >> (4 * i - 6)) & 0x03c003c0u) | 0x3c003c00u;
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, u), __builtin_bit_cast(f16x2, step), __builtin_bit_cast(f16x2, base)));
+// 1 + code / 16 for the codes i and i + 4 of a word: the code on top of the mantissa of 1.0.
+__device__ __forceinline__ f16x2 code_pair(uint32_t w, int i) {
+  return __builtin_bit_cast(f16x2, ((i < 2 ? w << (6 - 4 * i) : w >> (4 * i - 6)) & 0x03c003c0u) | 0x3c003c00u);
 }
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -35,10 +36,11 @@ __device__ __forceinline__ u32x4 lds_vec(uint32_t at) { return *(const lds_u32x4
 __device__ __forceinline__ void store_lds(uint32_t at, u32x4 x) { *(lds_u32x4 *)(uintptr_t)at = x; }
 
 template <int D, bool Q4>
-__global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(PShape s, PromptShape a, WinTable tab, float *part, float *part_ml, int64_t unit0) {
-  constexpr int RB = D * 2, PPR = RB / 16, KS = D / 16, NB = D / 32, W = kPromptWaves, R = kPromptRows;
+__global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(PShape s, PromptShape a, WinTable tab, float *part, float *part_ml, int64_t unit0) {
+  constexpr int RB = D * 2, PPR = RB / 16, KS = D / 16, NB = D / 32, W = prompt_waves(Q4), R = prompt_rows(Q4);
   constexpr int TILE = 32 * RB, IMG = 2 * TILE;              // a tile of 32 rows; two of them
-  __shared__ __align__(16) char img[2][2][IMG];              // turn, keys and values
+  constexpr int TURN = (Q4 ? 3 : 2) * IMG;                   // keys, values, (4 bits) what the keys' elements lack in fp16
+  __shared__ __align__(16) char img[2][TURN];
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int units = s.units_per_layer, turn = a.q0 + a.qn - 1 - (int)blockIdx.y, ch = blockIdx.x / units;     // the rows that see most come first
@@ -89,12 +91,14 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(PSha
   };
   const uint32_t img_a = lds_base_of(img);
   // bf16: a wave fetches half of one tile's rows, directly.  4 bits: a thread's words and scales, turned into fp16 on their way.
-  constexpr int NG = D / 32, VT = D == 128 ? 128 : 64;       // groups of a row; threads with values of a tile
-  uint32_t kw[NG], ksb[NG];
-  u32x4 vw, vst[2], vba[2];
-  const int side = wave >> 1, r128 = tid & 127;              // which of the two tiles
-  const int krow = r128 >> 2, krun = r128 & 3;               // 4 bits: the thread's key row and run; strip and words of the values
-  const int vq = r128 / (VT / 4), vj = (r128 % (VT / 4)) >> 4, vm = r128 & 15;
+  constexpr int NG = D / 32, VT = 2 * D;                     // groups of a row; threads with values of a tile
+  uint32_t kw[NG / 2], ksb[NG / 2];
+  u32x2 vw;
+  u32x4 vst, vba;
+  const int side = wave / (W / 2);                           // which of the two tiles
+  // 4 bits: the thread's key row, run and words of it; the values' strip, words 64 vj + 4 vm + 2 vh + (0, 1) of it
+  const int r256 = tid & 255, krow = r256 >> 3, krun = (r256 >> 1) & 3, kpl = (r256 & 1) * (NG / 2);
+  const int vq = r256 / (VT / 4), vj = r256 % (VT / 4) >> 5, vm = (r256 >> 1) & 15, vh = r256 & 1;
   auto request = [&](int i, int to) {                        // tiles i and i + 1 of the batch
     const int64_t page = (int64_t)__builtin_amdgcn_readlane(x_page, i + side) * s.page_bytes;
     const int row = __builtin_amdgcn_readlane(x_row, i + side);
@@ -103,7 +107,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(PSha
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
         const char *base = (kv ? c.V : c.K) + page + (int64_t)(row + 16 * (wave & 1)) * RB;
-        const uint32_t dst = img_a + to * (2 * IMG) + kv * IMG + side * TILE + (wave & 1) * (16 * RB);
+        const uint32_t dst = img_a + to * TURN + kv * IMG + side * TILE + (wave & 1) * (16 * RB);
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
           const int r = 16 * (wave & 1) + j * RPL + lane / PPR, sw = kv ? value_swz<D>(r) : tile_swz<MIXKV_BF16, D>(r);
@@ -113,44 +117,51 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(PSha
     } else {
       const char *kp = c.K + page, *vp = c.V + page;
       const int codes = s.P * (D / 2);
-      const uint32_t *kc = reinterpret_cast<const uint32_t *>(kp + (row + krow) * (D / 2) + krun * (NG * 4));
-      const uint32_t *kz = reinterpret_cast<const uint32_t *>(kp + codes + (row + krow) * (NG * 4));
+      const uint32_t *kc = reinterpret_cast<const uint32_t *>(kp + (row + krow) * (D / 2) + krun * (NG * 4)) + kpl;
+      const uint32_t *kz = reinterpret_cast<const uint32_t *>(kp + codes + (row + krow) * (NG * 4)) + kpl;
 #pragma unroll
-      for (int g = 0; g < NG; ++g) { kw[g] = kc[g]; ksb[g] = kz[g]; }
-      if (VT == 128 || r128 < VT) {
+      for (int g = 0; g < NG / 2; ++g) { kw[g] = kc[g]; ksb[g] = kz[g]; }
+      if (VT == 256 || r256 < VT) {
         const int strip = (row >> 5) * 4 + vq;
-        vw = *reinterpret_cast<const u32x4 *>(vp + (strip * D + 64 * vj + 4 * vm) * 4);
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const char *z = vp + codes + (strip * NG + 2 * vj + g) * 32;
-          vst[g] = *reinterpret_cast<const u32x4 *>(z);
-          vba[g] = *reinterpret_cast<const u32x4 *>(z + 16);
-        }
+        vw = *reinterpret_cast<const u32x2 *>(vp + (strip * D + 64 * vj + 4 * vm + 2 * vh) * 4);
+        const char *z = vp + codes + (strip * NG + 2 * vj + vh) * 32;
+        vst = *reinterpret_cast<const u32x4 *>(z);
+        vba = *reinterpret_cast<const u32x4 *>(z + 16);
       }
     }
   };
   // 4 bits: what was requested, in fp16, into an image; rows that do not exist are zeros among the values
   auto unpack = [&](int live, int to) {
-    const uint32_t k_a = img_a + to * (2 * IMG) + side * TILE, v_a = k_a + IMG;
+    const uint32_t k_a = img_a + to * TURN + side * TILE, v_a = k_a + IMG, l_a = v_a + IMG;
 #pragma unroll
-    for (int pl = 0; pl < NG; ++pl) {
-      const int g = D == 128 ? (pl & 1) * 2 + (pl >> 1) : pl;
-      const uint32_t step = (ksb[pl] & 0xffffu) * 0x10001u, base = (ksb[pl] >> 16) * 0x10001u;
-      u32x4 x;
+    for (int g = 0; g < NG / 2; ++g) {
+      const int pl = kpl + g, piece = 4 * (D == 128 ? (pl & 1) * 2 + (pl >> 1) : pl) + krun;
+      const f16x2 sb = __builtin_bit_cast(f16x2, ksb[g]), step = {sb[0], sb[0]}, base = {sb[1], sb[1]};
+      u32x4 hi, lo;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = half_pair(kw[pl], j, step, base);
-      store_lds(k_a + krow * RB + ((4 * g + krun) ^ tile_swz<MIXKV_BF16, D>(krow)) * 16, x);
+      for (int j = 0; j < 4; ++j) {
+        const f16x2 un = code_pair(kw[g], j), x = __builtin_elementwise_fma(un, step, base);
+        hi[j] = __builtin_bit_cast(uint32_t, x);
+        lo[j] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)(fmaf((float)un[0], (float)sb[0], (float)sb[1]) - (float)x[0]), (_Float16)(fmaf((float)un[1], (float)sb[0], (float)sb[1]) - (float)x[1])});
+      }
+      const uint32_t at = krow * RB + (piece ^ tile_swz<MIXKV_BF16, D>(krow)) * 16;
+      store_lds(k_a + at, hi);
+      store_lds(l_a + at, lo);
     }
-    if (VT == 128 || r128 < VT) {
-      uint32_t on[4];
+    if (VT == 256 || r256 < VT) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) on[j] = (4 * vq + j < live ? 0xffffu : 0u) | (16 + 4 * vq + j < live ? 0xffff0000u : 0u);
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t on = (4 * vq + j < live ? 0xffffu : 0u) | (16 + 4 * vq + j < live ? 0xffff0000u : 0u);
+        vst[j] &= on;
+        vba[j] &= on;
+      }
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
+      for (int w = 0; w < 2; ++w) {
         u32x4 x;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = half_pair(vw[w], j, vst[w >> 1][j] & on[j], vba[w >> 1][j] & on[j]);
-        store_lds(v_a + (vq * D + 64 * vj + 16 * w + vm) * 16, x);
+        for (int j = 0; j < 4; ++j)
+          x[j] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(code_pair(vw[w], j), __builtin_bit_cast(f16x2, (uint32_t)vst[j]), __builtin_bit_cast(f16x2, (uint32_t)vba[j])));
+        store_lds(v_a + (vq * D + 64 * vj + 16 * (2 * vh + w) + vm) * 16, x);
       }
     }
   };
@@ -189,12 +200,15 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(PSha
       f32x16 acc;
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-      const uint32_t k_a = img_a + to * (2 * IMG) + x * TILE, v_a = k_a + IMG;
+      const uint32_t k_a = img_a + to * TURN + x * TILE, v_a = k_a + IMG;
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         const u32x4 kf = lds_vec(k_a + l32 * RB + ((2 * k + half) ^ tile_swz<MIXKV_BF16, D>(l32)) * 16);
-        if constexpr (Q4) acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kf), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
-        else acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[k]), acc, 0, 0, 0);
+        if constexpr (Q4) {                                  // (the keys in two parts: a logit is off by no more than fp32 makes it, as lse and weights have to be)
+          const u32x4 lf = lds_vec(k_a + 2 * IMG + l32 * RB + ((2 * k + half) ^ tile_swz<MIXKV_BF16, D>(l32)) * 16);
+          acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lf), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
+          acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kf), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
+        } else acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[k]), acc, 0, 0, 0);
       }
       // ---- weights: register e is key 8 (e / 4) + 4 half + e % 4
       if (!whole) {
@@ -328,8 +342,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(PSha
 // Folds the chunks of a group's rows: D/4 threads to a row, in the order of the chunks.
 template <int D>
 __global__ __launch_bounds__(256) void prompt_merge_kernel(PShape s, PromptShape a, WinTable tab, const float *part, const float *part_ml, int64_t unit0) {
-  constexpr int T = D / 4, ROWS = 256 / T, R = kPromptRows;
-  const int t = threadIdx.x % T, i = blockIdx.y * ROWS + threadIdx.x / T, turn = a.q0 + blockIdx.z % a.qn, layer = blockIdx.z / a.qn, u = blockIdx.x;
+  constexpr int T = D / 4, ROWS = 256 / T;
+  const int R = prompt_rows(s.q4 != 0), t = threadIdx.x % T, i = blockIdx.y * ROWS + threadIdx.x / T, turn = a.q0 + blockIdx.z % a.qn, layer = blockIdx.z / a.qn, u = blockIdx.x;
   const int h = u % s.hkv;
   const WinLayer l = tab.l[layer];
   const View v = view_of(s, a.w, tab.c[layer], l, u, turn * R, R);
@@ -360,16 +374,17 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PShape s, PromptShape
 // Chunks of a group's tiles: one, unless the groups are fewer than the chip takes at once; then as many as fill it, of at least eight tiles.
 static PromptShape prompt_config(const PShape &s, const PWindow &w, int n_layers, int max_rows) {
   PromptShape a{};
+  const int rows = prompt_rows(s.q4 != 0), groups_at_once = s.q4 ? 256 : 512;
   a.w = w;
-  a.qtiles = (int)(((int64_t)w.max_count * s.G + kPromptRows - 1) / kPromptRows);
-  const int64_t groups = (int64_t)n_layers * s.units_per_layer * a.qtiles, tiles = most_tiles(s, w, max_rows, kPromptRows);
-  int64_t chunks = std::max<int64_t>(1, std::min<int64_t>(512 / groups, (tiles + 7) / 8));
+  a.qtiles = (int)(((int64_t)w.max_count * s.G + rows - 1) / rows);
+  const int64_t groups = (int64_t)n_layers * s.units_per_layer * a.qtiles, tiles = most_tiles(s, w, max_rows, rows);
+  int64_t chunks = std::max<int64_t>(1, std::min<int64_t>(groups_at_once / groups, (tiles + 7) / 8));
   a.ctiles = (int)(((tiles + chunks - 1) / chunks + 1) / 2 * 2);
   a.nchunks = (int)((tiles + a.ctiles - 1) / a.ctiles);
   return a;
 }
 static size_t prompt_slots(const PShape &s, const PromptShape &a, int n_layers) {
-  return a.nchunks == 1 ? 0 : (size_t)n_layers * s.units_per_layer * a.qtiles * a.nchunks * kPromptRows;
+  return a.nchunks == 1 ? 0 : (size_t)n_layers * s.units_per_layer * a.qtiles * a.nchunks * prompt_rows(s.q4 != 0);
 }
 
 size_t prompt_bytes(const PShape &s, const PWindow &w, int n_layers, int max_rows) {
@@ -382,7 +397,7 @@ mixkv_status launch_prompt(const PShape &s, const PWindow &w, const mixkv_paged_
   const size_t slots = prompt_slots(s, a, n_layers);
   float *part = static_cast<float *>(workspace), *part_ml = slots ? part + slots * s.D : nullptr;
   // a launch has at most 65535 groups of rows, and fewer than 2^32 threads
-  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 23) / ((int64_t)s.units_per_layer * std::max(a.nchunks, kPromptRows))));
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 22) / ((int64_t)s.units_per_layer * std::max(a.nchunks, prompt_rows(s.q4 != 0)))));
   for (int l0 = 0; l0 < n_layers;) {
     const int nl = (int)std::min<int64_t>(std::min(n_layers - l0, kLayersPerLaunch), std::max<int64_t>(1, most / a.qtiles));
     const WinTable t = window_table(caches + l0, queries + l0, nl, 2);
@@ -391,9 +406,9 @@ mixkv_status launch_prompt(const PShape &s, const PWindow &w, const mixkv_paged_
       a.qn = (int)std::min<int64_t>(a.qtiles - a.q0, std::max<int64_t>(1, most / nl));
       const dim3 grid((unsigned)(s.units_per_layer * a.nchunks), (unsigned)a.qn, (unsigned)nl);
       auto go = [&](auto kern, auto merge, int rows) {
-        hipLaunchKernelGGL(kern, grid, dim3(64 * kPromptWaves), 0, stream, s, a, t, part, part_ml, unit0);
+        hipLaunchKernelGGL(kern, grid, dim3(64 * prompt_waves(s.q4 != 0)), 0, stream, s, a, t, part, part_ml, unit0);
         if (a.nchunks > 1)
-          hipLaunchKernelGGL(merge, dim3((unsigned)s.units_per_layer, (unsigned)(kPromptRows / rows), (unsigned)(nl * a.qn)), dim3(256), 0, stream, s, a, t, (const float *)part,
+          hipLaunchKernelGGL(merge, dim3((unsigned)s.units_per_layer, (unsigned)(prompt_rows(s.q4 != 0) / rows), (unsigned)(nl * a.qn)), dim3(256), 0, stream, s, a, t, (const float *)part,
                              (const float *)part_ml, unit0);
       };
       if (s.q4) { if (s.D == 128) go(paged_prompt_kernel<128, true>, prompt_merge_kernel<128>, 8); else go(paged_prompt_kernel<64, true>, prompt_merge_kernel<64>, 16); }

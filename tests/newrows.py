@@ -37,9 +37,9 @@ class Rows:
     def args(self):
         return self.lay.args(), self.lay.table, self.lay.lengths, self.Q, self.start, self.count
 
-    def logit_error(self, scale, coarse):
-        """How far a logit may be off: a fp32 sum of D terms by D 2^-24 of their magnitudes' sum (4-bit keys are summed as S sum(q u) + B sum(q), whose terms are up
-        to 8 max |k| |q|); with `coarse` 4-bit elements are rounded to fp16 as well, by 2^-11 of themselves."""
+    def logit_error(self, scale):
+        """How far a logit may be off: a fp32 sum of D terms by D 2^-24 of their magnitudes' sum (4-bit keys are summed as S sum(q u) + B sum(q), or in two fp16
+        parts, with terms of up to 8 max |k| |q|)."""
         most = 0.0
         for b, h in np.ndindex(*self.lay.lengths.shape):
             k, _, there = O.rows_of(*self.lay.args(), self.lay.table, self.lay.lengths, b, h)
@@ -47,10 +47,7 @@ class Rows:
             if len(k):
                 q = np.abs(self.Q[:, h * self.G:(h + 1) * self.G])
                 most = max(most, float(q.sum(-1).max() * 8 * np.abs(k).max()) if self.lay.fmt == "4bit" else float((q.reshape(-1, self.lay.D) @ np.abs(k).T).max()))
-        error = self.lay.D * 2.0 ** -24 * most * scale
-        if coarse and self.lay.fmt == "4bit":
-            error += 2.0 ** -11 * most / 8 * scale
-        return error
+        return self.lay.D * 2.0 ** -24 * most * scale
 
 
 def attend(rows, window=ALL, first=0, scale=1.0, max_count=None, max_rows=None, strided=False, cache=None):
@@ -68,7 +65,7 @@ def check_attention(rows, q, window=ALL, first=0, scale=1.0, max_count=None):
     lay = rows.lay
     lay_v = max((float(np.abs(v[np.isfinite(v)]).max(initial=0.0)) for v in (O.rows_of(*lay.args(), lay.table, lay.lengths, b, h)[1] for b, h in np.ndindex(*lay.lengths.shape))), default=0.0)
     coarse = min(rows.max_count, max_count or rows.max_count) * rows.G > MANY
-    d = rows.logit_error(scale, coarse)
+    d = rows.logit_error(scale)
     out, lse = np.full(rows.Q.shape, 7.0), np.full(rows.Q.shape[:2], 7.0)
     with np.errstate(invalid="ignore"):
         O.window_attention(*rows.args(), window, first, max_count or rows.max_count, scale, out, lse)
@@ -97,7 +94,7 @@ def check_weights(rows, lse, before, got, window=ALL, first=0, scale=1.0, max_co
     lay = rows.lay
     want = before.astype(np.float64).copy()
     O.window_weights(*rows.args(), window, first, max_count or rows.max_count, scale, lse.astype(np.float64), want)
-    d = rows.logit_error(scale, False)
+    d = rows.logit_error(scale)
     same = np.isnan(want)
     assert np.array_equal(np.isnan(got), same)
     err = np.where(same, 0.0, np.abs(got - want))
