@@ -39,8 +39,9 @@ template <int D, bool Q4>
 __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(PShape s, PromptShape a, WinTable tab, float *part, float *part_ml, int64_t unit0) {
   constexpr int RB = D * 2, PPR = RB / 16, KS = D / 16, NB = D / 32, W = prompt_waves(Q4), R = prompt_rows(Q4);
   constexpr int TILE = 32 * RB, IMG = 2 * TILE;              // a tile of 32 rows; two of them
-  constexpr int TURN = (Q4 ? 3 : 2) * IMG;                   // keys, values, (4 bits) what the keys' elements lack in fp16
-  __shared__ __align__(16) char img[2][TURN];
+  constexpr int KEYS = (Q4 ? 2 : 1) * IMG;                   // keys' tiles, and (4 bits) behind them what their elements lack in fp16
+  __shared__ __align__(16) char img[2 * KEYS + 2 * IMG];
+  __shared__ int odd_s[W];
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int units = s.units_per_layer, turn = a.q0 + a.qn - 1 - (int)blockIdx.y, ch = blockIdx.x / units;     // the rows that see most come first
@@ -54,7 +55,6 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
 
   // ---- the lane's row: its query as the second operand, and its place
   const int mine = 32 * wave + l32, i_row = min(mine, v.ng - 1), place = v.place(s, i_row);
-  const bool busy = 32 * wave < v.ng;                        // the wave has rows
   const int wpa = v.place(s, min(32 * wave, v.ng - 1)), wpb = v.place(s, min(32 * wave + 31, v.ng - 1));
   u32x4 qf[KS];
   float c2 = s.scale_log2e;
@@ -79,60 +79,77 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
     }
   }
 
-  // ---- tiles: lane i knows where the i-th tile of a batch of 64 lies
-  int x_page = 0, x_row = 0, x_row0 = 0, x_live = 0;
-  auto batch = [&](int first) {
-    const int t = first + lane, tile = v.tile(t), at = tile >> (s.lp - 5);
-    const int id = t < t1 ? page_at(s, c, u, at) : -1;
-    x_page = max(id, 0);
-    x_row0 = tile * 32;
-    x_row = x_row0 & (s.P - 1);
-    x_live = id >= 0 ? min(max(v.len - x_row0, 0), 32) : 0;
+  // ---- tiles, two at a time: lane i knows where the i-th of a batch of 64 lies
+  struct Pair { int row0[2], live[2], page[2]; };
+  int x_page = 0, x_row0 = 0, x_live = 0;
+  const int n = t1 - t0;
+  auto pair_at = [&](int i) __attribute__((always_inline)) {     // (asked for in order; behind the last one there are tiles without rows)
+    if ((i & 63) == 0) {
+      const int t = t0 + i + lane, tile = v.tile(t), id = t < t1 ? page_at(s, c, u, tile >> (s.lp - 5)) : -1;
+      x_page = max(id, 0);
+      x_row0 = tile * 32;
+      x_live = id >= 0 ? min(max(v.len - x_row0, 0), 32) : 0;
+    }
+    Pair p;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      p.row0[x] = __builtin_amdgcn_readlane(x_row0, (i & 63) + x);
+      p.live[x] = __builtin_amdgcn_readlane(x_live, (i & 63) + x);
+      p.page[x] = __builtin_amdgcn_readlane(x_page, (i & 63) + x);
+    }
+    return p;
   };
   const uint32_t img_a = lds_base_of(img);
-  // bf16: a wave fetches half of one tile's rows, directly.  4 bits: a thread's words and scales, turned into fp16 on their way.
+  auto key_image = [&](int to) { return img_a + to * KEYS; };
+  auto value_image = [&](int to) { return img_a + 2 * KEYS + to * IMG; };
+  // where the lane reads: the rest of an address is a constant
+  uint32_t k_at[KS], v_at[NB];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) k_at[k] = img_a + l32 * RB + ((2 * k + half) ^ tile_swz<MIXKV_BF16, D>(l32)) * 16;
+#pragma unroll
+  for (int blk = 0; blk < NB; ++blk) {
+    const int l16 = lane & 15, sub = (lane >> 4) & 1, r = 4 * half + (l16 >> 2);       // (the rows that are 8 and 16 further have the same rotation)
+    v_at[blk] = img_a + 2 * KEYS + (Q4 ? (half * D + 32 * blk + l32) * 16 : r * RB + ((4 * blk + 2 * sub + ((l16 & 3) >> 1)) ^ value_swz<D>(r)) * 16 + (l16 & 1) * 8);
+  }
+  const int side = wave / (W / 2);                           // which of the two tiles the wave fetches
+
+  // bf16: a wave fetches 16 rows of one tile, directly
+  auto fetch = [&](const Pair &p, bool values, uint32_t to) __attribute__((always_inline)) {
+    constexpr int RPL = 64 / PPR, LOADS = 16 / RPL;          // rows of a load, loads of a wave
+    const int r0 = 16 * (wave & 1);
+    const char *base = (values ? c.V : c.K) + (int64_t)(side ? p.page[1] : p.page[0]) * s.page_bytes + (int64_t)(((side ? p.row0[1] : p.row0[0]) & (s.P - 1)) + r0) * RB;
+    const uint32_t dst = to + side * TILE + r0 * RB;
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int r = r0 + j * RPL + lane / PPR, sw = values ? value_swz<D>(r) : tile_swz<MIXKV_BF16, D>(r);
+      load_to_lds<false>(base + (uint32_t)((j * RPL + lane / PPR) * RB + ((lane % PPR) ^ sw) * 16), dst + j * 1024);
+    }
+  };
+  // 4 bits: a thread's words and scales of a tile, then in fp16 into the images.  The thread's key row, run and words of it; the values' strip, words
+  // 64 vj + 4 vm + 2 vh + (0, 1) of it
   constexpr int NG = D / 32, VT = 2 * D;                     // groups of a row; threads with values of a tile
+  const int r256 = tid & 255, krow = r256 >> 3, krun = (r256 >> 1) & 3, kpl = (r256 & 1) * (NG / 2);
+  const int vq = r256 / (VT / 4), vj = r256 % (VT / 4) >> 5, vm = (r256 >> 1) & 15, vh = r256 & 1, codes = s.P * (D / 2);
   uint32_t kw[NG / 2], ksb[NG / 2];
   u32x2 vw;
   u32x4 vst, vba;
-  const int side = wave / (W / 2);                           // which of the two tiles
-  // 4 bits: the thread's key row, run and words of it; the values' strip, words 64 vj + 4 vm + 2 vh + (0, 1) of it
-  const int r256 = tid & 255, krow = r256 >> 3, krun = (r256 >> 1) & 3, kpl = (r256 & 1) * (NG / 2);
-  const int vq = r256 / (VT / 4), vj = r256 % (VT / 4) >> 5, vm = (r256 >> 1) & 15, vh = r256 & 1;
-  auto request = [&](int i, int to) {                        // tiles i and i + 1 of the batch
-    const int64_t page = (int64_t)__builtin_amdgcn_readlane(x_page, i + side) * s.page_bytes;
-    const int row = __builtin_amdgcn_readlane(x_row, i + side);
-    if constexpr (!Q4) {
-      constexpr int RPL = 64 / PPR, LOADS = 16 / RPL;        // rows of a load, loads of a wave
+  auto ask_keys = [&](const Pair &p) __attribute__((always_inline)) {
+    const char *kp = c.K + (int64_t)(side ? p.page[1] : p.page[0]) * s.page_bytes;
+    const int row = ((side ? p.row0[1] : p.row0[0]) & (s.P - 1)) + krow;
+    const uint32_t *kc = reinterpret_cast<const uint32_t *>(kp + row * (D / 2) + krun * (NG * 4)) + kpl, *kz = reinterpret_cast<const uint32_t *>(kp + codes + row * (NG * 4)) + kpl;
 #pragma unroll
-      for (int kv = 0; kv < 2; ++kv) {
-        const char *base = (kv ? c.V : c.K) + page + (int64_t)(row + 16 * (wave & 1)) * RB;
-        const uint32_t dst = img_a + to * TURN + kv * IMG + side * TILE + (wave & 1) * (16 * RB);
-#pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
-          const int r = 16 * (wave & 1) + j * RPL + lane / PPR, sw = kv ? value_swz<D>(r) : tile_swz<MIXKV_BF16, D>(r);
-          load_to_lds<false>(base + (uint32_t)((j * RPL + lane / PPR) * RB + ((lane % PPR) ^ sw) * 16), dst + j * 1024);
-        }
-      }
-    } else {
-      const char *kp = c.K + page, *vp = c.V + page;
-      const int codes = s.P * (D / 2);
-      const uint32_t *kc = reinterpret_cast<const uint32_t *>(kp + (row + krow) * (D / 2) + krun * (NG * 4)) + kpl;
-      const uint32_t *kz = reinterpret_cast<const uint32_t *>(kp + codes + (row + krow) * (NG * 4)) + kpl;
-#pragma unroll
-      for (int g = 0; g < NG / 2; ++g) { kw[g] = kc[g]; ksb[g] = kz[g]; }
-      if (VT == 256 || r256 < VT) {
-        const int strip = (row >> 5) * 4 + vq;
-        vw = *reinterpret_cast<const u32x2 *>(vp + (strip * D + 64 * vj + 4 * vm + 2 * vh) * 4);
-        const char *z = vp + codes + (strip * NG + 2 * vj + vh) * 32;
-        vst = *reinterpret_cast<const u32x4 *>(z);
-        vba = *reinterpret_cast<const u32x4 *>(z + 16);
-      }
-    }
+    for (int g = 0; g < NG / 2; ++g) { kw[g] = kc[g]; ksb[g] = kz[g]; }
   };
-  // 4 bits: what was requested, in fp16, into an image; rows that do not exist are zeros among the values
-  auto unpack = [&](int live, int to) {
-    const uint32_t k_a = img_a + to * TURN + side * TILE, v_a = k_a + IMG, l_a = v_a + IMG;
+  auto ask_values = [&](const Pair &p) __attribute__((always_inline)) {
+    if (VT < 256 && r256 >= VT) return;
+    const char *vp = c.V + (int64_t)(side ? p.page[1] : p.page[0]) * s.page_bytes;
+    const int strip = (((side ? p.row0[1] : p.row0[0]) & (s.P - 1)) >> 5) * 4 + vq;
+    vw = *reinterpret_cast<const u32x2 *>(vp + (strip * D + 64 * vj + 4 * vm + 2 * vh) * 4);
+    const char *z = vp + codes + (strip * NG + 2 * vj + vh) * 32;
+    vst = *reinterpret_cast<const u32x4 *>(z);
+    vba = *reinterpret_cast<const u32x4 *>(z + 16);
+  };
+  auto unpack_keys = [&](uint32_t to) __attribute__((always_inline)) {
 #pragma unroll
     for (int g = 0; g < NG / 2; ++g) {
       const int pl = kpl + g, piece = 4 * (D == 128 ? (pl & 1) * 2 + (pl >> 1) : pl) + krun;
@@ -144,26 +161,77 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
         hi[j] = __builtin_bit_cast(uint32_t, x);
         lo[j] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)(fmaf((float)un[0], (float)sb[0], (float)sb[1]) - (float)x[0]), (_Float16)(fmaf((float)un[1], (float)sb[0], (float)sb[1]) - (float)x[1])});
       }
-      const uint32_t at = krow * RB + (piece ^ tile_swz<MIXKV_BF16, D>(krow)) * 16;
-      store_lds(k_a + at, hi);
-      store_lds(l_a + at, lo);
+      const uint32_t at = to + side * TILE + krow * RB + (piece ^ tile_swz<MIXKV_BF16, D>(krow)) * 16;
+      store_lds(at, hi);
+      store_lds(at + IMG, lo);
     }
-    if (VT == 256 || r256 < VT) {
+  };
+  auto unpack_values = [&](const Pair &p, uint32_t to) __attribute__((always_inline)) {      // rows that do not exist: zeros
+    if (VT < 256 && r256 >= VT) return;
+    const int live = (side ? p.live[1] : p.live[0]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t on = (4 * vq + j < live ? 0xffffu : 0u) | (16 + 4 * vq + j < live ? 0xffff0000u : 0u);
+      vst[j] &= on;
+      vba[j] &= on;
+    }
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      u32x4 x;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        x[j] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(code_pair(vw[w], j), __builtin_bit_cast(f16x2, (uint32_t)vst[j]), __builtin_bit_cast(f16x2, (uint32_t)vba[j])));
+      store_lds(to + side * TILE + (vq * D + 64 * vj + 16 * (2 * vh + w) + vm) * 16, x);
+    }
+  };
+
+  // ---- scores of 32 keys: register e is key 8 (e / 4) + 4 half + e % 4.  (4 bits: the keys in two parts, so that a logit is off by no more than fp32 makes it, as
+  // lse and weights have to be)
+  auto scores = [&](int at0) __attribute__((always_inline)) {
+    f32x16 acc;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const uint32_t at = k_at[k] + at0;
+      const u32x4 kf = lds_vec(at);
+      if constexpr (Q4) {
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lds_vec(at + IMG)), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kf), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
+      } else {
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[k]), acc, 0, 0, 0);
+      }
+    }
+    return acc;
+  };
+  // ---- the values of 16 keys and 32 elements as the second product's first operand
+  auto value = [&](int at0, int k, int blk) __attribute__((always_inline)) {
+    if constexpr (Q4) {
+      return lds_vec(v_at[blk] + at0 + 2 * k * D * 16);
+    } else {
+      const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(v_at[blk] + at0 + 16 * k * RB));
+      const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(v_at[blk] + at0 + (16 * k + 8) * RB));
+      return __builtin_bit_cast(u32x4, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  };
+  auto product = [&](u32x4 vf, u32x4 pf, f32x16 acc) __attribute__((always_inline)) {
+    if constexpr (Q4) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, vf), __builtin_bit_cast(f16x8, pf), acc, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pf), acc, 0, 0, 0);
+  };
+
+  // ---- weights of 32 keys against an offset, as the second product's second operand; their sum
+  auto weigh = [&](const f32x16 &x, float off, u32x4 (&pw)[2]) __attribute__((always_inline)) {
+    float total = 0.f;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint32_t on = (4 * vq + j < live ? 0xffffu : 0u) | (16 + 4 * vq + j < live ? 0xffff0000u : 0u);
-        vst[j] &= on;
-        vba[j] &= on;
+        const int e0 = Q4 ? 4 * k + j : 8 * k + 2 * j, e1 = Q4 ? 8 + 4 * k + j : e0 + 1;
+        const float p0 = fast_exp2(fmaf(x[e0], c2, -off)), p1 = fast_exp2(fmaf(x[e1], c2, -off));
+        total += p0 + p1;
+        pw[k][j] = Q4 ? __builtin_bit_cast(uint32_t, f16x2{(_Float16)p0, (_Float16)p1}) : __builtin_bit_cast(uint32_t, bf16x2{(__bf16)p0, (__bf16)p1});
       }
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        u32x4 x;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          x[j] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(code_pair(vw[w], j), __builtin_bit_cast(f16x2, (uint32_t)vst[j]), __builtin_bit_cast(f16x2, (uint32_t)vba[j])));
-        store_lds(v_a + (vq * D + 64 * vj + 16 * (2 * vh + w) + vm) * 16, x);
-      }
-    }
+    return total;
   };
 
   f32x16 o[NB];
@@ -173,146 +241,132 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
     for (int e = 0; e < 16; ++e) o[k][e] = 0.f;
   float m = -INFINITY, sum = 0.f;                            // the row's offset, this lane's share of its sum of weights
 
-  const int n = t1 - t0;
-  batch(t0);
-  request(0, 0);
-  if constexpr (Q4) unpack(__builtin_amdgcn_readlane(x_live, side), 0);
-  for (int i = 0; i < n; i += 2) {
-    const int at = i & 63, to = (i >> 1) & 1;
+  Pair cur = pair_at(0);
+  if constexpr (Q4) {
+    ask_keys(cur);
+    ask_values(cur);
+    unpack_keys(key_image(0));
+    unpack_values(cur, value_image(0));
+  } else {
+    fetch(cur, false, key_image(0));
+    fetch(cur, true, value_image(0));
+  }
+  auto turn_of = [&](int i, auto turn_c) __attribute__((always_inline)) {
+    constexpr int to = decltype(turn_c)::value;
     if constexpr (!Q4) wait_vm<0>();
     lds_barrier();
-    const int row0[2] = {__builtin_amdgcn_readlane(x_row0, at), __builtin_amdgcn_readlane(x_row0, at + 1)};
-    const int live[2] = {__builtin_amdgcn_readlane(x_live, at), __builtin_amdgcn_readlane(x_live, at + 1)};
-    const int page[2] = {__builtin_amdgcn_readlane(x_page, at), __builtin_amdgcn_readlane(x_page, at + 1)};
-    int next_live = 0;
+    const Pair nxt = pair_at(i + 2);
     if (i + 2 < n) {
-      if (((i + 2) & 63) == 0) batch(t0 + i + 2);
-      request((i + 2) & 63, to ^ 1);
-      next_live = __builtin_amdgcn_readlane(x_live, ((i + 2) & 63) + side);
-    }
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      if (!busy) continue;
-      const int r0 = row0[x];
-      if (live[x] == 0 || r0 > wpb || (r0 + 31 <= wpa - a.w.window && r0 >= a.w.first)) continue;
-      const bool whole = live[x] == 32 && r0 + 31 <= wpa && (r0 > wpb - a.w.window || r0 + 31 < a.w.first);
-      // ---- scores
-      f32x16 acc;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-      const uint32_t k_a = img_a + to * TURN + x * TILE, v_a = k_a + IMG;
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        const u32x4 kf = lds_vec(k_a + l32 * RB + ((2 * k + half) ^ tile_swz<MIXKV_BF16, D>(l32)) * 16);
-        if constexpr (Q4) {                                  // (the keys in two parts: a logit is off by no more than fp32 makes it, as lse and weights have to be)
-          const u32x4 lf = lds_vec(k_a + 2 * IMG + l32 * RB + ((2 * k + half) ^ tile_swz<MIXKV_BF16, D>(l32)) * 16);
-          acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lf), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
-          acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kf), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
-        } else acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[k]), acc, 0, 0, 0);
+      if constexpr (Q4) {
+        ask_keys(nxt);
+        ask_values(nxt);
+      } else {
+        fetch(nxt, false, key_image(to ^ 1));
+        fetch(nxt, true, value_image(to ^ 1));
       }
-      // ---- weights: register e is key 8 (e / 4) + 4 half + e % 4
-      if (!whole) {
+    }
+    f32x16 acc[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) acc[x] = scores(to * KEYS + x * TILE);
+    // ---- weights
+    bool whole = true;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) whole = whole && cur.live[x] == 32 && cur.row0[x] + 31 <= wpa && (cur.row0[x] > wpb - a.w.window || cur.row0[x] + 31 < a.w.first);
+    if (!whole) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int key = 8 * (e >> 2) + 4 * half + (e & 3);
-          acc[e] = key < live[x] && sees(a.w, place, r0 + key) ? acc[e] : -INFINITY;
+          acc[x][e] = key < cur.live[x] && sees(a.w, place, cur.row0[x] + key) ? acc[x][e] : -INFINITY;
         }
+    }
+    u32x4 pw[2][2];
+    float next = weigh(acc[0], m, pw[0]) + weigh(acc[1], m, pw[1]);
+    if (__builtin_amdgcn_ballot_w64(!((Q4 ? next : sum + next) < (Q4 ? kPromptSum16 : kPromptSum))) != 0) {
+      float t = -INFINITY;
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) t = fmaxf(t, acc[x][e]);
+      t = fmaxf(t, __shfl_xor(t, 32));
+      const float mn = fmaxf(m, t * c2 - (Q4 ? 8.f : 0.f)), mu = mn == -INFINITY ? 0.f : mn, f = fast_exp2(m - mu);
+      next = weigh(acc[0], mu, pw[0]) + weigh(acc[1], mu, pw[1]);
+      sum *= f;
+#pragma unroll
+      for (int k = 0; k < NB; ++k)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[k][e] *= f;
+      m = mn;
+    }
+    sum += next;
+    // ---- weighted values
+    // Values that are no numbers, in tiles that not all of the group's rows see all of: zeros in their places, and behind the product they themselves where
+    // their rows are seen.  A weight of zero does not make NaN of them.
+    bool mixed = false;
+    if constexpr (!Q4) {
+      bool all = true;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) all = all && cur.live[x] == 32 && cur.row0[x] + 31 <= v.pa && (cur.row0[x] > v.pb - a.w.window || cur.row0[x] + 31 < a.w.first);
+      if (!all) {
+        bool odd = false;
+#pragma unroll
+        for (int j = 0; j < IMG / (1024 * W); ++j) {
+          const uint32_t at = value_image(to) + (j * W + wave) * 1024 + lane * 16;
+          u32x4 w = lds_vec(at);
+          bool bad = false;
+#pragma unroll
+          for (int z = 0; z < 4; ++z) {
+            bad |= no_number<MIXKV_BF16>(w[z]);
+            w[z] = numbers_only<MIXKV_BF16>(w[z]);
+          }
+          if (bad) store_lds(at, w);
+          odd |= bad;
+        }
+        odd = __builtin_amdgcn_ballot_w64(odd) != 0;
+        if (lane == 0) odd_s[wave] = odd;
+        lds_barrier();
+#pragma unroll
+        for (int w = 0; w < W; ++w) mixed |= odd_s[w] != 0;
       }
-      float p[16], next = 0.f;
+    }
+    constexpr int v0 = to * IMG;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) { p[e] = fast_exp2(fmaf(acc[e], c2, -m)); next += p[e]; }
-      if (__builtin_amdgcn_ballot_w64(!((Q4 ? next : sum + next) < (Q4 ? kPromptSum16 : kPromptSum))) != 0) {
-        float t = acc[0];
-#pragma unroll
-        for (int e = 1; e < 16; ++e) t = fmaxf(t, acc[e]);
-        t = fmaxf(t, __shfl_xor(t, 32));
-        const float mn = fmaxf(m, t * c2 - (Q4 ? 8.f : 0.f)), mu = mn == -INFINITY ? 0.f : mn, f = fast_exp2(m - mu);
-        next = 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) { p[e] = fast_exp2(fmaf(acc[e], c2, -mu)); next += p[e]; }
-        sum *= f;
-#pragma unroll
-        for (int k = 0; k < NB; ++k)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[k][e] *= f;
-        m = mn;
-      }
-      sum += next;
-      // ---- weighted values
-      u32x4 pw[2];
+    for (int x = 0; x < 2; ++x)
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if constexpr (Q4) pw[k][j] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)p[4 * k + j], (_Float16)p[8 + 4 * k + j]});
-          else pw[k][j] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)p[8 * k + 2 * j], (__bf16)p[8 * k + 2 * j + 1]});
-        }
-      auto value = [&](int k, int blk) {
-        if constexpr (Q4) {
-          return lds_vec(v_a + ((2 * k + half) * D + 32 * blk + l32) * 16);
-        } else {
-          const int l16 = lane & 15, sub = (lane >> 4) & 1;
-          uint32_t at2[2];
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int r = 16 * k + 8 * j + 4 * half + (l16 >> 2);
-            at2[j] = v_a + r * RB + ((4 * blk + 2 * sub + ((l16 & 3) >> 1)) ^ value_swz<D>(r)) * 16 + (l16 & 1) * 8;
-          }
-          const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)at2[0]);
-          const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)at2[1]);
-          return __builtin_bit_cast(u32x4, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-        }
-      };
-      bool mixed = false;                                    // values that are no numbers, in a tile that not all of the wave's rows see all of
-      if constexpr (!Q4) {
-        if (!whole) {
-          bool odd = false;
-#pragma unroll
-          for (int j = 0; j < TILE / 1024; ++j) {
-            const u32x4 w = lds_vec(v_a + j * 1024 + lane * 16);
-#pragma unroll
-            for (int z = 0; z < 4; ++z) odd |= no_number<MIXKV_BF16>(w[z]);
-          }
-          mixed = __builtin_amdgcn_ballot_w64(odd) != 0;
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int blk = 0; blk < NB; ++blk) {
-          u32x4 vf = value(k, blk);
-          if constexpr (Q4) {
-            o[blk] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, vf), __builtin_bit_cast(f16x8, pw[k]), o[blk], 0, 0, 0);
-          } else {
-            if (mixed) {
-#pragma unroll
-              for (int z = 0; z < 4; ++z) vf[z] = numbers_only<MIXKV_BF16>(vf[z]);
-            }
-            o[blk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pw[k]), o[blk], 0, 0, 0);
-          }
-        }
-      if (mixed) {                                           // what went into the product as zeros, where its row is seen: a weight of zero does not make NaN of it
-        const char *from = c.V + (int64_t)page[x] * s.page_bytes + (int64_t)(r0 & (s.P - 1)) * RB;
+        for (int blk = 0; blk < NB; ++blk) o[blk] = product(value(v0 + x * TILE, k, blk), pw[x][k], o[blk]);
+    if (mixed) {
 #pragma unroll 1
-        for (int r = 0; r < live[x]; ++r) {
-          if (!sees(a.w, place, r0 + r)) continue;
+      for (int r = 0; r < 64; ++r) {
+        const int x = r >> 5, j = r & 31, r0 = x ? cur.row0[1] : cur.row0[0];
+        if (j >= (x ? cur.live[1] : cur.live[0]) || !sees(a.w, place, r0 + j)) continue;
+        const uint16_t *from = reinterpret_cast<const uint16_t *>(c.V + (int64_t)(x ? cur.page[1] : cur.page[0]) * s.page_bytes + (int64_t)((r0 & (s.P - 1)) + j) * RB);
 #pragma unroll
-          for (int blk = 0; blk < NB; ++blk)
+        for (int blk = 0; blk < NB; ++blk)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float y = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(from + r * RB)[32 * blk + 8 * (e >> 2) + 4 * half + (e & 3)] << 16);
-              if (no_number<MIXKV_F32>(__float_as_uint(y))) o[blk][e] += y;
-            }
-        }
+          for (int e = 0; e < 16; ++e) {
+            const float y = __uint_as_float((uint32_t)from[32 * blk + 8 * (e >> 2) + 4 * half + (e & 3)] << 16);
+            if (no_number<MIXKV_F32>(__float_as_uint(y))) o[blk][e] += y;
+          }
       }
     }
     if constexpr (Q4) {
-      if (i + 2 < n) unpack(next_live, to ^ 1);
+      if (i + 2 < n) {
+        unpack_keys(key_image(to ^ 1));
+        unpack_values(nxt, value_image(to ^ 1));
+      }
     }
+    cur = nxt;
+  };
+  for (int i = 0; i < n; i += 4) {
+    turn_of(i, std::integral_constant<int, 0>{});
+    if (i + 2 < n) turn_of(i + 2, std::integral_constant<int, 1>{});
   }
 
   // ---- lane (row, half) has the elements 32 blk + 8 (e / 4) + 4 half + e % 4
-  if (!busy || mine >= v.ng) return;
+  if (mine >= v.ng) return;
   sum += __shfl_xor(sum, 32);
   if (a.nchunks > 1) {
     const int64_t slot = (((unit0 + (int64_t)layer * units + u) * a.qtiles + turn) * a.nchunks + ch) * R + mine;
