@@ -16,6 +16,7 @@ constexpr int prompt_waves(bool q4) { return q4 ? 8 : 4; }
 constexpr int prompt_rows(bool q4) { return 32 * prompt_waves(q4); }
 // bf16 weights: a lane's sum of weights that reaches this moves the row's offset (the weighted values stay below it times the largest value).  fp16 weights: a
 // tile's sum of weights in a lane does, and the offset puts the largest weight at 2^8: fp16 then resolves weights down to 2^-32 of it.
+constexpr int kNowhere = 1 << 30;        // no head has so many rows
 constexpr float kPromptSum = 0x1p20f, kPromptSum16 = 0x1p14f;
 
 struct PromptShape {
@@ -33,6 +34,8 @@ __device__ __forceinline__ f16x2 code_pair(uint32_t w, int i) {
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 __device__ __forceinline__ u32x4 lds_vec(uint32_t at) { return *(const lds_u32x4 *)(uintptr_t)at; }
+// Four rows' elements, transposed.  (A parameter that is said to alias nothing: otherwise the compiler waits for every load on its way to LDS first.)
+__device__ __forceinline__ s16x4 read_transposed(lds_s16x4 *__restrict p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16(p); }
 __device__ __forceinline__ void store_lds(uint32_t at, u32x4 x) { *(lds_u32x4 *)(uintptr_t)at = x; }
 
 template <int D, bool Q4>
@@ -79,26 +82,30 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
     }
   }
 
-  // ---- tiles, two at a time: lane i knows where the i-th of a batch of 64 lies
-  struct Pair { int row0[2], live[2], page[2]; };
-  int x_page = 0, x_row0 = 0, x_live = 0;
+  // ---- tiles, two at a time: lane i knows where the i-th of a batch of 64 lies.  One that does not exist lies behind everything that is seen.
+  struct Pair { int row0[2], page[2]; };
+  int x_page = 0, x_row0 = 0;
   const int n = t1 - t0;
-  auto pair_at = [&](int i) __attribute__((always_inline)) {     // (asked for in order; behind the last one there are tiles without rows)
+  auto pair_at = [&](int i) __attribute__((always_inline)) {     // (asked for in order)
     if ((i & 63) == 0) {
       const int t = t0 + i + lane, tile = v.tile(t), id = t < t1 ? page_at(s, c, u, tile >> (s.lp - 5)) : -1;
       x_page = max(id, 0);
-      x_row0 = tile * 32;
-      x_live = id >= 0 ? min(max(v.len - x_row0, 0), 32) : 0;
+      x_row0 = id >= 0 ? tile * 32 : kNowhere;
     }
     Pair p;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       p.row0[x] = __builtin_amdgcn_readlane(x_row0, (i & 63) + x);
-      p.live[x] = __builtin_amdgcn_readlane(x_live, (i & 63) + x);
       p.page[x] = __builtin_amdgcn_readlane(x_page, (i & 63) + x);
     }
     return p;
   };
+  // tiles that all of the wave's rows see all of, and all of the group's
+  const int w_hi = wpa - 31, w_lo = wpb - a.w.window, g_hi = v.pa - 31, g_lo = v.pb - a.w.window, f_lo = a.w.first - 31;
+  const int behind = place - a.w.window, first = a.w.first;
+  const char *const K = c.K, *const V = c.V;
+  const int64_t page_bytes = s.page_bytes;
+  const int in_page = s.P - 1;
   const uint32_t img_a = lds_base_of(img);
   auto key_image = [&](int to) { return img_a + to * KEYS; };
   auto value_image = [&](int to) { return img_a + 2 * KEYS + to * IMG; };
@@ -113,16 +120,23 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
   }
   const int side = wave / (W / 2);                           // which of the two tiles the wave fetches
 
-  // bf16: a wave fetches 16 rows of one tile, directly
-  auto fetch = [&](const Pair &p, bool values, uint32_t to) __attribute__((always_inline)) {
-    constexpr int RPL = 64 / PPR, LOADS = 16 / RPL;          // rows of a load, loads of a wave
-    const int r0 = 16 * (wave & 1);
-    const char *base = (values ? c.V : c.K) + (int64_t)(side ? p.page[1] : p.page[0]) * s.page_bytes + (int64_t)(((side ? p.row0[1] : p.row0[0]) & (s.P - 1)) + r0) * RB;
-    const uint32_t dst = to + side * TILE + r0 * RB;
+  // bf16: a wave fetches 16 rows of one tile, directly: the lane's place in what each load takes
+  constexpr int RPL = 64 / PPR, LOADS = 16 / RPL;            // rows of a load, loads of a wave
+  const int f_row = 16 * (wave & 1);
+  uint32_t f_at[2][LOADS];
+#pragma unroll
+  for (int j = 0; j < LOADS; ++j) {
+    const int r = j * RPL + lane / PPR;                      // (the rows 16 further have the same rotations)
+    f_at[0][j] = r * RB + ((lane % PPR) ^ tile_swz<MIXKV_BF16, D>(r)) * 16;
+    f_at[1][j] = r * RB + ((lane % PPR) ^ value_swz<D>(r)) * 16;
+  }
+  auto fetch = [&](const Pair &p, int values, uint32_t to) __attribute__((always_inline)) {
+    const char *base = (values ? V : K) + (int64_t)(side ? p.page[1] : p.page[0]) * page_bytes + (((side ? p.row0[1] : p.row0[0]) & in_page) + f_row) * RB;
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
-      const int r = r0 + j * RPL + lane / PPR, sw = values ? value_swz<D>(r) : tile_swz<MIXKV_BF16, D>(r);
-      load_to_lds<false>(base + (uint32_t)((j * RPL + lane / PPR) * RB + ((lane % PPR) ^ sw) * 16), dst + j * 1024);
+      uint32_t at = f_at[values][j];
+      asm("" : "+v"(at));                                    // 32 bits beside a scalar base
+      load_to_lds<false>(base + at, to + side * TILE + f_row * RB + j * 1024);
     }
   };
   // 4 bits: a thread's words and scales of a tile, then in fp16 into the images.  The thread's key row, run and words of it; the values' strip, words
@@ -134,16 +148,16 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
   u32x2 vw;
   u32x4 vst, vba;
   auto ask_keys = [&](const Pair &p) __attribute__((always_inline)) {
-    const char *kp = c.K + (int64_t)(side ? p.page[1] : p.page[0]) * s.page_bytes;
-    const int row = ((side ? p.row0[1] : p.row0[0]) & (s.P - 1)) + krow;
+    const char *kp = K + (int64_t)(side ? p.page[1] : p.page[0]) * page_bytes;
+    const int row = ((side ? p.row0[1] : p.row0[0]) & in_page) + krow;
     const uint32_t *kc = reinterpret_cast<const uint32_t *>(kp + row * (D / 2) + krun * (NG * 4)) + kpl, *kz = reinterpret_cast<const uint32_t *>(kp + codes + row * (NG * 4)) + kpl;
 #pragma unroll
     for (int g = 0; g < NG / 2; ++g) { kw[g] = kc[g]; ksb[g] = kz[g]; }
   };
   auto ask_values = [&](const Pair &p) __attribute__((always_inline)) {
     if (VT < 256 && r256 >= VT) return;
-    const char *vp = c.V + (int64_t)(side ? p.page[1] : p.page[0]) * s.page_bytes;
-    const int strip = (((side ? p.row0[1] : p.row0[0]) & (s.P - 1)) >> 5) * 4 + vq;
+    const char *vp = V + (int64_t)(side ? p.page[1] : p.page[0]) * page_bytes;
+    const int strip = (((side ? p.row0[1] : p.row0[0]) & in_page) >> 5) * 4 + vq;
     vw = *reinterpret_cast<const u32x2 *>(vp + (strip * D + 64 * vj + 4 * vm + 2 * vh) * 4);
     const char *z = vp + codes + (strip * NG + 2 * vj + vh) * 32;
     vst = *reinterpret_cast<const u32x4 *>(z);
@@ -168,7 +182,7 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
   };
   auto unpack_values = [&](const Pair &p, uint32_t to) __attribute__((always_inline)) {      // rows that do not exist: zeros
     if (VT < 256 && r256 >= VT) return;
-    const int live = (side ? p.live[1] : p.live[0]);
+    const int live = v.len - (side ? p.row0[1] : p.row0[0]);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const uint32_t on = (4 * vq + j < live ? 0xffffu : 0u) | (16 + 4 * vq + j < live ? 0xffff0000u : 0u);
@@ -187,30 +201,42 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
 
   // ---- scores of 32 keys: register e is key 8 (e / 4) + 4 half + e % 4.  (4 bits: the keys in two parts, so that a logit is off by no more than fp32 makes it, as
   // lse and weights have to be)
-  auto scores = [&](int at0) __attribute__((always_inline)) {
-    f32x16 acc;
+  auto scores = [&](int at0, f32x16 (&acc)[2]) __attribute__((always_inline)) {
+    constexpr int AHEAD = Q4 ? KS / 2 : KS;                  // reads under way before the first product
+    constexpr int N = 2 * KS;
+    u32x4 kf[AHEAD], lf[Q4 ? AHEAD : 1];
+    auto read = [&](int i) __attribute__((always_inline)) {
+      const uint32_t at = k_at[i % KS] + at0 + i / KS * TILE;
+      kf[i % AHEAD] = lds_vec(at);
+      if constexpr (Q4) lf[i % AHEAD] = lds_vec(at + IMG);
+    };
 #pragma unroll
-    for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+    for (int i = 0; i < AHEAD; ++i) read(i);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      const uint32_t at = k_at[k] + at0;
-      const u32x4 kf = lds_vec(at);
-      if constexpr (Q4) {
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lds_vec(at + IMG)), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kf), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
-      } else {
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[k]), acc, 0, 0, 0);
+    for (int i = 0; i < N; ++i) {
+      const int x = i / KS, k = i % KS;
+      if (k == 0) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[x][e] = 0.f;
       }
+      if constexpr (Q4) {
+        acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lf[i % AHEAD]), __builtin_bit_cast(f16x8, qf[k]), acc[x], 0, 0, 0);
+        acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kf[i % AHEAD]), __builtin_bit_cast(f16x8, qf[k]), acc[x], 0, 0, 0);
+      } else {
+        acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[i % AHEAD]), __builtin_bit_cast(bf16x8, qf[k]), acc[x], 0, 0, 0);
+      }
+      if (i + AHEAD < N) read(i + AHEAD);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    return acc;
   };
   // ---- the values of 16 keys and 32 elements as the second product's first operand
   auto value = [&](int at0, int k, int blk) __attribute__((always_inline)) {
     if constexpr (Q4) {
       return lds_vec(v_at[blk] + at0 + 2 * k * D * 16);
     } else {
-      const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(v_at[blk] + at0 + 16 * k * RB));
-      const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(v_at[blk] + at0 + (16 * k + 8) * RB));
+      const s16x4 v0 = read_transposed((lds_s16x4 *)(uintptr_t)(v_at[blk] + at0 + 16 * k * RB));
+      const s16x4 v1 = read_transposed((lds_s16x4 *)(uintptr_t)(v_at[blk] + at0 + (16 * k + 8) * RB));
       return __builtin_bit_cast(u32x4, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
     }
   };
@@ -248,66 +274,29 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
     unpack_keys(key_image(0));
     unpack_values(cur, value_image(0));
   } else {
-    fetch(cur, false, key_image(0));
-    fetch(cur, true, value_image(0));
+    fetch(cur, 0, key_image(0));
+    fetch(cur, 1, value_image(0));
   }
   auto turn_of = [&](int i, auto turn_c) __attribute__((always_inline)) {
     constexpr int to = decltype(turn_c)::value;
     if constexpr (!Q4) wait_vm<0>();
     lds_barrier();
+    const int r0 = cur.row0[0], r1 = cur.row0[1];
     const Pair nxt = pair_at(i + 2);
     if (i + 2 < n) {
       if constexpr (Q4) {
         ask_keys(nxt);
         ask_values(nxt);
       } else {
-        fetch(nxt, false, key_image(to ^ 1));
-        fetch(nxt, true, value_image(to ^ 1));
+        fetch(nxt, 0, key_image(to ^ 1));
+        fetch(nxt, 1, value_image(to ^ 1));
       }
     }
-    f32x16 acc[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) acc[x] = scores(to * KEYS + x * TILE);
-    // ---- weights
-    bool whole = true;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) whole = whole && cur.live[x] == 32 && cur.row0[x] + 31 <= wpa && (cur.row0[x] > wpb - a.w.window || cur.row0[x] + 31 < a.w.first);
-    if (!whole) {
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int key = 8 * (e >> 2) + 4 * half + (e & 3);
-          acc[x][e] = key < cur.live[x] && sees(a.w, place, cur.row0[x] + key) ? acc[x][e] : -INFINITY;
-        }
-    }
-    u32x4 pw[2][2];
-    float next = weigh(acc[0], m, pw[0]) + weigh(acc[1], m, pw[1]);
-    if (__builtin_amdgcn_ballot_w64(!((Q4 ? next : sum + next) < (Q4 ? kPromptSum16 : kPromptSum))) != 0) {
-      float t = -INFINITY;
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) t = fmaxf(t, acc[x][e]);
-      t = fmaxf(t, __shfl_xor(t, 32));
-      const float mn = fmaxf(m, t * c2 - (Q4 ? 8.f : 0.f)), mu = mn == -INFINITY ? 0.f : mn, f = fast_exp2(m - mu);
-      next = weigh(acc[0], mu, pw[0]) + weigh(acc[1], mu, pw[1]);
-      sum *= f;
-#pragma unroll
-      for (int k = 0; k < NB; ++k)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[k][e] *= f;
-      m = mn;
-    }
-    sum += next;
-    // ---- weighted values
     // Values that are no numbers, in tiles that not all of the group's rows see all of: zeros in their places, and behind the product they themselves where
     // their rows are seen.  A weight of zero does not make NaN of them.
     bool mixed = false;
     if constexpr (!Q4) {
-      bool all = true;
-#pragma unroll
-      for (int x = 0; x < 2; ++x) all = all && cur.live[x] == 32 && cur.row0[x] + 31 <= v.pa && (cur.row0[x] > v.pb - a.w.window || cur.row0[x] + 31 < a.w.first);
+      const bool all = (r0 <= g_hi) & ((r0 > g_lo) | (r0 < f_lo)) & (r1 <= g_hi) & ((r1 > g_lo) | (r1 < f_lo));
       if (!all) {
         bool odd = false;
 #pragma unroll
@@ -330,19 +319,65 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
         for (int w = 0; w < W; ++w) mixed |= odd_s[w] != 0;
       }
     }
+    f32x16 acc[2];
+    scores(to * KEYS, acc);
+    // (bf16) the first tile's values, on their way while the weights are formed
     constexpr int v0 = to * IMG;
+    u32x4 vf[2][NB];
+    if constexpr (!Q4) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int blk = 0; blk < NB; ++blk) vf[k][blk] = value(v0, k, blk);
+    }
+    // ---- weights
+    const bool whole = (r0 <= w_hi) & ((r0 > w_lo) | (r0 < f_lo)) & (r1 <= w_hi) & ((r1 > w_lo) | (r1 < f_lo));
+    if (!whole) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int j = (x ? r1 : r0) + 8 * (e >> 2) + 4 * half + (e & 3);
+          acc[x][e] = (j <= place) & ((j > behind) | (j < first)) ? acc[x][e] : -INFINITY;
+          __builtin_amdgcn_sched_barrier(0);                 // (one after another: side by side they take more scalar registers than there are)
+        }
+    }
+    u32x4 pw[2][2];
+    float next = weigh(acc[0], m, pw[0]) + weigh(acc[1], m, pw[1]);
+    if (__builtin_amdgcn_ballot_w64(!((Q4 ? next : sum + next) < (Q4 ? kPromptSum16 : kPromptSum))) != 0) {
+      float t = -INFINITY;
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) t = fmaxf(t, acc[x][e]);
+      t = fmaxf(t, __shfl_xor(t, 32));
+      const float mn = fmaxf(m, t * c2 - (Q4 ? 8.f : 0.f)), mu = mn == -INFINITY ? 0.f : mn, f = fast_exp2(m - mu);
+      next = weigh(acc[0], mu, pw[0]) + weigh(acc[1], mu, pw[1]);
+      sum *= f;
+#pragma unroll
+      for (int k = 0; k < NB; ++k)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[k][e] *= f;
+      m = mn;
+    }
+    sum += next;
+    // ---- weighted values
 #pragma unroll
     for (int x = 0; x < 2; ++x)
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int blk = 0; blk < NB; ++blk) o[blk] = product(value(v0 + x * TILE, k, blk), pw[x][k], o[blk]);
+        for (int blk = 0; blk < NB; ++blk) {
+          o[blk] = product(Q4 ? value(v0 + x * TILE, k, blk) : vf[k][blk], pw[x][k], o[blk]);
+          if (!Q4 && x == 0) vf[k][blk] = value(v0 + TILE, k, blk);
+          if constexpr (!Q4) __builtin_amdgcn_sched_barrier(0);
+        }
     if (mixed) {
 #pragma unroll 1
       for (int r = 0; r < 64; ++r) {
-        const int x = r >> 5, j = r & 31, r0 = x ? cur.row0[1] : cur.row0[0];
-        if (j >= (x ? cur.live[1] : cur.live[0]) || !sees(a.w, place, r0 + j)) continue;
-        const uint16_t *from = reinterpret_cast<const uint16_t *>(c.V + (int64_t)(x ? cur.page[1] : cur.page[0]) * s.page_bytes + (int64_t)((r0 & (s.P - 1)) + j) * RB);
+        const int j = (r < 32 ? r0 : r1) + (r & 31);
+        if (!sees(a.w, place, j)) continue;
+        const uint16_t *from = reinterpret_cast<const uint16_t *>(V + page_at(s, c, u, j >> s.lp) * page_bytes + (j & in_page) * RB);
 #pragma unroll
         for (int blk = 0; blk < NB; ++blk)
 #pragma unroll
