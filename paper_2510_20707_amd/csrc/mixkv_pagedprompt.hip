@@ -1,6 +1,6 @@
 // Attention of many new rows (prompts, chunks of them) over the pages of a cache: mixkv_paged_window_attention where a unit has more rows than a few.
 //
-// A workgroup has 128 or 256 rows of a unit (new rows times the G query heads of a KV head, row i being query head i % G of new row i / G, so that a tile of
+// A workgroup has kPromptRows rows of a unit (new rows times the G query heads of a KV head, row i being query head i % G of new row i / G, so that a tile of
 // keys serves all of them), a wave 32 of them, and goes through the 32-row tiles that they see, two at a time, which travel through LDS.
 //   * Scores: S' = K Q', keys on the output rows of 32 x 32 x 16 products: a lane has 16 keys of one row, its neighbour 32 lanes on the other 16, so that the
 //     softmax stays in the lane.
@@ -11,9 +11,7 @@
 
 namespace mixkv {
 
-// Waves of a workgroup.  4-bit tiles are turned into fp16 once for all of its rows, and take half as much of LDS again.
-constexpr int prompt_waves(bool q4) { return q4 ? 8 : 4; }
-constexpr int prompt_rows(bool q4) { return 32 * prompt_waves(q4); }
+constexpr int kPromptWaves = 8, kPromptRows = 32 * kPromptWaves;
 // bf16 weights: a lane's sum of weights that reaches this moves the row's offset (the weighted values stay below it times the largest value).  fp16 weights: a
 // tile's sum of weights in a lane does, and the offset puts the largest weight at 2^8: fp16 then resolves weights down to 2^-32 of it.
 constexpr int kNowhere = 1 << 30;        // no head has so many rows
@@ -38,9 +36,13 @@ __device__ __forceinline__ u32x4 lds_vec(uint32_t at) { return *(const lds_u32x4
 __device__ __forceinline__ s16x4 read_transposed(lds_s16x4 *__restrict p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16(p); }
 __device__ __forceinline__ void store_lds(uint32_t at, u32x4 x) { *(lds_u32x4 *)(uintptr_t)at = x; }
 
+// Rotation of the 16-byte pieces of a value row: half a wave reads two pieces of four neighbouring rows at two places (those of 32 bytes further).
+template <int D>
+__device__ __forceinline__ int read_swz(int r) { return D == 128 ? (4 * r) & 15 : (2 * r) & 4; }
+
 template <int D, bool Q4>
-__global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(PShape s, PromptShape a, WinTable tab, float *part, float *part_ml, int64_t unit0) {
-  constexpr int RB = D * 2, PPR = RB / 16, KS = D / 16, NB = D / 32, W = prompt_waves(Q4), R = prompt_rows(Q4);
+__global__ __launch_bounds__(64 * kPromptWaves, 2) void paged_prompt_kernel(PShape s, PromptShape a, WinTable tab, float *part, float *part_ml, int64_t unit0) {
+  constexpr int RB = D * 2, PPR = RB / 16, KS = D / 16, NB = D / 32, W = kPromptWaves, R = kPromptRows;
   constexpr int TILE = 32 * RB, IMG = 2 * TILE;              // a tile of 32 rows; two of them
   constexpr int KEYS = (Q4 ? 2 : 1) * IMG;                   // keys' tiles, and (4 bits) behind them what their elements lack in fp16
   __shared__ __align__(16) char img[2 * KEYS + 2 * IMG];
@@ -58,7 +60,6 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
 
   // ---- the lane's row: its query as the second operand, and its place
   const int mine = 32 * wave + l32, i_row = min(mine, v.ng - 1), place = v.place(s, i_row);
-  const int wpa = v.place(s, min(32 * wave, v.ng - 1)), wpb = v.place(s, min(32 * wave + 31, v.ng - 1));
   u32x4 qf[KS];
   float c2 = s.scale_log2e;
   {
@@ -82,30 +83,35 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
     }
   }
 
-  // ---- tiles, two at a time: lane i knows where the i-th of a batch of 64 lies.  One that does not exist lies behind everything that is seen.
-  struct Pair { int row0[2], page[2]; };
-  int x_page = 0, x_row0 = 0;
+  // ---- tiles, two at a time: lane i knows where the i-th of a batch of 64 lies, and whether all of the group's rows see all of it.  One that does not exist lies
+  // behind everything that is seen.  (What a turn needs of it are a few words: scalar registers are short here.)
+  struct Pair { int row0[2], row; bool part; const char *k, *v; };            // first rows; not all seen by all; of the tile that the wave fetches: its first row, the pages
+  const int side = wave / (W / 2), in_page = s.P - 1;        // which of the two tiles the wave fetches
+  const int behind = place - a.w.window, first = a.w.first;
+  uint32_t x_word = 0, x_k[2] = {}, x_v[2] = {};
   const int n = t1 - t0;
   auto pair_at = [&](int i) __attribute__((always_inline)) {     // (asked for in order)
-    if ((i & 63) == 0) {
+    if (__builtin_expect((i & 63) == 0, 0)) {
       const int t = t0 + i + lane, tile = v.tile(t), id = t < t1 ? page_at(s, c, u, tile >> (s.lp - 5)) : -1;
-      x_page = max(id, 0);
-      x_row0 = id >= 0 ? tile * 32 : kNowhere;
+      const int row0 = id >= 0 ? tile * 32 : kNowhere;
+      const bool all = row0 + 31 <= v.pa && (row0 > v.pb - a.w.window || row0 + 31 < a.w.first);
+      const int64_t page = max(id, 0) * s.page_bytes;
+      const uint64_t k = reinterpret_cast<uint64_t>(c.K + page), w = reinterpret_cast<uint64_t>(c.V + page);
+      x_word = (uint32_t)row0 | (all ? 0u : 1u);
+      x_k[0] = (uint32_t)k; x_k[1] = (uint32_t)(k >> 32);
+      x_v[0] = (uint32_t)w; x_v[1] = (uint32_t)(w >> 32);
     }
+    auto word = [&](uint32_t x, int j) { return (uint32_t)__builtin_amdgcn_readlane((int)x, (i & 63) + j); };
     Pair p;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      p.row0[x] = __builtin_amdgcn_readlane(x_row0, (i & 63) + x);
-      p.page[x] = __builtin_amdgcn_readlane(x_page, (i & 63) + x);
-    }
+    const uint32_t w0 = word(x_word, 0), w1 = word(x_word, 1);
+    p.row0[0] = (int)(w0 & ~31u);
+    p.row0[1] = (int)(w1 & ~31u);
+    p.row = (side ? p.row0[1] : p.row0[0]) & in_page;
+    p.part = ((w0 | w1) & 1u) != 0;
+    p.k = reinterpret_cast<const char *>((uint64_t)word(x_k[1], side) << 32 | word(x_k[0], side));
+    p.v = reinterpret_cast<const char *>((uint64_t)word(x_v[1], side) << 32 | word(x_v[0], side));
     return p;
   };
-  // tiles that all of the wave's rows see all of, and all of the group's
-  const int w_hi = wpa - 31, w_lo = wpb - a.w.window, g_hi = v.pa - 31, g_lo = v.pb - a.w.window, f_lo = a.w.first - 31;
-  const int behind = place - a.w.window, first = a.w.first;
-  const char *const K = c.K, *const V = c.V;
-  const int64_t page_bytes = s.page_bytes;
-  const int in_page = s.P - 1;
   const uint32_t img_a = lds_base_of(img);
   auto key_image = [&](int to) { return img_a + to * KEYS; };
   auto value_image = [&](int to) { return img_a + 2 * KEYS + to * IMG; };
@@ -116,22 +122,21 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
 #pragma unroll
   for (int blk = 0; blk < NB; ++blk) {
     const int l16 = lane & 15, sub = (lane >> 4) & 1, r = 4 * half + (l16 >> 2);       // (the rows that are 8 and 16 further have the same rotation)
-    v_at[blk] = img_a + 2 * KEYS + (Q4 ? (half * D + 32 * blk + l32) * 16 : r * RB + ((4 * blk + 2 * sub + ((l16 & 3) >> 1)) ^ value_swz<D>(r)) * 16 + (l16 & 1) * 8);
+    v_at[blk] = img_a + 2 * KEYS + (Q4 ? (half * D + 32 * blk + l32) * 16 : r * RB + ((4 * blk + 2 * sub + ((l16 & 3) >> 1)) ^ read_swz<D>(r)) * 16 + (l16 & 1) * 8);
   }
-  const int side = wave / (W / 2);                           // which of the two tiles the wave fetches
 
-  // bf16: a wave fetches 16 rows of one tile, directly: the lane's place in what each load takes
-  constexpr int RPL = 64 / PPR, LOADS = 16 / RPL;            // rows of a load, loads of a wave
-  const int f_row = 16 * (wave & 1);
+  // bf16: a wave fetches 8 rows of one tile, directly: the lane's place in what each load takes
+  constexpr int RPL = 64 / PPR, FROWS = 64 / W, LOADS = FROWS / RPL;         // rows of a load; rows and loads of a wave
+  const int f_row = FROWS * (wave % (W / 2));
   uint32_t f_at[2][LOADS];
 #pragma unroll
   for (int j = 0; j < LOADS; ++j) {
-    const int r = j * RPL + lane / PPR;                      // (the rows 16 further have the same rotations)
-    f_at[0][j] = r * RB + ((lane % PPR) ^ tile_swz<MIXKV_BF16, D>(r)) * 16;
-    f_at[1][j] = r * RB + ((lane % PPR) ^ value_swz<D>(r)) * 16;
+    const int r = j * RPL + lane / PPR;
+    f_at[0][j] = r * RB + ((lane % PPR) ^ tile_swz<MIXKV_BF16, D>(f_row + r)) * 16;
+    f_at[1][j] = r * RB + ((lane % PPR) ^ read_swz<D>(f_row + r)) * 16;
   }
   auto fetch = [&](const Pair &p, int values, uint32_t to) __attribute__((always_inline)) {
-    const char *base = (values ? V : K) + (int64_t)(side ? p.page[1] : p.page[0]) * page_bytes + (((side ? p.row0[1] : p.row0[0]) & in_page) + f_row) * RB;
+    const char *base = (values ? p.v : p.k) + (p.row + f_row) * RB;
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
       uint32_t at = f_at[values][j];
@@ -148,16 +153,16 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
   u32x2 vw;
   u32x4 vst, vba;
   auto ask_keys = [&](const Pair &p) __attribute__((always_inline)) {
-    const char *kp = K + (int64_t)(side ? p.page[1] : p.page[0]) * page_bytes;
-    const int row = ((side ? p.row0[1] : p.row0[0]) & in_page) + krow;
+    const char *kp = p.k;
+    const int row = p.row + krow;
     const uint32_t *kc = reinterpret_cast<const uint32_t *>(kp + row * (D / 2) + krun * (NG * 4)) + kpl, *kz = reinterpret_cast<const uint32_t *>(kp + codes + row * (NG * 4)) + kpl;
 #pragma unroll
     for (int g = 0; g < NG / 2; ++g) { kw[g] = kc[g]; ksb[g] = kz[g]; }
   };
   auto ask_values = [&](const Pair &p) __attribute__((always_inline)) {
     if (VT < 256 && r256 >= VT) return;
-    const char *vp = V + (int64_t)(side ? p.page[1] : p.page[0]) * page_bytes;
-    const int strip = (((side ? p.row0[1] : p.row0[0]) & in_page) >> 5) * 4 + vq;
+    const char *vp = p.v;
+    const int strip = (p.row >> 5) * 4 + vq;
     vw = *reinterpret_cast<const u32x2 *>(vp + (strip * D + 64 * vj + 4 * vm + 2 * vh) * 4);
     const char *z = vp + codes + (strip * NG + 2 * vj + vh) * 32;
     vst = *reinterpret_cast<const u32x4 *>(z);
@@ -201,34 +206,26 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
 
   // ---- scores of 32 keys: register e is key 8 (e / 4) + 4 half + e % 4.  (4 bits: the keys in two parts, so that a logit is off by no more than fp32 makes it, as
   // lse and weights have to be)
-  auto scores = [&](int at0, f32x16 (&acc)[2]) __attribute__((always_inline)) {
-    constexpr int AHEAD = Q4 ? KS / 2 : KS;                  // reads under way before the first product
-    constexpr int N = 2 * KS;
-    u32x4 kf[AHEAD], lf[Q4 ? AHEAD : 1];
-    auto read = [&](int i) __attribute__((always_inline)) {
-      const uint32_t at = k_at[i % KS] + at0 + i / KS * TILE;
-      kf[i % AHEAD] = lds_vec(at);
-      if constexpr (Q4) lf[i % AHEAD] = lds_vec(at + IMG);
-    };
+  constexpr int AHEAD = Q4 ? KS / 2 : KS;                    // reads under way
+  u32x4 kf[AHEAD], lf[Q4 ? AHEAD : 1];
+  auto read_keys = [&](int at0, int i) __attribute__((always_inline)) {        // the i-th of a turn's 2 KS pieces
+    const uint32_t at = k_at[i % KS] + at0 + i / KS * TILE;
+    kf[i % AHEAD] = lds_vec(at);
+    if constexpr (Q4) lf[i % AHEAD] = lds_vec(at + IMG);
+  };
+  auto score = [&](int i, int at0, f32x16 &acc) __attribute__((always_inline)) {
+    const int k = i % KS;
+    if (k == 0) {
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) read(i);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int x = i / KS, k = i % KS;
-      if (k == 0) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[x][e] = 0.f;
-      }
-      if constexpr (Q4) {
-        acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lf[i % AHEAD]), __builtin_bit_cast(f16x8, qf[k]), acc[x], 0, 0, 0);
-        acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kf[i % AHEAD]), __builtin_bit_cast(f16x8, qf[k]), acc[x], 0, 0, 0);
-      } else {
-        acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[i % AHEAD]), __builtin_bit_cast(bf16x8, qf[k]), acc[x], 0, 0, 0);
-      }
-      if (i + AHEAD < N) read(i + AHEAD);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int e = 0; e < 16; ++e) acc[e] = 0.f;
     }
+    if constexpr (Q4) {
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lf[i % AHEAD]), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kf[i % AHEAD]), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
+    } else {
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[i % AHEAD]), __builtin_bit_cast(bf16x8, qf[k]), acc, 0, 0, 0);
+    }
+    if (i + AHEAD < 2 * KS) read_keys(at0, i + AHEAD);
   };
   // ---- the values of 16 keys and 32 elements as the second product's first operand
   auto value = [&](int at0, int k, int blk) __attribute__((always_inline)) {
@@ -245,19 +242,12 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
     else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pf), acc, 0, 0, 0);
   };
 
-  // ---- weights of 32 keys against an offset, as the second product's second operand; their sum
-  auto weigh = [&](const f32x16 &x, float off, u32x4 (&pw)[2]) __attribute__((always_inline)) {
-    float total = 0.f;
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int e0 = Q4 ? 4 * k + j : 8 * k + 2 * j, e1 = Q4 ? 8 + 4 * k + j : e0 + 1;
-        const float p0 = fast_exp2(fmaf(x[e0], c2, -off)), p1 = fast_exp2(fmaf(x[e1], c2, -off));
-        total += p0 + p1;
-        pw[k][j] = Q4 ? __builtin_bit_cast(uint32_t, f16x2{(_Float16)p0, (_Float16)p1}) : __builtin_bit_cast(uint32_t, bf16x2{(__bf16)p0, (__bf16)p1});
-      }
-    return total;
+  // ---- the weights of 32 keys against an offset as the second product's second operand: the i-th of eight pairs, and their sum
+  auto weigh = [&](const f32x16 &x, int i, float off, u32x4 (&pw)[2]) __attribute__((always_inline)) {
+    const int k = i / 4, j = i % 4, e0 = Q4 ? 4 * k + j : 8 * k + 2 * j, e1 = Q4 ? 8 + 4 * k + j : e0 + 1;
+    const float p0 = fast_exp2(fmaf(x[e0], c2, -off)), p1 = fast_exp2(fmaf(x[e1], c2, -off));
+    pw[k][j] = Q4 ? __builtin_bit_cast(uint32_t, f16x2{(_Float16)p0, (_Float16)p1}) : __builtin_bit_cast(uint32_t, bf16x2{(__bf16)p0, (__bf16)p1});
+    return p0 + p1;
   };
 
   f32x16 o[NB];
@@ -277,27 +267,42 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
     fetch(cur, 0, key_image(0));
     fetch(cur, 1, value_image(0));
   }
-  auto turn_of = [&](int i, auto turn_c) __attribute__((always_inline)) {
-    constexpr int to = decltype(turn_c)::value;
-    if constexpr (!Q4) wait_vm<0>();
-    lds_barrier();
-    const int r0 = cur.row0[0], r1 = cur.row0[1];
-    const Pair nxt = pair_at(i + 2);
-    if (i + 2 < n) {
-      if constexpr (Q4) {
-        ask_keys(nxt);
-        ask_values(nxt);
-      } else {
-        fetch(nxt, 0, key_image(to ^ 1));
-        fetch(nxt, 1, value_image(to ^ 1));
-      }
+  // What a row does not see has no weight.
+  auto hide = [&](int row0, f32x16 &acc) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int j = row0 + 8 * (e >> 2) + 4 * half + (e & 3);
+      acc[e] = (j <= place) & ((j > behind) | (j < first)) ? acc[e] : -INFINITY;
+      __builtin_amdgcn_sched_barrier(0);                     // (one after another: side by side they take more scalar registers than there are)
     }
-    // Values that are no numbers, in tiles that not all of the group's rows see all of: zeros in their places, and behind the product they themselves where
-    // their rows are seen.  A weight of zero does not make NaN of them.
+  };
+  // The offset moves where a sum of weights reaches its limit.
+  auto settle = [&](const f32x16 &acc, float next, u32x4 (&pw)[2]) __attribute__((always_inline)) {
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!((Q4 ? next : sum + next) < (Q4 ? kPromptSum16 : kPromptSum))) != 0, 0)) {
+      float t = acc[0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) t = fmaxf(t, acc[e]);
+      t = fmaxf(t, __shfl_xor(t, 32));
+      const float mn = fmaxf(m, t * c2 - (Q4 ? 8.f : 0.f)), mu = mn == -INFINITY ? 0.f : mn, f = fast_exp2(m - mu);
+      next = 0.f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) next += weigh(acc, k, mu, pw);
+      sum *= f;
+#pragma unroll
+      for (int k = 0; k < NB; ++k)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[k][e] *= f;
+      m = mn;
+    }
+    sum += next;
+  };
+  // Two tiles, that all of the group's rows see all of, or not (part).  Then values that are no numbers are turned to zeros, and added behind the product where their
+  // rows are seen: a weight of zero does not make NaN of them.
+  auto tiles_of = [&](int r0, int r1, bool part, auto turn_c) __attribute__((always_inline)) {
+    constexpr int to = decltype(turn_c)::value;
     bool mixed = false;
     if constexpr (!Q4) {
-      const bool all = (r0 <= g_hi) & ((r0 > g_lo) | (r0 < f_lo)) & (r1 <= g_hi) & ((r1 > g_lo) | (r1 < f_lo));
-      if (!all) {
+      if (__builtin_expect(part, 0)) {
         bool odd = false;
 #pragma unroll
         for (int j = 0; j < IMG / (1024 * W); ++j) {
@@ -319,65 +324,50 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
         for (int w = 0; w < W; ++w) mixed |= odd_s[w] != 0;
       }
     }
+    // The matrix unit works on one tile's product while the vector unit forms the other's weights: in the program's order, a product and what fits beside it.
+    constexpr int k0 = to * KEYS, v0 = to * IMG, SPP = 8 / KS, VPP = 8 / (2 * NB);
     f32x16 acc[2];
-    scores(to * KEYS, acc);
-    // (bf16) the first tile's values, on their way while the weights are formed
-    constexpr int v0 = to * IMG;
-    u32x4 vf[2][NB];
-    if constexpr (!Q4) {
+    u32x4 pw[2][2], vf[2][NB];
+    float next[2] = {0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+    for (int k = 0; k < AHEAD; ++k) read_keys(k0, k);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int blk = 0; blk < NB; ++blk) vf[k][blk] = value(v0, k, blk);
+    for (int k = 0; k < KS; ++k) {
+      score(k, k0, acc[0]);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    // ---- weights
-    const bool whole = (r0 <= w_hi) & ((r0 > w_lo) | (r0 < f_lo)) & (r1 <= w_hi) & ((r1 > w_lo) | (r1 < f_lo));
-    if (!whole) {
+    if (__builtin_expect(part, 0)) hide(r0, acc[0]);
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int j = (x ? r1 : r0) + 8 * (e >> 2) + 4 * half + (e & 3);
-          acc[x][e] = (j <= place) & ((j > behind) | (j < first)) ? acc[x][e] : -INFINITY;
-          __builtin_amdgcn_sched_barrier(0);                 // (one after another: side by side they take more scalar registers than there are)
-        }
+    for (int i = 0; i < 8; ++i) {
+      if (i % SPP == 0) score(KS + i / SPP, k0, acc[1]);
+      if (!Q4 && i % VPP == 0) vf[i / VPP / NB][i / VPP % NB] = value(v0, i / VPP / NB, i / VPP % NB);
+      next[0] += weigh(acc[0], i, m, pw[0]);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    u32x4 pw[2][2];
-    float next = weigh(acc[0], m, pw[0]) + weigh(acc[1], m, pw[1]);
-    if (__builtin_amdgcn_ballot_w64(!((Q4 ? next : sum + next) < (Q4 ? kPromptSum16 : kPromptSum))) != 0) {
-      float t = -INFINITY;
+    settle(acc[0], next[0], pw[0]);
+    if (__builtin_expect(part, 0)) hide(r1, acc[1]);
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) t = fmaxf(t, acc[x][e]);
-      t = fmaxf(t, __shfl_xor(t, 32));
-      const float mn = fmaxf(m, t * c2 - (Q4 ? 8.f : 0.f)), mu = mn == -INFINITY ? 0.f : mn, f = fast_exp2(m - mu);
-      next = weigh(acc[0], mu, pw[0]) + weigh(acc[1], mu, pw[1]);
-      sum *= f;
-#pragma unroll
-      for (int k = 0; k < NB; ++k)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[k][e] *= f;
-      m = mn;
+    for (int i = 0; i < 8; ++i) {
+      if (i % VPP == 0) {
+        const int k = i / VPP / NB, blk = i / VPP % NB;
+        o[blk] = product(Q4 ? value(v0, k, blk) : vf[k][blk], pw[0][k], o[blk]);
+        if constexpr (!Q4) vf[k][blk] = value(v0 + TILE, k, blk);
+      }
+      next[1] += weigh(acc[1], i, m, pw[1]);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    sum += next;
-    // ---- weighted values
+    settle(acc[1], next[1], pw[1]);
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int blk = 0; blk < NB; ++blk) {
-          o[blk] = product(Q4 ? value(v0 + x * TILE, k, blk) : vf[k][blk], pw[x][k], o[blk]);
-          if (!Q4 && x == 0) vf[k][blk] = value(v0 + TILE, k, blk);
-          if constexpr (!Q4) __builtin_amdgcn_sched_barrier(0);
-        }
-    if (mixed) {
+      for (int blk = 0; blk < NB; ++blk) o[blk] = product(Q4 ? value(v0 + TILE, k, blk) : vf[k][blk], pw[1][k], o[blk]);
+    if (__builtin_expect(mixed, 0)) {
 #pragma unroll 1
       for (int r = 0; r < 64; ++r) {
         const int j = (r < 32 ? r0 : r1) + (r & 31);
         if (!sees(a.w, place, j)) continue;
-        const uint16_t *from = reinterpret_cast<const uint16_t *>(V + page_at(s, c, u, j >> s.lp) * page_bytes + (j & in_page) * RB);
+        const uint16_t *from = reinterpret_cast<const uint16_t *>(c.V + page_at(s, c, u, j >> s.lp) * s.page_bytes + (j & in_page) * RB);
 #pragma unroll
         for (int blk = 0; blk < NB; ++blk)
 #pragma unroll
@@ -387,6 +377,24 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
           }
       }
     }
+  };
+  auto turn_of = [&](int i, auto turn_c) __attribute__((always_inline)) {
+    constexpr int to = decltype(turn_c)::value;
+    if constexpr (!Q4) wait_vm<0>();
+    lds_barrier();
+    const int r0 = cur.row0[0], r1 = cur.row0[1];
+    const bool part = cur.part;
+    const Pair nxt = pair_at(i + 2);
+    if (i + 2 < n) {
+      if constexpr (Q4) {
+        ask_keys(nxt);
+        ask_values(nxt);
+      } else {
+        fetch(nxt, 0, key_image(to ^ 1));
+        fetch(nxt, 1, value_image(to ^ 1));
+      }
+    }
+    tiles_of(r0, r1, part, turn_c);
     if constexpr (Q4) {
       if (i + 2 < n) {
         unpack_keys(key_image(to ^ 1));
@@ -432,7 +440,7 @@ __global__ __launch_bounds__(64 * prompt_waves(Q4), 2) void paged_prompt_kernel(
 template <int D>
 __global__ __launch_bounds__(256) void prompt_merge_kernel(PShape s, PromptShape a, WinTable tab, const float *part, const float *part_ml, int64_t unit0) {
   constexpr int T = D / 4, ROWS = 256 / T;
-  const int R = prompt_rows(s.q4 != 0), t = threadIdx.x % T, i = blockIdx.y * ROWS + threadIdx.x / T, turn = a.q0 + blockIdx.z % a.qn, layer = blockIdx.z / a.qn, u = blockIdx.x;
+  const int R = kPromptRows, t = threadIdx.x % T, i = blockIdx.y * ROWS + threadIdx.x / T, turn = a.q0 + blockIdx.z % a.qn, layer = blockIdx.z / a.qn, u = blockIdx.x;
   const int h = u % s.hkv;
   const WinLayer l = tab.l[layer];
   const View v = view_of(s, a.w, tab.c[layer], l, u, turn * R, R);
@@ -463,7 +471,7 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(PShape s, PromptShape
 // Chunks of a group's tiles: one, unless the groups are fewer than the chip takes at once; then as many as fill it, of at least eight tiles.
 static PromptShape prompt_config(const PShape &s, const PWindow &w, int n_layers, int max_rows) {
   PromptShape a{};
-  const int rows = prompt_rows(s.q4 != 0), groups_at_once = s.q4 ? 256 : 512;
+  const int rows = kPromptRows, groups_at_once = 256;
   a.w = w;
   a.qtiles = (int)(((int64_t)w.max_count * s.G + rows - 1) / rows);
   const int64_t groups = (int64_t)n_layers * s.units_per_layer * a.qtiles, tiles = most_tiles(s, w, max_rows, rows);
@@ -473,7 +481,7 @@ static PromptShape prompt_config(const PShape &s, const PWindow &w, int n_layers
   return a;
 }
 static size_t prompt_slots(const PShape &s, const PromptShape &a, int n_layers) {
-  return a.nchunks == 1 ? 0 : (size_t)n_layers * s.units_per_layer * a.qtiles * a.nchunks * prompt_rows(s.q4 != 0);
+  return a.nchunks == 1 ? 0 : (size_t)n_layers * s.units_per_layer * a.qtiles * a.nchunks * kPromptRows;
 }
 
 size_t prompt_bytes(const PShape &s, const PWindow &w, int n_layers, int max_rows) {
@@ -486,7 +494,7 @@ mixkv_status launch_prompt(const PShape &s, const PWindow &w, const mixkv_paged_
   const size_t slots = prompt_slots(s, a, n_layers);
   float *part = static_cast<float *>(workspace), *part_ml = slots ? part + slots * s.D : nullptr;
   // a launch has at most 65535 groups of rows, and fewer than 2^32 threads
-  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 22) / ((int64_t)s.units_per_layer * std::max(a.nchunks, prompt_rows(s.q4 != 0)))));
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 22) / ((int64_t)s.units_per_layer * std::max(a.nchunks, kPromptRows))));
   for (int l0 = 0; l0 < n_layers;) {
     const int nl = (int)std::min<int64_t>(std::min(n_layers - l0, kLayersPerLaunch), std::max<int64_t>(1, most / a.qtiles));
     const WinTable t = window_table(caches + l0, queries + l0, nl, 2);
@@ -495,9 +503,9 @@ mixkv_status launch_prompt(const PShape &s, const PWindow &w, const mixkv_paged_
       a.qn = (int)std::min<int64_t>(a.qtiles - a.q0, std::max<int64_t>(1, most / nl));
       const dim3 grid((unsigned)(s.units_per_layer * a.nchunks), (unsigned)a.qn, (unsigned)nl);
       auto go = [&](auto kern, auto merge, int rows) {
-        hipLaunchKernelGGL(kern, grid, dim3(64 * prompt_waves(s.q4 != 0)), 0, stream, s, a, t, part, part_ml, unit0);
+        hipLaunchKernelGGL(kern, grid, dim3(64 * kPromptWaves), 0, stream, s, a, t, part, part_ml, unit0);
         if (a.nchunks > 1)
-          hipLaunchKernelGGL(merge, dim3((unsigned)s.units_per_layer, (unsigned)(prompt_rows(s.q4 != 0) / rows), (unsigned)(nl * a.qn)), dim3(256), 0, stream, s, a, t, (const float *)part,
+          hipLaunchKernelGGL(merge, dim3((unsigned)s.units_per_layer, (unsigned)(kPromptRows / rows), (unsigned)(nl * a.qn)), dim3(256), 0, stream, s, a, t, (const float *)part,
                              (const float *)part_ml, unit0);
       };
       if (s.q4) { if (s.D == 128) go(paged_prompt_kernel<128, true>, prompt_merge_kernel<128>, 8); else go(paged_prompt_kernel<64, true>, prompt_merge_kernel<64>, 16); }
