@@ -24,17 +24,9 @@ struct PromptShape {
   int32_t nchunks, ctiles;               // chunks of a group's tiles, tiles of a chunk (even)
 };
 
-// 1 + code / 16 for the codes i and i + 4 of a word: the code on top of the mantissa of 1.0.
-__device__ __forceinline__ f16x2 code_pair(uint32_t w, int i) {
-  return __builtin_bit_cast(f16x2, ((i < 2 ? w << (6 - 4 * i) : w >> (4 * i - 6)) & 0x03c003c0u) | 0x3c003c00u);
-}
-
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
-__device__ __forceinline__ u32x4 lds_vec(uint32_t at) { return *(const lds_u32x4 *)(uintptr_t)at; }
 // Four rows' elements, transposed.  (A parameter that is said to alias nothing: otherwise the compiler waits for every load on its way to LDS first.)
 __device__ __forceinline__ s16x4 read_transposed(lds_s16x4 *__restrict p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16(p); }
-__device__ __forceinline__ void store_lds(uint32_t at, u32x4 x) { *(lds_u32x4 *)(uintptr_t)at = x; }
 
 // Rotation of the 16-byte pieces of a value row: half a wave reads two pieces of four neighbouring rows at two places (those of 32 bytes further).
 template <int D>

@@ -10,9 +10,6 @@ struct WeightPtrs { float *w[kLayersPerLaunch]; };
 
 constexpr int kSumRun = 64;              // steps of 16 rows whose weights are summed up on their own: 2^17 rows are then off by some 2^-18 at most
 
-// bf16 bits to fp16, times 2^up.
-__device__ __forceinline__ _Float16 scaled_half(uint32_t bits, int up) { return (_Float16)ldexpf(__uint_as_float(bits), up); }
-
 // ------------------------------------------------------------------------------------------------
 // weights_step_kernel (few rows): a wave to tiles of 32 keys, rows on the output rows of 16 x 16 products, keys on their columns, so that a lane has
 // two keys and their sums over four rows each.  With up to 16 rows in all (a step's single tokens) the queries are prepared once.
@@ -194,6 +191,278 @@ __global__ __launch_bounds__(256) void weights_step_kernel(PShape s, PWindow win
   }
 }
 
+// ------------------------------------------------------------------------------------------------
+// weights_many_kernel (many rows, bf16 and 4-bit pages): a workgroup of eight waves to a block of keys and a chunk of the unit's rows.  A wave's keys stay in
+// registers as the first operand of 32 x 32 x 16 products (4 bits: in two fp16 parts), the rows travel through LDS, 64 a turn, and are the second for all
+// of them: a lane has 16 keys of one row, adds their weights up over its rows, and the lanes are folded at the end.
+// ------------------------------------------------------------------------------------------------
+constexpr int kManyWaves = 8, kManyRows = 64, kManyRun = 256;       // turns whose weights a lane adds up: 2 each, so that they are off by 2^-15 at most
+constexpr int many_keys(bool q4) { return 32 * kManyWaves * (q4 ? 1 : 2); }    // keys of a workgroup
+
+struct ManyShape {
+  PWindow w;
+  int32_t chunk, nchunks;                // rows of a chunk (a multiple of 64), chunks of a unit
+  int32_t blocks;                        // blocks of keys of a unit in the launch; longer heads' are walked
+  int64_t stride;                        // keys of a unit among the partial sums
+};
+
+// Rows [i0, i1) that see some of the keys [k0, k1) of a unit.
+struct Rows { int i0, i1; };
+__device__ __forceinline__ Rows rows_that_see(const PShape &s, const PWindow &w, int len, int count, int k0, int k1) {
+  const int place0 = len - count, served = min(count, w.max_count);
+  const int lo = max(k0 - place0, 0), hi = k0 < w.first ? served : (int)min((int64_t)served, (int64_t)k1 - 1 + w.window - place0);
+  Rows r;
+  r.i0 = min(lo, served) * s.G;
+  r.i1 = max(hi, 0) * s.G;
+  return r;
+}
+
+template <int D, bool Q4>
+__global__ __launch_bounds__(64 * kManyWaves, 2) void weights_many_kernel(PShape s, ManyShape a, WinTable tab, WeightPtrs ptrs, float *part, int64_t unit0) {
+  constexpr int RB = D * 2, PPR = RB / 16, KS = D / 16, NG = D / 32, W = kManyWaves, KB = Q4 ? 1 : 2, KEYS = many_keys(Q4), R = kManyRows, IMG = R * RB;
+  __shared__ __align__(16) char img[2][IMG];
+  __shared__ float off_s[2][R], c2_s[2][R];
+  __shared__ int place_s[2][R];
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int units = s.units_per_layer, ch = blockIdx.x / units, u = dealt_unit((int)blockIdx.x - ch * units, (int)(blockIdx.y + ch), units), layer = blockIdx.z;
+  const int b = u / s.hkv, h = u - b * s.hkv;
+  const PCache c = tab.c[layer];
+  const WinLayer l = tab.l[layer];
+  float *weights = ptrs.w[layer];
+  const int len = head_rows(s, c, u), count = max(l.count[u], 0), start = l.start[u], place0 = len - count;
+  const uint32_t img_a = lds_base_of(img);
+  for (int block = blockIdx.y; (int64_t)block * KEYS < len; block += a.blocks) {
+    const int kA = block * KEYS, kB = min(kA + KEYS, len);
+    const Rows rows = rows_that_see(s, a.w, len, count, kA, kB);
+    const bool direct = a.nchunks == 1 || kA >= a.stride;    // (keys that the host did not know of: all their rows in one go)
+    if (direct && ch > 0) continue;                          // uniform
+    const int i0 = direct ? rows.i0 & ~(R - 1) : max(rows.i0 & ~(R - 1), ch * a.chunk), i1 = direct || ch == a.nchunks - 1 ? rows.i1 : min(rows.i1, (ch + 1) * a.chunk);
+    if (i0 >= i1 && !direct) continue;                       // uniform: nobody reads these sums
+    // ---- the wave's keys
+    int id[KB], key0[KB];
+    u32x4 kf[KB][KS], lf[KB][Q4 ? KS : 1];
+#pragma unroll
+    for (int x = 0; x < KB; ++x) {
+      key0[x] = kA + (wave * KB + x) * 32;
+      id[x] = key0[x] < len ? page_at(s, c, u, key0[x] >> s.lp) : -1;
+      const int row = (key0[x] & (s.P - 1)) + l32;
+      const char *page = c.K + (int64_t)max(id[x], 0) * s.page_bytes;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        if constexpr (Q4) {
+          const int g = k >> 1, run = 2 * (k & 1) + half, pl = D == 128 ? (g & 1) * 2 + (g >> 1) : g;
+          const uint32_t w = reinterpret_cast<const uint32_t *>(page + row * (D / 2))[run * NG + pl], z = reinterpret_cast<const uint32_t *>(page + s.P * (D / 2))[row * NG + pl];
+          const f16x2 sb = __builtin_bit_cast(f16x2, z), step = {sb[0], sb[0]}, base = {sb[1], sb[1]};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const f16x2 un = code_pair(w, j), y = __builtin_elementwise_fma(un, step, base);
+            kf[x][k][j] = __builtin_bit_cast(uint32_t, y);
+            lf[x][k][j] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)(fmaf((float)un[0], (float)sb[0], (float)sb[1]) - (float)y[0]), (_Float16)(fmaf((float)un[1], (float)sb[0], (float)sb[1]) - (float)y[1])});
+          }
+        } else {
+          kf[x][k] = *reinterpret_cast<const u32x4 *>(page + row * RB + (2 * k + half) * 16);
+        }
+      }
+    }
+    // ---- rows: what a thread stages, walked 64 a turn.  bf16: a wave's eight rows, directly; 4 bits: eight threads to a row, to fp16 by a power of two that brings
+    // its largest element to [2^13, 2^14)
+    struct At { int t, g; };
+    const int step_t = R / s.G, step_g = R - step_t * s.G;
+    auto at_row = [&](int i) { At x; x.t = i / s.G; x.g = i - x.t * s.G; return x; };
+    auto walk = [&](At &x) { x.t += step_t; x.g += step_g; if (x.g >= s.G) { x.g -= s.G; ++x.t; } };
+    const int last_t = max(i1 - 1, 0) / s.G, last_g = max(i1 - 1, 0) - last_t * s.G;
+    auto address = [&](const At &x) {                        // (rows behind the last one repeat it)
+      const bool in = x.t < last_t || (x.t == last_t && x.g <= last_g);
+      const int64_t row = min(max((int64_t)start + (in ? x.t : last_t), (int64_t)0), (int64_t)a.w.n_rows - 1);
+      return l.Q + row * l.qsn + (int64_t)(h * s.G + (in ? x.g : last_g)) * l.qsh;
+    };
+    constexpr int RPL = 64 / PPR, LOADS = Q4 ? 1 : 8 / RPL, PIECES = PPR / 8;    // bf16: rows of a load, loads of a wave; 4 bits: pieces of a thread
+    At q_at[LOADS], n_at{};
+    u32x4 q_raw[Q4 ? PIECES : 1];
+    float n_lse = 0.f;
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) q_at[j] = at_row(i0 + (Q4 ? tid >> 3 : 8 * wave + j * RPL + lane / PPR));
+    if (tid < R) n_at = at_row(i0 + tid);
+    bool n_there = false;
+    int n_place = -1;
+    auto request = [&](int to) {
+      if constexpr (!Q4) {
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+          const int r = 8 * wave + j * RPL + lane / PPR;
+          load_to_lds<false>(address(q_at[j]) + ((lane % PPR) ^ tile_swz<MIXKV_BF16, D>(r)) * 16, img_a + to * IMG + (8 * wave + j * RPL) * RB);
+        }
+      } else {
+        const char *q = address(q_at[0]) + (tid & 7) * (PIECES * 16);
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) q_raw[j] = *reinterpret_cast<const u32x4 *>(q + j * 16);
+      }
+#pragma unroll
+      for (int j = 0; j < LOADS; ++j) walk(q_at[j]);
+      if (tid < R) {
+        const int64_t row = (int64_t)start + n_at.t;
+        n_there = (n_at.t < last_t || (n_at.t == last_t && n_at.g <= last_g)) && row >= 0 && row < a.w.n_rows;
+        n_lse = l.lse[(n_there ? row : 0) * s.hq + h * s.G + n_at.g];
+        n_place = place0 + n_at.t;
+        walk(n_at);
+      }
+    };
+    auto settle = [&](int to) {                              // what was requested, into LDS
+      if (tid < R) {
+        off_s[to][tid] = n_lse * -1.44269504088896340736f;
+        place_s[to][tid] = n_there && n_lse != -INFINITY ? n_place : -1;       // -1: the row gives nothing
+      }
+      if constexpr (Q4) {
+        uint32_t most = 0;
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) most = max(most, max(q_raw[j][k] & 0x7fffu, (q_raw[j][k] >> 16) & 0x7fffu));
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o));
+        const int up = 13 - (min(max((int)(most >> 7), 1), 254) - 127), r = tid >> 3;
+        if ((tid & 7) == 0) c2_s[to][r] = fminf(fmaxf(ldexpf(s.scale_log2e, -up), 0x1p-126f), 0x1p100f);
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) {
+          u32x4 x;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            x[k] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)ldexpf(__uint_as_float(q_raw[j][k] << 16), up), (_Float16)ldexpf(__uint_as_float(q_raw[j][k] & 0xffff0000u), up)});
+          store_lds(img_a + to * IMG + r * RB + (((tid & 7) * PIECES + j) ^ tile_swz<MIXKV_BF16, D>(r)) * 16, x);
+        }
+      }
+    };
+    uint32_t q_off[KS];                                      // where the lane reads
+#pragma unroll
+    for (int k = 0; k < KS; ++k) q_off[k] = img_a + l32 * RB + ((2 * k + half) ^ tile_swz<MIXKV_BF16, D>(l32)) * 16;
+
+    // A lane's sums of a key's weights; and folded over the lanes, lane e of a half with the key 8 (e / 4) + 4 half + e % 4
+    float run[KB][16], mine[KB];
+    auto clear = [&]() {
+#pragma unroll
+      for (int x = 0; x < KB; ++x)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) run[x][e] = 0.f;
+    };
+    auto fold = [&]() {
+#pragma unroll
+      for (int x = 0; x < KB; ++x)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float t = run[x][e];
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) t += __shfl_xor(t, o);
+          mine[x] += l32 == e ? t : 0.f;
+        }
+    };
+#pragma unroll
+    for (int x = 0; x < KB; ++x) mine[x] = 0.f;
+    clear();
+    if (i0 < i1) {
+      request(0);
+      settle(0);
+    }
+    for (int i = i0, to = 0; i < i1; i += R, to ^= 1) {
+      if constexpr (!Q4) wait_vm<0>();
+      lds_barrier();
+      if (i + R < i1) request(to ^ 1);
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const float off = off_s[to][32 * y + l32], c2 = Q4 ? c2_s[to][32 * y + l32] : s.scale_log2e;
+        const int place = place_s[to][32 * y + l32], behind = place - a.w.window;
+        u32x4 qf[KS];
+#pragma unroll
+        for (int k = 0; k < KS; ++k) qf[k] = lds_vec(q_off[k] + to * IMG + y * 32 * RB);
+#pragma unroll
+        for (int x = 0; x < KB; ++x) {
+          const int k0 = key0[x];
+          if (__builtin_amdgcn_ballot_w64(k0 <= place && (k0 + 31 > behind || k0 < a.w.first)) == 0) continue;
+          const bool whole = __builtin_amdgcn_ballot_w64(k0 + 31 <= place && (k0 > behind || k0 + 31 < a.w.first)) == ~0ull;
+          f32x16 acc;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            if constexpr (Q4) {
+              acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lf[x][k]), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
+              acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kf[x][k]), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
+            } else {
+              acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[x][k]), __builtin_bit_cast(bf16x8, qf[k]), acc, 0, 0, 0);
+            }
+          }
+          if (whole) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) run[x][e] += fast_exp2(fmaf(acc[e], c2, off));
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int j = k0 + 8 * (e >> 2) + 4 * half + (e & 3);
+              run[x][e] += (j <= place) & ((j > behind) | (j < a.w.first)) ? fast_exp2(fmaf(acc[e], c2, off)) : 0.f;
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          }
+        }
+      }
+      if (i + R < i1) settle(to ^ 1);
+      if (__builtin_expect(((i - i0) / R & (kManyRun - 1)) == kManyRun - 1, 0)) { fold(); clear(); }
+    }
+    fold();
+#pragma unroll
+    for (int x = 0; x < KB; ++x) {
+      const int j = key0[x] + 8 * (l32 >> 2) + 4 * half + (l32 & 3);
+      if (l32 >= 16 || j >= len || id[x] < 0) continue;
+      if (!direct) {
+        part[((unit0 + (int64_t)layer * units + u) * a.nchunks + ch) * a.stride + j] = mine[x];
+      } else if (rows.i0 < rows.i1 || j >= place0) {
+        float *w = weights + ((int64_t)id[x] << s.lp) + (j & (s.P - 1));
+        *w = (j >= place0 ? 0.f : *w) + mine[x];
+      }
+    }
+    __syncthreads();                                         // the images are written anew
+  }
+}
+
+// Adds up the chunks' sums, in their order.
+__global__ __launch_bounds__(256) void weights_fold_kernel(PShape s, ManyShape a, WinTable tab, WeightPtrs ptrs, const float *part, int64_t unit0, int keys) {
+  const int u = blockIdx.x, layer = blockIdx.z;
+  const PCache c = tab.c[layer];
+  const WinLayer l = tab.l[layer];
+  const int len = head_rows(s, c, u), count = max(l.count[u], 0);
+  for (int j = blockIdx.y * 256 + threadIdx.x; j < len && j < a.stride; j += gridDim.y * 256) {
+    const int id = page_at(s, c, u, j >> s.lp);
+    if (id < 0) continue;
+    const int kA = j / keys * keys;
+    const Rows rows = rows_that_see(s, a.w, len, count, kA, min(kA + keys, len));
+    const bool fresh = j >= len - count;
+    if (rows.i0 >= rows.i1 && !fresh) continue;
+    float *w = ptrs.w[layer] + ((int64_t)id << s.lp) + (j & (s.P - 1));
+    float x = fresh ? 0.f : *w, sum = 0.f;
+    if (rows.i0 < rows.i1) {
+      const float *p = part + (unit0 + (int64_t)layer * s.units_per_layer + u) * a.nchunks * a.stride + j;
+      const int c0 = min(rows.i0 / a.chunk, a.nchunks - 1), c1 = min((rows.i1 - 1) / a.chunk, a.nchunks - 1);
+      for (int k = c0; k <= c1; ++k) sum += p[k * a.stride];
+    }
+    *w = x + sum;
+  }
+}
+
+// Chunks of rows: enough for sixteen workgroups to a compute unit (half of which have rows, in a prompt), of at least 1024 rows.
+static ManyShape many_config(const PShape &s, const PWindow &w, int n_layers, int max_rows) {
+  ManyShape a{};
+  a.w = w;
+  const int64_t rows = (int64_t)w.max_count * s.G, keys = many_keys(s.q4 != 0), blocks = ((int64_t)max_rows + keys - 1) / keys, units = (int64_t)n_layers * s.units_per_layer;
+  a.stride = blocks * keys;
+  const int64_t chunk = std::max<int64_t>(std::max<int64_t>(1024, rows * blocks / 4096 * units), rows * units >> 20);
+  a.chunk = (int)((std::min(chunk, rows) + kManyRows - 1) / kManyRows * kManyRows);
+  a.nchunks = (int)((rows + a.chunk - 1) / a.chunk);
+  a.blocks = (int)std::min<int64_t>(blocks, 65535);
+  return a;
+}
+static size_t many_bytes(const PShape &s, const ManyShape &a, int n_layers) {
+  return a.nchunks == 1 ? 0 : (size_t)n_layers * s.units_per_layer * a.nchunks * a.stride * sizeof(float);
+}
+
 // Tiles of a workgroup: as many workgroups as four to a compute unit take, a tile to a wave at least; a launch has at most 65535 along a head, and fewer than
 // 2^32 threads.
 static int step_tiles(const PShape &s, int nl, int max_rows) {
@@ -214,7 +483,8 @@ extern "C" mixkv_status mixkv_paged_weights_workspace_size(const mixkv_paged_par
   if (st != MIXKV_OK) return st;
   if ((st = make_window(s, n_rows, window, keep_first, max_count, max_rows, &w)) != MIXKV_OK) return st;
   if (!bytes || n_layers < 1 || n_layers > MIXKV_MAX_LAYERS) return MIXKV_ERR_INVALID_ARG;
-  *bytes = 0;
+  max_rows = std::min(max_rows, s.max_pages * s.P);
+  *bytes = many_rows(s, params->dtype, w) ? (many_bytes(s, many_config(s, w, n_layers, max_rows), n_layers) + 255) / 256 * 256 : 0;
   return MIXKV_OK;
 }
 
@@ -222,7 +492,6 @@ extern "C" mixkv_status mixkv_paged_weights(const mixkv_paged_params *params, co
                                             int32_t n_layers, int32_t n_rows, int32_t window, int32_t keep_first, int32_t max_count, int32_t max_rows,
                                             void *workspace, size_t workspace_bytes, void *hip_stream) {
   using namespace mixkv;
-  (void)workspace; (void)workspace_bytes;
   PShape s;
   PWindow w;
   mixkv_status st = make_pshape(params, &s);
@@ -236,11 +505,38 @@ extern "C" mixkv_status mixkv_paged_weights(const mixkv_paged_params *params, co
     if (!caches[l].K_pages || !weights[l] || misaligned(weights[l], 16)) return MIXKV_ERR_INVALID_ARG;
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   max_rows = std::min(max_rows, s.max_pages * s.P);
-  for (int l0 = 0; l0 < n_layers; l0 += kLayersPerLaunch) {
-    const int nl = std::min(n_layers - l0, kLayersPerLaunch);
+  const bool many = many_rows(s, params->dtype, w);
+  ManyShape a{};
+  if (many) a = many_config(s, w, n_layers, max_rows);
+  const size_t need = many ? many_bytes(s, a, n_layers) : 0;
+  if (need > 0) {
+    if (!workspace || misaligned(workspace, 256)) return MIXKV_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return MIXKV_ERR_WORKSPACE_TOO_SMALL;
+  }
+  float *part = static_cast<float *>(workspace);
+  // many rows: a launch has fewer than 2^32 threads
+  const int64_t fit = std::max<int64_t>(1, ((int64_t)1 << 22) / ((int64_t)s.units_per_layer * a.nchunks + 1));
+  if (many) a.blocks = (int)std::min<int64_t>(a.blocks, fit);
+  const int per = many ? (int)std::min<int64_t>(kLayersPerLaunch, std::max<int64_t>(1, fit / a.blocks)) : kLayersPerLaunch;
+  for (int l0 = 0; l0 < n_layers; l0 += per) {
+    const int nl = std::min(n_layers - l0, per);
+    const int64_t unit0 = (int64_t)l0 * s.units_per_layer;
     const WinTable t = window_table(caches + l0, queries + l0, nl, eb);
     WeightPtrs p{};
     for (int l = 0; l < nl; ++l) p.w[l] = weights[l0 + l];
+    if (many) {
+      const dim3 grid((unsigned)(s.units_per_layer * a.nchunks), (unsigned)a.blocks, (unsigned)nl);
+      auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(64 * kManyWaves), 0, stream, s, a, t, p, part, unit0); };
+      if (s.q4) { if (s.D == 128) go(weights_many_kernel<128, true>); else go(weights_many_kernel<64, true>); }
+      else { if (s.D == 128) go(weights_many_kernel<128, false>); else go(weights_many_kernel<64, false>); }
+      if (a.nchunks > 1) {
+        const int64_t y = std::min<int64_t>((a.stride + 255) / 256, std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 23) / ((int64_t)s.units_per_layer * nl))));
+        hipLaunchKernelGGL(weights_fold_kernel, dim3((unsigned)s.units_per_layer, (unsigned)y, (unsigned)nl), dim3(256), 0, stream, s, a, t, p, (const float *)part, unit0,
+                           many_keys(s.q4 != 0));
+      }
+      if (hipGetLastError() != hipSuccess) return MIXKV_ERR_HIP;
+      continue;
+    }
     const int ctiles = step_tiles(s, nl, max_rows);
     const dim3 grid((unsigned)s.units_per_layer, (unsigned)(((int64_t)max_rows + 32 * ctiles - 1) / (32 * ctiles)), (unsigned)nl);
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, stream, s, w, t, p, ctiles); };

@@ -78,6 +78,16 @@ __device__ __forceinline__ float row_result(float acc, float tot) { return tot =
 // Log-sum-exp from the offset, in exponents of 2, and the sum; no rows give -infinity.
 __device__ __forceinline__ float row_lse(float offset, float tot) { return tot == 0.f ? -INFINITY : (offset + __builtin_amdgcn_logf(tot)) * 0.69314718055994530942f; }
 
+// 1 + code / 16 for the codes i and i + 4 of a word: the code on top of the mantissa of 1.0.
+__device__ __forceinline__ f16x2 code_pair(uint32_t w, int i) {
+  return __builtin_bit_cast(f16x2, ((i < 2 ? w << (6 - 4 * i) : w >> (4 * i - 6)) & 0x03c003c0u) | 0x3c003c00u);
+}
+
+// 16 bytes of LDS by their address.
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+__device__ __forceinline__ u32x4 lds_vec(uint32_t at) { return *(const lds_u32x4 *)(uintptr_t)at; }
+__device__ __forceinline__ void store_lds(uint32_t at, u32x4 x) { *(lds_u32x4 *)(uintptr_t)at = x; }
+
 // Whether a word holds an infinity or a NaN, and the word with zeros in their places.
 template <int DT>
 __device__ __forceinline__ bool no_number(uint32_t w) {
