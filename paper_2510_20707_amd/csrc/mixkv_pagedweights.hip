@@ -232,6 +232,9 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void weights_many_kernel(PShape
   float *weights = ptrs.w[layer];
   const int len = head_rows(s, c, u), count = max(l.count[u], 0), start = l.start[u], place0 = len - count;
   const uint32_t img_a = lds_base_of(img);
+  const int G = s.G, step_t = R / G, step_g = R - step_t * G;
+  const int64_t qsn = l.qsn, qsh = l.qsh, step_q = step_t * qsn + step_g * qsh, wrap_q = qsn - G * qsh;
+  const char *const Q = l.Q + (int64_t)h * G * qsh;
   for (int block = blockIdx.y; (int64_t)block * KEYS < len; block += a.blocks) {
     const int kA = block * KEYS, kB = min(kA + KEYS, len);
     const Rows rows = rows_that_see(s, a.w, len, count, kA, kB);
@@ -265,53 +268,56 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void weights_many_kernel(PShape
         }
       }
     }
-    // ---- rows: what a thread stages, walked 64 a turn.  bf16: a wave's eight rows, directly; 4 bits: eight threads to a row, to fp16 by a power of two that brings
-    // its largest element to [2^13, 2^14)
-    struct At { int t, g; };
-    const int step_t = R / s.G, step_g = R - step_t * s.G;
-    auto at_row = [&](int i) { At x; x.t = i / s.G; x.g = i - x.t * s.G; return x; };
-    auto walk = [&](At &x) { x.t += step_t; x.g += step_g; if (x.g >= s.G) { x.g -= s.G; ++x.t; } };
-    const int last_t = max(i1 - 1, 0) / s.G, last_g = max(i1 - 1, 0) - last_t * s.G;
-    auto address = [&](const At &x) {                        // (rows behind the last one repeat it)
-      const bool in = x.t < last_t || (x.t == last_t && x.g <= last_g);
-      const int64_t row = min(max((int64_t)start + (in ? x.t : last_t), (int64_t)0), (int64_t)a.w.n_rows - 1);
-      return l.Q + row * l.qsn + (int64_t)(h * s.G + (in ? x.g : last_g)) * l.qsh;
+    // ---- rows: what a thread stages, walked 64 a turn, a wave eight of them.  bf16: directly; 4 bits: eight threads to a row, to fp16 by a power of two that brings its
+    // largest element to [2^13, 2^14).  A row that is none gives nothing, whatever is staged for it.
+    struct At { const char *q; int t, g; };
+    auto at_row = [&](int i) {
+      At x;
+      x.t = i / G;
+      x.g = i - x.t * G;
+      x.q = Q + ((int64_t)start + x.t) * qsn + (int64_t)x.g * qsh;
+      return x;
     };
+    auto walk = [&](At &x) __attribute__((always_inline)) {
+      x.t += step_t;
+      x.g += step_g;
+      x.q += step_q;
+      if (x.g >= G) { x.g -= G; ++x.t; x.q += wrap_q; }
+    };
+    auto there = [&](const At &x, int i) { return (i < i1) & ((uint32_t)(start + x.t) < (uint32_t)a.w.n_rows); };
     constexpr int RPL = 64 / PPR, LOADS = Q4 ? 1 : 8 / RPL, PIECES = PPR / 8;    // bf16: rows of a load, loads of a wave; 4 bits: pieces of a thread
-    At q_at[LOADS], n_at{};
+    const int r_row = 8 * wave + (Q4 ? lane >> 3 : lane / PPR);
+    At q_at[LOADS];
+    int n_t = (i0 + 8 * wave + (lane & 7)) / G, n_g = i0 + 8 * wave + (lane & 7) - n_t * G;      // the row whose normaliser the lane stages
     u32x4 q_raw[Q4 ? PIECES : 1];
     float n_lse = 0.f;
-#pragma unroll
-    for (int j = 0; j < LOADS; ++j) q_at[j] = at_row(i0 + (Q4 ? tid >> 3 : 8 * wave + j * RPL + lane / PPR));
-    if (tid < R) n_at = at_row(i0 + tid);
-    bool n_there = false;
     int n_place = -1;
-    auto request = [&](int to) {
-      if constexpr (!Q4) {
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
-          const int r = 8 * wave + j * RPL + lane / PPR;
-          load_to_lds<false>(address(q_at[j]) + ((lane % PPR) ^ tile_swz<MIXKV_BF16, D>(r)) * 16, img_a + to * IMG + (8 * wave + j * RPL) * RB);
+    for (int j = 0; j < LOADS; ++j) q_at[j] = at_row(i0 + r_row + j * RPL);
+    auto request = [&](int i, int to) __attribute__((always_inline)) {           // rows i ... i + 63
+#pragma unroll
+      for (int j = 0; j < LOADS; ++j) {
+        const int r = r_row + j * RPL;
+        const char *q = there(q_at[j], i + r) ? q_at[j].q : Q;
+        if constexpr (!Q4) {
+          load_to_lds<false>(q + ((lane % PPR) ^ tile_swz<MIXKV_BF16, D>(r)) * 16, img_a + to * IMG + (8 * wave + j * RPL) * RB);
+        } else {
+#pragma unroll
+          for (int k = 0; k < PIECES; ++k) q_raw[k] = *reinterpret_cast<const u32x4 *>(q + ((lane & 7) * PIECES + k) * 16);
         }
-      } else {
-        const char *q = address(q_at[0]) + (tid & 7) * (PIECES * 16);
-#pragma unroll
-        for (int j = 0; j < PIECES; ++j) q_raw[j] = *reinterpret_cast<const u32x4 *>(q + j * 16);
+        walk(q_at[j]);
       }
-#pragma unroll
-      for (int j = 0; j < LOADS; ++j) walk(q_at[j]);
-      if (tid < R) {
-        const int64_t row = (int64_t)start + n_at.t;
-        n_there = (n_at.t < last_t || (n_at.t == last_t && n_at.g <= last_g)) && row >= 0 && row < a.w.n_rows;
-        n_lse = l.lse[(n_there ? row : 0) * s.hq + h * s.G + n_at.g];
-        n_place = place0 + n_at.t;
-        walk(n_at);
-      }
+      const bool in = (i + 8 * wave + (lane & 7) < i1) & ((uint32_t)(start + n_t) < (uint32_t)a.w.n_rows);
+      n_lse = l.lse[in ? (int64_t)(start + n_t) * s.hq + h * G + n_g : 0];
+      n_place = in ? place0 + n_t : -1;
+      n_t += step_t;
+      n_g += step_g;
+      if (n_g >= G) { n_g -= G; ++n_t; }
     };
-    auto settle = [&](int to) {                              // what was requested, into LDS
-      if (tid < R) {
-        off_s[to][tid] = n_lse * -1.44269504088896340736f;
-        place_s[to][tid] = n_there && n_lse != -INFINITY ? n_place : -1;       // -1: the row gives nothing
+    auto settle = [&](int to) __attribute__((always_inline)) {                   // what was requested, into LDS
+      if (lane < 8) {
+        off_s[to][8 * wave + lane] = n_lse * -1.44269504088896340736f;
+        place_s[to][8 * wave + lane] = n_lse != -INFINITY ? n_place : -1;
       }
       if constexpr (Q4) {
         uint32_t most = 0;
@@ -321,15 +327,15 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void weights_many_kernel(PShape
           for (int k = 0; k < 4; ++k) most = max(most, max(q_raw[j][k] & 0x7fffu, (q_raw[j][k] >> 16) & 0x7fffu));
 #pragma unroll
         for (int o = 1; o < 8; o <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o));
-        const int up = 13 - (min(max((int)(most >> 7), 1), 254) - 127), r = tid >> 3;
-        if ((tid & 7) == 0) c2_s[to][r] = fminf(fmaxf(ldexpf(s.scale_log2e, -up), 0x1p-126f), 0x1p100f);
+        const int up = 13 - (min(max((int)(most >> 7), 1), 254) - 127);
+        if ((lane & 7) == 0) c2_s[to][r_row] = fminf(fmaxf(ldexpf(s.scale_log2e, -up), 0x1p-126f), 0x1p100f);
 #pragma unroll
         for (int j = 0; j < PIECES; ++j) {
           u32x4 x;
 #pragma unroll
           for (int k = 0; k < 4; ++k)
             x[k] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)ldexpf(__uint_as_float(q_raw[j][k] << 16), up), (_Float16)ldexpf(__uint_as_float(q_raw[j][k] & 0xffff0000u), up)});
-          store_lds(img_a + to * IMG + r * RB + (((tid & 7) * PIECES + j) ^ tile_swz<MIXKV_BF16, D>(r)) * 16, x);
+          store_lds(img_a + to * IMG + r_row * RB + (((lane & 7) * PIECES + j) ^ tile_swz<MIXKV_BF16, D>(r_row)) * 16, x);
         }
       }
     };
@@ -338,6 +344,8 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void weights_many_kernel(PShape
     for (int k = 0; k < KS; ++k) q_off[k] = img_a + l32 * RB + ((2 * k + half) ^ tile_swz<MIXKV_BF16, D>(l32)) * 16;
 
     // A lane's sums of a key's weights; and folded over the lanes, lane e of a half with the key 8 (e / 4) + 4 half + e % 4
+    const int kz = key0[KB - 1] + 31, window = a.w.window, first = a.w.first;
+    const float scale = s.scale_log2e;
     float run[KB][16], mine[KB];
     auto clear = [&]() {
 #pragma unroll
@@ -346,6 +354,8 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void weights_many_kernel(PShape
         for (int e = 0; e < 16; ++e) run[x][e] = 0.f;
     };
     auto fold = [&]() {
+      int at = l32;
+      asm volatile("" : "+v"(at));                           // (what is compared with it is not kept in scalar registers through the loop)
 #pragma unroll
       for (int x = 0; x < KB; ++x)
 #pragma unroll
@@ -353,52 +363,86 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void weights_many_kernel(PShape
           float t = run[x][e];
 #pragma unroll
           for (int o = 1; o < 32; o <<= 1) t += __shfl_xor(t, o);
-          mine[x] += l32 == e ? t : 0.f;
+          mine[x] += at == e ? t : 0.f;
         }
     };
 #pragma unroll
     for (int x = 0; x < KB; ++x) mine[x] = 0.f;
     clear();
     if (i0 < i1) {
-      request(0);
+      request(i0, 0);
       settle(0);
     }
     for (int i = i0, to = 0; i < i1; i += R, to ^= 1) {
       if constexpr (!Q4) wait_vm<0>();
       lds_barrier();
-      if (i + R < i1) request(to ^ 1);
+      if (i + R < i1) request(i + R, to ^ 1);
+      // four blocks of 32 rows and 32 keys (4 bits: two)
+      float off[2], c2[2];
+      int place[2];
+      bool all = true;
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        const float off = off_s[to][32 * y + l32], c2 = Q4 ? c2_s[to][32 * y + l32] : s.scale_log2e;
-        const int place = place_s[to][32 * y + l32], behind = place - a.w.window;
-        u32x4 qf[KS];
-#pragma unroll
-        for (int k = 0; k < KS; ++k) qf[k] = lds_vec(q_off[k] + to * IMG + y * 32 * RB);
-#pragma unroll
-        for (int x = 0; x < KB; ++x) {
-          const int k0 = key0[x];
-          if (__builtin_amdgcn_ballot_w64(k0 <= place && (k0 + 31 > behind || k0 < a.w.first)) == 0) continue;
-          const bool whole = __builtin_amdgcn_ballot_w64(k0 + 31 <= place && (k0 > behind || k0 + 31 < a.w.first)) == ~0ull;
-          f32x16 acc;
+        off[y] = off_s[to][32 * y + l32];
+        c2[y] = Q4 ? c2_s[to][32 * y + l32] : scale;
+        place[y] = place_s[to][32 * y + l32];
+        all = all & (kz <= place[y]) & ((key0[0] > place[y] - window) | (kz < first));
+      }
+      u32x4 qf[KS];
+      auto read_row = [&](int y, int k) __attribute__((always_inline)) { qf[k] = lds_vec(q_off[k] + to * IMG + y * 32 * RB); };
+      auto score = [&](int x, int k, f32x16 &acc) __attribute__((always_inline)) {
+        if (k == 0) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+        }
+        if constexpr (Q4) {
+          acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lf[x][k]), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
+          acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kf[x][k]), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
+        } else {
+          acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[x][k]), __builtin_bit_cast(bf16x8, qf[k]), acc, 0, 0, 0);
+        }
+      };
+#pragma unroll
+      for (int k = 0; k < KS; ++k) read_row(0, k);
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(all) == ~0ull, 1)) {
+        // every row sees every key: a block's products with the weights of the one before, in the program's order
+        constexpr int N = 2 * KB;
+        f32x16 acc[2];
+#pragma unroll
+        for (int n = 0; n <= N; ++n)
 #pragma unroll
           for (int k = 0; k < KS; ++k) {
-            if constexpr (Q4) {
-              acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lf[x][k]), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
-              acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kf[x][k]), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
-            } else {
-              acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[x][k]), __builtin_bit_cast(bf16x8, qf[k]), acc, 0, 0, 0);
+            if (n < N) {
+              score(n % KB, k, acc[n & 1]);
+              if (n == KB - 1) read_row(1, k);
             }
-          }
-          if (whole) {
+            if (n > 0) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) run[x][e] += fast_exp2(fmaf(acc[e], c2, off));
-          } else {
+              for (int e = k * 16 / KS; e < (k + 1) * 16 / KS; ++e)
+                run[(n - 1) % KB][e] += fast_exp2(fmaf(acc[(n - 1) & 1][e], c2[(n - 1) / KB], off[(n - 1) / KB]));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+      } else {
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          if (y) {
+#pragma unroll
+            for (int k = 0; k < KS; ++k) read_row(1, k);
+          }
+          const int behind = place[y] - window;
+          int at = 4 * half;
+          asm volatile("" : "+v"(at));
+#pragma unroll
+          for (int x = 0; x < KB; ++x) {
+            if (__builtin_amdgcn_ballot_w64((key0[x] <= place[y]) & ((key0[x] + 31 > behind) | (key0[x] < first))) == 0) continue;
+            f32x16 acc;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) score(x, k, acc);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-              const int j = k0 + 8 * (e >> 2) + 4 * half + (e & 3);
-              run[x][e] += (j <= place) & ((j > behind) | (j < a.w.first)) ? fast_exp2(fmaf(acc[e], c2, off)) : 0.f;
+              const int j = key0[x] + 8 * (e >> 2) + at + (e & 3);
+              run[x][e] += (j <= place[y]) & ((j > behind) | (j < first)) ? fast_exp2(fmaf(acc[e], c2[y], off[y])) : 0.f;
               __builtin_amdgcn_sched_barrier(0);
             }
           }
