@@ -520,7 +520,7 @@ mixkv_status mixkv_paged_weights(const mixkv_paged_params *params, const mixkv_p
  * it (>= 1): longer heads are served, slower.  Workspace: mixkv_paged_evict_workspace_size bytes (0: NULL is accepted), 256-byte aligned, no initialisation.
  */
 typedef struct {
-  const float *weights;      /* [n_pages, page_rows], of the caches' pages */
+  const float *weights;      /* [n_pages, page_rows], of the caches' pages; 16-byte aligned */
   float *weights_into;       /* the same of the pages of `into` (may be the same array), or NULL */
   const int32_t *keep;       /* [batch, n_kv_heads]; below 0: none */
   int32_t *kept;             /* [batch, n_kv_heads, max_keep] places, ascending, then -1 */

@@ -22,90 +22,188 @@ struct EvictShape { int32_t max_keep, first, last; };
 
 constexpr int kRankThreads = 1024, kMoveThreads = 256;
 
-// The order key of row i of a head of `len` rows: 0 if it does not exist.
-__device__ __forceinline__ uint32_t row_key(const PShape &s, const EvictShape &e, const PCache &c, const EvictLayer &l, int u, int len, int i) {
-  const int id = page_at(s, c, u, i >> s.lp);
-  if (id < 0) return 0u;
-  if (i < e.first || i >= len - e.last) return order_key_u(INFINITY);
-  const float x = l.weights[((int64_t)id << s.lp) + (i & (s.P - 1))];
-  return order_key_u(x == x ? x : -INFINITY);
+// The order key of a row's weight: the first and the last rows are infinite, NaN ranks last.  (0 is left for rows that do not exist.)
+__device__ __forceinline__ uint32_t weight_key(const EvictShape &e, int len, int i, float x) {
+  return order_key_u(i < e.first || i >= len - e.last ? INFINITY : (x == x ? x : -INFINITY));
+}
+// The keys of four neighbouring rows (of one page) from row i on, a multiple of four.
+__device__ __forceinline__ u32x4 four_keys(const EvictShape &e, int len, int i, int id, f32x4 w) {
+  u32x4 k;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) k[j] = id >= 0 && i + j < len ? weight_key(e, len, i + j, w[j]) : 0u;
+  return k;
+}
+// The places of a head that are kept: how many, and what lies behind them in the list.
+__device__ __forceinline__ int kept_rows(const EvictShape &e, const EvictLayer &l, int u, int exist, int32_t *kept, int threads) {
+  const int keep = min(min(max(l.keep[u], 0), e.max_keep), exist);
+  if (threadIdx.x == 0) l.n_kept[u] = keep;
+  for (int i = keep + threadIdx.x; i < e.max_keep; i += threads) kept[i] = -1;
+  return keep;
 }
 
 // ------------------------------------------------------------------------------------------------
-// evict_rank_kernel: a workgroup to a head.  Rows are counted by their key, eight bits at a time, until the key of the last kept one is known;
-// rows of that key are taken from the front.
+// evict_rank_kernel: a workgroup to a head, its rows' keys in registers, a thread to EPT neighbouring ones; the best by the threshold search of mixkv_topsel.h.
 // ------------------------------------------------------------------------------------------------
-__global__ __launch_bounds__(kRankThreads) void evict_rank_kernel(PShape s, EvictShape ev, EvictTable tab) {
-  __shared__ int count[256], wsum[kRankThreads / 64][2], found[2], exist;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, u = blockIdx.x, layer = blockIdx.z;
+template <int THREADS, int EPT>
+__global__ __launch_bounds__(THREADS) void evict_rank_kernel(PShape s, EvictShape ev, EvictTable tab) {
+  __shared__ MsScratch sc;
+  __shared__ int exist_s[THREADS / 64];
+  const int tid = threadIdx.x, u = blockIdx.x, layer = blockIdx.z, base = tid * EPT;
+  const PCache c = tab.c[layer];
+  const EvictLayer l = tab.l[layer];
+  const int id = page_at(s, c, u, base >> s.lp);           // (of all of the thread's rows)
+  const float *w = l.weights + ((int64_t)max(id, 0) << s.lp) + (base & (s.P - 1));
+  f32x4 raw[EPT / 4];
+#pragma unroll
+  for (int e = 0; e < EPT / 4; ++e) raw[e] = reinterpret_cast<const f32x4 *>(w)[e];
+  const int len = head_rows(s, c, u);
+  uint32_t key[EPT];
+  KeyRange range;
+  int mine = 0;
+#pragma unroll
+  for (int e = 0; e < EPT; e += 4) {
+    const u32x4 k = four_keys(ev, len, base + e, id, raw[e / 4]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      key[e + j] = k[j];
+      mine += k[j] != 0 ? 1 : 0;
+      range.add_or_none(k[j], k[j] != 0);
+    }
+  }
+  thresholds_begin<THREADS>(range, sc);
+  mine = wave_reduce<WSum>(mine, 0);
+  if ((tid & 63) == 0) exist_s[tid >> 6] = mine;
+  __syncthreads();
+  int exist = 0;
+#pragma unroll
+  for (int i = 0; i < THREADS / 64; ++i) exist += exist_s[i];
+  int32_t *kept = l.kept + (int64_t)u * ev.max_keep;
+  const int keep = kept_rows(ev, l, u, exist, kept, THREADS);
+  if (keep == 0) return;                                // uniform
+  top_select_keys<THREADS, EPT>(key, keep, kept, nullptr, 0, sc, [&](int e) { return base + e; });
+}
+
+// ------------------------------------------------------------------------------------------------
+// Longer heads.  evict_keys_kernel writes their keys one after another, in as many workgroups as there is work for; evict_long_kernel, a workgroup to a head,
+// counts them by eleven bits, eleven, and ten until the key of the last kept one is known, and lists the kept ones: each wave has a range of rows of its own, so that
+// one fold over the waves gives all of them their places.
+// ------------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void evict_keys_kernel(PShape s, EvictShape ev, EvictTable tab, uint32_t *keys, int64_t stride) {
+  const int u = blockIdx.x, layer = blockIdx.z;
   const PCache c = tab.c[layer];
   const EvictLayer l = tab.l[layer];
   const int len = head_rows(s, c, u);
+  uint32_t *out = keys + (layer * (int64_t)s.units_per_layer + u) * stride;
+  for (int64_t i = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4; i < len; i += (int64_t)gridDim.y * 1024) {
+    const int id = page_at(s, c, u, (int)i >> s.lp);
+    const f32x4 w = *reinterpret_cast<const f32x4 *>(l.weights + ((int64_t)max(id, 0) << s.lp) + ((int)i & (s.P - 1)));
+    *reinterpret_cast<u32x4 *>(out + i) = four_keys(ev, len, (int)i, id, w);
+  }
+}
+
+constexpr int kLongBins = 2048, kLongWaves = kRankThreads / 64;
+
+__global__ __launch_bounds__(kRankThreads) void evict_long_kernel(PShape s, EvictShape ev, EvictTable tab, const uint32_t *keys, int64_t stride) {
+  __shared__ int hist[kLongBins], wsum[kLongWaves][2], found[2], total;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, u = blockIdx.x, layer = blockIdx.z;
+  const PCache c = tab.c[layer];
+  const EvictLayer l = tab.l[layer];
+  const uint32_t *in = keys + (layer * (int64_t)s.units_per_layer + u) * stride;
+  const int len = head_rows(s, c, u);
   int32_t *kept = l.kept + (int64_t)u * ev.max_keep;
-  if (tid == 0) exist = 0;
+  constexpr int U = 8;                                  // 16-byte loads of a thread under way
+  // every key of the workgroup's, 4 a thread and turn
+  auto each = [&](auto &&f) {
+    for (int i0 = 0; i0 < len; i0 += 4 * U * kRankThreads) {
+      u32x4 k[U];
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        const int i = i0 + (j * kRankThreads + tid) * 4;
+        k[j] = i < len ? *reinterpret_cast<const u32x4 *>(in + i) : u32x4{0u, 0u, 0u, 0u};
+      }
+#pragma unroll
+      for (int j = 0; j < U; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f(k[j][e]);
+    }
+  };
+  // The bin that the need-th largest counted key is in, and how many of that bin are needed; `found` holds the bin and the keys above it.
+  auto find = [&](int need) {
+    const int hi = kLongBins - 1 - 2 * tid, a = hist[hi], b = hist[hi - 1];        // from above
+    int wtot;
+    const int inc = wave_scan_incl_add(a + b, &wtot);
+    if (lane == 0) wsum[wave][0] = wtot;
+    __syncthreads();
+    int excl = inc - a - b, all = 0;
+#pragma unroll
+    for (int w = 0; w < kLongWaves; ++w) { excl += w < wave ? wsum[w][0] : 0; all += wsum[w][0]; }
+    if (tid == 0) total = all;
+    if (excl < need && need <= excl + a) { found[0] = hi; found[1] = excl; }
+    else if (excl + a < need && need <= excl + a + b) { found[0] = hi - 1; found[1] = excl + a; }
+    __syncthreads();
+  };
+  auto clear = [&]() {
+    hist[tid] = 0;
+    hist[tid + kRankThreads] = 0;
+    __syncthreads();
+  };
+  clear();
+  each([&](uint32_t k) { hist_add(hist, (int)(k >> 21), k != 0); });
   __syncthreads();
-  int mine = 0;
-  for (int i = tid; i < len; i += kRankThreads) mine += page_at(s, c, u, i >> s.lp) >= 0 ? 1 : 0;
-  mine = wave_reduce<WSum>(mine, 0);
-  if (lane == 0) atomicAdd(&exist, mine);
-  __syncthreads();
-  const int keep = min(min(max(l.keep[u], 0), ev.max_keep), exist);
-  if (tid == 0) l.n_kept[u] = keep;
-  for (int i = keep + tid; i < ev.max_keep; i += kRankThreads) kept[i] = -1;
+  find(0);
+  const int keep = kept_rows(ev, l, u, total, kept, kRankThreads);
   if (keep == 0) return;                                // uniform
-  int need = keep;
-  uint32_t prefix = 0;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) count[tid] = 0;
+  find(keep);
+  uint32_t prefix = (uint32_t)found[0] << 21;
+  int need = keep - found[1];
+#pragma unroll 1
+  for (int shift = 10; shift >= 0; shift -= 10) {       // bits 20 ... 10, then 9 ... 0
+    const int upper = shift == 10 ? 21 : 10;
+    const uint32_t mask = shift == 10 ? 2047u : 1023u;
     __syncthreads();
-    for (int i0 = 0; i0 < len; i0 += kRankThreads) {
-      const uint32_t k = i0 + tid < len ? row_key(s, ev, c, l, u, len, i0 + tid) : 0u;
-      hist_add(count, (k >> shift) & 255, k != 0 && (shift == 24 || k >> (shift + 8) == prefix >> (shift + 8)));
-    }
+    clear();
+    each([&](uint32_t k) { hist_add(hist, (int)((k >> shift) & mask), k >> upper == prefix >> upper && k != 0); });
     __syncthreads();
-    if (wave == 0) {                                    // the bin that the last kept key is in, from above, four bins a lane
-      int n[4], sum = 0;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) { n[k] = count[255 - 4 * lane - k]; sum += n[k]; }
-      int upto = sum;
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        const int x = __shfl_up(upto, off);
-        upto += lane >= off ? x : 0;
-      }
-      int above = upto - sum;
-      if (above < need && need <= upto) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (above < need && need <= above + n[k]) { found[0] = 255 - 4 * lane - k; found[1] = need - above; }
-          above += n[k];
-        }
-      }
-    }
-    __syncthreads();
+    find(need);
     prefix |= (uint32_t)found[0] << shift;
-    need = found[1];
-    __syncthreads();
+    need -= found[1];
   }
-  int at = 0, ties = 0;                                 // need of the rows with key == prefix, and all above it
-  for (int i0 = 0; i0 < len; i0 += kRankThreads) {
-    const uint32_t k = i0 + tid < len ? row_key(s, ev, c, l, u, len, i0 + tid) : 0u;
-    const bool tie = k == prefix;                       // (no key that is wanted is 0)
-    const uint64_t tb = __builtin_amdgcn_ballot_w64(tie), below = ((uint64_t)1 << lane) - 1;
-    if (lane == 0) wsum[wave][0] = __popcll(tb);
-    __syncthreads();
-    int t = ties + __popcll(tb & below), t_all = 0;
-    for (int w = 0; w < kRankThreads / 64; ++w) { t_all += wsum[w][0]; if (w < wave) t += wsum[w][0]; }
-    const bool take = k > prefix || (tie && t < need);
-    ties += t_all;
+  // ---- the keys above `prefix`, and the first `need` that are it: a wave's range of rows, 64 at a time, counted and then listed
+  const int per = ((len + kLongWaves - 1) / kLongWaves + 63) / 64 * 64, r0 = min(wave * per, len), r1 = min(r0 + per, len);
+  auto rows = [&](auto &&f) {
+    constexpr int V = 16;
+    for (int i0 = r0; i0 < r1; i0 += 64 * V) {
+      uint32_t k[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int i = i0 + 64 * j + lane;
+        k[j] = i < r1 ? in[i] : 0u;
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) f(k[j], i0 + 64 * j + lane);
+    }
+  };
+  int above = 0, ties = 0;
+  rows([&](uint32_t k, int) { above += __popcll(__builtin_amdgcn_ballot_w64(k > prefix)); ties += __popcll(__builtin_amdgcn_ballot_w64(k == prefix)); });
+  __syncthreads();
+  if (lane == 0) { wsum[wave][0] = above; wsum[wave][1] = ties; }
+  __syncthreads();
+  int at = 0, before = 0;
+#pragma unroll
+  for (int w = 0; w < kLongWaves; ++w) {
+    if (w < wave) { at += wsum[w][0]; before += wsum[w][1]; }
+  }
+  at += min(before, need);
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  rows([&](uint32_t k, int i) {
+    const uint64_t tb = __builtin_amdgcn_ballot_w64(k == prefix);
+    const bool take = k > prefix || (k == prefix && before + __popcll(tb & below) < need);
+    before += __popcll(tb);
     const uint64_t kb = __builtin_amdgcn_ballot_w64(take);
-    if (lane == 0) wsum[wave][1] = __popcll(kb);
-    __syncthreads();
-    int o = at + __popcll(kb & below), o_all = 0;
-    for (int w = 0; w < kRankThreads / 64; ++w) { o_all += wsum[w][1]; if (w < wave) o += wsum[w][1]; }
-    if (take && o < keep) kept[o] = i0 + tid;
-    at += o_all;
-  }
+    const int o = at + __popcll(kb & below);
+    if (take && o < keep) kept[o] = i;
+    at += __popcll(kb);
+  });
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -190,6 +288,15 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(PShape s, Evic
   }
 }
 
+// Heads that a workgroup holds in registers; longer ones' keys lie in the workspace, a head's one after another.  (The rule goes by the page table's width: a head
+// can be as long as that, whatever the host thinks.)
+constexpr int kRankRows = 16384;
+static int64_t key_stride(const PShape &s) { return (int64_t)s.max_pages * s.P; }
+static size_t evict_bytes(const PShape &s, int n_layers, int max_rows) {
+  (void)max_rows;
+  return key_stride(s) <= kRankRows ? 0 : (size_t)std::min(n_layers, kEvictLayers) * s.units_per_layer * key_stride(s) * sizeof(uint32_t);
+}
+
 }  // namespace mixkv
 
 extern "C" mixkv_status mixkv_paged_evict_workspace_size(const mixkv_paged_params *params, int32_t n_layers, int32_t max_rows, size_t *bytes) {
@@ -198,7 +305,7 @@ extern "C" mixkv_status mixkv_paged_evict_workspace_size(const mixkv_paged_param
   const mixkv_status st = make_pshape(params, &s);
   if (st != MIXKV_OK) return st;
   if (!bytes || n_layers < 1 || n_layers > MIXKV_MAX_LAYERS || max_rows < 1) return MIXKV_ERR_INVALID_ARG;
-  *bytes = 0;
+  *bytes = (evict_bytes(s, n_layers, max_rows) + 255) / 256 * 256;
   return MIXKV_OK;
 }
 
@@ -206,7 +313,6 @@ extern "C" mixkv_status mixkv_paged_evict(const mixkv_paged_params *params, cons
                                           const mixkv_paged_evict_layer *layers, int32_t n_layers, int32_t max_keep, int32_t keep_first, int32_t keep_last,
                                           int32_t max_rows, void *workspace, size_t workspace_bytes, void *hip_stream) {
   using namespace mixkv;
-  (void)workspace; (void)workspace_bytes;
   PShape s;
   mixkv_status st = make_pshape(params, &s);
   if (st != MIXKV_OK) return st;
@@ -220,9 +326,16 @@ extern "C" mixkv_status mixkv_paged_evict(const mixkv_paged_params *params, cons
     if (!t.K_pages || !t.V_pages || t.K_pages == t.V_pages || misaligned(t.K_pages, 16) || misaligned(t.V_pages, 16) || misaligned(t.K_bounds, 16)) return MIXKV_ERR_INVALID_ARG;
     if (!t.page_table || misaligned(t.page_table, 4) || t.page_table == caches[l].page_table) return MIXKV_ERR_INVALID_ARG;
     if (!d.weights || !d.keep || !d.kept || !d.n_kept) return MIXKV_ERR_INVALID_ARG;
-    if (misaligned(d.weights, 4) || misaligned(d.weights_into, 4) || misaligned(d.keep, 4) || misaligned(d.kept, 4) || misaligned(d.n_kept, 4)) return MIXKV_ERR_INVALID_ARG;
+    if (misaligned(d.weights, 16) || misaligned(d.weights_into, 4) || misaligned(d.keep, 4) || misaligned(d.kept, 4) || misaligned(d.n_kept, 4)) return MIXKV_ERR_INVALID_ARG;
     if (d.n_kept == caches[l].lengths || d.n_kept == d.keep) return MIXKV_ERR_INVALID_ARG;
   }
+  const size_t need = evict_bytes(s, n_layers, max_rows);
+  if (need > 0) {
+    if (!workspace || misaligned(workspace, 256)) return MIXKV_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return MIXKV_ERR_WORKSPACE_TOO_SMALL;
+  }
+  uint32_t *keys = static_cast<uint32_t *>(workspace);
+  const int64_t stride = key_stride(s);
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   const EvictShape ev{max_keep, keep_first, keep_last};
   for (int l0 = 0; l0 < n_layers; l0 += kEvictLayers) {
@@ -239,9 +352,18 @@ extern "C" mixkv_status mixkv_paged_evict(const mixkv_paged_params *params, cons
                           static_cast<char *>(z.K_bounds), z.page_table};
     }
     const dim3 heads((unsigned)s.units_per_layer, 1, (unsigned)nl);
-    hipLaunchKernelGGL(evict_rank_kernel, heads, dim3(kRankThreads), 0, stream, s, ev, t);
-    // a workgroup to a page, fewer than 2^32 threads
-    const int64_t pages = ((int64_t)max_keep + s.P - 1) / s.P, most = std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 23) / ((int64_t)s.units_per_layer * nl)));
+    // fewer than 2^32 threads
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 23) / ((int64_t)s.units_per_layer * nl)));
+    auto rank = [&](auto kern, int threads) { hipLaunchKernelGGL(kern, heads, dim3((unsigned)threads), 0, stream, s, ev, t); };
+    if (stride <= 1024) rank(evict_rank_kernel<256, 4>, 256);
+    else if (stride <= 4096) rank(evict_rank_kernel<512, 8>, 512);
+    else if (stride <= kRankRows) rank(evict_rank_kernel<1024, 16>, 1024);
+    else {
+      const int64_t y = std::min(most, std::max<int64_t>(1, ((int64_t)std::min<int64_t>(max_rows, stride) + 1023) / 1024));
+      hipLaunchKernelGGL(evict_keys_kernel, dim3((unsigned)s.units_per_layer, (unsigned)y, (unsigned)nl), dim3(256), 0, stream, s, ev, t, keys, stride);
+      hipLaunchKernelGGL(evict_long_kernel, heads, dim3(kRankThreads), 0, stream, s, ev, t, (const uint32_t *)keys, stride);
+    }
+    const int64_t pages = ((int64_t)max_keep + s.P - 1) / s.P;
     const dim3 grid((unsigned)s.units_per_layer, (unsigned)std::min(pages, most), (unsigned)nl);
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(kMoveThreads), 0, stream, s, ev, t); };
     if (s.q4) { if (s.D == 128) go(evict_move_kernel<MIXKV_BF16, 128, true>); else go(evict_move_kernel<MIXKV_BF16, 64, true>); }

@@ -96,7 +96,7 @@ def test_workspaces():
 
 
 @pytest.mark.parametrize("kw", [dict(keep=0), dict(keep=16 * 64 + 1), dict(first=-1), dict(last=-1), dict(rows=0), dict(n=0), dict(n=129), dict(null=True), dict(weights=0),
-                                dict(keep_=0), dict(kept=0), dict(n_kept=0), dict(weights=0x1002), dict(weights_into=0x1001), dict(kept=0x3002), dict(n_kept=0x50000),
+                                dict(keep_=0), dict(kept=0), dict(n_kept=0), dict(weights=0x1008), dict(weights_into=0x1001), dict(kept=0x3002), dict(n_kept=0x50000),
                                 dict(n_kept=0x2000)])
 def test_bad_evictions(kw):
     if "keep_" in kw:
