@@ -34,29 +34,162 @@ __device__ __forceinline__ u32x4 four_keys(const EvictShape &e, int len, int i, 
   return k;
 }
 // The places of a head that are kept: how many, and what lies behind them in the list.
-__device__ __forceinline__ int kept_rows(const EvictShape &e, const EvictLayer &l, int u, int exist, int32_t *kept, int threads) {
-  const int keep = min(min(max(l.keep[u], 0), e.max_keep), exist);
+__device__ __forceinline__ int kept_rows(const EvictShape &e, const EvictLayer &l, int u, int budget, int exist, int32_t *kept, int threads) {
+  const int keep = min(min(max(budget, 0), e.max_keep), exist);
   if (threadIdx.x == 0) l.n_kept[u] = keep;
   for (int i = keep + threadIdx.x; i < e.max_keep; i += threads) kept[i] = -1;
   return keep;
 }
 
+// The rows of a head that a workgroup does not hold in registers: counted by eleven bits of their keys, eleven, and ten until the key of the last kept one is known, and then
+// listed.  A wave has a range of rows of its own, so that one fold over the waves gives all of them their places.  COPIES of the counts: keys of one head often
+// agree in their leading bits.  keys_at(i, there): the keys of the rows i ... i + 3, i a multiple of four, 0 where !there.
+constexpr int kLongBins = 2048;
+template <int COPIES> struct LongScratch { int hist[kLongBins * COPIES], wsum[kMsMaxWaves][2], found[2], total; };
+
+template <int THREADS, int COPIES, class KeysAt>
+__device__ __forceinline__ void rank_long(const EvictShape &ev, const EvictLayer &l, int u, int len, int budget, LongScratch<COPIES> &sc, KeysAt &&keys_at) {
+  constexpr int W = THREADS / 64, BPT = kLongBins / THREADS, U = 8;   // U: groups of four rows of a thread under way
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int32_t *kept = l.kept + (int64_t)u * ev.max_keep;
+  // every key, 4 a thread and turn
+  auto each = [&](auto &&f) {
+    for (int i0 = 0; i0 < len; i0 += 4 * U * THREADS) {
+      u32x4 k[U];
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        const int i = i0 + (j * THREADS + tid) * 4;
+        k[j] = keys_at(min(i, (len - 1) & ~3), i < len);
+      }
+#pragma unroll
+      for (int j = 0; j < U; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f(k[j][e]);
+    }
+  };
+  // The bin that the need-th largest counted key is in, and the keys above it, to `found`; all that were counted to `total`.
+  auto find = [&](int need) {
+    int n[BPT], sum = 0;                                // bins from above
+#pragma unroll
+    for (int b = 0; b < BPT; ++b) {
+      n[b] = 0;
+#pragma unroll
+      for (int k = 0; k < COPIES; ++k) n[b] += sc.hist[(kLongBins - 1 - tid * BPT - b) * COPIES + k];
+      sum += n[b];
+    }
+    int wtot;
+    const int inc = wave_scan_incl_add(sum, &wtot);
+    if (lane == 0) sc.wsum[wave][0] = wtot;
+    __syncthreads();
+    int excl = inc - sum, all = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) { excl += w < wave ? sc.wsum[w][0] : 0; all += sc.wsum[w][0]; }
+    if (tid == 0) sc.total = all;
+#pragma unroll
+    for (int b = 0; b < BPT; ++b) {
+      if (excl < need && need <= excl + n[b]) { sc.found[0] = kLongBins - 1 - tid * BPT - b; sc.found[1] = excl; }
+      excl += n[b];
+    }
+    __syncthreads();
+  };
+  auto clear = [&]() {
+    for (int i = tid; i < kLongBins * COPIES; i += THREADS) sc.hist[i] = 0;
+    __syncthreads();
+  };
+  clear();
+  each([&](uint32_t k) { if (k != 0) atomicAdd(&sc.hist[(k >> 21) * COPIES + (lane & (COPIES - 1))], 1); });
+  __syncthreads();
+  find(0);
+  const int keep = kept_rows(ev, l, u, budget, sc.total, kept, THREADS);
+  if (keep == 0) return;                                // uniform
+  find(keep);
+  uint32_t prefix = (uint32_t)sc.found[0] << 21;
+  int need = keep - sc.found[1];
+#pragma unroll 1
+  for (int shift = 10; shift >= 0; shift -= 10) {       // bits 20 ... 10, then 9 ... 0
+    const int upper = shift == 10 ? 21 : 10;
+    const uint32_t mask = shift == 10 ? 2047u : 1023u;
+    __syncthreads();
+    clear();
+    each([&](uint32_t k) { if (k >> upper == prefix >> upper && k != 0) atomicAdd(&sc.hist[((k >> shift) & mask) * COPIES + (lane & (COPIES - 1))], 1); });
+    __syncthreads();
+    find(need);
+    prefix |= (uint32_t)sc.found[0] << shift;
+    need -= sc.found[1];
+  }
+  // ---- the keys above `prefix`, and the first `need` that are it: a wave's range of rows, 256 at a time, counted and then listed
+  const int per = ((len + W - 1) / W + 255) / 256 * 256, r0 = min(wave * per, len), r1 = min(r0 + per, len);
+  auto rows = [&](auto &&f) {
+    constexpr int V = 4;
+    for (int i0 = r0; i0 < r1; i0 += 256 * V) {
+      u32x4 k[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int i = i0 + 256 * j + 4 * lane;
+        k[j] = keys_at(min(i, (len - 1) & ~3), i < r1);
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) f(k[j], i0 + 256 * j + 4 * lane);
+    }
+  };
+  int above = 0, ties = 0;                              // the lane's
+  rows([&](const u32x4 &k, int) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { above += k[e] > prefix ? 1 : 0; ties += k[e] == prefix ? 1 : 0; }
+  });
+  above = wave_reduce<WSum>(above, 0);
+  ties = wave_reduce<WSum>(ties, 0);
+  __syncthreads();
+  if (lane == 0) { sc.wsum[wave][0] = above; sc.wsum[wave][1] = ties; }
+  __syncthreads();
+  int at = 0, before = 0;                               // kept rows, and rows of the last key, in front of the wave's next ones
+#pragma unroll
+  for (int w = 0; w < W; ++w)
+    if (w < wave) { at += sc.wsum[w][0]; before += sc.wsum[w][1]; }
+  at += min(before, need);
+  rows([&](const u32x4 &k, int i) {
+    int a = 0, t = 0, wa, wt;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { a += k[e] > prefix ? 1 : 0; t += k[e] == prefix ? 1 : 0; }
+    const int ia = wave_scan_incl_add(a, &wa), it = wave_scan_incl_add(t, &wt);
+    int tie = before + it - t, o = at + (ia - a) + (min(tie, need) - min(before, need));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool last = k[e] == prefix, take = k[e] > prefix || (last && tie < need);
+      tie += last ? 1 : 0;
+      if (take && o < keep) kept[o] = i + e;
+      o += take ? 1 : 0;
+    }
+    at += wa + (min(before + wt, need) - min(before, need));
+    before += wt;
+  });
+}
+
 // ------------------------------------------------------------------------------------------------
-// evict_rank_kernel: a workgroup to a head, its rows' keys in registers, a thread to EPT neighbouring ones; the best by the threshold search of mixkv_topsel.h.
+// evict_rank_kernel: a workgroup to a head, its rows' keys in registers, a thread to EPT neighbouring ones; the best by the threshold search of mixkv_topsel.h.  Heads that
+// are longer than the host said are counted from memory.
 // ------------------------------------------------------------------------------------------------
 template <int THREADS, int EPT>
 __global__ __launch_bounds__(THREADS) void evict_rank_kernel(PShape s, EvictShape ev, EvictTable tab) {
-  __shared__ MsScratch sc;
+  __shared__ union { MsScratch ms; LongScratch<1> lg; } sc;
   __shared__ int exist_s[THREADS / 64];
   const int tid = threadIdx.x, u = blockIdx.x, layer = blockIdx.z, base = tid * EPT;
   const PCache c = tab.c[layer];
   const EvictLayer l = tab.l[layer];
   const int id = page_at(s, c, u, base >> s.lp);           // (of all of the thread's rows)
+  const int len = head_rows(s, c, u), budget = l.keep[u];
   const float *w = l.weights + ((int64_t)max(id, 0) << s.lp) + (base & (s.P - 1));
   f32x4 raw[EPT / 4];
 #pragma unroll
   for (int e = 0; e < EPT / 4; ++e) raw[e] = reinterpret_cast<const f32x4 *>(w)[e];
-  const int len = head_rows(s, c, u);
+  if (len > THREADS * EPT) {
+    rank_long<THREADS, 1>(ev, l, u, len, budget, sc.lg, [&](int i, bool there) {
+      const int at = page_at(s, c, u, i >> s.lp);
+      const f32x4 x = *reinterpret_cast<const f32x4 *>(l.weights + ((int64_t)max(at, 0) << s.lp) + (i & (s.P - 1)));
+      return four_keys(ev, len, i, there ? at : -1, x);
+    });
+    return;
+  }
   uint32_t key[EPT];
   KeyRange range;
   int mine = 0;
@@ -70,7 +203,7 @@ __global__ __launch_bounds__(THREADS) void evict_rank_kernel(PShape s, EvictShap
       range.add_or_none(k[j], k[j] != 0);
     }
   }
-  thresholds_begin<THREADS>(range, sc);
+  thresholds_begin<THREADS>(range, sc.ms);
   mine = wave_reduce<WSum>(mine, 0);
   if ((tid & 63) == 0) exist_s[tid >> 6] = mine;
   __syncthreads();
@@ -78,223 +211,278 @@ __global__ __launch_bounds__(THREADS) void evict_rank_kernel(PShape s, EvictShap
 #pragma unroll
   for (int i = 0; i < THREADS / 64; ++i) exist += exist_s[i];
   int32_t *kept = l.kept + (int64_t)u * ev.max_keep;
-  const int keep = kept_rows(ev, l, u, exist, kept, THREADS);
+  const int keep = kept_rows(ev, l, u, budget, exist, kept, THREADS);
   if (keep == 0) return;                                // uniform
-  top_select_keys<THREADS, EPT>(key, keep, kept, nullptr, 0, sc, [&](int e) { return base + e; });
+  top_select_keys<THREADS, EPT>(key, keep, kept, nullptr, 0, sc.ms, [&](int e) { return base + e; });
 }
 
 // ------------------------------------------------------------------------------------------------
-// Longer heads.  evict_keys_kernel writes their keys one after another, in as many workgroups as there is work for; evict_long_kernel, a workgroup to a head,
-// counts them by eleven bits, eleven, and ten until the key of the last kept one is known, and lists the kept ones: each wave has a range of rows of its own, so that
-// one fold over the waves gives all of them their places.
+// Longer heads.  evict_keys_kernel writes their keys one after another, in as many workgroups as there is work for; evict_long_kernel ranks them, a workgroup to a head.
 // ------------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void evict_keys_kernel(PShape s, EvictShape ev, EvictTable tab, uint32_t *keys, int64_t stride) {
   const int u = blockIdx.x, layer = blockIdx.z;
   const PCache c = tab.c[layer];
   const EvictLayer l = tab.l[layer];
-  const int len = head_rows(s, c, u);
+  const int len = (int)min((int64_t)head_rows(s, c, u), stride);
   uint32_t *out = keys + (layer * (int64_t)s.units_per_layer + u) * stride;
   for (int64_t i = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4; i < len; i += (int64_t)gridDim.y * 1024) {
     const int id = page_at(s, c, u, (int)i >> s.lp);
     const f32x4 w = *reinterpret_cast<const f32x4 *>(l.weights + ((int64_t)max(id, 0) << s.lp) + ((int)i & (s.P - 1)));
-    *reinterpret_cast<u32x4 *>(out + i) = four_keys(ev, len, (int)i, id, w);
+    *reinterpret_cast<u32x4 *>(out + i) = four_keys(ev, head_rows(s, c, u), (int)i, id, w);
   }
 }
-
-constexpr int kLongBins = 2048, kLongWaves = kRankThreads / 64;
 
 __global__ __launch_bounds__(kRankThreads) void evict_long_kernel(PShape s, EvictShape ev, EvictTable tab, const uint32_t *keys, int64_t stride) {
-  __shared__ int hist[kLongBins], wsum[kLongWaves][2], found[2], total;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, u = blockIdx.x, layer = blockIdx.z;
+  __shared__ LongScratch<8> sc;
+  const int u = blockIdx.x, layer = blockIdx.z;
   const PCache c = tab.c[layer];
   const EvictLayer l = tab.l[layer];
-  const uint32_t *in = keys + (layer * (int64_t)s.units_per_layer + u) * stride;
-  const int len = head_rows(s, c, u);
-  int32_t *kept = l.kept + (int64_t)u * ev.max_keep;
-  constexpr int U = 8;                                  // 16-byte loads of a thread under way
-  // every key of the workgroup's, 4 a thread and turn
-  auto each = [&](auto &&f) {
-    for (int i0 = 0; i0 < len; i0 += 4 * U * kRankThreads) {
-      u32x4 k[U];
-#pragma unroll
-      for (int j = 0; j < U; ++j) {
-        const int i = i0 + (j * kRankThreads + tid) * 4;
-        k[j] = i < len ? *reinterpret_cast<const u32x4 *>(in + i) : u32x4{0u, 0u, 0u, 0u};
-      }
-#pragma unroll
-      for (int j = 0; j < U; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f(k[j][e]);
-    }
-  };
-  // The bin that the need-th largest counted key is in, and how many of that bin are needed; `found` holds the bin and the keys above it.
-  auto find = [&](int need) {
-    const int hi = kLongBins - 1 - 2 * tid, a = hist[hi], b = hist[hi - 1];        // from above
-    int wtot;
-    const int inc = wave_scan_incl_add(a + b, &wtot);
-    if (lane == 0) wsum[wave][0] = wtot;
-    __syncthreads();
-    int excl = inc - a - b, all = 0;
-#pragma unroll
-    for (int w = 0; w < kLongWaves; ++w) { excl += w < wave ? wsum[w][0] : 0; all += wsum[w][0]; }
-    if (tid == 0) total = all;
-    if (excl < need && need <= excl + a) { found[0] = hi; found[1] = excl; }
-    else if (excl + a < need && need <= excl + a + b) { found[0] = hi - 1; found[1] = excl + a; }
-    __syncthreads();
-  };
-  auto clear = [&]() {
-    hist[tid] = 0;
-    hist[tid + kRankThreads] = 0;
-    __syncthreads();
-  };
-  clear();
-  each([&](uint32_t k) { hist_add(hist, (int)(k >> 21), k != 0); });
-  __syncthreads();
-  find(0);
-  const int keep = kept_rows(ev, l, u, total, kept, kRankThreads);
-  if (keep == 0) return;                                // uniform
-  find(keep);
-  uint32_t prefix = (uint32_t)found[0] << 21;
-  int need = keep - found[1];
-#pragma unroll 1
-  for (int shift = 10; shift >= 0; shift -= 10) {       // bits 20 ... 10, then 9 ... 0
-    const int upper = shift == 10 ? 21 : 10;
-    const uint32_t mask = shift == 10 ? 2047u : 1023u;
-    __syncthreads();
-    clear();
-    each([&](uint32_t k) { hist_add(hist, (int)((k >> shift) & mask), k >> upper == prefix >> upper && k != 0); });
-    __syncthreads();
-    find(need);
-    prefix |= (uint32_t)found[0] << shift;
-    need -= found[1];
+  const int len = head_rows(s, c, u), budget = l.keep[u];
+  if (len <= stride) {
+    const uint32_t *in = keys + (layer * (int64_t)s.units_per_layer + u) * stride;
+    rank_long<kRankThreads, 8>(ev, l, u, len, budget, sc, [&](int i, bool there) { return there ? *reinterpret_cast<const u32x4 *>(in + i) : u32x4{0u, 0u, 0u, 0u}; });
+  } else {
+    rank_long<kRankThreads, 8>(ev, l, u, len, budget, sc, [&](int i, bool there) {
+      const int at = page_at(s, c, u, i >> s.lp);
+      const f32x4 x = *reinterpret_cast<const f32x4 *>(l.weights + ((int64_t)max(at, 0) << s.lp) + (i & (s.P - 1)));
+      return four_keys(ev, len, i, there ? at : -1, x);
+    });
   }
-  // ---- the keys above `prefix`, and the first `need` that are it: a wave's range of rows, 64 at a time, counted and then listed
-  const int per = ((len + kLongWaves - 1) / kLongWaves + 63) / 64 * 64, r0 = min(wave * per, len), r1 = min(r0 + per, len);
-  auto rows = [&](auto &&f) {
-    constexpr int V = 16;
-    for (int i0 = r0; i0 < r1; i0 += 64 * V) {
-      uint32_t k[V];
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int i = i0 + 64 * j + lane;
-        k[j] = i < r1 ? in[i] : 0u;
-      }
-#pragma unroll
-      for (int j = 0; j < V; ++j) f(k[j], i0 + 64 * j + lane);
-    }
-  };
-  int above = 0, ties = 0;
-  rows([&](uint32_t k, int) { above += __popcll(__builtin_amdgcn_ballot_w64(k > prefix)); ties += __popcll(__builtin_amdgcn_ballot_w64(k == prefix)); });
-  __syncthreads();
-  if (lane == 0) { wsum[wave][0] = above; wsum[wave][1] = ties; }
-  __syncthreads();
-  int at = 0, before = 0;
-#pragma unroll
-  for (int w = 0; w < kLongWaves; ++w) {
-    if (w < wave) { at += wsum[w][0]; before += wsum[w][1]; }
-  }
-  at += min(before, need);
-  const uint64_t below = ((uint64_t)1 << lane) - 1;
-  rows([&](uint32_t k, int i) {
-    const uint64_t tb = __builtin_amdgcn_ballot_w64(k == prefix);
-    const bool take = k > prefix || (k == prefix && before + __popcll(tb & below) < need);
-    before += __popcll(tb);
-    const uint64_t kb = __builtin_amdgcn_ballot_w64(take);
-    const int o = at + __popcll(kb & below);
-    if (take && o < keep) kept[o] = i;
-    at += __popcll(kb);
-  });
 }
 
 // ------------------------------------------------------------------------------------------------
-// evict_move_kernel: a workgroup to a page of `into`, D/16 lanes to a row.
+// evict_move_kernel: every second workgroup of a head moves keys, a page of `into` after another (its bounds and weights too), D/16 lanes to a row; the others move values.  The
+// chain of loads behind a row (its place, that place's page, the row) is walked one row ahead.
+// 4-bit values: a strip of `into` holds eight rows, which come from up to eight strips.  A lane takes 16 bytes of the strip, four elements of all eight rows, out of the same 16
+// bytes of theirs.
 // ------------------------------------------------------------------------------------------------
+// The smallest and the largest elements of 32 rows of every wave, D/16 lanes to a row, to the bounds of their page, whose rows `waves` neighbouring waves (1, 2 or 4) have.  The lanes
+// share the words of a row's two ends out by halves: with the lane 32, 16, ... away each gives the half that the other one keeps.
+__device__ __forceinline__ uint32_t least_of(const RunRange<MIXKV_BF16> &, uint32_t a, uint32_t b) {
+  typedef RunRange<MIXKV_BF16>::s16x2 P;
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(P, a), __builtin_bit_cast(P, b)));
+}
+__device__ __forceinline__ uint32_t least_of(const RunRange<MIXKV_F32> &, uint32_t a, uint32_t b) { return __float_as_uint(fminf(__uint_as_float(a), __uint_as_float(b))); }
+
+template <int DT, int D>
+__device__ __forceinline__ void store_page_bounds(char *dst, bool there, int waves, const RunRange<DT> &ra, const RunRange<DT> &rb, char (&red)[4][2 * D * (DT == MIXKV_BF16 ? 2 : 4)]) {
+  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RB = D * EB, NW = 8 * EB;   // NW: words of a lane's two runs and two ends
+  constexpr uint32_t other = DT == MIXKV_BF16 ? 0xffffffffu : 0x80000000u;               // (largest elements as smallest ones of the other sign)
+  const int lane = threadIdx.x & 63;
+  uint32_t w[NW];
+  constexpr int Q = NW / 4;
+#pragma unroll
+  for (int i = 0; i < Q; ++i) {
+    if constexpr (DT == MIXKV_BF16) {
+      w[i] = __builtin_bit_cast(uint32_t, ra.lo[i]); w[Q + i] = __builtin_bit_cast(uint32_t, rb.lo[i]);
+      w[2 * Q + i] = __builtin_bit_cast(uint32_t, ra.hi[i]) ^ other; w[3 * Q + i] = __builtin_bit_cast(uint32_t, rb.hi[i]) ^ other;
+    } else {
+      w[i] = __float_as_uint(ra.lo[i]); w[Q + i] = __float_as_uint(rb.lo[i]);
+      w[2 * Q + i] = __float_as_uint(ra.hi[i]) ^ other; w[3 * Q + i] = __float_as_uint(rb.hi[i]) ^ other;
+    }
+  }
+  int size = NW / 2;
+#pragma unroll
+  for (int off = 32; off >= LPR; off >>= 1, size >>= 1) {
+    const bool up = lane & off;
+#pragma unroll
+    for (int i = 0; i < size; ++i) {
+      const uint32_t keep = up ? w[size + i] : w[i], give = up ? w[i] : w[size + i];
+      w[i] = least_of(ra, keep, (uint32_t)__shfl_xor((int)give, off));
+    }
+  }
+  constexpr int C = NW * LPR / 64;                          // the words that are left
+  struct alignas(4 * C) Words { uint32_t w[C]; };
+  const bool high = lane & 32;
+  const int at = (high ? RB : 0) + (lane & 16 ? RB / 2 : 0) + 8 * EB * (lane % LPR) + (lane & 15) / LPR * C * 4, wave = threadIdx.x >> 6;
+  auto words = [&](char *p) -> Words & { return *reinterpret_cast<Words *>(p + at); };
+  Words v;
+  if (waves > 1) {                                          // uniform
+#pragma unroll
+    for (int i = 0; i < C; ++i) v.w[i] = w[i];
+    words(red[wave]) = v;
+    __syncthreads();
+    for (int k = 1; k < waves; ++k) {
+      v = words(red[(wave & -waves) + ((wave + k) & (waves - 1))]);
+#pragma unroll
+      for (int i = 0; i < C; ++i) w[i] = least_of(ra, w[i], v.w[i]);
+    }
+    __syncthreads();
+    there = there && (wave & (waves - 1)) == 0;
+  }
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    if (high) w[i] ^= other;
+    if constexpr (DT == MIXKV_BF16) w[i] = __builtin_bit_cast(uint32_t, RunRange<DT>::turn(__builtin_bit_cast(typename RunRange<DT>::s16x2, w[i])));
+    v.w[i] = w[i];
+  }
+  if (there) words(dst) = v;
+}
+
+// The eight elements of a word of codes.  The code's bits are the upper ones of 1 + code / 16.
+__device__ __forceinline__ void word_values(uint32_t w, float step, float base, float (&x)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    constexpr int top = 19;                                 // the lowest of the four
+    const int sh = code_shift(e);
+    x[e] = fmaf(step, __uint_as_float(((sh < top ? w << (top - sh) : w >> (sh - top)) & 0x00780000u) | 0x3f800000u), base);
+  }
+}
+
+struct From { int page, row; };            // where a row comes from; page -1: there is none
+
 template <int DT, int D, bool Q4>
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(PShape s, EvictShape ev, EvictTable tab) {
-  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RS = kMoveThreads / LPR, RB = D * EB, RUNS = D / 8;
-  __shared__ uint32_t words[Q4 ? RS * RUNS : 1];           // codes of the value rows of a pass, a word per eight elements
-  __shared__ __align__(16) char red[4][2 * RB];
-  const int tid = threadIdx.x, j = tid % LPR, slot = tid / LPR, u = blockIdx.x, layer = blockIdx.z;
+  constexpr int EB = DT == MIXKV_BF16 ? 2 : 4, LPR = D / 16, RB = D * EB, NG = D / 32;
+  const int tid = threadIdx.x, lane = tid & 63, j = tid % LPR, u = blockIdx.x, layer = blockIdx.z;
   const PCache c = tab.c[layer];
   const EvictLayer l = tab.l[layer];
+  __shared__ __align__(16) char red[4][2 * RB];
   const PCache to{l.K, l.V, l.bounds, l.table, nullptr};
   const int32_t *kept = l.kept + (int64_t)u * ev.max_keep;
   const int n = l.n_kept[u];
-  for (int pg = blockIdx.y; (int64_t)pg << s.lp < n; pg += gridDim.y) {
-    const int id = page_at(s, to, u, pg);
-    if (id < 0) continue;                                  // uniform
-    const int first = pg << s.lp, rows = min(n - first, s.P);
-    char *kp = to.K + (int64_t)id * s.page_bytes, *vp = to.V + (int64_t)id * s.page_bytes;
+  auto place_of = [&](int i) { return i < n ? kept[i] : -1; };                  // of the i-th kept row
+  auto from_of = [&](int place) {                                             // (no place: none)
+    From f;
+    f.page = place >= 0 ? page_at(s, c, u, place >> s.lp) : -1;
+    f.row = place & (s.P - 1);
+    return f;
+  };
+
+  const int worker = blockIdx.y >> 1, workers = gridDim.y >> 1;
+  const bool keys = (blockIdx.y & 1) == 0;
+  if (keys || !Q4) {
+    // A wave has the 32 rows of a turn's 128 that are its own, RS at a time, U times RS under way.
+    constexpr int RS = 64 / LPR, U = D == 128 && DT == MIXKV_BF16 ? 4 : 2, PARTS = 32 / (RS * U);
+    const int slot = lane / LPR, wave = tid >> 6;
+    const bool bounds = keys && c.bounds && to.bounds;       // (uniform over the launch)
+    const float *w_in = keys && l.into ? l.weights : nullptr;
+    const char *from_pool = keys ? c.K : c.V;
+    char *to_pool = keys ? to.K : to.V;
+    auto row_at = [&](int q) { return (q / PARTS * workers + worker) * 128 + wave * 32 + q % PARTS * (RS * U) + slot; };    // of the wave's part q
+    From f[U];
+    int next[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) next[k] = place_of(row_at(0) + k * RS);
+#pragma unroll
+    for (int k = 0; k < U; ++k) f[k] = from_of(next[k]);
+#pragma unroll
+    for (int k = 0; k < U; ++k) next[k] = place_of(row_at(1) + k * RS);
     RunRange<DT> ra, rb;
-    ra.none(); rb.none();
-    for (int s0 = 0; s0 < rows; s0 += RS) {
-      const int r = s0 + slot;
-      const bool live = r < rows;
-      const int i = live ? kept[first + r] : 0, from = page_at(s, c, u, i >> s.lp), fr = i & (s.P - 1);
-      const bool there = live && from >= 0;                // (rows of no page are never kept)
-      const char *ks = c.K + (int64_t)max(from, 0) * s.page_bytes, *vs = c.V + (int64_t)max(from, 0) * s.page_bytes;
-      Run<DT> ka{}, kb{};
-      if constexpr (!Q4) {
-        if (there) {
-          const int64_t src = (int64_t)fr * RB + 8 * EB * j, dst = (int64_t)r * RB + 8 * EB * j;
-          Run<DT> va, vb;
-          ka.load(ks + src); kb.load(ks + src + RB / 2);
-          va.load(vs + src); vb.load(vs + src + RB / 2);
-          ka.store(kp + dst); kb.store(kp + dst + RB / 2);
-          va.store(vp + dst); vb.store(vp + dst + RB / 2);
-        }
-      } else {
-        if (there) {
-          const Place4<D> a(j, fr, s.P), z(j, r, s.P);
-          char *ksm = const_cast<char *>(ks), *vsm = const_cast<char *>(vs);
-          const u32x2 kw = *a.key_words(ksm), sc = *a.key_scales(ksm);
-          *z.key_words(kp) = kw;
-          if ((j & 3) == 0) *z.key_scales(kp) = sc;
-          if (c.bounds) {
-            float x0[8], x1[8];
+    for (int q = 0; (q / PARTS * workers + worker) * 128 < n; ++q) {   // (uniform over the workgroup)
+      const int i0 = row_at(q), id = (i0 & -32) < n ? page_at(s, to, u, i0 >> s.lp) : -1;
+      Run<DT> ka[U], kb[U];
+      u32x2 kw[U], sc[U];
+      float w[U];
+      // (a lane without a row reads the first page's, and stores nothing)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              x0[e] = code_value((kw[0] >> code_shift(e)) & 15u, f16_value(sc[0] & 0xffffu), f16_value(sc[0] >> 16));
-              x1[e] = code_value((kw[1] >> code_shift(e)) & 15u, f16_value(sc[1] & 0xffffu), f16_value(sc[1] >> 16));
+      for (int k = 0; k < U; ++k) {
+        const char *ks = from_pool + (int64_t)max(f[k].page, 0) * s.page_bytes;
+        if constexpr (!Q4) {
+          const char *src = ks + (int64_t)f[k].row * RB + 8 * EB * j;
+          ka[k].load(src); kb[k].load(src + RB / 2);
+        } else {
+          const Place4<D> a(j, f[k].row, s.P);
+          kw[k] = *a.key_words(const_cast<char *>(ks));
+          sc[k] = *a.key_scales(const_cast<char *>(ks));
+        }
+        if (w_in) w[k] = w_in[((int64_t)max(f[k].page, 0) << s.lp) + f[k].row];
+      }
+      From f1[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) f1[k] = from_of(next[k]);
+#pragma unroll
+      for (int k = 0; k < U; ++k) next[k] = place_of(row_at(q + 2) + k * RS);
+      if (PARTS == 1 || q % PARTS == 0) { ra.none(); rb.none(); }
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int r = (i0 + k * RS) & (s.P - 1);
+        if (id >= 0 && f[k].page >= 0) {
+          char *kp = to_pool + (int64_t)id * s.page_bytes;
+          if constexpr (!Q4) {
+            char *dst = kp + (int64_t)r * RB + 8 * EB * j;
+            ka[k].store(dst); kb[k].store(dst + RB / 2);
+          } else {
+            const Place4<D> z(j, r, s.P);
+            *z.key_words(kp) = kw[k];
+            if ((j & 3) == 0) *z.key_scales(kp) = sc[k];
+            if (bounds) {
+              float x0[8], x1[8];
+              word_values(kw[k][0], f16_value(sc[k][0] & 0xffffu), f16_value(sc[k][0] >> 16), x0);
+              word_values(kw[k][1], f16_value(sc[k][1] & 0xffffu), f16_value(sc[k][1] >> 16), x1);
+              ka[k].set(x0); kb[k].set(x1);
             }
-            ka.set(x0); kb.set(x1);
           }
-          if ((j & 3) == 0) {
-            const uint16_t *p0 = a.value_scale(vsm, a.ga()), *p1 = a.value_scale(vsm, a.gb());
-            uint16_t *q0 = z.value_scale(vp, z.ga()), *q1 = z.value_scale(vp, z.gb());
-            q0[0] = p0[0]; q0[8] = p0[8];
-            q1[0] = p1[0]; q1[8] = p1[8];
-          }
-          const uint32_t *strip = a.strip_words(vsm), sh = code_shift(a.e);
-          uint32_t w0 = 0, w1 = 0;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            w0 |= ((strip[Place4<D>::word_of(8 * j + e)] >> sh) & 15u) << code_shift(e);
-            w1 |= ((strip[Place4<D>::word_of(D / 2 + 8 * j + e)] >> sh) & 15u) << code_shift(e);
-          }
-          words[slot * RUNS + j] = w0;
-          words[slot * RUNS + LPR + j] = w1;
+          if (bounds) { ra.add(ka[k]); rb.add(kb[k]); }
+          if (w_in && j == 0) l.into[((int64_t)id << s.lp) + r] = w[k];
         }
-        __syncthreads();
-        store_strips<D, RS, kMoveThreads>(vp, words, s0, 0, rows);
-        __syncthreads();
+        f[k] = f1[k];
       }
-      if (there) {
-        if (c.bounds && to.bounds) { ra.add(ka); rb.add(kb); }
-        if (l.into && j == 0) l.into[((int64_t)id << s.lp) + r] = l.weights[((int64_t)from << s.lp) + fr];
-      }
+      if (bounds && (q + 1) % PARTS == 0) store_page_bounds<DT, D>(to.bounds + (int64_t)id * 2 * RB, id >= 0, s.P >> 5, ra, rb, red);
     }
-    if (c.bounds && to.bounds) store_bounds<DT, D>(to.bounds + (int64_t)id * 2 * RB, ra, rb, red, false);   // uniform
+  } else {
+    // a wave to the strips of half a tile of 32 rows (D = 128), or of a whole one
+    constexpr int LS = D / 4, SW = 64 / LS, WT = 4 / SW;     // lanes of a strip, strips of a wave, waves of a tile
+    const int wave = tid >> 6, part = wave % WT, step = workers * (4 / WT), tiles = (n + 31) >> 5;
+    const int l32 = lane & 31, sl = part * SW + lane / LS, at = lane % LS;
+    int t = worker * (4 / WT) + wave / WT;
+    From f = from_of(place_of(t < tiles ? t * 32 + l32 : INT32_MAX));           // lane i: the tile's row i
+    int next = tiles - t > step ? place_of((t + step) * 32 + l32) : -1;
+    while (t < tiles) {
+      const int id = page_at(s, to, u, (t * 32) >> s.lp);
+      const From f1 = from_of(next);
+      next = tiles - t > 2 * (int64_t)step ? place_of((t + 2 * step) * 32 + l32) : -1;
+      if (id >= 0) {                                         // uniform over the wave
+        char *vp = to.V + (int64_t)id * s.page_bytes;
+        const int r0 = (t * 32) & (s.P - 1);
+        u32x4 *dst = reinterpret_cast<u32x4 *>(reinterpret_cast<uint32_t *>(vp) + ((r0 >> 5) * 4 + sl) * D + 4 * at);
+        u32x4 x[8];
+        int sh[8];
+        bool full = true;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int from = 4 * sl + (e >> 1) + 16 * (e & 1), page = __shfl(f.page, from), row = __shfl(f.row, from);
+          sh[e] = page >= 0 ? code_shift(2 * (row & 3) + ((row >> 4) & 1)) : -1;
+          full = full && page >= 0;
+          x[e] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const uint32_t *>(c.V + (int64_t)max(page, 0) * s.page_bytes) + ((row >> 5) * 4 + ((row & 15) >> 2)) * D + 4 * at);
+        }
+        // steps and bases: a lane to a row of the wave's strips and a group
+        const int row_s = lane / NG, g = lane % NG, strip_s = row_s / 8, e_s = row_s % 8;
+        const int from = 4 * (part * SW + strip_s) + (e_s >> 1) + 16 * (e_s & 1), page = __shfl(f.page, from), row = __shfl(f.row, from);
+        if (page >= 0) {
+          const Place4<D> pa(0, row, s.P), pz(0, r0 + from, s.P);
+          const uint16_t *p = pa.value_scale(c.V + (int64_t)page * s.page_bytes, g);
+          uint16_t *z = pz.value_scale(vp, g);
+          z[0] = p[0];
+          z[8] = p[8];
+        }
+        u32x4 w = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) w[k] |= sh[e] >= 0 ? ((x[e][k] >> sh[e]) & 15u) << code_shift(e) : 0u;
+        if (!full) {                                         // codes of rows that are not written stay
+          const u32x4 old = *dst;
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] |= sh[e] >= 0 ? 0u : old[k] & (15u << code_shift(e));
+        }
+        *dst = w;
+      }
+      f = f1;
+      if (tiles - t <= step) break;
+      t += step;
+    }
   }
 }
 
-// Heads that a workgroup holds in registers; longer ones' keys lie in the workspace, a head's one after another.  (The rule goes by the page table's width: a head
-// can be as long as that, whatever the host thinks.)
+// Heads that a workgroup holds in registers, as long as the host says; longer ones' keys lie in the workspace, a head's one after another.
 constexpr int kRankRows = 16384;
-static int64_t key_stride(const PShape &s) { return (int64_t)s.max_pages * s.P; }
+static int64_t most_rows(const PShape &s, int max_rows) { return std::min<int64_t>(max_rows, (int64_t)s.max_pages * s.P); }
+static int64_t key_stride(const PShape &s, int max_rows) { return (most_rows(s, max_rows) + 3) / 4 * 4; }
 static size_t evict_bytes(const PShape &s, int n_layers, int max_rows) {
-  (void)max_rows;
-  return key_stride(s) <= kRankRows ? 0 : (size_t)std::min(n_layers, kEvictLayers) * s.units_per_layer * key_stride(s) * sizeof(uint32_t);
+  return most_rows(s, max_rows) <= kRankRows ? 0 : (size_t)std::min(n_layers, kEvictLayers) * s.units_per_layer * key_stride(s, max_rows) * sizeof(uint32_t);
 }
 
 }  // namespace mixkv
@@ -335,7 +523,7 @@ extern "C" mixkv_status mixkv_paged_evict(const mixkv_paged_params *params, cons
     if (workspace_bytes < need) return MIXKV_ERR_WORKSPACE_TOO_SMALL;
   }
   uint32_t *keys = static_cast<uint32_t *>(workspace);
-  const int64_t stride = key_stride(s);
+  const int64_t rows = most_rows(s, max_rows), stride = key_stride(s, max_rows);
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   const EvictShape ev{max_keep, keep_first, keep_last};
   for (int l0 = 0; l0 < n_layers; l0 += kEvictLayers) {
@@ -355,16 +543,18 @@ extern "C" mixkv_status mixkv_paged_evict(const mixkv_paged_params *params, cons
     // fewer than 2^32 threads
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 23) / ((int64_t)s.units_per_layer * nl)));
     auto rank = [&](auto kern, int threads) { hipLaunchKernelGGL(kern, heads, dim3((unsigned)threads), 0, stream, s, ev, t); };
-    if (stride <= 1024) rank(evict_rank_kernel<256, 4>, 256);
-    else if (stride <= 4096) rank(evict_rank_kernel<512, 8>, 512);
-    else if (stride <= kRankRows) rank(evict_rank_kernel<1024, 16>, 1024);
+    if (rows <= 1024) rank(evict_rank_kernel<256, 4>, 256);
+    else if (rows <= 4096) rank(evict_rank_kernel<512, 8>, 512);
+    else if (rows <= kRankRows) rank(evict_rank_kernel<1024, 16>, 1024);
     else {
-      const int64_t y = std::min(most, std::max<int64_t>(1, ((int64_t)std::min<int64_t>(max_rows, stride) + 1023) / 1024));
+      const int64_t y = std::min(most, std::max<int64_t>(1, (rows + 1023) / 1024));
       hipLaunchKernelGGL(evict_keys_kernel, dim3((unsigned)s.units_per_layer, (unsigned)y, (unsigned)nl), dim3(256), 0, stream, s, ev, t, keys, stride);
       hipLaunchKernelGGL(evict_long_kernel, heads, dim3(kRankThreads), 0, stream, s, ev, t, (const uint32_t *)keys, stride);
     }
-    const int64_t pages = ((int64_t)max_keep + s.P - 1) / s.P;
-    const dim3 grid((unsigned)s.units_per_layer, (unsigned)std::min(pages, most), (unsigned)nl);
+    // Workers of a head: one for 32 rows, as long as all of them are on the chip together.
+    // Workgroups of a head: one for 128 rows of keys and one for as many of values, as long as all of them are on the chip together.
+    const int64_t work = ((int64_t)max_keep + 127) / 128, fit = std::max<int64_t>(1, 4096 / ((int64_t)s.units_per_layer * nl));
+    const dim3 grid((unsigned)s.units_per_layer, (unsigned)(2 * std::min(work, std::min(fit, (most + 1) / 2))), (unsigned)nl);
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(kMoveThreads), 0, stream, s, ev, t); };
     if (s.q4) { if (s.D == 128) go(evict_move_kernel<MIXKV_BF16, 128, true>); else go(evict_move_kernel<MIXKV_BF16, 64, true>); }
     else if (params->dtype == MIXKV_BF16) { if (s.D == 128) go(evict_move_kernel<MIXKV_BF16, 128, false>); else go(evict_move_kernel<MIXKV_BF16, 64, false>); }
