@@ -41,15 +41,19 @@ __device__ __forceinline__ int kept_rows(const EvictShape &e, const EvictLayer &
   return keep;
 }
 
-// The rows of a head that a workgroup does not hold in registers: counted by eleven bits of their keys, eleven, and ten until the key of the last kept one is known, and then
-// listed.  A wave has a range of rows of its own, so that one fold over the waves gives all of them their places.  COPIES of the counts: keys of one head often
-// agree in their leading bits.  keys_at(i, there): the keys of the rows i ... i + 3, i a multiple of four, 0 where !there.
+// A head that is longer than the host said, by one workgroup from memory: its keys counted by eleven bits, eleven, and ten until the key of the last kept one is known, and then
+// listed.  A wave has a range of rows of its own, so that one fold over the waves gives all of them their places.
 constexpr int kLongBins = 2048;
-template <int COPIES> struct LongScratch { int hist[kLongBins * COPIES], wsum[kMsMaxWaves][2], found[2], total; };
+struct LongScratch { int hist[kLongBins], wsum[kMsMaxWaves][2], found[2], total; };
 
-template <int THREADS, int COPIES, class KeysAt>
-__device__ __forceinline__ void rank_long(const EvictShape &ev, const EvictLayer &l, int u, int len, int budget, LongScratch<COPIES> &sc, KeysAt &&keys_at) {
+template <int THREADS>
+__device__ __forceinline__ void rank_long(const PShape &s, const PCache &c, const EvictShape &ev, const EvictLayer &l, int u, int len, int budget, LongScratch &sc) {
   constexpr int W = THREADS / 64, BPT = kLongBins / THREADS, U = 8;   // U: groups of four rows of a thread under way
+  auto keys_at = [&](int i, bool there) {                             // of the rows i ... i + 3, i a multiple of four; 0 where !there
+    const int at = page_at(s, c, u, i >> s.lp);
+    const f32x4 x = *reinterpret_cast<const f32x4 *>(l.weights + ((int64_t)max(at, 0) << s.lp) + (i & (s.P - 1)));
+    return four_keys(ev, len, i, there ? at : -1, x);
+  };
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int32_t *kept = l.kept + (int64_t)u * ev.max_keep;
   // every key, 4 a thread and turn
@@ -72,9 +76,7 @@ __device__ __forceinline__ void rank_long(const EvictShape &ev, const EvictLayer
     int n[BPT], sum = 0;                                // bins from above
 #pragma unroll
     for (int b = 0; b < BPT; ++b) {
-      n[b] = 0;
-#pragma unroll
-      for (int k = 0; k < COPIES; ++k) n[b] += sc.hist[(kLongBins - 1 - tid * BPT - b) * COPIES + k];
+      n[b] = sc.hist[kLongBins - 1 - tid * BPT - b];
       sum += n[b];
     }
     int wtot;
@@ -93,11 +95,11 @@ __device__ __forceinline__ void rank_long(const EvictShape &ev, const EvictLayer
     __syncthreads();
   };
   auto clear = [&]() {
-    for (int i = tid; i < kLongBins * COPIES; i += THREADS) sc.hist[i] = 0;
+    for (int i = tid; i < kLongBins; i += THREADS) sc.hist[i] = 0;
     __syncthreads();
   };
   clear();
-  each([&](uint32_t k) { if (k != 0) atomicAdd(&sc.hist[(k >> 21) * COPIES + (lane & (COPIES - 1))], 1); });
+  each([&](uint32_t k) { if (k != 0) atomicAdd(&sc.hist[k >> 21], 1); });
   __syncthreads();
   find(0);
   const int keep = kept_rows(ev, l, u, budget, sc.total, kept, THREADS);
@@ -111,7 +113,7 @@ __device__ __forceinline__ void rank_long(const EvictShape &ev, const EvictLayer
     const uint32_t mask = shift == 10 ? 2047u : 1023u;
     __syncthreads();
     clear();
-    each([&](uint32_t k) { if (k >> upper == prefix >> upper && k != 0) atomicAdd(&sc.hist[((k >> shift) & mask) * COPIES + (lane & (COPIES - 1))], 1); });
+    each([&](uint32_t k) { if (k >> upper == prefix >> upper && k != 0) atomicAdd(&sc.hist[(k >> shift) & mask], 1); });
     __syncthreads();
     find(need);
     prefix |= (uint32_t)sc.found[0] << shift;
@@ -171,7 +173,7 @@ __device__ __forceinline__ void rank_long(const EvictShape &ev, const EvictLayer
 // ------------------------------------------------------------------------------------------------
 template <int THREADS, int EPT>
 __global__ __launch_bounds__(THREADS) void evict_rank_kernel(PShape s, EvictShape ev, EvictTable tab) {
-  __shared__ union { MsScratch ms; LongScratch<1> lg; } sc;
+  __shared__ union { MsScratch ms; LongScratch lg; } sc;
   __shared__ int exist_s[THREADS / 64];
   const int tid = threadIdx.x, u = blockIdx.x, layer = blockIdx.z, base = tid * EPT;
   const PCache c = tab.c[layer];
@@ -183,11 +185,7 @@ __global__ __launch_bounds__(THREADS) void evict_rank_kernel(PShape s, EvictShap
 #pragma unroll
   for (int e = 0; e < EPT / 4; ++e) raw[e] = reinterpret_cast<const f32x4 *>(w)[e];
   if (len > THREADS * EPT) {
-    rank_long<THREADS, 1>(ev, l, u, len, budget, sc.lg, [&](int i, bool there) {
-      const int at = page_at(s, c, u, i >> s.lp);
-      const f32x4 x = *reinterpret_cast<const f32x4 *>(l.weights + ((int64_t)max(at, 0) << s.lp) + (i & (s.P - 1)));
-      return four_keys(ev, len, i, there ? at : -1, x);
-    });
+    rank_long<THREADS>(s, c, ev, l, u, len, budget, sc.lg);
     return;
   }
   uint32_t key[EPT];
@@ -217,36 +215,184 @@ __global__ __launch_bounds__(THREADS) void evict_rank_kernel(PShape s, EvictShap
 }
 
 // ------------------------------------------------------------------------------------------------
-// Longer heads.  evict_keys_kernel writes their keys one after another, in as many workgroups as there is work for; evict_long_kernel ranks them, a workgroup to a head.
+// Longer heads, a workgroup to a segment of one.  evict_count_kernel<0> writes the segment's keys one after another and counts them by their upper eleven bits.
+// evict_count_kernel<1> adds up the counts of the head's segments, finds the eleven bits of the last kept key, and counts the keys that have them by the next eleven; <2> likewise by
+// the last ten.  evict_list_kernel then knows that key, and how many keys above it and how many like it lie in earlier segments, and lists its own.  Each launch reads what the one
+// before wrote, and nothing is added up by atomics in memory.
 // ------------------------------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void evict_keys_kernel(PShape s, EvictShape ev, EvictTable tab, uint32_t *keys, int64_t stride) {
-  const int u = blockIdx.x, layer = blockIdx.z;
+constexpr int kSegRows = 8192, kMostSegs = 32, kCopies = 4;   // kCopies: of a workgroup's counts, because keys of one head often agree in their leading bits
+struct LongPlan {
+  uint32_t *keys;                          // [head][stride]
+  int *counts;                             // [head][level][segs][kLongBins]
+  int4 *states;                            // [head][segs]: the last kept key's bits so far, keys to keep of those that have them, keys above them in earlier segments, keys to keep
+  int64_t stride;
+  int32_t segs, seg;                       // seg: rows of a segment
+};
+struct FoldScratch { int wsum[kMsMaxWaves], above[kMsMaxWaves], found[3]; };
+struct Fold { int bin, above, above_before, in_before; };   // keys in higher bins, and in this one: of all segments, of those in front of `seg`
+
+// The bin that the need_of(all counted keys)-th largest key is in.
+template <class NeedOf>
+__device__ __forceinline__ Fold fold_counts(const int *counts, int n_seg, int seg, FoldScratch &sc, NeedOf &&need_of) {
+  constexpr int G = 8;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, low = kLongBins - 2 - 2 * tid;   // the thread's bins: low + 1, low
+  static_assert(kLongBins == 2 * kRankThreads, "two bins a thread");
+  int all[2] = {0, 0}, before[2] = {0, 0};
+  for (int g = 0; g < n_seg; g += G) {
+    int2 v[G];
+#pragma unroll
+    for (int k = 0; k < G; ++k) v[k] = *reinterpret_cast<const int2 *>(counts + min(g + k, n_seg - 1) * kLongBins + low);
+#pragma unroll
+    for (int k = 0; k < G; ++k) {
+      const int a = g + k < n_seg ? v[k].y : 0, b = g + k < n_seg ? v[k].x : 0;
+      all[0] += a; all[1] += b;
+      before[0] += g + k < seg ? a : 0; before[1] += g + k < seg ? b : 0;
+    }
+  }
+  int wtot;
+  const int sum = all[0] + all[1], inc = wave_scan_incl_add(sum, &wtot);
+  if (lane == 0) sc.wsum[wave] = wtot;
+  __syncthreads();
+  int excl = inc - sum, total = 0;
+#pragma unroll
+  for (int w = 0; w < kRankThreads / 64; ++w) { excl += w < wave ? sc.wsum[w] : 0; total += sc.wsum[w]; }
+  const int need = need_of(total);
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    if (excl < need && need <= excl + all[b]) { sc.found[0] = low + 1 - b; sc.found[1] = excl; sc.found[2] = before[b]; }
+    excl += all[b];
+  }
+  if (need <= 0) return Fold{0, 0, 0, 0};                     // uniform
+  __syncthreads();
+  Fold f{sc.found[0], sc.found[1], 0, sc.found[2]};
+  const int above = wave_reduce<WSum>((low + 1 > f.bin ? before[0] : 0) + (low > f.bin ? before[1] : 0), 0);
+  if (lane == 0) sc.above[wave] = above;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kRankThreads / 64; ++w) f.above_before += sc.above[w];
+  return f;
+}
+
+template <int LEVEL>
+__global__ __launch_bounds__(kRankThreads) void evict_count_kernel(PShape s, EvictShape ev, EvictTable tab, LongPlan p) {
+  __shared__ int hist[kLongBins * kCopies];
+  __shared__ FoldScratch sc;
+  const int tid = threadIdx.x, copy = tid & (kCopies - 1), u = blockIdx.x, seg = blockIdx.y, layer = blockIdx.z;
   const PCache c = tab.c[layer];
   const EvictLayer l = tab.l[layer];
-  const int len = (int)min((int64_t)head_rows(s, c, u), stride);
-  uint32_t *out = keys + (layer * (int64_t)s.units_per_layer + u) * stride;
-  for (int64_t i = ((int64_t)blockIdx.y * 256 + threadIdx.x) * 4; i < len; i += (int64_t)gridDim.y * 1024) {
-    const int id = page_at(s, c, u, (int)i >> s.lp);
-    const f32x4 w = *reinterpret_cast<const f32x4 *>(l.weights + ((int64_t)max(id, 0) << s.lp) + ((int)i & (s.P - 1)));
-    *reinterpret_cast<u32x4 *>(out + i) = four_keys(ev, head_rows(s, c, u), (int)i, id, w);
+  const int len = head_rows(s, c, u);
+  const int64_t head = layer * (int64_t)s.units_per_layer + u, r0 = (int64_t)seg * p.seg, r1 = min(r0 + p.seg, (int64_t)len);
+  if (len > p.stride || (seg > 0 && r0 >= len)) return;       // (an empty head: the first segment counts nothing)
+  uint32_t *keys = p.keys + head * p.stride;
+  int *counts = p.counts + head * 3 * p.segs * kLongBins;
+  const int n_seg = max(1, (int)(((int64_t)len + p.seg - 1) / p.seg));
+  for (int i = tid; i < kLongBins * kCopies; i += kRankThreads) hist[i] = 0;
+  uint32_t prefix = 0;
+  if constexpr (LEVEL == 1) {
+    const int budget = l.keep[u];
+    int keep = 0;
+    const Fold f = fold_counts(counts, n_seg, seg, sc, [&](int total) { return keep = min(min(max(budget, 0), ev.max_keep), total); });
+    prefix = (uint32_t)f.bin << 21;
+    if (tid == 0) p.states[head * p.segs + seg] = int4{(int)prefix, keep - f.above, f.above_before, keep};
+    if (keep == 0) return;                                    // uniform
+  } else if constexpr (LEVEL == 2) {
+    const int4 st = p.states[head * p.segs + seg];
+    if (st.w == 0) return;                                    // uniform
+    const Fold f = fold_counts(counts + p.segs * kLongBins, n_seg, seg, sc, [&](int) { return st.y; });
+    prefix = (uint32_t)st.x | (uint32_t)f.bin << 10;
+    if (tid == 0) p.states[head * p.segs + seg] = int4{(int)prefix, st.y - f.above, st.z + f.above_before, st.w};   // (each thread has read it: fold_counts has barriers)
+  }
+  __syncthreads();
+  for (int64_t i0 = r0 + 4 * tid; i0 < r1; i0 += 8 * kRankThreads) {
+    u32x4 k[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t i = i0 + h * 4 * kRankThreads;
+      k[h] = u32x4{0u, 0u, 0u, 0u};
+      if (i >= r1) continue;
+      if constexpr (LEVEL == 0) {
+        const int id = page_at(s, c, u, (int)i >> s.lp);
+        const f32x4 w = *reinterpret_cast<const f32x4 *>(l.weights + ((int64_t)max(id, 0) << s.lp) + ((int)i & (s.P - 1)));
+        k[h] = four_keys(ev, len, (int)i, id, w);
+        *reinterpret_cast<u32x4 *>(keys + i) = k[h];
+      } else k[h] = *reinterpret_cast<const u32x4 *>(keys + i);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t x = k[h][e];
+        if constexpr (LEVEL == 0) { if (x != 0) atomicAdd(&hist[(x >> 21) * kCopies + copy], 1); }
+        if constexpr (LEVEL == 1) { if (x != 0 && x >> 21 == prefix >> 21) atomicAdd(&hist[((x >> 10) & 2047u) * kCopies + copy], 1); }
+        if constexpr (LEVEL == 2) { if (x != 0 && x >> 10 == prefix >> 10) atomicAdd(&hist[(x & 1023u) * kCopies + copy], 1); }
+      }
+  }
+  __syncthreads();
+  for (int b = tid; b < kLongBins; b += kRankThreads) {
+    int n = 0;
+#pragma unroll
+    for (int k = 0; k < kCopies; ++k) n += hist[b * kCopies + k];
+    counts[(LEVEL * p.segs + seg) * kLongBins + b] = n;
   }
 }
 
-__global__ __launch_bounds__(kRankThreads) void evict_long_kernel(PShape s, EvictShape ev, EvictTable tab, const uint32_t *keys, int64_t stride) {
-  __shared__ LongScratch<8> sc;
-  const int u = blockIdx.x, layer = blockIdx.z;
+__global__ __launch_bounds__(kRankThreads) void evict_list_kernel(PShape s, EvictShape ev, EvictTable tab, LongPlan p) {
+  __shared__ union { FoldScratch fold; LongScratch lg; int wsum[kMsMaxWaves][2]; } sc;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, u = blockIdx.x, seg = blockIdx.y, layer = blockIdx.z;
   const PCache c = tab.c[layer];
   const EvictLayer l = tab.l[layer];
-  const int len = head_rows(s, c, u), budget = l.keep[u];
-  if (len <= stride) {
-    const uint32_t *in = keys + (layer * (int64_t)s.units_per_layer + u) * stride;
-    rank_long<kRankThreads, 8>(ev, l, u, len, budget, sc, [&](int i, bool there) { return there ? *reinterpret_cast<const u32x4 *>(in + i) : u32x4{0u, 0u, 0u, 0u}; });
-  } else {
-    rank_long<kRankThreads, 8>(ev, l, u, len, budget, sc, [&](int i, bool there) {
-      const int at = page_at(s, c, u, i >> s.lp);
-      const f32x4 x = *reinterpret_cast<const f32x4 *>(l.weights + ((int64_t)max(at, 0) << s.lp) + (i & (s.P - 1)));
-      return four_keys(ev, len, i, there ? at : -1, x);
-    });
+  const int len = head_rows(s, c, u);
+  const int64_t head = layer * (int64_t)s.units_per_layer + u, r0 = (int64_t)seg * p.seg, r1 = min(r0 + p.seg, (int64_t)len);
+  if (seg > 0 && r0 >= len) return;
+  if (len > p.stride) {
+    if (seg == 0) rank_long<kRankThreads>(s, c, ev, l, u, len, l.keep[u], sc.lg);
+    return;
+  }
+  const uint32_t *keys = p.keys + head * p.stride;
+  const int4 st = p.states[head * p.segs + seg];
+  int32_t *kept = l.kept + (int64_t)u * ev.max_keep;
+  if (seg == 0) kept_rows(ev, l, u, st.w, st.w, kept, kRankThreads);
+  if (st.w == 0) return;                                      // uniform
+  const int n_seg = (int)(((int64_t)len + p.seg - 1) / p.seg);
+  const Fold f = fold_counts(p.counts + (head * 3 + 2) * p.segs * kLongBins, n_seg, seg, sc.fold, [&](int) { return st.y; });
+  const uint32_t last = (uint32_t)st.x | (uint32_t)f.bin;     // the last kept key; the first `need` that are it stay
+  const int need = st.y - f.above, keep = st.w;
+  int above = st.z + f.above_before, ties = f.in_before;      // in front of the turn's rows
+  for (int64_t t0 = r0; t0 < r1; t0 += 8 * kRankThreads) {
+    const int64_t i = t0 + 8 * tid;
+    uint32_t k[8];
+    int a = 0, t = 0, wa, wt;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const u32x4 x = i + 4 * h < r1 ? *reinterpret_cast<const u32x4 *>(keys + i + 4 * h) : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        k[4 * h + e] = x[e];
+        a += x[e] > last ? 1 : 0;
+        t += x[e] == last ? 1 : 0;
+      }
+    }
+    const int ia = wave_scan_incl_add(a, &wa), it = wave_scan_incl_add(t, &wt);
+    __syncthreads();
+    if (lane == 0) { sc.wsum[wave][0] = wa; sc.wsum[wave][1] = wt; }
+    __syncthreads();
+    int oa = above + ia - a, ot = ties + it - t;
+#pragma unroll
+    for (int w = 0; w < kRankThreads / 64; ++w) {
+      const int na = sc.wsum[w][0], nt = sc.wsum[w][1];
+      above += na; ties += nt;
+      oa += w < wave ? na : 0; ot += w < wave ? nt : 0;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bool like = k[e] == last;
+      if (k[e] > last || (like && ot < need)) {
+        const int o = oa + min(ot, need);
+        if (o < keep) kept[o] = (int32_t)(i + e);
+      }
+      oa += k[e] > last ? 1 : 0;
+      ot += like ? 1 : 0;
+    }
   }
 }
 
@@ -477,12 +623,24 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(PShape s, Evic
   }
 }
 
-// Heads that a workgroup holds in registers, as long as the host says; longer ones' keys lie in the workspace, a head's one after another.
+// Heads that a workgroup holds in registers, as long as the host says; longer ones have keys and counts in the workspace.
 constexpr int kRankRows = 16384;
 static int64_t most_rows(const PShape &s, int max_rows) { return std::min<int64_t>(max_rows, (int64_t)s.max_pages * s.P); }
-static int64_t key_stride(const PShape &s, int max_rows) { return (most_rows(s, max_rows) + 3) / 4 * 4; }
-static size_t evict_bytes(const PShape &s, int n_layers, int max_rows) {
-  return most_rows(s, max_rows) <= kRankRows ? 0 : (size_t)std::min(n_layers, kEvictLayers) * s.units_per_layer * key_stride(s, max_rows) * sizeof(uint32_t);
+static size_t evict_plan(const PShape &s, int n_layers, int max_rows, void *workspace, LongPlan *p) {
+  const int64_t rows = most_rows(s, max_rows), heads = (int64_t)std::min(n_layers, kEvictLayers) * s.units_per_layer;
+  *p = LongPlan{};
+  if (rows <= kRankRows) return 0;
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kMostSegs, ((int64_t)1 << 21) / heads));        // fewer than 2^32 threads
+  p->stride = (rows + 3) / 4 * 4;
+  p->seg = (int32_t)(((rows + most - 1) / most + kSegRows - 1) / kSegRows * kSegRows);
+  p->segs = (int32_t)((rows + p->seg - 1) / p->seg);
+  const size_t states = (size_t)heads * p->segs * sizeof(int4), counts = (size_t)heads * 3 * p->segs * kLongBins * sizeof(int);
+  p->states = static_cast<int4 *>(workspace);
+  if (workspace) {
+    p->counts = reinterpret_cast<int *>(static_cast<char *>(workspace) + states);
+    p->keys = reinterpret_cast<uint32_t *>(static_cast<char *>(workspace) + states + counts);
+  }
+  return states + counts + (size_t)heads * p->stride * sizeof(uint32_t);
 }
 
 }  // namespace mixkv
@@ -493,7 +651,8 @@ extern "C" mixkv_status mixkv_paged_evict_workspace_size(const mixkv_paged_param
   const mixkv_status st = make_pshape(params, &s);
   if (st != MIXKV_OK) return st;
   if (!bytes || n_layers < 1 || n_layers > MIXKV_MAX_LAYERS || max_rows < 1) return MIXKV_ERR_INVALID_ARG;
-  *bytes = (evict_bytes(s, n_layers, max_rows) + 255) / 256 * 256;
+  LongPlan plan;
+  *bytes = (evict_plan(s, n_layers, max_rows, nullptr, &plan) + 255) / 256 * 256;
   return MIXKV_OK;
 }
 
@@ -517,13 +676,13 @@ extern "C" mixkv_status mixkv_paged_evict(const mixkv_paged_params *params, cons
     if (misaligned(d.weights, 16) || misaligned(d.weights_into, 4) || misaligned(d.keep, 4) || misaligned(d.kept, 4) || misaligned(d.n_kept, 4)) return MIXKV_ERR_INVALID_ARG;
     if (d.n_kept == caches[l].lengths || d.n_kept == d.keep) return MIXKV_ERR_INVALID_ARG;
   }
-  const size_t need = evict_bytes(s, n_layers, max_rows);
+  LongPlan plan;
+  const size_t need = evict_plan(s, n_layers, max_rows, workspace, &plan);
   if (need > 0) {
     if (!workspace || misaligned(workspace, 256)) return MIXKV_ERR_INVALID_ARG;
     if (workspace_bytes < need) return MIXKV_ERR_WORKSPACE_TOO_SMALL;
   }
-  uint32_t *keys = static_cast<uint32_t *>(workspace);
-  const int64_t rows = most_rows(s, max_rows), stride = key_stride(s, max_rows);
+  const int64_t rows = most_rows(s, max_rows);
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   const EvictShape ev{max_keep, keep_first, keep_last};
   for (int l0 = 0; l0 < n_layers; l0 += kEvictLayers) {
@@ -547,11 +706,13 @@ extern "C" mixkv_status mixkv_paged_evict(const mixkv_paged_params *params, cons
     else if (rows <= 4096) rank(evict_rank_kernel<512, 8>, 512);
     else if (rows <= kRankRows) rank(evict_rank_kernel<1024, 16>, 1024);
     else {
-      const int64_t y = std::min(most, std::max<int64_t>(1, (rows + 1023) / 1024));
-      hipLaunchKernelGGL(evict_keys_kernel, dim3((unsigned)s.units_per_layer, (unsigned)y, (unsigned)nl), dim3(256), 0, stream, s, ev, t, keys, stride);
-      hipLaunchKernelGGL(evict_long_kernel, heads, dim3(kRankThreads), 0, stream, s, ev, t, (const uint32_t *)keys, stride);
+      const dim3 parts((unsigned)s.units_per_layer, (unsigned)plan.segs, (unsigned)nl);
+      auto part = [&](auto kern) { hipLaunchKernelGGL(kern, parts, dim3(kRankThreads), 0, stream, s, ev, t, plan); };
+      part(evict_count_kernel<0>);
+      part(evict_count_kernel<1>);
+      part(evict_count_kernel<2>);
+      part(evict_list_kernel);
     }
-    // Workers of a head: one for 32 rows, as long as all of them are on the chip together.
     // Workgroups of a head: one for 128 rows of keys and one for as many of values, as long as all of them are on the chip together.
     const int64_t work = ((int64_t)max_keep + 127) / 128, fit = std::max<int64_t>(1, 4096 / ((int64_t)s.units_per_layer * nl));
     const dim3 grid((unsigned)s.units_per_layer, (unsigned)(2 * std::min(work, std::min(fit, (most + 1) / 2))), (unsigned)nl);
