@@ -17,9 +17,9 @@ struct AttnTable { PCache c[kLayersPerLaunch]; AttnLayer l[kLayersPerLaunch]; };
 
 struct AShape {
   int32_t nchunks, ctiles;     // chunks of a head in the launch, tiles of a chunk
-  int32_t gchunks, gt;         // groups of up to kAttnHeads rows (query heads, with WIN of all new rows), and the rows of a full one
+  int32_t gchunks, gt;         // groups of up to kAttnHeads rows (query heads; WIN: gsize rows, query heads of all new rows), and the rows of a full one
   int32_t keep;                // entries of a head's list of selected pages, 0: all pages
-  int32_t gc0, gcn;            // WIN: groups of the launch
+  int32_t gc0, gcn, gsize;     // WIN: groups of the launch, rows of a group
   PWindow w;                   // WIN
 };
 
@@ -158,7 +158,8 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gcs = WIN ? a.gcn : a.gchunks;
-  const int u = blockIdx.x, ch = blockIdx.y, layer = blockIdx.z / gcs, gc = blockIdx.z - layer * gcs + (WIN ? a.gc0 : 0);
+  const int u = blockIdx.x, ch = WIN ? blockIdx.y / gcs : blockIdx.y, layer = WIN ? blockIdx.z : blockIdx.z / gcs;
+  const int gc = WIN ? blockIdx.y - ch * gcs + a.gc0 : blockIdx.z - layer * gcs;     // WIN: the groups of a chunk side by side, so that they find its rows in the L2
   const int b = u / s.hkv, h = u - b * s.hkv;
   const PCache c = tab.c[layer];
   const Layer<WIN> l = tab.l[layer];
@@ -458,7 +459,7 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
 // do not overflow, whatever the logits behind them.
 constexpr float kRowsSumLimit = 0x1p20f;
 
-template <int DT, int D, bool ONCE, bool WIN>
+template <int DT, int D, bool ONCE, bool WIN, int NQ = 1>
 __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Table<WIN> tab, float *part, float *part_ml, int64_t unit0) {
   constexpr bool F32 = DT == MIXKV_F32;
   constexpr int EB = F32 ? 4 : 2, RB = D * EB, PPR = RB / 16, NC = PPR / 4, NB = D / 16, H = kAttnHeads, W = 4;
@@ -468,13 +469,14 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Tab
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gcs = WIN ? a.gcn : a.gchunks;
-  const int u = blockIdx.x, ch = blockIdx.y, layer = blockIdx.z / gcs, gc = blockIdx.z - layer * gcs + (WIN ? a.gc0 : 0);
+  const int u = blockIdx.x, ch = WIN ? blockIdx.y / gcs : blockIdx.y, layer = WIN ? blockIdx.z : blockIdx.z / gcs;
+  const int gc = WIN ? blockIdx.y - ch * gcs + a.gc0 : blockIdx.z - layer * gcs;     // WIN: the groups of a chunk side by side, so that they find its rows in the L2
   const int b = u / s.hkv, h = u - b * s.hkv;
   const PCache c = tab.c[layer];
   const Layer<WIN> l = tab.l[layer];
   View v;
   if constexpr (WIN) {
-    v = view_of(s, a.w, c, l, u, gc * H, H);
+    v = view_of(s, a.w, c, l, u, gc * NQ * H, NQ * H);
     if (v.ng <= 0) return;
   }
   const int ng = WIN ? v.ng : min(H, s.G - gc * H);
@@ -483,11 +485,12 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Tab
     if constexpr (WIN) return v.query(s, a.w, l, h, i);
     else return l.Q + (q0 + i) * RB;
   };
-  u32x4 qf[NC];
-  {
-    const char *q = q_row(l16 < ng ? l16 : 0);
+  u32x4 qf[NQ][NC];
 #pragma unroll
-    for (int k = 0; k < NC; ++k) qf[k] = *reinterpret_cast<const u32x4 *>(q + (4 * k + quad) * 16);
+  for (int y = 0; y < NQ; ++y) {
+    const char *q = q_row(16 * y + l16 < ng ? 16 * y + l16 : 0);
+#pragma unroll
+    for (int k = 0; k < NC; ++k) qf[y][k] = *reinterpret_cast<const u32x4 *>(q + (4 * k + quad) * 16);
   }
   const int t0 = ch * a.ctiles;
   int place, tile = 0;
@@ -496,19 +499,27 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Tab
     else return tile_entry(s, a, c, l, u, t, place);
   };
   int entry = entry_of(t0 + wave + lane * W);                  // lane i: where the wave's i-th tile of 64 lies
-  int len, tiles, seen = 0;                                    // WIN: the last place that row l16 sees
-  if constexpr (WIN) { len = v.len; tiles = v.tiles; seen = v.place(s, min(l16, ng - 1)); }
-  else { len = head_rows(s, c, u); tiles = head_tiles(s, a, l, u, len); }
+  int len, tiles, seen[NQ];                                    // WIN: the last place that row 16 y + l16 sees
+  if constexpr (WIN) {
+    len = v.len; tiles = v.tiles;
+#pragma unroll
+    for (int y = 0; y < NQ; ++y) seen[y] = v.place(s, min(16 * y + l16, ng - 1));
+  } else { len = head_rows(s, c, u); tiles = head_tiles(s, a, l, u, len); }
   const int t1 = chunk_end(a, tiles, ch);
   if (t0 >= t1 && ch > 0) return;
-#pragma unroll
-  for (int k = 0; k < NC; ++k)
-    if (l16 >= ng) qf[k] = u32x4{0u, 0u, 0u, 0u};              // heads past the group are zero columns
   const float c2 = s.scale_log2e;
-  float m = -INFINITY, sum = 0.f;                              // the head's offset, this lane's share of its sum of weights
-  f32x4 o[NB];
+  float m[NQ], sum[NQ];                                        // the head's offset, this lane's share of its sum of weights
+  f32x4 o[NQ][NB];
 #pragma unroll
-  for (int k = 0; k < NB; ++k) o[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int y = 0; y < NQ; ++y) {
+#pragma unroll
+    for (int k = 0; k < NC; ++k)
+      if (16 * y + l16 >= ng) qf[y][k] = u32x4{0u, 0u, 0u, 0u};   // heads past the group are zero columns
+    m[y] = -INFINITY;
+    sum[y] = 0.f;
+#pragma unroll
+    for (int k = 0; k < NB; ++k) o[y][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
   char *img = reinterpret_cast<char *>(o_s[wave]);             // bf16: a tile of values, 32 rows
   static_assert(F32 || 32 * RB <= H * D * 4, "the image lies in the wave's share of the output");
   const uint32_t img_a = (uint32_t)(uintptr_t)(lds_void_t *)img;
@@ -553,89 +564,104 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Tab
       const int live = __builtin_amdgcn_readlane(x_rows, i) >> 8, row0 = __builtin_amdgcn_readlane(x_row0, i);
 #pragma unroll 1
       for (int r = 0; r < live; ++r) {
-        if (!sees(a.w, seen, row0 + r)) continue;
 #pragma unroll
-        for (int k = 0; k < NB; ++k)
+        for (int y = 0; y < NQ; ++y) {
+          if (!sees(a.w, seen[y], row0 + r)) continue;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float x;
-            if constexpr (F32) x = reinterpret_cast<const float *>(p + r * RB)[64 * (k >> 2) + 4 * (4 * quad + e) + (k & 3)];
-            else x = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(p + r * RB)[16 * k + 4 * quad + e] << 16);
-            if (no_number<MIXKV_F32>(__float_as_uint(x))) o[k][e] += x;
-          }
+          for (int k = 0; k < NB; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float x;
+              if constexpr (F32) x = reinterpret_cast<const float *>(p + r * RB)[64 * (k >> 2) + 4 * (4 * quad + e) + (k & 3)];
+              else x = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(p + r * RB)[16 * k + 4 * quad + e] << 16);
+              if (no_number<MIXKV_F32>(__float_as_uint(x))) o[y][k][e] += x;
+            }
+        }
       }
     };
     load_keys(0);
     load_values(0);
     for (int i = 0; i < n; ++i) {
       const int live = __builtin_amdgcn_readlane(x_rows, i) >> 8;
-      f32x4 acc[2];
+      f32x4 acc[NQ][2];
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int r = 0; r < 2; ++r)
 #pragma unroll
-        for (int k = 0; k < NC; ++k) {
-          if constexpr (F32) {
+        for (int y = 0; y < NQ; ++y) {
+          acc[y][r] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              acc[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[r][k][e]), __uint_as_float(qf[k][e]), acc[r], 0, 0, 0);
-          } else {
-            acc[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[r][k]), __builtin_bit_cast(bf16x8, qf[k]), acc[r], 0, 0, 0);
-          }
-        }
-      }
-      if (i + 1 < n) load_keys(i + 1);
-      float x8[8], p[8];
+          for (int k = 0; k < NC; ++k) {
+            if constexpr (F32) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float v = e < 4 ? acc[0][e & 3] : acc[1][e & 3];
-        x8[e] = 16 * (e >> 2) + 4 * quad + (e & 3) < live ? v : -INFINITY;
-      }
-      bool mixed = false;                                      // values that are no numbers, in rows that only some of the group's rows see
-      if constexpr (WIN) {
-        const int row0 = __builtin_amdgcn_readlane(x_row0, i);
-        if (!whole_tile(a.w, v, row0, live)) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x8[e] = sees(a.w, seen, row0 + 16 * (e >> 2) + 4 * quad + (e & 3)) ? x8[e] : -INFINITY;
-          if (v.pa != v.pb) {
-            bool odd = false;
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-              for (int w = 0; w < 4; ++w) odd |= no_number<DT>(vr[j][w]);
-            mixed = __builtin_amdgcn_ballot_w64(odd) != 0;
-            if (mixed) {
-#pragma unroll
-              for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) vr[j][w] = numbers_only<DT>(vr[j][w]);
+              for (int e = 0; e < 4; ++e)
+                acc[y][r] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[r][k][e]), __uint_as_float(qf[y][k][e]), acc[y][r], 0, 0, 0);
+            } else {
+              acc[y][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[r][k]), __builtin_bit_cast(bf16x8, qf[y][k]), acc[y][r], 0, 0, 0);
             }
           }
         }
+      if (i + 1 < n) load_keys(i + 1);
+      bool mixed = false, whole = true;                        // mixed: values that are no numbers, in rows that only some of the group's rows see
+      int row0 = 0;
+      if constexpr (WIN) {
+        row0 = __builtin_amdgcn_readlane(x_row0, i);
+        whole = whole_tile(a.w, v, row0, live);
+        if (!whole && v.pa != v.pb) {
+          bool odd = false;
+#pragma unroll
+          for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) odd |= no_number<DT>(vr[j][w]);
+          mixed = __builtin_amdgcn_ballot_w64(odd) != 0;
+          if (mixed) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+              for (int w = 0; w < 4; ++w) vr[j][w] = numbers_only<DT>(vr[j][w]);
+          }
+        }
       }
+      float p[NQ][8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = fast_exp2(fmaf(x8[e], c2, -m));
-      float next = sum + (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])));
-      if (__builtin_amdgcn_ballot_w64(!(next < kRowsSumLimit)) != 0) {
-        float t = fmaxf(fmaxf(fmaxf(x8[0], x8[1]), fmaxf(x8[2], x8[3])), fmaxf(fmaxf(x8[4], x8[5]), fmaxf(x8[6], x8[7])));
-        t = fmaxf(t, __shfl_xor(t, 16));
-        t = fmaxf(t, __shfl_xor(t, 32));
-        const float mn = fmaxf(m, t * c2), mu = mn == -INFINITY ? 0.f : mn;
-        const float f = fast_exp2(m - mu);                     // 0 while there is no offset yet
+      for (int y = 0; y < NQ; ++y) {
+        float x8[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = fast_exp2(fmaf(x8[e], c2, -mu));
-        next = sum * f + (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])));
+        for (int e = 0; e < 8; ++e) {
+          const float v = e < 4 ? acc[y][0][e & 3] : acc[y][1][e & 3];
+          x8[e] = 16 * (e >> 2) + 4 * quad + (e & 3) < live ? v : -INFINITY;
+        }
+        if constexpr (WIN) {
+          if (!whole) {
 #pragma unroll
-        for (int k = 0; k < NB; ++k) o[k] *= f;
-        m = mn;
+            for (int e = 0; e < 8; ++e) x8[e] = sees(a.w, seen[y], row0 + 16 * (e >> 2) + 4 * quad + (e & 3)) ? x8[e] : -INFINITY;
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[y][e] = fast_exp2(fmaf(x8[e], c2, -m[y]));
+        float next = sum[y] + (((p[y][0] + p[y][1]) + (p[y][2] + p[y][3])) + ((p[y][4] + p[y][5]) + (p[y][6] + p[y][7])));
+        if (__builtin_amdgcn_ballot_w64(!(next < kRowsSumLimit)) != 0) {
+          float t = fmaxf(fmaxf(fmaxf(x8[0], x8[1]), fmaxf(x8[2], x8[3])), fmaxf(fmaxf(x8[4], x8[5]), fmaxf(x8[6], x8[7])));
+          t = fmaxf(t, __shfl_xor(t, 16));
+          t = fmaxf(t, __shfl_xor(t, 32));
+          const float mn = fmaxf(m[y], t * c2), mu = mn == -INFINITY ? 0.f : mn;
+          const float f = fast_exp2(m[y] - mu);                // 0 while there is no offset yet
+#pragma unroll
+          for (int e = 0; e < 8; ++e) p[y][e] = fast_exp2(fmaf(x8[e], c2, -mu));
+          next = sum[y] * f + (((p[y][0] + p[y][1]) + (p[y][2] + p[y][3])) + ((p[y][4] + p[y][5]) + (p[y][6] + p[y][7])));
+#pragma unroll
+          for (int k = 0; k < NB; ++k) o[y][k] *= f;
+          m[y] = mn;
+        }
+        sum[y] = next;
       }
-      sum = next;
       if constexpr (F32) {
 #pragma unroll
         for (int k = 0; k < NB; ++k)
 #pragma unroll
           for (int e = 0; e < 8; ++e)                          // block k: elements 64 (k / 4) + 4 i + k % 4
-            o[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[(k >> 2) * 8 + e][k & 3]), p[e], o[k], 0, 0, 0);
+#pragma unroll
+            for (int y = 0; y < NQ; ++y)
+              o[y][k] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[(k >> 2) * 8 + e][k & 3]), p[y][e], o[y][k], 0, 0, 0);
         if (i + 1 < n) load_values(i + 1);
         if constexpr (WIN) {
           if (mixed) add_odd(i);
@@ -648,13 +674,15 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Tab
         }
         if (i + 1 < n) load_values(i + 1);
         wave_lds_fence();
-        bf16x8 ph, pl;
+        bf16x8 ph[NQ], pl[NQ];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const __bf16 hi = (__bf16)p[e];
-          ph[e] = hi;
-          pl[e] = (__bf16)(p[e] - (float)hi);
-        }
+        for (int y = 0; y < NQ; ++y)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const __bf16 hi = (__bf16)p[y][e];
+            ph[y][e] = hi;
+            pl[y][e] = (__bf16)(p[y][e] - (float)hi);
+          }
         const uint32_t r0 = 4 * quad + (l16 >> 2);             // rows 4 quad ... and 16 + 4 quad ... of block k of 16 elements
 #pragma unroll
         for (int k = 0; k < NB; ++k) {
@@ -665,8 +693,11 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Tab
           const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)at[0]);
           const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)at[1]);
           const bf16x8 vv = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-          o[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, ph, o[k], 0, 0, 0);
-          o[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, pl, o[k], 0, 0, 0);
+#pragma unroll
+          for (int y = 0; y < NQ; ++y) {
+            o[y][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, ph[y], o[y][k], 0, 0, 0);
+            o[y][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, pl[y], o[y][k], 0, 0, 0);
+          }
         }
         wave_lds_fence();
         if constexpr (WIN) {
@@ -677,15 +708,21 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Tab
   }
 
   // ---- the waves' shares: lane (head, quad) has rows 4 quad + e of every block
-  sum += __shfl_xor(sum, 16);
-  sum += __shfl_xor(sum, 32);
-  if (quad == 0) { m_s[wave][l16] = m; l_s[wave][l16] = sum; }
 #pragma unroll
-  for (int k = 0; k < NB; ++k)
+  for (int y = 0; y < NQ; ++y) {
+    if (NQ > 1 && 16 * y >= ng) break;                         // uniform
+    if (y > 0) __syncthreads();
+    sum[y] += __shfl_xor(sum[y], 16);
+    sum[y] += __shfl_xor(sum[y], 32);
+    if (quad == 0) { m_s[wave][l16] = m[y]; l_s[wave][l16] = sum[y]; }
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      o_s[wave][l16][(F32 ? 64 * (k >> 2) + 4 * (4 * quad + e) + (k & 3) : 16 * k + 4 * quad + e) ^ l16] = o[k][e];
-  finish_chunk<DT, D, WIN>(s, a, l, o_s, m_s, l_s, part, part_ml, slot_of(s, a, unit0, layer, u, gc, ch), q0, ng, chunks_used(a, tiles) <= 1, v, h);
+    for (int k = 0; k < NB; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        o_s[wave][l16][(F32 ? 64 * (k >> 2) + 4 * (4 * quad + e) + (k & 3) : 16 * k + 4 * quad + e) ^ l16] = o[y][k][e];
+    finish_chunk<DT, D, WIN>(s, a, l, o_s, m_s, l_s, part, part_ml, slot_of(s, a, unit0, layer, u, gc, ch) + 16 * y, q0, min(ng - 16 * y, H), chunks_used(a, tiles) <= 1, v, h);
+    if constexpr (WIN) v.i0 += 16;
+  }
 }
 
 // Folds the chunks of one query head: slices of D/4 threads take every S-th chunk, 16 bytes of its row a thread, and are summed in order.
@@ -702,7 +739,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PShape s, AShape a, Ta
   const PCache c = tab.c[layer];
   const Layer<WIN> l = tab.l[layer];
   View v;
-  if constexpr (WIN) v = view_of(s, a.w, c, l, u, gc * kAttnHeads, kAttnHeads);
+  if constexpr (WIN) v = view_of(s, a.w, c, l, u, gc * a.gsize, a.gsize);
   if (g >= (WIN ? v.ng : min(kAttnHeads, s.G - gc * kAttnHeads))) return;
   const int64_t slot = slot_of(s, a, unit0, layer, u, gc, 0) + g;
   const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + slot;
@@ -788,15 +825,15 @@ static size_t attn_bytes(const PShape &s, const AShape &a, int n_layers) { retur
 // ONCE: the rows pass the caches by.  With more query heads to a KV head than a workgroup takes, several workgroups read the same rows, and they go
 // through the caches.  us by the caches and through them, rows of 128: 4-bit, 64 sequences of 8192, 4 query heads to a KV head 125 and 138, 48 heads
 // to one KV head 60 and 51; bf16, 16 of 8192, 4 to a head 94 and 107, 32 to a head 56 and 54; fp32, 32 to a head 103 and 98.
-template <bool ONCE, bool WIN, typename Go>
+template <bool ONCE, bool WIN, int NQ = 1, typename Go>
 static void launch_attention(const PShape &s, int dtype, Go &&go) {
   constexpr int B16 = MIXKV_BF16, F32 = MIXKV_F32;
   if (s.q4) {
     if (s.D == 128) go(paged_q4_kernel<128, ONCE, WIN>, paged_merge_kernel<B16, 128, WIN>);
     else go(paged_q4_kernel<64, ONCE, WIN>, paged_merge_kernel<B16, 64, WIN>);
   } else if (dtype == B16) {
-    if (s.D == 128) go(paged_rows_kernel<B16, 128, ONCE, WIN>, paged_merge_kernel<B16, 128, WIN>);
-    else go(paged_rows_kernel<B16, 64, ONCE, WIN>, paged_merge_kernel<B16, 64, WIN>);
+    if (s.D == 128) go(paged_rows_kernel<B16, 128, ONCE, WIN, NQ>, paged_merge_kernel<B16, 128, WIN>);
+    else go(paged_rows_kernel<B16, 64, ONCE, WIN, NQ>, paged_merge_kernel<B16, 64, WIN>);
   } else {
     if (s.D == 128) go(paged_rows_kernel<F32, 128, ONCE, WIN>, paged_merge_kernel<F32, 128, WIN>);
     else go(paged_rows_kernel<F32, 64, ONCE, WIN>, paged_merge_kernel<F32, 64, WIN>);
@@ -918,11 +955,12 @@ WinTable window_table(const mixkv_paged_cache *c, const mixkv_paged_queries *q, 
 
 // The same dealing for groups of rows with a window: the tiles that a group may see, at most.  Chunks grow without end where there are groups enough, as
 // there are for prompts.
-static void window_config(const PShape &s, const PWindow &w, int n_layers, int max_rows, AShape *a) {
+static void window_config(const PShape &s, const PWindow &w, int dtype, int n_layers, int max_rows, AShape *a) {
   const int64_t rows = (int64_t)w.max_count * s.G;
-  a->gchunks = (int)((rows + kAttnHeads - 1) / kAttnHeads);
-  a->gt = (int)std::min<int64_t>(rows, kAttnHeads);
-  const int64_t groups = (int64_t)n_layers * s.units_per_layer * a->gchunks, tiles = most_tiles(s, w, max_rows, kAttnHeads), all = tiles * groups;
+  a->gsize = dtype == MIXKV_BF16 && !s.q4 && rows > kAttnHeads ? 2 * kAttnHeads : kAttnHeads;
+  a->gchunks = (int)((rows + a->gsize - 1) / a->gsize);
+  a->gt = (int)std::min<int64_t>(rows, a->gsize);
+  const int64_t groups = (int64_t)n_layers * s.units_per_layer * a->gchunks, tiles = most_tiles(s, w, max_rows, a->gsize), all = tiles * groups;
   int64_t ct = std::max<int64_t>(4, std::max(std::min<int64_t>((all + 255) / 256, 16), (all + 511) / 512));
   if (tiles <= 12) ct = tiles;
   a->ctiles = (int)((std::min(ct, tiles) + 3) / 4 * 4);
@@ -945,7 +983,7 @@ extern "C" mixkv_status mixkv_paged_window_attention_workspace_size(const mixkv_
   max_rows = clamp_rows(s, max_rows);
   AShape a{};
   const bool many = many_rows(s, params->dtype, w);
-  if (!many) window_config(s, w, n_layers, max_rows, &a);
+  if (!many) window_config(s, w, params->dtype, n_layers, max_rows, &a);
   *bytes = ((many ? prompt_bytes(s, w, n_layers, max_rows) : attn_bytes(s, a, n_layers)) + 255) / 256 * 256;
   return MIXKV_OK;
 }
@@ -965,7 +1003,7 @@ extern "C" mixkv_status mixkv_paged_window_attention(const mixkv_paged_params *p
   max_rows = clamp_rows(s, max_rows);
   AShape a{};
   const bool many = many_rows(s, params->dtype, w);
-  if (!many) window_config(s, w, n_layers, max_rows, &a);
+  if (!many) window_config(s, w, params->dtype, n_layers, max_rows, &a);
   const size_t need = many ? prompt_bytes(s, w, n_layers, max_rows) : attn_bytes(s, a, n_layers);
   if (need > 0) {
     if (!workspace || misaligned(workspace, 256)) return MIXKV_ERR_INVALID_ARG;
@@ -981,14 +1019,17 @@ extern "C" mixkv_status mixkv_paged_window_attention(const mixkv_paged_params *p
     const WinTable t = window_table(caches + l0, queries + l0, nl, eb);
     const int64_t unit0 = (int64_t)l0 * s.units_per_layer;
     for (a.gc0 = 0; a.gc0 < a.gchunks; a.gc0 += a.gcn) {
-      a.gcn = (int)std::min<int64_t>(a.gchunks - a.gc0, std::max<int64_t>(1, most / nl));
+      a.gcn = (int)std::min<int64_t>(a.gchunks - a.gc0, std::max<int64_t>(1, std::min<int64_t>(most / nl, 65535 / a.nchunks)));
       const unsigned z = (unsigned)(nl * a.gcn);
       auto go = [&](auto kern, auto merge) {
-        hipLaunchKernelGGL(kern, dim3((unsigned)s.units_per_layer, (unsigned)a.nchunks, z), dim3(256), 0, stream, s, a, t, part, part_ml, unit0);
+        hipLaunchKernelGGL(kern, dim3((unsigned)s.units_per_layer, (unsigned)(a.nchunks * a.gcn), (unsigned)nl), dim3(256), 0, stream, s, a, t, part, part_ml, unit0);
         if (a.nchunks > 1)
           hipLaunchKernelGGL(merge, dim3((unsigned)s.units_per_layer, (unsigned)a.gt, z), dim3(256), 0, stream, s, a, t, (const float *)part, (const float *)part_ml, unit0);
       };
-      if (a.gchunks == 1) launch_attention<true, true>(s, params->dtype, go);
+      if (a.gsize > kAttnHeads) {
+        if (a.gchunks == 1) launch_attention<true, true, 2>(s, params->dtype, go);
+        else launch_attention<false, true, 2>(s, params->dtype, go);
+      } else if (a.gchunks == 1) launch_attention<true, true>(s, params->dtype, go);
       else launch_attention<false, true>(s, params->dtype, go);
       if (hipGetLastError() != hipSuccess) return MIXKV_ERR_HIP;
     }
