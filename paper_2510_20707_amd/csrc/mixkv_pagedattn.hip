@@ -460,7 +460,7 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
 constexpr float kRowsSumLimit = 0x1p20f;
 
 template <int DT, int D, bool ONCE, bool WIN, int NQ = 1>
-__global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Table<WIN> tab, float *part, float *part_ml, int64_t unit0) {
+__global__ __launch_bounds__(256, NQ) void paged_rows_kernel(PShape s, AShape a, Table<WIN> tab, float *part, float *part_ml, int64_t unit0) {
   constexpr bool F32 = DT == MIXKV_F32;
   constexpr int EB = F32 ? 4 : 2, RB = D * EB, PPR = RB / 16, NC = PPR / 4, NB = D / 16, H = kAttnHeads, W = 4;
   constexpr int NV = F32 ? 8 * (D / 64) : 32 * PPR / 64, RPL = 64 / PPR;     // 16-byte loads of a lane for a tile of values
@@ -667,10 +667,12 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Tab
           if (mixed) add_odd(i);
         }
       } else {
+        int ln = lane;
+        if constexpr (NQ > 1) asm volatile("" : "+v"(ln));      // the image's addresses are made anew: kept, their 24 registers leave the SIMD one wave
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-          const int row = value_row(j);
-          reinterpret_cast<u32x4 *>(img)[row * PPR + ((lane % PPR) ^ value_swz<D>(row))] = vr[j];
+          const int row = RPL * j + ln / PPR;
+          reinterpret_cast<u32x4 *>(img)[row * PPR + ((ln % PPR) ^ value_swz<D>(row))] = vr[j];
         }
         if (i + 1 < n) load_values(i + 1);
         wave_lds_fence();
@@ -683,13 +685,13 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(PShape s, AShape a, Tab
             ph[y][e] = hi;
             pl[y][e] = (__bf16)(p[y][e] - (float)hi);
           }
-        const uint32_t r0 = 4 * quad + (l16 >> 2);             // rows 4 quad ... and 16 + 4 quad ... of block k of 16 elements
+        const uint32_t r0 = 4 * (ln >> 4) + ((ln & 15) >> 2);   // rows 4 quad ... and 16 + 4 quad ... of block k of 16 elements
 #pragma unroll
         for (int k = 0; k < NB; ++k) {
           uint32_t at[2];
 #pragma unroll
           for (int r = 0; r < 2; ++r)
-            at[r] = img_a + (r0 + 16 * r) * RB + ((2 * k + ((l16 & 3) >> 1)) ^ value_swz<D>(r0 + 16 * r)) * 16 + (l16 & 1) * 8;
+            at[r] = img_a + (r0 + 16 * r) * RB + ((2 * k + ((ln & 3) >> 1)) ^ value_swz<D>(r0 + 16 * r)) * 16 + (ln & 1) * 8;
           const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)at[0]);
           const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)at[1]);
           const bf16x8 vv = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -961,7 +963,7 @@ static void window_config(const PShape &s, const PWindow &w, int dtype, int n_la
   a->gchunks = (int)((rows + a->gsize - 1) / a->gsize);
   a->gt = (int)std::min<int64_t>(rows, a->gsize);
   const int64_t groups = (int64_t)n_layers * s.units_per_layer * a->gchunks, tiles = most_tiles(s, w, max_rows, a->gsize), all = tiles * groups;
-  int64_t ct = std::max<int64_t>(4, std::max(std::min<int64_t>((all + 255) / 256, 16), (all + 511) / 512));
+  int64_t ct = std::max<int64_t>(4, std::max(std::min<int64_t>((all + 255) / 256, 16), s.q4 ? (all + 511) / 512 : std::min<int64_t>((all + 511) / 512, 64)));
   if (tiles <= 12) ct = tiles;
   a->ctiles = (int)((std::min(ct, tiles) + 3) / 4 * 4);
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 23) / s.units_per_layer));
