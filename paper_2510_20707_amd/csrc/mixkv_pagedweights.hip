@@ -137,6 +137,7 @@ __global__ __launch_bounds__(256) void weights_step_kernel(PShape s, PWindow win
       const int i1 = work ? (once ? served : hi) * s.G : 0;
       for (int i0 = once ? 0 : lo * s.G; i0 < i1; i0 += 16) {
         if (!once) rows_from(i0, i1);
+        f32x4 xs[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           f32x4 x = {0.f, 0.f, 0.f, 0.f};
@@ -165,9 +166,14 @@ __global__ __launch_bounds__(256) void weights_step_kernel(PShape s, PWindow win
               }
             }
           }
+          xs[r] = x;
+        }
+        if (i0 + 16 >= i1 && i + 1 < n) request(i + 1);
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
           const int j = k0 + 16 * r + l16;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) run[r] += sees(win, place[e], j) ? fast_exp2(fmaf(x[e], Q4 ? c2[e] : s.scale_log2e, off[e])) : 0.f;
+          for (int e = 0; e < 4; ++e) run[r] += sees(win, place[e], j) ? fast_exp2(fmaf(xs[r][e], Q4 ? c2[e] : s.scale_log2e, off[e])) : 0.f;
         }
         if (++steps == kSumRun) {
           steps = 0;
@@ -175,7 +181,7 @@ __global__ __launch_bounds__(256) void weights_step_kernel(PShape s, PWindow win
           for (int r = 0; r < 2; ++r) { sum[r] += run[r]; run[r] = 0.f; }
         }
       }
-      if (i + 1 < n) request(i + 1);
+      if (!work && i + 1 < n) request(i + 1);
       const bool fresh = k0 + live > place0;               // the tile has new rows
       if (id < 0 || !(work || fresh)) continue;
       float x[2];
@@ -512,7 +518,7 @@ static size_t many_bytes(const PShape &s, const ManyShape &a, int n_layers) {
 static int step_tiles(const PShape &s, int nl, int max_rows) {
   const int64_t tiles = ((int64_t)max_rows + 31) / 32, units = (int64_t)s.units_per_layer * nl;
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 23) / units));
-  const int64_t ct = std::max<int64_t>(std::max<int64_t>(4, (tiles * units + 1023) / 1024), (tiles + most - 1) / most);
+  const int64_t ct = std::max<int64_t>(std::max<int64_t>(4, std::min<int64_t>((tiles * units + 1023) / 1024, 16)), (tiles + most - 1) / most);
   return (int)((std::min(ct, tiles) + 3) / 4 * 4);
 }
 
