@@ -199,15 +199,16 @@ __global__ __launch_bounds__(256) void weights_step_kernel(PShape s, PWindow win
 
 // ------------------------------------------------------------------------------------------------
 // weights_many_kernel (many rows, bf16 and 4-bit pages): a workgroup of eight waves to a block of keys and a chunk of the unit's rows.  A wave's keys stay in
-// registers as the first operand of 32 x 32 x 16 products (4 bits: in two fp16 parts), the rows travel through LDS, 64 a turn, and are the second for all
+// registers as the first operand of 32 x 32 x 16 products (4 bits: in two fp16 parts), the rows travel through LDS, 64 or 128 a turn, and are the second for all
 // of them: a lane has 16 keys of one row, adds their weights up over its rows, and the lanes are folded at the end.
 // ------------------------------------------------------------------------------------------------
-constexpr int kManyWaves = 8, kManyRows = 64, kManyRun = 256;       // turns whose weights a lane adds up: 2 each, so that they are off by 2^-15 at most
+constexpr int kManyWaves = 8, kManyRun = 16384;                     // rows whose weights a lane adds up on its own, every 32nd: they are off by 2^-15 at most
+constexpr int many_rows(bool q4) { return q4 ? 64 : 128; }          // rows of a turn
 constexpr int many_keys(bool q4) { return 32 * kManyWaves * (q4 ? 1 : 2); }    // keys of a workgroup
 
 struct ManyShape {
   PWindow w;
-  int32_t chunk, nchunks;                // rows of a chunk (a multiple of 64), chunks of a unit
+  int32_t chunk, nchunks;                // rows that a block's chunk should have, the most chunks of a block
   int32_t blocks;                        // blocks of keys of a unit in the launch; longer heads' are walked
   int64_t stride;                        // keys of a unit among the partial sums
 };
@@ -223,10 +224,16 @@ __device__ __forceinline__ Rows rows_that_see(const PShape &s, const PWindow &w,
   return r;
 }
 
+// The chunks of equal size, whole turns of R, that a block's rows fall into: rows of one.
+__device__ __forceinline__ int chunk_rows(const ManyShape &a, const Rows &r, int R) {
+  const int n = max(r.i1 - (r.i0 & -R), 1), pieces = min(a.nchunks, (n - 1) / a.chunk + 1);
+  return ((n - 1) / pieces / R + 1) * R;
+}
+
 template <int D, bool Q4>
 __global__ __launch_bounds__(64 * kManyWaves, 2) void weights_many_kernel(PShape s, ManyShape a, WinTable tab, WeightPtrs ptrs, float *part, int64_t unit0) {
-  constexpr int RB = D * 2, PPR = RB / 16, KS = D / 16, NG = D / 32, W = kManyWaves, KB = Q4 ? 1 : 2, KEYS = many_keys(Q4), R = kManyRows, IMG = R * RB;
-  __shared__ __align__(16) char img[2][IMG];
+  constexpr int RB = D * 2, PPR = RB / 16, KS = D / 16, NG = D / 32, W = kManyWaves, KB = Q4 ? 1 : 2, KEYS = many_keys(Q4), R = many_rows(Q4), WR = R / W, NY = R / 32, IMG = R * RB;
+  __shared__ __align__(256) char img[2][IMG];
   __shared__ float off_s[2][R], c2_s[2][R];
   __shared__ int place_s[2][R];
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
@@ -239,14 +246,14 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void weights_many_kernel(PShape
   const int len = head_rows(s, c, u), count = max(l.count[u], 0), start = l.start[u], place0 = len - count;
   const uint32_t img_a = lds_base_of(img);
   const int G = s.G, step_t = R / G, step_g = R - step_t * G;
-  const int64_t qsn = l.qsn, qsh = l.qsh, step_q = step_t * qsn + step_g * qsh, wrap_q = qsn - G * qsh;
+  const int64_t qsn = l.qsn, qsh = l.qsh;
   const char *const Q = l.Q + (int64_t)h * G * qsh;
   for (int block = blockIdx.y; (int64_t)block * KEYS < len; block += a.blocks) {
     const int kA = block * KEYS, kB = min(kA + KEYS, len);
     const Rows rows = rows_that_see(s, a.w, len, count, kA, kB);
     const bool direct = a.nchunks == 1 || kA >= a.stride;    // (keys that the host did not know of: all their rows in one go)
     if (direct && ch > 0) continue;                          // uniform
-    const int i0 = direct ? rows.i0 & ~(R - 1) : max(rows.i0 & ~(R - 1), ch * a.chunk), i1 = direct || ch == a.nchunks - 1 ? rows.i1 : min(rows.i1, (ch + 1) * a.chunk);
+    const int size = chunk_rows(a, rows, R), i0 = (rows.i0 & -R) + (direct ? 0 : ch * size), i1 = direct ? rows.i1 : (int)min((int64_t)rows.i1, (int64_t)i0 + size);
     if (i0 >= i1 && !direct) continue;                       // uniform: nobody reads these sums
     // ---- the wave's keys
     int id[KB], key0[KB];
@@ -274,56 +281,44 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void weights_many_kernel(PShape
         }
       }
     }
-    // ---- rows: what a thread stages, walked 64 a turn, a wave eight of them.  bf16: directly; 4 bits: eight threads to a row, to fp16 by a power of two that brings its
-    // largest element to [2^13, 2^14).  A row that is none gives nothing, whatever is staged for it.
-    struct At { const char *q; int t, g; };
-    auto at_row = [&](int i) {
-      At x;
-      x.t = i / G;
-      x.g = i - x.t * G;
-      x.q = Q + ((int64_t)start + x.t) * qsn + (int64_t)x.g * qsh;
-      return x;
-    };
-    auto walk = [&](At &x) __attribute__((always_inline)) {
-      x.t += step_t;
-      x.g += step_g;
-      x.q += step_q;
-      if (x.g >= G) { x.g -= G; ++x.t; x.q += wrap_q; }
-    };
-    auto there = [&](const At &x, int i) { return (i < i1) & ((uint32_t)(start + x.t) < (uint32_t)a.w.n_rows); };
-    constexpr int RPL = 64 / PPR, LOADS = Q4 ? 1 : 8 / RPL, PIECES = PPR / 8;    // bf16: rows of a load, loads of a wave; 4 bits: pieces of a thread
-    const int r_row = 8 * wave + (Q4 ? lane >> 3 : lane / PPR);
-    At q_at[LOADS];
-    int n_t = (i0 + 8 * wave + (lane & 7)) / G, n_g = i0 + 8 * wave + (lane & 7) - n_t * G;      // the row whose normaliser the lane stages
+    // ---- rows, walked R a turn, a wave staging WR of them.  Lane e of WR knows where row e of the wave lies and takes its normaliser; the lanes that load a row ask it.  bf16: straight
+    // to LDS; 4 bits: eight lanes to a row, to fp16 by a power of two that brings its largest element to [2^13, 2^14).  A row that is none gives nothing, whatever is staged for it.
+    // Row i + r of the turn that begins with row i = T G + g0 is (T, g0) and what r is of its own, and one new row on where the query heads come to G.  Rows [first_row, last_row) exist.
+    constexpr int RPL = 64 / PPR, LOADS = Q4 ? 1 : WR / RPL, PIECES = PPR / 8;   // bf16: rows of a load, loads of a wave; 4 bits: pieces of a thread
+    static_assert(!Q4 || WR == 8, "eight lanes to a row");
+    const int my_row = WR * wave + (lane & (WR - 1)), my_t = my_row / G, my_g = my_row - my_t * G;
+    const int64_t my_q = my_t * qsn + my_g * qsh, wrap_q = qsn - G * qsh;
+    const int first_row = (int)min((int64_t)max(-(int64_t)start, (int64_t)0) * G, (int64_t)i1), last_row = (int)min(max((int64_t)a.w.n_rows - start, (int64_t)0) * G, (int64_t)i1);
+    const int from = Q4 ? lane >> 3 : lane / PPR, r_row = WR * wave + from;      // the row of the lane's first load
+    int T = i0 / G, g0 = i0 - T * G;                         // of the next turn
     u32x4 q_raw[Q4 ? PIECES : 1];
     float n_lse = 0.f;
     int n_place = -1;
-#pragma unroll
-    for (int j = 0; j < LOADS; ++j) q_at[j] = at_row(i0 + r_row + j * RPL);
-    auto request = [&](int i, int to) __attribute__((always_inline)) {           // rows i ... i + 63
+    auto request = [&](int i, int to) __attribute__((always_inline)) {           // rows i ... i + R - 1, a turn after the other
+      const int64_t row0 = (int64_t)start + T;
+      const bool in = (i + my_row >= first_row) & (i + my_row < last_row), wraps = my_g >= G - g0;
+      const int64_t at = in ? row0 * qsn + g0 * qsh + my_q + (wraps ? wrap_q : 0) : 0;
 #pragma unroll
       for (int j = 0; j < LOADS; ++j) {
-        const int r = r_row + j * RPL;
-        const char *q = there(q_at[j], i + r) ? q_at[j].q : Q;
+        const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)at, from + j * RPL), hi = (uint32_t)__shfl((int)(uint32_t)(at >> 32), from + j * RPL);
+        const char *q = Q + (int64_t)((uint64_t)hi << 32 | lo);
         if constexpr (!Q4) {
-          load_to_lds<false>(q + ((lane % PPR) ^ tile_swz<MIXKV_BF16, D>(r)) * 16, img_a + to * IMG + (8 * wave + j * RPL) * RB);
+          load_to_lds<false>(q + ((lane % PPR) ^ tile_swz<MIXKV_BF16, D>(r_row + j * RPL)) * 16, img_a + to * IMG + (WR * wave + j * RPL) * RB);
         } else {
 #pragma unroll
           for (int k = 0; k < PIECES; ++k) q_raw[k] = *reinterpret_cast<const u32x4 *>(q + ((lane & 7) * PIECES + k) * 16);
         }
-        walk(q_at[j]);
       }
-      const bool in = (i + 8 * wave + (lane & 7) < i1) & ((uint32_t)(start + n_t) < (uint32_t)a.w.n_rows);
-      n_lse = l.lse[in ? (int64_t)(start + n_t) * s.hq + h * G + n_g : 0];
-      n_place = in ? place0 + n_t : -1;
-      n_t += step_t;
-      n_g += step_g;
-      if (n_g >= G) { n_g -= G; ++n_t; }
+      n_lse = l.lse[in ? row0 * s.hq + h * G + g0 + (my_t * s.hq + my_g) + (wraps ? s.hq - G : 0) : 0];
+      n_place = in ? place0 + T + my_t + (wraps ? 1 : 0) : -1;
+      T += step_t;
+      g0 += step_g;
+      if (g0 >= G) { g0 -= G; ++T; }
     };
     auto settle = [&](int to) __attribute__((always_inline)) {                   // what was requested, into LDS
-      if (lane < 8) {
-        off_s[to][8 * wave + lane] = n_lse * -1.44269504088896340736f;
-        place_s[to][8 * wave + lane] = n_lse != -INFINITY ? n_place : -1;
+      if (lane < WR) {
+        off_s[to][WR * wave + lane] = n_lse * -1.44269504088896340736f;
+        place_s[to][WR * wave + lane] = n_lse != -INFINITY ? n_place : -1;
       }
       if constexpr (Q4) {
         uint32_t most = 0;
@@ -345,11 +340,10 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void weights_many_kernel(PShape
         }
       }
     };
-    uint32_t q_off[KS];                                      // where the lane reads
-#pragma unroll
-    for (int k = 0; k < KS; ++k) q_off[k] = img_a + l32 * RB + ((2 * k + half) ^ tile_swz<MIXKV_BF16, D>(l32)) * 16;
+    const uint32_t q_off = img_a + l32 * RB + (half ^ tile_swz<MIXKV_BF16, D>(l32)) * 16;     // where the lane reads; piece 2 k + half of a row: 32 k ^ this one
 
-    // A lane's sums of a key's weights; and folded over the lanes, lane e of a half with the key 8 (e / 4) + 4 half + e % 4
+    // A lane's sums of a key's weights; and folded over the lanes of a half, lanes 2 e and 2 e + 1 with the key 8 (e / 4) + 4 half + e % 4.  The lanes share the sums out by halves: each
+    // gives the lane 16, 8, 4, 2 away those that it does not keep.
     const int kz = key0[KB - 1] + 31, window = a.w.window, first = a.w.first;
     const float scale = s.scale_log2e;
     float run[KB][16], mine[KB];
@@ -360,17 +354,19 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void weights_many_kernel(PShape
         for (int e = 0; e < 16; ++e) run[x][e] = 0.f;
     };
     auto fold = [&]() {
-      int at = l32;
-      asm volatile("" : "+v"(at));                           // (what is compared with it is not kept in scalar registers through the loop)
 #pragma unroll
-      for (int x = 0; x < KB; ++x)
+      for (int x = 0; x < KB; ++x) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          float t = run[x][e];
+        for (int st = 0; st < 4; ++st) {
+          const bool up = lane & (16 >> st);
 #pragma unroll
-          for (int o = 1; o < 32; o <<= 1) t += __shfl_xor(t, o);
-          mine[x] += at == e ? t : 0.f;
+          for (int e = 0; e < 8 >> st; ++e) {
+            const float a = run[x][e], b = run[x][(8 >> st) + e];
+            run[x][e] = (up ? b : a) + __shfl_xor(up ? a : b, 16 >> st);
+          }
         }
+        mine[x] += run[x][0] + __shfl_xor(run[x][0], 1);
+      }
     };
 #pragma unroll
     for (int x = 0; x < KB; ++x) mine[x] = 0.f;
@@ -379,89 +375,133 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void weights_many_kernel(PShape
       request(i0, 0);
       settle(0);
     }
-    for (int i = i0, to = 0; i < i1; i += R, to ^= 1) {
+    // A turn begins: its rows are in LDS, the lane's first operands are asked for; then the next turn's rows are, and it is seen whether every row sees every key.
+    int to = 0;
+    float off[NY], c2[NY];
+    bool all = false;
+    u32x4 qf[KS];
+    uint32_t q_now;
+    auto read_row = [&](int y, int k) __attribute__((always_inline)) {
+      asm volatile("" : "+v"(q_now));                        // (the KS addresses are not kept)
+      qf[k] = lds_vec((q_now ^ (32 * k)) + y * 32 * RB);
+    };
+    auto begin = [&]() __attribute__((always_inline)) {
       if constexpr (!Q4) wait_vm<0>();
       lds_barrier();
-      if (i + R < i1) request(i + R, to ^ 1);
-      // four blocks of 32 rows and 32 keys (4 bits: two)
-      float off[2], c2[2];
-      int place[2];
-      bool all = true;
+      q_now = q_off + to * IMG;
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
+      for (int y = 0; y < NY; ++y) {
         off[y] = off_s[to][32 * y + l32];
         c2[y] = Q4 ? c2_s[to][32 * y + l32] : scale;
-        place[y] = place_s[to][32 * y + l32];
-        all = all & (kz <= place[y]) & ((key0[0] > place[y] - window) | (kz < first));
       }
-      u32x4 qf[KS];
-      auto read_row = [&](int y, int k) __attribute__((always_inline)) { qf[k] = lds_vec(q_off[k] + to * IMG + y * 32 * RB); };
-      auto score = [&](int x, int k, f32x16 &acc) __attribute__((always_inline)) {
-        if (k == 0) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-        }
-        if constexpr (Q4) {
-          acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lf[x][k]), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
-          acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kf[x][k]), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
-        } else {
-          acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[x][k]), __builtin_bit_cast(bf16x8, qf[k]), acc, 0, 0, 0);
-        }
-      };
 #pragma unroll
       for (int k = 0; k < KS; ++k) read_row(0, k);
-      if (__builtin_expect(__builtin_amdgcn_ballot_w64(all) == ~0ull, 1)) {
-        // every row sees every key: a block's products with the weights of the one before, in the program's order
-        constexpr int N = 2 * KB;
-        f32x16 acc[2];
+    };
+    auto look = [&](int i) __attribute__((always_inline)) {
+      if (i + R < i1) request(i + R, to ^ 1);
+      all = true;
 #pragma unroll
-        for (int n = 0; n <= N; ++n)
+      for (int y = 0; y < NY; ++y) {
+        const int place = place_s[to][32 * y + l32];
+        all = all & (kz <= place) & ((key0[0] > place - window) | (kz < first));
+      }
+      all = __builtin_amdgcn_ballot_w64(all) == ~0ull;
+    };
+    auto score = [&](int x, int k, f32x16 &acc) __attribute__((always_inline)) {
+      if (k == 0) {
 #pragma unroll
-          for (int k = 0; k < KS; ++k) {
-            if (n < N) {
-              score(n % KB, k, acc[n & 1]);
-              if (n == KB - 1) read_row(1, k);
-            }
-            if (n > 0) {
-#pragma unroll
-              for (int e = k * 16 / KS; e < (k + 1) * 16 / KS; ++e)
-                run[(n - 1) % KB][e] += fast_exp2(fmaf(acc[(n - 1) & 1][e], c2[(n - 1) / KB], off[(n - 1) / KB]));
-            }
-            __builtin_amdgcn_sched_barrier(0);
-          }
+        for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+      }
+      if constexpr (Q4) {
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, lf[x][k]), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, kf[x][k]), __builtin_bit_cast(f16x8, qf[k]), acc, 0, 0, 0);
       } else {
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[x][k]), __builtin_bit_cast(bf16x8, qf[k]), acc, 0, 0, 0);
+      }
+    };
+    for (int i = i0; i < i1;) {
+      const int ib = min(i1 - i, kManyRun) + i;
+      begin();
+      look(i);
+      while (i < ib) {
+        if (__builtin_expect(all, 1)) {
+          // every row sees every key: a block's products with the weights of the one before, in the program's order; the last weights while the next turn's operands are on their way
+          constexpr int N = NY * KB;
+          do {
+            f32x16 acc[2];
+            auto weigh = [&](int n, int e, float o, float c) __attribute__((always_inline)) { run[n % KB][e] += fast_exp2(fmaf(acc[n & 1][e], c, o)); };
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          if (y) {
+            for (int n = 0; n < N; ++n)
 #pragma unroll
-            for (int k = 0; k < KS; ++k) read_row(1, k);
-          }
-          const int behind = place[y] - window;
-          int at = 4 * half;
-          asm volatile("" : "+v"(at));
+              for (int k = 0; k < KS; ++k) {
+                score(n % KB, k, acc[n & 1]);
+                if (n % KB == KB - 1 && n + 1 < N) read_row(n / KB + 1, k);
+                if (n > 0) {
+                  float t[16 / KS];                          // (side by side, not one after the other in one register)
 #pragma unroll
-          for (int x = 0; x < KB; ++x) {
-            if (__builtin_amdgcn_ballot_w64((key0[x] <= place[y]) & ((key0[x] + 31 > behind) | (key0[x] < first))) == 0) continue;
-            f32x16 acc;
+                  for (int e = 0; e < 16 / KS; ++e) t[e] = fmaf(acc[(n - 1) & 1][k * 16 / KS + e], c2[(n - 1) / KB], off[(n - 1) / KB]);
+                  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int k = 0; k < KS; ++k) score(x, k, acc);
+                  for (int e = 0; e < 16 / KS; ++e) t[e] = fast_exp2(t[e]);
+                  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int j = key0[x] + 8 * (e >> 2) + at + (e & 3);
-              run[x][e] += (j <= place[y]) & ((j > behind) | (j < first)) ? fast_exp2(fmaf(acc[e], c2[y], off[y])) : 0.f;
-              __builtin_amdgcn_sched_barrier(0);
+                  for (int e = 0; e < 16 / KS; ++e) run[(n - 1) % KB][k * 16 / KS + e] += t[e];
+                }
+                __builtin_amdgcn_sched_barrier(0);
+              }
+#pragma unroll
+            for (int x = 0; x < KB; ++x)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) asm volatile("" : "+v"(run[x][e]));   // (the sums are made here, not behind the loop's branches)
+            const float o = off[NY - 1], c = c2[NY - 1];
+            if (i + R < i1) settle(to ^ 1);
+            i += R;
+            to ^= 1;
+            if (i < ib) begin();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) weigh(N - 1, e, o, c);
+            if (i < ib) look(i);
+          } while (i < ib && all);
+        } else {
+#pragma unroll
+          for (int y = 0; y < NY; ++y) {
+            if (y) {
+#pragma unroll
+              for (int k = 0; k < KS; ++k) read_row(y, k);
             }
+            const int place = place_s[to][32 * y + l32], behind = place - window;
+            int at = 4 * half;
+            asm volatile("" : "+v"(at));
+#pragma unroll
+            for (int x = 0; x < KB; ++x) {
+              if (__builtin_amdgcn_ballot_w64((key0[x] <= place) & ((key0[x] + 31 > behind) | (key0[x] < first))) == 0) continue;
+              f32x16 acc;
+#pragma unroll
+              for (int k = 0; k < KS; ++k) score(x, k, acc);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const int j = key0[x] + 8 * (e >> 2) + at + (e & 3);
+                run[x][e] += (j <= place) & ((j > behind) | (j < first)) ? fast_exp2(fmaf(acc[e], c2[y], off[y])) : 0.f;
+                __builtin_amdgcn_sched_barrier(0);
+              }
+            }
+          }
+          if (i + R < i1) settle(to ^ 1);
+          i += R;
+          to ^= 1;
+          if (i < ib) {
+            begin();
+            look(i);
           }
         }
       }
-      if (i + R < i1) settle(to ^ 1);
-      if (__builtin_expect(((i - i0) / R & (kManyRun - 1)) == kManyRun - 1, 0)) { fold(); clear(); }
+      fold();
+      clear();
     }
-    fold();
 #pragma unroll
     for (int x = 0; x < KB; ++x) {
-      const int j = key0[x] + 8 * (l32 >> 2) + 4 * half + (l32 & 3);
-      if (l32 >= 16 || j >= len || id[x] < 0) continue;
+      const int j = key0[x] + 8 * (l32 >> 3) + 4 * half + (l32 >> 1 & 3);
+      if ((l32 & 1) || j >= len || id[x] < 0) continue;
       if (!direct) {
         part[((unit0 + (int64_t)layer * units + u) * a.nchunks + ch) * a.stride + j] = mine[x];
       } else if (rows.i0 < rows.i1 || j >= place0) {
@@ -474,7 +514,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void weights_many_kernel(PShape
 }
 
 // Adds up the chunks' sums, in their order.
-__global__ __launch_bounds__(256) void weights_fold_kernel(PShape s, ManyShape a, WinTable tab, WeightPtrs ptrs, const float *part, int64_t unit0, int keys) {
+__global__ __launch_bounds__(256) void weights_fold_kernel(PShape s, ManyShape a, WinTable tab, WeightPtrs ptrs, const float *part, int64_t unit0, int keys, int R) {
   const int u = blockIdx.x, layer = blockIdx.z;
   const PCache c = tab.c[layer];
   const WinLayer l = tab.l[layer];
@@ -490,21 +530,23 @@ __global__ __launch_bounds__(256) void weights_fold_kernel(PShape s, ManyShape a
     float x = fresh ? 0.f : *w, sum = 0.f;
     if (rows.i0 < rows.i1) {
       const float *p = part + (unit0 + (int64_t)layer * s.units_per_layer + u) * a.nchunks * a.stride + j;
-      const int c0 = min(rows.i0 / a.chunk, a.nchunks - 1), c1 = min((rows.i1 - 1) / a.chunk, a.nchunks - 1);
-      for (int k = c0; k <= c1; ++k) sum += p[k * a.stride];
+      const int n = (rows.i1 - 1 - (rows.i0 & -R)) / chunk_rows(a, rows, R) + 1;
+      for (int k = 0; k < n; ++k) sum += p[k * a.stride];
     }
     *w = x + sum;
   }
 }
 
-// Chunks of rows: enough for sixteen workgroups to a compute unit (half of which have rows, in a prompt), of at least 1024 rows.
+// Chunks of the rows that see a block of keys (those of the first keys, which every row sees, are as many and longer): enough for thirty-two workgroups to a compute unit, of
+// at least 1024 rows.
 static ManyShape many_config(const PShape &s, const PWindow &w, int n_layers, int max_rows) {
   ManyShape a{};
   a.w = w;
-  const int64_t rows = (int64_t)w.max_count * s.G, keys = many_keys(s.q4 != 0), blocks = ((int64_t)max_rows + keys - 1) / keys, units = (int64_t)n_layers * s.units_per_layer;
+  const int64_t R = many_rows(s.q4 != 0), keys = many_keys(s.q4 != 0), blocks = ((int64_t)max_rows + keys - 1) / keys, units = (int64_t)n_layers * s.units_per_layer;
+  const int64_t rows = std::min<int64_t>(w.max_count, (int64_t)w.window + keys) * s.G;
   a.stride = blocks * keys;
-  const int64_t chunk = std::max<int64_t>(std::max<int64_t>(1024, rows * blocks / 4096 * units), rows * units >> 20);
-  a.chunk = (int)((std::min(chunk, rows) + kManyRows - 1) / kManyRows * kManyRows);
+  const int64_t chunk = std::max<int64_t>(std::max<int64_t>(1024, rows * blocks / 8192 * units), rows * units >> 20);
+  a.chunk = (int)((std::min(chunk, rows) + R - 1) / R * R);
   a.nchunks = (int)((rows + a.chunk - 1) / a.chunk);
   a.blocks = (int)std::min<int64_t>(blocks, 65535);
   return a;
@@ -582,7 +624,7 @@ extern "C" mixkv_status mixkv_paged_weights(const mixkv_paged_params *params, co
       if (a.nchunks > 1) {
         const int64_t y = std::min<int64_t>((a.stride + 255) / 256, std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 23) / ((int64_t)s.units_per_layer * nl))));
         hipLaunchKernelGGL(weights_fold_kernel, dim3((unsigned)s.units_per_layer, (unsigned)y, (unsigned)nl), dim3(256), 0, stream, s, a, t, p, (const float *)part, unit0,
-                           many_keys(s.q4 != 0));
+                           many_keys(s.q4 != 0), many_rows(s.q4 != 0));
       }
       if (hipGetLastError() != hipSuccess) return MIXKV_ERR_HIP;
       continue;
