@@ -427,14 +427,14 @@ __device__ __forceinline__ void store_page_bounds(char *dst, bool there, int wav
       w[2 * Q + i] = __float_as_uint(ra.hi[i]) ^ other; w[3 * Q + i] = __float_as_uint(rb.hi[i]) ^ other;
     }
   }
-  int size = NW / 2;
 #pragma unroll
-  for (int off = 32; off >= LPR; off >>= 1, size >>= 1) {
-    const bool up = lane & off;
+  for (int st = 0; 32 >> st >= LPR; ++st) {
+    const bool up = lane & (32 >> st);
+    constexpr int half = NW / 2;
 #pragma unroll
-    for (int i = 0; i < size; ++i) {
-      const uint32_t keep = up ? w[size + i] : w[i], give = up ? w[i] : w[size + i];
-      w[i] = least_of(ra, keep, (uint32_t)__shfl_xor((int)give, off));
+    for (int i = 0; i < half >> st; ++i) {
+      const uint32_t a = w[i], b = w[(half >> st) + i];
+      w[i] = least_of(ra, up ? b : a, (uint32_t)__shfl_xor((int)(up ? a : b), 32 >> st));
     }
   }
   constexpr int C = NW * LPR / 64;                          // the words that are left
