@@ -102,10 +102,20 @@ def test_weights_that_are_equal_or_no_numbers(what, n):
             assert kept[0, h, :len(want)].tolist() == want and (kept[0, h, len(want):] == -1).all(), (what, keep, h)
 
 
-@pytest.mark.parametrize("n", [3000, 8193, 16384, 16385, 40000, 70000, 140000])
+@pytest.mark.parametrize("n", [3000, 8193, 16384, 16385, 40000, 70000, 140000, 300000])
 def test_long_heads(n):
     """Heads around what a workgroup takes at once, the choice compared with a sort."""
-    print(f"[case] evict long n={n}", flush=True)
+    _long(n, n)
+
+
+@pytest.mark.parametrize("n,max_rows", [(3000, 100), (6000, 3000), (20000, 16000), (20000, 16385), (40000, 17000)])
+def test_heads_longer_than_the_host_said(n, max_rows):
+    """They are served all the same, whichever kernel was chosen for shorter ones."""
+    _long(n, max_rows)
+
+
+def _long(n, max_rows):
+    print(f"[case] evict long n={n} max_rows={max_rows}", flush=True)
     rng = np.random.default_rng([84, n])
     D, P = 64, 32
     pages = -(-n // P)
@@ -133,7 +143,7 @@ def test_long_heads(n):
             at += m
         into = B.PagedCache(*out, T.i32(into_table), T.i32(np.zeros((1, 3))))
         w_into = torch.zeros((n_pages, P), device=T.DEV)
-        (kept,) = B.mixkv_paged_evict(p, [cache], [into], [torch.from_numpy(w).to(T.DEV)], [T.i32(keep)], int(keep.max()), first, last, weights_into=[w_into], max_rows=n)
+        (kept,) = B.mixkv_paged_evict(p, [cache], [into], [torch.from_numpy(w).to(T.DEV)], [T.i32(keep)], int(keep.max()), first, last, weights_into=[w_into], max_rows=max_rows)
         kept = kept.cpu().numpy()
         assert np.array_equal(into.lengths.cpu().numpy(), keep)
         for h in range(3):
@@ -149,6 +159,40 @@ def test_long_heads(n):
             r = torch.from_numpy(best % P).to(T.DEV)
             assert torch.equal(out[0][dst, i % P], K[src, r]) and torch.equal(out[1][dst, i % P], V[src, r])
             assert np.array_equal(w_into.cpu().numpy()[into_table[0, h, np.arange(len(best)) // P], np.arange(len(best)) % P], w[table[0, h, best // P], best % P])
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS)
+def test_long_heads_with_missing_pages_beside_short_ones(fmt, dtype):
+    rng = np.random.default_rng(86)
+    lay = T.Layer(rng, fmt, dtype, 64, 128, [[18000, 0], [40, 16700]], 141, spare=220, bounds=True, fill=False)
+    lay.K &= np.uint8(0xbf)                            # numbers below 2, of both signs, and steps and bases of the same kind
+    lay.table[0, 0, 3], lay.table[0, 0, 100], lay.table[1, 1, 0] = -1, lay.n_pages, -9
+    w = _weights(rng, lay)
+    for keep, first, last in (([[9000, 5], [40, 16000]], 10, 300), ([[17999, 1], [7, 0]], 0, 0)):
+        _check(rng, lay, w, np.array(keep, np.int32), 17999, first, last, own_pool=False)
+
+
+def test_long_heads_of_several_layers():
+    """Each layer's choice is what a call for it alone gives."""
+    rng = np.random.default_rng(87)
+    n, P, D = 17500, 128, 64
+    pages = -(-n // P)
+    p = B.make_paged_params("bf16", "rows", 2, 2, 2, D, P, pages, 8 * pages)
+    caches, into, ws, keeps = [], [], [], []
+    for i in range(3):
+        ids = rng.permutation(8 * pages).astype(np.int32)
+        K, V = (torch.randn((8 * pages, P, D), device=T.DEV).bfloat16() for _ in range(2))
+        caches.append(B.PagedCache(K, V, T.i32(ids[:4 * pages].reshape(2, 2, pages)), T.i32([[n, n - 1000 * i], [30, 16385 + i]])))
+        into.append(lambda K=K, V=V, ids=ids: B.PagedCache(K.clone(), V.clone(), T.i32(ids[4 * pages:].reshape(2, 2, pages)), T.i32(np.zeros((2, 2)))))
+        ws.append(torch.from_numpy(np.exp(rng.standard_normal((8 * pages, P))).astype(np.float32)).to(T.DEV))
+        keeps.append(T.i32([[8000, 9000], [20, 16000]]))
+    together = [z() for z in into]
+    kept = B.mixkv_paged_evict(p, caches, together, ws, keeps, 16000, 4, 64)
+    for i in range(3):
+        alone = into[i]()
+        (one,) = B.mixkv_paged_evict(p, [caches[i]], [alone], [ws[i]], [keeps[i]], 16000, 4, 64)
+        assert torch.equal(one, kept[i]) and torch.equal(alone.lengths, together[i].lengths)
+        assert torch.equal(alone.K_pages, together[i].K_pages) and torch.equal(alone.V_pages, together[i].V_pages)
 
 
 def test_many_layers_and_a_captured_call():

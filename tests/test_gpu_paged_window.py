@@ -90,6 +90,41 @@ def test_a_chunk_behind_a_long_cache(fmt, dtype, D, G):
 
 
 @pytest.mark.parametrize("fmt,dtype", KINDS)
+@pytest.mark.parametrize("count", [1, 6, 400])
+def test_heads_longer_than_the_host_said(fmt, dtype, count):
+    rng = np.random.default_rng([74, count])
+    lay = T.Layer(rng, fmt, dtype, 64, 64, [[1800, 900]], 29, fill=True)
+    rows = R.Rows(rng, lay, 8, [count])
+    for window, first in ((R.ALL, 0), (700, 40)):
+        _both(rng, rows, window, first, max_rows=300)
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS)
+@pytest.mark.parametrize("D,G,count", [(128, 33, 1), (64, 80, 1), (64, 130, 2), (128, 257, 1)])
+def test_more_query_heads_than_a_group(fmt, dtype, D, G, count):
+    rng = np.random.default_rng([75, G])
+    lay = T.Layer(rng, fmt, dtype, D, 64, [[70, 300], [1, 129]], 5, fill=True)
+    rows = R.Rows(rng, lay, 2 * G, [count] * 2)
+    for window, first in ((R.ALL, 0), (50, 3)):
+        _both(rng, rows, window, first, strided=True)
+
+
+@pytest.mark.parametrize("fmt,dtype", [("rows", "bf16"), ("4bit", "bf16")])
+@pytest.mark.parametrize("window,first", [(R.ALL, 0), (100, 600), (900, 10)])
+def test_prompts_of_several_blocks_and_chunks(fmt, dtype, window, first):
+    """More keys than a workgroup takes, more rows than a chunk has, first rows that fill a block."""
+    print(f"[case] blocks {fmt} window={window} first={first}", flush=True)
+    rng = np.random.default_rng([76, first])
+    lay = T.Layer(rng, fmt, dtype, 64, 128, [[1500, 700]], 12, fill=True)
+    rows = R.Rows(rng, lay, 6, np.array([[1500, 700]]))
+    q = _both(rng, rows, window, first)
+    w = [torch.zeros((lay.n_pages, lay.P), device=T.DEV) for _ in range(2)]
+    for x in w:
+        B.mixkv_paged_weights(lay.params(rows.hq), [lay.device()], [q], [x], window, first)
+    assert torch.equal(*w)                                                           # repeated bit for bit
+
+
+@pytest.mark.parametrize("fmt,dtype", KINDS)
 @pytest.mark.parametrize("count", [1, 4, 90])
 def test_rows_and_pages_that_are_none(fmt, dtype, count):
     """Entries that are no page, lengths beyond the table and below zero, more new rows than the head has, rows outside the dense ones, more than max_count."""
