@@ -454,6 +454,8 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
 // Offsets as in decode_mfma_kernel, with a limit of their own.
 // Bound: memory, a tile of each wave in flight and not always whole: value loads are branches (rows that may not exist), so that a tile's values are waited for
 // before its last score product, and the next tile's keys alone are on their way during the weights.  bf16, 16 sequences of 8192 rows, 8 heads of 128, 537 MB in 94 us, 5.7 TB/s.
+// NQ: blocks of 16 rows of a group, for new rows (WIN), each with its own weights and sums, on one read of the tile: 16 sequences of 3000 to 32 768 rows, five new rows each, 1.27 GB
+// in 254 us, 5.0 TB/s.
 // ------------------------------------------------------------------------------------------------
 // A lane's sum of weights that reaches this moves the head's offset.  The weighted values stay below it times the largest value: values of up to 2^100
 // do not overflow, whatever the logits behind them.
@@ -956,14 +958,18 @@ WinTable window_table(const mixkv_paged_cache *c, const mixkv_paged_queries *q, 
 }
 
 // The same dealing for groups of rows with a window: the tiles that a group may see, at most.  Chunks grow without end where there are groups enough, as
-// there are for prompts.
+// there are for fp32 prompts.  Heads of unequal length want more chunks than the chip takes at once, on full-precision pages: five new rows of 16 sequences of up
+// to 32 768 rows, 32 query heads on 8, 254 us in chunks of 64 tiles (2048 in all, if every head were the longest), 282 of 32, 272 of 128, 287 of 256; 4-bit pages do
+// not: 64 sequences of up to 16 384 rows, window 4096, 56 us in chunks of 130, 64 to 68 of 32 to 128.
+// Rows of a group: 16, or 32 in bf16 where there are more than 16, so that keys and values are read once for them: the five new rows took 382 us in groups of 16 side by
+// side (432 one after another, without the L2).  fp32 has no registers for it, and 4 bits not for as many waves.
 static void window_config(const PShape &s, const PWindow &w, int dtype, int n_layers, int max_rows, AShape *a) {
   const int64_t rows = (int64_t)w.max_count * s.G;
   a->gsize = dtype == MIXKV_BF16 && !s.q4 && rows > kAttnHeads ? 2 * kAttnHeads : kAttnHeads;
   a->gchunks = (int)((rows + a->gsize - 1) / a->gsize);
   a->gt = (int)std::min<int64_t>(rows, a->gsize);
   const int64_t groups = (int64_t)n_layers * s.units_per_layer * a->gchunks, tiles = most_tiles(s, w, max_rows, a->gsize), all = tiles * groups;
-  int64_t ct = std::max<int64_t>(4, std::max(std::min<int64_t>((all + 255) / 256, 16), s.q4 ? (all + 511) / 512 : std::min<int64_t>((all + 511) / 512, 64)));
+  int64_t ct = std::max<int64_t>(4, std::max(std::min<int64_t>((all + 255) / 256, 16), (all + (s.q4 ? 511 : 2047)) / (s.q4 ? 512 : 2048)));
   if (tiles <= 12) ct = tiles;
   a->ctiles = (int)((std::min(ct, tiles) + 3) / 4 * 4);
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 23) / s.units_per_layer));

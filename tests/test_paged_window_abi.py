@@ -90,6 +90,8 @@ def test_workspaces():
         kw = dict(p=p, window=1 << 30, first=0, count=count, most=most)
         assert _attend(ws=None, **kw) == _attend(ws=0x900080, **kw) == INVALID and _attend(size=need - 256, **kw) == SMALL
     assert B.mixkv_paged_window_attention_workspace_size(_params(), 1, 100, 64, 0, 1, 1 << 30) == 0        # a short window: whole
+    p = _params(dtype="f32", format="rows", max_pages=4000)
+    assert B.mixkv_paged_window_attention_workspace_size(p, 1, 16384, 1 << 30, 0, 16384, 16384) == 0        # fp32 prompts: groups enough, no partial sums
     for size in (B.lib().mixkv_paged_window_attention_workspace_size, B.lib().mixkv_paged_weights_workspace_size):
         assert size(C.byref(_params()), 1, 10, 5, 0, 1, 100, None) == INVALID and size(C.byref(_params()), 0, 10, 5, 0, 1, 100, C.byref(C.c_size_t())) == INVALID
     assert B.lib().mixkv_paged_evict_workspace_size(C.byref(_params()), 1, 0, C.byref(C.c_size_t())) == INVALID
