@@ -961,6 +961,7 @@ WinTable window_table(const mixkv_paged_cache *c, const mixkv_paged_queries *q, 
 // there are for fp32 prompts.  Heads of unequal length want more chunks than the chip takes at once, on full-precision pages: five new rows of 16 sequences of up
 // to 32 768 rows, 32 query heads on 8, 254 us in chunks of 64 tiles (2048 in all, if every head were the longest), 282 of 32, 272 of 128, 287 of 256; 4-bit pages do
 // not: 64 sequences of up to 16 384 rows, window 4096, 56 us in chunks of 130, 64 to 68 of 32 to 128.
+// Few tiles go to one workgroup each, without a merge: 208 groups of 25 tiles 18 us, in two chunks 26; 4 groups of 33 tiles 20 us, in nine chunks 12.
 // Rows of a group: 16, or 32 in bf16 where there are more than 16, so that keys and values are read once for them: the five new rows took 382 us in groups of 16 side by
 // side (432 one after another, without the L2).  fp32 has no registers for it, and 4 bits not for as many waves.
 static void window_config(const PShape &s, const PWindow &w, int dtype, int n_layers, int max_rows, AShape *a) {
@@ -970,7 +971,7 @@ static void window_config(const PShape &s, const PWindow &w, int dtype, int n_la
   a->gt = (int)std::min<int64_t>(rows, a->gsize);
   const int64_t groups = (int64_t)n_layers * s.units_per_layer * a->gchunks, tiles = most_tiles(s, w, max_rows, a->gsize), all = tiles * groups;
   int64_t ct = std::max<int64_t>(4, std::max(std::min<int64_t>((all + 255) / 256, 16), (all + (s.q4 ? 511 : 2047)) / (s.q4 ? 512 : 2048)));
-  if (tiles <= 12) ct = tiles;
+  if (tiles <= (groups >= 128 ? 32 : 12)) ct = tiles;
   a->ctiles = (int)((std::min(ct, tiles) + 3) / 4 * 4);
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 23) / s.units_per_layer));
   a->nchunks = (int)std::min(most, std::max<int64_t>(1, (tiles + a->ctiles - 1) / a->ctiles));
