@@ -832,12 +832,13 @@ static size_t attn_bytes(const PShape &s, const AShape &a, int n_layers) { retur
 template <bool ONCE, bool WIN, int NQ = 1, typename Go>
 static void launch_attention(const PShape &s, int dtype, Go &&go) {
   constexpr int B16 = MIXKV_BF16, F32 = MIXKV_F32;
+  constexpr int N16 = WIN && !ONCE ? 2 : NQ;                 // (more than one group of new rows: of 32)
   if (s.q4) {
     if (s.D == 128) go(paged_q4_kernel<128, ONCE, WIN>, paged_merge_kernel<B16, 128, WIN>);
     else go(paged_q4_kernel<64, ONCE, WIN>, paged_merge_kernel<B16, 64, WIN>);
   } else if (dtype == B16) {
-    if (s.D == 128) go(paged_rows_kernel<B16, 128, ONCE, WIN, NQ>, paged_merge_kernel<B16, 128, WIN>);
-    else go(paged_rows_kernel<B16, 64, ONCE, WIN, NQ>, paged_merge_kernel<B16, 64, WIN>);
+    if (s.D == 128) go(paged_rows_kernel<B16, 128, ONCE, WIN, N16>, paged_merge_kernel<B16, 128, WIN>);
+    else go(paged_rows_kernel<B16, 64, ONCE, WIN, N16>, paged_merge_kernel<B16, 64, WIN>);
   } else {
     if (s.D == 128) go(paged_rows_kernel<F32, 128, ONCE, WIN>, paged_merge_kernel<F32, 128, WIN>);
     else go(paged_rows_kernel<F32, 64, ONCE, WIN>, paged_merge_kernel<F32, 64, WIN>);
