@@ -16,7 +16,7 @@ struct EvictLayer {
 };
 constexpr int kEvictLayers = 24;          // pointer-table entries of a launch
 struct EvictTable { PCache c[kEvictLayers]; EvictLayer l[kEvictLayers]; };
-static_assert(sizeof(EvictTable) <= 3072, "kernel arguments have to fit in 4 KB");
+static_assert(sizeof(EvictTable) <= 3500, "kernel arguments have to fit in 4 KB");
 
 struct EvictShape { int32_t max_keep, first, last; };
 

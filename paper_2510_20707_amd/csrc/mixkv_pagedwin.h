@@ -15,7 +15,7 @@ struct WinLayer {
   float *lse;
 };
 struct WinTable { PCache c[kLayersPerLaunch]; WinLayer l[kLayersPerLaunch]; };
-static_assert(sizeof(WinTable) <= 3072, "kernel arguments have to fit in 4 KB");
+static_assert(sizeof(WinTable) <= 3500, "kernel arguments have to fit in 4 KB");
 
 // A row at place p sees the places j <= p with j > p - window or j < first.
 struct PWindow {
