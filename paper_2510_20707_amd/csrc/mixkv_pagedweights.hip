@@ -17,7 +17,7 @@ constexpr int kSumRun = 64;              // steps of 16 rows whose weights are s
 // Bound: memory, a tile of each wave in flight, the next one asked for before the exponentials: 32 sequences of up to 16 384 rows, 32 query heads on 8, 570 MB in 120 us, 4.7 TB/s.
 // Workgroups of 16 tiles: heads of unequal length then end together (121 us; 64 tiles 133, 128 156, 4 144).  Loads past the caches: 124.
 // ------------------------------------------------------------------------------------------------
-template <int DT, int D, bool Q4>
+template <int DT, int D, bool Q4, bool AHEAD = false>
 __global__ __launch_bounds__(256) void weights_step_kernel(PShape s, PWindow win, WinTable tab, WeightPtrs ptrs, int ctiles) {
   constexpr bool F32 = DT == MIXKV_F32;
   constexpr int EB = F32 ? 4 : 2, RB = D * EB, NC = RB / 64, NG = D / 32, W = 4;
@@ -30,46 +30,57 @@ __global__ __launch_bounds__(256) void weights_step_kernel(PShape s, PWindow win
   float *weights = ptrs.w[layer];
   const int len = head_rows(s, c, u), count = max(l.count[u], 0), start = l.start[u];
   const int place0 = len - count, served = min(count, win.max_count), all = (len + 31) >> 5;
-  const int t0 = blockIdx.y * ctiles, t1 = blockIdx.y + 1 == gridDim.y ? all : min(all, t0 + ctiles);
+  // the tiles of the first rows, and those from the first new row's window on
+  const int ns = (min(win.first, len) + 31) >> 5, w0 = max(ns, max(0, max(place0, 0) - win.window + 1) >> 5), tiles = ns + max(0, all - w0);
+  auto tile_at = [&](int t) { return t < ns ? t : w0 + (t - ns); };
+  const int t0 = blockIdx.y * ctiles, t1 = blockIdx.y + 1 == gridDim.y ? tiles : min(tiles, t0 + ctiles);
   if (t0 >= t1) return;
 
-  // ---- 16 rows: their queries, and of the rows 4 quad + e the normalisers and places
-  u32x4 qf[Q4 ? NG : NC];
+  // ---- 16 rows: their queries, and of the rows 4 quad + e the normalisers and places.  AHEAD (fp32 of many rows): the next ones are asked for while one is worked on.
+  constexpr int NQ = Q4 ? NG : NC;
+  u32x4 qf[NQ], qn[NQ];
   f16x8 qs;
-  float off[4], c2[4];
-  int place[4];
-  auto rows_from = [&](int i0, int i1) {
-    {
-      const int i = min(i0 + l16, i1 - 1), t = i / s.G, g = i - t * s.G;
-      const int64_t row = min(max((int64_t)start + t, (int64_t)0), (int64_t)win.n_rows - 1);
-      const char *q = l.Q + row * l.qsn + (int64_t)(h * s.G + g) * l.qsh;
-      if constexpr (!Q4) {
+  float off[4], c2[4], lse = 0.f;
+  int place[4], place_n = -1, row_t = 0, row_g = 0;          // row l16 of the next 16: its new row and query head
+  const int step_t = 16 / s.G, step_g = 16 - step_t * s.G;
+  auto begin_rows = [&](int i0) { row_t = (i0 + l16) / s.G; row_g = i0 + l16 - row_t * s.G; };
+  auto ask_rows = [&](int i0, int i1) {                      // one after another
+    const int64_t row = (int64_t)start + row_t, near = min(max(row, (int64_t)0), (int64_t)win.n_rows - 1);
+    const char *q = l.Q + near * l.qsn + (int64_t)(h * s.G + row_g) * l.qsh;
 #pragma unroll
-        for (int k = 0; k < NC; ++k) qf[k] = *reinterpret_cast<const u32x4 *>(q + (4 * k + quad) * 16);
-      } else {
-        // to fp16, by a power of two that brings the row's largest element to [2^13, 2^14); their sums over each group in two parts, against a key's (S, B) pairs
-        u32x4 qr[NG];
+    for (int k = 0; k < NQ; ++k) qn[k] = *reinterpret_cast<const u32x4 *>(q + (Q4 ? (32 * (D == 128 ? (k & 1) * 2 + (k >> 1) : k) + 8 * quad) * 2 : (4 * k + quad) * 16));
+    const bool there = i0 + l16 < i1 && near == row;
+    lse = l.lse[near * s.hq + h * s.G + row_g];
+    place_n = there ? place0 + row_t : -1;
+    row_t += step_t;
+    row_g += step_g;
+    if (row_g >= s.G) { row_g -= s.G; ++row_t; }
+  };
+  auto take_rows = [&]() {
+    if constexpr (!Q4) {
+#pragma unroll
+      for (int k = 0; k < NQ; ++k) qf[k] = qn[k];
+    } else {
+        // to fp16, by a power of two that brings the row's largest element to [2^13, 2^14); their sums over each group in three parts, against a key's (S, B) pairs
         uint32_t most = 0;
 #pragma unroll
-        for (int pl = 0; pl < NG; ++pl) {
-          qr[pl] = *reinterpret_cast<const u32x4 *>(q + (32 * (D == 128 ? (pl & 1) * 2 + (pl >> 1) : pl) + 8 * quad) * 2);
+        for (int pl = 0; pl < NG; ++pl)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) most = max(most, max(qr[pl][j] & 0x7fffu, (qr[pl][j] >> 16) & 0x7fffu));
-        }
+          for (int j = 0; j < 4; ++j) most = max(most, max(qn[pl][j] & 0x7fffu, (qn[pl][j] >> 16) & 0x7fffu));
         most = max(most, (uint32_t)__shfl_xor((int)most, 16));
         most = max(most, (uint32_t)__shfl_xor((int)most, 32));
         const int up = 13 - (min(max((int)(most >> 7), 1), 254) - 127);
         const float back = fminf(fmaxf(ldexpf(s.scale_log2e, 20 - up), 0x1p-126f), 0x1p100f);   // (as in paged_q4_kernel: neither zero nor infinite)
 #pragma unroll
         for (int e = 0; e < 4; ++e) c2[e] = __shfl(back, 4 * quad + e);
-        float hi[NG], lo[NG];
+        float part[NG];
 #pragma unroll
         for (int pl = 0; pl < NG; ++pl) {
           float sum = 0.f;
           f16x8 x;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const uint32_t w = qr[pl][e >> 1];
+            const uint32_t w = qn[pl][e >> 1];
             const float v = ldexpf(__uint_as_float(e & 1 ? w & 0xffff0000u : w << 16), up);
             sum += v;
             x[e] = (_Float16)((e >> 1) & 1 ? v * 0.0625f : v);
@@ -78,35 +89,34 @@ __global__ __launch_bounds__(256) void weights_step_kernel(PShape s, PWindow win
           sum += __shfl_xor(sum, 16);
           sum += __shfl_xor(sum, 32);
           sum *= 0.00390625f;
-          hi[pl] = (float)(_Float16)sum;
-          lo[pl] = sum - hi[pl];
+          const float hi = (float)(_Float16)sum, mid = (float)(_Float16)(sum - hi);
+          part[pl] = quad == 0 ? hi : quad == 1 ? mid : quad == 2 ? sum - hi - mid : 0.f;
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) qs[e] = (_Float16)(e / 2 < NG ? (quad == 0 ? hi[e / 2 % NG] : (quad == 1 ? lo[e / 2 % NG] : 0.f)) : 0.f);
-      }
+        for (int e = 0; e < 8; ++e) qs[e] = (_Float16)(e / 2 < NG ? part[e / 2 % NG] : 0.f);
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int i = i0 + 4 * quad + e, t = min(i, i1 - 1) / s.G, g = min(i, i1 - 1) - t * s.G;
-      const int64_t row = (int64_t)start + t;
-      const bool there = i < i1 && row >= 0 && row < win.n_rows;
-      const float lse = l.lse[(there ? row : 0) * s.hq + h * s.G + g];
-      off[e] = lse * -1.44269504088896340736f;
-      place[e] = there && lse != -INFINITY ? place0 + t : -1;           // -1: the row gives nothing
+      off[e] = __shfl(lse * -1.44269504088896340736f, 4 * quad + e);
+      place[e] = __shfl(lse != -INFINITY ? place_n : -1, 4 * quad + e);  // -1: the row gives nothing
     }
   };
   const bool once = (int64_t)served * s.G <= 16;
-  if (once && served > 0) rows_from(0, served * s.G);
+  if (once && served > 0) {
+    begin_rows(0);
+    ask_rows(0, served * s.G);
+    take_rows();
+  }
 
   for (int first = t0 + wave; first < t1; first += 64 * W) {
     // lane i: where the wave's i-th tile of 64 lies
     const int mine = first + lane * W;
-    const int id_of = mine < t1 ? page_at(s, c, u, mine >> (s.lp - 5)) : -1;
+    const int id_of = mine < t1 ? page_at(s, c, u, tile_at(mine) >> (s.lp - 5)) : -1;
     const int n = min((t1 - first + W - 1) / W, 64);
     u32x4 kr[2][NK];
     float old = 0.f;
     auto request = [&](int i) {
-      const int id = max(__builtin_amdgcn_readlane(id_of, i), 0), row0 = (first + i * W) * 32 & (s.P - 1);
+      const int id = max(__builtin_amdgcn_readlane(id_of, i), 0), row0 = tile_at(first + i * W) * 32 & (s.P - 1);
       const char *page = c.K + (int64_t)id * s.page_bytes;
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
@@ -129,7 +139,7 @@ __global__ __launch_bounds__(256) void weights_step_kernel(PShape s, PWindow win
     };
     request(0);
     for (int i = 0; i < n; ++i) {
-      const int tile = first + i * W, k0 = tile * 32, live = min(len - k0, 32), id = __builtin_amdgcn_readlane(id_of, i);
+      const int k0 = tile_at(first + i * W) * 32, live = min(len - k0, 32), id = __builtin_amdgcn_readlane(id_of, i);
       const float was = old;
       // new rows [lo, hi) see some of the tile's keys
       const int lo = max(k0 - place0, 0), hi = k0 < win.first ? served : (int)min((int64_t)served, (int64_t)k0 + 31 + win.window - place0);
@@ -137,8 +147,16 @@ __global__ __launch_bounds__(256) void weights_step_kernel(PShape s, PWindow win
       float sum[2] = {0.f, 0.f}, run[2] = {0.f, 0.f};
       int steps = 0;
       const int i1 = work ? (once ? served : hi) * s.G : 0;
+      if (work && !once) {
+        begin_rows(lo * s.G);
+        if constexpr (AHEAD) ask_rows(lo * s.G, i1);
+      }
       for (int i0 = once ? 0 : lo * s.G; i0 < i1; i0 += 16) {
-        if (!once) rows_from(i0, i1);
+        if (!once) {
+          if constexpr (!AHEAD) ask_rows(i0, i1);
+          take_rows();
+          if (AHEAD && i0 + 16 < i1) ask_rows(i0 + 16, i1);
+        }
         f32x4 xs[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
@@ -157,18 +175,19 @@ __global__ __launch_bounds__(256) void weights_step_kernel(PShape s, PWindow win
 #pragma unroll
               for (int e = 0; e < 4; ++e) x[e] = fmaf(step, y[e], x[e]);
             }
-          } else {
+          } else if constexpr (!F32) {
 #pragma unroll
-            for (int k = 0; k < NC; ++k) {
-              if constexpr (F32) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(qf[k][e]), __uint_as_float(kr[r][k][e]), x, 0, 0, 0);
-              } else {
-                x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qf[k]), __builtin_bit_cast(bf16x8, kr[r][k]), x, 0, 0, 0);
-              }
-            }
+            for (int k = 0; k < NC; ++k) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qf[k]), __builtin_bit_cast(bf16x8, kr[r][k]), x, 0, 0, 0);
           }
           xs[r] = x;
+        }
+        if constexpr (F32) {                                 // the two keys by turns: no product waits for the one before
+#pragma unroll
+          for (int k = 0; k < NC; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int r = 0; r < 2; ++r) xs[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(qf[k][e]), __uint_as_float(kr[r][k][e]), xs[r], 0, 0, 0);
         }
         if (i0 + 16 >= i1 && i + 1 < n) request(i + 1);
 #pragma unroll
@@ -543,17 +562,18 @@ __global__ __launch_bounds__(256) void weights_fold_kernel(PShape s, ManyShape a
   }
 }
 
-// Chunks of the rows that see a block of keys (those of the first keys, which every row sees, are as many and longer): enough for thirty-two workgroups to a compute unit (of which
-// a causal prompt leaves half empty), of at least 1024 rows: two prompts 1.19 ms, with half as many 1.22.
+// Chunks of the rows that see a block of keys (those of the first keys, which every row sees, are up to twice as long): enough for thirty-two workgroups to a compute unit (of which
+// a causal prompt leaves half empty), of at least 512 rows: two prompts 1.19 ms, with half as many 1.22.
 static ManyShape many_config(const PShape &s, const PWindow &w, int n_layers, int max_rows) {
   ManyShape a{};
   a.w = w;
   const int64_t R = many_rows(s.q4 != 0), keys = many_keys(s.q4 != 0), blocks = ((int64_t)max_rows + keys - 1) / keys, units = (int64_t)n_layers * s.units_per_layer;
   const int64_t rows = std::min<int64_t>(w.max_count, (int64_t)w.window + keys) * s.G;
   a.stride = blocks * keys;
-  const int64_t chunk = std::max<int64_t>(std::max<int64_t>(1024, rows * blocks / 8192 * units), rows * units >> 20);
+  const int64_t chunk = std::max<int64_t>(std::max<int64_t>(512, rows * blocks / 8192 * units), rows * units >> 20);
   a.chunk = (int)((std::min(chunk, rows) + R - 1) / R * R);
-  a.nchunks = (int)((rows + a.chunk - 1) / a.chunk);
+  const int64_t all = w.first > 0 ? (int64_t)w.max_count * s.G : rows;
+  a.nchunks = (int)std::max<int64_t>((rows + a.chunk - 1) / a.chunk, std::min<int64_t>((all + 2 * a.chunk - 1) / (2 * a.chunk), 256));
   a.blocks = (int)std::min<int64_t>(blocks, 65535);
   return a;
 }
@@ -563,8 +583,8 @@ static size_t many_bytes(const PShape &s, const ManyShape &a, int n_layers) {
 
 // Tiles of a workgroup: as many workgroups as four to a compute unit take, a tile to a wave at least; a launch has at most 65535 along a head, and fewer than
 // 2^32 threads.
-static int step_tiles(const PShape &s, int nl, int max_rows) {
-  const int64_t tiles = ((int64_t)max_rows + 31) / 32, units = (int64_t)s.units_per_layer * nl;
+static int step_tiles(const PShape &s, int nl, int64_t tiles) {
+  const int64_t units = (int64_t)s.units_per_layer * nl;
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 23) / units));
   const int64_t ct = std::max<int64_t>(std::max<int64_t>(4, std::min<int64_t>((tiles * units + 1023) / 1024, 16)), (tiles + most - 1) / most);
   return (int)((std::min(ct, tiles) + 3) / 4 * 4);
@@ -635,12 +655,14 @@ extern "C" mixkv_status mixkv_paged_weights(const mixkv_paged_params *params, co
       if (hipGetLastError() != hipSuccess) return MIXKV_ERR_HIP;
       continue;
     }
-    const int ctiles = step_tiles(s, nl, max_rows);
-    const dim3 grid((unsigned)s.units_per_layer, (unsigned)(((int64_t)max_rows + 32 * ctiles - 1) / (32 * ctiles)), (unsigned)nl);
+    const int64_t tiles = most_tiles(s, w, max_rows, (int)std::min<int64_t>((int64_t)w.max_count * s.G, INT32_MAX / 2));
+    const int ctiles = step_tiles(s, nl, tiles);
+    const dim3 grid((unsigned)s.units_per_layer, (unsigned)((tiles + ctiles - 1) / ctiles), (unsigned)nl);
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, stream, s, w, t, p, ctiles); };
     if (s.q4) { if (s.D == 128) go(weights_step_kernel<MIXKV_BF16, 128, true>); else go(weights_step_kernel<MIXKV_BF16, 64, true>); }
     else if (params->dtype == MIXKV_BF16) { if (s.D == 128) go(weights_step_kernel<MIXKV_BF16, 128, false>); else go(weights_step_kernel<MIXKV_BF16, 64, false>); }
-    else { if (s.D == 128) go(weights_step_kernel<MIXKV_F32, 128, false>); else go(weights_step_kernel<MIXKV_F32, 64, false>); }
+    else if ((int64_t)w.max_count * s.G <= 16) { if (s.D == 128) go(weights_step_kernel<MIXKV_F32, 128, false>); else go(weights_step_kernel<MIXKV_F32, 64, false>); }
+    else { if (s.D == 128) go(weights_step_kernel<MIXKV_F32, 128, false, true>); else go(weights_step_kernel<MIXKV_F32, 64, false, true>); }
     if (hipGetLastError() != hipSuccess) return MIXKV_ERR_HIP;
   }
   return MIXKV_OK;
