@@ -273,7 +273,11 @@ __global__ __launch_bounds__(256, kQ4Waves) void paged_q4_kernel(PShape s, AShap
       lo[pl] = sum - hi[pl];
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) qs[e] = (_Float16)(e / 2 < NG ? (quad == 0 ? hi[e / 2 % NG] : (quad == 1 ? lo[e / 2 % NG] : 0.f)) : 0.f);
+    for (int e = 0; e < 8; ++e) {
+      const int pl = e / 2 % NG;
+      const float rest = WIN ? lo[pl] - (float)(_Float16)lo[pl] : 0.f;         // (a third part, for the log-sum-exp: two leave logits off by 2^-22 of the bases' share)
+      qs[e] = (_Float16)(e / 2 < NG ? (quad == 0 ? hi[pl] : quad == 1 ? lo[pl] : quad == 2 ? rest : 0.f) : 0.f);
+    }
   }
   uint32_t one_f16;                                            // an and-or takes one scalar constant: the other one is kept in a register
   asm("v_mov_b32 %0, 0x3c003c00" : "=v"(one_f16));
