@@ -225,7 +225,8 @@ __global__ __launch_bounds__(256) void weights_step_kernel(PShape s, PWindow win
 // A block's products stand beside the weights of the one before, two exponentials to a product, and a turn's last weights behind the barrier, while the next turn's operands come.
 // Addresses of rows: a lane computes one row's, the lanes that load it ask for it; three 64-bit products a load took as long as a tenth of the turn.
 // Bound: the vector unit: an exponential, a multiply-add and an addition are 16 to 20 cycles of a SIMD for 64 weights, its product 16, and they share the issue.  Prompts of 16 384 and
-// 8731 rows, window 8192, 28 query heads on 4: 3.9e9 weights in 1.19 ms, 0.84 PFLOP/s (a large library product 1.22).  Turns of 64 rows: 1.41 ms.
+// 8731 rows, window 8192, 28 query heads on 4: 3.9e9 weights in 1.18 ms, 0.84 PFLOP/s (a large library product 1.22).  Turns of 64 rows: 1.41 ms.  A turn takes 4.8 us, a workgroup's
+// beginning and end 10: the compiler waits for the next turn's rows behind the first products of a turn, and forms without that wait had no registers left for the loop (1.26 to 1.31 ms).
 // ------------------------------------------------------------------------------------------------
 constexpr int kManyWaves = 8, kManyRun = 16384;                     // rows whose weights a lane adds up on its own, every 32nd: they are off by 2^-15 at most
 constexpr int many_rows(bool q4) { return q4 ? 64 : 128; }          // rows of a turn
@@ -482,11 +483,17 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void weights_many_kernel(PShape
             if (i + R < i1) settle(to ^ 1);
             i += R;
             to ^= 1;
-            if (i < ib) begin();
+            if (i < ib) {
+              begin();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) weigh(N - 1, e, o, c);
-            if (i < ib) look(i);
-          } while (i < ib && all);
+              for (int e = 0; e < 16; ++e) weigh(N - 1, e, o, c);
+              look(i);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) weigh(N - 1, e, o, c);
+              break;                                         // (a path without the wait that leads back here would make the compiler wait for the rows under way)
+            }
+          } while (all);
         } else {
 #pragma unroll
           for (int y = 0; y < NY; ++y) {
