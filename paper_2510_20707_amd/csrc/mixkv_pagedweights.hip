@@ -235,7 +235,8 @@ constexpr int many_keys(bool q4) { return 32 * kManyWaves * (q4 ? 1 : 2); }    /
 struct ManyShape {
   PWindow w;
   int32_t chunk, nchunks;                // rows that a block's chunk should have, the most chunks of a block
-  int32_t blocks;                        // blocks of keys of a unit in the launch; longer heads' are walked
+  int32_t block0, end;                   // the launch's blocks of keys of a unit: from block0 on, in front of `end`
+  int32_t blocks;                        // those of them that have workgroups; longer heads' are walked
   int64_t stride;                        // keys of a unit among the partial sums
 };
 
@@ -274,7 +275,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void weights_many_kernel(PShape
   const int G = s.G, step_t = R / G, step_g = R - step_t * G;
   const int64_t qsn = l.qsn, qsh = l.qsh;
   const char *const Q = l.Q + (int64_t)h * G * qsh;
-  for (int block = blockIdx.y; (int64_t)block * KEYS < len; block += a.blocks) {
+  for (int block = a.block0 + blockIdx.y; block < a.end && (int64_t)block * KEYS < len; block += a.blocks) {
     const int kA = block * KEYS, kB = min(kA + KEYS, len);
     const Rows rows = rows_that_see(s, a.w, len, count, kA, kB);
     const bool direct = a.nchunks == 1 || kA >= a.stride;    // (keys that the host did not know of: all their rows in one go)
@@ -551,7 +552,7 @@ __global__ __launch_bounds__(256) void weights_fold_kernel(PShape s, ManyShape a
   const PCache c = tab.c[layer];
   const WinLayer l = tab.l[layer];
   const int len = head_rows(s, c, u), count = max(l.count[u], 0);
-  for (int j = blockIdx.y * 256 + threadIdx.x; j < len && j < a.stride; j += gridDim.y * 256) {
+  for (int j = a.block0 * keys + blockIdx.y * 256 + threadIdx.x; j < len && j < a.stride; j += gridDim.y * 256) {
     const int id = page_at(s, c, u, j >> s.lp);
     if (id < 0) continue;
     const int kA = j / keys * keys;
@@ -569,24 +570,36 @@ __global__ __launch_bounds__(256) void weights_fold_kernel(PShape s, ManyShape a
   }
 }
 
-// Chunks of the rows that see a block of keys (those of the first keys, which every row sees, are up to twice as long): enough for thirty-two workgroups to a compute unit (of which
-// a causal prompt leaves half empty), of at least 512 rows: two prompts 1.19 ms, with half as many 1.22.
-static ManyShape many_config(const PShape &s, const PWindow &w, int n_layers, int max_rows) {
+// Chunks of the rows that see a block of keys: enough for thirty-two workgroups to a compute unit (of which a causal prompt leaves half empty), of at least 512 rows: two prompts 1.18 ms, with
+// half as many 1.22.  Blocks of first keys, which every row sees, are a launch of their own where the other blocks' chunks would be more than twice as long with their rows (two prompts of up to
+// 2970 rows in a window of 19, one first row: 64 us, in the other blocks' two chunks 335).  Returns the number of launches.
+static int many_config(const PShape &s, const PWindow &w, int n_layers, int max_rows, ManyShape (&out)[2]) {
   ManyShape a{};
   a.w = w;
   const int64_t R = many_rows(s.q4 != 0), keys = many_keys(s.q4 != 0), blocks = ((int64_t)max_rows + keys - 1) / keys, units = (int64_t)n_layers * s.units_per_layer;
-  const int64_t rows = std::min<int64_t>(w.max_count, (int64_t)w.window + keys) * s.G;
+  const int64_t firsts = std::min(blocks, (w.first + keys - 1) / keys), all = (int64_t)w.max_count * s.G;
+  const int64_t rows = firsts == blocks ? all : std::min<int64_t>(w.max_count, (int64_t)w.window + keys) * s.G;
   a.stride = blocks * keys;
   const int64_t chunk = std::max<int64_t>(std::max<int64_t>(512, rows * blocks / 8192 * units), rows * units >> 20);
   a.chunk = (int)((std::min(chunk, rows) + R - 1) / R * R);
-  const int64_t all = w.first > 0 ? (int64_t)w.max_count * s.G : rows;
-  a.nchunks = (int)std::max<int64_t>((rows + a.chunk - 1) / a.chunk, std::min<int64_t>((all + 2 * a.chunk - 1) / (2 * a.chunk), 256));
+  a.nchunks = (int)((rows + a.chunk - 1) / a.chunk);
+  a.end = INT32_MAX;
   a.blocks = (int)std::min<int64_t>(blocks, 65535);
-  return a;
+  out[0] = a;
+  if (firsts == 0 || firsts == blocks || (all + 2 * a.chunk - 1) / (2 * a.chunk) <= a.nchunks) return 1;
+  out[0].block0 = (int)firsts;
+  out[0].blocks = (int)std::min<int64_t>(blocks - firsts, 65535);
+  a.nchunks = (int)std::min<int64_t>((all + a.chunk - 1) / a.chunk, 256);
+  a.end = (int)firsts;
+  a.blocks = (int)std::min<int64_t>(firsts, 65535);
+  a.stride = firsts * keys;
+  out[1] = a;
+  return 2;
 }
 static size_t many_bytes(const PShape &s, const ManyShape &a, int n_layers) {
   return a.nchunks == 1 ? 0 : (size_t)n_layers * s.units_per_layer * a.nchunks * a.stride * sizeof(float);
 }
+static size_t many_bytes(const PShape &s, const ManyShape (&a)[2], int n, int n_layers) { return many_bytes(s, a[0], n_layers) + (n > 1 ? many_bytes(s, a[1], n_layers) : 0); }
 
 // Tiles of a workgroup: as many workgroups as four to a compute unit take, a tile to a wave at least; a launch has at most 65535 along a head, and fewer than
 // 2^32 threads.
@@ -609,7 +622,12 @@ extern "C" mixkv_status mixkv_paged_weights_workspace_size(const mixkv_paged_par
   if ((st = make_window(s, n_rows, window, keep_first, max_count, max_rows, &w)) != MIXKV_OK) return st;
   if (!bytes || n_layers < 1 || n_layers > MIXKV_MAX_LAYERS) return MIXKV_ERR_INVALID_ARG;
   max_rows = std::min(max_rows, s.max_pages * s.P);
-  *bytes = many_rows(s, params->dtype, w) ? (many_bytes(s, many_config(s, w, n_layers, max_rows), n_layers) + 255) / 256 * 256 : 0;
+  *bytes = 0;
+  if (many_rows(s, params->dtype, w)) {
+    ManyShape a[2];
+    const int n = many_config(s, w, n_layers, max_rows, a);
+    *bytes = (many_bytes(s, a, n, n_layers) + 255) / 256 * 256;
+  }
   return MIXKV_OK;
 }
 
@@ -631,18 +649,21 @@ extern "C" mixkv_status mixkv_paged_weights(const mixkv_paged_params *params, co
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   max_rows = std::min(max_rows, s.max_pages * s.P);
   const bool many = many_rows(s, params->dtype, w);
-  ManyShape a{};
-  if (many) a = many_config(s, w, n_layers, max_rows);
-  const size_t need = many ? many_bytes(s, a, n_layers) : 0;
+  ManyShape many_shapes[2] = {};
+  const int launches = many ? many_config(s, w, n_layers, max_rows, many_shapes) : 0;
+  const size_t need = many ? many_bytes(s, many_shapes, launches, n_layers) : 0;
   if (need > 0) {
     if (!workspace || misaligned(workspace, 256)) return MIXKV_ERR_INVALID_ARG;
     if (workspace_bytes < need) return MIXKV_ERR_WORKSPACE_TOO_SMALL;
   }
-  float *part = static_cast<float *>(workspace);
   // many rows: a launch has fewer than 2^32 threads
-  const int64_t fit = std::max<int64_t>(1, ((int64_t)1 << 22) / ((int64_t)s.units_per_layer * a.nchunks + 1));
-  if (many) a.blocks = (int)std::min<int64_t>(a.blocks, fit);
-  const int per = many ? (int)std::min<int64_t>(kLayersPerLaunch, std::max<int64_t>(1, fit / a.blocks)) : kLayersPerLaunch;
+  int per = kLayersPerLaunch;
+  for (int i = 0; i < launches; ++i) {
+    ManyShape &a = many_shapes[i];
+    const int64_t fit = std::max<int64_t>(1, ((int64_t)1 << 22) / ((int64_t)s.units_per_layer * a.nchunks + 1));
+    a.blocks = (int)std::min<int64_t>(a.blocks, fit);
+    per = (int)std::min<int64_t>(per, std::max<int64_t>(1, fit / a.blocks));
+  }
   for (int l0 = 0; l0 < n_layers; l0 += per) {
     const int nl = std::min(n_layers - l0, per);
     const int64_t unit0 = (int64_t)l0 * s.units_per_layer;
@@ -650,14 +671,19 @@ extern "C" mixkv_status mixkv_paged_weights(const mixkv_paged_params *params, co
     WeightPtrs p{};
     for (int l = 0; l < nl; ++l) p.w[l] = weights[l0 + l];
     if (many) {
-      const dim3 grid((unsigned)(s.units_per_layer * a.nchunks), (unsigned)a.blocks, (unsigned)nl);
-      auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(64 * kManyWaves), 0, stream, s, a, t, p, part, unit0); };
-      if (s.q4) { if (s.D == 128) go(weights_many_kernel<128, true>); else go(weights_many_kernel<64, true>); }
-      else { if (s.D == 128) go(weights_many_kernel<128, false>); else go(weights_many_kernel<64, false>); }
-      if (a.nchunks > 1) {
-        const int64_t y = std::min<int64_t>((a.stride + 255) / 256, std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 23) / ((int64_t)s.units_per_layer * nl))));
-        hipLaunchKernelGGL(weights_fold_kernel, dim3((unsigned)s.units_per_layer, (unsigned)y, (unsigned)nl), dim3(256), 0, stream, s, a, t, p, (const float *)part, unit0,
-                           many_keys(s.q4 != 0), many_rows(s.q4 != 0));
+      float *part = static_cast<float *>(workspace);
+      for (int i = 0; i < launches; ++i) {
+        const ManyShape &a = many_shapes[i];
+        const dim3 grid((unsigned)(s.units_per_layer * a.nchunks), (unsigned)a.blocks, (unsigned)nl);
+        auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(64 * kManyWaves), 0, stream, s, a, t, p, part, unit0); };
+        if (s.q4) { if (s.D == 128) go(weights_many_kernel<128, true>); else go(weights_many_kernel<64, true>); }
+        else { if (s.D == 128) go(weights_many_kernel<128, false>); else go(weights_many_kernel<64, false>); }
+        if (a.nchunks > 1) {
+          const int64_t y = std::min<int64_t>((a.stride + 255) / 256, std::max<int64_t>(1, std::min<int64_t>(65535, ((int64_t)1 << 23) / ((int64_t)s.units_per_layer * nl))));
+          hipLaunchKernelGGL(weights_fold_kernel, dim3((unsigned)s.units_per_layer, (unsigned)y, (unsigned)nl), dim3(256), 0, stream, s, a, t, p, (const float *)part, unit0,
+                             many_keys(s.q4 != 0), many_rows(s.q4 != 0));
+        }
+        part += many_bytes(s, a, n_layers) / sizeof(float);
       }
       if (hipGetLastError() != hipSuccess) return MIXKV_ERR_HIP;
       continue;

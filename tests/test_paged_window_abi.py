@@ -92,6 +92,9 @@ def test_workspaces():
     assert B.mixkv_paged_window_attention_workspace_size(_params(), 1, 100, 64, 0, 1, 1 << 30) == 0        # a short window: whole
     p = _params(dtype="f32", format="rows", max_pages=4000)
     assert B.mixkv_paged_window_attention_workspace_size(p, 1, 16384, 1 << 30, 0, 16384, 16384) == 0        # fp32 prompts: groups enough, no partial sums
+    for layers in (1, 32):                                                             # first rows, which every row sees, do not make the sums of all keys longer
+        few, more = (B.mixkv_paged_weights_workspace_size(_params(max_pages=2048), layers, 131072, 1024, first, 131072, 131072) for first in (0, 16))
+        assert few <= more <= few + layers * 2 * 4 * 256 * 512 * 4
     for size in (B.lib().mixkv_paged_window_attention_workspace_size, B.lib().mixkv_paged_weights_workspace_size):
         assert size(C.byref(_params()), 1, 10, 5, 0, 1, 100, None) == INVALID and size(C.byref(_params()), 0, 10, 5, 0, 1, 100, C.byref(C.c_size_t())) == INVALID
     assert B.lib().mixkv_paged_evict_workspace_size(C.byref(_params()), 1, 0, C.byref(C.c_size_t())) == INVALID
