@@ -225,7 +225,7 @@ __global__ __launch_bounds__(THREADS) void evict_rank_kernel(PShape s, EvictShap
 constexpr int kSegRows = 8192, kMostSegs = 32, kCopies = 4;   // kCopies: of a workgroup's counts, because keys of one head often agree in their leading bits
 struct LongPlan {
   uint32_t *keys;                          // [head][stride]
-  int *counts;                             // [head][level][segs][kLongBins]
+  int *counts;                             // [head][2][segs][kLongBins]: the first and the third level, the second
   int4 *states;                            // [head][segs]: the last kept key's bits so far, keys to keep of those that have them, keys above them in earlier segments, keys to keep
   int64_t stride;
   int32_t segs, seg;                       // seg: rows of a segment
@@ -286,7 +286,7 @@ __global__ __launch_bounds__(kRankThreads) void evict_count_kernel(PShape s, Evi
   const int64_t head = layer * (int64_t)s.units_per_layer + u, r0 = (int64_t)seg * p.seg, r1 = min(r0 + p.seg, (int64_t)len);
   if (len > p.stride || (seg > 0 && r0 >= len)) return;       // (an empty head: the first segment counts nothing)
   uint32_t *keys = p.keys + head * p.stride;
-  int *counts = p.counts + head * 3 * p.segs * kLongBins;
+  int *counts = p.counts + head * 2 * p.segs * kLongBins;
   const int n_seg = max(1, (int)(((int64_t)len + p.seg - 1) / p.seg));
   for (int i = tid; i < kLongBins * kCopies; i += kRankThreads) hist[i] = 0;
   uint32_t prefix = 0;
@@ -334,7 +334,7 @@ __global__ __launch_bounds__(kRankThreads) void evict_count_kernel(PShape s, Evi
     int n = 0;
 #pragma unroll
     for (int k = 0; k < kCopies; ++k) n += hist[b * kCopies + k];
-    counts[(LEVEL * p.segs + seg) * kLongBins + b] = n;
+    counts[((LEVEL & 1) * p.segs + seg) * kLongBins + b] = n;      // (the last level takes the first one's place, which nobody reads any more)
   }
 }
 
@@ -356,7 +356,7 @@ __global__ __launch_bounds__(kRankThreads) void evict_list_kernel(PShape s, Evic
   if (seg == 0) kept_rows(ev, l, u, st.w, st.w, kept, kRankThreads);
   if (st.w == 0) return;                                      // uniform
   const int n_seg = (int)(((int64_t)len + p.seg - 1) / p.seg);
-  const Fold f = fold_counts(p.counts + (head * 3 + 2) * p.segs * kLongBins, n_seg, seg, sc.fold, [&](int) { return st.y; });
+  const Fold f = fold_counts(p.counts + head * 2 * p.segs * kLongBins, n_seg, seg, sc.fold, [&](int) { return st.y; });
   const uint32_t last = (uint32_t)st.x | (uint32_t)f.bin;     // the last kept key; the first `need` that are it stay
   const int need = st.y - f.above, keep = st.w;
   int above = st.z + f.above_before, ties = f.in_before;      // in front of the turn's rows
@@ -639,7 +639,7 @@ static size_t evict_plan(const PShape &s, int n_layers, int max_rows, void *work
   p->stride = (rows + 3) / 4 * 4;
   p->seg = (int32_t)(((rows + most - 1) / most + kSegRows - 1) / kSegRows * kSegRows);
   p->segs = (int32_t)((rows + p->seg - 1) / p->seg);
-  const size_t states = (size_t)heads * p->segs * sizeof(int4), counts = (size_t)heads * 3 * p->segs * kLongBins * sizeof(int);
+  const size_t states = (size_t)heads * p->segs * sizeof(int4), counts = (size_t)heads * 2 * p->segs * kLongBins * sizeof(int);
   p->states = static_cast<int4 *>(workspace);
   if (workspace) {
     p->counts = reinterpret_cast<int *>(static_cast<char *>(workspace) + states);
