@@ -12,9 +12,10 @@ constexpr int kSumRun = 64;              // steps of 16 rows whose weights are s
 
 // ------------------------------------------------------------------------------------------------
 // weights_step_kernel (few rows): a wave to tiles of 32 keys, rows on the output rows of 16 x 16 products, keys on their columns, so that a lane has
-// two keys and their sums over four rows each.  With up to 16 rows in all (a step's single tokens) the queries are prepared once.
+// two keys and their sums over four rows each.  With up to 16 rows in all (a step's single tokens) every wave prepares the queries once, with up to 64 the workgroup does.
 // 4-bit keys as in paged_q4_kernel: codes as fp16 subnormals, a product for each group of 32 elements, steps and bases behind it in fp32.
 // Bound: memory, a tile of each wave in flight, the next one asked for before the exponentials: 32 sequences of up to 16 384 rows, 32 query heads on 8, 570 MB in 120 us, 4.7 TB/s.
+// Five new rows of 16 sequences of 8192 rows: 4 bits 36 us, bf16 49; with the queries prepared anew for every tile 72 and 69.
 // Workgroups of 16 tiles: heads of unequal length then end together (121 us; 64 tiles 133, 128 156, 4 144).  Loads past the caches: 124.
 // ------------------------------------------------------------------------------------------------
 template <int DT, int D, bool Q4, bool AHEAD = false>
@@ -36,6 +37,11 @@ __global__ __launch_bounds__(256) void weights_step_kernel(PShape s, PWindow win
   const int t0 = blockIdx.y * ctiles, t1 = blockIdx.y + 1 == gridDim.y ? tiles : min(tiles, t0 + ctiles);
   if (t0 >= t1) return;
 
+  // Up to 64 rows that are not fp32 are prepared once, a wave 16 of them, and lie in LDS for all of the workgroup's tiles.
+  constexpr bool KEPT = !F32;
+  static_assert(kFewRows <= 16 * W, "a wave to 16 rows");
+  constexpr int NV = (Q4 ? NG + 2 : NC) + 2;               // 16-byte words of a lane: queries; (4 bits) factors and sums; normalisers, places
+  __shared__ u32x4 kept_s[4][NV][64];
   // ---- 16 rows: their queries, and of the rows 4 quad + e the normalisers and places.  AHEAD (fp32 of many rows): the next ones are asked for while one is worked on.
   constexpr int NQ = Q4 ? NG : NC;
   u32x4 qf[NQ], qn[NQ];
@@ -102,10 +108,45 @@ __global__ __launch_bounds__(256) void weights_step_kernel(PShape s, PWindow win
     }
   };
   const bool once = (int64_t)served * s.G <= 16;
+  auto keep_rows = [&](int step) {
+    u32x4(&to)[NV][64] = kept_s[step];
+#pragma unroll
+    for (int k = 0; k < NQ; ++k) to[k][lane] = qf[k];
+    if constexpr (Q4) {
+      to[NQ][lane] = u32x4{__float_as_uint(c2[0]), __float_as_uint(c2[1]), __float_as_uint(c2[2]), __float_as_uint(c2[3])};
+      to[NQ + 1][lane] = __builtin_bit_cast(u32x4, qs);
+    }
+    to[NV - 2][lane] = u32x4{__float_as_uint(off[0]), __float_as_uint(off[1]), __float_as_uint(off[2]), __float_as_uint(off[3])};
+    to[NV - 1][lane] = u32x4{(uint32_t)place[0], (uint32_t)place[1], (uint32_t)place[2], (uint32_t)place[3]};
+  };
+  auto kept_rows = [&](int step) {
+    const u32x4(&from)[NV][64] = kept_s[step];
+#pragma unroll
+    for (int k = 0; k < NQ; ++k) qf[k] = from[k][lane];
+    const u32x4 o = from[NV - 2][lane], p = from[NV - 1][lane];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      off[e] = __uint_as_float(o[e]);
+      place[e] = (int)p[e];
+      if constexpr (Q4) c2[e] = __uint_as_float(from[NQ][lane][e]);
+    }
+    if constexpr (Q4) qs = __builtin_bit_cast(f16x8, (u32x4)from[NQ + 1][lane]);
+  };
   if (once && served > 0) {
     begin_rows(0);
     ask_rows(0, served * s.G);
     take_rows();
+  }
+  if constexpr (KEPT) {
+    if (!once) {                                             // uniform
+      if (wave * 16 < served * s.G) {
+        begin_rows(wave * 16);
+        ask_rows(wave * 16, served * s.G);
+        take_rows();
+        keep_rows(wave);
+      }
+      __syncthreads();
+    }
   }
 
   for (int first = t0 + wave; first < t1; first += 64 * W) {
@@ -147,15 +188,18 @@ __global__ __launch_bounds__(256) void weights_step_kernel(PShape s, PWindow win
       float sum[2] = {0.f, 0.f}, run[2] = {0.f, 0.f};
       int steps = 0;
       const int i1 = work ? (once ? served : hi) * s.G : 0;
-      if (work && !once) {
+      if (!KEPT && work && !once) {
         begin_rows(lo * s.G);
         if constexpr (AHEAD) ask_rows(lo * s.G, i1);
       }
-      for (int i0 = once ? 0 : lo * s.G; i0 < i1; i0 += 16) {
+      for (int i0 = once ? 0 : KEPT ? lo * s.G & ~15 : lo * s.G; i0 < i1; i0 += 16) {
         if (!once) {
-          if constexpr (!AHEAD) ask_rows(i0, i1);
-          take_rows();
-          if (AHEAD && i0 + 16 < i1) ask_rows(i0 + 16, i1);
+          if constexpr (KEPT) kept_rows(i0 >> 4);
+          else {
+            if constexpr (!AHEAD) ask_rows(i0, i1);
+            take_rows();
+            if (AHEAD && i0 + 16 < i1) ask_rows(i0 + 16, i1);
+          }
         }
         f32x4 xs[2];
 #pragma unroll
@@ -570,8 +614,8 @@ __global__ __launch_bounds__(256) void weights_fold_kernel(PShape s, ManyShape a
   }
 }
 
-// Chunks of the rows that see a block of keys: enough for thirty-two workgroups to a compute unit (of which a causal prompt leaves half empty), of at least 512 rows: two prompts 1.18 ms, with
-// half as many 1.22.  Blocks of first keys, which every row sees, are a launch of their own where the other blocks' chunks would be more than twice as long with their rows (two prompts of up to
+// Chunks of the rows that see a block of keys: sixteen turns, fewer (of at least 512 rows) where that makes less than four workgroups to a compute unit, more where it makes over thirty-two (of
+// which a causal prompt leaves half empty).  Two prompts, window 8192: 15 turns 1.18 ms, 28 turns 1.22.  Blocks of first keys, which every row sees, are a launch of their own where the other blocks' chunks would be more than twice as long with their rows (two prompts of up to
 // 2970 rows in a window of 19, one first row: 64 us, in the other blocks' two chunks 335).  Returns the number of launches.
 static int many_config(const PShape &s, const PWindow &w, int n_layers, int max_rows, ManyShape (&out)[2]) {
   ManyShape a{};
@@ -580,7 +624,7 @@ static int many_config(const PShape &s, const PWindow &w, int n_layers, int max_
   const int64_t firsts = std::min(blocks, (w.first + keys - 1) / keys), all = (int64_t)w.max_count * s.G;
   const int64_t rows = firsts == blocks ? all : std::min<int64_t>(w.max_count, (int64_t)w.window + keys) * s.G;
   a.stride = blocks * keys;
-  const int64_t chunk = std::max<int64_t>(std::max<int64_t>(512, rows * blocks / 8192 * units), rows * units >> 20);
+  const int64_t work = rows * blocks * units, chunk = std::max<int64_t>(std::max<int64_t>(std::min<int64_t>(std::max<int64_t>(work / 1024, 512), 16 * R), work / 8192), rows * units >> 20);
   a.chunk = (int)((std::min(chunk, rows) + R - 1) / R * R);
   a.nchunks = (int)((rows + a.chunk - 1) / a.chunk);
   a.end = INT32_MAX;
