@@ -616,7 +616,8 @@ __global__ __launch_bounds__(256) void weights_fold_kernel(PShape s, ManyShape a
 
 // Chunks of the rows that see a block of keys: sixteen turns, fewer (of at least 512 rows) where that makes less than four workgroups to a compute unit, more where it makes over thirty-two (of
 // which a causal prompt leaves half empty).  Two prompts, window 8192: 15 turns 1.18 ms, 28 turns 1.22.  Blocks of first keys, which every row sees, are a launch of their own where the other blocks' chunks would be more than twice as long with their rows (two prompts of up to
-// 2970 rows in a window of 19, one first row: 64 us, in the other blocks' two chunks 335).  Returns the number of launches.
+// 2970 rows in a window of 19, one first row: 64 us, in the other blocks' two chunks 335).  That launch has at most 256 chunks a block and 2^16 workgroups in all, layers together: a compute
+// unit's 256 fill it whatever their lengths, and the sums of its chunks stay below 128 MiB, where many short sequences stand beside one long prompt.  Returns the number of launches.
 static int many_config(const PShape &s, const PWindow &w, int n_layers, int max_rows, ManyShape (&out)[2]) {
   ManyShape a{};
   a.w = w;
@@ -624,16 +625,18 @@ static int many_config(const PShape &s, const PWindow &w, int n_layers, int max_
   const int64_t firsts = std::min(blocks, (w.first + keys - 1) / keys), all = (int64_t)w.max_count * s.G;
   const int64_t rows = firsts == blocks ? all : std::min<int64_t>(w.max_count, (int64_t)w.window + keys) * s.G;
   a.stride = blocks * keys;
-  const int64_t work = rows * blocks * units, chunk = std::max<int64_t>(std::max<int64_t>(std::min<int64_t>(std::max<int64_t>(work / 1024, 512), 16 * R), work / 8192), rows * units >> 20);
+  const int64_t work = rows * std::min<int64_t>(blocks * units, 8192), chunk = std::max<int64_t>(std::max<int64_t>(std::min<int64_t>(std::max<int64_t>(work / 1024, 512), 16 * R), work / 8192), rows * units >> 20);
   a.chunk = (int)((std::min(chunk, rows) + R - 1) / R * R);
   a.nchunks = (int)((rows + a.chunk - 1) / a.chunk);
   a.end = INT32_MAX;
   a.blocks = (int)std::min<int64_t>(blocks, 65535);
   out[0] = a;
-  if (firsts == 0 || firsts == blocks || (all + 2 * a.chunk - 1) / (2 * a.chunk) <= a.nchunks) return 1;
+  if (firsts == 0 || firsts == blocks || (all + 2 * (int64_t)a.chunk - 1) / (2 * (int64_t)a.chunk) <= a.nchunks) return 1;
+  const int first_chunks = (int)std::min<int64_t>((all + a.chunk - 1) / a.chunk, std::min<int64_t>(256, 65536 / (units * firsts)));
+  if (first_chunks <= a.nchunks) return 1;
   out[0].block0 = (int)firsts;
   out[0].blocks = (int)std::min<int64_t>(blocks - firsts, 65535);
-  a.nchunks = (int)std::min<int64_t>((all + a.chunk - 1) / a.chunk, 256);
+  a.nchunks = first_chunks;
   a.end = (int)firsts;
   a.blocks = (int)std::min<int64_t>(firsts, 65535);
   a.stride = firsts * keys;

@@ -1,0 +1,40 @@
+"""Launches and workspaces of the calls on new rows at the ends of what they accept (no GPU; tests/launches.py): a launch has fewer than 2^32 threads and at most 65535 workgroups along y and z."""
+import itertools
+import math
+
+import pytest
+
+from tests import launches
+
+# (batch, query heads, KV heads): one sequence, and the most that a call takes, in heads and in sequences
+SHAPES = [(1, 28, 4), (64, 32, 8), (4096, 8, 8), (512, 512, 8), (1, 1 << 18, 1 << 18), (1 << 18, 1, 1)]
+KINDS = [("rows", "bf16"), ("4bit", "bf16"), ("rows", "f32")]
+
+
+def _params(shape, kind):
+    batch, hq, hkv = shape
+    return dict(format=kind[0], dtype=kind[1], batch=batch, n_q_heads=hq, n_kv_heads=hkv, page_rows=64, max_pages=1 << 24, n_pages=40)
+
+
+def _check(calls, tmp_path, most_bytes=None):
+    made = 0
+    for call, (status, need, launched) in zip(calls, launches.record(calls, tmp_path)):
+        assert status == 0 and launched, call
+        assert most_bytes is None or need <= most_bytes, (need, call)
+        for name, grid, block in launched:
+            assert min(grid) > 0 and max(grid[1:]) <= 65535 and math.prod(grid) * math.prod(block) < 1 << 32, (name, grid, block, call)
+        made += len(launched)
+    assert made >= len(calls)
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+def test_weights(shape, tmp_path):
+    """One long prompt among many short sequences, windows short and long, first rows that every row sees: the sums of chunks are those of at most 16384 blocks of 512 keys, and of
+    65536 blocks of first keys."""
+    calls = []
+    for kind, layers, rows, count in itertools.product(KINDS, (1, 24, 128), (1000, 163840, 1 << 30), (1, 1000, 163840)):
+        if (kind[1] == "f32" and count > 1000) or count * shape[1] >= 1 << 31:
+            continue
+        calls += [("weigh", _params(shape, kind), dict(n=layers, rows=count, window=window, first=first, count=count, most=rows))
+                  for window, first in ((1 << 30, 0), (64, 16), (64, 100000), (1, 1 << 30))]
+    _check(calls, tmp_path, (16384 + 65536) * 512 * 4)
