@@ -630,9 +630,11 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(PShape s, Evic
 
 // Heads that a workgroup holds in registers, as long as the host says; longer ones have keys and counts in the workspace.
 constexpr int kRankRows = 16384;
+// Layers of a launch: at a thousand threads a head, fewer than 2^32.
+static int evict_layers(const PShape &s, int n_layers) { return std::min(std::min(n_layers, kEvictLayers), ((1 << 22) - 1) / s.units_per_layer); }
 static int64_t most_rows(const PShape &s, int max_rows) { return std::min<int64_t>(max_rows, (int64_t)s.max_pages * s.P); }
 static size_t evict_plan(const PShape &s, int n_layers, int max_rows, void *workspace, LongPlan *p) {
-  const int64_t rows = most_rows(s, max_rows), heads = (int64_t)std::min(n_layers, kEvictLayers) * s.units_per_layer;
+  const int64_t rows = most_rows(s, max_rows), heads = (int64_t)evict_layers(s, n_layers) * s.units_per_layer;
   *p = LongPlan{};
   if (rows <= kRankRows) return 0;
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(kMostSegs, ((int64_t)1 << 21) / heads));        // fewer than 2^32 threads
@@ -690,8 +692,9 @@ extern "C" mixkv_status mixkv_paged_evict(const mixkv_paged_params *params, cons
   const int64_t rows = most_rows(s, max_rows);
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   const EvictShape ev{max_keep, keep_first, keep_last};
-  for (int l0 = 0; l0 < n_layers; l0 += kEvictLayers) {
-    const int nl = std::min(n_layers - l0, kEvictLayers);
+  const int per = evict_layers(s, n_layers);
+  for (int l0 = 0; l0 < n_layers; l0 += per) {
+    const int nl = std::min(n_layers - l0, per);
     EvictTable t;
     for (int l = 0; l < kEvictLayers; ++l) {
       t.c[l] = PCache{};

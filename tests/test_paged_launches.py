@@ -38,3 +38,20 @@ def test_weights(shape, tmp_path):
         calls += [("weigh", _params(shape, kind), dict(n=layers, rows=count, window=window, first=first, count=count, most=rows))
                   for window, first in ((1 << 30, 0), (64, 16), (64, 100000), (1, 1 << 30))]
     _check(calls, tmp_path, (16384 + 65536) * 512 * 4)
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+def test_eviction(shape, tmp_path):
+    _check([("evict", _params(shape, kind), dict(n=layers, keep=rows, rows=rows))
+            for kind, layers, rows in itertools.product(KINDS, (1, 16, 24, 128), (1, 1000, 4096, 16384, 163840, 1 << 30))], tmp_path)
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+def test_attention(shape, tmp_path):
+    """Few rows of the most heads, many of a few."""
+    calls = []
+    for kind, layers, rows, count in itertools.product(KINDS, (1, 24, 128), (1000, 163840, 1 << 30), (1, 5, 64, 163840)):
+        if count * math.prod(shape[:2]) * layers > 1 << 26 or count * shape[1] >= 1 << 31:
+            continue
+        calls += [("attend", _params(shape, kind), dict(n=layers, rows=count, window=window, first=first, count=count, most=rows)) for window, first in ((1 << 30, 0), (64, 16), (64, 100000))]
+    _check(calls, tmp_path)
