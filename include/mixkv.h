@@ -499,7 +499,7 @@ mixkv_status mixkv_paged_window_attention(const mixkv_paged_params *params, cons
  *     sum over the new rows that see j, and over the G query heads, of exp(softmax_scale * q . k_j - lse),
  * in fp32; the weights of the new rows themselves begin at zero.  A place's weight lies beside its page: weights[l][page][row of the page], 16-byte aligned.  Rows
  * whose lse is -infinity give nothing.  Weights of rows that do not exist, and of old rows that no new row sees, keep their contents.  A head's
- * rows beyond max_count are not served; max_rows as above.  V_pages are not used and may be NULL.  Sums repeat bit for bit for the same
+ * rows beyond max_count are not served; max_rows as above.  n_rows * n_q_heads <= 2^30.  V_pages are not used and may be NULL.  Sums repeat bit for bit for the same
  * arguments.  Workspace: mixkv_paged_weights_workspace_size bytes (0: NULL is accepted), 256-byte aligned, no initialisation.
  */
 mixkv_status mixkv_paged_weights_workspace_size(const mixkv_paged_params *params, int32_t n_layers, int32_t n_rows, int32_t window, int32_t keep_first,

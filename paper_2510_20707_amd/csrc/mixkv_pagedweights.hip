@@ -643,6 +643,12 @@ static int many_config(const PShape &s, const PWindow &w, int n_layers, int max_
   out[1] = a;
   return 2;
 }
+// Rows of a unit are counted in 32 bits; a chunk that a block does not have begins up to a unit's rows behind the block's first one, and a turn ends behind the last.
+static mixkv_status make_weights_window(const PShape &s, int n_rows, int window, int first, int max_count, int max_rows, PWindow *w) {
+  const mixkv_status st = make_window(s, n_rows, window, first, max_count, max_rows, w);
+  return st == MIXKV_OK && (int64_t)n_rows * s.hq > 1 << 30 ? MIXKV_ERR_UNSUPPORTED : st;
+}
+
 static size_t many_bytes(const PShape &s, const ManyShape &a, int n_layers) {
   return a.nchunks == 1 ? 0 : (size_t)n_layers * s.units_per_layer * a.nchunks * a.stride * sizeof(float);
 }
@@ -666,7 +672,7 @@ extern "C" mixkv_status mixkv_paged_weights_workspace_size(const mixkv_paged_par
   PWindow w;
   mixkv_status st = make_pshape(params, &s);
   if (st != MIXKV_OK) return st;
-  if ((st = make_window(s, n_rows, window, keep_first, max_count, max_rows, &w)) != MIXKV_OK) return st;
+  if ((st = make_weights_window(s, n_rows, window, keep_first, max_count, max_rows, &w)) != MIXKV_OK) return st;
   if (!bytes || n_layers < 1 || n_layers > MIXKV_MAX_LAYERS) return MIXKV_ERR_INVALID_ARG;
   max_rows = std::min(max_rows, s.max_pages * s.P);
   *bytes = 0;
@@ -686,7 +692,7 @@ extern "C" mixkv_status mixkv_paged_weights(const mixkv_paged_params *params, co
   PWindow w;
   mixkv_status st = make_pshape(params, &s);
   if (st != MIXKV_OK) return st;
-  if ((st = make_window(s, n_rows, window, keep_first, max_count, max_rows, &w)) != MIXKV_OK) return st;
+  if ((st = make_weights_window(s, n_rows, window, keep_first, max_count, max_rows, &w)) != MIXKV_OK) return st;
   if ((st = check_caches(caches, n_layers, false, false)) != MIXKV_OK) return st;
   const int eb = params->dtype == MIXKV_BF16 ? 2 : 4;
   if ((st = check_queries(s, eb, queries, n_layers, n_rows, false)) != MIXKV_OK) return st;

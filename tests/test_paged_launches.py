@@ -1,10 +1,13 @@
 """Launches and workspaces of the calls on new rows at the ends of what they accept (no GPU; tests/launches.py): a launch has fewer than 2^32 threads and at most 65535 workgroups along y and z."""
+import ctypes as C
 import itertools
 import math
 
 import pytest
 
+from paper_2510_20707_amd import binding as B
 from tests import launches
+from tests import test_paged_window_abi as W
 
 # (batch, query heads, KV heads): one sequence, and the most that a call takes, in heads and in sequences
 SHAPES = [(1, 28, 4), (64, 32, 8), (4096, 8, 8), (512, 512, 8), (1, 1 << 18, 1 << 18), (1 << 18, 1, 1)]
@@ -55,3 +58,13 @@ def test_attention(shape, tmp_path):
             continue
         calls += [("attend", _params(shape, kind), dict(n=layers, rows=count, window=window, first=first, count=count, most=rows)) for window, first in ((1 << 30, 0), (64, 16), (64, 100000))]
     _check(calls, tmp_path)
+
+
+def test_rows_that_32_bits_do_not_count():
+    """Chunks of rows that a block of keys does not have, and the turns behind a unit's last row, stay below 2^31: weights take up to 2^30 rows times query heads."""
+    for hq, hkv in ((1, 1), (28, 4), (8, 1), (1 << 18, 1)):
+        p, need = W._params(n_q_heads=hq, n_kv_heads=hkv, batch=1, format="rows"), C.c_size_t()
+        most = (1 << 30) // hq
+        size = lambda rows: B.lib().mixkv_paged_weights_workspace_size(C.byref(p), 1, rows, 1 << 30, 0, rows, 1 << 20, C.byref(need))  # noqa: E731
+        assert size(most) == B.MIXKV_OK and size(most + 1) == size((2 ** 31 - 1) // hq) == B.MIXKV_ERR_UNSUPPORTED
+        assert W._weigh(p, rows=most + 1, count=most + 1) == B.MIXKV_ERR_UNSUPPORTED
