@@ -8,7 +8,9 @@ namespace mixkv {
 
 struct WeightPtrs { float *w[kLayersPerLaunch]; };
 
-constexpr int kSumRun = 64;              // steps of 16 rows whose weights are summed up on their own: 2^17 rows are then off by some 2^-18 at most
+// Steps of 16 rows whose weights are summed up on their own.  A lane adds four rows a step: 256 additions a run, and one a run behind them, each off by at most 2^-24 of the sum: 2^17 rows, 128
+// runs, by at most 2^-15.4; 2^12 rows by 2^-16.
+constexpr int kSumRun = 64;
 
 // ------------------------------------------------------------------------------------------------
 // weights_step_kernel (few rows): a wave to tiles of 32 keys, rows on the output rows of 16 x 16 products, keys on their columns, so that a lane has
