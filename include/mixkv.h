@@ -497,7 +497,9 @@ mixkv_status mixkv_paged_window_attention(const mixkv_paged_params *params, cons
  * The attention that cached rows have been given, summed up: with the lse that mixkv_paged_window_attention left for the same queries, window and
  * keep_first (or any other normaliser), row j of KV head h has its weight raised by
  *     sum over the new rows that see j, and over the G query heads, of exp(softmax_scale * q . k_j - lse),
- * in fp32; the weights of the new rows themselves begin at zero.  A place's weight lies beside its page: weights[l][page][row of the page], 16-byte aligned.  Rows
+ * in fp32; the weights of the new rows themselves begin at zero.  A place's weight lies beside its page: weights[l][page][row of the page], 16-byte aligned.  It is read,
+ * raised and written without atomics, as pages are: a page may be listed for one place of one (sequence, head) only here, also where it is shared for reading (a
+ * common prefix), since each of two heads would lose what the other adds.  Rows
  * whose lse is -infinity give nothing.  Weights of rows that do not exist, and of old rows that no new row sees, keep their contents.  A head's
  * rows beyond max_count are not served; max_rows as above.  n_rows * n_q_heads <= 2^30.  V_pages are not used and may be NULL.  Sums repeat bit for bit for the same
  * arguments.  Workspace: mixkv_paged_weights_workspace_size bytes (0: NULL is accepted), 256-byte aligned, no initialisation.
