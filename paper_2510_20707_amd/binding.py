@@ -819,7 +819,7 @@ def _weight_pool(p: MixkvPagedParams, t: torch.Tensor, name: str, device) -> tor
 
 class PreparedPagedWeights:
     """The C arguments of one mixkv_paged_weights call.  queries: per layer a PagedQueries with the `lse` of the attention; weights: per layer
-    [n_pages, page_rows] f32, raised in place."""
+    [n_pages, page_rows] f32, raised in place (a page is listed for one place of one head)."""
 
     def __init__(self, p: MixkvPagedParams, caches: Sequence[PagedCache], queries: Sequence[PagedQueries], weights: Sequence[torch.Tensor],
                  window: int = EVERY_ROW, keep_first: int = 0, max_count: Optional[int] = None, max_rows: Optional[int] = None, workspace="alloc"):
