@@ -460,7 +460,7 @@ mixkv_status mixkv_paged_attention(const mixkv_paged_params *params, const mixkv
 /*
  * Queries of new rows: a prompt's, a few drafted tokens', a step's single ones, of ragged sequences one after another with unused rows
  * behind them.  The rows of (b, h) are [row_start[b][h], row_start[b][h] + row_count[b][h]), for each the G query heads that KV head h
- * serves; those outside [0, n_rows) are left out.  Their keys and values are in the cache already (mixkv_paged_append, which takes the same
+ * serves; those outside [0, n_rows) are left out, and a row belongs to one sequence only.  Their keys and values are in the cache already (mixkv_paged_append, which takes the same
  * row_start and row_count, and whose Q_out is Q here): row t of a head's row_count[b][h] rows has the place p = lengths[b][h] - row_count[b][h] + t,
  * and sees the places j <= p with
  *     j > p - window   or   j < keep_first:

@@ -403,9 +403,9 @@ __global__ __launch_bounds__(kRankThreads) void evict_list_kernel(PShape s, Evic
 // The chain of loads behind a row (its place, that place's page, the row) is walked one turn ahead.
 // 4-bit values: a strip of `into` holds eight rows, which come from up to eight strips.  A lane takes 16 bytes of the strip, four elements of all eight rows, out of the same 16
 // bytes of theirs.
-// Bound: 4 bits: memory, and beside it the vector unit (codes to values for the bounds, codes from strip to strip): 256 heads, 2.4e6 rows, of which 1.2e6 stay, 0.55 GB with the lines that hold
-// rows of both kinds in 167 us, 3.3 TB/s (a large copy 5.1); keys alone 83, values alone 92, and loads a further turn ahead change nothing.  With one row of a lane under way, and the bounds by
-// butterflies over whole workgroups, 300.  bf16: memory: 8 heads, 1.0e5 rows stay, 104 MB in 31 us.
+// Bound: 4 bits: neither memory nor the vector unit alone (codes to values for the bounds, codes from strip to strip): 256 heads, 2.4e6 rows, of which 1.2e6 stay, 0.55 GB with the lines that hold
+// rows of both kinds in 167 us, 3.3 TB/s (a large copy 5.1), the vector unit 46 % busy, the waves waiting 65 % of their time; keys alone 83, values alone 92, and loads a further turn ahead change nothing.
+// With one row of a lane under way, and the bounds by butterflies over whole workgroups, 300.  bf16: memory: 8 heads, 1.0e5 rows stay, 104 MB in 31 us.
 // ------------------------------------------------------------------------------------------------
 // The smallest and the largest elements of 32 rows of every wave, D/16 lanes to a row, to the bounds of their page, whose rows `waves` neighbouring waves (1, 2 or 4) have.  The lanes
 // share the words of a row's two ends out by halves: with the lane 32, 16, ... away each gives the half that the other one keeps.

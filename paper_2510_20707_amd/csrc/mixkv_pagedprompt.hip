@@ -12,8 +12,9 @@
 //   * 4-bit keys in two fp16 parts (one is off by 2^-12: logits, lse and weights then by some 1e-4), values and weights in one, as in paged_q4_kernel.
 //   * In the program's order a product stands beside what the vector unit does of the other tile meanwhile, and the reads of its operands in front; everything that a turn
 //     needs to know of its pages comes by lane reads from words made for 64 tiles at once.  256 rows to a workgroup: 2467 us (two prompts), 128 rows 2645.
-// Bound: the matrix unit.  bf16, prompts of 16 384 and 9349 rows, 28 query heads on 4 of 128, 2.37 ms, 1.08 PFLOP/s, where a large library product reaches 1.22 and the products
-// alone took 1.63 ms.  4 bits, 32 768 rows, window 4096 and 16 first rows, 2.70 ms: 1.5 times the products, at the same rate.
+// Bound: the matrix unit.  bf16, prompts of 16 384 and 9349 rows, 28 query heads on 4 of 128, 2.33 to 2.52 ms, 1.01 to 1.09 PFLOP/s, 85 to 89 % of what a large library
+// product reaches on the same card; the products alone took 1.63 ms.  4 bits, 32 768 rows, window 4096 and 16 first rows, 2.64 to 2.86 ms: 1.5 times the products, at the same rate.  Short windows: tiles at their edges are
+// masked select by select, with a barrier more a turn: 16 384 rows, 32 query heads on 8, window 1024 383 us, 256 196, 1.8 and 3 times their products' time.
 #include "mixkv_pagedwin.h"
 
 namespace mixkv {

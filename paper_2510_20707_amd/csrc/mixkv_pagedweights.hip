@@ -16,7 +16,7 @@ constexpr int kSumRun = 64;
 // weights_step_kernel (few rows): a wave to tiles of 32 keys, rows on the output rows of 16 x 16 products, keys on their columns, so that a lane has
 // two keys and their sums over four rows each.  With up to 16 rows in all (a step's single tokens) every wave prepares the queries once, with up to 64 the workgroup does.
 // 4-bit keys as in paged_q4_kernel: codes as fp16 subnormals, a product for each group of 32 elements, steps and bases behind it in fp32.
-// Bound: memory, a tile of each wave in flight, the next one asked for before the exponentials: 32 sequences of up to 16 384 rows, 32 query heads on 8, 570 MB in 120 us, 4.7 TB/s.
+// Bound: memory, a tile of each wave in flight, the next one asked for before the exponentials: 32 sequences of up to 16 384 rows, 32 query heads on 8, 570 MB in 121 to 124 us, 4.6 to 4.7 TB/s.
 // Five new rows of 16 sequences of 8192 rows: 4 bits 36 us, bf16 49; with the queries prepared anew for every tile 72 and 69.
 // Workgroups of 16 tiles: heads of unequal length then end together (121 us; 64 tiles 133, 128 156, 4 144).  Loads past the caches: 124.
 // ------------------------------------------------------------------------------------------------
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(256) void weights_step_kernel(PShape s, PWindow win
 // A block's products stand beside the weights of the one before, two exponentials to a product, and a turn's last weights behind the barrier, while the next turn's operands come.
 // Addresses of rows: a lane computes one row's, the lanes that load it ask for it; three 64-bit products a load took as long as a tenth of the turn.
 // Bound: the vector unit: an exponential, a multiply-add and an addition are 16 to 20 cycles of a SIMD for 64 weights, its product 16, and they share the issue.  Prompts of 16 384 and
-// 8731 rows, window 8192, 28 query heads on 4: 3.9e9 weights in 1.18 ms, 0.84 PFLOP/s (a large library product 1.22).  Turns of 64 rows: 1.41 ms.  A turn takes 4.8 us, a workgroup's
+// 8731 rows, window 8192, 28 query heads on 4: 3.9e9 weights in 1.18 to 1.24 ms, 0.80 to 0.84 PFLOP/s (a large library product 1.19 to 1.22).  Turns of 64 rows: 1.41 ms.  A turn takes 4.8 us, a workgroup's
 // beginning and end 10: the compiler waits for the next turn's rows behind the first products of a turn, and forms without that wait had no registers left for the loop (1.26 to 1.31 ms).
 // ------------------------------------------------------------------------------------------------
 constexpr int kManyWaves = 8, kManyRun = 16384;                     // rows whose weights a lane adds up on its own, every 32nd: they are off by 2^-15 at most
