@@ -85,11 +85,13 @@ def test_tiles_without_weight_within_the_oracles_tolerance(dtype, D, P, count):
 
 
 @pytest.mark.parametrize("fmt,dtype", [("rows", "bf16"), ("4bit", "bf16")])
-def test_first_keys_of_many_heads(fmt, dtype):
-    """One prompt of 7000 rows beside 6000 sequences, of which a few have a token and the others none: the chunks of the rows that see the first keys are those that the heads leave."""
-    print(f"[case] first keys {fmt}", flush=True)
+@pytest.mark.parametrize("batch", [6000, 70000])
+def test_first_keys_of_many_heads(fmt, dtype, batch):
+    """One prompt of 7000 rows beside thousands of sequences, of which a few have a token and the others none: the chunks of the rows that see the first keys are those that the heads leave, ten or
+    none of their own."""
+    print(f"[case] first keys {fmt} {batch}", flush=True)
     rng = np.random.default_rng(93)
-    n, batch, P = 7000, 6000, 128
+    n, P = 7000, 128
     lens = np.zeros((batch, 1), np.int32)
     lens[17], lens[18:40] = n, rng.integers(1, 300, (22, 1))
     lay = T.Layer(rng, fmt, dtype, 64, P, lens, -(-n // P), fill=True)
