@@ -268,8 +268,9 @@ extern "C" mixkv_status mixkv_paged_select(const mixkv_paged_params *params, con
   if (workspace_bytes < select_bytes(s, n_layers)) return MIXKV_ERR_WORKSPACE_TOO_SMALL;
   hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
   uint32_t *keys = static_cast<uint32_t *>(workspace);
-  for (int l0 = 0; l0 < n_layers; l0 += kLayersPerLaunch) {
-    const int nl = n_layers - l0 < kLayersPerLaunch ? n_layers - l0 : kLayersPerLaunch;
+  const int per = std::min(kLayersPerLaunch, ((1 << 22) - 1) / s.units_per_layer);       // of up to a thousand threads a head: fewer than 2^32 in a launch
+  for (int l0 = 0; l0 < n_layers; l0 += per) {
+    const int nl = std::min(n_layers - l0, per);
     SelTable t;
     for (int l = 0; l < kLayersPerLaunch; ++l) {
       t.c[l] = PCache{};
@@ -285,7 +286,8 @@ extern "C" mixkv_status mixkv_paged_select(const mixkv_paged_params *params, con
     // 32 sequences of up to 1024 pages, 8 heads of 128, in at least 512, 1024 and 2048 workgroups: 25.5, 24.3, 23.6.
     const int pages = 4 * 8 * (64 / (2 * s.D * eb / 16));
     const int64_t all = (s.max_pages + pages - 1) / pages;
-    const int64_t steps = std::min<int64_t>(std::max<int64_t>((all * units + 2047) / 2048, all / 65535 + 1), std::max<int64_t>(8, all / 65535 + 1));
+    const int64_t least = std::max<int64_t>(all / 65535, all * units >> 23) + 1;          // at most 65535 workgroups along a head, and fewer than 2^24 in all
+    const int64_t steps = std::min<int64_t>(std::max<int64_t>((all * units + 2047) / 2048, least), std::max<int64_t>(8, least));
     const dim3 grid((unsigned)s.units_per_layer, (unsigned)((all + steps - 1) / steps), (unsigned)nl), one((unsigned)s.units_per_layer, 1, (unsigned)nl);
     auto score = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(kSelThreads), 0, stream, s, t, keys, unit0, stride, (int)steps); };
     if (params->dtype == MIXKV_BF16) { if (s.D == 128) score(page_score_kernel<MIXKV_BF16, 128>); else score(page_score_kernel<MIXKV_BF16, 64>); }

@@ -1,5 +1,5 @@
 """What a call launches, without a GPU: the library's host code runs in a process of its own over tests/c/launch_recorder.c, which writes launches down and makes none.  The calls are those of
-tests/test_paged_window_abi.py, whose addresses nothing looks behind."""
+tests/test_paged_window_abi.py and tests/test_paged_abi.py, whose addresses nothing looks behind."""
 import ctypes as C
 import json
 import os
@@ -17,7 +17,7 @@ class _Launch(C.Structure):
 
 
 def record(calls, tmp_path):
-    """calls: (entry point, params, sizes) each, as tests.test_paged_window_abi names them.  Returns per call (status, bytes of workspace or None, [(kernel, grid, block)])."""
+    """calls: (entry point, params, sizes) each, as the two name them (single: the attention of one token).  Returns per call (status, bytes of workspace or None, [(kernel, grid, block)])."""
     gcc = shutil.which("gcc")
     if gcc is None:
         pytest.skip("no C compiler")
@@ -33,6 +33,7 @@ def _main(path):
     recorder.recorder_launch.restype = C.POINTER(_Launch)
     C.CDLL(os.path.join(ROOT, "paper_2510_20707_amd", "libmixkv.so"))          # before torch, which has kernels of its own to register
     from paper_2510_20707_amd import binding as B
+    from tests import test_paged_abi as A
     from tests import test_paged_window_abi as W
     B.lib()
     results = []
@@ -40,7 +41,11 @@ def _main(path):
         p, n = W._params(**params), sizes.get("n", 1)
         strides = dict(q_stride_n=p.n_q_heads * p.head_dim, q_stride_h=p.head_dim, out=1 << 56, lse=1 << 57)
         recorder.recorder_clear()
-        if op == "evict":
+        if op in ("select", "single"):
+            kw = dict(n=n, size=1 << 62)
+            status = A._select(p, A._caches(n), **kw) if op == "select" else A._attend(p, A._caches(n), rows=sizes["rows"], selected=0, n_selected=0, **kw)
+            need = B.mixkv_paged_select_workspace_size(p, n) if op == "select" else B.mixkv_paged_attention_workspace_size(p, n, sizes["rows"])
+        elif op == "evict":
             status = W._evict(p, n=n, size=1 << 62, **{k: v for k, v in sizes.items() if k != "n"})
             need = B.mixkv_paged_evict_workspace_size(p, n, sizes["rows"])
         else:

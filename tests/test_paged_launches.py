@@ -1,4 +1,4 @@
-"""Launches and workspaces of the calls on new rows at the ends of what they accept (no GPU; tests/launches.py): a launch has fewer than 2^32 threads and at most 65535 workgroups along y and z."""
+"""Launches and workspaces of the calls on pages at the ends of what they accept (no GPU; tests/launches.py): a launch has fewer than 2^32 threads and at most 65535 workgroups along y and z."""
 import ctypes as C
 import itertools
 import math
@@ -57,6 +57,16 @@ def test_attention(shape, tmp_path):
         if count * math.prod(shape[:2]) * layers > 1 << 26 or count * shape[1] >= 1 << 31:
             continue
         calls += [("attend", _params(shape, kind), dict(n=layers, rows=count, window=window, first=first, count=count, most=rows)) for window, first in ((1 << 30, 0), (64, 16), (64, 100000))]
+    _check(calls, tmp_path)
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+def test_selection_and_single_tokens(shape, tmp_path):
+    """Tables of few pages and of the most (attention refuses more groups of query heads than a launch has places for)."""
+    calls = []
+    for kind, layers, pages in itertools.product(KINDS, (1, 16, 32, 128), (16, 4097, 1 << 24)):
+        p = dict(_params(shape, kind), max_pages=pages)
+        calls += [("select", p, dict(n=layers))] + [("single", p, dict(n=layers, rows=rows)) for rows in (1000, 1 << 30) if shape[1] // shape[2] <= 1 << 14]
     _check(calls, tmp_path)
 
 
